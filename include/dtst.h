@@ -468,6 +468,111 @@ dtst_status dtst_plan_kernel_timing(dtst_plan* plan, int kind, int64_t* launches
 dtst_status dtst_plan_last_cuda_error(const dtst_plan* plan, int* code, const char** text);
 
 /*
+ * Recurrent memory around the layer: operators for models that carry a state over frames of a field (the paper's
+ * model treats time as one more grid dimension; a rollout over many frames needs a state instead).
+ *   - the root-mean-square norm over channels with the residual's addition in front, forward and backward, with an
+ *     output in the tensors' type or in 8 bits;
+ *   - the matrix product of 8-bit operands with a scale per block of 128;
+ *   - the gated linear recurrence along one dimension, forward, backward and for single steps.
+ * No plan is involved.  Tensors are device pointers to float32, bfloat16 or float16 elements (`dtype`), aligned to
+ * their element size (the fast kernels run where they are aligned to 16 bytes); all arithmetic, statistics, states
+ * and weight gradients are float32, and a value is rounded once, when it is stored.  8-bit values are e4m3 (4
+ * exponent and 3 mantissa bits, largest finite value 448).  An extent of zero is legal where a batch may be empty:
+ * nothing is read or written then.  Where a call takes a workspace, it is caller-owned, 256-byte aligned and filled
+ * with zeros ONCE before its first use; calls that share one must be stream-ordered.  Its first word is a status word
+ * as for plans (dtst_workspace_status).
+ */
+enum { DTST_F32 = 0, DTST_BF16 = 1, DTST_F16 = 2 };
+
+/*
+ * Root-mean-square norm of x [outer, channels, inner] over the channels (inner = 1: token-major rows; inner > 1:
+ * channels-first fields), contiguous:
+ *   s = x + residual,  rstd = 1 / sqrt(mean_c s^2 + eps),  y = s * rstd * weight[c]
+ * residual may be NULL (s = x); s and rstd [outer, inner] float32 may be NULL where they are not needed (the backward
+ * pass needs both).  y is formed from the unrounded sum.  s may be x or residual itself, y may be x.  weight
+ * [channels] float32.
+ * Backward for grad_y and, where s went on as the residual stream, grad_s (or NULL):
+ *   grad_x = rstd (weight grad_y - n mean_c(weight grad_y n)) + grad_s with n = s rstd   (also the residual's gradient)
+ *   grad_weight[c] = sum over outer and inner of grad_y n, summed in a fixed order: same bits on every run.
+ * grad_x may be grad_y or grad_s itself; grad_weight may be NULL, grad_x may not.  scratch:
+ * dtst_rms_norm_scratch_bytes, needed for grad_weight (DTST_ERR_WORKSPACE if missing or too small).
+ */
+dtst_status dtst_rms_norm(int dtype, int64_t outer, int64_t channels, int64_t inner, float eps, const void* x,
+                          const void* residual, const float* weight, void* s, void* y, float* rstd, void* stream);
+dtst_status dtst_rms_norm_scratch_bytes(int64_t channels, size_t* bytes);
+dtst_status dtst_rms_norm_backward(int dtype, int64_t outer, int64_t channels, int64_t inner, const void* grad_y,
+                                   const void* s, const float* weight, const float* rstd, const void* grad_s,
+                                   void* grad_x, float* grad_weight, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * The same norm of rows x [rows, channels] with its output in 8 bits, the operand of dtst_matmul_fp8:
+ *   q[r, c] = e4m3(y[r, c] / scale[c / 128, r]),  scale = amax / 448 over the block's channels of the row
+ * q: rows q_ld bytes apart (q_ld >= channels); scale [ceil(channels / 128), rows] float32.  A block of zeros gets a tiny
+ * scale and zeros; a NaN stays a NaN; a block with an infinity has the scale infinity.
+ * dtst_quantize_fp8: the same without the norm, rows x_ld elements apart.
+ * dtst_quantize_fp8_weight: w [rows, cols] (rows w_ld elements apart) with one scale per 128 x 128 block,
+ *   scale [ceil(rows / 128), ceil(cols / 128)].
+ */
+dtst_status dtst_rms_norm_fp8(int dtype, int64_t rows, int64_t channels, float eps, const void* x, const void* residual,
+                              const float* weight, void* s, void* q, int64_t q_ld, float* scale, void* stream);
+dtst_status dtst_quantize_fp8(int dtype, int64_t rows, int64_t channels, const void* x, int64_t x_ld, void* q,
+                              int64_t q_ld, float* scale, void* stream);
+dtst_status dtst_quantize_fp8_weight(int dtype, int64_t rows, int64_t cols, const void* w, int64_t w_ld, void* q,
+                                     int64_t q_ld, float* scale, void* stream);
+
+/*
+ * out[m, n] = sum_k x[m, k] x_scale[k / 128, m] * w[n, k] w_scale[n / 128, k / 128], summed in float32.
+ *   x [m, k], w [n, k] e4m3, rows x_ld / w_ld bytes apart; both base pointers 16-byte aligned and both strides
+ *   multiples of 16 bytes (what lies between k and the stride is not used), else DTST_ERR_INVALID_ARG;
+ *   x_scale [ceil(k / 128), m], w_scale [ceil(n / 128), ceil(k / 128)] float32, contiguous;
+ *   out [m, n] of out_dtype, rows out_ld elements apart (out_ld >= n).  k >= 1.
+ *   workspace: at least 256 bytes (the status word).
+ * Every product of a row of x is the same whatever the other rows are, and the same on every run.
+ */
+dtst_status dtst_matmul_fp8(int out_dtype, int64_t m, int64_t n, int64_t k, const void* x, int64_t x_ld,
+                            const float* x_scale, const void* w, int64_t w_ld, const float* w_scale, void* out,
+                            int64_t out_ld, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gated linear recurrence along `length` of tensors [outer, length, inner]; inner = 1: the steps are contiguous (the
+ * time axis of a channels-first field), inner > 1: token-major sequences, or any other axis of a grid:
+ *   h_t = a_t h_{t-1} + u_t,   h_{-1} = h0
+ *   DTST_GATE_SIGMOID: a = 1 / (1 + exp(-g)), u = (1 - a) v        DTST_GATE_DECAY: a = g, u = v
+ * v, g: in_stride = elements between outer entries and between steps (the same for both; zero repeats an entry); the
+ * inner stride is 1, and with inner = 1 the step stride must be 1.  h contiguous.  h0, h_last [outer, inner] float32; either
+ * may be NULL (zeros; not wanted), and they may be the same buffer (a running state).  lengths [outer] int32 or NULL:
+ * entry o has lengths[o] steps (taken into 0..length); what lies behind them is not used, h is zero there, and h_last is
+ * the state behind the entry's own last step (h0 for an entry without steps).
+ * checkpoints: NULL, or dtst_gated_scan_sizes' count of floats, which receive the states the backward pass restarts from.
+ *
+ * Backward for grad_h [outer, length, inner] (contiguous) and grad_last [outer, inner] (or NULL), with
+ *   delta_t = grad_h_t + a_{t+1} delta_{t+1}:
+ *   SIGMOID: grad_v = delta (1 - a), grad_g = delta (h_{t-1} - v) a (1 - a);   DECAY: grad_v = delta, grad_g = delta h_{t-1};
+ *   grad_h0 = a_0 delta_0 (may be NULL).  grad_v, grad_g: both with grad_stride, which must not make elements coincide;
+ * zero behind an entry's own length.  v, g, h0, lengths and checkpoints as in the forward call.  h is not needed.
+ * Both passes take the workspace of dtst_gated_scan_sizes.
+ */
+enum { DTST_GATE_SIGMOID = 0, DTST_GATE_DECAY = 1 };
+typedef struct {
+  int32_t dtype, gate;
+  int64_t outer, length, inner;
+  int64_t in_stride[2];      /* v and g: outer, step */
+  int64_t grad_stride[2];    /* grad_v and grad_g: outer, step */
+} dtst_scan_desc;
+dtst_status dtst_gated_scan_sizes(const dtst_scan_desc* desc, size_t* workspace_bytes, int64_t* checkpoint_floats);
+dtst_status dtst_gated_scan(const dtst_scan_desc* desc, const void* v, const void* g, const float* h0,
+                            const int32_t* lengths, void* h, float* h_last, float* checkpoints, void* workspace,
+                            size_t workspace_bytes, void* stream);
+dtst_status dtst_gated_scan_backward(const dtst_scan_desc* desc, const void* grad_h, const float* grad_last,
+                                     const void* v, const void* g, const float* h0, const int32_t* lengths,
+                                     const float* checkpoints, void* grad_v, void* grad_g, float* grad_h0,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Synchronises `stream` and reports the status word at the head of a workspace of the calls above: DTST_OK, or
+ * DTST_ERR_DEVICE_TIMEOUT if a bounded wait inside a kernel gave up (its output is undefined then).  Clears the word. */
+dtst_status dtst_workspace_status(void* workspace, void* stream);
+
+/*
  * Diagnostics read once from the environment (for A/B measurements; not for production use):
  *   DTST_NO_PDL=1            launch every kernel without the programmatic-dependent-launch attribute
  *   DTST_NO_COLFUSE=1        forward-type transforms: contract the third dimension in a launch of its own instead of

@@ -44,7 +44,17 @@ EXPORTED = [
     "dtst_backward_complex", "dtst_plan_set_contraction_order", "dtst_plan_get_contraction_order",
     "dtst_plan_tune_contraction_order", "dtst_plan_host_io_bytes", "dtst_plan_enable_host_io", "dtst_step_host",
     "dtst_host_io_wait", "dtst_plan_set_column_contraction", "dtst_plan_set_arithmetic",
+    "dtst_rms_norm", "dtst_rms_norm_scratch_bytes", "dtst_rms_norm_backward", "dtst_rms_norm_fp8", "dtst_quantize_fp8",
+    "dtst_quantize_fp8_weight", "dtst_matmul_fp8", "dtst_gated_scan_sizes", "dtst_gated_scan",
+    "dtst_gated_scan_backward", "dtst_workspace_status",
 ]
+
+
+class ScanDesc(ctypes.Structure):
+    """dtst_scan_desc"""
+    _fields_ = [("dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("outer", ctypes.c_int64),
+                ("length", ctypes.c_int64), ("inner", ctypes.c_int64), ("in_stride", ctypes.c_int64 * 2),
+                ("grad_stride", ctypes.c_int64 * 2)]
 
 
 class DtstError(RuntimeError):
@@ -114,6 +124,19 @@ def lib() -> ctypes.CDLL:
     L.dtst_plan_enable_kernel_timing.argtypes = [vp, i32]
     L.dtst_plan_kernel_timing.argtypes = [vp, i32, i64p, ctypes.POINTER(ctypes.c_double)]
     L.dtst_plan_last_cuda_error.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_char_p)]
+    i64, sz, f32 = ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
+    descp = ctypes.POINTER(ScanDesc)
+    L.dtst_rms_norm.argtypes = [i32, i64, i64, i64, f32] + [vp] * 7
+    L.dtst_rms_norm_scratch_bytes.argtypes = [i64, ctypes.POINTER(sz)]
+    L.dtst_rms_norm_backward.argtypes = [i32, i64, i64, i64] + [vp] * 8 + [sz, vp]
+    L.dtst_rms_norm_fp8.argtypes = [i32, i64, i64, f32, vp, vp, vp, vp, vp, i64, vp, vp]
+    L.dtst_quantize_fp8.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp]
+    L.dtst_quantize_fp8_weight.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp]
+    L.dtst_matmul_fp8.argtypes = [i32, i64, i64, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, sz, vp]
+    L.dtst_gated_scan_sizes.argtypes = [descp, ctypes.POINTER(sz), i64p]
+    L.dtst_gated_scan.argtypes = [descp] + [vp] * 8 + [sz, vp]
+    L.dtst_gated_scan_backward.argtypes = [descp] + [vp] * 11 + [sz, vp]
+    L.dtst_workspace_status.argtypes = [vp, vp]
     L.dtst_status_string.argtypes = [i32]
     L.dtst_status_string.restype = ctypes.c_char_p
     L.dtst_version.argtypes = []

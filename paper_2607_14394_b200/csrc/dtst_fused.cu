@@ -69,6 +69,20 @@ bool make_points_map(CUtensorMap* map, const float* base, long long rows, long l
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// 8-bit tensor [rows][cols], rows `ld` bytes apart, viewed through [box_rows x 128] boxes with the 128-byte swizzle;
+// whatever a box holds beyond the tensor is filled with zeros
+bool make_bytes_map(CUtensorMap* map, const void* base, long long rows, long long cols, long long ld, int box_rows) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)ld};
+  cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Shapes the plane kernels are instantiated for: (N3, k3, N2, k2).
 static bool plane_supported(int N3, int K3, int N2, int K2) {
 #define DTST_MATCH(a, b, c, d) if (N3 == a && K3 == b && N2 == c && K2 == d) return true;

@@ -1,0 +1,65 @@
+// Launchers of the recurrent-memory operators (arguments already checked by the C entry points).
+#pragma once
+
+#include "dtst_common.cuh"
+
+namespace dtst {
+
+constexpr int kNormParts = 592;           // most CTAs (and rows of partial sums) of a norm's backward pass: 4 per SM
+constexpr int kNormFieldChannels = 128;   // most channels a channels-first norm holds in registers
+
+struct NormCall {
+  int dtype;
+  long long outer, channels, inner;
+  float eps;
+  const void *x, *residual;
+  const float* weight;     // null: quantise x as it is
+  void *s, *y;
+  uint8_t* q;              // non-null: 8-bit output instead of y
+  float *scale, *rstd;
+  long long x_ld, q_ld;    // elements between rows of x (rows only), bytes between rows of q
+};
+cudaError_t launch_norm_forward(const NormCall& n, cudaStream_t st);
+
+struct NormBackCall {
+  int dtype;
+  long long outer, channels, inner;
+  const void *grad_y, *s, *grad_s;
+  const float *weight, *rstd;
+  void* grad_x;
+  float *grad_weight, *partial;
+};
+cudaError_t launch_norm_backward(const NormBackCall& n, cudaStream_t st);
+
+struct ScanCall {
+  int dtype, gate;
+  long long outer, length, inner;
+  long long in_outer, in_step, grad_outer, grad_step;   // strides in elements; inner stride 1
+  const void *v, *g, *grad_h;
+  const float *h0, *grad_last;
+  const int* lengths;
+  void *h, *grad_v, *grad_g;
+  float *h_last, *grad_h0, *checkpoints;
+  void* workspace;
+};
+// steps between saved states for this problem (the whole length where nothing is saved)
+long long scan_chunk(int dtype, long long length, long long inner);
+size_t scan_workspace_bytes(int dtype, long long outer, long long length, long long inner);
+cudaError_t launch_scan_forward(const ScanCall& c, cudaStream_t st);
+cudaError_t launch_scan_backward(const ScanCall& c, cudaStream_t st);
+
+cudaError_t launch_quantize_weight(int dtype, const void* w, long long w_ld, uint8_t* q, long long q_ld, float* scale,
+                                   long long rows, long long cols, cudaStream_t st);
+
+struct MatmulCall {
+  int out_dtype;
+  long long m, n, k, x_ld, w_ld, out_ld;
+  const uint8_t *x, *w;
+  const float *x_scale, *w_scale;
+  void* out;
+  int* status;
+};
+bool matmul_fp8_available();
+cudaError_t launch_matmul_fp8(const MatmulCall& c, cudaStream_t st);
+
+}  // namespace dtst

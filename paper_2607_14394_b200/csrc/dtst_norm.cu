@@ -1,0 +1,757 @@
+// Root-mean-square norm over channels, with the residual's addition in front and, on request, an output in 8 bits:
+//     s = x + r,   rstd = 1 / sqrt(mean_c s^2 + eps),   y = s rstd w
+//     q = e4m3(y 448 / amax),  scale = amax / 448,  amax over 128 neighbouring channels of a row
+// and its backward pass, with n = s rstd:
+//     grad_x = rstd (w gy - n mean_c(w gy n)) + grad_s,   grad_w = sum over positions of gy n
+// (the gradient of the residual is the same tensor).  Everything is in 32 bits; y is formed from the unrounded sum,
+// so a 16-bit s costs y nothing.
+//
+// All of it is bound by memory: 2..4 tensors in or out per pass, a few operations per element.  Two layouts:
+//   rows      [rows][C], C contiguous (token-major): a row is held by 32..512 threads in registers, each thread a
+//             16-byte group of channels every TPR groups, so a group of 128 channels is 16 (32 for fp32)
+//             neighbouring lanes and its amax a few shuffles;
+//   fields    [outer][C][inner], inner contiguous (channels-first): lanes run along the positions, warps share the
+//             channels, the sums over channels meet in shared memory.
+// The weight gradient is summed in registers over all positions a CTA visits and in a fixed order over CTAs by a
+// second launch: same bits on every run.
+#include "dtst_common.cuh"
+#include "dtst_memory.cuh"
+#include "dtst_types.cuh"
+
+namespace dtst {
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ rows
+template <typename T>
+constexpr int kVec = 16 / (int)sizeof(T);
+
+// Sum over the TPR threads of a row; `red` holds two alternating sets of 16 partial sums (one barrier per call).
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* red, int& phase) {
+  v = warp_sum(v);
+  if constexpr (TPR > 32) {
+    float* r = red + phase * 32;
+    phase ^= 1;
+    if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = v;
+    __syncthreads();
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < TPR / 32; ++i) t += r[i];
+    v = t;
+  }
+  return v;
+}
+
+constexpr int kWarpRowWarps = 4;   // rows per CTA where one warp holds a row
+
+template <int TPR>
+constexpr int kRowThreads = TPR == 32 ? 32 * kWarpRowWarps : TPR;
+
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void load_group(Pack<T, kVec<T>>& p, const T* row, long long c, long long C) {
+  if (ALIGNED) {
+    if (c < C) p.load(row + c); else p.zero();
+  } else {
+    const long long left = C - c;
+    p.load_part(row + c, left > kVec<T> ? kVec<T> : (int)left);
+  }
+}
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void store_group(const Pack<T, kVec<T>>& p, T* row, long long c, long long C) {
+  if (ALIGNED) {
+    if (c < C) p.store(row + c);
+  } else {
+    const long long left = C - c;
+    p.store_part(row + c, left > kVec<T> ? kVec<T> : (int)left);
+  }
+}
+
+// quantises the group of VEC values this thread holds; the threads of a 128-channel group are neighbours in a warp
+template <int VEC>
+__device__ __forceinline__ void quantise_store(const float (&y)[VEC], uint8_t* q_row, float* scale, long long c,
+                                               long long C, long long scale_ld, long long row, bool q_aligned) {
+  float amax = kAmaxFloor;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) amax = fmaxf(amax, fabsf(y[i]));
+#pragma unroll
+  for (int o = kFp8Block / VEC / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+  if (c >= C) return;
+  const float inv = __fdiv_rn(kE4m3Max, amax);
+  if (c % kFp8Block == 0) scale[(c / kFp8Block) * scale_ld + row] = __fdiv_rn(amax, kE4m3Max);
+  uint32_t w[VEC / 4];
+#pragma unroll
+  for (int i = 0; i < VEC / 4; ++i)
+    w[i] = pack_e4m3(y[4 * i] * inv, y[4 * i + 1] * inv, y[4 * i + 2] * inv, y[4 * i + 3] * inv);
+  if (q_aligned && c + VEC <= C) {
+    if constexpr (VEC == 8) *reinterpret_cast<uint2*>(q_row + c) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(q_row + c) = w[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (c + i < C) q_row[c + i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+  }
+}
+
+struct RowArgs {
+  const void *x, *residual;
+  const float* weight;
+  void *s, *y;
+  uint8_t* q;
+  float *scale, *rstd;
+  long long rows, C, x_ld, q_ld;
+  float eps;
+  int q_aligned;
+};
+
+// NORM false: quantise x as it is (no residual, no weight).
+template <typename T, int TPR, int ITEMS, bool QUANT, bool NORM, bool ALIGNED>
+__global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_kernel(const RowArgs a) {
+  constexpr int VEC = kVec<T>;
+  constexpr int RPC = kRowThreads<TPR> / TPR;
+  __shared__ float red[64];
+  pdl_trigger();
+  pdl_wait();
+  const int tr = threadIdx.x % TPR;
+  const float inv_c = 1.0f / (float)a.C;
+  const T* x = static_cast<const T*>(a.x);
+  const T* res = static_cast<const T*>(a.residual);
+  int phase = 0;
+  for (long long row = (long long)blockIdx.x * RPC + threadIdx.x / TPR; row < a.rows; row += (long long)gridDim.x * RPC) {
+    float v[ITEMS][VEC];
+    Pack<T, VEC> px[ITEMS], pr[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) load_group<T, ALIGNED>(px[k], x + row * a.x_ld, (long long)(tr + k * TPR) * VEC, a.C);
+    if (NORM && res != nullptr) {
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) load_group<T, ALIGNED>(pr[k], res + row * a.C, (long long)(tr + k * TPR) * VEC, a.C);
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        v[k][i] = px[k].get(i);
+        if (NORM && res != nullptr) v[k][i] += pr[k].get(i);
+        sum = fmaf(v[k][i], v[k][i], sum);
+      }
+    float rstd = 1.f;
+    if (NORM) {
+      if (a.s != nullptr) {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) px[k].put(i, v[k][i]);
+          store_group<T, ALIGNED>(px[k], static_cast<T*>(a.s) + row * a.C, (long long)(tr + k * TPR) * VEC, a.C);
+        }
+      }
+      rstd = rsqrtf(fmaf(row_sum<TPR>(sum, red, phase), inv_c, a.eps));
+      if (a.rstd != nullptr && tr == 0) a.rstd[row] = rstd;
+    }
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const long long c = (long long)(tr + k * TPR) * VEC;
+      float y[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) y[i] = v[k][i];
+      if (NORM) {
+        float w[VEC];
+        if (ALIGNED) {
+          if (c < a.C) {
+#pragma unroll
+            for (int i = 0; i < VEC; i += 4) {
+              const float4 t = __ldg(reinterpret_cast<const float4*>(a.weight + c + i));
+              w[i] = t.x, w[i + 1] = t.y, w[i + 2] = t.z, w[i + 3] = t.w;
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[i] = 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) w[i] = c + i < a.C ? __ldg(a.weight + c + i) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) y[i] *= rstd * w[i];
+      }
+      if (QUANT) {
+        quantise_store<VEC>(y, a.q + row * a.q_ld, a.scale, c, a.C, a.rows, row, a.q_aligned != 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) px[k].put(i, y[i]);
+        store_group<T, ALIGNED>(px[k], static_cast<T*>(a.y) + row * a.C, c, a.C);
+      }
+    }
+  }
+}
+
+// Rows longer than the register kernels hold (16384 channels, 8192 in fp32): one CTA per row, the row read twice,
+// the second time from L2.
+template <typename T, bool QUANT, bool NORM>
+__global__ void __launch_bounds__(512) norm_long_rows_kernel(const RowArgs a) {
+  __shared__ float red[64];
+  pdl_trigger();
+  pdl_wait();
+  int phase = 0;
+  const T* res = static_cast<const T*>(a.residual);
+  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
+    float rstd = 1.f;
+    if (NORM) {
+      float sum = 0.f;
+      for (long long c = threadIdx.x; c < a.C; c += 512) {
+        float v = Elem<T>::get(x[c]);
+        if (res != nullptr) v += Elem<T>::get(res[row * a.C + c]);
+        sum = fmaf(v, v, sum);
+      }
+      rstd = rsqrtf(fmaf(row_sum<512>(sum, red, phase), 1.0f / (float)a.C, a.eps));
+      if (a.rstd != nullptr && threadIdx.x == 0) a.rstd[row] = rstd;
+    }
+    for (long long c0 = 0; c0 < a.C; c0 += 2048) {   // 16 warps x 128 channels, four to a lane
+      const long long c = c0 + 4 * (long long)threadIdx.x;
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[i] = 0.f;
+        if (c + i < a.C) {
+          float v = Elem<T>::get(x[c + i]);
+          if (NORM) {
+            if (res != nullptr) v += Elem<T>::get(res[row * a.C + c + i]);
+            if (a.s != nullptr) static_cast<T*>(a.s)[row * a.C + c + i] = Elem<T>::put(v);
+            v *= rstd * __ldg(a.weight + c + i);
+          }
+          y[i] = v;
+        }
+      }
+      if (QUANT) {
+        quantise_store<4>(y, a.q + row * a.q_ld, a.scale, c, a.C, a.rows, row, a.q_aligned != 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (c + i < a.C) static_cast<T*>(a.y)[row * a.C + c + i] = Elem<T>::put(y[i]);
+      }
+    }
+  }
+}
+
+template <typename T, bool QUANT, bool NORM>
+cudaError_t launch_rows(const RowArgs& a, cudaStream_t st) {
+  constexpr int VEC = kVec<T>;
+  const long long groups = (a.C + VEC - 1) / VEC;
+  const bool al = a.C % VEC == 0 && a.x_ld % VEC == 0 && aligned_to(a.x, 16) && aligned_to(a.residual, 16) &&
+                  aligned_to(a.s, 16) && (QUANT || aligned_to(a.y, 16)) && aligned_to(a.weight, 16);
+  const long long most = (long long)num_sms() * 32;
+#define DTST_ROWS(TPR, ITEMS)                                                                                     \
+  {                                                                                                               \
+    const long long ctas = (a.rows + kRowThreads<TPR> / TPR - 1) / (kRowThreads<TPR> / TPR);                      \
+    const dim3 grid((unsigned)(ctas < most ? ctas : most)), block(kRowThreads<TPR>);                              \
+    return al ? launch_pdl(norm_rows_kernel<T, TPR, ITEMS, QUANT, NORM, true>, grid, block, 0, st, a)             \
+              : launch_pdl(norm_rows_kernel<T, TPR, ITEMS, QUANT, NORM, false>, grid, block, 0, st, a);           \
+  }
+  if (groups <= 32) DTST_ROWS(32, 1)
+  if (groups <= 64) DTST_ROWS(32, 2)
+  if (groups <= 128) DTST_ROWS(128, 1)
+  if (groups <= 256) DTST_ROWS(256, 1)
+  if (groups <= 512) DTST_ROWS(256, 2)
+  if (groups <= 1024) DTST_ROWS(512, 2)
+  if (groups <= 2048) DTST_ROWS(512, 4)
+#undef DTST_ROWS
+  const dim3 grid((unsigned)(a.rows < most ? a.rows : most));
+  return launch_pdl(norm_long_rows_kernel<T, QUANT, NORM>, grid, dim3(512), 0, st, a);
+}
+
+// ---- backward, rows
+struct RowBackArgs {
+  const void *gy, *s, *gs;
+  const float *weight, *rstd;
+  void* gx;
+  float* partial;   // [gridDim.x][C]
+  long long rows, C;
+};
+
+template <typename T, int TPR, int ITEMS, bool ALIGNED>
+__global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_backward_kernel(const RowBackArgs a) {
+  constexpr int VEC = kVec<T>;
+  constexpr int RPC = kRowThreads<TPR> / TPR;
+  __shared__ float red[64];
+  extern __shared__ float gw_s[];   // RPC > 1: [RPC][ITEMS * TPR * VEC]
+  pdl_trigger();
+  pdl_wait();
+  const int tr = threadIdx.x % TPR;
+  const float inv_c = 1.0f / (float)a.C;
+  const T* gy = static_cast<const T*>(a.gy);
+  const T* s = static_cast<const T*>(a.s);
+  const T* gs = static_cast<const T*>(a.gs);
+  float gw[ITEMS][VEC], w[ITEMS][VEC];
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const long long c = (long long)(tr + k * TPR) * VEC + i;
+      gw[k][i] = 0.f;
+      w[k][i] = c < a.C ? __ldg(a.weight + c) : 0.f;
+    }
+  int phase = 0;
+  for (long long row = (long long)blockIdx.x * RPC + threadIdx.x / TPR; row < a.rows; row += (long long)gridDim.x * RPC) {
+    Pack<T, VEC> pg[ITEMS], ps[ITEMS], pr[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const long long c = (long long)(tr + k * TPR) * VEC;
+      load_group<T, ALIGNED>(pg[k], gy + row * a.C, c, a.C);
+      load_group<T, ALIGNED>(ps[k], s + row * a.C, c, a.C);
+      if (gs != nullptr) load_group<T, ALIGNED>(pr[k], gs + row * a.C, c, a.C);
+    }
+    const float rstd = __ldg(a.rstd + row);
+    float dot = 0.f;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float g = pg[k].get(i), n = ps[k].get(i) * rstd;
+        gw[k][i] = fmaf(g, n, gw[k][i]);
+        dot = fmaf(w[k][i] * g, n, dot);
+      }
+    dot = row_sum<TPR>(dot, red, phase) * inv_c;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float n = ps[k].get(i) * rstd;
+        float g = rstd * fmaf(-n, dot, w[k][i] * pg[k].get(i));
+        if (gs != nullptr) g += pr[k].get(i);
+        ps[k].put(i, g);
+      }
+      store_group<T, ALIGNED>(ps[k], static_cast<T*>(a.gx) + row * a.C, (long long)(tr + k * TPR) * VEC, a.C);
+    }
+  }
+  if (a.partial == nullptr) return;
+  float* out = a.partial + (long long)blockIdx.x * a.C;
+  if constexpr (RPC > 1) {   // the CTA's rows meet in shared memory, in row order
+    constexpr int W = ITEMS * TPR * VEC;
+    const int rw = threadIdx.x / TPR;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) gw_s[rw * W + (tr + k * TPR) * VEC + i] = gw[k][i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < W && c < a.C; c += blockDim.x) {
+      float t = 0.f;
+#pragma unroll
+      for (int r = 0; r < RPC; ++r) t += gw_s[r * W + c];
+      out[c] = t;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const long long c = (long long)(tr + k * TPR) * VEC + i;
+        if (c < a.C) out[c] = gw[k][i];
+      }
+  }
+}
+
+// Longer rows: grad_x by one CTA per row (the row read twice), then the weight gradient column by column.
+template <typename T>
+__global__ void __launch_bounds__(512) norm_long_rows_backward_kernel(const RowBackArgs a) {
+  __shared__ float red[64];
+  pdl_trigger();
+  pdl_wait();
+  int phase = 0;
+  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* gy = static_cast<const T*>(a.gy) + row * a.C;
+    const T* s = static_cast<const T*>(a.s) + row * a.C;
+    const float rstd = a.rstd[row];
+    float dot = 0.f;
+    for (long long c = threadIdx.x; c < a.C; c += 512)
+      dot = fmaf(__ldg(a.weight + c) * Elem<T>::get(gy[c]), Elem<T>::get(s[c]) * rstd, dot);
+    dot = row_sum<512>(dot, red, phase) / (float)a.C;
+    for (long long c = threadIdx.x; c < a.C; c += 512) {
+      float g = rstd * fmaf(-(Elem<T>::get(s[c]) * rstd), dot, __ldg(a.weight + c) * Elem<T>::get(gy[c]));
+      if (a.gs != nullptr) g += Elem<T>::get(static_cast<const T*>(a.gs)[row * a.C + c]);
+      static_cast<T*>(a.gx)[row * a.C + c] = Elem<T>::put(g);
+    }
+  }
+}
+template <typename T>
+__global__ void __launch_bounds__(256) norm_long_rows_weight_kernel(const RowBackArgs a) {
+  pdl_trigger();
+  pdl_wait();
+  const long long c = (long long)blockIdx.x * 256 + threadIdx.x;   // blockIdx.y: a share of the rows
+  if (c >= a.C) return;
+  float t = 0.f;
+  for (long long row = blockIdx.y; row < a.rows; row += gridDim.y)
+    t = fmaf(Elem<T>::get(static_cast<const T*>(a.gy)[row * a.C + c]),
+             Elem<T>::get(static_cast<const T*>(a.s)[row * a.C + c]) * __ldg(a.rstd + row), t);
+  a.partial[(long long)blockIdx.y * a.C + c] = t;
+}
+
+// ------------------------------------------------------------------------------------------------ fields
+struct FieldArgs {
+  const void *x, *residual, *gy, *gs;
+  const float* weight;
+  const float* rstd_in;
+  void *s, *y;          // backward: y is grad_x, x is s
+  float *rstd, *partial;
+  long long outer, C, inner, tiles;   // tiles per outer entry
+  float eps;
+};
+
+template <typename T, int VEC, int NCH>
+__global__ void __launch_bounds__(256) norm_field_kernel(const FieldArgs a) {
+  __shared__ float red[2][8][32 * VEC];
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x, wy = threadIdx.y, ny = blockDim.y;
+  const float inv_c = 1.0f / (float)a.C;
+  const T* res = static_cast<const T*>(a.residual);
+  int phase = 0;
+  for (long long t = blockIdx.x; t < a.outer * a.tiles; t += gridDim.x) {
+    const long long o = t / a.tiles, p = (t % a.tiles) * (32 * VEC) + lane * VEC;
+    const long long base = o * a.C * a.inner + p;
+    const bool live = p < a.inner;
+    Pack<T, VEC> px[NCH], pr[NCH];
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      const int c = wy + k * ny;
+      const bool on = live && c < a.C;
+      if (on) px[k].load(static_cast<const T*>(a.x) + base + c * a.inner); else px[k].zero();
+      if (res != nullptr) {
+        if (on) pr[k].load(res + base + c * a.inner); else pr[k].zero();
+      }
+    }
+    float v[NCH][VEC], sum[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NCH; ++k)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        v[k][i] = px[k].get(i);
+        if (res != nullptr) v[k][i] += pr[k].get(i);
+        sum[i] = fmaf(v[k][i], v[k][i], sum[i]);
+      }
+    if (a.s != nullptr && live) {
+#pragma unroll
+      for (int k = 0; k < NCH; ++k) {
+        const int c = wy + k * ny;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) px[k].put(i, v[k][i]);
+        if (c < a.C) px[k].store(static_cast<T*>(a.s) + base + c * a.inner);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) red[phase][wy][lane * VEC + i] = sum[i];
+    __syncthreads();
+    float rstd[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      float q = 0.f;
+      for (int y = 0; y < ny; ++y) q += red[phase][y][lane * VEC + i];
+      rstd[i] = rsqrtf(fmaf(q, inv_c, a.eps));
+    }
+    phase ^= 1;
+    if (!live) continue;
+    if (a.rstd != nullptr && wy == 0) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) a.rstd[o * a.inner + p + i] = rstd[i];
+    }
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      const int c = wy + k * ny;
+      if (c >= a.C) continue;
+      const float w = __ldg(a.weight + c);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) px[k].put(i, v[k][i] * (rstd[i] * w));
+      px[k].store(static_cast<T*>(a.y) + base + c * a.inner);
+    }
+  }
+}
+
+template <typename T, int VEC, int NCH>
+__global__ void __launch_bounds__(256) norm_field_backward_kernel(const FieldArgs a) {
+  __shared__ float red[2][8][32 * VEC];
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x, wy = threadIdx.y, ny = blockDim.y;
+  const float inv_c = 1.0f / (float)a.C;
+  const T* gs = static_cast<const T*>(a.gs);
+  float gw[NCH], w[NCH];
+#pragma unroll
+  for (int k = 0; k < NCH; ++k) {
+    const int c = wy + k * ny;
+    gw[k] = 0.f;
+    w[k] = c < a.C ? __ldg(a.weight + c) : 0.f;
+  }
+  int phase = 0;
+  for (long long t = blockIdx.x; t < a.outer * a.tiles; t += gridDim.x) {
+    const long long o = t / a.tiles, p = (t % a.tiles) * (32 * VEC) + lane * VEC;
+    const long long base = o * a.C * a.inner + p;
+    const bool live = p < a.inner;
+    Pack<T, VEC> pg[NCH], ps[NCH], pr[NCH];
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      const int c = wy + k * ny;
+      const bool on = live && c < a.C;
+      if (on) pg[k].load(static_cast<const T*>(a.gy) + base + c * a.inner); else pg[k].zero();
+      if (on) ps[k].load(static_cast<const T*>(a.x) + base + c * a.inner); else ps[k].zero();
+      if (gs != nullptr) {
+        if (on) pr[k].load(gs + base + c * a.inner); else pr[k].zero();
+      }
+    }
+    float rstd[VEC], dot[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      rstd[i] = live ? __ldg(a.rstd_in + o * a.inner + p + i) : 0.f;
+      dot[i] = 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < NCH; ++k)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float g = pg[k].get(i), n = ps[k].get(i) * rstd[i];
+        gw[k] = fmaf(g, n, gw[k]);
+        dot[i] = fmaf(w[k] * g, n, dot[i]);
+      }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) red[phase][wy][lane * VEC + i] = dot[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      float q = 0.f;
+      for (int y = 0; y < ny; ++y) q += red[phase][y][lane * VEC + i];
+      dot[i] = q * inv_c;
+    }
+    phase ^= 1;
+    if (!live) continue;
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      const int c = wy + k * ny;
+      if (c >= a.C) continue;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        float g = rstd[i] * fmaf(-(ps[k].get(i) * rstd[i]), dot[i], w[k] * pg[k].get(i));
+        if (gs != nullptr) g += pr[k].get(i);
+        ps[k].put(i, g);
+      }
+      ps[k].store(static_cast<T*>(a.y) + base + c * a.inner);
+    }
+  }
+  if (a.partial == nullptr) return;
+#pragma unroll
+  for (int k = 0; k < NCH; ++k) {
+    const int c = wy + k * ny;
+    const float t = warp_sum(gw[k]);
+    if (lane == 0 && c < a.C) a.partial[(long long)blockIdx.x * a.C + c] = t;
+  }
+}
+
+// More channels than the register kernels hold (128): a thread per position, the channels walked twice.
+template <typename T>
+__global__ void __launch_bounds__(128) norm_wide_field_kernel(const FieldArgs a) {
+  pdl_trigger();
+  pdl_wait();
+  const T* res = static_cast<const T*>(a.residual);
+  const float inv_c = 1.0f / (float)a.C;
+  const long long n = a.outer * a.inner;
+  for (long long t = (long long)blockIdx.x * 128 + threadIdx.x; t < n; t += (long long)gridDim.x * 128) {
+    const long long base = (t / a.inner) * a.C * a.inner + t % a.inner;
+    float sum = 0.f;
+    for (long long c = 0; c < a.C; ++c) {
+      float v = Elem<T>::get(static_cast<const T*>(a.x)[base + c * a.inner]);
+      if (res != nullptr) v += Elem<T>::get(res[base + c * a.inner]);
+      sum = fmaf(v, v, sum);
+    }
+    const float rstd = rsqrtf(fmaf(sum, inv_c, a.eps));
+    if (a.rstd != nullptr) a.rstd[t] = rstd;
+    for (long long c = 0; c < a.C; ++c) {
+      float v = Elem<T>::get(static_cast<const T*>(a.x)[base + c * a.inner]);
+      if (res != nullptr) v += Elem<T>::get(res[base + c * a.inner]);
+      if (a.s != nullptr) static_cast<T*>(a.s)[base + c * a.inner] = Elem<T>::put(v);
+      static_cast<T*>(a.y)[base + c * a.inner] = Elem<T>::put(v * (rstd * __ldg(a.weight + c)));
+    }
+  }
+}
+template <typename T>
+__global__ void __launch_bounds__(128) norm_wide_field_backward_kernel(const FieldArgs a) {
+  pdl_trigger();
+  pdl_wait();
+  const T* gy = static_cast<const T*>(a.gy);
+  const T* s = static_cast<const T*>(a.x);
+  const T* gs = static_cast<const T*>(a.gs);
+  const float inv_c = 1.0f / (float)a.C;
+  const long long n = a.outer * a.inner;
+  for (long long t = (long long)blockIdx.x * 128 + threadIdx.x; t < n; t += (long long)gridDim.x * 128) {
+    const long long base = (t / a.inner) * a.C * a.inner + t % a.inner;
+    const float rstd = a.rstd_in[t];
+    float dot = 0.f;
+    for (long long c = 0; c < a.C; ++c)
+      dot = fmaf(__ldg(a.weight + c) * Elem<T>::get(gy[base + c * a.inner]), Elem<T>::get(s[base + c * a.inner]) * rstd, dot);
+    dot *= inv_c;
+    for (long long c = 0; c < a.C; ++c) {
+      float g = rstd * fmaf(-(Elem<T>::get(s[base + c * a.inner]) * rstd), dot,
+                            __ldg(a.weight + c) * Elem<T>::get(gy[base + c * a.inner]));
+      if (gs != nullptr) g += Elem<T>::get(gs[base + c * a.inner]);
+      static_cast<T*>(a.y)[base + c * a.inner] = Elem<T>::put(g);
+    }
+  }
+}
+// weight gradient of one channel (blockIdx.x) over a share (blockIdx.y) of the positions
+template <typename T>
+__global__ void __launch_bounds__(256) norm_wide_field_weight_kernel(const FieldArgs a) {
+  __shared__ float red[64];
+  pdl_trigger();
+  pdl_wait();
+  int phase = 0;
+  const long long c = blockIdx.x, n = a.outer * a.inner;
+  float t = 0.f;
+  for (long long p = (long long)blockIdx.y * 256 + threadIdx.x; p < n; p += (long long)gridDim.y * 256) {
+    const long long at = (p / a.inner) * a.C * a.inner + c * a.inner + p % a.inner;
+    t = fmaf(Elem<T>::get(static_cast<const T*>(a.gy)[at]), Elem<T>::get(static_cast<const T*>(a.x)[at]) * a.rstd_in[p], t);
+  }
+  t = row_sum<256>(t, red, phase);
+  if (threadIdx.x == 0) a.partial[(long long)blockIdx.y * a.C + c] = t;
+}
+
+// grad_w[c] = sum over parts, in a fixed order: 8 warps take every eighth part, their sums meet in warp order.
+__global__ void __launch_bounds__(256) norm_weight_sum_kernel(const float* __restrict__ partial, float* __restrict__ gw,
+                                                             int parts, long long C) {
+  __shared__ float red[8][32];
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const long long c = (long long)blockIdx.x * 32 + lane;
+  float t = 0.f;
+  if (c < C)
+    for (int p = w; p < parts; p += 8) t += partial[(long long)p * C + c];
+  red[w][lane] = t;
+  __syncthreads();
+  if (w == 0 && c < C) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t += red[i][lane];
+    gw[c] = t;
+  }
+}
+
+template <typename T, bool BACK>
+cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
+  constexpr int WIDE = 16 / (int)sizeof(T) < 4 ? 16 / (int)sizeof(T) : 4;   // 16 bytes of fp32, 8 bytes of a 16-bit type
+  if (a.C > kNormFieldChannels) {
+    const long long n = a.outer * a.inner, most = (long long)num_sms() * 16;
+    const long long ctas = (n + 127) / 128;
+    const dim3 grid((unsigned)(ctas < most ? ctas : most));
+    if (!BACK) return launch_pdl(norm_wide_field_kernel<T>, grid, dim3(128), 0, st, a);
+    cudaError_t e = cudaSuccess;
+    if (a.y != nullptr) e = launch_pdl(norm_wide_field_backward_kernel<T>, grid, dim3(128), 0, st, a);
+    if (e == cudaSuccess && a.partial != nullptr) {
+      *parts = 8;
+      e = launch_pdl(norm_wide_field_weight_kernel<T>, dim3((unsigned)a.C, 8), dim3(256), 0, st, a);
+    }
+    return e;
+  }
+  const size_t need = WIDE * sizeof(T);
+  const bool vec = a.inner % WIDE == 0 && aligned_to(a.x, need) && aligned_to(a.residual, need) && aligned_to(a.gy, need) &&
+                   aligned_to(a.gs, need) && aligned_to(a.s, need) && aligned_to(a.y, need);
+  const int ny = a.C <= 32 ? 4 : 8, nch = (int)((a.C + ny - 1) / ny);
+  const int per = 32 * (vec ? WIDE : 1);
+  a.tiles = (a.inner + per - 1) / per;
+  // the weight gradient's partial sums are one row per CTA
+  const long long most = BACK ? (long long)kNormParts : (long long)num_sms() * 32, all = a.outer * a.tiles;
+  const dim3 grid((unsigned)(all < most ? all : most)), block(32, ny);
+  *parts = (int)grid.x;
+#define DTST_FIELD(N)                                                                                             \
+  if (nch <= N) {                                                                                                 \
+    if (BACK)                                                                                                     \
+      return vec ? launch_pdl(norm_field_backward_kernel<T, WIDE, N>, grid, block, 0, st, a)                      \
+                 : launch_pdl(norm_field_backward_kernel<T, 1, N>, grid, block, 0, st, a);                        \
+    return vec ? launch_pdl(norm_field_kernel<T, WIDE, N>, grid, block, 0, st, a)                                 \
+               : launch_pdl(norm_field_kernel<T, 1, N>, grid, block, 0, st, a);                                   \
+  }
+  DTST_FIELD(2)
+  DTST_FIELD(5)
+  DTST_FIELD(8)
+  DTST_FIELD(16)
+#undef DTST_FIELD
+  return cudaErrorNotSupported;
+}
+
+template <typename T>
+cudaError_t launch_rows_backward(const RowBackArgs& a, int* parts, cudaStream_t st) {
+  constexpr int VEC = kVec<T>;
+  const long long groups = (a.C + VEC - 1) / VEC;
+  const bool al = a.C % VEC == 0 && aligned_to(a.gy, 16) && aligned_to(a.s, 16) && aligned_to(a.gs, 16) && aligned_to(a.gx, 16);
+#define DTST_ROWS(TPR, ITEMS)                                                                                     \
+  {                                                                                                               \
+    constexpr int RPC = kRowThreads<TPR> / TPR;                                                                   \
+    const long long ctas = (a.rows + RPC - 1) / RPC;                                                              \
+    *parts = (int)(ctas < kNormParts ? ctas : kNormParts);                                                        \
+    const dim3 grid((unsigned)*parts), block(kRowThreads<TPR>);                                                   \
+    const size_t smem = RPC > 1 ? sizeof(float) * RPC * ITEMS * TPR * VEC : 0;                                    \
+    return al ? launch_pdl(norm_rows_backward_kernel<T, TPR, ITEMS, true>, grid, block, smem, st, a)              \
+              : launch_pdl(norm_rows_backward_kernel<T, TPR, ITEMS, false>, grid, block, smem, st, a);            \
+  }
+  if (groups <= 32) DTST_ROWS(32, 1)
+  if (groups <= 64) DTST_ROWS(32, 2)
+  if (groups <= 128) DTST_ROWS(128, 1)
+  if (groups <= 256) DTST_ROWS(256, 1)
+  if (groups <= 512) DTST_ROWS(512, 1)
+  if (groups <= 1024) DTST_ROWS(512, 2)
+#undef DTST_ROWS
+  const long long most = (long long)num_sms() * 4;
+  cudaError_t e = launch_pdl(norm_long_rows_backward_kernel<T>, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(512), 0, st, a);
+  if (e == cudaSuccess && a.partial != nullptr) {
+    *parts = (int)(a.rows < 64 ? a.rows : 64);
+    e = launch_pdl(norm_long_rows_weight_kernel<T>, dim3((unsigned)((a.C + 255) / 256), (unsigned)*parts), dim3(256), 0, st, a);
+  }
+  return e;
+}
+
+template <typename T>
+cudaError_t forward_t(const NormCall& n, cudaStream_t st) {
+  if (n.inner == 1 || n.q != nullptr) {
+    RowArgs a{n.x, n.residual, n.weight, n.s, n.y, n.q, n.scale, n.rstd, n.outer, n.channels, n.x_ld, n.q_ld, n.eps, 0};
+    if (n.q == nullptr) return launch_rows<T, false, true>(a, st);
+    a.q_aligned = n.q_ld % 8 == 0 && aligned_to(n.q, 8);
+    return n.weight != nullptr ? launch_rows<T, true, true>(a, st) : launch_rows<T, true, false>(a, st);
+  }
+  FieldArgs a{n.x, n.residual, nullptr, nullptr, n.weight, nullptr, n.s, n.y, n.rstd, nullptr, n.outer, n.channels, n.inner, 0, n.eps};
+  int parts = 0;
+  return launch_field<T, false>(a, &parts, st);
+}
+
+template <typename T>
+cudaError_t backward_t(const NormBackCall& n, cudaStream_t st) {
+  int parts = 0;
+  cudaError_t e;
+  float* partial = n.grad_weight != nullptr ? n.partial : nullptr;
+  if (n.inner == 1) {
+    RowBackArgs a{n.grad_y, n.s, n.grad_s, n.weight, n.rstd, n.grad_x, partial, n.outer, n.channels};
+    e = launch_rows_backward<T>(a, &parts, st);
+  } else {
+    FieldArgs a{n.s, nullptr, n.grad_y, n.grad_s, n.weight, n.rstd, nullptr, n.grad_x, nullptr, partial, n.outer, n.channels, n.inner, 0, 0.f};
+    e = launch_field<T, true>(a, &parts, st);
+  }
+  if (e != cudaSuccess || partial == nullptr) return e;
+  return launch_pdl(norm_weight_sum_kernel, dim3((unsigned)((n.channels + 31) / 32)), dim3(256), 0, st,
+                    static_cast<const float*>(partial), n.grad_weight, parts, (long long)n.channels);
+}
+
+}  // namespace
+
+cudaError_t launch_norm_forward(const NormCall& n, cudaStream_t st) {
+  switch (n.dtype) {
+    case DTST_F32: return forward_t<float>(n, st);
+    case DTST_BF16: return forward_t<__nv_bfloat16>(n, st);
+    default: return forward_t<__half>(n, st);
+  }
+}
+
+cudaError_t launch_norm_backward(const NormBackCall& n, cudaStream_t st) {
+  switch (n.dtype) {
+    case DTST_F32: return backward_t<float>(n, st);
+    case DTST_BF16: return backward_t<__nv_bfloat16>(n, st);
+    default: return backward_t<__half>(n, st);
+  }
+}
+
+}  // namespace dtst

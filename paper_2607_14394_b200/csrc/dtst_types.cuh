@@ -1,0 +1,91 @@
+// Element types of the recurrent-memory operators (norm, 8-bit product, recurrence) and their vector loads/stores.
+// Arithmetic is in 32 bits for every type; a value is rounded once, when it is stored.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace dtst {
+
+template <typename T>
+struct Elem;
+
+template <>
+struct Elem<float> {
+  static __device__ __forceinline__ float get(float v) { return v; }
+  static __device__ __forceinline__ float put(float v) { return v; }
+};
+template <>
+struct Elem<__nv_bfloat16> {
+  static __device__ __forceinline__ float get(__nv_bfloat16 v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
+};
+template <>
+struct Elem<__half> {
+  static __device__ __forceinline__ float get(__half v) { return __half2float(v); }
+  static __device__ __forceinline__ __half put(float v) { return __float2half_rn(v); }
+};
+
+template <int BYTES>
+struct RawOf;
+template <>
+struct RawOf<2> { using type = uint16_t; };
+template <>
+struct RawOf<4> { using type = uint32_t; };
+template <>
+struct RawOf<8> { using type = uint2; };
+template <>
+struct RawOf<16> { using type = uint4; };
+
+// N elements as they lie in memory.  `load` and `store` move them in one access (the address is aligned to N
+// elements); the `_part` forms touch only the first `n` of them, one by one.
+template <typename T, int N>
+struct Pack {
+  using Raw = typename RawOf<N * (int)sizeof(T)>::type;
+  union {
+    Raw raw;
+    T v[N];
+  };
+  __device__ __forceinline__ Pack() {}
+  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
+  __device__ __forceinline__ void load_part(const T* p, int n) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = i < n ? p[i] : Elem<T>::put(0.f);
+  }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Raw*>(p) = raw; }
+  __device__ __forceinline__ void store_part(T* p, int n) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = v[i];
+  }
+  __device__ __forceinline__ float get(int i) const { return Elem<T>::get(v[i]); }
+  __device__ __forceinline__ void put(int i, float x) { v[i] = Elem<T>::put(x); }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = Elem<T>::put(0.f);
+  }
+};
+
+constexpr float kE4m3Max = 448.f;
+constexpr float kAmaxFloor = 0x1p-100f;   // a block of zeros keeps a finite scale, and its values stay zero
+constexpr int kFp8Block = 128;            // values that share a scale along the contracted dimension
+
+// four fp32 values -> four e4m3 values in a word, to nearest even, the largest finite value beyond the range
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+  return lo | (hi << 16);
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+}  // namespace dtst

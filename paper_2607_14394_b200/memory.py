@@ -1,0 +1,512 @@
+"""Recurrent memory around the layer: the root-mean-square norm, the 8-bit product, the gated linear recurrence, and
+two blocks made of them.
+
+The spectral layer of a 3D+time operator treats time as one more grid dimension; a rollout over many frames needs a
+state that is carried from frame to frame instead.  `RmsNorm`, `GatedScan` and `Fp8Linear` are thin wrappers over the
+C entry points (`dtst_rms_norm*`, `dtst_gated_scan*`, `dtst_matmul_fp8`): they check arguments, allocate outputs that
+the caller did not bring, and pass device pointers on; every arithmetic step runs in the CUDA library.  Every call runs
+on the current stream, or on the one given as `stream=`.
+
+`FieldMemory` is a trainable block on channels-first fields [B, C, n..., T] whose last axis is time; `RolloutMemory`
+is the serving form on latent vectors [B, T, D] with 8-bit projections, a whole history or one frame at a time.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+from typing import List, Optional, Sequence, Tuple
+
+import torch
+
+from . import binding as Bn
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+GATES = {"sigmoid": 0, "decay": 1}
+FP8 = torch.float8_e4m3fn
+BLOCK = 128
+
+
+def _device(device) -> int:
+    d = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    if d.type != "cuda":
+        raise ValueError("the memory operators live on a CUDA device")
+    return torch.cuda.current_device() if d.index is None else d.index
+
+
+def _addr(t: Optional[torch.Tensor], name: str, dev: int, dtype: torch.dtype, shape=None, contiguous=True) -> int:
+    """Device address of t after the checks every tensor goes through (0 for None)."""
+    if t is None:
+        return 0
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be a tensor on cuda:{dev}, got {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _on_stream(fn):
+    """Gives a call its `stream` keyword: the whole call, the allocation of its outputs included, runs on that stream."""
+
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kwargs):
+        if stream is None:
+            return fn(*args, **kwargs)
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream))
+        with torch.cuda.stream(stream):
+            return fn(*args, **kwargs)
+
+    return call
+
+
+def _call(fn, where: str, dev: int, *args) -> None:
+    """fn(*args, current stream) with `dev` current."""
+    s = torch.cuda.current_stream(dev).cuda_stream
+    if torch.cuda.current_device() == dev:
+        status = fn(*args, s)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, s)
+    if status != Bn.DTST_OK:
+        raise Bn.DtstError(status, where)
+
+
+def _rows16(k: int) -> int:
+    """Bytes between rows of k 8-bit values: rows start on 16-byte boundaries."""
+    return -(-k // 16) * 16
+
+
+def empty_fp8(rows: int, k: int, device=None) -> torch.Tensor:
+    """An uninitialised [rows, k] 8-bit tensor whose rows start on 16-byte boundaries."""
+    dev = torch.device("cuda", _device(device))
+    return torch.empty((rows, _rows16(k)), dtype=FP8, device=dev)[:, :k]
+
+
+class RmsNorm:
+    """y = s rstd weight, s = x + residual, rstd = (mean s^2 + eps)^-1/2 over dimension `dim` of `shape`.
+
+    `dim` is the last dimension (token-major rows) or any other one (channels-first fields).
+    """
+
+    def __init__(self, shape: Sequence[int], dim: int = -1, dtype: torch.dtype = torch.float32, eps: float = 1e-6,
+                 device=None):
+        self.shape = torch.Size(int(n) for n in shape)
+        nd = len(self.shape)
+        if nd < 1 or not -nd <= dim < nd:
+            raise ValueError(f"dim {dim} is no dimension of shape {tuple(self.shape)}")
+        if dtype not in DTYPES:
+            raise ValueError(f"dtype must be one of {list(DTYPES)}, got {dtype}")
+        self.dim, self.dtype, self.eps, self.dev = dim % nd, dtype, float(eps), _device(device)
+        self.device = torch.device("cuda", self.dev)
+        self.channels = self.shape[self.dim]
+        if self.channels < 1:
+            raise ValueError("the normalised dimension is empty")
+        self.outer = self.shape[:self.dim].numel()
+        self.inner = self.shape[self.dim + 1:].numel()
+        self._type = DTYPES[dtype]
+        self._rest = self.shape[:self.dim] + self.shape[self.dim + 1:]
+        self._wshape = torch.Size((self.channels,))
+        self._scratch = None
+        self._lib = Bn.lib()
+
+    def _empty(self):
+        return torch.empty(self.shape, dtype=self.dtype, device=self.device)
+
+    @_on_stream
+    def forward(self, x, weight, residual=None, out=None, sum_out=None, rstd=None):
+        """Returns (y, s, rstd); without a residual s is x itself."""
+        if out is None:
+            out = self._empty()
+        if residual is not None and sum_out is None:
+            sum_out = self._empty()
+        if rstd is None:
+            rstd = torch.empty(self._rest, dtype=torch.float32, device=self.device)
+        d, t, sh = self.dev, self.dtype, self.shape
+        _call(self._lib.dtst_rms_norm, "dtst_rms_norm", d, self._type, self.outer, self.channels, self.inner,
+              self.eps, _addr(x, "x", d, t, sh), _addr(residual, "residual", d, t, sh),
+              _addr(weight, "weight", d, torch.float32, self._wshape), _addr(sum_out, "sum_out", d, t, sh),
+              _addr(out, "out", d, t, sh), _addr(rstd, "rstd", d, torch.float32, self._rest))
+        return out, (x if sum_out is None else sum_out), rstd
+
+    @_on_stream
+    def forward_fp8(self, x, weight, residual=None, q=None, scale=None, sum_out=None):
+        """Returns (q, scale, s): the norm of token-major rows in 8 bits, [rows, channels], and its scales
+        [ceil(channels / 128), rows] - what Fp8Linear takes."""
+        if self.inner != 1:
+            raise ValueError("an 8-bit output needs the channels in the last dimension")
+        rows, c, d, t, sh = self.outer, self.channels, self.dev, self.dtype, self.shape
+        if q is None:
+            q = torch.empty((rows, _rows16(c)), dtype=FP8, device=self.device)
+            if c % 16:
+                q = q[:, :c]
+        if scale is None:
+            scale = torch.empty((-(-c // BLOCK), rows), dtype=torch.float32, device=self.device)
+        if residual is not None and sum_out is None:
+            sum_out = self._empty()
+        ld = _q_stride(q, rows, c)
+        _call(self._lib.dtst_rms_norm_fp8, "dtst_rms_norm_fp8", d, self._type, rows, c, self.eps,
+              _addr(x, "x", d, t, sh), _addr(residual, "residual", d, t, sh),
+              _addr(weight, "weight", d, torch.float32, self._wshape), _addr(sum_out, "sum_out", d, t, sh),
+              _addr(q, "q", d, FP8, None, False), ld,
+              _addr(scale, "scale", d, torch.float32, (-(-c // BLOCK), rows)))
+        return q, scale, (x if sum_out is None else sum_out)
+
+    @_on_stream
+    def backward(self, grad_y, s, weight, rstd, grad_s=None, grad_x=None, grad_weight=None, need_grad_weight=True):
+        """Returns (grad_x, grad_weight); grad_x is the gradient of x and of the residual."""
+        d, t, sh = self.dev, self.dtype, self.shape
+        if grad_x is None:
+            grad_x = self._empty()
+        scratch = 0
+        if need_grad_weight:
+            if grad_weight is None:
+                grad_weight = torch.empty(self._wshape, dtype=torch.float32, device=self.device)
+            if self._scratch is None:
+                n = ctypes.c_size_t()
+                Bn._check(self._lib.dtst_rms_norm_scratch_bytes(self.channels, ctypes.byref(n)),
+                          "dtst_rms_norm_scratch_bytes")
+                self._scratch = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+            scratch = self._scratch.data_ptr()
+        _call(self._lib.dtst_rms_norm_backward, "dtst_rms_norm_backward", d, self._type, self.outer,
+              self.channels, self.inner, _addr(grad_y, "grad_y", d, t, sh), _addr(s, "s", d, t, sh),
+              _addr(weight, "weight", d, torch.float32, self._wshape),
+              _addr(rstd, "rstd", d, torch.float32, self._rest), _addr(grad_s, "grad_s", d, t, sh),
+              _addr(grad_x, "grad_x", d, t, sh), _addr(grad_weight, "grad_weight", d, torch.float32, self._wshape),
+              scratch, self._scratch.numel() if scratch else 0)
+        return grad_x, grad_weight
+
+
+def _q_stride(q: torch.Tensor, rows: int, k: int) -> int:
+    if q.shape != (rows, k):
+        raise ValueError(f"8-bit tensor must have shape {(rows, k)}, got {tuple(q.shape)}")
+    if k > 1 and q.stride(1) != 1:
+        raise ValueError("the rows of an 8-bit tensor must be contiguous")
+    return q.stride(0) if rows > 1 else max(q.stride(0), _rows16(k))
+
+
+@_on_stream
+def quantize_fp8(x: torch.Tensor, q=None, scale=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rows x [rows, k] (contiguous along k) -> (q [rows, k] in 8 bits, scale [ceil(k / 128), rows])."""
+    if x.dim() != 2 or x.dtype not in DTYPES or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("quantize_fp8 takes rows [rows, k] of float32, bfloat16 or float16, contiguous along k")
+    rows, k = x.shape
+    dev = x.get_device()
+    if q is None:
+        q = empty_fp8(rows, k, x.device)
+    if scale is None:
+        scale = torch.empty((-(-k // BLOCK), rows), dtype=torch.float32, device=x.device)
+    _call(Bn.lib().dtst_quantize_fp8, "dtst_quantize_fp8", dev, DTYPES[x.dtype], rows, k,
+          _addr(x, "x", dev, x.dtype, None, False), x.stride(0), _addr(q, "q", dev, FP8, None, False),
+          _q_stride(q, rows, k), _addr(scale, "scale", dev, torch.float32, (-(-k // BLOCK), rows)))
+    return q, scale
+
+
+@_on_stream
+def quantize_fp8_weight(w: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """w [n, k] -> (8-bit values [n, k], scale [ceil(n / 128), ceil(k / 128)]), one scale per 128 x 128 block."""
+    if w.dim() != 2 or w.dtype not in DTYPES or (w.shape[1] > 1 and w.stride(1) != 1):
+        raise ValueError("quantize_fp8_weight takes w [n, k] of float32, bfloat16 or float16, contiguous along k")
+    n, k = w.shape
+    dev = w.get_device()
+    q = empty_fp8(n, k, w.device)
+    scale = torch.empty((-(-n // BLOCK), -(-k // BLOCK)), dtype=torch.float32, device=w.device)
+    _call(Bn.lib().dtst_quantize_fp8_weight, "dtst_quantize_fp8_weight", dev, DTYPES[w.dtype], n, k,
+          _addr(w, "w", dev, w.dtype, None, False), max(w.stride(0), k), _addr(q, "q", dev, FP8, None, False),
+          _q_stride(q, n, k), _addr(scale, "scale", dev, torch.float32))
+    return q, scale
+
+
+def _workspace(nbytes: int, dev: int) -> torch.Tensor:
+    """Zeroed memory that calls on any stream may use from now on."""
+    ws = torch.zeros(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev))
+    torch.cuda.current_stream(dev).synchronize()
+    return ws
+
+
+class _Workspace:
+    """Operators with a workspace: calls of one object share it and must be stream-ordered."""
+
+    @_on_stream
+    def status(self) -> int:
+        """DTST_OK, or DTST_ERR_DEVICE_TIMEOUT if a bounded wait gave up since the last query; synchronises."""
+        with torch.cuda.device(self.dev):
+            return int(Bn.lib().dtst_workspace_status(self.workspace.data_ptr(), Bn._stream_ptr(None)))
+
+
+class Fp8Linear(_Workspace):
+    """out = x w^T for 8-bit x [m, k] (scale [ceil(k / 128), m]) and weights [n, k] (a scale per 128 x 128 block)."""
+
+    def __init__(self, weight: torch.Tensor, weight_scale: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16):
+        if weight.dim() != 2 or weight.dtype != FP8:
+            raise ValueError("weight must be an 8-bit tensor [n, k] (see from_weight)")
+        if out_dtype not in DTYPES:
+            raise ValueError(f"out_dtype must be one of {list(DTYPES)}, got {out_dtype}")
+        self.dev = weight.get_device()
+        if self.dev < 0:
+            raise ValueError("weight must be a CUDA tensor")
+        self.device = weight.device
+        self.n, self.k = weight.shape
+        self.weight, self.weight_scale, self.out_dtype = weight, weight_scale, out_dtype
+        self._ld = _q_stride(weight, self.n, self.k)
+        self._kb = -(-self.k // BLOCK)
+        self._w = _addr(weight, "weight", self.dev, FP8, None, False)
+        self._ws = _addr(weight_scale, "weight_scale", self.dev, torch.float32, (-(-self.n // BLOCK), self._kb))
+        self.workspace = _workspace(256, self.dev)
+        self._type = DTYPES[out_dtype]
+        self._lib = Bn.lib()
+
+    @classmethod
+    def from_weight(cls, w: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16) -> "Fp8Linear":
+        """Quantises w [n, k] (float32, bfloat16 or float16) once."""
+        return cls(*quantize_fp8_weight(w), out_dtype=out_dtype)
+
+    @_on_stream
+    def forward(self, x: torch.Tensor, x_scale: torch.Tensor, out: Optional[torch.Tensor] = None):
+        m, d = x.shape[0], self.dev
+        if out is None:
+            out = torch.empty((m, self.n), dtype=self.out_dtype, device=self.device)
+        elif out.shape != (m, self.n) or (self.n > 1 and out.stride(1) != 1):
+            raise ValueError(f"out must have shape {(m, self.n)} and contiguous rows")
+        _call(self._lib.dtst_matmul_fp8, "dtst_matmul_fp8", d, self._type, m, self.n, self.k,
+              _addr(x, "x", d, FP8, None, False), _q_stride(x, m, self.k),
+              _addr(x_scale, "x_scale", d, torch.float32, (self._kb, m)), self._w, self._ld, self._ws,
+              _addr(out, "out", d, self.out_dtype, None, False), max(out.stride(0), self.n), self.workspace.data_ptr(),
+              256)
+        return out
+
+    __call__ = forward
+
+
+class GatedScan(_Workspace):
+    """h_t = a_t h_{t-1} + u_t along dimension `dim` of `shape`, forward and backward.
+
+    gate "sigmoid": a = sigmoid(g), u = (1 - a) v; "decay": a = g, u = v.  The states (h0, h_last) are float32 of the
+    shape without `dim`.  v and g may be strided in the dimensions in front of the last (both alike), e.g. the two
+    halves of one projection's output; h and the upstream gradient are contiguous.
+    """
+
+    def __init__(self, shape: Sequence[int], dim: int = 1, dtype: torch.dtype = torch.float32, gate: str = "sigmoid",
+                 device=None):
+        self.shape = torch.Size(int(n) for n in shape)
+        nd = len(self.shape)
+        if nd < 1 or not -nd <= dim < nd:
+            raise ValueError(f"dim {dim} is no dimension of shape {tuple(self.shape)}")
+        if dtype not in DTYPES:
+            raise ValueError(f"dtype must be one of {list(DTYPES)}, got {dtype}")
+        if gate not in GATES:
+            raise ValueError(f"gate must be one of {list(GATES)}, got {gate!r}")
+        self.dim, self.dtype, self.gate, self.dev = dim % nd, dtype, gate, _device(device)
+        self.device = torch.device("cuda", self.dev)
+        self.length = self.shape[self.dim]
+        self.outer_shape, inner_shape = self.shape[:self.dim], self.shape[self.dim + 1:]
+        self.outer, self.inner = self.outer_shape.numel(), inner_shape.numel()
+        if self.inner < 1:
+            raise ValueError("the dimensions behind the recurrence's must not be empty")
+        self.state_shape = self.outer_shape + inner_shape
+        dense = (self.length * self.inner, self.inner)
+        self._dense = dense
+        self._desc = Bn.ScanDesc(DTYPES[dtype], GATES[gate], self.outer, self.length, self.inner, dense, dense)
+        self._ref = ctypes.byref(self._desc)
+        self._lib = Bn.lib()
+        n, ck = ctypes.c_size_t(), ctypes.c_int64()
+        Bn._check(self._lib.dtst_gated_scan_sizes(self._ref, ctypes.byref(n), ctypes.byref(ck)), "dtst_gated_scan_sizes")
+        self.checkpoint_floats = int(ck.value)
+        self.workspace = _workspace(int(n.value), self.dev)
+        self._ws = (self.workspace.data_ptr(), int(n.value))
+
+    def new_checkpoints(self) -> torch.Tensor:
+        """A buffer for the states that a forward pass saves for its backward pass."""
+        return torch.empty(self.checkpoint_floats, dtype=torch.float32, device=self.device)
+
+    def _strides(self, t: torch.Tensor, name: str) -> Tuple[int, int]:
+        """(outer, step) strides of t, whose other dimensions must lie together."""
+        if t.shape != self.shape:
+            raise ValueError(f"{name} must have shape {tuple(self.shape)}, got {tuple(t.shape)}")
+        if t.is_contiguous():
+            return self._dense
+        st, sh, k = t.stride(), self.shape, self.dim
+
+        def joined(dims: range) -> Optional[int]:        # the stride of several dimensions taken as one
+            at = None
+            for i in reversed(dims):
+                if sh[i] == 1:
+                    continue
+                if at is not None and st[i] != at[1]:
+                    raise ValueError(f"{name}: the dimensions on each side of the recurrence's must lie together")
+                at = (st[i] if at is None else at[0], st[i] * sh[i])
+            return None if at is None else at[0]
+
+        inner, outer = joined(range(k + 1, len(sh))), joined(range(0, k))
+        if inner not in (None, 1):
+            raise ValueError(f"{name}: the last dimension must be contiguous")
+        step = st[k] if sh[k] != 1 else self.inner
+        if self.inner == 1 and step != 1:
+            raise ValueError(f"{name}: the recurrence's dimension must be contiguous when it is the last one")
+        return (self._dense[0] if outer is None else outer), step
+
+    def _inputs(self, v, g):
+        a, b = self._strides(v, "v"), self._strides(g, "g")
+        if a != b:
+            raise ValueError(f"v and g must have the same strides, got {v.stride()} and {g.stride()}")
+        self._desc.in_stride[0], self._desc.in_stride[1] = a
+
+    @_on_stream
+    def forward(self, v, g, h0=None, lengths=None, out=None, h_last=None, checkpoints=None):
+        """Returns (h, h_last).  lengths: int32 per outer entry; checkpoints: see new_checkpoints."""
+        d, t = self.dev, self.dtype
+        self._inputs(v, g)
+        if out is None:
+            out = torch.empty(self.shape, dtype=t, device=self.device)
+        if h_last is None:
+            h_last = torch.empty(self.state_shape, dtype=torch.float32, device=self.device)
+        _call(self._lib.dtst_gated_scan, "dtst_gated_scan", d, self._ref, _addr(v, "v", d, t, None, False),
+              _addr(g, "g", d, t, None, False), _addr(h0, "h0", d, torch.float32, self.state_shape),
+              self._lengths(lengths), _addr(out, "out", d, t, self.shape),
+              _addr(h_last, "h_last", d, torch.float32, self.state_shape),
+              _addr(checkpoints, "checkpoints", d, torch.float32, (self.checkpoint_floats,)), *self._ws)
+        return out, h_last
+
+    def _lengths(self, lengths) -> int:
+        return 0 if lengths is None else _addr(lengths, "lengths", self.dev, torch.int32, self.outer_shape)
+
+    @_on_stream
+    def backward(self, grad_h, v, g, checkpoints, h0=None, lengths=None, grad_last=None, grad_v=None, grad_g=None,
+                 grad_h0=None, need_grad_h0=True):
+        """Returns (grad_v, grad_g, grad_h0); v, g, h0, lengths and checkpoints as in the forward call."""
+        d, t = self.dev, self.dtype
+        self._inputs(v, g)
+        if grad_v is None:
+            grad_v = torch.empty(self.shape, dtype=t, device=self.device)
+        if grad_g is None:
+            grad_g = torch.empty(self.shape, dtype=t, device=self.device)
+        a, b = self._strides(grad_v, "grad_v"), self._strides(grad_g, "grad_g")
+        if a != b:
+            raise ValueError(f"grad_v and grad_g must have the same strides, got {grad_v.stride()} and {grad_g.stride()}")
+        self._desc.grad_stride[0], self._desc.grad_stride[1] = a
+        if grad_h0 is None and need_grad_h0:
+            grad_h0 = torch.empty(self.state_shape, dtype=torch.float32, device=self.device)
+        _call(self._lib.dtst_gated_scan_backward, "dtst_gated_scan_backward", d, self._ref,
+              _addr(grad_h, "grad_h", d, t, self.shape), _addr(grad_last, "grad_last", d, torch.float32, self.state_shape),
+              _addr(v, "v", d, t, None, False), _addr(g, "g", d, t, None, False),
+              _addr(h0, "h0", d, torch.float32, self.state_shape), self._lengths(lengths),
+              _addr(checkpoints, "checkpoints", d, torch.float32, (self.checkpoint_floats,)),
+              _addr(grad_v, "grad_v", d, t, None, False), _addr(grad_g, "grad_g", d, t, None, False),
+              _addr(grad_h0, "grad_h0", d, torch.float32, self.state_shape), *self._ws)
+        return grad_v, grad_g, grad_h0
+
+
+class FieldMemory:
+    """A trainable memory along the time axis of fields x [B, C, n..., T] (float32, T last), pre-normalised and residual:
+
+        y = norm(x);  v = W_v y + b_v;  g = W_g y + b_g;  h = scan(v, g);  out = x + W_o h
+
+    forward(x) -> out and backward(grad_out) -> gradients of x and of every parameter; point-wise maps are
+    dtst_pointwise_linear (C <= 32, points % 4 == 0).  Parameters are plain tensors owned by this object.
+    """
+
+    def __init__(self, B: int, C: int, grid: Sequence[int], device=None, seed: int = 0):
+        shape = (B, C) + tuple(int(n) for n in grid)
+        self.norm = RmsNorm(shape, 1, device=device)
+        self.scan = GatedScan(shape, len(shape) - 1, device=device)
+        dev = self.device = self.norm.device
+        self.shape, self.C = shape, C
+        gen = torch.Generator(device=dev).manual_seed(seed)
+        rn = lambda *s: torch.randn(s, device=dev, generator=gen)
+        self.weight = torch.ones(C, device=dev)
+        self.W_v, self.W_g, self.W_o = (rn(C, C) / C ** 0.5 for _ in range(3))
+        self.b_v, self.b_g = torch.zeros(C, device=dev), torch.full((C,), 2.0, device=dev)
+        n = Bn.dtst_pointwise_linear_scratch_bytes(C, C)
+        self._scratch = torch.empty(n, dtype=torch.uint8, device=dev)
+        new = lambda: torch.empty(shape, device=dev)
+        self.y, self.v, self.g, self.h, self.out = new(), new(), new(), new(), new()
+        self.rstd = torch.empty((B,) + shape[2:], device=dev)
+        self.checkpoints = self.scan.new_checkpoints()
+        self.x = self.h0 = self.lengths = None
+
+    @_on_stream
+    def forward(self, x, h0=None):
+        """Returns (out, h_last); both passes work in this object's buffers."""
+        self.x, self.h0 = x, h0
+        self.norm.forward(x, self.weight, out=self.y, rstd=self.rstd)
+        Bn.dtst_pointwise_linear(self.y, self.W_v, self.b_v, self.v)
+        Bn.dtst_pointwise_linear(self.y, self.W_g, self.b_g, self.g)
+        _, last = self.scan.forward(self.v, self.g, h0, out=self.h, checkpoints=self.checkpoints)
+        Bn.dtst_pointwise_linear(self.h, self.W_o, None, self.out)
+        self.out.add_(x)
+        return self.out, last
+
+    @_on_stream
+    def backward(self, grad_out, grad_last=None) -> dict:
+        e = torch.empty_like
+        gr = {"W_o": e(self.W_o), "W_v": e(self.W_v), "W_g": e(self.W_g), "b_v": e(self.b_v), "b_g": e(self.b_g)}
+        gh, gy, gyg = e(self.h), e(self.y), e(self.y)
+        back = Bn.dtst_pointwise_linear_backward
+        back(grad_out, self.h, self.W_o, gh, gr["W_o"], None, self._scratch)
+        gv, gg, gr["h0"] = self.scan.backward(gh, self.v, self.g, self.checkpoints, self.h0, grad_last=grad_last,
+                                              need_grad_h0=self.h0 is not None)
+        back(gv, self.y, self.W_v, gy, gr["W_v"], gr["b_v"], self._scratch)
+        back(gg, self.y, self.W_g, gyg, gr["W_g"], gr["b_g"], self._scratch)
+        gy.add_(gyg)
+        # the residual's gradient joins inside the norm's backward pass
+        gr["x"], gr["weight"] = self.norm.backward(gy, self.x, self.weight, self.rstd, grad_s=grad_out)
+        return gr
+
+
+class RolloutMemory:
+    """Recurrent layers on latent vectors with 8-bit projections, for serving: a history [B, T, D] at once, then frame
+    by frame [B, 1, D] with the state carried on.
+
+        r_0 = x;  per layer: [v | g] = W_in q(norm(r_l)), h = scan(v, g), r_{l+1} = r_l + W_out q(h);  out = norm(r_L)
+
+    x and out are `dtype` (bfloat16 by default); the residual's addition runs inside the next layer's norm.
+    weights: per layer (W_in [2 H, D], W_out [D, H], norm weight [D]); final_weight [D].
+    """
+
+    def __init__(self, weights: List[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]], final_weight: torch.Tensor,
+                 batch: int, dtype: torch.dtype = torch.bfloat16, eps: float = 1e-6):
+        self.B, self.dtype, self.eps = int(batch), dtype, eps
+        self.D = final_weight.numel()
+        self.final_weight, self.device = final_weight, final_weight.device
+        self.layers = []
+        for w_in, w_out, nw in weights:
+            if w_in.shape[1] != self.D or w_in.shape[0] != 2 * w_out.shape[1] or w_out.shape[0] != self.D or nw.numel() != self.D:
+                raise ValueError("RolloutMemory: weights are (W_in [2 H, D], W_out [D, H], norm weight [D])")
+            self.layers.append((Fp8Linear.from_weight(w_in, dtype), Fp8Linear.from_weight(w_out, dtype), nw))
+        self.states = [torch.zeros((self.B, lin.k), device=self.device) for _, lin, _ in self.layers]
+        self._plans: dict = {}
+
+    def reset(self) -> None:
+        for s in self.states:
+            s.zero_()
+
+    def _plan(self, T: int):
+        if T not in self._plans:
+            norm = RmsNorm((self.B * T, self.D), -1, self.dtype, self.eps, self.device)
+            scans = [GatedScan((self.B, T, lin.k), 1, self.dtype, device=self.device) for _, lin, _ in self.layers]
+            self._plans[T] = (norm, scans)
+        return self._plans[T]
+
+    @_on_stream
+    def forward(self, x: torch.Tensor, lengths=None) -> torch.Tensor:
+        """x [B, T, D] -> out [B, T, D]; the layers' states move on by T frames (by lengths[b] where given)."""
+        B, T, D = x.shape
+        if (B, D) != (self.B, self.D):
+            raise ValueError(f"x must be [{self.B}, T, {self.D}], got {tuple(x.shape)}")
+        norm, scans = self._plan(T)
+        r, delta = x.view(B * T, D), None
+        for (lin_in, lin_out, nw), scan, state in zip(self.layers, scans, self.states):
+            q, sc, r = norm.forward_fp8(r, nw, residual=delta)
+            vg = lin_in.forward(q, sc).view(B, T, 2 * lin_out.k)
+            h, _ = scan.forward(vg[..., :lin_out.k], vg[..., lin_out.k:], state, lengths=lengths, h_last=state)
+            delta = lin_out.forward(*quantize_fp8(h.view(B * T, lin_out.k)))
+        y, _, _ = norm.forward(r, self.final_weight, residual=delta)
+        return y.view(B, T, D)
+
+    @_on_stream
+    def step(self, frame: torch.Tensor) -> torch.Tensor:
+        """One new frame [B, D] -> [B, D]."""
+        return self.forward(frame.view(self.B, 1, self.D)).view(self.B, self.D)

@@ -178,12 +178,25 @@ struct ScanArgs {
   int* status;
 };
 
-// a = 1 / (1 + e^-g) and b = 1 - a, each formed without cancellation
+// a = 1 / (1 + e^-g) and b = 1 - a, each formed without cancellation.  The approximate exponential and reciprocal are good
+// to about 2^-22; what they flush to zero (|g| > 87) is below the smallest normal number anyway.
 __device__ __forceinline__ void gate_of(float g, float& a, float& b) {
-  const float e = __expf(-fabsf(g));
-  const float r = __fdividef(1.0f, 1.0f + e);
-  a = g >= 0.f ? r : e * r;
-  b = g >= 0.f ? e * r : r;
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(g) * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  const float er = e * r;
+  a = g >= 0.f ? r : er;
+  b = g >= 0.f ? er : r;
+}
+// h_t = a h_{t-1} + b v_t
+__device__ __forceinline__ void terms(int sigmoid, float g, float& a, float& b) {
+  if (sigmoid) gate_of(g, a, b);
+  else a = g, b = 1.f;
+}
+// the gate of a step that leaves the state alone (with v = 0): a = 1
+template <typename T>
+__device__ __forceinline__ T neutral_gate(int sigmoid) {
+  return Elem<T>::put(sigmoid ? __int_as_float(0x7f800000) : 1.f);
 }
 
 __device__ __forceinline__ long long clamp_len(const int* lengths, long long o, long long L) {
@@ -270,6 +283,7 @@ __global__ void __launch_bounds__(S::THREADS, 1024 / S::THREADS) scan_cols_kerne
   const T* g = p.g + at.o * p.in_o + at.i0;
   T* h = p.h + at.o * p.L * p.inner + at.i0;
   const long long states = p.outer * p.inner;
+  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
   float state = SLOTS > 1 && at.keeper && c_first == 0 && p.h0 != nullptr ? p.h0[at.ch] : 0.f;
 
 #pragma unroll 1
@@ -278,23 +292,17 @@ __global__ void __launch_bounds__(S::THREADS, 1024 / S::THREADS) scan_cols_kerne
     Pack<T, VEC> pv[R], pg[R];
     const T *lv = v + t0 * p.in_t, *lg = g + t0 * p.in_t;
 #pragma unroll
-    for (int r = 0; r < R; ++r, lv += p.in_t, lg += p.in_t)
+    for (int r = 0; r < R; ++r, lv += p.in_t, lg += p.in_t) {
       if (t0 + r < at.end) pv[r].load(lv), pg[r].load(lg);
+      else pv[r].fill(none_v), pg[r].fill(none_g);
+    }
     float a[R][VEC], u[R][VEC], s[VEC];
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        a[r][j] = 1.f, u[r][j] = 0.f;
-        if (t0 + r < at.end) {
-          if (p.sigmoid) {
-            float b;
-            gate_of(pg[r].get(j), a[r][j], b);
-            u[r][j] = b * pv[r].get(j);
-          } else {
-            a[r][j] = pg[r].get(j), u[r][j] = pv[r].get(j);
-          }
-        }
+        terms(p.sigmoid, pg[r].get(j), a[r][j], u[r][j]);
+        u[r][j] *= pv[r].get(j);
       }
     if constexpr (SLOTS == 1) {
 #pragma unroll
@@ -390,6 +398,7 @@ __global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backwa
   T* gv = p.gv + at.o * p.gr_o + at.i0;
   T* gg = p.gg + at.o * p.gr_o + at.i0;
   const long long states = p.outer * p.inner;
+  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
   const int ch_last = at.ch_end > 0 ? (int)((at.ch_end - 1) / LC) : 0;     // the chunk of the sequence's last step
   float grad = SLOTS > 1 && at.keeper && p.g_last != nullptr ? p.g_last[at.ch] : 0.f;
 
@@ -400,8 +409,10 @@ __global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backwa
     Pack<T, VEC> pv[R], pg[R], pd[R];
     const T *lv = v + t0 * p.in_t, *lg = g + t0 * p.in_t, *ld = gh + t0 * p.inner;
 #pragma unroll
-    for (int r = 0; r < R; ++r, lv += p.in_t, lg += p.in_t, ld += p.inner)
+    for (int r = 0; r < R; ++r, lv += p.in_t, lg += p.in_t, ld += p.inner) {
       if (t0 + r < at.end) pv[r].load(lv), pg[r].load(lg), pd[r].load(ld);
+      else pv[r].fill(none_v), pg[r].fill(none_g), pd[r].fill(none_v);
+    }
     const bool active = at.keeper && c * LC < at.ch_end, mine = at.keeper && (active || c == 0);
     float before = 0.f;      // the state in front of the chunk: saved, or the sequence's own beginning
     if (SLOTS > 1 && mine) before = p.ckpt != nullptr ? p.ckpt[c * states + at.ch] : p.h0 != nullptr ? p.h0[at.ch] : 0.f;
@@ -410,16 +421,8 @@ __global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backwa
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        a[r][j] = 1.f, w[r][j] = 0.f;
-        if (t0 + r < at.end) {
-          if (p.sigmoid) {
-            float b;
-            gate_of(pg[r].get(j), a[r][j], b);
-            w[r][j] = b * pv[r].get(j);
-          } else {
-            a[r][j] = pg[r].get(j), w[r][j] = pv[r].get(j);
-          }
-        }
+        terms(p.sigmoid, pg[r].get(j), a[r][j], w[r][j]);
+        w[r][j] *= pv[r].get(j);
       }
     if constexpr (SLOTS == 1) {
 #pragma unroll
@@ -437,7 +440,7 @@ __global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backwa
           H = fmaf(a[r][j], H, w[r][j]);
         }
 #pragma unroll
-        for (int r = R - 1; r >= 0; --r) D = a[r][j] * (D + (t0 + r < at.end ? pd[r].get(j) : 0.f));
+        for (int r = R - 1; r >= 0; --r) D = a[r][j] * (D + pd[r].get(j));
         runs[at.slot][at.x * VEC + j] = make_float2(A, H);
         backs[at.slot][at.x * VEC + j] = D;
       }
@@ -491,15 +494,9 @@ __global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backwa
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float u = w[r][j];
-        if (t0 + r < at.end) {
-          if (p.sigmoid) {
-            float aa, b;
-            gate_of(pg[r].get(j), aa, b);
-            w[r][j] = (s[j] - pv[r].get(j)) * aa * b;
-          } else {
-            w[r][j] = s[j];
-          }
-        }
+        float aa, b;
+        terms(p.sigmoid, pg[r].get(j), aa, b);
+        w[r][j] = p.sigmoid ? (s[j] - pv[r].get(j)) * (a[r][j] * b) : s[j];
         s[j] = fmaf(a[r][j], s[j], u);
       }
     T *sv = gv + (t0 + R - 1) * p.gr_t, *sg = gg + (t0 + R - 1) * p.gr_t;
@@ -512,11 +509,8 @@ __global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backwa
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
           const float delta = d[j] + pd[r].get(j);
-          float b = 1.f;
-          if (p.sigmoid) {
-            float aa;
-            gate_of(pg[r].get(j), aa, b);
-          }
+          float aa, b;
+          terms(p.sigmoid, pg[r].get(j), aa, b);
           ov.put(j, delta * b);
           og.put(j, delta * w[r][j]);
           d[j] = a[r][j] * delta;
@@ -540,280 +534,375 @@ __global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backwa
 }
 
 // ------------------------------------------------------------------------------------------------ rows
-// [outer][L], the steps contiguous.  P neighbouring lanes share a row, 16 steps each; tiles come and go through
-// shared memory with one word of padding behind every 16 steps (a warp's lanes then walk their runs without bank
-// conflicts), the lanes' runs are joined by shuffles.  Global accesses are 16 bytes wide: a tile of whole rows is one
-// contiguous piece of memory, cut into vectors regardless of where rows begin.
-constexpr int kRowSteps = 16;
-constexpr int kRowPitch = kRowSteps + 1;
-constexpr int kTileFloats = kScanThreads * kRowPitch;
+// [outer][L], the steps contiguous, L >= 8.  A warp takes a unit of at most 512 neighbouring elements - whole rows, or a
+// chunk of a long one - in 16-byte vectors straight from global memory: K vectors a lane, the k-th at (32 k + lane) V.  Each
+// vector is composed in its lane, the lanes are joined by a warp scan that does not reach across a row's first step
+// (forward) or last step (backward), and the K scans are joined one after the other.  No shared memory, no barriers.
+// Where rows begin off a vector the unit starts at the vector before; the elements in front are left alone.
+constexpr int kUnit = 512, kRowWarps = 8;
 
-// A tile of `rows` rows of n steps, rows `stride` elements apart in memory.  WIDE: 16-byte accesses - the tile is one
-// contiguous piece, or its rows begin and end on vectors; element by element otherwise.
-template <typename T, int P, bool WIDE>
-struct RowTile {
-  static constexpr int V = 16 / (int)sizeof(T), N = kRowSteps / V;    // vectors per thread
-  uint32_t rows, n, magic;          // magic: division by n through the high word of a product (exact below 2^16)
-  __device__ __forceinline__ RowTile(uint32_t rows_, uint32_t n_) : rows(rows_), n(n_), magic(0xffffffffu / n_ + 1u) {}
-  __device__ __forceinline__ void split(uint32_t e, uint32_t& row, uint32_t& t) const {
-    row = n == 1 ? e : __umulhi(e, magic);
-    t = e - row * n;
-  }
-  static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t t) { return row * (P * kRowPitch) + t + t / kRowSteps; }
-  // global -> registers (WIDE; all loads of a tile are under way before the first is used)
-  __device__ __forceinline__ void fetch(Pack<T, V> (&r)[N], const T* base, long long stride) const {
-    if constexpr (WIDE) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        uint32_t row, t;
-        const uint32_t e = (threadIdx.x + k * kScanThreads) * V;
-        split(e, row, t);
-        const T* at = base + row * stride + t;
-        if (e + V <= rows * n) r[k].load(at);
-        else if (e < rows * n) r[k].load_part(at, (int)(rows * n - e));
-      }
+// steps of a chunk (a chunk of odd rows leaves room for a shifted beginning)
+__host__ __device__ constexpr int row_chunk(long long L) { return L % 8 == 0 ? kUnit : kUnit - 8; }
+
+enum RowMode { kWholeRows = 0, kWalk = 1, kChained = 2 };
+
+// Vector k of a unit: its first element's index (below 0 in front of the unit) and step, and the element that is a row's
+// first step (V: none; at most one, since L >= V).
+template <int V>
+struct RowVec {
+  int rel, t, spos;
+};
+
+template <typename T, bool WIDE, int MODE, bool RAGGED>
+struct RowUnit {
+  static constexpr int V = 16 / (int)sizeof(T), K = kUnit / 32 / V;
+  using Vec = RowVec<V>;
+  long long row0;       // first row
+  int n, t0, shift;     // elements; step of the first one; elements of its vector in front of it
+  int L, span;          // lanes that a row may reach across
+  uint32_t magic;       // division by L (whole rows: L <= 512, elements < 1024)
+  __device__ __forceinline__ Vec vec(int k, int& row) const {
+    Vec v;
+    v.rel = (k * 32 + (int)(threadIdx.x & 31)) * V - shift;
+    v.spos = V;
+    v.t = t0 + v.rel;
+    row = 0;
+    if (MODE == kWholeRows) {
+      row = v.rel > 0 ? (int)__umulhi((uint32_t)v.rel, magic) : 0;
+      v.t = v.rel - row * L;
+      const int s = v.t <= 0 ? -v.t : L - v.t;     // (it may lie behind the unit; nothing in the unit comes after it then)
+      if (s < V) v.spos = s;
     }
+    return v;
   }
-  // registers (or, element by element, global) -> shared memory
-  __device__ __forceinline__ void scatter(float* tile, const Pack<T, V> (&r)[N], const T* base, long long stride) const {
-    if constexpr (WIDE) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        uint32_t row, t;
-        split((threadIdx.x + k * kScanThreads) * V, row, t);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          if (row < rows) tile[place(row, t)] = r[k].get(i);
-          if (++t == n) t = 0, ++row;
-        }
-      }
+  // whether the last step of the vector's first row lies in the vector and in the unit
+  __device__ __forceinline__ bool ends(const Vec& v) const {
+    return MODE == kWholeRows && v.t >= 0 && L - v.t <= V && v.rel + (L - v.t) <= n;
+  }
+  __device__ __forceinline__ bool starts(const Vec& v) const { return MODE == kWholeRows && v.spos < V && v.rel + v.spos < n; }
+  __device__ __forceinline__ bool full(const Vec& v) const { return v.rel >= 0 && v.rel + V <= n; }
+  __device__ __forceinline__ bool on(const Vec& v, int i) const { return v.rel + i >= 0 && v.rel + i < n; }
+  // the vector's elements of a tensor whose unit begins at `base`; elements outside the unit become `none`.  Not WIDE: rows
+  // lie `stride` apart and vectors are loaded one by one.
+  __device__ __forceinline__ void load(Pack<T, V>& r, const Vec& v, int row, const T* base, long long stride, T none) const {
+    if (WIDE && full(v)) {
+      r.load(base + v.rel);
     } else {
-#pragma unroll 4
-      for (uint32_t e = threadIdx.x; e < rows * n; e += kScanThreads) {
-        uint32_t row, t;
-        split(e, row, t);
-        tile[place(row, t)] = Elem<T>::get(base[row * stride + t]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        r.v[i] = none;
+        if (on(v, i)) r.v[i] = base[WIDE ? v.rel + i : offset(v, row, i, stride)];
       }
     }
   }
-  __device__ __forceinline__ void store(T* base, const float* tile, long long stride) const {
-    if constexpr (WIDE) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        Pack<T, V> r;
-        uint32_t row, t;
-        const uint32_t e = (threadIdx.x + k * kScanThreads) * V;
-        split(e, row, t);
-        T* at = base + row * stride + t;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          if (row < rows) r.put(i, tile[place(row, t)]);
-          if (++t == n) t = 0, ++row;
-        }
-        if (e + V <= rows * n) r.store(at);
-        else if (e < rows * n) r.store_part(at, (int)(rows * n - e));
-      }
+  __device__ __forceinline__ void store(const Pack<T, V>& r, const Vec& v, int row, T* base, long long stride) const {
+    if (WIDE && full(v)) {
+      r.store(base + v.rel);
     } else {
-#pragma unroll 4
-      for (uint32_t e = threadIdx.x; e < rows * n; e += kScanThreads) {
-        uint32_t row, t;
-        split(e, row, t);
-        base[row * stride + t] = Elem<T>::put(tile[place(row, t)]);
-      }
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (on(v, i)) base[WIDE ? v.rel + i : offset(v, row, i, stride)] = r.v[i];
     }
+  }
+  __device__ __forceinline__ long long offset(const Vec& v, int row, int i, long long stride) const {
+    if (MODE != kWholeRows) return v.rel + i;
+    const bool next = v.t + i >= L;
+    return (row + (next ? 1 : 0)) * stride + (v.t + i - (next ? L : 0));
+  }
+  // RAGGED: which elements are steps of their sequences, as bits
+  __device__ __forceinline__ uint32_t steps(const Vec& v, int row, const int* lengths, long long end) const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) m |= on(v, i) ? 1u << i : 0u;
+    if (m == 0) return 0;
+    long long e0 = end, e1 = 0;
+    if (MODE == kWholeRows) e0 = lengths[row0 + row], e1 = v.t > 0 && starts(v) ? lengths[row0 + row + 1] : 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const bool next = MODE == kWholeRows && v.t + i >= L;
+      if (next ? v.t + i - L >= e1 : v.t + i >= e0) m &= ~(1u << i);
+    }
+    return m;
   }
 };
 
-template <typename T, int P, bool WIDE, bool CHAIN>
-__global__ void __launch_bounds__(kScanThreads, 3) scan_rows_kernel(const ScanArgs<T> p) {
-  constexpr int ROWS = kScanThreads / P, LC = P * kRowSteps;
-  using Tile = RowTile<T, P, WIDE>;
-  __shared__ float sv[kTileFloats], sg[kTileFloats];
-  __shared__ unsigned ticket[2];
-  pdl_trigger();
-  pdl_wait();
-  unsigned tag = 0, tile = blockIdx.x;
-  if (CHAIN) tile = take_ticket(p.ctrl, ticket, tag);
-  const int c_first = CHAIN ? (int)(tile / (unsigned)p.chains) : 0, c_end = CHAIN ? c_first + 1 : p.chunks;
-  const long long r0 = (long long)(CHAIN ? tile % (unsigned)p.chains : tile) * ROWS;
-  const int slot = threadIdx.x % P;
-  const long long row = r0 + threadIdx.x / P;
-  const uint32_t rows = (uint32_t)(p.outer - r0 < ROWS ? p.outer - r0 : ROWS);
-  const bool live = row < p.outer;
-  const long long end = live ? clamp_len(p.lengths, row, p.L) : 0;
-  float carry = live && p.h0 != nullptr ? p.h0[row] : 0.f;
-  float* mv = sv + threadIdx.x * kRowPitch;
-  float* mg = sg + threadIdx.x * kRowPitch;
-#pragma unroll 1
-  for (int c = c_first; c < c_end; ++c) {
-    const long long t0 = (long long)c * LC;
-    const Tile m(rows, (uint32_t)(p.L - t0 < LC ? p.L - t0 : LC));
-    {
-      const T *bv = p.v + r0 * p.in_o + t0, *bg = p.g + r0 * p.in_o + t0;
-      Pack<T, Tile::V> rv[Tile::N], rg[Tile::N];
-      m.fetch(rv, bv, p.in_o);
-      m.fetch(rg, bg, p.in_o);
-      m.scatter(sv, rv, bv, p.in_o);
-      m.scatter(sg, rg, bg, p.in_o);
-    }
-    __syncthreads();
-    float a[kRowSteps], u[kRowSteps], A = 1.f, H = 0.f;
-    const long long ts = t0 + slot * kRowSteps;
-    const int have = end - ts >= kRowSteps ? kRowSteps : end > ts ? (int)(end - ts) : 0;
+// Joins the lanes of one scan in which lanes of `marks` hold a summary that starts afresh: (A, H) of a lane becomes that of
+// all lanes from the nearest mark up to it.  No summary reaches across `span` lanes or more.
+template <bool UP>
+__device__ __forceinline__ bool segmented_scan(float& A, float& H, unsigned marks, int span) {
+  const int lane = threadIdx.x & 31;
+  const unsigned seen = UP ? marks & (0xffffffffu >> (31 - lane)) : marks & (0xffffffffu << lane);
+  const bool fresh = seen != 0;
+  const int room = UP ? (fresh ? lane - 31 + __clz(seen) : lane) : (fresh ? __ffs(seen) - 1 - lane : 31 - lane);
 #pragma unroll
-    for (int r = 0; r < kRowSteps; ++r) {
-      a[r] = 1.f, u[r] = 0.f;
-      if (r < have) {
-        if (p.sigmoid) {
-          float b;
-          gate_of(mg[r], a[r], b);
-          u[r] = b * mv[r];
-        } else {
-          a[r] = mg[r], u[r] = mv[r];
-        }
-      }
-      A *= a[r];
-      H = fmaf(a[r], H, u[r]);
-    }
-#pragma unroll
-    for (int k = 1; k < P; k *= 2) {
-      const float A1 = __shfl_up_sync(0xffffffffu, A, k, P), H1 = __shfl_up_sync(0xffffffffu, H, k, P);
-      if (slot >= k) H = fmaf(A, H1, H), A *= A1;
-    }
-    const long long at = (long long)c * p.outer + row;
-    // a warp holds one row where tiles are chained, so the row's lanes look back together
-    const bool active = t0 < end, more = t0 + LC < end;
-    if (CHAIN && active && c > 0) {
-      if (more && slot == P - 1) put_sum(p.sums + at, A, H, tag);
-      carry = look_back_warp(p.sums + at - p.outer, p.ends + at - p.outer, -p.outer, c, tag, p.status);
-    }
-    if (p.ckpt != nullptr && live && slot == 0 && (active || c == 0)) p.ckpt[at] = carry;
-    const float full = fmaf(A, carry, H);                  // the state behind this lane's run
-    float s = __shfl_up_sync(0xffffffffu, full, 1, P);
-    if (slot == 0) s = carry;
-    carry = __shfl_sync(0xffffffffu, full, P - 1, P);
-    if (CHAIN && more && slot == 0) put_end(p.ends + at, carry, tag);
-    if (live && slot == 0 && p.h_last != nullptr && ((active && !more) || (c == 0 && end == 0))) p.h_last[row] = carry;
-#pragma unroll
-    for (int r = 0; r < kRowSteps; ++r) {
-      s = fmaf(a[r], s, u[r]);
-      mv[r] = r < have ? s : 0.f;
-    }
-    __syncthreads();
-    m.store(p.h + r0 * p.L + t0, sv, p.L);
-    if (!CHAIN) __syncthreads();
+  for (int o = 1; o < 32; o *= 2) {
+    if (o >= span) break;
+    const float A1 = UP ? __shfl_up_sync(0xffffffffu, A, o) : __shfl_down_sync(0xffffffffu, A, o);
+    const float H1 = UP ? __shfl_up_sync(0xffffffffu, H, o) : __shfl_down_sync(0xffffffffu, H, o);
+    if (o <= room) H = fmaf(A, H1, H), A *= A1;
   }
-  if (CHAIN) leave_chain(p.ctrl, tag);
+  return fresh;
 }
 
-template <typename T, int P, bool WIDE, bool CHAIN>
-__global__ void __launch_bounds__(kScanThreads, 2) scan_rows_backward_kernel(const ScanArgs<T> p) {
-  constexpr int ROWS = kScanThreads / P, LC = P * kRowSteps;
-  using Tile = RowTile<T, P, WIDE>;
-  extern __shared__ float tiles[];
-  __shared__ unsigned ticket[2];
-  float* sv = tiles;
-  float* sg = sv + kTileFloats;
-  float* sd = sg + kTileFloats;
+// the unit of this warp; false if there is none.  `c` = its chunk, counted from the front.
+template <class U, typename T, int MODE, bool BACK>
+__device__ __forceinline__ bool first_unit(const ScanArgs<T>& p, U& u, int& c, unsigned& tag) {
+  const long long id = (long long)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+  u.L = (int)p.L;
+  u.magic = 0xffffffffu / (uint32_t)p.L + 1u;
+  u.span = MODE == kWholeRows ? (u.L + U::V - 2) / U::V + 1 : 32;
+  c = 0, tag = 0;
+  if (MODE == kWholeRows) {
+    u.row0 = id * p.groups;                       // groups: rows of a unit
+    if (u.row0 >= p.outer) return false;
+    u.n = (int)((p.outer - u.row0 < p.groups ? p.outer - u.row0 : p.groups) * p.L);
+    u.t0 = 0;
+  } else if (MODE == kWalk) {
+    if (id >= p.outer) return false;
+    u.row0 = id;
+    c = BACK ? p.chunks - 1 : 0;
+  } else {
+    if (id >= p.outer * p.chunks) return false;   // as many tickets as units
+    unsigned t = 0;
+    if ((threadIdx.x & 31) == 0) {
+      tag = *(volatile unsigned*)&p.ctrl->epoch + 1u;
+      t = atomicAdd(&p.ctrl->ticket, 1u);
+    }
+    tag = __shfl_sync(0xffffffffu, tag, 0);
+    t = __shfl_sync(0xffffffffu, t, 0);
+    u.row0 = t % (unsigned)p.outer;
+    c = (int)(t / (unsigned)p.outer);
+    if (BACK) c = p.chunks - 1 - c;
+  }
+  return true;
+}
+template <class U, typename T, int MODE>
+__device__ __forceinline__ void place_unit(const ScanArgs<T>& p, U& u, int c) {
+  if (MODE != kWholeRows) {
+    const int step = row_chunk(p.L);
+    u.t0 = c * step;
+    u.n = (int)(p.L - u.t0 < step ? p.L - u.t0 : step);
+  }
+  // rows that begin off a vector: only contiguous tensors are read wide then, all with the same shift
+  u.shift = p.L % U::V == 0 ? 0 : (int)((u.row0 * p.L + u.t0) % U::V);
+}
+template <typename T>
+__device__ __forceinline__ void leave_unit(const ScanArgs<T>& p, unsigned tag) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) {
+    __threadfence();
+    if (atomicAdd(&p.ctrl->done, 1u) == (unsigned)(p.outer * p.chunks) - 1u) {
+      p.ctrl->ticket = 0;
+      p.ctrl->done = 0;
+      p.ctrl->epoch = tag == 0xffffffffu ? 0u : tag;
+    }
+  }
+}
+
+template <typename T, bool WIDE, int MODE, bool RAGGED>
+__global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const ScanArgs<T> p) {
+  using U = RowUnit<T, WIDE, MODE, RAGGED>;
+  constexpr int V = U::V, K = U::K;
   pdl_trigger();
   pdl_wait();
-  unsigned tag = 0, tile = blockIdx.x;
-  if (CHAIN) tile = take_ticket(p.ctrl, ticket, tag);
-  const int n_first = CHAIN ? (int)(tile / (unsigned)p.chains) : 0, n_end = CHAIN ? n_first + 1 : p.chunks;
-  const long long r0 = (long long)(CHAIN ? tile % (unsigned)p.chains : tile) * ROWS;
-  const int slot = threadIdx.x % P;
-  const long long row = r0 + threadIdx.x / P;
-  const uint32_t rows = (uint32_t)(p.outer - r0 < ROWS ? p.outer - r0 : ROWS);
-  const bool live = row < p.outer;
-  const long long end = live ? clamp_len(p.lengths, row, p.L) : 0;
-  const int last = end > 0 ? (int)((end - 1) / LC) : 0;     // the chunk of the row's last step
-  float carry = live && p.g_last != nullptr ? p.g_last[row] : 0.f;
-  float* mv = sv + threadIdx.x * kRowPitch;
-  float* mg = sg + threadIdx.x * kRowPitch;
-  float* md = sd + threadIdx.x * kRowPitch;
+  const int lane = threadIdx.x & 31;
+  U u;
+  int c;
+  unsigned tag;
+  if (!first_unit<U, T, MODE, false>(p, u, c, tag)) return;
+  const long long end = MODE == kWholeRows ? p.L : clamp_len(p.lengths, u.row0, p.L);
+  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
+  float carry = 0.f;
+  if (MODE != kWholeRows && c == 0 && p.h0 != nullptr) carry = p.h0[u.row0];
 #pragma unroll 1
-  for (int k0 = n_first; k0 < n_end; ++k0) {
-    const int c = p.chunks - 1 - k0;
-    const long long t0 = (long long)c * LC;
-    const Tile m(rows, (uint32_t)(p.L - t0 < LC ? p.L - t0 : LC));
-    {
-      const T *bv = p.v + r0 * p.in_o + t0, *bg = p.g + r0 * p.in_o + t0, *bd = p.gh + r0 * p.L + t0;
-      Pack<T, Tile::V> rv[Tile::N], rg[Tile::N], rd[Tile::N];
-      m.fetch(rv, bv, p.in_o);
-      m.fetch(rg, bg, p.in_o);
-      m.fetch(rd, bd, p.L);
-      m.scatter(sv, rv, bv, p.in_o);
-      m.scatter(sg, rg, bg, p.in_o);
-      m.scatter(sd, rd, bd, p.L);
-    }
-    const float* before = p.ckpt != nullptr ? p.ckpt + (long long)c * p.outer : p.h0;
-    const bool active = t0 < end;
-    const float start = live && before != nullptr && (active || c == 0) ? before[row] : 0.f;
-    __syncthreads();
-    float a[kRowSteps], w[kRowSteps], A = 1.f, H = 0.f, D = 0.f;
-    const long long ts = t0 + slot * kRowSteps;
-    const int have = end - ts >= kRowSteps ? kRowSteps : end > ts ? (int)(end - ts) : 0;
+  for (;; ++c) {
+    place_unit<U, T, MODE>(p, u, c);
+    typename U::Vec x[K];
+    int row[K];
+    Pack<T, V> pv[K], pg[K];
+    float h0v[K];
+    uint32_t live[K];
 #pragma unroll
-    for (int r = 0; r < kRowSteps; ++r) {
-      a[r] = 1.f, w[r] = 0.f;
-      if (r < have) {
-        if (p.sigmoid) {
-          float b;
-          gate_of(mg[r], a[r], b);
-          w[r] = b * mv[r];
-          mg[r] = b;
-        } else {
-          a[r] = mg[r], w[r] = mv[r];
-          mg[r] = 1.f;
-        }
+    for (int k = 0; k < K; ++k) {
+      x[k] = u.vec(k, row[k]);
+      u.load(pv[k], x[k], row[k], p.v + u.row0 * p.in_o + u.t0, p.in_o, none_v);
+      u.load(pg[k], x[k], row[k], p.g + u.row0 * p.in_o + u.t0, p.in_o, none_g);
+      h0v[k] = 0.f;
+      if (u.starts(x[k]) && p.h0 != nullptr) h0v[k] = p.h0[u.row0 + row[k] + (x[k].t > 0 ? 1 : 0)];
+      if (RAGGED) live[k] = u.steps(x[k], row[k], p.lengths, end);
+    }
+    float a[K][V], b[K][V], A[K], H[K];
+    bool fresh[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      A[k] = 1.f, H[k] = 0.f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (RAGGED && !(live[k] >> i & 1u)) pv[k].v[i] = none_v, pg[k].v[i] = none_g;
+        terms(p.sigmoid, pg[k].get(i), a[k][i], b[k][i]);
+        b[k][i] *= pv[k].get(i);
+        if (MODE == kWholeRows && i == x[k].spos) H[k] = h0v[k];
+        A[k] *= a[k][i];
+        H[k] = fmaf(a[k][i], H[k], b[k][i]);
       }
-      A *= a[r];
-      H = fmaf(a[r], H, w[r]);
+      fresh[k] = segmented_scan<true>(A[k], H[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, x[k].spos < V) : 0u, u.span);
     }
+    const bool active = MODE == kWholeRows || u.t0 < end, more = MODE != kWholeRows && u.t0 + u.n < end;
+    const long long at = (long long)c * p.outer + u.row0;
+    if (MODE == kChained && active && c > 0) {
+      if (more) {           // the whole chunk's summary, the vectors joined in order
+        float tA = 1.f, tH = 0.f;
 #pragma unroll
-    for (int r = kRowSteps - 1; r >= 0; --r) D = a[r] * (D + (r < have ? md[r] : 0.f));
-    float Af = A, Ab = A;
-#pragma unroll
-    for (int k = 1; k < P; k *= 2) {
-      const float A1 = __shfl_up_sync(0xffffffffu, Af, k, P), H1 = __shfl_up_sync(0xffffffffu, H, k, P);
-      const float A2 = __shfl_down_sync(0xffffffffu, Ab, k, P), D2 = __shfl_down_sync(0xffffffffu, D, k, P);
-      if (slot >= k) H = fmaf(Af, H1, H), Af *= A1;
-      if (slot + k < P) D = fmaf(Ab, D2, D), Ab *= A2;
+        for (int k = 0; k < K; ++k) tH = fmaf(A[k], tH, H[k]), tA *= A[k];
+        if (lane == 31) put_sum(p.sums + at, tA, tH, tag);
+      }
+      carry = look_back_warp(p.sums + at - p.outer, p.ends + at - p.outer, -p.outer, c, tag, p.status);
     }
-    const long long at = (long long)c * p.outer + row;
-    if (CHAIN && active && c < last) {
-      if (c > 0 && slot == 0) put_sum(p.sums + at, Ab, D, tag);
+    if (MODE != kWholeRows && p.ckpt != nullptr && lane == 0 && (active || c == 0)) p.ckpt[at] = carry;
+    float in[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const float s = fresh[k] ? H[k] : fmaf(A[k], carry, H[k]);
+      in[k] = __shfl_up_sync(0xffffffffu, s, 1);
+      if (lane == 0) in[k] = carry;
+      carry = __shfl_sync(0xffffffffu, s, 31);
+    }
+    if (MODE == kChained && more && lane == 0) put_end(p.ends + at, carry, tag);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float s = in[k], last = 0.f;
+      Pack<T, V> out;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (MODE == kWholeRows && i == x[k].spos) last = s, s = h0v[k];
+        s = fmaf(a[k][i], s, b[k][i]);
+        out.put(i, !RAGGED || (live[k] >> i & 1u) ? s : 0.f);
+      }
+      u.store(out, x[k], row[k], p.h + u.row0 * p.L + u.t0, p.L);
+      if (p.h_last != nullptr && u.ends(x[k])) p.h_last[u.row0 + row[k]] = u.L - x[k].t == V ? s : last;
+    }
+    if (MODE != kWholeRows && lane == 0 && p.h_last != nullptr && ((active && !more) || (c == 0 && end == 0))) p.h_last[u.row0] = carry;
+    if (MODE != kWalk || c + 1 == p.chunks) break;
+  }
+  if (MODE == kChained) leave_unit(p, tag);
+}
+
+template <typename T, bool WIDE, int MODE, bool RAGGED>
+__global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(const ScanArgs<T> p) {
+  using U = RowUnit<T, WIDE, MODE, RAGGED>;
+  constexpr int V = U::V, K = U::K;
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  U u;
+  int c;
+  unsigned tag;
+  if (!first_unit<U, T, MODE, true>(p, u, c, tag)) return;
+  const long long end = MODE == kWholeRows ? p.L : clamp_len(p.lengths, u.row0, p.L);
+  const int last = end > 0 ? (int)((end - 1) / row_chunk(p.L)) : 0;      // the chunk of the row's last step
+  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
+  float carry = 0.f;
+  if (MODE != kWholeRows && p.g_last != nullptr) carry = p.g_last[u.row0];
+#pragma unroll 1
+  for (;; --c) {
+    place_unit<U, T, MODE>(p, u, c);
+    typename U::Vec x[K];
+    int row[K];
+    Pack<T, V> pv[K], pg[K], pd[K];
+    float h0v[K], glv[K];
+    uint32_t live[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      x[k] = u.vec(k, row[k]);
+      u.load(pv[k], x[k], row[k], p.v + u.row0 * p.in_o + u.t0, p.in_o, none_v);
+      u.load(pg[k], x[k], row[k], p.g + u.row0 * p.in_o + u.t0, p.in_o, none_g);
+      u.load(pd[k], x[k], row[k], p.gh + u.row0 * p.L + u.t0, p.L, none_v);
+      h0v[k] = glv[k] = 0.f;
+      if (u.starts(x[k]) && p.h0 != nullptr) h0v[k] = p.h0[u.row0 + row[k] + (x[k].t > 0 ? 1 : 0)];
+      if (u.ends(x[k]) && p.g_last != nullptr) glv[k] = p.g_last[u.row0 + row[k]];
+      if (RAGGED) live[k] = u.steps(x[k], row[k], p.lengths, end);
+    }
+    const bool active = MODE == kWholeRows || u.t0 < end;
+    const long long at = (long long)c * p.outer + u.row0;
+    float start = 0.f;            // the state in front of the chunk: saved, or the row's own beginning
+    if (MODE != kWholeRows && (active || c == 0)) start = p.ckpt != nullptr ? p.ckpt[at] : p.h0 != nullptr ? p.h0[u.row0] : 0.f;
+    float a[K][V], b[K][V], A[K], H[K], B[K], D[K];
+    bool fresh_up[K], fresh_down[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      A[k] = 1.f, H[k] = 0.f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (RAGGED && !(live[k] >> i & 1u)) pv[k].v[i] = none_v, pg[k].v[i] = none_g, pd[k].v[i] = none_v;
+        terms(p.sigmoid, pg[k].get(i), a[k][i], b[k][i]);
+        if (MODE == kWholeRows && i == x[k].spos) H[k] = h0v[k];
+        A[k] *= a[k][i];
+        H[k] = fmaf(a[k][i], H[k], b[k][i] * pv[k].get(i));
+      }
+      D[k] = glv[k];             // (0, or a row's end at the vector's)
+#pragma unroll
+      for (int i = V - 1; i >= 0; --i) {
+        D[k] = a[k][i] * (D[k] + pd[k].get(i));
+        if (MODE == kWholeRows && i == x[k].spos) D[k] = glv[k];
+      }
+      B[k] = A[k];
+      fresh_up[k] = segmented_scan<true>(A[k], H[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, x[k].spos < V) : 0u, u.span);
+      fresh_down[k] = segmented_scan<false>(B[k], D[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, u.ends(x[k])) : 0u, u.span);
+    }
+    if (MODE == kChained && active && c < last) {
+      if (c > 0) {
+        float tA = 1.f, tD = 0.f;
+#pragma unroll
+        for (int k = K - 1; k >= 0; --k) tD = fmaf(B[k], tD, D[k]), tA *= B[k];
+        if (lane == 0) put_sum(p.sums + at, tA, tD, tag);
+      }
       carry = look_back_warp(p.sums + at + p.outer, p.ends + at + p.outer, p.outer, last - c, tag, p.status);
     }
-    float s = __shfl_up_sync(0xffffffffu, fmaf(Af, start, H), 1, P);
-    if (slot == 0) s = start;
-    const float all = fmaf(Ab, carry, D);
-    float d = __shfl_down_sync(0xffffffffu, all, 1, P);
-    if (slot == P - 1) d = carry;
-    carry = __shfl_sync(0xffffffffu, all, 0, P);
-    if (CHAIN && active && c > 0 && slot == 0) put_end(p.ends + at, carry, tag);
-    if (c == 0 && live && slot == 0 && p.gh0 != nullptr) p.gh0[row] = carry;
-    // forward once more: u is replaced by what delta is multiplied with for the gate's gradient
+    float in[K], din[K];
 #pragma unroll
-    for (int r = 0; r < kRowSteps; ++r) {
-      const float u = w[r];
-      if (r < have) w[r] = p.sigmoid ? (s - mv[r]) * a[r] * mg[r] : s;
-      s = fmaf(a[r], s, u);
+    for (int k = 0; k < K; ++k) {
+      const float s = fresh_up[k] ? H[k] : fmaf(A[k], start, H[k]);
+      in[k] = __shfl_up_sync(0xffffffffu, s, 1);
+      if (lane == 0) in[k] = start;
+      start = __shfl_sync(0xffffffffu, s, 31);
     }
 #pragma unroll
-    for (int r = kRowSteps - 1; r >= 0; --r) {
-      const bool on = r < have;
-      const float delta = d + (on ? md[r] : 0.f);
-      mv[r] = on ? delta * mg[r] : 0.f;
-      mg[r] = on ? delta * w[r] : 0.f;
-      d = a[r] * delta;
+    for (int k = K - 1; k >= 0; --k) {
+      const float d = fresh_down[k] ? D[k] : fmaf(B[k], carry, D[k]);
+      din[k] = __shfl_down_sync(0xffffffffu, d, 1);
+      if (lane == 31) din[k] = carry;
+      carry = __shfl_sync(0xffffffffu, d, 0);
     }
-    __syncthreads();
-    m.store(p.gv + r0 * p.gr_o + t0, sv, p.gr_o);
-    m.store(p.gg + r0 * p.gr_o + t0, sg, p.gr_o);
-    if (!CHAIN) __syncthreads();
+    if (MODE == kChained && active && c > 0 && lane == 0) put_end(p.ends + at, carry, tag);
+    if (MODE != kWholeRows && c == 0 && lane == 0 && p.gh0 != nullptr) p.gh0[u.row0] = carry;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float w[V], s = in[k], g0 = 0.f;
+      float d = u.ends(x[k]) && u.L - x[k].t == V ? glv[k] : din[k];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {       // what delta is multiplied with for the gate's gradient
+        if (MODE == kWholeRows && i == x[k].spos) s = h0v[k];
+        const float v = pv[k].get(i);
+        w[i] = p.sigmoid ? (s - v) * (a[k][i] * b[k][i]) : s;
+        s = fmaf(a[k][i], s, b[k][i] * v);
+      }
+      Pack<T, V> ov, og;
+#pragma unroll
+      for (int i = V - 1; i >= 0; --i) {
+        const bool step = !RAGGED || (live[k] >> i & 1u);
+        const float delta = d + pd[k].get(i);
+        ov.put(i, step ? delta * b[k][i] : 0.f);
+        og.put(i, step ? delta * w[i] : 0.f);
+        d = a[k][i] * delta;
+        if (MODE == kWholeRows && i == x[k].spos) g0 = d, d = glv[k];
+      }
+      u.store(ov, x[k], row[k], p.gv + u.row0 * p.gr_o + u.t0, p.gr_o);
+      u.store(og, x[k], row[k], p.gg + u.row0 * p.gr_o + u.t0, p.gr_o);
+      if (u.starts(x[k]) && p.gh0 != nullptr) p.gh0[u.row0 + row[k] + (x[k].t > 0 ? 1 : 0)] = g0;
+    }
+    if (MODE != kWalk || c == 0) break;
   }
-  if (CHAIN) leave_chain(p.ctrl, tag);
+  if (MODE == kChained) leave_unit(p, tag);
 }
 
 // length 0: the state passes through
@@ -827,14 +916,10 @@ __global__ void __launch_bounds__(256) scan_copy_kernel(const float* __restrict_
 // bytes in front of the chain's entries: status word, then its control words
 constexpr size_t kChainHead = kStatusBytes + 256;
 
-int row_lanes(long long length) {
-  int P = 1;
-  while (P < 32 && P * kRowSteps < length) P *= 2;
-  return P;
-}
-
 // Whether the chunks of a sequence become chained tiles (true) or a CTA walks through them (false): see the rule below.
-bool chained(long long chains, long long chunks) { return chunks > 1 && chains * chunks <= 0x7fffffff && chains < 4 * (long long)num_sms(); }
+bool chained(long long ctas, long long chunks, long long tiles) {
+  return chunks > 1 && tiles <= 0x7fffffff && ctas < 4 * (long long)num_sms();
+}
 
 template <typename T>
 void chain(ScanArgs<T>& p, const ScanCall& c) {
@@ -852,7 +937,7 @@ cudaError_t launch_cols(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
   const dim3 block(S::THREADS);
   // only the longest tiles ever come in several
   if constexpr (S::LC >= kSave) {
-    if (chained(p.chains, p.chunks)) {
+    if (chained(p.chains, p.chunks, p.chains * p.chunks)) {
       chain(p, c);
       const dim3 grid((unsigned)(p.chains * p.chunks));
       if constexpr (BACK) return launch_pdl(scan_cols_backward_kernel<T, S, true>, grid, block, 0, st, p);
@@ -864,33 +949,45 @@ cudaError_t launch_cols(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
   else return launch_pdl(scan_cols_kernel<T, S, false>, grid, block, 0, st, p);
 }
 
-template <typename T, int P, bool WIDE, bool CHAIN, bool BACK>
-cudaError_t launch_rows_kernel(const ScanArgs<T>& p, long long tiles, cudaStream_t st) {
-  const dim3 grid((unsigned)tiles), block(kScanThreads);
-  if constexpr (!BACK) return launch_pdl(scan_rows_kernel<T, P, WIDE, CHAIN>, grid, block, 0, st, p);
-  constexpr int smem = 3 * (int)sizeof(float) * kTileFloats;
-  cudaError_t e = cudaFuncSetAttribute(scan_rows_backward_kernel<T, P, WIDE, CHAIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  return e != cudaSuccess ? e : launch_pdl(scan_rows_backward_kernel<T, P, WIDE, CHAIN>, grid, block, smem, st, p);
+template <typename T, bool WIDE, int MODE, bool BACK>
+cudaError_t launch_rows_kernel(const ScanArgs<T>& p, long long units, cudaStream_t st) {
+  const dim3 grid((unsigned)((units + kRowWarps - 1) / kRowWarps)), block(32 * kRowWarps);
+  if constexpr (BACK)
+    return p.lengths != nullptr ? launch_pdl(scan_rows_backward_kernel<T, WIDE, MODE, true>, grid, block, 0, st, p)
+                                : launch_pdl(scan_rows_backward_kernel<T, WIDE, MODE, false>, grid, block, 0, st, p);
+  else
+    return p.lengths != nullptr ? launch_pdl(scan_rows_kernel<T, WIDE, MODE, true>, grid, block, 0, st, p)
+                                : launch_pdl(scan_rows_kernel<T, WIDE, MODE, false>, grid, block, 0, st, p);
 }
 
-template <typename T, int P, bool BACK>
+template <typename T, bool BACK>
 cudaError_t launch_rows(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
   constexpr int V = 16 / (int)sizeof(T);
-  p.chains = (p.outer + kScanThreads / P - 1) / (kScanThreads / P);
-  p.chunks = (int)((p.L + P * kRowSteps - 1) / (P * kRowSteps));
-  auto wide = [&](const void* base, long long stride) {   // tiles begin at multiples of 8 rows, chunks at multiples of 512 steps
-    return base == nullptr || (aligned_to(base, 16) && ((p.chunks == 1 && stride == p.L) || (p.L % V == 0 && stride % V == 0)));
+  const int step = row_chunk(p.L);
+  p.chunks = (int)((p.L + step - 1) / step);
+  // one vector grid for all tensors: contiguous rows, or (a chunk is part of one row) rows that begin on vectors
+  auto wide = [&](const void* base, long long stride) {
+    return base == nullptr || (aligned_to(base, 16) && (stride == p.L || (p.chunks > 1 && p.L % V == 0 && stride % V == 0)));
   };
   const bool w = wide(c.v, c.in_outer) && wide(c.g, c.in_outer) && wide(c.h, p.L) && wide(c.grad_h, p.L) &&
                  wide(c.grad_v, c.grad_outer) && wide(c.grad_g, c.grad_outer);
-  if constexpr (P == 32) {
-    if (chained(p.chains, p.chunks)) {
-      chain(p, c);
-      return w ? launch_rows_kernel<T, P, true, true, BACK>(p, p.chains * p.chunks, st)
-               : launch_rows_kernel<T, P, false, true, BACK>(p, p.chains * p.chunks, st);
-    }
+  if (p.chunks == 1) {
+    // rows of a unit: as many as fit, and units that begin and end on vectors where that many are a multiple
+    p.groups = (p.L % 8 == 0 ? kUnit : kUnit - 8) / p.L;
+    for (long long m = V; m > 1; m /= 2)
+      if (p.groups >= m && p.L % m != 0) {
+        p.groups -= p.groups % m;
+        break;
+      }
+    const long long units = (p.outer + p.groups - 1) / p.groups;
+    return w ? launch_rows_kernel<T, true, kWholeRows, BACK>(p, units, st) : launch_rows_kernel<T, false, kWholeRows, BACK>(p, units, st);
   }
-  return w ? launch_rows_kernel<T, P, true, false, BACK>(p, p.chains, st) : launch_rows_kernel<T, P, false, false, BACK>(p, p.chains, st);
+  if (chained((p.outer + kRowWarps - 1) / kRowWarps, p.chunks, p.outer * p.chunks)) {
+    chain(p, c);
+    return w ? launch_rows_kernel<T, true, kChained, BACK>(p, p.outer * p.chunks, st)
+             : launch_rows_kernel<T, false, kChained, BACK>(p, p.outer * p.chunks, st);
+  }
+  return w ? launch_rows_kernel<T, true, kWalk, BACK>(p, p.outer, st) : launch_rows_kernel<T, false, kWalk, BACK>(p, p.outer, st);
 }
 
 template <typename T, bool BACK>
@@ -903,16 +1000,7 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   p.outer = c.outer, p.L = c.length, p.inner = c.inner;
   p.in_o = c.in_outer, p.in_t = c.in_step, p.gr_o = c.grad_outer, p.gr_t = c.grad_step;
   p.sigmoid = c.gate == DTST_GATE_SIGMOID;
-  if (c.inner == 1) {
-    switch (row_lanes(c.length)) {
-      case 1: return launch_rows<T, 1, BACK>(p, c, st);
-      case 2: return launch_rows<T, 2, BACK>(p, c, st);
-      case 4: return launch_rows<T, 4, BACK>(p, c, st);
-      case 8: return launch_rows<T, 8, BACK>(p, c, st);
-      case 16: return launch_rows<T, 16, BACK>(p, c, st);
-      default: return launch_rows<T, 32, BACK>(p, c, st);
-    }
-  }
+  if (c.inner == 1 && c.length >= 8) return launch_rows<T, BACK>(p, c, st);
   const size_t need = 4 * sizeof(T);
   bool vec = c.inner % 4 == 0 && c.in_outer % 4 == 0 && c.in_step % 4 == 0 && aligned_to(c.v, need) && aligned_to(c.g, need);
   if (BACK) vec = vec && c.grad_outer % 4 == 0 && c.grad_step % 4 == 0 && aligned_to(c.grad_h, need) && aligned_to(c.grad_v, need) && aligned_to(c.grad_g, need);
@@ -932,10 +1020,10 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
 
 }  // namespace
 
-// States are saved every 64 steps of [outer][L][inner] sequences, every 512 of contiguous ones - or once, in front of a
-// sequence that fits one tile.
+// States are saved every 64 steps of [outer][L][inner] sequences, every 512 (or 504) of contiguous ones - or once, in
+// front of a sequence that fits one tile.
 long long scan_chunk(int, long long length, long long inner) {
-  const long long lc = inner == 1 ? kRowSteps * row_lanes(length) : kSave;
+  const long long lc = inner == 1 ? row_chunk(length) : kSave;
   return length <= lc ? (length < 1 ? 1 : length) : lc;
 }
 

@@ -63,6 +63,10 @@ struct Pack {
   }
   __device__ __forceinline__ float get(int i) const { return Elem<T>::get(v[i]); }
   __device__ __forceinline__ void put(int i, float x) { v[i] = Elem<T>::put(x); }
+  __device__ __forceinline__ void fill(T x) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = x;
+  }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = Elem<T>::put(0.f);

@@ -235,6 +235,8 @@ SCAN_SHAPES = [
     (1, 1000, 7), (2, 513, 260), (40, 5, 3), (1, 2500, 64),
     (1, 1, 1), (7, 1, 1), (300, 2, 1), (1000, 16, 1), (515, 17, 1), (1000, 30, 1), (130, 64, 1), (70, 100, 1), (33, 512, 1),
     (9, 513, 1), (3, 2000, 1),
+    (50, 7, 1), (200, 8, 1), (131, 9, 1), (64, 15, 1), (20, 127, 1), (11, 255, 1), (5, 504, 1), (5, 505, 1), (4, 511, 1),
+    (3, 1016, 1), (2, 1009, 1), (1, 9001, 1), (2, 3000, 20), (1, 4099, 3),
 ]
 
 

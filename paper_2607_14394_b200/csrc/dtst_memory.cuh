@@ -1,9 +1,24 @@
 // Launchers of the recurrent-memory operators (arguments already checked by the C entry points).
 #pragma once
 
+#include <atomic>
+
 #include "dtst_common.cuh"
 
 namespace dtst {
+
+// Lets a kernel have `bytes` of shared memory, once per device and kernel (`seen`: a bit per device, kept by the caller's
+// static of that kernel; a racing second call sets the same value).
+inline cudaError_t allow_smem(const void* kern, size_t bytes, std::atomic<uint64_t>& seen) {
+  if (bytes <= 48 * 1024) return cudaSuccess;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 64 && (seen.load(std::memory_order_relaxed) >> dev & 1u)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess && dev < 64) seen.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return e;
+}
 
 constexpr int kNormParts = 592;           // most CTAs (and rows of partial sums) of a norm's backward pass: 4 per SM
 constexpr int kNormFieldChannels = 128;   // most channels a channels-first norm holds in registers

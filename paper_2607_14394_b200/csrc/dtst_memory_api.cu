@@ -41,7 +41,7 @@ dtst_status check_scan(const dtst_scan_desc* d) {
         !small_product(d->grad_stride[k], k == 0 ? d->outer : d->length, 1))
       return DTST_ERR_INVALID_ARG;
   if (d->inner == 1 && d->length > 1 && (d->in_stride[1] != 1 || d->grad_stride[1] != 1)) return DTST_ERR_INVALID_ARG;
-  if (d->length > ((int64_t)1 << 30) || d->outer * d->inner > ((int64_t)1 << 33)) return DTST_ERR_UNSUPPORTED;
+  if (d->length > ((int64_t)1 << 30) || d->inner > ((int64_t)1 << 30) || d->outer * d->inner > ((int64_t)1 << 33)) return DTST_ERR_UNSUPPORTED;
   return DTST_OK;
 }
 

@@ -29,7 +29,7 @@ constexpr int kScanThreads = 256;
 struct ChainCtrl {
   unsigned ticket, done, epoch;
 };
-constexpr uint32_t kChainPolls = 1u << 20;
+constexpr uint32_t kChainPolls = 1u << 18;
 
 __device__ __forceinline__ unsigned long long tagged(float v, unsigned tag) {
   return (unsigned long long)tag << 32 | __float_as_uint(v);
@@ -53,62 +53,55 @@ __device__ __forceinline__ unsigned long long get_end(const unsigned long long* 
 __device__ __forceinline__ float value_of(unsigned long long w) { return __uint_as_float((uint32_t)w); }
 __device__ __forceinline__ bool has_tag(unsigned long long w, unsigned tag) { return (unsigned)(w >> 32) == tag; }
 
-// State in front of a chunk for CPW channels of a warp; lane = depth group * CPW + channel.  `want`: this lane's channel
-// asks; `n` chunks precede it, `sum` / `end` point at the nearest one's entries, `stride` entries further lies the one
-// before that.  kLook chunks are read at once, spread over the depth groups.
-template <int CPW, int kLook>
-__device__ __forceinline__ float look_back(bool want, const ulonglong2* sum, const unsigned long long* end, long long stride,
-                                           int n, unsigned tag, int* status) {
-  constexpr int DG = 32 / CPW, NI = kLook / DG;
-  const int depth = (threadIdx.x & 31) / CPW, ch = (threadIdx.x & 31) % CPW;
-  float result = 0.f;
-  bool open = want;
+// Which earlier chunk to start from, by one warp: lane k looks at the hint of the k-th tile back (`hint` = the nearest
+// one's, `stride` entries between them, `n` of them).  A hint is written when (most of) a tile's entries have been:
+// kind 1 = its summary, 2 = its end state; the reader of the entries still checks their tags.  -1: gave up.
+__device__ __forceinline__ int poll_hints(const unsigned long long* hint, long long stride, int n, unsigned tag) {
+  const int lane = threadIdx.x & 31;
   for (uint32_t poll = 0; poll < kChainPolls; ++poll) {
-    unsigned long long e[NI];
-    ulonglong2 q[NI];
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int k = depth + DG * i;
-      e[i] = 0, q[i] = make_ulonglong2(0, 0);
-      if (open && k < n) {
-        e[i] = get_end(end + k * stride);
-        q[i] = get_sum(sum + k * stride);
-      }
-    }
-    int found = kLook, gap = kLook;       // the nearest chunk with an end state, and without a summary
-    float s = 0.f;
-#pragma unroll
-    for (int i = NI - 1; i >= 0; --i) {
-      if (open && has_tag(e[i], tag)) found = depth + DG * i, s = value_of(e[i]);
-      if (!(has_tag(q[i].x, tag) && has_tag(q[i].y, tag))) gap = depth + DG * i;
-    }
-    const int mine = found;
-#pragma unroll
-    for (int o = CPW; o < 32; o *= 2) {
-      found = min(found, __shfl_xor_sync(0xffffffffu, found, o));
-      gap = min(gap, __shfl_xor_sync(0xffffffffu, gap, o));
-    }
-    const unsigned has = __ballot_sync(0xffffffffu, mine == found);
-    // the lane of this channel that holds the end state
-    unsigned of_ch = 0;
-#pragma unroll
-    for (int d = 0; d < DG; ++d) of_ch |= has & (1u << (d * CPW + ch));
-    s = __shfl_sync(0xffffffffu, s, of_ch != 0 ? __ffs(of_ch) - 1 : 0);
-#pragma unroll
-    for (int k = kLook - 1; k >= 0; --k) {
-      const float A = __shfl_sync(0xffffffffu, value_of(q[k / DG].x), (k % DG) * CPW + ch);
-      const float H = __shfl_sync(0xffffffffu, value_of(q[k / DG].y), (k % DG) * CPW + ch);
-      if (k < found) s = fmaf(A, s, H);
-    }
-    if (open && found < kLook && gap >= found) {
-      result = s;
-      open = false;
-    }
-    if (!__any_sync(0xffffffffu, open)) return result;
+    const unsigned long long w = lane < n ? get_end(hint + lane * stride) : 0ull;
+    const bool mine = has_tag(w, tag);
+    const unsigned ends = __ballot_sync(0xffffffffu, mine && (unsigned)w == 2u), any = __ballot_sync(0xffffffffu, mine);
+    const int found = __ffs(ends) - 1;
+    if (found >= 0 && (any & ((1u << found) - 1u)) == (1u << found) - 1u) return found;
     __nanosleep(20);
   }
-  if (open) atomicExch(status, 1);
-  return result;
+  return -1;
+}
+__device__ __forceinline__ void put_hint(unsigned long long* at, unsigned kind, unsigned tag) { put_end(at, __uint_as_float(kind), tag); }
+
+// State in front of a chunk for CPW channels of a warp, from the end state `found` (< 32, the same for the whole warp) chunks
+// further back than the nearest one and the summaries in between; lane = depth group * CPW + channel.  `want`: this lane's
+// channel exists; `sum` / `end` point at the nearest chunk's entries, `stride` entries further lies the one before that.
+template <int CPW>
+__device__ __forceinline__ float look_back(bool want, const ulonglong2* sum, const unsigned long long* end, long long stride,
+                                           int found, unsigned tag, int* status) {
+  constexpr int DG = 32 / CPW;
+  const int depth = (threadIdx.x & 31) / CPW, ch = (threadIdx.x & 31) % CPW;
+  float s = 0.f;
+  bool ok = !want;
+  for (uint32_t poll = 0; poll < kChainPolls && !ok; ++poll) {
+    const unsigned long long e = get_end(end + found * stride);
+    ok = has_tag(e, tag);
+    s = value_of(e);
+  }
+  if (!ok) atomicExch(status, 1);
+  for (int k0 = found - 1; k0 >= 0; k0 -= DG) {       // the farthest first, DG at once
+    const int k = k0 - depth;
+    float A = 1.f, H = 0.f;
+    ok = !want || k < 0;
+    for (uint32_t poll = 0; poll < kChainPolls && !ok; ++poll) {
+      const ulonglong2 q = get_sum(sum + k * stride);
+      ok = has_tag(q.x, tag) && has_tag(q.y, tag);
+      A = value_of(q.x), H = value_of(q.y);
+    }
+    if (!ok) atomicExch(status, 1);
+    __syncwarp();
+    const int n = k0 + 1 < DG ? k0 + 1 : DG;
+    for (int d = 0; d < n; ++d)
+      s = fmaf(__shfl_sync(0xffffffffu, A, d * CPW + ch), s, __shfl_sync(0xffffffffu, H, d * CPW + ch));
+  }
+  return s;
 }
 
 // The same by a whole warp for one sequence: lane k looks at the k-th chunk back.
@@ -137,16 +130,6 @@ __device__ __forceinline__ float look_back_warp(const ulonglong2* sum, const uns
   return 0.f;
 }
 
-// takes a ticket; all threads of the CTA get (tile, tag)
-__device__ __forceinline__ unsigned take_ticket(ChainCtrl* ctrl, unsigned* shared2, unsigned& tag) {
-  if (threadIdx.x == 0) {
-    shared2[1] = *(volatile unsigned*)&ctrl->epoch + 1u;
-    shared2[0] = atomicAdd(&ctrl->ticket, 1u);
-  }
-  __syncthreads();
-  tag = shared2[1];
-  return shared2[0];
-}
 // after a CTA's last use of the chain; the last one prepares the next call (tag 0 is what a fresh workspace holds)
 __device__ __forceinline__ void leave_chain(ChainCtrl* ctrl, unsigned tag) {
   __syncthreads();
@@ -169,24 +152,26 @@ struct ScanArgs {
   float *h_last, *gh0, *ckpt;
   long long outer, L, inner, groups, total;     // groups of VEC channels per outer entry, outer * groups
   long long in_o, in_t, gr_o, gr_t;
-  long long chains;            // CTAs side by side; each has `chunks` tiles one behind the other
+  long long chains;            // tiles side by side, `chunks` of them one behind the other
+  unsigned per_outer;          // chains of an outer entry
   int chunks, sigmoid;
   // chained tiles (null: a CTA walks through its chunks by itself)
   ChainCtrl* ctrl;
   ulonglong2* sums;            // [chunks][outer * inner]: (A, tag), (H, tag) of a chunk
   unsigned long long* ends;    // [chunks][outer * inner]: (state behind a chunk, tag)
+  unsigned long long* hints;   // [chunks][chains] (columns)
   int* status;
 };
 
-// a = 1 / (1 + e^-g) and b = 1 - a, each formed without cancellation.  The approximate exponential and reciprocal are good
-// to about 2^-22; what they flush to zero (|g| > 87) is below the smallest normal number anyway.
+// a = 1 / (1 + e^-g) and b = 1 - a = e^-g / (1 + e^-g), both without cancellation.  The exponent is kept below 2^126 (a NaN
+// stays one); the approximate exponential and reciprocal are good to about 2^-22, and what they flush to zero (g > 87) is
+// below the smallest normal number.
 __device__ __forceinline__ void gate_of(float g, float& a, float& b) {
   float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(g) * -1.4426950408889634f));
+  asm("{\n\t.reg .f32 x;\n\tmul.f32 x, %1, 0fBFB8AA3B;\n\tmin.NaN.f32 x, x, 0f42FC0000;\n\tex2.approx.ftz.f32 %0, x;\n\t}" : "=f"(e) : "f"(g));   // 2^min(-g log2 e, 126)
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  const float er = e * r;
-  a = g >= 0.f ? r : er;
-  b = g >= 0.f ? er : r;
+  a = r;
+  b = e * r;
 }
 // h_t = a h_{t-1} + b v_t
 __device__ __forceinline__ void terms(int sigmoid, float g, float& a, float& b) {
@@ -206,18 +191,19 @@ __device__ __forceinline__ long long clamp_len(const int* lengths, long long o, 
 }
 
 // ------------------------------------------------------------------------------------------------ columns
-// [outer][L][inner], inner contiguous.  A tile is TX groups of VEC channels (groups run on across outer entries) times
-// SLOTS runs of R steps, a run per thread.
-template <int VEC_, int R_, int SLOTS_, int THREADS_>
+// [outer][L][inner], inner contiguous.  A tile is TX groups of VEC channels times SLOTS runs of R steps, a run per thread.
+// Long sequences: the tiles of one outer entry lie side by side over its channels (a chain of chunks each).  Short ones
+// (one tile holds them): groups run on across outer entries, so that few channels fill a CTA too.
+template <int VEC_, int R_, int SLOTS_>
 struct ColShape {
-  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_, THREADS = THREADS_;
-  static constexpr int TX = THREADS / SLOTS, W = TX * VEC, LC = SLOTS * R;
+  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_;
+  static constexpr int TX = kScanThreads / SLOTS, W = TX * VEC, LC = SLOTS * R;
   // while runs are joined a warp has CPW channels, DG lanes each, and a lane has JOIN neighbouring runs of its channel
-  static constexpr int CPW = W / (THREADS / 32) < 32 ? W / (THREADS / 32) : 32, DG = 32 / CPW;
+  static constexpr int WARPS = kScanThreads / 32, CPW = W / WARPS < 32 ? W / WARPS : 32, DG = 32 / CPW;
   static constexpr int JOIN = SLOTS >= DG ? SLOTS / DG : 1;
 };
-constexpr int kSave = 64;         // steps between saved states
-constexpr int kColTile = 128;     // steps of a forward tile where a sequence has several
+constexpr int kColTile = 256;     // steps of a long sequence's tile, and between saved states
+enum ColMode { kOneTile = 0, kColWalk = 1, kColChained = 2 };
 
 // joins (A, H) over the DG lanes of a channel, in lane order (UP) or against it; returns the summary of all of them and
 // leaves in (A, H) that of the lanes before this one
@@ -241,69 +227,161 @@ __device__ __forceinline__ float2 join_lanes(float& A, float& H) {
   return all;
 }
 
-// where a thread stands in its tile while it walks steps, and while it joins runs
-template <typename T, class S>
-struct ColPlace {
-  int x, slot;              // group of the tile and run
-  bool live;
-  long long o, i0, end;     // outer entry, first channel, steps of the sequence
-  int jx, jq;               // joining: channel of the tile, first run
-  bool keeper, first;       // the channel exists; its first lane
-  long long ch, ch_end;     // index of the channel's state, steps of its sequence
-  __device__ __forceinline__ ColPlace(const ScanArgs<T>& p, long long g0) {
-    x = threadIdx.x % S::TX, slot = threadIdx.x / S::TX;
-    const long long gid = g0 + x;
-    live = gid < p.total;
-    o = live ? gid / p.groups : 0, i0 = live ? (gid - o * p.groups) * S::VEC : 0;
-    end = live ? clamp_len(p.lengths, o, p.L) : 0;
-    const int lane = threadIdx.x & 31;
-    jx = (threadIdx.x / 32) * S::CPW + lane % S::CPW, jq = lane / S::CPW * S::JOIN;
-    first = lane < S::CPW;
-    const long long jg = g0 + jx / S::VEC;
-    keeper = jg < p.total;
-    const long long jo = keeper ? jg / p.groups : 0;
-    ch = keeper ? jo * p.inner + (jg - jo * p.groups) * S::VEC + jx % S::VEC : 0;
-    ch_end = keeper ? clamp_len(p.lengths, jo, p.L) : 0;
+// A thread's part of a tile on its way through shared memory: only the thread itself touches its slots, so the copies of
+// the next tile start as soon as this one's are in registers, and no barrier is needed.
+template <typename T, class S, int TENSORS>
+struct ColSlots {
+  static constexpr int VEC = S::VEC, R = S::R, BYTES = VEC * (int)sizeof(T);
+  static constexpr bool ASYNC = BYTES >= 4;      // (cp.async moves 4, 8 or 16 bytes)
+  static constexpr size_t SMEM = (size_t)TENSORS * R * kScanThreads * BYTES;
+  using P = Pack<T, VEC>;
+  unsigned char* base;
+  __device__ __forceinline__ P* slot(int tensor, int r) const {
+    return reinterpret_cast<P*>(base + ((size_t)(tensor * R + r) * kScanThreads + threadIdx.x) * BYTES);
   }
+  // the first `have` steps from src on; `none` for the others
+  __device__ __forceinline__ void fetch(int tensor, const T* src, long long stride, int have, T none) const {
+#pragma unroll
+    for (int r = 0; r < R; ++r, src += stride) {
+      P* d = slot(tensor, r);
+      if (r >= have) {
+        P n;
+        n.fill(none);
+        *d = n;
+      } else if constexpr (ASYNC) {
+        const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(d));
+        if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(src) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(src), "n"(BYTES) : "memory");
+      } else {
+        d->load(src);
+      }
+    }
+  }
+  static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 };
 
-template <typename T, class S, bool CHAIN>
-__global__ void __launch_bounds__(S::THREADS, 1024 / S::THREADS) scan_cols_kernel(const ScanArgs<T> p) {
+// Where a tile lies.  Long sequences: the same for all threads of the CTA.
+struct ColTile {
+  int c;               // chunk
+  unsigned o;          // outer entry
+  long long g0;        // first group in it
+  int end;             // steps of the sequence
+};
+
+template <typename T, class S, int MODE>
+__device__ __forceinline__ ColTile col_tile(const ScanArgs<T>& p, unsigned chain, int c) {
+  ColTile t;
+  t.c = c;
+  t.o = MODE == kOneTile ? 0u : chain / p.per_outer;
+  t.g0 = (long long)(MODE == kOneTile ? chain : chain - t.o * p.per_outer) * S::TX;
+  t.end = MODE == kOneTile ? 0 : (int)clamp_len(p.lengths, t.o, p.L);
+  return t;
+}
+
+// A group of a tile: its outer entry, first channel and steps (0: no such group)
+struct ColGroup {
+  long long o;
+  int i0, end;
+  bool live;
+};
+template <typename T, class S, int MODE>
+__device__ __forceinline__ ColGroup col_group(const ScanArgs<T>& p, const ColTile& t, int x) {
+  ColGroup g;
+  if (MODE == kOneTile) {
+    const long long gid = t.g0 + x;
+    g.live = gid < p.total;
+    g.o = g.live ? (p.total <= 0xffffffffll ? (long long)((unsigned)gid / (unsigned)p.groups) : gid / p.groups) : 0;
+    g.i0 = g.live ? (int)(gid - g.o * p.groups) * S::VEC : 0;
+    g.end = g.live ? (int)clamp_len(p.lengths, g.o, p.L) : 0;
+  } else {
+    g.live = t.g0 + x < p.groups;
+    g.o = t.o;
+    g.i0 = g.live ? (int)(t.g0 + x) * S::VEC : 0;
+    g.end = g.live ? t.end : 0;
+  }
+  return g;
+}
+
+// The chained tiles of a CTA: by ticket, the next tile's ticket drawn and its loads started while a tile is worked on (a
+// held ticket waits for earlier ones only, so the earliest unfinished tile is always being worked on).
+struct ColDraw {
+  ColTile tile;
+  unsigned chain, tag;
+  int more;            // the ticket is a tile
+};
+
+template <typename T, class S, bool BACK>
+__device__ __forceinline__ void draw_tile(const ScanArgs<T>& p, unsigned ticket, ColDraw* out) {
+  const unsigned chains = (unsigned)p.chains;
+  const unsigned n = ticket / chains;
+  out->more = n < (unsigned)p.chunks;
+  out->chain = ticket - n * chains;
+  if (out->more) out->tile = col_tile<T, S, kColChained>(p, out->chain, BACK ? p.chunks - 1 - (int)n : (int)n);
+}
+
+template <typename T, class S, int MODE>
+__global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
+  constexpr bool CHAIN = MODE == kColChained;
+  using Slots = ColSlots<T, S, 2>;
   __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];     // (A, H) of every run; then its first state in x
-  __shared__ unsigned ticket[2];
+  __shared__ ColDraw drawn[2];
+  __shared__ int depth_s;
+  extern __shared__ __align__(16) unsigned char raw[];
+  const Slots slots{raw};
   pdl_trigger();
   pdl_wait();
-  unsigned tag = 0, tile = blockIdx.x;
-  if (CHAIN) tile = take_ticket(p.ctrl, ticket, tag);
-  const int c_first = CHAIN ? (int)(tile / (unsigned)p.chains) : 0, c_end = CHAIN ? c_first + 1 : p.chunks;
-  const long long g0 = (long long)(CHAIN ? tile % (unsigned)p.chains : tile) * S::TX;
-  const ColPlace<T, S> at(p, g0);
-  const T* v = p.v + at.o * p.in_o + at.i0;
-  const T* g = p.g + at.o * p.in_o + at.i0;
-  T* h = p.h + at.o * p.L * p.inner + at.i0;
-  const long long states = p.outer * p.inner;
+  ColTile tile;
+  unsigned tag = 0, chain = blockIdx.x;
+  bool go = true;
+  if (CHAIN) {
+    if (threadIdx.x == 0) {
+      drawn[1].tag = *(volatile unsigned*)&p.ctrl->epoch + 1u;
+      draw_tile<T, S, false>(p, atomicAdd(&p.ctrl->ticket, 1u), &drawn[1]);
+    }
+    __syncthreads();
+    tag = drawn[1].tag, tile = drawn[1].tile, chain = drawn[1].chain, go = drawn[1].more != 0;
+  } else {
+    tile = col_tile<T, S, MODE>(p, chain, 0);
+  }
+  const int slot = threadIdx.x / S::TX, x = threadIdx.x % S::TX;
   const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
-  float state = SLOTS > 1 && at.keeper && c_first == 0 && p.h0 != nullptr ? p.h0[at.ch] : 0.f;
+  const long long states = p.outer * p.inner;
+  const int lane = threadIdx.x & 31;
+  const int jx = (threadIdx.x / 32) * S::CPW + lane % S::CPW, jq = lane / S::CPW * S::JOIN;   // while joining: channel, first run
+  const bool first = lane < S::CPW;
+  auto fetch = [&](const ColTile& t) {
+    const ColGroup g = col_group<T, S, MODE>(p, t, x);
+    const int t0 = t.c * LC + slot * R;
+    const long long from = g.o * p.in_o + g.i0 + t0 * p.in_t;
+    slots.fetch(0, p.v + from, p.in_t, g.end - t0, none_v);
+    slots.fetch(1, p.g + from, p.in_t, g.end - t0, none_g);
+  };
+  if (go) fetch(tile);
+  float state = 0.f;
 
 #pragma unroll 1
-  for (int c = c_first; c < c_end; ++c) {
-    const int t0 = c * LC + at.slot * R;
-    Pack<T, VEC> pv[R], pg[R];
-    const T *lv = v + t0 * p.in_t, *lg = g + t0 * p.in_t;
-#pragma unroll
-    for (int r = 0; r < R; ++r, lv += p.in_t, lg += p.in_t) {
-      if (t0 + r < at.end) pv[r].load(lv), pg[r].load(lg);
-      else pv[r].fill(none_v), pg[r].fill(none_g);
-    }
+  while (go) {
+    const int c = tile.c;
+    const ColGroup at = col_group<T, S, MODE>(p, tile, x);
+    unsigned draw = 0;
+    if (CHAIN && threadIdx.x == 0) draw = atomicAdd(&p.ctrl->ticket, 1u);
     float a[R][VEC], u[R][VEC], s[VEC];
+    Slots::wait();
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+      float gv[VEC], vv[VEC];
+      slots.slot(1, r)->unpack(gv);
+      slots.slot(0, r)->unpack(vv);
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        terms(p.sigmoid, pg[r].get(j), a[r][j], u[r][j]);
-        u[r][j] *= pv[r].get(j);
+        terms(p.sigmoid, gv[j], a[r][j], u[r][j]);
+        u[r][j] *= vv[j];
       }
+    }
+    ColTile next;
+    unsigned next_chain = 0;
+    bool more_tiles = false;
     if constexpr (SLOTS == 1) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) s[j] = at.live && p.h0 != nullptr ? p.h0[at.o * p.inner + at.i0 + j] : 0.f;
@@ -316,114 +394,171 @@ __global__ void __launch_bounds__(S::THREADS, 1024 / S::THREADS) scan_cols_kerne
           A *= a[r][j];
           H = fmaf(a[r][j], H, u[r][j]);
         }
-        runs[at.slot][at.x * VEC + j] = make_float2(A, H);
+        runs[slot][x * VEC + j] = make_float2(A, H);
       }
+      if (CHAIN && threadIdx.x == 0) draw_tile<T, S, false>(p, draw, &drawn[0]);
       __syncthreads();
+      if (CHAIN) {        // the next tile's values are on their way from here on
+        next = drawn[0].tile, next_chain = drawn[0].chain, more_tiles = drawn[0].more != 0;
+      } else {
+        next = tile;
+        ++next.c;
+        more_tiles = next.c < p.chunks;
+      }
+      if (more_tiles) fetch(next);
+      const ColGroup jg = col_group<T, S, MODE>(p, tile, jx / VEC);
+      const long long ch = jg.o * p.inner + jg.i0 + jx % VEC;
+      if (c == 0) state = jg.live && p.h0 != nullptr ? p.h0[ch] : 0.f;
       float A = 1.f, H = 0.f;
       float2 m[S::JOIN];
 #pragma unroll
       for (int q = 0; q < S::JOIN; ++q) {
-        m[q] = runs[at.jq + q][at.jx];
+        m[q] = runs[jq + q][jx];
         A *= m[q].x;
         H = fmaf(m[q].x, H, m[q].y);
       }
       const float2 all = join_lanes<S::CPW, true>(A, H);
       // a chunk in which a sequence has no step leaves its state alone, and nobody waits for it
-      const bool active = at.keeper && c * LC < at.ch_end;
-      const bool more = active && (c + 1) * (long long)LC < at.ch_end;
-      const long long entry = c * states + at.ch;
-      if (CHAIN && c > 0) {
-        if (more && at.first) put_sum(p.sums + entry, all.x, all.y, tag);
-        state = look_back<S::CPW, 32>(active, p.sums + entry - states, p.ends + entry - states, -states, c, tag, p.status);
+      const bool active = c * LC < jg.end, more = (c + 1) * (long long)LC < jg.end;
+      const long long entry = c * states + ch;
+      if (CHAIN && c > 0 && c * LC < tile.end) {
+        if (more && first) put_sum(p.sums + entry, all.x, all.y, tag);
+        if (threadIdx.x < 32) {
+          unsigned long long* hint = p.hints + (long long)c * p.chains + chain;
+          if (threadIdx.x == 0) put_hint(hint, 1u, tag);
+          const int d = poll_hints(hint - p.chains, -p.chains, c, tag);
+          if (threadIdx.x == 0) {
+            depth_s = d < 0 ? 0 : d;
+            if (d < 0) atomicExch(p.status, 1);
+          }
+        }
+        __syncthreads();
+        state = look_back<S::CPW>(active, p.sums + entry - states, p.ends + entry - states, -states, depth_s, tag, p.status);
       }
       float run = fmaf(A, state, H);
+      if (MODE != kOneTile && p.ckpt != nullptr && first && jg.live && (active || c == 0)) p.ckpt[entry] = run;
 #pragma unroll
       for (int q = 0; q < S::JOIN; ++q) {
-        runs[at.jq + q][at.jx].x = run;
-        const int step = c * LC + (at.jq + q) * R;
-        if (p.ckpt != nullptr && at.keeper && step % kSave == 0 && (step < at.ch_end || step == 0))
-          p.ckpt[step / kSave * states + at.ch] = run;
+        runs[jq + q][jx].x = run;
         run = fmaf(m[q].x, run, m[q].y);
       }
       state = fmaf(all.x, state, all.y);
-      if (at.first) {
+      if (first && jg.live) {
         if (CHAIN && more) put_end(p.ends + entry, state, tag);
-        if (at.keeper && (active || c == 0) && !more && p.h_last != nullptr) p.h_last[at.ch] = state;
+        if ((active || c == 0) && !more && p.h_last != nullptr) p.h_last[ch] = state;
       }
+      if (CHAIN && threadIdx.x == 0) put_hint(p.hints + (long long)c * p.chains + chain, 2u, tag);
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) s[j] = runs[at.slot][at.x * VEC + j].x;
+      for (int j = 0; j < VEC; ++j) s[j] = runs[slot][x * VEC + j].x;
     }
-    T* sh = h + t0 * p.inner;
+    const int t0 = c * LC + slot * R, left = at.live ? (int)p.L - t0 : 0;
+    T* h = p.h + (at.o * p.L + t0) * p.inner + at.i0;
 #pragma unroll
-    for (int r = 0; r < R; ++r, sh += p.inner) {
+    for (int r = 0; r < R; ++r, h += p.inner) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) s[j] = fmaf(a[r][j], s[j], u[r][j]);
       Pack<T, VEC> out;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        s[j] = fmaf(a[r][j], s[j], u[r][j]);
-        out.put(j, t0 + r < at.end ? s[j] : 0.f);
-      }
-      if (at.live && t0 + r < p.L) out.store(sh);
+      out.pack(s);
+      if (t0 + r >= at.end) out.zero();
+      if (r < left) out.store(h);
     }
     if constexpr (SLOTS == 1) {
       if (at.live && p.h_last != nullptr) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) p.h_last[at.o * p.inner + at.i0 + j] = s[j];
       }
-    } else if (!CHAIN) {
-      __syncthreads();       // the runs' states are read before the next chunk's summaries replace them
     }
+    if (MODE == kOneTile) return;
+    __syncthreads();       // the runs' states are read before the next chunk's summaries replace them
+    tile = next, chain = CHAIN ? next_chain : chain, go = more_tiles;
   }
   if (CHAIN) leave_chain(p.ctrl, tag);
 }
 
-template <typename T, class S, bool CHAIN>
-__global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backward_kernel(const ScanArgs<T> p) {
+template <typename T, class S, int MODE>
+__global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
+  constexpr bool CHAIN = MODE == kColChained;
+  using Slots = ColSlots<T, S, 3>;
   // (A, H) and D of every run; then the state in front of it (x) and the gradient that comes to it from behind
   __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
   __shared__ float backs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
-  __shared__ unsigned ticket[2];
+  __shared__ ColDraw drawn[2];
+  __shared__ int depth_s;
+  extern __shared__ __align__(16) unsigned char raw[];
+  const Slots slots{raw};
   pdl_trigger();
   pdl_wait();
-  unsigned tag = 0, tile = blockIdx.x;
-  if (CHAIN) tile = take_ticket(p.ctrl, ticket, tag);
-  // chunks from the last to the first
-  const int n_first = CHAIN ? (int)(tile / (unsigned)p.chains) : 0, n_end = CHAIN ? n_first + 1 : p.chunks;
-  const long long g0 = (long long)(CHAIN ? tile % (unsigned)p.chains : tile) * S::TX;
-  const ColPlace<T, S> at(p, g0);
-  const T* v = p.v + at.o * p.in_o + at.i0;
-  const T* g = p.g + at.o * p.in_o + at.i0;
-  const T* gh = p.gh + at.o * p.L * p.inner + at.i0;
-  T* gv = p.gv + at.o * p.gr_o + at.i0;
-  T* gg = p.gg + at.o * p.gr_o + at.i0;
-  const long long states = p.outer * p.inner;
+  ColTile tile;
+  unsigned tag = 0, chain = blockIdx.x;
+  bool go = true;
+  if (CHAIN) {
+    if (threadIdx.x == 0) {
+      drawn[1].tag = *(volatile unsigned*)&p.ctrl->epoch + 1u;
+      draw_tile<T, S, true>(p, atomicAdd(&p.ctrl->ticket, 1u), &drawn[1]);
+    }
+    __syncthreads();
+    tag = drawn[1].tag, tile = drawn[1].tile, chain = drawn[1].chain, go = drawn[1].more != 0;
+  } else {
+    tile = col_tile<T, S, MODE>(p, chain, p.chunks - 1);        // chunks from the last to the first
+  }
+  const int slot = threadIdx.x / S::TX, x = threadIdx.x % S::TX;
   const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
-  const int ch_last = at.ch_end > 0 ? (int)((at.ch_end - 1) / LC) : 0;     // the chunk of the sequence's last step
-  float grad = SLOTS > 1 && at.keeper && p.g_last != nullptr ? p.g_last[at.ch] : 0.f;
+  const long long states = p.outer * p.inner;
+  const int lane = threadIdx.x & 31;
+  const int jx = (threadIdx.x / 32) * S::CPW + lane % S::CPW, jq = lane / S::CPW * S::JOIN;   // while joining: channel, first run
+  const bool first = lane < S::CPW;
+  auto fetch = [&](const ColTile& t) {
+    const ColGroup g = col_group<T, S, MODE>(p, t, x);
+    const int t0 = t.c * LC + slot * R;
+    const long long from = g.o * p.in_o + g.i0 + t0 * p.in_t;
+    slots.fetch(0, p.v + from, p.in_t, g.end - t0, none_v);
+    slots.fetch(1, p.g + from, p.in_t, g.end - t0, none_g);
+    slots.fetch(2, p.gh + (g.o * p.L + t0) * p.inner + g.i0, p.inner, g.end - t0, none_v);
+  };
+  if (go) fetch(tile);
+  float grad = 0.f;
 
 #pragma unroll 1
-  for (int n = n_first; n < n_end; ++n) {
-    const int c = p.chunks - 1 - n;
-    const int t0 = c * LC + at.slot * R;
-    Pack<T, VEC> pv[R], pg[R], pd[R];
-    const T *lv = v + t0 * p.in_t, *lg = g + t0 * p.in_t, *ld = gh + t0 * p.inner;
-#pragma unroll
-    for (int r = 0; r < R; ++r, lv += p.in_t, lg += p.in_t, ld += p.inner) {
-      if (t0 + r < at.end) pv[r].load(lv), pg[r].load(lg), pd[r].load(ld);
-      else pv[r].fill(none_v), pg[r].fill(none_g), pd[r].fill(none_v);
-    }
-    const bool active = at.keeper && c * LC < at.ch_end, mine = at.keeper && (active || c == 0);
+  while (go) {
+    const int c = tile.c;
+    const ColGroup at = col_group<T, S, MODE>(p, tile, x);
+    unsigned draw = 0;
+    if (CHAIN && threadIdx.x == 0) draw = atomicAdd(&p.ctrl->ticket, 1u);
+    const ColGroup jg = col_group<T, S, MODE>(p, tile, jx / VEC);
+    const long long ch = jg.o * p.inner + jg.i0 + jx % VEC, entry = c * states + ch;
+    const int last = jg.end > 0 ? (jg.end - 1) / LC : 0;     // the chunk of the sequence's last step
+    const bool active = c * LC < jg.end, mine = SLOTS > 1 && jg.live && (active || c == 0);
     float before = 0.f;      // the state in front of the chunk: saved, or the sequence's own beginning
-    if (SLOTS > 1 && mine) before = p.ckpt != nullptr ? p.ckpt[c * states + at.ch] : p.h0 != nullptr ? p.h0[at.ch] : 0.f;
-    float a[R][VEC], w[R][VEC], s[VEC], d[VEC];
+    if (mine) {
+      if (MODE != kOneTile && p.ckpt != nullptr) before = p.ckpt[entry];
+      else if (p.h0 != nullptr) before = p.h0[ch];
+      if (c >= last) grad = p.g_last != nullptr ? p.g_last[ch] : 0.f;
+    }
+    Slots::wait();
+    // q: 1 - a (sigmoid) or a (decay); a is formed again where it is used
+    float q[R][VEC], v[R][VEC], s[VEC], d[VEC];
+    Pack<T, VEC> pd[R];
+    const float ka = p.sigmoid ? -1.f : 1.f, kb = p.sigmoid ? 1.f : 0.f;
+    auto a_of = [&](float qq) { return fmaf(qq, ka, kb); };
+    auto b_of = [&](float qq) { return p.sigmoid ? qq : 1.f; };
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+      pd[r] = *slots.slot(2, r);
+      slots.slot(1, r)->unpack(q[r]);
+      slots.slot(0, r)->unpack(v[r]);
+      if (p.sigmoid) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        terms(p.sigmoid, pg[r].get(j), a[r][j], w[r][j]);
-        w[r][j] *= pv[r].get(j);
+        for (int j = 0; j < VEC; ++j) {
+          float a;
+          gate_of(q[r][j], a, q[r][j]);
+        }
       }
+    }
+    ColTile next;
+    unsigned next_chain = 0;
+    bool more_tiles = false;
     if constexpr (SLOTS == 1) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
@@ -431,94 +566,120 @@ __global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backwa
         d[j] = at.live && p.g_last != nullptr ? p.g_last[at.o * p.inner + at.i0 + j] : 0.f;
       }
     } else {
+      float D[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        float A = 1.f, H = 0.f, D = 0.f;
+        float A = 1.f, H = 0.f;
+        D[j] = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          A *= a[r][j];
-          H = fmaf(a[r][j], H, w[r][j]);
+          const float a = a_of(q[r][j]);
+          A *= a;
+          H = fmaf(a, H, b_of(q[r][j]) * v[r][j]);
         }
-#pragma unroll
-        for (int r = R - 1; r >= 0; --r) D = a[r][j] * (D + pd[r].get(j));
-        runs[at.slot][at.x * VEC + j] = make_float2(A, H);
-        backs[at.slot][at.x * VEC + j] = D;
+        runs[slot][x * VEC + j] = make_float2(A, H);
       }
+#pragma unroll
+      for (int r = R - 1; r >= 0; --r) {
+        float gh[VEC];
+        pd[r].unpack(gh);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) D[j] = a_of(q[r][j]) * (D[j] + gh[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) backs[slot][x * VEC + j] = D[j];
+      if (CHAIN && threadIdx.x == 0) draw_tile<T, S, true>(p, draw, &drawn[0]);
       __syncthreads();
-      float A = 1.f, H = 0.f, B = 1.f, D = 0.f;
+      if (CHAIN) {        // the next tile's values are on their way from here on
+        next = drawn[0].tile, next_chain = drawn[0].chain, more_tiles = drawn[0].more != 0;
+      } else {
+        next = tile;
+        --next.c;
+        more_tiles = next.c >= 0;
+      }
+      if (more_tiles) fetch(next);
+      float A = 1.f, H = 0.f, B = 1.f, E = 0.f;
       float2 m[S::JOIN];
       float md[S::JOIN];
 #pragma unroll
-      for (int q = 0; q < S::JOIN; ++q) {
-        m[q] = runs[at.jq + q][at.jx];
-        md[q] = backs[at.jq + q][at.jx];
-        A *= m[q].x;
-        H = fmaf(m[q].x, H, m[q].y);
+      for (int k = 0; k < S::JOIN; ++k) {
+        m[k] = runs[jq + k][jx];
+        md[k] = backs[jq + k][jx];
+        A *= m[k].x;
+        H = fmaf(m[k].x, H, m[k].y);
       }
 #pragma unroll
-      for (int q = S::JOIN - 1; q >= 0; --q) D = fmaf(m[q].x, D, md[q]);
+      for (int k = S::JOIN - 1; k >= 0; --k) E = fmaf(m[k].x, E, md[k]);
       B = A;
       join_lanes<S::CPW, true>(A, H);
-      const float2 all = join_lanes<S::CPW, false>(B, D);
-      if (CHAIN) {
-        const long long entry = c * states + at.ch;
-        const bool asks = active && c < ch_last;
-        if (asks && c > 0 && at.first) put_sum(p.sums + entry, all.x, all.y, tag);
-        const float in = look_back<S::CPW, 16>(asks, p.sums + entry + states, p.ends + entry + states, states, ch_last - c, tag, p.status);
-        if (asks) grad = in;
+      const float2 all = join_lanes<S::CPW, false>(B, E);
+      if (CHAIN && tile.end > 0 && c < (tile.end - 1) / LC) {
+        if (jg.live && c > 0 && first) put_sum(p.sums + entry, all.x, all.y, tag);
+        if (threadIdx.x < 32) {
+          unsigned long long* hint = p.hints + (long long)c * p.chains + chain;
+          if (threadIdx.x == 0) put_hint(hint, 1u, tag);
+          const int n = (tile.end - 1) / LC - c;
+          const int dd = poll_hints(hint + p.chains, p.chains, n, tag);
+          if (threadIdx.x == 0) {
+            depth_s = dd < 0 ? 0 : dd;
+            if (dd < 0) atomicExch(p.status, 1);
+          }
+        }
+        __syncthreads();
+        grad = look_back<S::CPW>(jg.live, p.sums + entry + states, p.ends + entry + states, states, depth_s, tag, p.status);
       }
       float run = fmaf(A, before, H);
 #pragma unroll
-      for (int q = 0; q < S::JOIN; ++q) {
-        runs[at.jq + q][at.jx].x = run;
-        run = fmaf(m[q].x, run, m[q].y);
+      for (int k = 0; k < S::JOIN; ++k) {
+        runs[jq + k][jx].x = run;
+        run = fmaf(m[k].x, run, m[k].y);
       }
-      run = fmaf(B, grad, D);
+      run = fmaf(B, grad, E);
 #pragma unroll
-      for (int q = S::JOIN - 1; q >= 0; --q) {
-        backs[at.jq + q][at.jx] = run;
-        run = fmaf(m[q].x, run, md[q]);
+      for (int k = S::JOIN - 1; k >= 0; --k) {
+        backs[jq + k][jx] = run;
+        run = fmaf(m[k].x, run, md[k]);
       }
       if (mine) grad = fmaf(all.x, grad, all.y);
-      if (mine && at.first) {
-        if (CHAIN && c > 0) put_end(p.ends + c * states + at.ch, grad, tag);
-        if (c == 0 && p.gh0 != nullptr) p.gh0[at.ch] = grad;
+      if (mine && first) {
+        if (CHAIN && c > 0) put_end(p.ends + entry, grad, tag);
+        if (c == 0 && p.gh0 != nullptr) p.gh0[ch] = grad;
       }
+      if (CHAIN && threadIdx.x == 0) put_hint(p.hints + (long long)c * p.chains + chain, 2u, tag);
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) s[j] = runs[at.slot][at.x * VEC + j].x, d[j] = backs[at.slot][at.x * VEC + j];
+      for (int j = 0; j < VEC; ++j) s[j] = runs[slot][x * VEC + j].x, d[j] = backs[slot][x * VEC + j];
     }
-    // forward once more: u is replaced by what delta is multiplied with for the gate's gradient
+    // forward once more: v is replaced by what delta is multiplied with for the gate's gradient
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float u = w[r][j];
-        float aa, b;
-        terms(p.sigmoid, pg[r].get(j), aa, b);
-        w[r][j] = p.sigmoid ? (s[j] - pv[r].get(j)) * (a[r][j] * b) : s[j];
-        s[j] = fmaf(a[r][j], s[j], u);
+        const float a = a_of(q[r][j]), u = b_of(q[r][j]) * v[r][j];
+        v[r][j] = p.sigmoid ? (s[j] - v[r][j]) * (a * q[r][j]) : s[j];
+        s[j] = fmaf(a, s[j], u);
       }
-    T *sv = gv + (t0 + R - 1) * p.gr_t, *sg = gg + (t0 + R - 1) * p.gr_t;
+    const int t0 = c * LC + slot * R, left = at.live ? (int)p.L - t0 : 0;
+    const long long back = at.o * p.gr_o + at.i0 + (t0 + R - 1) * p.gr_t;
+    T *gv = p.gv + back, *gg = p.gg + back;
 #pragma unroll
-    for (int r = R - 1; r >= 0; --r, sv -= p.gr_t, sg -= p.gr_t) {
+    for (int r = R - 1; r >= 0; --r, gv -= p.gr_t, gg -= p.gr_t) {
+      float x1[VEC], x2[VEC];
+      pd[r].unpack(x1);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float delta = d[j] + x1[j];
+        x1[j] = delta * b_of(q[r][j]);
+        x2[j] = delta * v[r][j];
+        d[j] = a_of(q[r][j]) * delta;
+      }
       Pack<T, VEC> ov, og;
-      ov.zero();
-      og.zero();
-      if (t0 + r < at.end) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const float delta = d[j] + pd[r].get(j);
-          float aa, b;
-          terms(p.sigmoid, pg[r].get(j), aa, b);
-          ov.put(j, delta * b);
-          og.put(j, delta * w[r][j]);
-          d[j] = a[r][j] * delta;
-        }
-      }
-      if (at.live && t0 + r < p.L) {
-        ov.store(sv);
-        og.store(sg);
+      ov.pack(x1);
+      og.pack(x2);
+      if (t0 + r >= at.end) ov.zero(), og.zero();
+      if (r < left) {
+        ov.store(gv);
+        og.store(gg);
       }
     }
     if constexpr (SLOTS == 1) {
@@ -526,9 +687,10 @@ __global__ void __launch_bounds__(S::THREADS, 512 / S::THREADS) scan_cols_backwa
 #pragma unroll
         for (int j = 0; j < VEC; ++j) p.gh0[at.o * p.inner + at.i0 + j] = d[j];
       }
-    } else if (!CHAIN) {
-      __syncthreads();
     }
+    if (MODE == kOneTile) return;
+    __syncthreads();
+    tile = next, chain = CHAIN ? next_chain : chain, go = more_tiles;
   }
   if (CHAIN) leave_chain(p.ctrl, tag);
 }
@@ -927,26 +1089,48 @@ void chain(ScanArgs<T>& p, const ScanCall& c) {
   p.ctrl = reinterpret_cast<ChainCtrl*>(ws + kStatusBytes);
   p.sums = reinterpret_cast<ulonglong2*>(ws + kChainHead);
   p.ends = reinterpret_cast<unsigned long long*>(p.sums + (long long)p.chunks * c.outer * c.inner);
+  p.hints = p.ends + (long long)p.chunks * c.outer * c.inner;
   p.status = reinterpret_cast<int*>(ws);
 }
 
-template <typename T, class S, bool BACK>
-cudaError_t launch_cols(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
-  p.chains = (p.total + S::TX - 1) / S::TX;
-  p.chunks = (int)((p.L + S::LC - 1) / S::LC);
-  const dim3 block(S::THREADS);
-  // only the longest tiles ever come in several
-  if constexpr (S::LC >= kSave) {
-    if (chained(p.chains, p.chunks, p.chains * p.chunks)) {
-      chain(p, c);
-      const dim3 grid((unsigned)(p.chains * p.chunks));
-      if constexpr (BACK) return launch_pdl(scan_cols_backward_kernel<T, S, true>, grid, block, 0, st, p);
-      else return launch_pdl(scan_cols_kernel<T, S, true>, grid, block, 0, st, p);
-    }
+template <typename T, class S, int MODE, bool BACK>
+cudaError_t launch_cols_kernel(const ScanArgs<T>& p, cudaStream_t st) {
+  void (*kern)(const ScanArgs<T>);
+  constexpr size_t smem = ColSlots<T, S, BACK ? 3 : 2>::SMEM;
+  if constexpr (BACK) kern = scan_cols_backward_kernel<T, S, MODE>;
+  else kern = scan_cols_kernel<T, S, MODE>;
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), smem + 4096 + sizeof(float) * 3 * S::SLOTS * S::W, allowed);
+  if (e != cudaSuccess) return e;
+  long long ctas = p.chains;
+  if (MODE == kColChained) {       // as many CTAs as run at once (only a running CTA draws tickets, so none has to)
+    const long long most = 2 * (long long)num_sms();
+    ctas = p.chains * p.chunks < most ? p.chains * p.chunks : most;
   }
-  const dim3 grid((unsigned)p.chains);
-  if constexpr (BACK) return launch_pdl(scan_cols_backward_kernel<T, S, false>, grid, block, 0, st, p);
-  else return launch_pdl(scan_cols_kernel<T, S, false>, grid, block, 0, st, p);
+  return launch_pdl(kern, dim3((unsigned)ctas), dim3(kScanThreads), smem, st, p);
+}
+
+// sequences that fit one tile
+template <typename T, class S, bool BACK>
+cudaError_t launch_short_cols(ScanArgs<T> p, cudaStream_t st) {
+  p.total = p.outer * p.groups;
+  p.chains = (p.total + S::TX - 1) / S::TX;
+  p.chunks = 1;
+  return launch_cols_kernel<T, S, kOneTile, BACK>(p, st);
+}
+template <typename T, class S, bool BACK>
+cudaError_t launch_long_cols(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
+  static_assert(S::LC == kColTile, "tiles end where states are saved");
+  const long long per_outer = (p.groups + S::TX - 1) / S::TX;
+  p.per_outer = (unsigned)per_outer;
+  p.chains = p.outer * per_outer;
+  if (p.chains > 0x7fffffff) return cudaErrorNotSupported;
+  p.chunks = (int)((p.L + S::LC - 1) / S::LC);
+  if (chained(p.chains, p.chunks, p.chains * p.chunks)) {
+    chain(p, c);
+    return launch_cols_kernel<T, S, kColChained, BACK>(p, st);
+  }
+  return launch_cols_kernel<T, S, kColWalk, BACK>(p, st);
 }
 
 template <typename T, bool WIDE, int MODE, bool BACK>
@@ -1006,31 +1190,29 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   if (BACK) vec = vec && c.grad_outer % 4 == 0 && c.grad_step % 4 == 0 && aligned_to(c.grad_h, need) && aligned_to(c.grad_v, need) && aligned_to(c.grad_g, need);
   else vec = vec && aligned_to(c.h, need);
   p.groups = vec ? c.inner / 4 : c.inner;
-  p.total = c.outer * p.groups;
-  // forward tiles of 128 steps, backward ones of the 64 between saved states; shorter ones for short sequences
   if (vec) {
-    if (c.length <= 4) return launch_cols<T, ColShape<4, 4, 1, 256>, BACK>(p, c, st);
-    if (c.length <= 32) return launch_cols<T, ColShape<4, 4, 8, 256>, BACK>(p, c, st);
-    return launch_cols<T, ColShape<4, 4, BACK ? 16 : 32, BACK ? 256 : 512>, BACK>(p, c, st);
+    if (c.length <= 8) return launch_short_cols<T, ColShape<4, 8, 1>, BACK>(p, st);
+    if (c.length <= 64) return launch_short_cols<T, ColShape<4, 8, 8>, BACK>(p, st);
+    return launch_long_cols<T, ColShape<4, 8, 32>, BACK>(p, c, st);
   }
-  if (c.length <= 8) return launch_cols<T, ColShape<1, 8, 1, 256>, BACK>(p, c, st);
-  if (c.length <= 32) return launch_cols<T, ColShape<1, 8, 4, 256>, BACK>(p, c, st);
-  return launch_cols<T, ColShape<1, 8, BACK ? 8 : 16, BACK ? 256 : 512>, BACK>(p, c, st);
+  if (c.length <= 8) return launch_short_cols<T, ColShape<1, 8, 1>, BACK>(p, st);
+  if (c.length <= 64) return launch_short_cols<T, ColShape<1, 8, 8>, BACK>(p, st);
+  return launch_long_cols<T, ColShape<1, 32, 8>, BACK>(p, c, st);
 }
 
 }  // namespace
 
-// States are saved every 64 steps of [outer][L][inner] sequences, every 512 (or 504) of contiguous ones - or once, in
+// States are saved every 256 steps of [outer][L][inner] sequences, every 512 (or 504) of contiguous ones - or once, in
 // front of a sequence that fits one tile.
 long long scan_chunk(int, long long length, long long inner) {
-  const long long lc = inner == 1 ? row_chunk(length) : kSave;
+  const long long lc = inner == 1 ? row_chunk(length) : kColTile;
   return length <= lc ? (length < 1 ? 1 : length) : lc;
 }
 
 size_t scan_workspace_bytes(int dtype, long long outer, long long length, long long inner) {
   const long long lc = scan_chunk(dtype, length, inner), chunks = (length + lc - 1) / lc;
   if (chunks < 2) return kStatusBytes;
-  return kChainHead + (size_t)chunks * (size_t)outer * (size_t)inner * (sizeof(ulonglong2) + sizeof(unsigned long long));
+  return kChainHead + (size_t)chunks * (size_t)outer * (size_t)inner * (sizeof(ulonglong2) + 2 * sizeof(unsigned long long));   // (at most one hint per state)
 }
 
 cudaError_t launch_scan_forward(const ScanCall& c, cudaStream_t st) {

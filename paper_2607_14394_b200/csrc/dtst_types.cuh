@@ -63,6 +63,44 @@ struct Pack {
   }
   __device__ __forceinline__ float get(int i) const { return Elem<T>::get(v[i]); }
   __device__ __forceinline__ void put(int i, float x) { v[i] = Elem<T>::put(x); }
+  // all elements at once, two 16-bit ones to an instruction
+  __device__ __forceinline__ void unpack(float (&x)[N]) const {
+    if constexpr (sizeof(T) == 2 && N >= 2) {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(&raw);
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) unpack2(w[i], x[2 * i], x[2 * i + 1], T());
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = get(i);
+    }
+  }
+  __device__ __forceinline__ void pack(const float (&x)[N]) {
+    if constexpr (sizeof(T) == 2 && N >= 2) {
+      uint32_t* w = reinterpret_cast<uint32_t*>(&raw);
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) w[i] = pack2(x[2 * i], x[2 * i + 1], T());
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) put(i, x[i]);
+    }
+  }
+  static __device__ __forceinline__ void unpack2(uint32_t w, float& a, float& b, __nv_bfloat16) {
+    a = __uint_as_float(w << 16), b = __uint_as_float(w & 0xffff0000u);
+  }
+  static __device__ __forceinline__ void unpack2(uint32_t w, float& a, float& b, __half) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    a = f.x, b = f.y;
+  }
+  static __device__ __forceinline__ void unpack2(uint32_t, float&, float&, float) {}
+  static __device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint32_t pack2(float a, float b, __half) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint32_t pack2(float, float, float) { return 0u; }
   __device__ __forceinline__ void fill(T x) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = x;

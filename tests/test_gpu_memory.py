@@ -237,6 +237,7 @@ SCAN_SHAPES = [
     (9, 513, 1), (3, 2000, 1),
     (50, 7, 1), (200, 8, 1), (131, 9, 1), (64, 15, 1), (20, 127, 1), (11, 255, 1), (5, 504, 1), (5, 505, 1), (4, 511, 1),
     (3, 1016, 1), (2, 1009, 1), (1, 9001, 1), (2, 3000, 20), (1, 4099, 3),
+    (3, 256, 40), (3, 257, 40), (2, 511, 33), (2, 513, 5), (1, 5000, 132), (700, 300, 20), (5, 66, 7),
 ]
 
 

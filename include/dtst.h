@@ -478,9 +478,7 @@ dtst_status dtst_plan_last_cuda_error(const dtst_plan* plan, int* code, const ch
  * their element size (the fast kernels run where they are aligned to 16 bytes); all arithmetic, statistics, states
  * and weight gradients are float32, and a value is rounded once, when it is stored.  8-bit values are e4m3 (4
  * exponent and 3 mantissa bits, largest finite value 448).  An extent of zero is legal where a batch may be empty:
- * nothing is read or written then.  Where a call takes a workspace, it is caller-owned, 256-byte aligned and filled
- * with zeros ONCE before its first use; calls that share one must be stream-ordered.  Its first word is a status word
- * as for plans (dtst_workspace_status).
+ * nothing is read or written then.
  */
 enum { DTST_F32 = 0, DTST_BF16 = 1, DTST_F16 = 2 };
 
@@ -526,7 +524,8 @@ dtst_status dtst_quantize_fp8_weight(int dtype, int64_t rows, int64_t cols, cons
  *   multiples of 16 bytes (what lies between k and the stride is not used), else DTST_ERR_INVALID_ARG;
  *   x_scale [ceil(k / 128), m], w_scale [ceil(n / 128), ceil(k / 128)] float32, contiguous;
  *   out [m, n] of out_dtype, rows out_ld elements apart (out_ld >= n).  k >= 1.
- *   workspace: at least 256 bytes (the status word).
+ *   workspace: at least 256 bytes, 256-byte aligned, caller-owned, filled with zeros once before its first use; calls
+ *   that share one must be stream-ordered.  Its first word is a status word as for plans (dtst_workspace_status).
  * Every product of a row of x is the same whatever the other rows are, and the same on every run.
  */
 dtst_status dtst_matmul_fp8(int out_dtype, int64_t m, int64_t n, int64_t k, const void* x, int64_t x_ld,
@@ -543,14 +542,14 @@ dtst_status dtst_matmul_fp8(int out_dtype, int64_t m, int64_t n, int64_t k, cons
  * may be NULL (zeros; not wanted), and they may be the same buffer (a running state).  lengths [outer] int32 or NULL:
  * entry o has lengths[o] steps (taken into 0..length); what lies behind them is not used, h is zero there, and h_last is
  * the state behind the entry's own last step (h0 for an entry without steps).
- * checkpoints: NULL, or dtst_gated_scan_sizes' count of floats, which receive the states the backward pass restarts from.
+ * checkpoints: NULL, or dtst_gated_scan_checkpoints floats, which receive the states the backward pass restarts from.
  *
  * Backward for grad_h [outer, length, inner] (contiguous) and grad_last [outer, inner] (or NULL), with
  *   delta_t = grad_h_t + a_{t+1} delta_{t+1}:
  *   SIGMOID: grad_v = delta (1 - a), grad_g = delta (h_{t-1} - v) a (1 - a);   DECAY: grad_v = delta, grad_g = delta h_{t-1};
  *   grad_h0 = a_0 delta_0 (may be NULL).  grad_v, grad_g: both with grad_stride, which must not make elements coincide;
  * zero behind an entry's own length.  v, g, h0, lengths and checkpoints as in the forward call.  h is not needed.
- * Both passes take the workspace of dtst_gated_scan_sizes.
+ * Neither pass needs a workspace, and both give the same bits on every run.
  */
 enum { DTST_GATE_SIGMOID = 0, DTST_GATE_DECAY = 1 };
 typedef struct {
@@ -559,16 +558,15 @@ typedef struct {
   int64_t in_stride[2];      /* v and g: outer, step */
   int64_t grad_stride[2];    /* grad_v and grad_g: outer, step */
 } dtst_scan_desc;
-dtst_status dtst_gated_scan_sizes(const dtst_scan_desc* desc, size_t* workspace_bytes, int64_t* checkpoint_floats);
+dtst_status dtst_gated_scan_checkpoints(const dtst_scan_desc* desc, int64_t* checkpoint_floats);
 dtst_status dtst_gated_scan(const dtst_scan_desc* desc, const void* v, const void* g, const float* h0,
-                            const int32_t* lengths, void* h, float* h_last, float* checkpoints, void* workspace,
-                            size_t workspace_bytes, void* stream);
+                            const int32_t* lengths, void* h, float* h_last, float* checkpoints, void* stream);
 dtst_status dtst_gated_scan_backward(const dtst_scan_desc* desc, const void* grad_h, const float* grad_last,
                                      const void* v, const void* g, const float* h0, const int32_t* lengths,
                                      const float* checkpoints, void* grad_v, void* grad_g, float* grad_h0,
-                                     void* workspace, size_t workspace_bytes, void* stream);
+                                     void* stream);
 
-/* Synchronises `stream` and reports the status word at the head of a workspace of the calls above: DTST_OK, or
+/* Synchronises `stream` and reports the status word at the head of a workspace of dtst_matmul_fp8: DTST_OK, or
  * DTST_ERR_DEVICE_TIMEOUT if a bounded wait inside a kernel gave up (its output is undefined then).  Clears the word. */
 dtst_status dtst_workspace_status(void* workspace, void* stream);
 

@@ -45,7 +45,7 @@ EXPORTED = [
     "dtst_plan_tune_contraction_order", "dtst_plan_host_io_bytes", "dtst_plan_enable_host_io", "dtst_step_host",
     "dtst_host_io_wait", "dtst_plan_set_column_contraction", "dtst_plan_set_arithmetic",
     "dtst_rms_norm", "dtst_rms_norm_scratch_bytes", "dtst_rms_norm_backward", "dtst_rms_norm_fp8", "dtst_quantize_fp8",
-    "dtst_quantize_fp8_weight", "dtst_matmul_fp8", "dtst_gated_scan_sizes", "dtst_gated_scan",
+    "dtst_quantize_fp8_weight", "dtst_matmul_fp8", "dtst_gated_scan_checkpoints", "dtst_gated_scan",
     "dtst_gated_scan_backward", "dtst_workspace_status",
 ]
 
@@ -133,9 +133,9 @@ def lib() -> ctypes.CDLL:
     L.dtst_quantize_fp8.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp]
     L.dtst_quantize_fp8_weight.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp]
     L.dtst_matmul_fp8.argtypes = [i32, i64, i64, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, sz, vp]
-    L.dtst_gated_scan_sizes.argtypes = [descp, ctypes.POINTER(sz), i64p]
-    L.dtst_gated_scan.argtypes = [descp] + [vp] * 8 + [sz, vp]
-    L.dtst_gated_scan_backward.argtypes = [descp] + [vp] * 11 + [sz, vp]
+    L.dtst_gated_scan_checkpoints.argtypes = [descp, i64p]
+    L.dtst_gated_scan.argtypes = [descp] + [vp] * 8
+    L.dtst_gated_scan_backward.argtypes = [descp] + [vp] * 11
     L.dtst_workspace_status.argtypes = [vp, vp]
     L.dtst_status_string.argtypes = [i32]
     L.dtst_status_string.restype = ctypes.c_char_p

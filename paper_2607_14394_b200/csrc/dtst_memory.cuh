@@ -55,11 +55,9 @@ struct ScanCall {
   const int* lengths;
   void *h, *grad_v, *grad_g;
   float *h_last, *grad_h0, *checkpoints;
-  void* workspace;
 };
 // steps between saved states for this problem (the whole length where nothing is saved)
 long long scan_chunk(int dtype, long long length, long long inner);
-size_t scan_workspace_bytes(int dtype, long long outer, long long length, long long inner);
 cudaError_t launch_scan_forward(const ScanCall& c, cudaStream_t st);
 cudaError_t launch_scan_backward(const ScanCall& c, cudaStream_t st);
 

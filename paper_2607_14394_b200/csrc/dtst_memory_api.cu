@@ -163,18 +163,17 @@ dtst_status dtst_matmul_fp8(int out_dtype, int64_t m, int64_t n, int64_t k, cons
   return done(launch_matmul_fp8(c, static_cast<cudaStream_t>(stream)));
 }
 
-dtst_status dtst_gated_scan_sizes(const dtst_scan_desc* d, size_t* workspace_bytes, int64_t* checkpoint_floats) {
+dtst_status dtst_gated_scan_checkpoints(const dtst_scan_desc* d, int64_t* checkpoint_floats) {
   const dtst_status s = check_scan(d);
   if (s != DTST_OK) return s;
-  if (workspace_bytes == nullptr || checkpoint_floats == nullptr) return DTST_ERR_INVALID_ARG;
-  *workspace_bytes = scan_workspace_bytes(d->dtype, d->outer, d->length, d->inner);
+  if (checkpoint_floats == nullptr) return DTST_ERR_INVALID_ARG;
   const int64_t lc = scan_chunk(d->dtype, d->length, d->inner);
   *checkpoint_floats = (d->length + lc - 1) / lc * d->outer * d->inner;
   return DTST_OK;
 }
 
 dtst_status dtst_gated_scan(const dtst_scan_desc* d, const void* v, const void* g, const float* h0, const int32_t* lengths,
-                            void* h, float* h_last, float* checkpoints, void* workspace, size_t workspace_bytes, void* stream) {
+                            void* h, float* h_last, float* checkpoints, void* stream) {
   const dtst_status s = check_scan(d);
   if (s != DTST_OK) return s;
   if (!f32(h0) || !f32(h_last) || !f32(lengths) || !f32(checkpoints)) return DTST_ERR_INVALID_ARG;
@@ -182,17 +181,14 @@ dtst_status dtst_gated_scan(const dtst_scan_desc* d, const void* v, const void* 
   if (d->length > 0 && (v == nullptr || g == nullptr || h == nullptr || h == v || h == g || !fits(v, d->dtype) ||
                         !fits(g, d->dtype) || !fits(h, d->dtype) || (checkpoints != nullptr && checkpoints == h0)))
     return DTST_ERR_INVALID_ARG;
-  if (workspace == nullptr || workspace_bytes < scan_workspace_bytes(d->dtype, d->outer, d->length, d->inner)) return DTST_ERR_WORKSPACE;
-  if (!workspace_ok(workspace)) return DTST_ERR_INVALID_ARG;
   ScanCall c = scan_call(d);
-  c.v = v, c.g = g, c.h0 = h0, c.lengths = lengths, c.h = h, c.h_last = h_last, c.checkpoints = checkpoints, c.workspace = workspace;
+  c.v = v, c.g = g, c.h0 = h0, c.lengths = lengths, c.h = h, c.h_last = h_last, c.checkpoints = checkpoints;
   return done(launch_scan_forward(c, static_cast<cudaStream_t>(stream)));
 }
 
 dtst_status dtst_gated_scan_backward(const dtst_scan_desc* d, const void* grad_h, const float* grad_last, const void* v,
                                      const void* g, const float* h0, const int32_t* lengths, const float* checkpoints,
-                                     void* grad_v, void* grad_g, float* grad_h0, void* workspace, size_t workspace_bytes,
-                                     void* stream) {
+                                     void* grad_v, void* grad_g, float* grad_h0, void* stream) {
   const dtst_status s = check_scan(d);
   if (s != DTST_OK) return s;
   if (!f32(h0) || !f32(grad_last) || !f32(lengths) || !f32(checkpoints) || !f32(grad_h0)) return DTST_ERR_INVALID_ARG;
@@ -205,12 +201,10 @@ dtst_status dtst_gated_scan_backward(const dtst_scan_desc* d, const void* grad_h
     // a pass longer than one chunk restarts from saved states
     if (checkpoints == nullptr && d->length > scan_chunk(d->dtype, d->length, d->inner)) return DTST_ERR_INVALID_ARG;
   }
-  if (workspace == nullptr || workspace_bytes < scan_workspace_bytes(d->dtype, d->outer, d->length, d->inner)) return DTST_ERR_WORKSPACE;
-  if (!workspace_ok(workspace)) return DTST_ERR_INVALID_ARG;
   ScanCall c = scan_call(d);
   c.grad_h = grad_h, c.grad_last = grad_last, c.v = v, c.g = g, c.h0 = h0, c.lengths = lengths;
   c.checkpoints = const_cast<float*>(checkpoints);
-  c.grad_v = grad_v, c.grad_g = grad_g, c.grad_h0 = grad_h0, c.workspace = workspace;
+  c.grad_v = grad_v, c.grad_g = grad_g, c.grad_h0 = grad_h0;
   return done(launch_scan_backward(c, static_cast<cudaStream_t>(stream)));
 }
 

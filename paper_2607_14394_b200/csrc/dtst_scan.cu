@@ -20,127 +20,29 @@ namespace {
 
 constexpr int kScanThreads = 256;
 
-// Chained tiles.  Where there are few sequences, the chunks of one sequence are tiles of their own, handed out in
-// time order by a ticket counter.  A tile publishes the summary (A, H) of its chunk, looks back for the nearest chunk
-// whose end state is known, applies the summaries in between to it - one after the other, so the result has the same
-// bits whichever state it started from - and publishes its own end state.  Every 32-bit value travels in one 64-bit
-// word with the call's number, so no fence and no clearing is needed; the last CTA advances the number.  A tile waits only
-// for tiles with earlier tickets, which are running or done; the wait is bounded all the same.
-struct ChainCtrl {
-  unsigned ticket, done, epoch;
-};
-constexpr uint32_t kChainPolls = 1u << 18;
-
-__device__ __forceinline__ unsigned long long tagged(float v, unsigned tag) {
-  return (unsigned long long)tag << 32 | __float_as_uint(v);
+// Where there are few sequences, a thread-block cluster shares one: its CTAs take chunks side by side, exchange the chunks'
+// summaries through distributed shared memory once per round, and each applies those of the chunks in front of its own to
+// the state that all of them carry - in chunk order, so the bits are the same on every run and for every cluster size.
+__device__ __forceinline__ int cluster_size() {
+  int n;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
 }
-__device__ __forceinline__ void put_sum(ulonglong2* at, float A, float H, unsigned tag) {
-  asm volatile("st.relaxed.gpu.global.v2.b64 [%0], {%1, %2};" ::"l"(at), "l"(tagged(A, tag)), "l"(tagged(H, tag)) : "memory");
+__device__ __forceinline__ int cluster_rank() {
+  int n;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(n));
+  return n;
 }
-__device__ __forceinline__ void put_end(unsigned long long* at, float s, unsigned tag) {
-  asm volatile("st.relaxed.gpu.global.b64 [%0], %1;" ::"l"(at), "l"(tagged(s, tag)) : "memory");
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ ulonglong2 get_sum(const ulonglong2* at) {
-  ulonglong2 v;
-  asm volatile("ld.relaxed.gpu.global.v2.b64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "l"(at) : "memory");
+// the value at `p` in the shared memory of CTA `rank` of the cluster
+__device__ __forceinline__ float2 cluster_read(const float2* p, int rank) {
+  uint32_t at;
+  float2 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
   return v;
-}
-__device__ __forceinline__ unsigned long long get_end(const unsigned long long* at) {
-  unsigned long long v;
-  asm volatile("ld.relaxed.gpu.global.b64 %0, [%1];" : "=l"(v) : "l"(at) : "memory");
-  return v;
-}
-__device__ __forceinline__ float value_of(unsigned long long w) { return __uint_as_float((uint32_t)w); }
-__device__ __forceinline__ bool has_tag(unsigned long long w, unsigned tag) { return (unsigned)(w >> 32) == tag; }
-
-// Which earlier chunk to start from, by one warp: lane k looks at the hint of the k-th tile back (`hint` = the nearest
-// one's, `stride` entries between them, `n` of them).  A hint is written when (most of) a tile's entries have been:
-// kind 1 = its summary, 2 = its end state; the reader of the entries still checks their tags.  -1: gave up.
-__device__ __forceinline__ int poll_hints(const unsigned long long* hint, long long stride, int n, unsigned tag) {
-  const int lane = threadIdx.x & 31;
-  for (uint32_t poll = 0; poll < kChainPolls; ++poll) {
-    const unsigned long long w = lane < n ? get_end(hint + lane * stride) : 0ull;
-    const bool mine = has_tag(w, tag);
-    const unsigned ends = __ballot_sync(0xffffffffu, mine && (unsigned)w == 2u), any = __ballot_sync(0xffffffffu, mine);
-    const int found = __ffs(ends) - 1;
-    if (found >= 0 && (any & ((1u << found) - 1u)) == (1u << found) - 1u) return found;
-    __nanosleep(20);
-  }
-  return -1;
-}
-__device__ __forceinline__ void put_hint(unsigned long long* at, unsigned kind, unsigned tag) { put_end(at, __uint_as_float(kind), tag); }
-
-// State in front of a chunk for CPW channels of a warp, from the end state `found` (< 32, the same for the whole warp) chunks
-// further back than the nearest one and the summaries in between; lane = depth group * CPW + channel.  `want`: this lane's
-// channel exists; `sum` / `end` point at the nearest chunk's entries, `stride` entries further lies the one before that.
-template <int CPW>
-__device__ __forceinline__ float look_back(bool want, const ulonglong2* sum, const unsigned long long* end, long long stride,
-                                           int found, unsigned tag, int* status) {
-  constexpr int DG = 32 / CPW;
-  const int depth = (threadIdx.x & 31) / CPW, ch = (threadIdx.x & 31) % CPW;
-  float s = 0.f;
-  bool ok = !want;
-  for (uint32_t poll = 0; poll < kChainPolls && !ok; ++poll) {
-    const unsigned long long e = get_end(end + found * stride);
-    ok = has_tag(e, tag);
-    s = value_of(e);
-  }
-  if (!ok) atomicExch(status, 1);
-  for (int k0 = found - 1; k0 >= 0; k0 -= DG) {       // the farthest first, DG at once
-    const int k = k0 - depth;
-    float A = 1.f, H = 0.f;
-    ok = !want || k < 0;
-    for (uint32_t poll = 0; poll < kChainPolls && !ok; ++poll) {
-      const ulonglong2 q = get_sum(sum + k * stride);
-      ok = has_tag(q.x, tag) && has_tag(q.y, tag);
-      A = value_of(q.x), H = value_of(q.y);
-    }
-    if (!ok) atomicExch(status, 1);
-    __syncwarp();
-    const int n = k0 + 1 < DG ? k0 + 1 : DG;
-    for (int d = 0; d < n; ++d)
-      s = fmaf(__shfl_sync(0xffffffffu, A, d * CPW + ch), s, __shfl_sync(0xffffffffu, H, d * CPW + ch));
-  }
-  return s;
-}
-
-// The same by a whole warp for one sequence: lane k looks at the k-th chunk back.
-__device__ __forceinline__ float look_back_warp(const ulonglong2* sum, const unsigned long long* end, long long stride, int n,
-                                                unsigned tag, int* status) {
-  const int lane = threadIdx.x & 31;
-  for (uint32_t poll = 0; poll < kChainPolls; ++poll) {
-    unsigned long long e = 0;
-    ulonglong2 q = make_ulonglong2(0, 0);
-    if (lane < n) {
-      e = get_end(end + lane * stride);
-      q = get_sum(sum + lane * stride);
-    }
-    const unsigned ends = __ballot_sync(0xffffffffu, lane < n && has_tag(e, tag));
-    const unsigned sums = __ballot_sync(0xffffffffu, lane < n && has_tag(q.x, tag) && has_tag(q.y, tag));
-    const int found = __ffs(ends) - 1;
-    if (found >= 0 && (sums & ((1u << found) - 1u)) == (1u << found) - 1u) {
-      float s = __shfl_sync(0xffffffffu, value_of(e), found);
-      for (int k = found - 1; k >= 0; --k)
-        s = fmaf(__shfl_sync(0xffffffffu, value_of(q.x), k), s, __shfl_sync(0xffffffffu, value_of(q.y), k));
-      return s;
-    }
-    __nanosleep(32);
-  }
-  if (lane == 0) atomicExch(status, 1);
-  return 0.f;
-}
-
-// after a CTA's last use of the chain; the last one prepares the next call (tag 0 is what a fresh workspace holds)
-__device__ __forceinline__ void leave_chain(ChainCtrl* ctrl, unsigned tag) {
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    if (atomicAdd(&ctrl->done, 1u) == gridDim.x - 1) {
-      ctrl->ticket = 0;
-      ctrl->done = 0;
-      ctrl->epoch = tag == 0xffffffffu ? 0u : tag;
-    }
-  }
 }
 
 template <typename T>
@@ -153,14 +55,9 @@ struct ScanArgs {
   long long outer, L, inner, groups, total;     // groups of VEC channels per outer entry, outer * groups
   long long in_o, in_t, gr_o, gr_t;
   long long chains;            // tiles side by side, `chunks` of them one behind the other
+  int rounds;                  // ... taken a cluster's worth at a time
   unsigned per_outer;          // chains of an outer entry
   int chunks, sigmoid;
-  // chained tiles (null: a CTA walks through its chunks by itself)
-  ChainCtrl* ctrl;
-  ulonglong2* sums;            // [chunks][outer * inner]: (A, tag), (H, tag) of a chunk
-  unsigned long long* ends;    // [chunks][outer * inner]: (state behind a chunk, tag)
-  unsigned long long* hints;   // [chunks][chains] (columns)
-  int* status;
 };
 
 // a = 1 / (1 + e^-g) and b = 1 - a = e^-g / (1 + e^-g), both without cancellation.  The exponent is kept below 2^126 (a NaN
@@ -192,8 +89,8 @@ __device__ __forceinline__ long long clamp_len(const int* lengths, long long o, 
 
 // ------------------------------------------------------------------------------------------------ columns
 // [outer][L][inner], inner contiguous.  A tile is TX groups of VEC channels times SLOTS runs of R steps, a run per thread.
-// Long sequences: the tiles of one outer entry lie side by side over its channels (a chain of chunks each).  Short ones
-// (one tile holds them): groups run on across outer entries, so that few channels fill a CTA too.
+// Long sequences: the tiles of one outer entry lie side by side over its channels; a CTA (or a cluster) walks along L.
+// Short ones (one tile holds them): groups run on across outer entries, so that few channels fill a CTA too.
 template <int VEC_, int R_, int SLOTS_>
 struct ColShape {
   static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_;
@@ -203,7 +100,7 @@ struct ColShape {
   static constexpr int JOIN = SLOTS >= DG ? SLOTS / DG : 1;
 };
 constexpr int kColTile = 256;     // steps of a long sequence's tile, and between saved states
-enum ColMode { kOneTile = 0, kColWalk = 1, kColChained = 2 };
+enum ColMode { kOneTile = 0, kLong = 1 };
 
 // joins (A, H) over the DG lanes of a channel, in lane order (UP) or against it; returns the summary of all of them and
 // leaves in (A, H) that of the lanes before this one
@@ -260,112 +157,87 @@ struct ColSlots {
   static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 };
 
-// Where a tile lies.  Long sequences: the same for all threads of the CTA.
-struct ColTile {
-  int c;               // chunk
-  unsigned o;          // outer entry
-  long long g0;        // first group in it
-  int end;             // steps of the sequence
-};
-
-template <typename T, class S, int MODE>
-__device__ __forceinline__ ColTile col_tile(const ScanArgs<T>& p, unsigned chain, int c) {
-  ColTile t;
-  t.c = c;
-  t.o = MODE == kOneTile ? 0u : chain / p.per_outer;
-  t.g0 = (long long)(MODE == kOneTile ? chain : chain - t.o * p.per_outer) * S::TX;
-  t.end = MODE == kOneTile ? 0 : (int)clamp_len(p.lengths, t.o, p.L);
-  return t;
-}
-
 // A group of a tile: its outer entry, first channel and steps (0: no such group)
 struct ColGroup {
   long long o;
   int i0, end;
   bool live;
 };
+// group x of tile `tile`
 template <typename T, class S, int MODE>
-__device__ __forceinline__ ColGroup col_group(const ScanArgs<T>& p, const ColTile& t, int x) {
+__device__ __forceinline__ ColGroup col_group(const ScanArgs<T>& p, unsigned tile, int x) {
   ColGroup g;
   if (MODE == kOneTile) {
-    const long long gid = t.g0 + x;
+    const long long gid = (long long)tile * S::TX + x;
     g.live = gid < p.total;
     g.o = g.live ? (p.total <= 0xffffffffll ? (long long)((unsigned)gid / (unsigned)p.groups) : gid / p.groups) : 0;
     g.i0 = g.live ? (int)(gid - g.o * p.groups) * S::VEC : 0;
-    g.end = g.live ? (int)clamp_len(p.lengths, g.o, p.L) : 0;
   } else {
-    g.live = t.g0 + x < p.groups;
-    g.o = t.o;
-    g.i0 = g.live ? (int)(t.g0 + x) * S::VEC : 0;
-    g.end = g.live ? t.end : 0;
+    g.o = tile / p.per_outer;
+    const long long at = (long long)(tile - (unsigned)g.o * p.per_outer) * S::TX + x;
+    g.live = at < p.groups;
+    g.i0 = g.live ? (int)at * S::VEC : 0;
   }
+  g.end = g.live ? (int)clamp_len(p.lengths, g.o, p.L) : 0;
   return g;
 }
 
-// The chained tiles of a CTA: by ticket, the next tile's ticket drawn and its loads started while a tile is worked on (a
-// held ticket waits for earlier ones only, so the earliest unfinished tile is always being worked on).
-struct ColDraw {
-  ColTile tile;
-  unsigned chain, tag;
-  int more;            // the ticket is a tile
-};
-
-template <typename T, class S, bool BACK>
-__device__ __forceinline__ void draw_tile(const ScanArgs<T>& p, unsigned ticket, ColDraw* out) {
-  const unsigned chains = (unsigned)p.chains;
-  const unsigned n = ticket / chains;
-  out->more = n < (unsigned)p.chunks;
-  out->chain = ticket - n * chains;
-  if (out->more) out->tile = col_tile<T, S, kColChained>(p, out->chain, BACK ? p.chunks - 1 - (int)n : (int)n);
+// What the chunks of a round leave behind: `all` = this CTA's chunk, `state` = in front of the round (then: behind it).
+// Returns the state in front of this CTA's chunk.  A lane of depth group d reads the d-th CTA's summary.
+template <class S>
+__device__ __forceinline__ float join_round(const float2 all, float& state, float2 (*box)[S::W], int round, int size, int rank, int jx) {
+  static_assert(S::DG >= 8, "a depth group per CTA of the largest cluster");
+  if (size == 1) {
+    const float start = state;
+    state = fmaf(all.x, state, all.y);
+    return start;
+  }
+  const int lane = threadIdx.x & 31, d = lane / S::CPW, ch = lane % S::CPW;
+  float2* mine = box[round & 1];          // (two boxes: a CTA may be a round ahead of a reader)
+  if (d == 0) mine[jx] = all;
+  cluster_sync();
+  float2 m = make_float2(1.f, 0.f);
+  if (d < size) m = cluster_read(mine + jx, d);
+  float start = 0.f;
+  for (int k = 0; k < size; ++k) {
+    if (k == rank) start = state;
+    state = fmaf(__shfl_sync(0xffffffffu, m.x, k * S::CPW + ch), state, __shfl_sync(0xffffffffu, m.y, k * S::CPW + ch));
+  }
+  return start;
 }
 
 template <typename T, class S, int MODE>
 __global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
-  constexpr bool CHAIN = MODE == kColChained;
   using Slots = ColSlots<T, S, 2>;
   __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];     // (A, H) of every run; then its first state in x
-  __shared__ ColDraw drawn[2];
-  __shared__ int depth_s;
+  __shared__ float2 box[2][SLOTS > 1 ? W : 1];
   extern __shared__ __align__(16) unsigned char raw[];
   const Slots slots{raw};
   pdl_trigger();
   pdl_wait();
-  ColTile tile;
-  unsigned tag = 0, chain = blockIdx.x;
-  bool go = true;
-  if (CHAIN) {
-    if (threadIdx.x == 0) {
-      drawn[1].tag = *(volatile unsigned*)&p.ctrl->epoch + 1u;
-      draw_tile<T, S, false>(p, atomicAdd(&p.ctrl->ticket, 1u), &drawn[1]);
-    }
-    __syncthreads();
-    tag = drawn[1].tag, tile = drawn[1].tile, chain = drawn[1].chain, go = drawn[1].more != 0;
-  } else {
-    tile = col_tile<T, S, MODE>(p, chain, 0);
-  }
+  const int size = MODE == kLong ? cluster_size() : 1, rank = MODE == kLong ? cluster_rank() : 0;
+  const unsigned tile = blockIdx.x / size;
   const int slot = threadIdx.x / S::TX, x = threadIdx.x % S::TX;
   const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
   const long long states = p.outer * p.inner;
   const int lane = threadIdx.x & 31;
   const int jx = (threadIdx.x / 32) * S::CPW + lane % S::CPW, jq = lane / S::CPW * S::JOIN;   // while joining: channel, first run
   const bool first = lane < S::CPW;
-  auto fetch = [&](const ColTile& t) {
-    const ColGroup g = col_group<T, S, MODE>(p, t, x);
-    const int t0 = t.c * LC + slot * R;
-    const long long from = g.o * p.in_o + g.i0 + t0 * p.in_t;
-    slots.fetch(0, p.v + from, p.in_t, g.end - t0, none_v);
-    slots.fetch(1, p.g + from, p.in_t, g.end - t0, none_g);
+  const ColGroup at = col_group<T, S, MODE>(p, tile, x), jg = col_group<T, S, MODE>(p, tile, jx / VEC);
+  const long long ch = jg.o * p.inner + jg.i0 + jx % VEC;
+  auto fetch = [&](int c) {
+    const int t0 = c * LC + slot * R;
+    const long long from = at.o * p.in_o + at.i0 + t0 * p.in_t;
+    slots.fetch(0, p.v + from, p.in_t, at.end - t0, none_v);
+    slots.fetch(1, p.g + from, p.in_t, at.end - t0, none_g);
   };
-  if (go) fetch(tile);
-  float state = 0.f;
+  fetch(rank);
+  float state = SLOTS > 1 && jg.live && p.h0 != nullptr ? p.h0[ch] : 0.f;
 
 #pragma unroll 1
-  while (go) {
-    const int c = tile.c;
-    const ColGroup at = col_group<T, S, MODE>(p, tile, x);
-    unsigned draw = 0;
-    if (CHAIN && threadIdx.x == 0) draw = atomicAdd(&p.ctrl->ticket, 1u);
+  for (int round = 0; round < p.rounds; ++round) {
+    const int c = round * size + rank;
     float a[R][VEC], u[R][VEC], s[VEC];
     Slots::wait();
 #pragma unroll
@@ -379,9 +251,6 @@ __global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_
         u[r][j] *= vv[j];
       }
     }
-    ColTile next;
-    unsigned next_chain = 0;
-    bool more_tiles = false;
     if constexpr (SLOTS == 1) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) s[j] = at.live && p.h0 != nullptr ? p.h0[at.o * p.inner + at.i0 + j] : 0.f;
@@ -396,19 +265,8 @@ __global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_
         }
         runs[slot][x * VEC + j] = make_float2(A, H);
       }
-      if (CHAIN && threadIdx.x == 0) draw_tile<T, S, false>(p, draw, &drawn[0]);
       __syncthreads();
-      if (CHAIN) {        // the next tile's values are on their way from here on
-        next = drawn[0].tile, next_chain = drawn[0].chain, more_tiles = drawn[0].more != 0;
-      } else {
-        next = tile;
-        ++next.c;
-        more_tiles = next.c < p.chunks;
-      }
-      if (more_tiles) fetch(next);
-      const ColGroup jg = col_group<T, S, MODE>(p, tile, jx / VEC);
-      const long long ch = jg.o * p.inner + jg.i0 + jx % VEC;
-      if (c == 0) state = jg.live && p.h0 != nullptr ? p.h0[ch] : 0.f;
+      if (MODE == kLong && round + 1 < p.rounds) fetch(c + size);      // the next chunk's values are on their way from here on
       float A = 1.f, H = 0.f;
       float2 m[S::JOIN];
 #pragma unroll
@@ -418,36 +276,21 @@ __global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_
         H = fmaf(m[q].x, H, m[q].y);
       }
       const float2 all = join_lanes<S::CPW, true>(A, H);
-      // a chunk in which a sequence has no step leaves its state alone, and nobody waits for it
+      float start = state;
+      if constexpr (MODE == kLong) start = join_round<S>(all, state, box, round, size, rank, jx);
+      else state = fmaf(all.x, state, all.y);
+      float run = fmaf(A, start, H);
+      // (a chunk in which a sequence has no step leaves its state alone)
       const bool active = c * LC < jg.end, more = (c + 1) * (long long)LC < jg.end;
-      const long long entry = c * states + ch;
-      if (CHAIN && c > 0 && c * LC < tile.end) {
-        if (more && first) put_sum(p.sums + entry, all.x, all.y, tag);
-        if (threadIdx.x < 32) {
-          unsigned long long* hint = p.hints + (long long)c * p.chains + chain;
-          if (threadIdx.x == 0) put_hint(hint, 1u, tag);
-          const int d = poll_hints(hint - p.chains, -p.chains, c, tag);
-          if (threadIdx.x == 0) {
-            depth_s = d < 0 ? 0 : d;
-            if (d < 0) atomicExch(p.status, 1);
-          }
-        }
-        __syncthreads();
-        state = look_back<S::CPW>(active, p.sums + entry - states, p.ends + entry - states, -states, depth_s, tag, p.status);
+      if (first && jg.live && (active || c == 0)) {
+        if (MODE == kLong && p.ckpt != nullptr) p.ckpt[c * states + ch] = start;
+        if (!more && p.h_last != nullptr) p.h_last[ch] = fmaf(all.x, start, all.y);
       }
-      float run = fmaf(A, state, H);
-      if (MODE != kOneTile && p.ckpt != nullptr && first && jg.live && (active || c == 0)) p.ckpt[entry] = run;
 #pragma unroll
       for (int q = 0; q < S::JOIN; ++q) {
         runs[jq + q][jx].x = run;
         run = fmaf(m[q].x, run, m[q].y);
       }
-      state = fmaf(all.x, state, all.y);
-      if (first && jg.live) {
-        if (CHAIN && more) put_end(p.ends + entry, state, tag);
-        if ((active || c == 0) && !more && p.h_last != nullptr) p.h_last[ch] = state;
-      }
-      if (CHAIN && threadIdx.x == 0) put_hint(p.hints + (long long)c * p.chains + chain, 2u, tag);
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < VEC; ++j) s[j] = runs[slot][x * VEC + j].x;
@@ -471,70 +314,50 @@ __global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_
     }
     if (MODE == kOneTile) return;
     __syncthreads();       // the runs' states are read before the next chunk's summaries replace them
-    tile = next, chain = CHAIN ? next_chain : chain, go = more_tiles;
   }
-  if (CHAIN) leave_chain(p.ctrl, tag);
+  if (size > 1) cluster_sync();       // nobody leaves while its box may be read
 }
 
 template <typename T, class S, int MODE>
 __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
-  constexpr bool CHAIN = MODE == kColChained;
   using Slots = ColSlots<T, S, 3>;
   // (A, H) and D of every run; then the state in front of it (x) and the gradient that comes to it from behind
   __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
   __shared__ float backs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
-  __shared__ ColDraw drawn[2];
-  __shared__ int depth_s;
+  __shared__ float2 box[2][SLOTS > 1 ? W : 1];
   extern __shared__ __align__(16) unsigned char raw[];
   const Slots slots{raw};
   pdl_trigger();
   pdl_wait();
-  ColTile tile;
-  unsigned tag = 0, chain = blockIdx.x;
-  bool go = true;
-  if (CHAIN) {
-    if (threadIdx.x == 0) {
-      drawn[1].tag = *(volatile unsigned*)&p.ctrl->epoch + 1u;
-      draw_tile<T, S, true>(p, atomicAdd(&p.ctrl->ticket, 1u), &drawn[1]);
-    }
-    __syncthreads();
-    tag = drawn[1].tag, tile = drawn[1].tile, chain = drawn[1].chain, go = drawn[1].more != 0;
-  } else {
-    tile = col_tile<T, S, MODE>(p, chain, p.chunks - 1);        // chunks from the last to the first
-  }
+  const int size = MODE == kLong ? cluster_size() : 1, rank = MODE == kLong ? cluster_rank() : 0;
+  const unsigned tile = blockIdx.x / size;
   const int slot = threadIdx.x / S::TX, x = threadIdx.x % S::TX;
   const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
   const long long states = p.outer * p.inner;
   const int lane = threadIdx.x & 31;
   const int jx = (threadIdx.x / 32) * S::CPW + lane % S::CPW, jq = lane / S::CPW * S::JOIN;   // while joining: channel, first run
   const bool first = lane < S::CPW;
-  auto fetch = [&](const ColTile& t) {
-    const ColGroup g = col_group<T, S, MODE>(p, t, x);
-    const int t0 = t.c * LC + slot * R;
-    const long long from = g.o * p.in_o + g.i0 + t0 * p.in_t;
-    slots.fetch(0, p.v + from, p.in_t, g.end - t0, none_v);
-    slots.fetch(1, p.g + from, p.in_t, g.end - t0, none_g);
-    slots.fetch(2, p.gh + (g.o * p.L + t0) * p.inner + g.i0, p.inner, g.end - t0, none_v);
+  const ColGroup at = col_group<T, S, MODE>(p, tile, x), jg = col_group<T, S, MODE>(p, tile, jx / VEC);
+  const long long ch = jg.o * p.inner + jg.i0 + jx % VEC;
+  // chunks from the last to the first; a chunk before the first has no steps
+  auto fetch = [&](int c) {
+    const int t0 = c * LC + slot * R, end = c < 0 ? t0 : at.end;
+    const long long from = at.o * p.in_o + at.i0 + t0 * p.in_t;
+    slots.fetch(0, p.v + from, p.in_t, end - t0, none_v);
+    slots.fetch(1, p.g + from, p.in_t, end - t0, none_g);
+    slots.fetch(2, p.gh + (at.o * p.L + t0) * p.inner + at.i0, p.inner, end - t0, none_v);
   };
-  if (go) fetch(tile);
-  float grad = 0.f;
+  fetch(p.chunks - 1 - rank);
+  float grad = SLOTS > 1 && jg.live && p.g_last != nullptr ? p.g_last[ch] : 0.f;
 
 #pragma unroll 1
-  while (go) {
-    const int c = tile.c;
-    const ColGroup at = col_group<T, S, MODE>(p, tile, x);
-    unsigned draw = 0;
-    if (CHAIN && threadIdx.x == 0) draw = atomicAdd(&p.ctrl->ticket, 1u);
-    const ColGroup jg = col_group<T, S, MODE>(p, tile, jx / VEC);
-    const long long ch = jg.o * p.inner + jg.i0 + jx % VEC, entry = c * states + ch;
-    const int last = jg.end > 0 ? (jg.end - 1) / LC : 0;     // the chunk of the sequence's last step
-    const bool active = c * LC < jg.end, mine = SLOTS > 1 && jg.live && (active || c == 0);
+  for (int round = 0; round < p.rounds; ++round) {
+    const int c = p.chunks - 1 - (round * size + rank);
     float before = 0.f;      // the state in front of the chunk: saved, or the sequence's own beginning
-    if (mine) {
-      if (MODE != kOneTile && p.ckpt != nullptr) before = p.ckpt[entry];
+    if (SLOTS > 1 && jg.live && c >= 0 && (c * LC < jg.end || c == 0)) {
+      if (MODE == kLong && p.ckpt != nullptr) before = p.ckpt[c * states + ch];
       else if (p.h0 != nullptr) before = p.h0[ch];
-      if (c >= last) grad = p.g_last != nullptr ? p.g_last[ch] : 0.f;
     }
     Slots::wait();
     // q: 1 - a (sigmoid) or a (decay); a is formed again where it is used
@@ -556,9 +379,6 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(con
         }
       }
     }
-    ColTile next;
-    unsigned next_chain = 0;
-    bool more_tiles = false;
     if constexpr (SLOTS == 1) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
@@ -588,16 +408,8 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(con
       }
 #pragma unroll
       for (int j = 0; j < VEC; ++j) backs[slot][x * VEC + j] = D[j];
-      if (CHAIN && threadIdx.x == 0) draw_tile<T, S, true>(p, draw, &drawn[0]);
       __syncthreads();
-      if (CHAIN) {        // the next tile's values are on their way from here on
-        next = drawn[0].tile, next_chain = drawn[0].chain, more_tiles = drawn[0].more != 0;
-      } else {
-        next = tile;
-        --next.c;
-        more_tiles = next.c >= 0;
-      }
-      if (more_tiles) fetch(next);
+      if (MODE == kLong && round + 1 < p.rounds) fetch(c - size);      // the next chunk's values are on their way from here on
       float A = 1.f, H = 0.f, B = 1.f, E = 0.f;
       float2 m[S::JOIN];
       float md[S::JOIN];
@@ -613,39 +425,21 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(con
       B = A;
       join_lanes<S::CPW, true>(A, H);
       const float2 all = join_lanes<S::CPW, false>(B, E);
-      if (CHAIN && tile.end > 0 && c < (tile.end - 1) / LC) {
-        if (jg.live && c > 0 && first) put_sum(p.sums + entry, all.x, all.y, tag);
-        if (threadIdx.x < 32) {
-          unsigned long long* hint = p.hints + (long long)c * p.chains + chain;
-          if (threadIdx.x == 0) put_hint(hint, 1u, tag);
-          const int n = (tile.end - 1) / LC - c;
-          const int dd = poll_hints(hint + p.chains, p.chains, n, tag);
-          if (threadIdx.x == 0) {
-            depth_s = dd < 0 ? 0 : dd;
-            if (dd < 0) atomicExch(p.status, 1);
-          }
-        }
-        __syncthreads();
-        grad = look_back<S::CPW>(jg.live, p.sums + entry + states, p.ends + entry + states, states, depth_s, tag, p.status);
-      }
+      float behind = grad;
+      if constexpr (MODE == kLong) behind = join_round<S>(all, grad, box, round, size, rank, jx);
+      if (c == 0 && jg.live && first && p.gh0 != nullptr) p.gh0[ch] = fmaf(all.x, behind, all.y);
       float run = fmaf(A, before, H);
 #pragma unroll
       for (int k = 0; k < S::JOIN; ++k) {
         runs[jq + k][jx].x = run;
         run = fmaf(m[k].x, run, m[k].y);
       }
-      run = fmaf(B, grad, E);
+      run = fmaf(B, behind, E);
 #pragma unroll
       for (int k = S::JOIN - 1; k >= 0; --k) {
         backs[jq + k][jx] = run;
         run = fmaf(m[k].x, run, md[k]);
       }
-      if (mine) grad = fmaf(all.x, grad, all.y);
-      if (mine && first) {
-        if (CHAIN && c > 0) put_end(p.ends + entry, grad, tag);
-        if (c == 0 && p.gh0 != nullptr) p.gh0[ch] = grad;
-      }
-      if (CHAIN && threadIdx.x == 0) put_hint(p.hints + (long long)c * p.chains + chain, 2u, tag);
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < VEC; ++j) s[j] = runs[slot][x * VEC + j].x, d[j] = backs[slot][x * VEC + j];
@@ -659,7 +453,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(con
         v[r][j] = p.sigmoid ? (s[j] - v[r][j]) * (a * q[r][j]) : s[j];
         s[j] = fmaf(a, s[j], u);
       }
-    const int t0 = c * LC + slot * R, left = at.live ? (int)p.L - t0 : 0;
+    const int t0 = c * LC + slot * R, left = at.live && c >= 0 ? (int)p.L - t0 : 0;
     const long long back = at.o * p.gr_o + at.i0 + (t0 + R - 1) * p.gr_t;
     T *gv = p.gv + back, *gg = p.gg + back;
 #pragma unroll
@@ -690,9 +484,8 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(con
     }
     if (MODE == kOneTile) return;
     __syncthreads();
-    tile = next, chain = CHAIN ? next_chain : chain, go = more_tiles;
   }
-  if (CHAIN) leave_chain(p.ctrl, tag);
+  if (size > 1) cluster_sync();
 }
 
 // ------------------------------------------------------------------------------------------------ rows
@@ -706,7 +499,7 @@ constexpr int kUnit = 512, kRowWarps = 8;
 // steps of a chunk (a chunk of odd rows leaves room for a shifted beginning)
 __host__ __device__ constexpr int row_chunk(long long L) { return L % 8 == 0 ? kUnit : kUnit - 8; }
 
-enum RowMode { kWholeRows = 0, kWalk = 1, kChained = 2 };
+enum RowMode { kWholeRows = 0, kWalk = 1, kTeam = 2 };
 
 // Vector k of a unit: its first element's index (below 0 in front of the unit) and step, and the element that is a row's
 // first step (V: none; at most one, since L >= V).
@@ -806,14 +599,15 @@ __device__ __forceinline__ bool segmented_scan(float& A, float& H, unsigned mark
   return fresh;
 }
 
-// the unit of this warp; false if there is none.  `c` = its chunk, counted from the front.
-template <class U, typename T, int MODE, bool BACK>
-__device__ __forceinline__ bool first_unit(const ScanArgs<T>& p, U& u, int& c, unsigned& tag) {
-  const long long id = (long long)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+// the first unit of this warp; false if there is none.  A team (the warps of a cluster) shares a row: `me` of `members`.
+template <class U, typename T, int MODE>
+__device__ __forceinline__ bool first_unit(const ScanArgs<T>& p, U& u, int& me, int& members) {
+  const int warp = threadIdx.x >> 5;
+  const long long id = (long long)blockIdx.x * kRowWarps + warp;
   u.L = (int)p.L;
   u.magic = 0xffffffffu / (uint32_t)p.L + 1u;
   u.span = MODE == kWholeRows ? (u.L + U::V - 2) / U::V + 1 : 32;
-  c = 0, tag = 0;
+  me = 0, members = 1;
   if (MODE == kWholeRows) {
     u.row0 = id * p.groups;                       // groups: rows of a unit
     if (u.row0 >= p.outer) return false;
@@ -822,45 +616,41 @@ __device__ __forceinline__ bool first_unit(const ScanArgs<T>& p, U& u, int& c, u
   } else if (MODE == kWalk) {
     if (id >= p.outer) return false;
     u.row0 = id;
-    c = BACK ? p.chunks - 1 : 0;
   } else {
-    if (id >= p.outer * p.chunks) return false;   // as many tickets as units
-    unsigned t = 0;
-    if ((threadIdx.x & 31) == 0) {
-      tag = *(volatile unsigned*)&p.ctrl->epoch + 1u;
-      t = atomicAdd(&p.ctrl->ticket, 1u);
-    }
-    tag = __shfl_sync(0xffffffffu, tag, 0);
-    t = __shfl_sync(0xffffffffu, t, 0);
-    u.row0 = t % (unsigned)p.outer;
-    c = (int)(t / (unsigned)p.outer);
-    if (BACK) c = p.chunks - 1 - c;
+    const int size = cluster_size();
+    me = cluster_rank() * kRowWarps + warp, members = size * kRowWarps;
+    u.row0 = blockIdx.x / size;
   }
   return true;
+}
+// One round of a team: as join_round, a lane per member (at most 32).
+__device__ __forceinline__ float join_team(const float2 all, float& state, float2 (*box)[kRowWarps], int round, int me, int members) {
+  const int lane = threadIdx.x & 31;
+  float2* mine = box[round & 1];
+  if (lane == 0) mine[threadIdx.x >> 5] = all;
+  if (members > kRowWarps) cluster_sync(); else __syncthreads();
+  float A = 1.f, H = 0.f;
+  if (lane < members) {
+    const float2 m = members > kRowWarps ? cluster_read(mine + lane % kRowWarps, lane / kRowWarps) : mine[lane];
+    A = m.x, H = m.y;
+  }
+  segmented_scan<true>(A, H, 0u, 32);
+  const float s = fmaf(A, state, H);               // behind member `lane`
+  const float start = me == 0 ? state : __shfl_sync(0xffffffffu, s, me > 0 ? me - 1 : 0);
+  state = __shfl_sync(0xffffffffu, s, 31);
+  return start;
 }
 template <class U, typename T, int MODE>
 __device__ __forceinline__ void place_unit(const ScanArgs<T>& p, U& u, int c) {
   if (MODE != kWholeRows) {
     const int step = row_chunk(p.L);
     u.t0 = c * step;
-    u.n = (int)(p.L - u.t0 < step ? p.L - u.t0 : step);
+    u.n = c < 0 || u.t0 >= p.L ? 0 : (int)(p.L - u.t0 < step ? p.L - u.t0 : step);     // (no chunk there: no elements)
+    if (u.n == 0) u.t0 = 0;
   }
   // rows that begin off a vector: only contiguous tensors are read wide then, all with the same shift
   u.shift = p.L % U::V == 0 ? 0 : (int)((u.row0 * p.L + u.t0) % U::V);
 }
-template <typename T>
-__device__ __forceinline__ void leave_unit(const ScanArgs<T>& p, unsigned tag) {
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) {
-    __threadfence();
-    if (atomicAdd(&p.ctrl->done, 1u) == (unsigned)(p.outer * p.chunks) - 1u) {
-      p.ctrl->ticket = 0;
-      p.ctrl->done = 0;
-      p.ctrl->epoch = tag == 0xffffffffu ? 0u : tag;
-    }
-  }
-}
-
 template <typename T, bool WIDE, int MODE, bool RAGGED>
 __global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const ScanArgs<T> p) {
   using U = RowUnit<T, WIDE, MODE, RAGGED>;
@@ -868,16 +658,17 @@ __global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const Scan
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31;
+  __shared__ float2 box[2][kRowWarps];
   U u;
-  int c;
-  unsigned tag;
-  if (!first_unit<U, T, MODE, false>(p, u, c, tag)) return;
+  int me, members;
+  if (!first_unit<U, T, MODE>(p, u, me, members)) return;
   const long long end = MODE == kWholeRows ? p.L : clamp_len(p.lengths, u.row0, p.L);
   const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
   float carry = 0.f;
-  if (MODE != kWholeRows && c == 0 && p.h0 != nullptr) carry = p.h0[u.row0];
+  if (MODE != kWholeRows && p.h0 != nullptr) carry = p.h0[u.row0];
 #pragma unroll 1
-  for (;; ++c) {
+  for (int round = 0; round < p.rounds; ++round) {
+    const int c = round * members + me;
     place_unit<U, T, MODE>(p, u, c);
     typename U::Vec x[K];
     int row[K];
@@ -909,16 +700,18 @@ __global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const Scan
       }
       fresh[k] = segmented_scan<true>(A[k], H[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, x[k].spos < V) : 0u, u.span);
     }
-    const bool active = MODE == kWholeRows || u.t0 < end, more = MODE != kWholeRows && u.t0 + u.n < end;
+    const bool active = MODE == kWholeRows || (u.n > 0 && u.t0 < end), more = MODE != kWholeRows && u.t0 + u.n < end;
     const long long at = (long long)c * p.outer + u.row0;
-    if (MODE == kChained && active && c > 0) {
-      if (more) {           // the whole chunk's summary, the vectors joined in order
-        float tA = 1.f, tH = 0.f;
+    float after = 0.f;            // the state that the team carries on
+    if (MODE == kTeam) {          // the whole chunk's summary, the vectors joined in order
+      float tA = 1.f, tH = 0.f;
 #pragma unroll
-        for (int k = 0; k < K; ++k) tH = fmaf(A[k], tH, H[k]), tA *= A[k];
-        if (lane == 31) put_sum(p.sums + at, tA, tH, tag);
+      for (int k = 0; k < K; ++k) {
+        const float A1 = __shfl_sync(0xffffffffu, A[k], 31), H1 = __shfl_sync(0xffffffffu, H[k], 31);
+        tH = fmaf(A1, tH, H1), tA *= A1;
       }
-      carry = look_back_warp(p.sums + at - p.outer, p.ends + at - p.outer, -p.outer, c, tag, p.status);
+      after = carry;
+      carry = join_team(make_float2(tA, tH), after, box, round, me, members);
     }
     if (MODE != kWholeRows && p.ckpt != nullptr && lane == 0 && (active || c == 0)) p.ckpt[at] = carry;
     float in[K];
@@ -929,7 +722,6 @@ __global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const Scan
       if (lane == 0) in[k] = carry;
       carry = __shfl_sync(0xffffffffu, s, 31);
     }
-    if (MODE == kChained && more && lane == 0) put_end(p.ends + at, carry, tag);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float s = in[k], last = 0.f;
@@ -944,9 +736,9 @@ __global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const Scan
       if (p.h_last != nullptr && u.ends(x[k])) p.h_last[u.row0 + row[k]] = u.L - x[k].t == V ? s : last;
     }
     if (MODE != kWholeRows && lane == 0 && p.h_last != nullptr && ((active && !more) || (c == 0 && end == 0))) p.h_last[u.row0] = carry;
-    if (MODE != kWalk || c + 1 == p.chunks) break;
+    if (MODE == kTeam) carry = after;
   }
-  if (MODE == kChained) leave_unit(p, tag);
+  if (MODE == kTeam && members > kRowWarps) cluster_sync();       // nobody leaves while its box may be read
 }
 
 template <typename T, bool WIDE, int MODE, bool RAGGED>
@@ -956,17 +748,17 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31;
+  __shared__ float2 box[2][kRowWarps];
   U u;
-  int c;
-  unsigned tag;
-  if (!first_unit<U, T, MODE, true>(p, u, c, tag)) return;
+  int me, members;
+  if (!first_unit<U, T, MODE>(p, u, me, members)) return;
   const long long end = MODE == kWholeRows ? p.L : clamp_len(p.lengths, u.row0, p.L);
-  const int last = end > 0 ? (int)((end - 1) / row_chunk(p.L)) : 0;      // the chunk of the row's last step
   const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
   float carry = 0.f;
   if (MODE != kWholeRows && p.g_last != nullptr) carry = p.g_last[u.row0];
 #pragma unroll 1
-  for (;; --c) {
+  for (int round = 0; round < p.rounds; ++round) {
+    const int c = p.chunks - 1 - (round * members + me);
     place_unit<U, T, MODE>(p, u, c);
     typename U::Vec x[K];
     int row[K];
@@ -984,7 +776,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
       if (u.ends(x[k]) && p.g_last != nullptr) glv[k] = p.g_last[u.row0 + row[k]];
       if (RAGGED) live[k] = u.steps(x[k], row[k], p.lengths, end);
     }
-    const bool active = MODE == kWholeRows || u.t0 < end;
+    const bool active = MODE == kWholeRows || (u.n > 0 && u.t0 < end);
     const long long at = (long long)c * p.outer + u.row0;
     float start = 0.f;            // the state in front of the chunk: saved, or the row's own beginning
     if (MODE != kWholeRows && (active || c == 0)) start = p.ckpt != nullptr ? p.ckpt[at] : p.h0 != nullptr ? p.h0[u.row0] : 0.f;
@@ -1011,14 +803,16 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
       fresh_up[k] = segmented_scan<true>(A[k], H[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, x[k].spos < V) : 0u, u.span);
       fresh_down[k] = segmented_scan<false>(B[k], D[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, u.ends(x[k])) : 0u, u.span);
     }
-    if (MODE == kChained && active && c < last) {
-      if (c > 0) {
-        float tA = 1.f, tD = 0.f;
+    float after = 0.f;
+    if (MODE == kTeam) {
+      float tA = 1.f, tD = 0.f;
 #pragma unroll
-        for (int k = K - 1; k >= 0; --k) tD = fmaf(B[k], tD, D[k]), tA *= B[k];
-        if (lane == 0) put_sum(p.sums + at, tA, tD, tag);
+      for (int k = K - 1; k >= 0; --k) {
+        const float B1 = __shfl_sync(0xffffffffu, B[k], 0), D1 = __shfl_sync(0xffffffffu, D[k], 0);
+        tD = fmaf(B1, tD, D1), tA *= B1;
       }
-      carry = look_back_warp(p.sums + at + p.outer, p.ends + at + p.outer, p.outer, last - c, tag, p.status);
+      after = carry;
+      carry = join_team(make_float2(tA, tD), after, box, round, me, members);
     }
     float in[K], din[K];
 #pragma unroll
@@ -1035,7 +829,6 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
       if (lane == 31) din[k] = carry;
       carry = __shfl_sync(0xffffffffu, d, 0);
     }
-    if (MODE == kChained && active && c > 0 && lane == 0) put_end(p.ends + at, carry, tag);
     if (MODE != kWholeRows && c == 0 && lane == 0 && p.gh0 != nullptr) p.gh0[u.row0] = carry;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -1062,9 +855,9 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
       u.store(og, x[k], row[k], p.gg + u.row0 * p.gr_o + u.t0, p.gr_o);
       if (u.starts(x[k]) && p.gh0 != nullptr) p.gh0[u.row0 + row[k] + (x[k].t > 0 ? 1 : 0)] = g0;
     }
-    if (MODE != kWalk || c == 0) break;
+    if (MODE == kTeam) carry = after;
   }
-  if (MODE == kChained) leave_unit(p, tag);
+  if (MODE == kTeam && members > kRowWarps) cluster_sync();
 }
 
 // length 0: the state passes through
@@ -1075,39 +868,44 @@ __global__ void __launch_bounds__(256) scan_copy_kernel(const float* __restrict_
     out[i] = in != nullptr ? in[i] : 0.f;
 }
 
-// bytes in front of the chain's entries: status word, then its control words
-constexpr size_t kChainHead = kStatusBytes + 256;
-
-// Whether the chunks of a sequence become chained tiles (true) or a CTA walks through them (false): see the rule below.
-bool chained(long long ctas, long long chunks, long long tiles) {
-  return chunks > 1 && tiles <= 0x7fffffff && ctas < 4 * (long long)num_sms();
+// CTAs of a cluster that shares a sequence: enough that all of them together fill the GPU twice, no more than there are
+// chunks, at most `most`.
+int cluster_for(long long tiles, long long chunks, int most) {
+  int n = 1;
+  while (n < most && n < chunks && tiles * n < 2 * (long long)num_sms()) n *= 2;
+  return n;
 }
 
-template <typename T>
-void chain(ScanArgs<T>& p, const ScanCall& c) {
-  unsigned char* ws = static_cast<unsigned char*>(c.workspace);
-  p.ctrl = reinterpret_cast<ChainCtrl*>(ws + kStatusBytes);
-  p.sums = reinterpret_cast<ulonglong2*>(ws + kChainHead);
-  p.ends = reinterpret_cast<unsigned long long*>(p.sums + (long long)p.chunks * c.outer * c.inner);
-  p.hints = p.ends + (long long)p.chunks * c.outer * c.inner;
-  p.status = reinterpret_cast<int*>(ws);
+template <typename Kern, typename Args>
+cudaError_t launch_clusters(Kern kern, long long tiles, int cluster, int threads, size_t smem, cudaStream_t st, const Args& p) {
+  if (tiles * cluster > 0x7fffffff) return cudaErrorNotSupported;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * cluster));
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
 template <typename T, class S, int MODE, bool BACK>
-cudaError_t launch_cols_kernel(const ScanArgs<T>& p, cudaStream_t st) {
+cudaError_t launch_cols_kernel(const ScanArgs<T>& p, int cluster, cudaStream_t st) {
   void (*kern)(const ScanArgs<T>);
   constexpr size_t smem = ColSlots<T, S, BACK ? 3 : 2>::SMEM;
   if constexpr (BACK) kern = scan_cols_backward_kernel<T, S, MODE>;
   else kern = scan_cols_kernel<T, S, MODE>;
   static std::atomic<uint64_t> allowed{0};
-  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), smem + 4096 + sizeof(float) * 3 * S::SLOTS * S::W, allowed);
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), smem + 2048 + sizeof(float) * 3 * S::SLOTS * S::W, allowed);
   if (e != cudaSuccess) return e;
-  long long ctas = p.chains;
-  if (MODE == kColChained) {       // as many CTAs as run at once (only a running CTA draws tickets, so none has to)
-    const long long most = 2 * (long long)num_sms();
-    ctas = p.chains * p.chunks < most ? p.chains * p.chunks : most;
-  }
-  return launch_pdl(kern, dim3((unsigned)ctas), dim3(kScanThreads), smem, st, p);
+  if (MODE == kOneTile) return launch_pdl(kern, dim3((unsigned)p.chains), dim3(kScanThreads), smem, st, p);
+  return launch_clusters(kern, p.chains, cluster, kScanThreads, smem, st, p);
 }
 
 // sequences that fit one tile
@@ -1115,33 +913,31 @@ template <typename T, class S, bool BACK>
 cudaError_t launch_short_cols(ScanArgs<T> p, cudaStream_t st) {
   p.total = p.outer * p.groups;
   p.chains = (p.total + S::TX - 1) / S::TX;
-  p.chunks = 1;
-  return launch_cols_kernel<T, S, kOneTile, BACK>(p, st);
+  p.chunks = p.rounds = 1;
+  if (p.chains > 0x7fffffff) return cudaErrorNotSupported;
+  return launch_cols_kernel<T, S, kOneTile, BACK>(p, 1, st);
 }
 template <typename T, class S, bool BACK>
-cudaError_t launch_long_cols(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
+cudaError_t launch_long_cols(ScanArgs<T> p, cudaStream_t st) {
   static_assert(S::LC == kColTile, "tiles end where states are saved");
   const long long per_outer = (p.groups + S::TX - 1) / S::TX;
   p.per_outer = (unsigned)per_outer;
   p.chains = p.outer * per_outer;
-  if (p.chains > 0x7fffffff) return cudaErrorNotSupported;
   p.chunks = (int)((p.L + S::LC - 1) / S::LC);
-  if (chained(p.chains, p.chunks, p.chains * p.chunks)) {
-    chain(p, c);
-    return launch_cols_kernel<T, S, kColChained, BACK>(p, st);
-  }
-  return launch_cols_kernel<T, S, kColWalk, BACK>(p, st);
+  const int cluster = cluster_for(p.chains, p.chunks, 8);
+  p.rounds = (p.chunks + cluster - 1) / cluster;
+  return launch_cols_kernel<T, S, kLong, BACK>(p, cluster, st);
 }
 
 template <typename T, bool WIDE, int MODE, bool BACK>
-cudaError_t launch_rows_kernel(const ScanArgs<T>& p, long long units, cudaStream_t st) {
-  const dim3 grid((unsigned)((units + kRowWarps - 1) / kRowWarps)), block(32 * kRowWarps);
-  if constexpr (BACK)
-    return p.lengths != nullptr ? launch_pdl(scan_rows_backward_kernel<T, WIDE, MODE, true>, grid, block, 0, st, p)
-                                : launch_pdl(scan_rows_backward_kernel<T, WIDE, MODE, false>, grid, block, 0, st, p);
-  else
-    return p.lengths != nullptr ? launch_pdl(scan_rows_kernel<T, WIDE, MODE, true>, grid, block, 0, st, p)
-                                : launch_pdl(scan_rows_kernel<T, WIDE, MODE, false>, grid, block, 0, st, p);
+cudaError_t launch_rows_kernel(const ScanArgs<T>& p, long long tiles, int cluster, cudaStream_t st) {
+  void (*kern)(const ScanArgs<T>);
+  if constexpr (BACK) kern = p.lengths != nullptr ? scan_rows_backward_kernel<T, WIDE, MODE, true> : scan_rows_backward_kernel<T, WIDE, MODE, false>;
+  else kern = p.lengths != nullptr ? scan_rows_kernel<T, WIDE, MODE, true> : scan_rows_kernel<T, WIDE, MODE, false>;
+  if (MODE == kTeam) return launch_clusters(kern, tiles, cluster, 32 * kRowWarps, 0, st, p);
+  const long long ctas = (tiles + kRowWarps - 1) / kRowWarps;       // a unit per warp
+  if (ctas > 0x7fffffff) return cudaErrorNotSupported;
+  return launch_pdl(kern, dim3((unsigned)ctas), dim3(32 * kRowWarps), 0, st, p);
 }
 
 template <typename T, bool BACK>
@@ -1164,14 +960,17 @@ cudaError_t launch_rows(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
         break;
       }
     const long long units = (p.outer + p.groups - 1) / p.groups;
-    return w ? launch_rows_kernel<T, true, kWholeRows, BACK>(p, units, st) : launch_rows_kernel<T, false, kWholeRows, BACK>(p, units, st);
+    p.rounds = 1;
+    return w ? launch_rows_kernel<T, true, kWholeRows, BACK>(p, units, 1, st) : launch_rows_kernel<T, false, kWholeRows, BACK>(p, units, 1, st);
   }
-  if (chained((p.outer + kRowWarps - 1) / kRowWarps, p.chunks, p.outer * p.chunks)) {
-    chain(p, c);
-    return w ? launch_rows_kernel<T, true, kChained, BACK>(p, p.outer * p.chunks, st)
-             : launch_rows_kernel<T, false, kChained, BACK>(p, p.outer * p.chunks, st);
+  // a warp per row where that fills the GPU's 16 warps per SM, else the warps of a CTA or cluster share it
+  if (p.outer >= 16 * (long long)num_sms()) {
+    p.rounds = p.chunks;
+    return w ? launch_rows_kernel<T, true, kWalk, BACK>(p, p.outer, 1, st) : launch_rows_kernel<T, false, kWalk, BACK>(p, p.outer, 1, st);
   }
-  return w ? launch_rows_kernel<T, true, kWalk, BACK>(p, p.outer, st) : launch_rows_kernel<T, false, kWalk, BACK>(p, p.outer, st);
+  const int cluster = cluster_for(p.outer, (p.chunks + kRowWarps - 1) / kRowWarps, 32 / kRowWarps), team = cluster * kRowWarps;
+  p.rounds = (p.chunks + team - 1) / team;
+  return w ? launch_rows_kernel<T, true, kTeam, BACK>(p, p.outer, cluster, st) : launch_rows_kernel<T, false, kTeam, BACK>(p, p.outer, cluster, st);
 }
 
 template <typename T, bool BACK>
@@ -1193,11 +992,11 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   if (vec) {
     if (c.length <= 8) return launch_short_cols<T, ColShape<4, 8, 1>, BACK>(p, st);
     if (c.length <= 64) return launch_short_cols<T, ColShape<4, 8, 8>, BACK>(p, st);
-    return launch_long_cols<T, ColShape<4, 8, 32>, BACK>(p, c, st);
+    return launch_long_cols<T, ColShape<4, 8, 32>, BACK>(p, st);
   }
   if (c.length <= 8) return launch_short_cols<T, ColShape<1, 8, 1>, BACK>(p, st);
   if (c.length <= 64) return launch_short_cols<T, ColShape<1, 8, 8>, BACK>(p, st);
-  return launch_long_cols<T, ColShape<1, 32, 8>, BACK>(p, c, st);
+  return launch_long_cols<T, ColShape<1, 32, 8>, BACK>(p, st);
 }
 
 }  // namespace
@@ -1207,12 +1006,6 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
 long long scan_chunk(int, long long length, long long inner) {
   const long long lc = inner == 1 ? row_chunk(length) : kColTile;
   return length <= lc ? (length < 1 ? 1 : length) : lc;
-}
-
-size_t scan_workspace_bytes(int dtype, long long outer, long long length, long long inner) {
-  const long long lc = scan_chunk(dtype, length, inner), chunks = (length + lc - 1) / lc;
-  if (chunks < 2) return kStatusBytes;
-  return kChainHead + (size_t)chunks * (size_t)outer * (size_t)inner * (sizeof(ulonglong2) + 2 * sizeof(unsigned long long));   // (at most one hint per state)
 }
 
 cudaError_t launch_scan_forward(const ScanCall& c, cudaStream_t st) {

@@ -220,24 +220,7 @@ def quantize_fp8_weight(w: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     return q, scale
 
 
-def _workspace(nbytes: int, dev: int) -> torch.Tensor:
-    """Zeroed memory that calls on any stream may use from now on."""
-    ws = torch.zeros(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev))
-    torch.cuda.current_stream(dev).synchronize()
-    return ws
-
-
-class _Workspace:
-    """Operators with a workspace: calls of one object share it and must be stream-ordered."""
-
-    @_on_stream
-    def status(self) -> int:
-        """DTST_OK, or DTST_ERR_DEVICE_TIMEOUT if a bounded wait gave up since the last query; synchronises."""
-        with torch.cuda.device(self.dev):
-            return int(Bn.lib().dtst_workspace_status(self.workspace.data_ptr(), Bn._stream_ptr(None)))
-
-
-class Fp8Linear(_Workspace):
+class Fp8Linear:
     """out = x w^T for 8-bit x [m, k] (scale [ceil(k / 128), m]) and weights [n, k] (a scale per 128 x 128 block)."""
 
     def __init__(self, weight: torch.Tensor, weight_scale: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16):
@@ -255,7 +238,9 @@ class Fp8Linear(_Workspace):
         self._kb = -(-self.k // BLOCK)
         self._w = _addr(weight, "weight", self.dev, FP8, None, False)
         self._ws = _addr(weight_scale, "weight_scale", self.dev, torch.float32, (-(-self.n // BLOCK), self._kb))
-        self.workspace = _workspace(256, self.dev)
+        # zeroed memory that calls on any stream may use from now on; calls that share it must be stream-ordered
+        self.workspace = torch.zeros(256, dtype=torch.uint8, device=self.device)
+        torch.cuda.current_stream(self.dev).synchronize()
         self._type = DTYPES[out_dtype]
         self._lib = Bn.lib()
 
@@ -280,8 +265,14 @@ class Fp8Linear(_Workspace):
 
     __call__ = forward
 
+    @_on_stream
+    def status(self) -> int:
+        """DTST_OK, or DTST_ERR_DEVICE_TIMEOUT if a bounded wait gave up since the last query; synchronises."""
+        with torch.cuda.device(self.dev):
+            return int(Bn.lib().dtst_workspace_status(self.workspace.data_ptr(), Bn._stream_ptr(None)))
 
-class GatedScan(_Workspace):
+
+class GatedScan:
     """h_t = a_t h_{t-1} + u_t along dimension `dim` of `shape`, forward and backward.
 
     gate "sigmoid": a = sigmoid(g), u = (1 - a) v; "decay": a = g, u = v.  The states (h0, h_last) are float32 of the
@@ -312,11 +303,9 @@ class GatedScan(_Workspace):
         self._desc = Bn.ScanDesc(DTYPES[dtype], GATES[gate], self.outer, self.length, self.inner, dense, dense)
         self._ref = ctypes.byref(self._desc)
         self._lib = Bn.lib()
-        n, ck = ctypes.c_size_t(), ctypes.c_int64()
-        Bn._check(self._lib.dtst_gated_scan_sizes(self._ref, ctypes.byref(n), ctypes.byref(ck)), "dtst_gated_scan_sizes")
-        self.checkpoint_floats = int(ck.value)
-        self.workspace = _workspace(int(n.value), self.dev)
-        self._ws = (self.workspace.data_ptr(), int(n.value))
+        n = ctypes.c_int64()
+        Bn._check(self._lib.dtst_gated_scan_checkpoints(self._ref, ctypes.byref(n)), "dtst_gated_scan_checkpoints")
+        self.checkpoint_floats = int(n.value)
 
     def new_checkpoints(self) -> torch.Tensor:
         """A buffer for the states that a forward pass saves for its backward pass."""
@@ -367,7 +356,7 @@ class GatedScan(_Workspace):
               _addr(g, "g", d, t, None, False), _addr(h0, "h0", d, torch.float32, self.state_shape),
               self._lengths(lengths), _addr(out, "out", d, t, self.shape),
               _addr(h_last, "h_last", d, torch.float32, self.state_shape),
-              _addr(checkpoints, "checkpoints", d, torch.float32, (self.checkpoint_floats,)), *self._ws)
+              _addr(checkpoints, "checkpoints", d, torch.float32, (self.checkpoint_floats,)))
         return out, h_last
 
     def _lengths(self, lengths) -> int:
@@ -395,7 +384,7 @@ class GatedScan(_Workspace):
               _addr(h0, "h0", d, torch.float32, self.state_shape), self._lengths(lengths),
               _addr(checkpoints, "checkpoints", d, torch.float32, (self.checkpoint_floats,)),
               _addr(grad_v, "grad_v", d, t, None, False), _addr(grad_g, "grad_g", d, t, None, False),
-              _addr(grad_h0, "grad_h0", d, torch.float32, self.state_shape), *self._ws)
+              _addr(grad_h0, "grad_h0", d, torch.float32, self.state_shape))
         return grad_v, grad_g, grad_h0
 
 

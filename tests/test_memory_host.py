@@ -91,7 +91,7 @@ def test_empty_batches_need_no_pointers():
     assert L.dtst_quantize_fp8(1, 0, 64, NULL, 64, NULL, 64, NULL, NULL) == Bn.DTST_OK
     assert L.dtst_matmul_fp8(1, 0, 8, 16, NULL, 16, NULL, NULL, 16, NULL, NULL, 8, NULL, 0, NULL) == Bn.DTST_OK
     d = Bn.ScanDesc(0, 0, 0, 4, 8, (32, 8), (32, 8))
-    assert L.dtst_gated_scan(ctypes.byref(d), NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, 0, NULL) == Bn.DTST_OK
+    assert L.dtst_gated_scan(ctypes.byref(d), NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL) == Bn.DTST_OK
 
 
 @pytest.mark.parametrize("bad,want", [
@@ -130,40 +130,39 @@ def test_quantisers_refuse():
     (dict(dtype=5), -1), (dict(gate=2), -1), (dict(outer=-1), -1), (dict(length=-1), -1), (dict(inner=0), -1),
     (dict(in_stride=(-1, 8)), -1), (dict(inner=1, in_stride=(4, 2)), -1), (dict(inner=1, in_stride=(4, 1), grad_stride=(4, 3)), -1),
     (dict(length=1 << 32, in_stride=(1 << 35, 8), grad_stride=(1 << 35, 8)), -2), (dict(outer=1 << 44, inner=1 << 44), -1)])
-def test_scan_sizes_refuse(fields, want):
+def test_scan_descriptions_are_refused(fields, want):
     f = dict(dtype=0, gate=0, outer=3, length=4, inner=8, in_stride=(32, 8), grad_stride=(32, 8))
     f.update(fields)
     d = Bn.ScanDesc(f["dtype"], f["gate"], f["outer"], f["length"], f["inner"], f["in_stride"], f["grad_stride"])
-    n, c = ctypes.c_size_t(), ctypes.c_int64()
-    assert Bn.lib().dtst_gated_scan_sizes(ctypes.byref(d), ctypes.byref(n), ctypes.byref(c)) == want
+    c = ctypes.c_int64()
+    assert Bn.lib().dtst_gated_scan_checkpoints(ctypes.byref(d), ctypes.byref(c)) == want
 
 
 def _scan(length=4, grad_stride=(32, 8), back=False, **k):
     d = Bn.ScanDesc(0, 0, 3, length, 8, (length * 8, 8), grad_stride)
-    a = dict(v=A, g=B_, h=C, h0=NULL, last=NULL, ck=NULL, ws=WS, nws=1 << 30, gv=D, gg=E, g0=NULL)
+    a = dict(v=A, g=B_, h=C, h0=NULL, last=NULL, ck=NULL, gv=D, gg=E, g0=NULL)
     a.update(k)
     r = ctypes.byref(d)
     if back:
         return Bn.lib().dtst_gated_scan_backward(r, a["h"], a["last"], a["v"], a["g"], a["h0"], NULL, a["ck"], a["gv"], a["gg"],
-                                                 a["g0"], a["ws"], a["nws"], NULL)
-    return Bn.lib().dtst_gated_scan(r, a["v"], a["g"], a["h0"], NULL, a["h"], a["last"], a["ck"], a["ws"], a["nws"], NULL)
+                                                 a["g0"], NULL)
+    return Bn.lib().dtst_gated_scan(r, a["v"], a["g"], a["h0"], NULL, a["h"], a["last"], a["ck"], NULL)
 
 
 def test_scan_refuses():
     assert _scan(v=NULL) == -1 and _scan(h=A) == -1 and _scan(h=ctypes.c_void_p(0x30002)) == -1
-    assert _scan(ws=NULL) == -5 and _scan(nws=16) == -5 and _scan(ws=ctypes.c_void_p(0x100008)) == -1
     assert _scan(h0=ctypes.c_void_p(0x40001)) == -1
     assert _scan(back=True, gv=E) == -1 and _scan(back=True, gv=A) == -1 and _scan(back=True, gg=NULL) == -1
     assert _scan(back=True, grad_stride=(32, 4)) == -1 and _scan(back=True, grad_stride=(0, 8)) == -1   # elements coincide
     assert _scan(back=True, length=4000, grad_stride=(32000, 8)) == -1                                  # no checkpoints
-    assert Bn.lib().dtst_gated_scan(None, A, B_, NULL, NULL, C, NULL, NULL, WS, 1 << 20, NULL) == -1
+    assert Bn.lib().dtst_gated_scan(None, A, B_, NULL, NULL, C, NULL, NULL, NULL) == -1
     assert Bn.lib().dtst_workspace_status(NULL, NULL) == -1
 
 
-def test_scan_sizes():
-    n, c = ctypes.c_size_t(), ctypes.c_int64()
+def test_scan_checkpoint_counts():
+    c = ctypes.c_int64()
     for outer, length, inner in [(3, 0, 8), (3, 1, 8), (2, 1000, 8), (5, 30, 1), (5, 3000, 1)]:
         d = Bn.ScanDesc(1, 0, outer, length, inner, (length * inner, inner), (length * inner, inner))
-        assert Bn.lib().dtst_gated_scan_sizes(ctypes.byref(d), ctypes.byref(n), ctypes.byref(c)) == 0
-        assert n.value >= 256 and c.value % (outer * inner) == 0
-        assert (c.value == 0) == (length == 0)
+        assert Bn.lib().dtst_gated_scan_checkpoints(ctypes.byref(d), ctypes.byref(c)) == 0
+        assert c.value % (outer * inner) == 0 and (c.value == 0) == (length == 0)
+        assert c.value <= outer * inner * (1 + length // 256)

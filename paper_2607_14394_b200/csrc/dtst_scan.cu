@@ -18,7 +18,6 @@ namespace dtst {
 
 namespace {
 
-constexpr int kScanThreads = 256;
 
 // Where there are few sequences, a thread-block cluster shares one: its CTAs take chunks side by side, exchange the chunks'
 // summaries through distributed shared memory once per round, and each applies those of the chunks in front of its own to
@@ -91,12 +90,12 @@ __device__ __forceinline__ long long clamp_len(const int* lengths, long long o, 
 // [outer][L][inner], inner contiguous.  A tile is TX groups of VEC channels times SLOTS runs of R steps, a run per thread.
 // Long sequences: the tiles of one outer entry lie side by side over its channels; a CTA (or a cluster) walks along L.
 // Short ones (one tile holds them): groups run on across outer entries, so that few channels fill a CTA too.
-template <int VEC_, int R_, int SLOTS_>
+template <int VEC_, int R_, int SLOTS_, int THREADS_ = 256>
 struct ColShape {
-  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_;
-  static constexpr int TX = kScanThreads / SLOTS, W = TX * VEC, LC = SLOTS * R;
+  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_, THREADS = THREADS_;
+  static constexpr int TX = THREADS / SLOTS, W = TX * VEC, LC = SLOTS * R;
   // while runs are joined a warp has CPW channels, DG lanes each, and a lane has JOIN neighbouring runs of its channel
-  static constexpr int WARPS = kScanThreads / 32, CPW = W / WARPS < 32 ? W / WARPS : 32, DG = 32 / CPW;
+  static constexpr int WARPS = THREADS / 32, CPW = W / WARPS < 32 ? W / WARPS : 32, DG = 32 / CPW;
   static constexpr int JOIN = SLOTS >= DG ? SLOTS / DG : 1;
 };
 constexpr int kColTile = 256;     // steps of a long sequence's tile, and between saved states
@@ -124,19 +123,33 @@ __device__ __forceinline__ float2 join_lanes(float& A, float& H) {
   return all;
 }
 
-// A thread's part of a tile on its way through shared memory: only the thread itself touches its slots, so the copies of
-// the next tile start as soon as this one's are in registers, and no barrier is needed.
-template <typename T, class S, int TENSORS>
+// The coming tiles on their way through shared memory, kStages of them under way.
+// WIDE: 16-byte copies past L1, shared among the threads - a row of the tile is W elements, and the rows of a run are
+// followed by a gap of one row where that keeps the runs of half a warp in different banks.  The copies are waited for in
+// front of the barrier that ends a round.  (8-byte copies go through L1, whose lines then bound what can be in flight:
+// measured 198 us against 110 for the same 65536 x 1024 pass.)
+// Otherwise a thread copies and reads its own steps, element group by element group.
+template <typename T, class S, int TENSORS, bool WIDE>
 struct ColSlots {
   static constexpr int VEC = S::VEC, R = S::R, BYTES = VEC * (int)sizeof(T);
   static constexpr bool ASYNC = BYTES >= 4;      // (cp.async moves 4, 8 or 16 bytes)
-  static constexpr size_t SMEM = (size_t)TENSORS * R * kScanThreads * BYTES;
+  static constexpr int ROW = S::W * (int)sizeof(T), GAP = WIDE && ROW < 128 ? ROW : 0, RUN = R * ROW + GAP;
+  static constexpr int PER_ROW = ROW / 16 > 0 ? ROW / 16 : 1, ROWS = S::THREADS / PER_ROW;      // copies of a row, rows at a time
+  static constexpr size_t TENSOR = WIDE ? (size_t)S::SLOTS * RUN : (size_t)R * S::THREADS * BYTES, STAGE = TENSORS * TENSOR;
+  static constexpr int kStages = WIDE && STAGE < 45000 ? 2 : 1;       // (two CTAs to an SM)
+  static constexpr size_t SMEM = kStages * STAGE;
   using P = Pack<T, VEC>;
   unsigned char* base;
+  uint32_t stage = 0;
   __device__ __forceinline__ P* slot(int tensor, int r) const {
-    return reinterpret_cast<P*>(base + ((size_t)(tensor * R + r) * kScanThreads + threadIdx.x) * BYTES);
+    unsigned char* b = base + stage + tensor * TENSOR;
+    if (WIDE) return reinterpret_cast<P*>(b + threadIdx.x / S::TX * RUN + r * ROW + threadIdx.x % S::TX * BYTES);
+    return reinterpret_cast<P*>(b + ((size_t)r * S::THREADS + threadIdx.x) * BYTES);
   }
-  // the first `have` steps from src on; `none` for the others
+  __device__ __forceinline__ void advance() { stage = stage + STAGE == SMEM ? 0u : stage + (uint32_t)STAGE; }
+  static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory"); }
+  // this thread's own steps from src on; `none` where there are fewer than R
   __device__ __forceinline__ void fetch(int tensor, const T* src, long long stride, int have, T none) const {
 #pragma unroll
     for (int r = 0; r < R; ++r, src += stride) {
@@ -154,7 +167,25 @@ struct ColSlots {
       }
     }
   }
-  static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+  // the tile's rows from src (its first element) on, `have` of them, the first `cols` elements of each
+  __device__ __forceinline__ void fetch_rows(int tensor, const T* src, long long stride, int have, int cols, T none) const {
+    constexpr int E = 16 / (int)sizeof(T);
+    const int col = (threadIdx.x % PER_ROW) * E, row0 = threadIdx.x / PER_ROW;
+    src += row0 * stride + col;
+    const uint32_t b = static_cast<uint32_t>(__cvta_generic_to_shared(base)) + stage + (uint32_t)(tensor * TENSOR) + col * (int)sizeof(T);
+#pragma unroll
+    for (int k = 0; k < S::LC / ROWS; ++k, src += ROWS * stride) {
+      const int row = row0 + k * ROWS;
+      const uint32_t at = b + row / R * RUN + row % R * ROW;
+      if (row < have && col < cols) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(src) : "memory");
+      } else {
+        Pack<T, E> n;
+        n.fill(none);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(n.raw.x), "r"(n.raw.y), "r"(n.raw.z), "r"(n.raw.w) : "memory");
+      }
+    }
+  }
 };
 
 // A group of a tile: its outer entry, first channel and steps (0: no such group)
@@ -206,14 +237,14 @@ __device__ __forceinline__ float join_round(const float2 all, float& state, floa
   return start;
 }
 
-template <typename T, class S, int MODE>
-__global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_kernel(const ScanArgs<T> p) {
+template <typename T, class S, int MODE, bool WIDE>
+__global__ void __launch_bounds__(S::THREADS, 2) scan_cols_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
-  using Slots = ColSlots<T, S, 2>;
+  using Slots = ColSlots<T, S, 2, WIDE>;
   __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];     // (A, H) of every run; then its first state in x
   __shared__ float2 box[2][SLOTS > 1 ? W : 1];
   extern __shared__ __align__(16) unsigned char raw[];
-  const Slots slots{raw};
+  Slots slots{raw};
   pdl_trigger();
   pdl_wait();
   const int size = MODE == kLong ? cluster_size() : 1, rank = MODE == kLong ? cluster_rank() : 0;
@@ -226,25 +257,52 @@ __global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_
   const bool first = lane < S::CPW;
   const ColGroup at = col_group<T, S, MODE>(p, tile, x), jg = col_group<T, S, MODE>(p, tile, jx / VEC);
   const long long ch = jg.o * p.inner + jg.i0 + jx % VEC;
+  // the tile's first channel, the channels there are from it on, and the steps of its sequence
+  const int i_tile = MODE == kLong ? (int)(tile % p.per_outer) * W : 0, cols = (int)p.inner - i_tile;
+  const int e_tile = MODE == kLong ? (int)clamp_len(p.lengths, at.o, p.L) : 0;
   auto fetch = [&](int c) {
-    const int t0 = c * LC + slot * R;
-    const long long from = at.o * p.in_o + at.i0 + t0 * p.in_t;
-    slots.fetch(0, p.v + from, p.in_t, at.end - t0, none_v);
-    slots.fetch(1, p.g + from, p.in_t, at.end - t0, none_g);
+    if constexpr (WIDE) {
+      const long long from = at.o * p.in_o + i_tile + (long long)c * LC * p.in_t;
+      slots.fetch_rows(0, p.v + from, p.in_t, e_tile - c * LC, cols, none_v);
+      slots.fetch_rows(1, p.g + from, p.in_t, e_tile - c * LC, cols, none_g);
+    } else {
+      const int t0 = c * LC + slot * R;
+      const long long from = at.o * p.in_o + at.i0 + t0 * p.in_t;
+      slots.fetch(0, p.v + from, p.in_t, at.end - t0, none_v);
+      slots.fetch(1, p.g + from, p.in_t, at.end - t0, none_g);
+    }
   };
-  fetch(rank);
+#pragma unroll
+  for (int k = 0; k < Slots::kStages; ++k) {
+    if (k < p.rounds) fetch(rank + k * size);
+    Slots::commit();
+    slots.advance();
+  }
+  if (WIDE) {
+    Slots::wait();
+    __syncthreads();
+  }
   float state = SLOTS > 1 && jg.live && p.h0 != nullptr ? p.h0[ch] : 0.f;
 
 #pragma unroll 1
   for (int round = 0; round < p.rounds; ++round) {
     const int c = round * size + rank;
     float a[R][VEC], u[R][VEC], s[VEC];
-    Slots::wait();
+    if (!WIDE) Slots::wait();
+    Pack<T, VEC> pv[R], pg[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) pv[r] = *slots.slot(0, r), pg[r] = *slots.slot(1, r);
+    auto refill = [&]() {      // the values of a later chunk are on their way from here on
+      if (round + Slots::kStages < p.rounds) fetch(c + Slots::kStages * size);
+      Slots::commit();
+      slots.advance();
+    };
+    if (!WIDE && MODE == kLong) refill();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float gv[VEC], vv[VEC];
-      slots.slot(1, r)->unpack(gv);
-      slots.slot(0, r)->unpack(vv);
+      pg[r].unpack(gv);
+      pv[r].unpack(vv);
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         terms(p.sigmoid, gv[j], a[r][j], u[r][j]);
@@ -266,7 +324,7 @@ __global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_
         runs[slot][x * VEC + j] = make_float2(A, H);
       }
       __syncthreads();
-      if (MODE == kLong && round + 1 < p.rounds) fetch(c + size);      // the next chunk's values are on their way from here on
+      if (WIDE) refill();
       float A = 1.f, H = 0.f;
       float2 m[S::JOIN];
 #pragma unroll
@@ -313,21 +371,22 @@ __global__ void __launch_bounds__(kScanThreads, S::SLOTS > 1 ? 2 : 3) scan_cols_
       }
     }
     if (MODE == kOneTile) return;
-    __syncthreads();       // the runs' states are read before the next chunk's summaries replace them
+    if (WIDE) Slots::wait();
+    __syncthreads();       // the runs' states are read before the next chunk's summaries replace them, the next tile is here
   }
   if (size > 1) cluster_sync();       // nobody leaves while its box may be read
 }
 
-template <typename T, class S, int MODE>
-__global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(const ScanArgs<T> p) {
+template <typename T, class S, int MODE, bool WIDE>
+__global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
-  using Slots = ColSlots<T, S, 3>;
+  using Slots = ColSlots<T, S, 3, WIDE>;
   // (A, H) and D of every run; then the state in front of it (x) and the gradient that comes to it from behind
   __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
   __shared__ float backs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
   __shared__ float2 box[2][SLOTS > 1 ? W : 1];
   extern __shared__ __align__(16) unsigned char raw[];
-  const Slots slots{raw};
+  Slots slots{raw};
   pdl_trigger();
   pdl_wait();
   const int size = MODE == kLong ? cluster_size() : 1, rank = MODE == kLong ? cluster_rank() : 0;
@@ -340,15 +399,35 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(con
   const bool first = lane < S::CPW;
   const ColGroup at = col_group<T, S, MODE>(p, tile, x), jg = col_group<T, S, MODE>(p, tile, jx / VEC);
   const long long ch = jg.o * p.inner + jg.i0 + jx % VEC;
+  // the tile's first channel, the channels there are from it on, and the steps of its sequence
+  const int i_tile = MODE == kLong ? (int)(tile % p.per_outer) * W : 0, cols = (int)p.inner - i_tile;
+  const int e_tile = MODE == kLong ? (int)clamp_len(p.lengths, at.o, p.L) : 0;
   // chunks from the last to the first; a chunk before the first has no steps
   auto fetch = [&](int c) {
-    const int t0 = c * LC + slot * R, end = c < 0 ? t0 : at.end;
-    const long long from = at.o * p.in_o + at.i0 + t0 * p.in_t;
-    slots.fetch(0, p.v + from, p.in_t, end - t0, none_v);
-    slots.fetch(1, p.g + from, p.in_t, end - t0, none_g);
-    slots.fetch(2, p.gh + (at.o * p.L + t0) * p.inner + at.i0, p.inner, end - t0, none_v);
+    if constexpr (WIDE) {
+      const int have = c < 0 ? 0 : e_tile - c * LC;
+      const long long from = at.o * p.in_o + i_tile + (long long)c * LC * p.in_t;
+      slots.fetch_rows(0, p.v + from, p.in_t, have, cols, none_v);
+      slots.fetch_rows(1, p.g + from, p.in_t, have, cols, none_g);
+      slots.fetch_rows(2, p.gh + (at.o * p.L + (long long)c * LC) * p.inner + i_tile, p.inner, have, cols, none_v);
+    } else {
+      const int t0 = c * LC + slot * R, end = c < 0 ? t0 : at.end;
+      const long long from = at.o * p.in_o + at.i0 + t0 * p.in_t;
+      slots.fetch(0, p.v + from, p.in_t, end - t0, none_v);
+      slots.fetch(1, p.g + from, p.in_t, end - t0, none_g);
+      slots.fetch(2, p.gh + (at.o * p.L + t0) * p.inner + at.i0, p.inner, end - t0, none_v);
+    }
   };
-  fetch(p.chunks - 1 - rank);
+#pragma unroll
+  for (int k = 0; k < Slots::kStages; ++k) {
+    if (k < p.rounds) fetch(p.chunks - 1 - (rank + k * size));
+    Slots::commit();
+    slots.advance();
+  }
+  if (WIDE) {
+    Slots::wait();
+    __syncthreads();
+  }
   float grad = SLOTS > 1 && jg.live && p.g_last != nullptr ? p.g_last[ch] : 0.f;
 
 #pragma unroll 1
@@ -359,18 +438,26 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(con
       if (MODE == kLong && p.ckpt != nullptr) before = p.ckpt[c * states + ch];
       else if (p.h0 != nullptr) before = p.h0[ch];
     }
-    Slots::wait();
+    if (!WIDE) Slots::wait();
     // q: 1 - a (sigmoid) or a (decay); a is formed again where it is used
     float q[R][VEC], v[R][VEC], s[VEC], d[VEC];
     Pack<T, VEC> pd[R];
     const float ka = p.sigmoid ? -1.f : 1.f, kb = p.sigmoid ? 1.f : 0.f;
     auto a_of = [&](float qq) { return fmaf(qq, ka, kb); };
     auto b_of = [&](float qq) { return p.sigmoid ? qq : 1.f; };
+    Pack<T, VEC> pv[R], pg[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) pv[r] = *slots.slot(0, r), pg[r] = *slots.slot(1, r), pd[r] = *slots.slot(2, r);
+    auto refill = [&]() {      // the values of a later chunk are on their way from here on
+      if (round + Slots::kStages < p.rounds) fetch(c - Slots::kStages * size);
+      Slots::commit();
+      slots.advance();
+    };
+    if (!WIDE && MODE == kLong) refill();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      pd[r] = *slots.slot(2, r);
-      slots.slot(1, r)->unpack(q[r]);
-      slots.slot(0, r)->unpack(v[r]);
+      pg[r].unpack(q[r]);
+      pv[r].unpack(v[r]);
       if (p.sigmoid) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
@@ -409,7 +496,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(con
 #pragma unroll
       for (int j = 0; j < VEC; ++j) backs[slot][x * VEC + j] = D[j];
       __syncthreads();
-      if (MODE == kLong && round + 1 < p.rounds) fetch(c - size);      // the next chunk's values are on their way from here on
+      if (WIDE) refill();
       float A = 1.f, H = 0.f, B = 1.f, E = 0.f;
       float2 m[S::JOIN];
       float md[S::JOIN];
@@ -483,6 +570,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_cols_backward_kernel(con
       }
     }
     if (MODE == kOneTile) return;
+    if (WIDE) Slots::wait();
     __syncthreads();
   }
   if (size > 1) cluster_sync();
@@ -895,17 +983,17 @@ cudaError_t launch_clusters(Kern kern, long long tiles, int cluster, int threads
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
-template <typename T, class S, int MODE, bool BACK>
+template <typename T, class S, int MODE, bool WIDE, bool BACK>
 cudaError_t launch_cols_kernel(const ScanArgs<T>& p, int cluster, cudaStream_t st) {
   void (*kern)(const ScanArgs<T>);
-  constexpr size_t smem = ColSlots<T, S, BACK ? 3 : 2>::SMEM;
-  if constexpr (BACK) kern = scan_cols_backward_kernel<T, S, MODE>;
-  else kern = scan_cols_kernel<T, S, MODE>;
+  constexpr size_t smem = ColSlots<T, S, BACK ? 3 : 2, WIDE>::SMEM;
+  if constexpr (BACK) kern = scan_cols_backward_kernel<T, S, MODE, WIDE>;
+  else kern = scan_cols_kernel<T, S, MODE, WIDE>;
   static std::atomic<uint64_t> allowed{0};
   const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), smem + 2048 + sizeof(float) * 3 * S::SLOTS * S::W, allowed);
   if (e != cudaSuccess) return e;
-  if (MODE == kOneTile) return launch_pdl(kern, dim3((unsigned)p.chains), dim3(kScanThreads), smem, st, p);
-  return launch_clusters(kern, p.chains, cluster, kScanThreads, smem, st, p);
+  if (MODE == kOneTile) return launch_pdl(kern, dim3((unsigned)p.chains), dim3(S::THREADS), smem, st, p);
+  return launch_clusters(kern, p.chains, cluster, S::THREADS, smem, st, p);
 }
 
 // sequences that fit one tile
@@ -915,10 +1003,10 @@ cudaError_t launch_short_cols(ScanArgs<T> p, cudaStream_t st) {
   p.chains = (p.total + S::TX - 1) / S::TX;
   p.chunks = p.rounds = 1;
   if (p.chains > 0x7fffffff) return cudaErrorNotSupported;
-  return launch_cols_kernel<T, S, kOneTile, BACK>(p, 1, st);
+  return launch_cols_kernel<T, S, kOneTile, false, BACK>(p, 1, st);
 }
 template <typename T, class S, bool BACK>
-cudaError_t launch_long_cols(ScanArgs<T> p, cudaStream_t st) {
+cudaError_t launch_long_cols(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
   static_assert(S::LC == kColTile, "tiles end where states are saved");
   const long long per_outer = (p.groups + S::TX - 1) / S::TX;
   p.per_outer = (unsigned)per_outer;
@@ -926,7 +1014,12 @@ cudaError_t launch_long_cols(ScanArgs<T> p, cudaStream_t st) {
   p.chunks = (int)((p.L + S::LC - 1) / S::LC);
   const int cluster = cluster_for(p.chains, p.chunks, 8);
   p.rounds = (p.chunks + cluster - 1) / cluster;
-  return launch_cols_kernel<T, S, kLong, BACK>(p, cluster, st);
+  if constexpr (S::VEC > 1) {
+    constexpr int E = 16 / (int)sizeof(T);
+    if (p.inner % E == 0 && p.in_o % E == 0 && p.in_t % E == 0 && aligned_to(c.v, 16) && aligned_to(c.g, 16) && aligned_to(c.grad_h, 16))
+      return launch_cols_kernel<T, S, kLong, true, BACK>(p, cluster, st);
+  }
+  return launch_cols_kernel<T, S, kLong, false, BACK>(p, cluster, st);
 }
 
 template <typename T, bool WIDE, int MODE, bool BACK>
@@ -992,11 +1085,11 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   if (vec) {
     if (c.length <= 8) return launch_short_cols<T, ColShape<4, 8, 1>, BACK>(p, st);
     if (c.length <= 64) return launch_short_cols<T, ColShape<4, 8, 8>, BACK>(p, st);
-    return launch_long_cols<T, ColShape<4, 8, 32>, BACK>(p, st);
+    return launch_long_cols<T, ColShape<4, 8, 32>, BACK>(p, c, st);
   }
   if (c.length <= 8) return launch_short_cols<T, ColShape<1, 8, 1>, BACK>(p, st);
   if (c.length <= 64) return launch_short_cols<T, ColShape<1, 8, 8>, BACK>(p, st);
-  return launch_long_cols<T, ColShape<1, 32, 8>, BACK>(p, st);
+  return launch_long_cols<T, ColShape<1, 32, 8>, BACK>(p, c, st);
 }
 
 }  // namespace

@@ -308,7 +308,8 @@ cudaError_t launch_tile(const MatmulCall& c, MatmulArgs p, cudaStream_t st) {
   p.lane_tiles = (int)((lanes + kLanes - 1) / kLanes);
   p.col_tiles = (int)((cols + BN - 1) / BN);
   auto kern = matmul_fp8_kernel<T, BN, SWAP>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::SMEM);
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), Cfg::SMEM, allowed);
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)p.lane_tiles * p.col_tiles;
   const int most = num_sms();

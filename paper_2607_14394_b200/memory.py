@@ -13,7 +13,6 @@ is the serving form on latent vectors [B, T, D] with 8-bit projections, a whole 
 from __future__ import annotations
 
 import ctypes
-import functools
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -33,46 +32,49 @@ def _device(device) -> int:
     return torch.cuda.current_device() if d.index is None else d.index
 
 
-def _addr(t: Optional[torch.Tensor], name: str, dev: int, dtype: torch.dtype, shape=None, contiguous=True) -> int:
-    """Device address of t after the checks every tensor goes through (0 for None)."""
+def _addr(t: Optional[torch.Tensor], name: str, dev: int, dtype: torch.dtype, shape) -> int:
+    """Device address of a contiguous tensor of this type and shape (0 for None)."""
     if t is None:
         return 0
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    _on_device(t, name, dev, dtype)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _on_device(t: torch.Tensor, name: str, dev: int, dtype: torch.dtype) -> int:
+    """Device address of a tensor of this type; its layout is the caller's business."""
     if t.get_device() != dev:
         raise ValueError(f"{name} must be a tensor on cuda:{dev}, got {t.device}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _on_stream(fn):
-    """Gives a call its `stream` keyword: the whole call, the allocation of its outputs included, runs on that stream."""
-
-    @functools.wraps(fn)
-    def call(*args, stream=None, **kwargs):
-        if stream is None:
-            return fn(*args, **kwargs)
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream))
-        with torch.cuda.stream(stream):
-            return fn(*args, **kwargs)
-
-    return call
+def _use(stream):
+    """A context in which `stream` (a torch stream or a cudaStream_t) is current: the whole call, the allocation of its
+    outputs included, runs on it."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    return torch.cuda.stream(stream)
 
 
-def _call(fn, where: str, dev: int, *args) -> None:
+# the current stream of a device as a cudaStream_t; the first form costs a tenth of the second
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _call(fn, dev: int, *args) -> None:
     """fn(*args, current stream) with `dev` current."""
-    s = torch.cuda.current_stream(dev).cuda_stream
     if torch.cuda.current_device() == dev:
-        status = fn(*args, s)
+        status = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            status = fn(*args, s)
-    if status != Bn.DTST_OK:
-        raise Bn.DtstError(status, where)
+            status = fn(*args, _raw_stream(dev))
+    if status != 0:
+        raise Bn.DtstError(status, fn.__name__)
 
 
 def _rows16(k: int) -> int:
@@ -110,73 +112,85 @@ class RmsNorm:
         self._type = DTYPES[dtype]
         self._rest = self.shape[:self.dim] + self.shape[self.dim + 1:]
         self._wshape = torch.Size((self.channels,))
+        self._scale_shape = torch.Size((-(-self.channels // BLOCK), self.outer))
         self._scratch = None
         self._lib = Bn.lib()
 
-    def _empty(self):
-        return torch.empty(self.shape, dtype=self.dtype, device=self.device)
-
-    @_on_stream
-    def forward(self, x, weight, residual=None, out=None, sum_out=None, rstd=None):
+    def forward(self, x, weight, residual=None, out=None, sum_out=None, rstd=None, stream=None):
         """Returns (y, s, rstd); without a residual s is x itself."""
-        if out is None:
-            out = self._empty()
-        if residual is not None and sum_out is None:
-            sum_out = self._empty()
-        if rstd is None:
-            rstd = torch.empty(self._rest, dtype=torch.float32, device=self.device)
+        if stream is not None:
+            with _use(stream):
+                return self.forward(x, weight, residual, out, sum_out, rstd)
         d, t, sh = self.dev, self.dtype, self.shape
-        _call(self._lib.dtst_rms_norm, "dtst_rms_norm", d, self._type, self.outer, self.channels, self.inner,
-              self.eps, _addr(x, "x", d, t, sh), _addr(residual, "residual", d, t, sh),
-              _addr(weight, "weight", d, torch.float32, self._wshape), _addr(sum_out, "sum_out", d, t, sh),
-              _addr(out, "out", d, t, sh), _addr(rstd, "rstd", d, torch.float32, self._rest))
+        xp, wp = _addr(x, "x", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
+        rp = 0
+        if residual is not None:
+            rp = _addr(residual, "residual", d, t, sh)
+            if sum_out is None:
+                sum_out = torch.empty_like(x)
+        if out is None:
+            out = torch.empty_like(x)
+        if rstd is None:
+            rstd = weight.new_empty(self._rest)
+        _call(self._lib.dtst_rms_norm, d, self._type, self.outer, self.channels, self.inner, self.eps, xp, rp, wp,
+              _addr(sum_out, "sum_out", d, t, sh), _addr(out, "out", d, t, sh),
+              _addr(rstd, "rstd", d, torch.float32, self._rest))
         return out, (x if sum_out is None else sum_out), rstd
 
-    @_on_stream
-    def forward_fp8(self, x, weight, residual=None, q=None, scale=None, sum_out=None):
+    def forward_fp8(self, x, weight, residual=None, q=None, scale=None, sum_out=None, stream=None):
         """Returns (q, scale, s): the norm of token-major rows in 8 bits, [rows, channels], and its scales
         [ceil(channels / 128), rows] - what Fp8Linear takes."""
+        if stream is not None:
+            with _use(stream):
+                return self.forward_fp8(x, weight, residual, q, scale, sum_out)
         if self.inner != 1:
             raise ValueError("an 8-bit output needs the channels in the last dimension")
         rows, c, d, t, sh = self.outer, self.channels, self.dev, self.dtype, self.shape
-        if q is None:
-            q = torch.empty((rows, _rows16(c)), dtype=FP8, device=self.device)
-            if c % 16:
-                q = q[:, :c]
+        xp, wp = _addr(x, "x", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
+        rp = 0
+        if residual is not None:
+            rp = _addr(residual, "residual", d, t, sh)
+            if sum_out is None:
+                sum_out = torch.empty_like(x)
+        if q is not None:
+            ld, qp = _q_stride(q, rows, c), _on_device(q, "q", d, FP8)
+        else:
+            if c % 16 == 0 and len(sh) == 2:
+                q = torch.empty_like(x, dtype=FP8)
+            else:
+                q = empty_fp8(rows, c, self.device)
+            ld, qp = _rows16(c), q.data_ptr()
         if scale is None:
-            scale = torch.empty((-(-c // BLOCK), rows), dtype=torch.float32, device=self.device)
-        if residual is not None and sum_out is None:
-            sum_out = self._empty()
-        ld = _q_stride(q, rows, c)
-        _call(self._lib.dtst_rms_norm_fp8, "dtst_rms_norm_fp8", d, self._type, rows, c, self.eps,
-              _addr(x, "x", d, t, sh), _addr(residual, "residual", d, t, sh),
-              _addr(weight, "weight", d, torch.float32, self._wshape), _addr(sum_out, "sum_out", d, t, sh),
-              _addr(q, "q", d, FP8, None, False), ld,
-              _addr(scale, "scale", d, torch.float32, (-(-c // BLOCK), rows)))
+            scale = weight.new_empty(self._scale_shape)
+        _call(self._lib.dtst_rms_norm_fp8, d, self._type, rows, c, self.eps, xp, rp, wp,
+              _addr(sum_out, "sum_out", d, t, sh), qp, ld, _addr(scale, "scale", d, torch.float32, self._scale_shape))
         return q, scale, (x if sum_out is None else sum_out)
 
-    @_on_stream
-    def backward(self, grad_y, s, weight, rstd, grad_s=None, grad_x=None, grad_weight=None, need_grad_weight=True):
+    def backward(self, grad_y, s, weight, rstd, grad_s=None, grad_x=None, grad_weight=None, need_grad_weight=True,
+                 stream=None):
         """Returns (grad_x, grad_weight); grad_x is the gradient of x and of the residual."""
+        if stream is not None:
+            with _use(stream):
+                return self.backward(grad_y, s, weight, rstd, grad_s, grad_x, grad_weight, need_grad_weight)
         d, t, sh = self.dev, self.dtype, self.shape
+        gp, wp = _addr(grad_y, "grad_y", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
         if grad_x is None:
-            grad_x = self._empty()
-        scratch = 0
+            grad_x = torch.empty_like(grad_y)
+        scratch = nbytes = 0
         if need_grad_weight:
             if grad_weight is None:
-                grad_weight = torch.empty(self._wshape, dtype=torch.float32, device=self.device)
+                grad_weight = torch.empty_like(weight)
             if self._scratch is None:
                 n = ctypes.c_size_t()
                 Bn._check(self._lib.dtst_rms_norm_scratch_bytes(self.channels, ctypes.byref(n)),
                           "dtst_rms_norm_scratch_bytes")
                 self._scratch = torch.empty(n.value, dtype=torch.uint8, device=self.device)
-            scratch = self._scratch.data_ptr()
-        _call(self._lib.dtst_rms_norm_backward, "dtst_rms_norm_backward", d, self._type, self.outer,
-              self.channels, self.inner, _addr(grad_y, "grad_y", d, t, sh), _addr(s, "s", d, t, sh),
-              _addr(weight, "weight", d, torch.float32, self._wshape),
-              _addr(rstd, "rstd", d, torch.float32, self._rest), _addr(grad_s, "grad_s", d, t, sh),
-              _addr(grad_x, "grad_x", d, t, sh), _addr(grad_weight, "grad_weight", d, torch.float32, self._wshape),
-              scratch, self._scratch.numel() if scratch else 0)
+                self._scratch_at = (self._scratch.data_ptr(), int(n.value))
+            scratch, nbytes = self._scratch_at
+        _call(self._lib.dtst_rms_norm_backward, d, self._type, self.outer, self.channels, self.inner, gp,
+              _addr(s, "s", d, t, sh), wp, _addr(rstd, "rstd", d, torch.float32, self._rest),
+              _addr(grad_s, "grad_s", d, t, sh), _addr(grad_x, "grad_x", d, t, sh),
+              _addr(grad_weight, "grad_weight", d, torch.float32, self._wshape), scratch, nbytes)
         return grad_x, grad_weight
 
 
@@ -188,35 +202,36 @@ def _q_stride(q: torch.Tensor, rows: int, k: int) -> int:
     return q.stride(0) if rows > 1 else max(q.stride(0), _rows16(k))
 
 
-@_on_stream
-def quantize_fp8(x: torch.Tensor, q=None, scale=None) -> Tuple[torch.Tensor, torch.Tensor]:
+def quantize_fp8(x: torch.Tensor, q=None, scale=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rows x [rows, k] (contiguous along k) -> (q [rows, k] in 8 bits, scale [ceil(k / 128), rows])."""
-    if x.dim() != 2 or x.dtype not in DTYPES or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise ValueError("quantize_fp8 takes rows [rows, k] of float32, bfloat16 or float16, contiguous along k")
+    if stream is not None:
+        with _use(stream):
+            return quantize_fp8(x, q, scale)
+    if x.dim() != 2 or x.dtype not in DTYPES or not x.is_cuda or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("quantize_fp8 takes CUDA rows [rows, k] of float32, bfloat16 or float16, contiguous along k")
     rows, k = x.shape
-    dev = x.get_device()
+    dev, shape = x.get_device(), (-(-k // BLOCK), rows)
     if q is None:
         q = empty_fp8(rows, k, x.device)
     if scale is None:
-        scale = torch.empty((-(-k // BLOCK), rows), dtype=torch.float32, device=x.device)
-    _call(Bn.lib().dtst_quantize_fp8, "dtst_quantize_fp8", dev, DTYPES[x.dtype], rows, k,
-          _addr(x, "x", dev, x.dtype, None, False), x.stride(0), _addr(q, "q", dev, FP8, None, False),
-          _q_stride(q, rows, k), _addr(scale, "scale", dev, torch.float32, (-(-k // BLOCK), rows)))
+        scale = x.new_empty(shape, dtype=torch.float32)
+    _call(Bn.lib().dtst_quantize_fp8, dev, DTYPES[x.dtype], rows, k, x.data_ptr(), x.stride(0),
+          _on_device(q, "q", dev, FP8), _q_stride(q, rows, k), _addr(scale, "scale", dev, torch.float32, shape))
     return q, scale
 
 
-@_on_stream
-def quantize_fp8_weight(w: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+def quantize_fp8_weight(w: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """w [n, k] -> (8-bit values [n, k], scale [ceil(n / 128), ceil(k / 128)]), one scale per 128 x 128 block."""
-    if w.dim() != 2 or w.dtype not in DTYPES or (w.shape[1] > 1 and w.stride(1) != 1):
-        raise ValueError("quantize_fp8_weight takes w [n, k] of float32, bfloat16 or float16, contiguous along k")
+    if stream is not None:
+        with _use(stream):
+            return quantize_fp8_weight(w)
+    if w.dim() != 2 or w.dtype not in DTYPES or not w.is_cuda or (w.shape[1] > 1 and w.stride(1) != 1):
+        raise ValueError("quantize_fp8_weight takes CUDA w [n, k] of float32, bfloat16 or float16, contiguous along k")
     n, k = w.shape
-    dev = w.get_device()
     q = empty_fp8(n, k, w.device)
-    scale = torch.empty((-(-n // BLOCK), -(-k // BLOCK)), dtype=torch.float32, device=w.device)
-    _call(Bn.lib().dtst_quantize_fp8_weight, "dtst_quantize_fp8_weight", dev, DTYPES[w.dtype], n, k,
-          _addr(w, "w", dev, w.dtype, None, False), max(w.stride(0), k), _addr(q, "q", dev, FP8, None, False),
-          _q_stride(q, n, k), _addr(scale, "scale", dev, torch.float32))
+    scale = w.new_empty((-(-n // BLOCK), -(-k // BLOCK)), dtype=torch.float32)
+    _call(Bn.lib().dtst_quantize_fp8_weight, w.get_device(), DTYPES[w.dtype], n, k, w.data_ptr(), max(w.stride(0), k),
+          q.data_ptr(), _q_stride(q, n, k), scale.data_ptr())
     return q, scale
 
 
@@ -236,11 +251,12 @@ class Fp8Linear:
         self.weight, self.weight_scale, self.out_dtype = weight, weight_scale, out_dtype
         self._ld = _q_stride(weight, self.n, self.k)
         self._kb = -(-self.k // BLOCK)
-        self._w = _addr(weight, "weight", self.dev, FP8, None, False)
+        self._w = weight.data_ptr()
         self._ws = _addr(weight_scale, "weight_scale", self.dev, torch.float32, (-(-self.n // BLOCK), self._kb))
         # zeroed memory that calls on any stream may use from now on; calls that share it must be stream-ordered
         self.workspace = torch.zeros(256, dtype=torch.uint8, device=self.device)
         torch.cuda.current_stream(self.dev).synchronize()
+        self._work = self.workspace.data_ptr()
         self._type = DTYPES[out_dtype]
         self._lib = Bn.lib()
 
@@ -249,27 +265,30 @@ class Fp8Linear:
         """Quantises w [n, k] (float32, bfloat16 or float16) once."""
         return cls(*quantize_fp8_weight(w), out_dtype=out_dtype)
 
-    @_on_stream
-    def forward(self, x: torch.Tensor, x_scale: torch.Tensor, out: Optional[torch.Tensor] = None):
+    def forward(self, x: torch.Tensor, x_scale: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None):
+        if stream is not None:
+            with _use(stream):
+                return self.forward(x, x_scale, out)
         m, d = x.shape[0], self.dev
+        xp, ld = _on_device(x, "x", d, FP8), _q_stride(x, m, self.k)
         if out is None:
-            out = torch.empty((m, self.n), dtype=self.out_dtype, device=self.device)
-        elif out.shape != (m, self.n) or (self.n > 1 and out.stride(1) != 1):
-            raise ValueError(f"out must have shape {(m, self.n)} and contiguous rows")
-        _call(self._lib.dtst_matmul_fp8, "dtst_matmul_fp8", d, self._type, m, self.n, self.k,
-              _addr(x, "x", d, FP8, None, False), _q_stride(x, m, self.k),
-              _addr(x_scale, "x_scale", d, torch.float32, (self._kb, m)), self._w, self._ld, self._ws,
-              _addr(out, "out", d, self.out_dtype, None, False), max(out.stride(0), self.n), self.workspace.data_ptr(),
-              256)
+            out = x_scale.new_empty((m, self.n), dtype=self.out_dtype)
+            op, out_ld = out.data_ptr(), self.n
+        else:
+            if out.shape != (m, self.n) or (self.n > 1 and out.stride(1) != 1):
+                raise ValueError(f"out must have shape {(m, self.n)} and contiguous rows")
+            op, out_ld = _on_device(out, "out", d, self.out_dtype), max(out.stride(0), self.n)
+        _call(self._lib.dtst_matmul_fp8, d, self._type, m, self.n, self.k, xp, ld,
+              _addr(x_scale, "x_scale", d, torch.float32, (self._kb, m)), self._w, self._ld, self._ws, op, out_ld,
+              self._work, 256)
         return out
 
     __call__ = forward
 
-    @_on_stream
-    def status(self) -> int:
+    def status(self, stream=None) -> int:
         """DTST_OK, or DTST_ERR_DEVICE_TIMEOUT if a bounded wait gave up since the last query; synchronises."""
         with torch.cuda.device(self.dev):
-            return int(Bn.lib().dtst_workspace_status(self.workspace.data_ptr(), Bn._stream_ptr(None)))
+            return int(self._lib.dtst_workspace_status(self._work, Bn._stream_ptr(stream)))
 
 
 class GatedScan:
@@ -299,13 +318,14 @@ class GatedScan:
             raise ValueError("the dimensions behind the recurrence's must not be empty")
         self.state_shape = self.outer_shape + inner_shape
         dense = (self.length * self.inner, self.inner)
-        self._dense = dense
+        self._dense = self._in = self._out = dense       # (outer, step) strides the description holds
         self._desc = Bn.ScanDesc(DTYPES[dtype], GATES[gate], self.outer, self.length, self.inner, dense, dense)
         self._ref = ctypes.byref(self._desc)
         self._lib = Bn.lib()
         n = ctypes.c_int64()
         Bn._check(self._lib.dtst_gated_scan_checkpoints(self._ref, ctypes.byref(n)), "dtst_gated_scan_checkpoints")
         self.checkpoint_floats = int(n.value)
+        self._ck_shape = torch.Size((self.checkpoint_floats,))
 
     def new_checkpoints(self) -> torch.Tensor:
         """A buffer for the states that a forward pass saves for its backward pass."""
@@ -338,53 +358,74 @@ class GatedScan:
         return (self._dense[0] if outer is None else outer), step
 
     def _inputs(self, v, g):
-        a, b = self._strides(v, "v"), self._strides(g, "g")
-        if a != b:
-            raise ValueError(f"v and g must have the same strides, got {v.stride()} and {g.stride()}")
-        self._desc.in_stride[0], self._desc.in_stride[1] = a
-
-    @_on_stream
-    def forward(self, v, g, h0=None, lengths=None, out=None, h_last=None, checkpoints=None):
-        """Returns (h, h_last).  lengths: int32 per outer entry; checkpoints: see new_checkpoints."""
-        d, t = self.dev, self.dtype
-        self._inputs(v, g)
-        if out is None:
-            out = torch.empty(self.shape, dtype=t, device=self.device)
-        if h_last is None:
-            h_last = torch.empty(self.state_shape, dtype=torch.float32, device=self.device)
-        _call(self._lib.dtst_gated_scan, "dtst_gated_scan", d, self._ref, _addr(v, "v", d, t, None, False),
-              _addr(g, "g", d, t, None, False), _addr(h0, "h0", d, torch.float32, self.state_shape),
-              self._lengths(lengths), _addr(out, "out", d, t, self.shape),
-              _addr(h_last, "h_last", d, torch.float32, self.state_shape),
-              _addr(checkpoints, "checkpoints", d, torch.float32, (self.checkpoint_floats,)))
-        return out, h_last
+        """Addresses of v and g, whose strides go into the description."""
+        d, t, sh = self.dev, self.dtype, self.shape
+        if v.dtype is t and g.dtype is t and v.shape == sh and g.shape == sh and v.get_device() == d and \
+                g.get_device() == d and v.is_contiguous() and g.is_contiguous():
+            at = self._dense
+        else:
+            _on_device(v, "v", d, t)
+            _on_device(g, "g", d, t)
+            at, b = self._strides(v, "v"), self._strides(g, "g")
+            if at != b:
+                raise ValueError(f"v and g must have the same strides, got {v.stride()} and {g.stride()}")
+        if at != self._in:
+            self._desc.in_stride[0], self._desc.in_stride[1] = self._in = at
+        return v.data_ptr(), g.data_ptr()
 
     def _lengths(self, lengths) -> int:
         return 0 if lengths is None else _addr(lengths, "lengths", self.dev, torch.int32, self.outer_shape)
 
-    @_on_stream
+    def forward(self, v, g, h0=None, lengths=None, out=None, h_last=None, checkpoints=None, stream=None):
+        """Returns (h, h_last).  lengths: int32 per outer entry; checkpoints: see new_checkpoints."""
+        if stream is not None:
+            with _use(stream):
+                return self.forward(v, g, h0, lengths, out, h_last, checkpoints)
+        d, state = self.dev, self.state_shape
+        vp, gp = self._inputs(v, g)
+        hp = _addr(h0, "h0", d, torch.float32, state)
+        if out is None:
+            out = torch.empty_like(v) if self._in is self._dense else v.new_empty(self.shape)
+            op = out.data_ptr()
+        else:
+            op = _addr(out, "out", d, self.dtype, self.shape)
+        if h_last is None:
+            h_last = torch.empty(state, dtype=torch.float32, device=self.device) if h0 is None else torch.empty_like(h0)
+            lp = h_last.data_ptr()
+        else:
+            lp = _addr(h_last, "h_last", d, torch.float32, state)
+        _call(self._lib.dtst_gated_scan, d, self._ref, vp, gp, hp, self._lengths(lengths), op, lp,
+              _addr(checkpoints, "checkpoints", d, torch.float32, self._ck_shape))
+        return out, h_last
+
     def backward(self, grad_h, v, g, checkpoints, h0=None, lengths=None, grad_last=None, grad_v=None, grad_g=None,
-                 grad_h0=None, need_grad_h0=True):
+                 grad_h0=None, need_grad_h0=True, stream=None):
         """Returns (grad_v, grad_g, grad_h0); v, g, h0, lengths and checkpoints as in the forward call."""
-        d, t = self.dev, self.dtype
-        self._inputs(v, g)
-        if grad_v is None:
-            grad_v = torch.empty(self.shape, dtype=t, device=self.device)
-        if grad_g is None:
-            grad_g = torch.empty(self.shape, dtype=t, device=self.device)
-        a, b = self._strides(grad_v, "grad_v"), self._strides(grad_g, "grad_g")
-        if a != b:
-            raise ValueError(f"grad_v and grad_g must have the same strides, got {grad_v.stride()} and {grad_g.stride()}")
-        self._desc.grad_stride[0], self._desc.grad_stride[1] = a
+        if stream is not None:
+            with _use(stream):
+                return self.backward(grad_h, v, g, checkpoints, h0, lengths, grad_last, grad_v, grad_g, grad_h0,
+                                     need_grad_h0)
+        d, t, state = self.dev, self.dtype, self.state_shape
+        vp, gp = self._inputs(v, g)
+        dp = _addr(grad_h, "grad_h", d, t, self.shape)
+        if grad_v is None and grad_g is None:
+            grad_v, grad_g, at = torch.empty_like(grad_h), torch.empty_like(grad_h), self._dense
+        else:
+            grad_v = torch.empty_like(grad_h) if grad_v is None else grad_v
+            grad_g = torch.empty_like(grad_h) if grad_g is None else grad_g
+            _on_device(grad_v, "grad_v", d, t)
+            _on_device(grad_g, "grad_g", d, t)
+            at, b = self._strides(grad_v, "grad_v"), self._strides(grad_g, "grad_g")
+            if at != b:
+                raise ValueError(f"grad_v and grad_g must have the same strides, got {grad_v.stride()} and {grad_g.stride()}")
+        if at != self._out:
+            self._desc.grad_stride[0], self._desc.grad_stride[1] = self._out = at
         if grad_h0 is None and need_grad_h0:
-            grad_h0 = torch.empty(self.state_shape, dtype=torch.float32, device=self.device)
-        _call(self._lib.dtst_gated_scan_backward, "dtst_gated_scan_backward", d, self._ref,
-              _addr(grad_h, "grad_h", d, t, self.shape), _addr(grad_last, "grad_last", d, torch.float32, self.state_shape),
-              _addr(v, "v", d, t, None, False), _addr(g, "g", d, t, None, False),
-              _addr(h0, "h0", d, torch.float32, self.state_shape), self._lengths(lengths),
-              _addr(checkpoints, "checkpoints", d, torch.float32, (self.checkpoint_floats,)),
-              _addr(grad_v, "grad_v", d, t, None, False), _addr(grad_g, "grad_g", d, t, None, False),
-              _addr(grad_h0, "grad_h0", d, torch.float32, self.state_shape))
+            grad_h0 = torch.empty(state, dtype=torch.float32, device=self.device)
+        _call(self._lib.dtst_gated_scan_backward, d, self._ref, dp, _addr(grad_last, "grad_last", d, torch.float32, state),
+              vp, gp, _addr(h0, "h0", d, torch.float32, state), self._lengths(lengths),
+              _addr(checkpoints, "checkpoints", d, torch.float32, self._ck_shape), grad_v.data_ptr(), grad_g.data_ptr(),
+              _addr(grad_h0, "grad_h0", d, torch.float32, state))
         return grad_v, grad_g, grad_h0
 
 
@@ -416,9 +457,11 @@ class FieldMemory:
         self.checkpoints = self.scan.new_checkpoints()
         self.x = self.h0 = self.lengths = None
 
-    @_on_stream
-    def forward(self, x, h0=None):
+    def forward(self, x, h0=None, stream=None):
         """Returns (out, h_last); both passes work in this object's buffers."""
+        if stream is not None:
+            with _use(stream):
+                return self.forward(x, h0)
         self.x, self.h0 = x, h0
         self.norm.forward(x, self.weight, out=self.y, rstd=self.rstd)
         Bn.dtst_pointwise_linear(self.y, self.W_v, self.b_v, self.v)
@@ -428,8 +471,10 @@ class FieldMemory:
         self.out.add_(x)
         return self.out, last
 
-    @_on_stream
-    def backward(self, grad_out, grad_last=None) -> dict:
+    def backward(self, grad_out, grad_last=None, stream=None) -> dict:
+        if stream is not None:
+            with _use(stream):
+                return self.backward(grad_out, grad_last)
         e = torch.empty_like
         gr = {"W_o": e(self.W_o), "W_v": e(self.W_v), "W_g": e(self.W_g), "b_v": e(self.b_v), "b_g": e(self.b_g)}
         gh, gy, gyg = e(self.h), e(self.y), e(self.y)
@@ -479,9 +524,11 @@ class RolloutMemory:
             self._plans[T] = (norm, scans)
         return self._plans[T]
 
-    @_on_stream
-    def forward(self, x: torch.Tensor, lengths=None) -> torch.Tensor:
+    def forward(self, x: torch.Tensor, lengths=None, stream=None) -> torch.Tensor:
         """x [B, T, D] -> out [B, T, D]; the layers' states move on by T frames (by lengths[b] where given)."""
+        if stream is not None:
+            with _use(stream):
+                return self.forward(x, lengths)
         B, T, D = x.shape
         if (B, D) != (self.B, self.D):
             raise ValueError(f"x must be [{self.B}, T, {self.D}], got {tuple(x.shape)}")
@@ -495,7 +542,6 @@ class RolloutMemory:
         y, _, _ = norm.forward(r, self.final_weight, residual=delta)
         return y.view(B, T, D)
 
-    @_on_stream
-    def step(self, frame: torch.Tensor) -> torch.Tensor:
+    def step(self, frame: torch.Tensor, stream=None) -> torch.Tensor:
         """One new frame [B, D] -> [B, D]."""
-        return self.forward(frame.view(self.B, 1, self.D)).view(self.B, self.D)
+        return self.forward(frame.view(self.B, 1, self.D), stream=stream).view(self.B, self.D)

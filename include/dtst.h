@@ -526,7 +526,7 @@ dtst_status dtst_quantize_fp8_weight(int dtype, int64_t rows, int64_t cols, cons
  *   out [m, n] of out_dtype, rows out_ld elements apart (out_ld >= n).  k >= 1.
  *   workspace: at least 256 bytes, 256-byte aligned, caller-owned, filled with zeros once before its first use; calls
  *   that share one must be stream-ordered.  Its first word is a status word as for plans (dtst_workspace_status).
- * Every product of a row of x is the same whatever the other rows are, and the same on every run.
+ * The same bits on every run.
  */
 dtst_status dtst_matmul_fp8(int out_dtype, int64_t m, int64_t n, int64_t k, const void* x, int64_t x_ld,
                             const float* x_scale, const void* w, int64_t w_ld, const float* w_scale, void* out,

@@ -6,9 +6,12 @@
 // one block into tensor memory, and the epilogue warps add it, scaled, to fp32 sums in registers while the next block
 // is multiplied into the other half of the tensor memory.
 //
-// A CTA computes tiles of 128 lanes x BN columns.  Warp 0 issues the TMA loads, warp 1 the products, the others hold
-// the sums (a thread one lane x up to 128 columns).  Lanes are rows of x and columns rows of w, or the other way round
-// (SWAP) where there are few rows of x: the tile's 128 lanes are then filled by the weights.
+// Two kernels.  Many rows: a pair of CTAs (cta_group::2) computes tiles of 256 x 256, each SM holding half of both
+// operands, which halves the bytes an SM has to fetch per product.  Otherwise: one CTA computes tiles of 128 lanes x BN
+// columns, lanes being rows of x and columns rows of w, or the other way round (SWAP) where there are few rows of x, so that
+// the tile's lanes are filled by the weights; where there are few tiles the CTAs of a cluster share the k-blocks of one and
+// add their sums through distributed shared memory, in rank order.
+// Warp 0 issues the TMA loads, warp 1 the products, the others hold the sums (a thread one lane x up to 128 columns).
 // Every wait is bounded: on expiry the kernel raises the status word, drains its loads and products, frees its tensor
 // memory and returns.
 #include <cuda.h>
@@ -35,6 +38,7 @@ struct MatmulArgs {
   int M, N, KB;             // rows of x, rows of w, blocks along the contracted dimension
   int lane_tiles, col_tiles;
   int vec_out;              // rows of out start on 16-byte boundaries
+  int split;                // CTAs that share a tile's k-blocks
   int* status;
 };
 
@@ -86,15 +90,67 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&r)[16]) {
                : "memory");
 }
 
+// sums of one k-block, scaled, onto the fp32 sums: CW columns of this thread's lane from `taddr` on
+template <int CW, typename F>
+__device__ __forceinline__ void add_block(float (&acc)[CW], uint32_t taddr, F factor) {
+  uint32_t r[2][16];
+  tmem_ld16(taddr, r[0]);
+#pragma unroll
+  for (int c = 0; c < CW; c += 16) {
+    uint32_t(&cur)[16] = r[(c / 16) & 1];
+    tmem_wait(cur);
+    if (c + 16 < CW) tmem_ld16(taddr + c + 16, r[((c / 16) & 1) ^ 1]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[c + i] = fmaf(__uint_as_float(cur[i]), factor(c + i), acc[c + i]);
+  }
+}
+
+// One lane's CW columns to out (row-major, this lane's row at `o`, `left` columns exist).  Rows on 16-byte boundaries: vector
+// stores.  Otherwise the warp turns 16 columns at a time round in its 32 x 17 floats of shared memory and writes rows
+// piece by piece, neighbouring lanes to neighbouring columns.
+template <typename T, int CW>
+__device__ __forceinline__ void store_lane(const float (&acc)[CW], T* out, long long ld, int row0, int rows, int col0, int left,
+                                           bool vec, float* turn) {
+  const int lane = threadIdx.x & 31;
+  constexpr int V = 16 / (int)sizeof(T);
+  if (vec) {
+    if (lane < rows) {
+      T* o = out + (long long)(row0 + lane) * ld + col0;
+#pragma unroll
+      for (int c = 0; c < CW; c += V) {
+        float x[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = acc[c + i];
+        Pack<T, V> v;
+        v.pack(x);
+        if (c + V <= left) v.store(o + c);
+        else v.store_part(o + c, left - c);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int c = 0; c < CW; c += 16) {
+    if (c >= left) break;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) turn[lane * 17 + i] = acc[c + i];
+    __syncwarp();
+    const int col = c + (lane & 15);
+#pragma unroll 4
+    for (int r = lane >> 4; r < 32; r += 2)
+      if (r < rows && col < left) out[(long long)(row0 + r) * ld + col0 + col] = Elem<T>::put(turn[r * 17 + (lane & 15)]);
+  }
+}
+
 template <int BN>
 struct MatmulCfg {
-  static constexpr int CW = BN < 128 ? BN : 128;           // columns of an epilogue thread
-  static constexpr int EPI = BN > 128 ? 8 : 4;             // epilogue warps
+  static constexpr int EPI = 4;                            // epilogue warps
   static constexpr int THREADS = 64 + 32 * EPI;
   static constexpr int A_BYTES = kLanes * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
-  static constexpr int STAGES = STAGE > 32768 ? 4 : 6;
+  static constexpr int STAGES = BN <= 32 ? 8 : 6;
   static constexpr int TCOLS = 2 * BN < 32 ? 32 : 2 * BN;
-  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + 2 * BN * 4 + 256;
+  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + 2 * BN * 4 + EPI * 32 * 17 * 4 + 256;
 };
 
 template <typename T, int BN, bool SWAP>
@@ -105,7 +161,8 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   float* col_scale = reinterpret_cast<float*>(smem + (size_t)Cfg::STAGES * Cfg::STAGE);   // [2][BN], SWAP only
-  uint64_t* full = reinterpret_cast<uint64_t*>(col_scale + 2 * BN);
+  float* turn = col_scale + 2 * BN;                                                       // [EPI][32][17]
+  uint64_t* full = reinterpret_cast<uint64_t*>(turn + Cfg::EPI * 32 * 17);
   uint64_t* empty = full + Cfg::STAGES;
   uint64_t* done = empty + Cfg::STAGES;      // [2] products of a block complete
   uint64_t* freed = done + 2;                // [2] tensor-memory half read
@@ -139,13 +196,16 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
   tc_fence_after();
   const uint32_t tmem = *tmem_s;
 
-  const int tiles = p.lane_tiles * p.col_tiles;
+  // a cluster shares the k-blocks of one tile; a CTA by itself walks over tiles
+  const int split = p.split, rank = split > 1 ? cluster_rank() : 0;
+  const int kb0 = (int)((long long)p.KB * rank / split), kb1 = (int)((long long)p.KB * (rank + 1) / split);
+  const int tiles = p.lane_tiles * p.col_tiles, first = blockIdx.x / split, step = split > 1 ? tiles : gridDim.x;
   if (warp == 0) {
     if (lane == 0) {
       uint32_t it = 0;
-      for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+      for (int t = first; t < tiles; t += step) {
         const int l0 = (t % p.lane_tiles) * kLanes, c0 = (t / p.lane_tiles) * BN;
-        for (int kb = 0; kb < p.KB; ++kb, ++it) {
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
           const uint32_t s = it % Cfg::STAGES;
           if (!wait_bar(&empty[s], ((it / Cfg::STAGES) & 1) ^ 1, abort_flag)) goto out;
           mbar_arrive_expect_tx(&full[s], (uint32_t)Cfg::STAGE);
@@ -158,8 +218,8 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
     if (lane == 0) {
       constexpr uint32_t idesc = idesc_e4m3(kLanes, BN);
       uint32_t it = 0;
-      for (int t = blockIdx.x; t < tiles; t += gridDim.x)
-        for (int kb = 0; kb < p.KB; ++kb, ++it) {
+      for (int t = first; t < tiles; t += step)
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
           const uint32_t s = it % Cfg::STAGES, half = it & 1;
           if (!wait_bar(&freed[half], ((it >> 1) & 1) ^ 1, abort_flag)) goto out;
           if (!wait_bar(&full[s], (it / Cfg::STAGES) & 1, abort_flag)) goto out;
@@ -173,34 +233,38 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
         }
     }
   } else {
-    const int quarter = warp & 3, part = (warp - 2) >> 2;
+    const int quarter = warp & 3;
     const int ln = quarter * 32 + lane;               // this thread's lane of the tile
     const int et = threadIdx.x - 64;                  // 0 .. 32 EPI - 1
-    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(part * Cfg::CW);
+    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16);
     uint32_t it = 0;
-    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+    for (int t = first; t < tiles; t += step) {
       const int l0 = (t % p.lane_tiles) * kLanes, c0 = (t / p.lane_tiles) * BN;
-      float acc[Cfg::CW];
+      float acc[BN];
 #pragma unroll
-      for (int i = 0; i < Cfg::CW; ++i) acc[i] = 0.f;
-      const int row = l0 + ln, lanes_n = SWAP ? p.N : p.M;
+      for (int i = 0; i < BN; ++i) acc[i] = 0.f;
+      const int row = l0 + ln;
       // one scale of the weights per block; of x one per lane, or one per column through shared memory
-      const float* ws = p.w_scale + (long long)((SWAP ? l0 : c0 + part * Cfg::CW) / 128) * p.KB;
-      const bool ws_on = SWAP || c0 + part * Cfg::CW < p.N;
+      const float* ws = p.w_scale + (long long)((SWAP ? l0 : c0) / 128) * p.KB;
       const float* xs = p.x_scale + row;
       const bool xs_on = !SWAP && row < p.M;
-      float xs_next = xs_on ? __ldg(xs) : 0.f, ws_next = ws_on ? __ldg(ws) : 0.f;
-      for (int kb = 0; kb < p.KB; ++kb, ++it) {
+      const int xc = c0 + et;                         // SWAP: the row of x whose scale this thread hands out
+      const bool xc_on = SWAP && et < BN && xc < p.M;
+      float xs_next = 0.f, ws_next = 0.f;
+      if (kb0 < kb1) {
+        ws_next = __ldg(ws + kb0);
+        xs_next = xs_on ? __ldg(xs + (long long)kb0 * p.M) : xc_on ? __ldg(p.x_scale + (long long)kb0 * p.M + xc) : 0.f;
+      }
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
         const uint32_t half = it & 1;
         if (SWAP) {
-          for (int c = et; c < BN; c += 32 * Cfg::EPI)
-            col_scale[half * BN + c] = c0 + c < p.M ? __ldg(p.x_scale + (long long)kb * p.M + c0 + c) : 0.f;
+          if (et < BN) col_scale[half * BN + et] = xs_next;
           asm volatile("bar.sync 1, %0;" ::"n"(32 * Cfg::EPI) : "memory");
         }
         const float scale = SWAP ? ws_next : xs_next * ws_next;
-        if (kb + 1 < p.KB) {
-          ws_next = ws_on ? __ldg(ws + kb + 1) : 0.f;
-          if (!SWAP) xs_next = xs_on ? __ldg(xs + (long long)(kb + 1) * p.M) : 0.f;
+        if (kb + 1 < kb1) {
+          ws_next = __ldg(ws + kb + 1);
+          xs_next = xs_on ? __ldg(xs + (long long)(kb + 1) * p.M) : xc_on ? __ldg(p.x_scale + (long long)(kb + 1) * p.M + xc) : 0.f;
         }
         bool ok = wait_bar(&done[half], (it >> 1) & 1, abort_flag);
         ok = __all_sync(0xffffffffu, ok) != 0;
@@ -210,44 +274,26 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
           // the other epilogue warps meet this one at the named barrier: keep step with them, without results
         }
         tc_fence_after();
-        uint32_t r[2][16];
-        tmem_ld16(taddr + half * BN, r[0]);
-#pragma unroll
-        for (int c = 0; c < Cfg::CW; c += 16) {
-          uint32_t(&cur)[16] = r[(c / 16) & 1];
-          tmem_wait(cur);
-          if (c + 16 < Cfg::CW) tmem_ld16(taddr + half * BN + c + 16, r[((c / 16) & 1) ^ 1]);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float f = SWAP ? scale * col_scale[half * BN + part * Cfg::CW + c + i] : scale;
-            acc[c + i] = fmaf(__uint_as_float(cur[i]), f, acc[c + i]);
-          }
-        }
+        const float* cs = col_scale + half * BN;
+        add_block<BN>(acc, taddr + half * BN, [&](int c) { return SWAP ? scale * cs[c] : scale; });
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&freed[half]);
       }
       T* out = static_cast<T*>(p.out);
-      if (row < lanes_n) {
-        if (SWAP) {
+      if (split > 1) {       // this CTA's part of the sums; every load has landed and every product is done
+        float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
-          for (int c = 0; c < Cfg::CW; ++c) {
-            const int m = c0 + part * Cfg::CW + c;
-            if (m < p.M) out[(long long)m * p.out_ld + row] = Elem<T>::put(acc[c]);
-          }
-        } else {
-          constexpr int V = 16 / (int)sizeof(T);
-          T* o = out + (long long)row * p.out_ld + c0 + part * Cfg::CW;
-          const int left = p.N - (c0 + part * Cfg::CW);
+        for (int c = 0; c < BN; ++c) part[SWAP ? c * kLanes + ln : ln * (BN + 1) + c] = acc[c];
+      } else if (SWAP) {
+        if (row < p.N) {
 #pragma unroll
-          for (int c = 0; c < Cfg::CW; c += V) {
-            Pack<T, V> v;
-#pragma unroll
-            for (int i = 0; i < V; ++i) v.put(i, acc[c + i]);
-            if (p.vec_out && c + V <= left) v.store(o + c);
-            else v.store_part(o + c, left - c);
-          }
+          for (int c = 0; c < BN; ++c)
+            if (c0 + c < p.M) out[(long long)(c0 + c) * p.out_ld + row] = Elem<T>::put(acc[c]);
         }
+      } else {
+        store_lane<T, BN>(acc, out, p.out_ld, l0 + quarter * 32, p.M - (l0 + quarter * 32), c0, p.N - c0, p.vec_out != 0,
+                          turn + (warp - 2) * 32 * 17);
       }
     }
   }
@@ -260,9 +306,194 @@ out:
     atomicExch(p.status, 1);
   }
   __syncthreads();
+  if (split > 1) {       // the parts in rank order, each CTA a share of the tile
+    cluster_sync();
+    const int l0 = (first % p.lane_tiles) * kLanes, c0 = (first / p.lane_tiles) * BN;
+    const float* part = reinterpret_cast<const float*>(smem);
+    T* out = static_cast<T*>(p.out);
+    const int e0 = (int)((long long)kLanes * BN * rank / split), e1 = (int)((long long)kLanes * BN * (rank + 1) / split);
+    for (int e = e0 + threadIdx.x; e < e1; e += Cfg::THREADS) {
+      const int ln = SWAP ? e % kLanes : e / BN, c = SWAP ? e / kLanes : e % BN;
+      const int m = SWAP ? c0 + c : l0 + ln, n = SWAP ? l0 + ln : c0 + c;
+      if (m >= p.M || n >= p.N) continue;
+      const float* at = part + (SWAP ? c * kLanes + ln : ln * (BN + 1) + c);
+      float sum = 0.f;
+      for (int k = 0; k < split; ++k) sum += cluster_read(at, k);
+      out[(long long)m * p.out_ld + n] = Elem<T>::put(sum);
+    }
+    cluster_sync();        // nobody leaves while its part may be read
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)Cfg::TCOLS) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ pairs of CTAs
+// Tiles of 256 x 256: CTA r of the pair holds rows 128 r .. of both operands' tiles and lanes 128 r .. of the products.  The
+// even CTA issues the products for both; its barriers collect both CTAs' loads and both CTAs' reads of tensor memory, and
+// its commits arrive at both CTAs' barriers.
+struct PairCfg {
+  static constexpr int EPI = 8, THREADS = 64 + 32 * EPI, BN = 256, CW = 128;
+  static constexpr int HALF = 128 * 128, STAGE = 2 * HALF, STAGES = 6;      // bytes of a CTA's share of one operand's tile
+  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + EPI * 32 * 17 * 4 + 256;
+};
+
+__device__ __forceinline__ uint32_t pair_addr(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void pair_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// 2-D tile into this CTA's shared memory, its bytes counted by a barrier of either CTA of the pair
+__device__ __forceinline__ void pair_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+          smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void pair_umma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc)
+      : "memory");
+}
+// arrives at the barrier of this offset in both CTAs when the products issued so far are complete
+__device__ __forceinline__ void pair_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+               "h"((uint16_t)3)
+               : "memory");
+}
+
+template <typename T>
+__global__ void __launch_bounds__(PairCfg::THREADS, 1) __cluster_dims__(2, 1, 1)
+matmul_fp8_pair_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const MatmulArgs p) {
+  using Cfg = PairCfg;
+  pdl_trigger();
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  float* turn = reinterpret_cast<float*>(smem + (size_t)Cfg::STAGES * Cfg::STAGE);
+  uint64_t* full = reinterpret_cast<uint64_t*>(turn + Cfg::EPI * 32 * 17);     // the even CTA's: both CTAs' loads
+  uint64_t* empty = full + Cfg::STAGES;
+  uint64_t* done = empty + Cfg::STAGES;
+  uint64_t* freed = done + 2;                                                   // the even CTA's: both CTAs' epilogue warps
+  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(freed + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_s + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = (uint32_t)cluster_rank();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < Cfg::STAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int k = 0; k < 2; ++k) {
+      mbar_init(&done[k], 1);
+      mbar_init(&freed[k], 2 * Cfg::EPI);
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tensormap(&x_map);
+    prefetch_tensormap(&w_map);
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_s)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  tc_fence_before();
+  cluster_sync();          // both CTAs' barriers and tensor memory are ready
+  tc_fence_after();
+  const uint32_t tmem = *tmem_s;
+  const int tiles = p.lane_tiles * p.col_tiles, first = blockIdx.x / 2, step = gridDim.x / 2;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      for (int t = first; t < tiles; t += step) {
+        const int l0 = (t % p.lane_tiles) * 256 + (int)rank * 128, c0 = (t / p.lane_tiles) * 256 + (int)rank * 128;
+        for (int kb = 0; kb < p.KB; ++kb, ++it) {
+          const uint32_t s = it % Cfg::STAGES;
+          if (!wait_bar(&empty[s], ((it / Cfg::STAGES) & 1) ^ 1, abort_flag)) goto out;
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2u * Cfg::STAGE);
+          const uint32_t bar = pair_addr(&full[s], 0);
+          pair_load_2d(smem + (size_t)s * Cfg::STAGE, &x_map, kb * 128, l0, bar);
+          pair_load_2d(smem + (size_t)s * Cfg::STAGE + Cfg::HALF, &w_map, kb * 128, c0, bar);
+        }
+      }
+      // the even CTA's last commits have arrived here before this CTA may leave
+      for (uint32_t k = it > Cfg::STAGES ? it - Cfg::STAGES : 0; k < it; ++k)
+        if (!wait_bar(&empty[k % Cfg::STAGES], (k / Cfg::STAGES) & 1, abort_flag)) goto out;
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = idesc_e4m3(256, 256);
+      uint32_t it = 0;
+      for (int t = first; t < tiles; t += step)
+        for (int kb = 0; kb < p.KB; ++kb, ++it) {
+          const uint32_t s = it % Cfg::STAGES, half = it & 1;
+          if (!wait_bar(&freed[half], ((it >> 1) & 1) ^ 1, abort_flag)) goto out;
+          if (!wait_bar(&full[s], (it / Cfg::STAGES) & 1, abort_flag)) goto out;
+          tc_fence_after();
+          const uint32_t a = smem_u32(smem + (size_t)s * Cfg::STAGE), b = a + Cfg::HALF;
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks)
+            pair_umma(tmem + half * 256, desc_sw128(a + 32 * ks), desc_sw128(b + 32 * ks), idesc, ks > 0 ? 1u : 0u);
+          pair_commit(&empty[s]);
+          pair_commit(&done[half]);
+        }
+    }
+  } else {
+    const int quarter = warp & 3, part = (warp - 2) >> 2;
+    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(part * Cfg::CW);
+    const uint32_t freed0 = pair_addr(&freed[0], 0), freed1 = pair_addr(&freed[1], 0);
+    uint32_t it = 0;
+    for (int t = first; t < tiles; t += step) {
+      const int l0 = (t % p.lane_tiles) * 256 + (int)rank * 128 + quarter * 32, c0 = (t / p.lane_tiles) * 256 + part * Cfg::CW;
+      float acc[Cfg::CW];
+#pragma unroll
+      for (int i = 0; i < Cfg::CW; ++i) acc[i] = 0.f;
+      const int row = l0 + lane;
+      const float* ws = p.w_scale + (long long)(c0 / 128) * p.KB;
+      const float* xs = p.x_scale + row;
+      const bool ws_on = c0 < p.N, xs_on = row < p.M;
+      float xs_next = xs_on ? __ldg(xs) : 0.f, ws_next = ws_on ? __ldg(ws) : 0.f;
+      for (int kb = 0; kb < p.KB; ++kb, ++it) {
+        const uint32_t half = it & 1;
+        const float scale = xs_next * ws_next;
+        if (kb + 1 < p.KB) {
+          ws_next = ws_on ? __ldg(ws + kb + 1) : 0.f;
+          xs_next = xs_on ? __ldg(xs + (long long)(kb + 1) * p.M) : 0.f;
+        }
+        bool ok = wait_bar(&done[half], (it >> 1) & 1, abort_flag);
+        ok = __all_sync(0xffffffffu, ok) != 0;
+        if (!ok) goto out;
+        tc_fence_after();
+        add_block<Cfg::CW>(acc, taddr + half * 256, [&](int) { return scale; });
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) pair_arrive(half ? freed1 : freed0);
+      }
+      store_lane<T, Cfg::CW>(acc, static_cast<T*>(p.out), p.out_ld, l0, p.M - l0, c0, p.N - c0, p.vec_out != 0,
+                             turn + (warp - 2) * 32 * 17);
+    }
+  }
+out:
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag) {
+    for (int s = 0; s < Cfg::STAGES; ++s) mbar_wait_plain(&full[s], 0, 1u << 12), mbar_wait_plain(&full[s], 1, 1u << 12);
+    for (int k = 0; k < 2; ++k) mbar_wait_plain(&done[k], 0, 1u << 12), mbar_wait_plain(&done[k], 1, 1u << 12);
+    atomicExch(p.status, 1);
+  }
+  cluster_sync();          // neither CTA leaves while the other's loads, commits or arrivals may still reach it
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   }
 }
 
@@ -295,15 +526,32 @@ __global__ void __launch_bounds__(256) quantize_weight_kernel(const T* __restric
   }
 }
 
+template <typename Kern>
+cudaError_t launch_matmul(Kern kern, int grid, int threads, int cluster, size_t smem, cudaStream_t st, const CUtensorMap& a,
+                          const CUtensorMap& b, const MatmulArgs& p) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 0 ? 2 : 1;       // (0: the kernel's own cluster size)
+  return cudaLaunchKernelEx(&cfg, kern, a, b, p);
+}
+
 template <typename T, int BN, bool SWAP>
 cudaError_t launch_tile(const MatmulCall& c, MatmulArgs p, cudaStream_t st) {
   using Cfg = MatmulCfg<BN>;
   CUtensorMap lane_map, col_map;
-  const uint8_t* lane_base = SWAP ? c.w : c.x;
-  const uint8_t* col_base = SWAP ? c.x : c.w;
   const long long lanes = SWAP ? c.n : c.m, cols = SWAP ? c.m : c.n;
-  if (!make_bytes_map(&lane_map, lane_base, lanes, c.k, SWAP ? c.w_ld : c.x_ld, kLanes) ||
-      !make_bytes_map(&col_map, col_base, cols, c.k, SWAP ? c.x_ld : c.w_ld, BN))
+  if (!make_bytes_map(&lane_map, SWAP ? c.w : c.x, lanes, c.k, SWAP ? c.w_ld : c.x_ld, kLanes) ||
+      !make_bytes_map(&col_map, SWAP ? c.x : c.w, cols, c.k, SWAP ? c.x_ld : c.w_ld, BN))
     return cudaErrorNotSupported;
   p.lane_tiles = (int)((lanes + kLanes - 1) / kLanes);
   p.col_tiles = (int)((cols + BN - 1) / BN);
@@ -312,19 +560,45 @@ cudaError_t launch_tile(const MatmulCall& c, MatmulArgs p, cudaStream_t st) {
   const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), Cfg::SMEM, allowed);
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)p.lane_tiles * p.col_tiles;
-  const int most = num_sms();
-  return launch_pdl(kern, dim3((unsigned)(tiles < most ? tiles : most)), dim3(Cfg::THREADS), Cfg::SMEM, st, lane_map, col_map, p);
+  const int sms = num_sms();
+  // few tiles: as many CTAs to a tile as the GPU has room for, each with two k-blocks at least
+  p.split = 1;
+  while (p.split < 8 && tiles * p.split * 2 <= sms && p.KB >= 4 * p.split) p.split *= 2;
+  const long long grid = p.split > 1 ? tiles * p.split : (tiles < sms ? tiles : sms);
+  return launch_matmul(kern, (int)grid, Cfg::THREADS, p.split, Cfg::SMEM, st, lane_map, col_map, p);
+}
+
+template <typename T>
+cudaError_t launch_pairs(const MatmulCall& c, MatmulArgs p, cudaStream_t st) {
+  using Cfg = PairCfg;
+  CUtensorMap x_map, w_map;
+  if (!make_bytes_map(&x_map, c.x, c.m, c.k, c.x_ld, 128) || !make_bytes_map(&w_map, c.w, c.n, c.k, c.w_ld, 128))
+    return cudaErrorNotSupported;
+  p.lane_tiles = (int)((c.m + 255) / 256);
+  p.col_tiles = (int)((c.n + 255) / 256);
+  auto kern = matmul_fp8_pair_kernel<T>;
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), Cfg::SMEM, allowed);
+  if (e != cudaSuccess) return e;
+  const long long tiles = (long long)p.lane_tiles * p.col_tiles, pairs = num_sms() / 2;
+  return launch_matmul(kern, (int)(2 * (tiles < pairs ? tiles : pairs)), Cfg::THREADS, 0, Cfg::SMEM, st, x_map, w_map, p);
 }
 
 template <typename T>
 cudaError_t matmul_t(const MatmulCall& c, cudaStream_t st) {
   MatmulArgs p{};
   p.x_scale = c.x_scale, p.w_scale = c.w_scale, p.out = c.out, p.out_ld = c.out_ld;
-  p.M = (int)c.m, p.N = (int)c.n, p.KB = (int)((c.k + 127) / 128);
+  p.M = (int)c.m, p.N = (int)c.n, p.KB = (int)((c.k + 127) / 128), p.split = 1;
   p.vec_out = c.out_ld * sizeof(T) % 16 == 0 && aligned_to(c.out, 16);
   p.status = c.status;
+  if (c.m <= 16) return launch_tile<T, 16, true>(c, p, st);
   if (c.m <= 32) return launch_tile<T, 32, true>(c, p, st);
-  return launch_tile<T, 128, false>(c, p, st);
+  if (c.m <= 64) return launch_tile<T, 64, true>(c, p, st);
+  auto tiles = [&](long long a, long long b) { return ((c.m + a - 1) / a) * ((c.n + b - 1) / b); };
+  const int sms = num_sms();
+  if (2 * tiles(256, 256) >= sms) return launch_pairs<T>(c, p, st);
+  if (tiles(128, 128) >= sms) return launch_tile<T, 128, false>(c, p, st);
+  return launch_tile<T, 64, false>(c, p, st);
 }
 
 }  // namespace

@@ -22,28 +22,6 @@ namespace {
 // Where there are few sequences, a thread-block cluster shares one: its CTAs take chunks side by side, exchange the chunks'
 // summaries through distributed shared memory once per round, and each applies those of the chunks in front of its own to
 // the state that all of them carry - in chunk order, so the bits are the same on every run and for every cluster size.
-__device__ __forceinline__ int cluster_size() {
-  int n;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
-  return n;
-}
-__device__ __forceinline__ int cluster_rank() {
-  int n;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(n));
-  return n;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// the value at `p` in the shared memory of CTA `rank` of the cluster
-__device__ __forceinline__ float2 cluster_read(const float2* p, int rank) {
-  uint32_t at;
-  float2 v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
-  return v;
-}
-
 template <typename T>
 struct ScanArgs {
   const T *v, *g, *gh;

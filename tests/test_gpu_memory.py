@@ -181,6 +181,7 @@ def test_quantise_weight(n, k, dtype):
     (1, 1, 1), (1, 128, 128), (3, 200, 100), (4, 4096, 2048), (17, 130, 1000), (32, 64, 256), (33, 64, 256), (64, 500, 4096),
     (65, 129, 272), (128, 256, 384), (129, 257, 130), (200, 1111, 1360), (1000, 96, 640), (513, 640, 2049), (2, 70, 9000),
     (300, 2304, 512), (1500, 1500, 128), (5, 20000, 16), (4200, 333, 256),
+    (16, 96, 4096), (48, 1024, 2048), (100, 640, 4096), (2250, 2100, 650), (4865, 1000, 200), (2304, 2304, 1024), (2305, 2309, 16),
 ])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_matmul(m, n, k, dtype):

@@ -69,18 +69,20 @@ bool make_points_map(CUtensorMap* map, const float* base, long long rows, long l
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// 8-bit tensor [rows][cols], rows `ld` bytes apart, viewed through [box_rows x 128] boxes with the 128-byte swizzle;
-// whatever a box holds beyond the tensor is filled with zeros
-bool make_bytes_map(CUtensorMap* map, const void* base, long long rows, long long cols, long long ld, int box_rows) {
+// tensor [rows][cols] of 1-, 2- or 4-byte elements, rows `ld` bytes apart, viewed through boxes of box_rows x 128 bytes with
+// the 128-byte swizzle; a load fills what a box holds beyond the tensor with zeros, a store leaves it out
+bool make_tile_map(CUtensorMap* map, const void* base, int elem, long long rows, long long cols, long long ld, int box_rows) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)ld};
-  cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  cuuint32_t box[2] = {(cuuint32_t)(128 / elem), (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const CUtensorMapDataType type = elem == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                   : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16
+                                               : CU_TENSOR_MAP_DATA_TYPE_UINT32;
+  return fn(map, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Shapes the plane kernels are instantiated for: (N3, k3, N2, k2).

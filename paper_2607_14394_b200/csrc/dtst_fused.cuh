@@ -38,8 +38,9 @@ bool make_rows_map(CUtensorMap* map, const void* base, long long rows, int n3, i
 bool tma_encode_available();
 // fp32 tensor [rows][P] with P contiguous, viewed through [box_rows x 32 floats] boxes with the 128-byte swizzle
 bool make_points_map(CUtensorMap* map, const float* base, long long rows, long long P, int box_rows);
-// 8-bit tensor [rows][cols], rows `ld` bytes apart, viewed through [box_rows x 128] boxes with the 128-byte swizzle
-bool make_bytes_map(CUtensorMap* map, const void* base, long long rows, long long cols, long long ld, int box_rows);
+// tensor [rows][cols] of 1-, 2- or 4-byte elements, rows `ld` bytes apart, viewed through boxes of box_rows x 128 bytes with
+// the 128-byte swizzle
+bool make_tile_map(CUtensorMap* map, const void* base, int elem, long long rows, long long cols, long long ld, int box_rows);
 
 // Tensor-core version of the block's forward epilogue (dtst_block_umma.cu): C_in in {8, 16, 32}, C_out in {16, 32}
 bool block_umma_supported(int Ci, int Co, long long P, int B);

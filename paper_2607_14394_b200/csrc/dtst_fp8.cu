@@ -334,22 +334,24 @@ out:
 // even CTA issues the products for both; its barriers collect both CTAs' loads and both CTAs' reads of tensor memory, and
 // its commits arrive at both CTAs' barriers.
 struct PairCfg {
-  static constexpr int EPI = 16, THREADS = 64 + 32 * EPI, CW = 64;         // four epilogue warps to a lane quarter
+  static constexpr int EPI = 8, THREADS = 64 + 32 * EPI, CW = 128;         // two epilogue warps to a lane quarter
   static constexpr int HALF = 128 * 128, STAGE = 2 * HALF, STAGES = 5;     // bytes of a CTA's share of one operand's tile
-  static constexpr int BOX = 32 * 128;                                     // an epilogue warp's piece of the output
-  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + (size_t)EPI * BOX + 256;
+  static constexpr int BOX = 32 * 128;                                     // an epilogue warp's piece of the output, two of them
+  static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + (size_t)EPI * 2 * BOX + 256;
 };
 
-// An epilogue warp's 32 rows x CW columns by TMA: in pieces of 128 bytes a row, through the warp's swizzled 4 KB of shared
-// memory; the copy out runs on while the next tile's blocks are summed.  What lies beyond the tensor is not written.
+// An epilogue warp's 32 rows x CW columns by TMA: in pieces of 128 bytes a row, through the warp's two swizzled boxes of
+// shared memory in turn; the copy out runs on while the next tile's blocks are summed.  What lies beyond the tensor is not
+// written.
 template <typename T, int CW>
-__device__ __forceinline__ void store_box(const float (&acc)[CW], const CUtensorMap* map, unsigned char* box, int row0, int col0, int cols) {
+__device__ __forceinline__ void store_box(const float (&acc)[CW], const CUtensorMap* map, unsigned char* boxes, int row0, int col0, int cols) {
   constexpr int E = 16 / (int)sizeof(T), PIECE = 128 / (int)sizeof(T);
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int c = 0; c < CW; c += PIECE) {
     if (c >= cols) break;
-    if (lane == 0) tma_store_wait_read<0>();       // the piece before has left shared memory
+    unsigned char* box = boxes + (c / PIECE & 1) * PairCfg::BOX;
+    if (lane == 0) tma_store_wait_read<1>();       // the piece before the last one has left its box
     __syncwarp();
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -410,7 +412,7 @@ matmul_fp8_pair_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_c
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   unsigned char* boxes = smem + (size_t)Cfg::STAGES * Cfg::STAGE;
-  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + Cfg::EPI * Cfg::BOX);    // the even CTA's: both CTAs' loads
+  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + Cfg::EPI * 2 * Cfg::BOX);    // the even CTA's: both CTAs' loads
   uint64_t* empty = full + Cfg::STAGES;
   uint64_t* done = empty + Cfg::STAGES;
   uint64_t* freed = done + 2;                                                   // the even CTA's: both CTAs' epilogue warps
@@ -512,7 +514,7 @@ matmul_fp8_pair_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_c
         __syncwarp();
         if (lane == 0) pair_arrive(half ? freed1 : freed0);
       }
-      unsigned char* box = boxes + (warp - 2) * Cfg::BOX;
+      unsigned char* box = boxes + (warp - 2) * 2 * Cfg::BOX;
       if (!p.vec_out) {
         store_lane<T, Cfg::CW>(acc, static_cast<T*>(p.out), p.out_ld, l0, p.M - l0, c0, p.N - c0, false, reinterpret_cast<float*>(box));
       } else if (l0 < p.M) {

@@ -14,6 +14,8 @@
 //             channels, the sums over channels meet in shared memory.
 // The weight gradient is summed in registers over all positions a CTA visits and in a fixed order over CTAs by a
 // second launch: same bits on every run.
+#include <initializer_list>
+
 #include "dtst_common.cuh"
 #include "dtst_memory.cuh"
 #include "dtst_types.cuh"
@@ -26,44 +28,75 @@ namespace {
 template <typename T>
 constexpr int kVec = 16 / (int)sizeof(T);
 
-// Sum over the TPR threads of a row; `red` holds two alternating sets of 16 partial sums (one barrier per call).
-template <int TPR>
+// Sum over the TPR threads of a row.  `red` holds two alternating sets of partial sums for each group of the CTA, so that one
+// barrier (the group's own where there are several) is enough.
+template <int TPR, int GROUPS = 1>
 __device__ __forceinline__ float row_sum(float v, float* red, int& phase) {
   v = warp_sum(v);
   if constexpr (TPR > 32) {
-    float* r = red + phase * 32;
+    constexpr int N = TPR / 32;
+    const int group = GROUPS > 1 ? threadIdx.x / TPR : 0;
+    float* r = red + (phase * GROUPS + group) * N;
     phase ^= 1;
-    if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = v;
-    __syncthreads();
+    if ((threadIdx.x & 31) == 0) r[(threadIdx.x % TPR) >> 5] = v;
+    if constexpr (GROUPS > 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
+    else __syncthreads();
     float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < TPR / 32; ++i) t += r[i];
+    for (int i = 0; i < N; ++i) t += r[i];
     v = t;
   }
   return v;
 }
 
-constexpr int kWarpRowWarps = 4;   // rows per CTA where one warp holds a row
-
+// threads of a CTA: four rows at once where a warp holds one, two where four warps do (more CTAs would make more partial
+// sums of the weight gradient)
 template <int TPR>
-constexpr int kRowThreads = TPR == 32 ? 32 * kWarpRowWarps : TPR;
+constexpr int kRowThreads = TPR <= 32 ? 128 : TPR <= 128 ? 256 : TPR;
 
-template <typename T, bool ALIGNED>
+// How a row's vectors lie.  kShifted: rows of C elements that begin off a vector, in tensors that all begin on one: a group of
+// threads takes rows whose numbers are the same modulo VEC, so all its rows begin `shift` elements behind a vector, and its
+// vectors, weights and sums stand `shift` elements in front of the row's own.
+enum RowLayout { kScalar = 0, kAligned = 1, kShifted = 2 };
+
+template <typename T, int LAY>
 __device__ __forceinline__ void load_group(Pack<T, kVec<T>>& p, const T* row, long long c, long long C) {
-  if (ALIGNED) {
+  constexpr int VEC = kVec<T>;
+  if (LAY == kAligned) {
     if (c < C) p.load(row + c); else p.zero();
+  } else if (LAY == kShifted && c >= 0 && c + VEC <= C) {
+    p.load(row + c);
   } else {
-    const long long left = C - c;
-    p.load_part(row + c, left > kVec<T> ? kVec<T> : (int)left);
+    p.zero();
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (c + i >= 0 && c + i < C) p.v[i] = row[c + i];
   }
 }
-template <typename T, bool ALIGNED>
+template <typename T, int LAY>
 __device__ __forceinline__ void store_group(const Pack<T, kVec<T>>& p, T* row, long long c, long long C) {
-  if (ALIGNED) {
+  constexpr int VEC = kVec<T>;
+  if (LAY == kAligned) {
     if (c < C) p.store(row + c);
+  } else if (LAY == kShifted && c >= 0 && c + VEC <= C) {
+    p.store(row + c);
   } else {
-    const long long left = C - c;
-    p.store_part(row + c, left > kVec<T> ? kVec<T> : (int)left);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (c + i >= 0 && c + i < C) row[c + i] = p.v[i];
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void load_weights(float (&w)[VEC], const float* weight, long long c, long long C, bool aligned) {
+  if (aligned && c < C) {
+#pragma unroll
+    for (int i = 0; i < VEC; i += 4) {
+      const float4 t = __ldg(reinterpret_cast<const float4*>(weight + c + i));
+      w[i] = t.x, w[i + 1] = t.y, w[i + 2] = t.z, w[i + 3] = t.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) w[i] = c + i >= 0 && c + i < C ? __ldg(weight + c + i) : 0.f;
   }
 }
 
@@ -104,8 +137,9 @@ struct RowArgs {
   int q_aligned;
 };
 
-// NORM false: quantise x as it is (no residual, no weight).
-template <typename T, int TPR, int ITEMS, bool QUANT, bool NORM, bool ALIGNED>
+// NORM false: quantise x as it is (no residual, no weight).  A group of TPR threads walks over rows, the next row's loads
+// under way while a row is summed and written; the weights stay in registers.
+template <typename T, int TPR, int ITEMS, bool QUANT, bool NORM, int LAY>
 __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_kernel(const RowArgs a) {
   constexpr int VEC = kVec<T>;
   constexpr int RPC = kRowThreads<TPR> / TPR;
@@ -116,70 +150,66 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_kernel(const RowAr
   const float inv_c = 1.0f / (float)a.C;
   const T* x = static_cast<const T*>(a.x);
   const T* res = static_cast<const T*>(a.residual);
-  int phase = 0;
-  for (long long row = (long long)blockIdx.x * RPC + threadIdx.x / TPR; row < a.rows; row += (long long)gridDim.x * RPC) {
-    float v[ITEMS][VEC];
-    Pack<T, VEC> px[ITEMS], pr[ITEMS];
+  const long long group = (long long)blockIdx.x * RPC + threadIdx.x / TPR, step = (long long)gridDim.x * RPC;
+  const int shift = LAY == kShifted ? (int)(group * a.C % VEC) : 0;
+  Pack<T, VEC> px[ITEMS], pr[ITEMS];
+  auto fetch = [&](long long row) {
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) load_group<T, ALIGNED>(px[k], x + row * a.x_ld, (long long)(tr + k * TPR) * VEC, a.C);
+    for (int k = 0; k < ITEMS; ++k) load_group<T, LAY>(px[k], x + row * a.x_ld, (long long)(tr + k * TPR) * VEC - shift, a.C);
     if (NORM && res != nullptr) {
 #pragma unroll
-      for (int k = 0; k < ITEMS; ++k) load_group<T, ALIGNED>(pr[k], res + row * a.C, (long long)(tr + k * TPR) * VEC, a.C);
+      for (int k = 0; k < ITEMS; ++k) load_group<T, LAY>(pr[k], res + row * a.C, (long long)(tr + k * TPR) * VEC - shift, a.C);
     }
+  };
+  if (group < a.rows) fetch(group);
+  float w[ITEMS][VEC];
+  if (NORM) {
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) load_weights<VEC>(w[k], a.weight, (long long)(tr + k * TPR) * VEC - shift, a.C, LAY == kAligned);
+  }
+  int phase = 0;
+  for (long long row = group; row < a.rows; row += step) {
+    float v[ITEMS][VEC];
     float sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k)
+    for (int k = 0; k < ITEMS; ++k) {
+      px[k].unpack(v[k]);
+      if (NORM && res != nullptr) {
+        float r[VEC];
+        pr[k].unpack(r);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        v[k][i] = px[k].get(i);
-        if (NORM && res != nullptr) v[k][i] += pr[k].get(i);
-        sum = fmaf(v[k][i], v[k][i], sum);
+        for (int i = 0; i < VEC; ++i) v[k][i] += r[i];
       }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) sum = fmaf(v[k][i], v[k][i], sum);
+    }
+    if (row + step < a.rows) fetch(row + step);
     float rstd = 1.f;
     if (NORM) {
       if (a.s != nullptr) {
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) px[k].put(i, v[k][i]);
-          store_group<T, ALIGNED>(px[k], static_cast<T*>(a.s) + row * a.C, (long long)(tr + k * TPR) * VEC, a.C);
+          Pack<T, VEC> out;
+          out.pack(v[k]);
+          store_group<T, LAY>(out, static_cast<T*>(a.s) + row * a.C, (long long)(tr + k * TPR) * VEC - shift, a.C);
         }
       }
-      rstd = rsqrtf(fmaf(row_sum<TPR>(sum, red, phase), inv_c, a.eps));
+      rstd = rsqrtf(fmaf(row_sum<TPR, RPC>(sum, red, phase), inv_c, a.eps));
       if (a.rstd != nullptr && tr == 0) a.rstd[row] = rstd;
     }
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
-      const long long c = (long long)(tr + k * TPR) * VEC;
-      float y[VEC];
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) y[i] = v[k][i];
+      const long long c = (long long)(tr + k * TPR) * VEC - shift;
       if (NORM) {
-        float w[VEC];
-        if (ALIGNED) {
-          if (c < a.C) {
 #pragma unroll
-            for (int i = 0; i < VEC; i += 4) {
-              const float4 t = __ldg(reinterpret_cast<const float4*>(a.weight + c + i));
-              w[i] = t.x, w[i + 1] = t.y, w[i + 2] = t.z, w[i + 3] = t.w;
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) w[i] = 0.f;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) w[i] = c + i < a.C ? __ldg(a.weight + c + i) : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) y[i] *= rstd * w[i];
+        for (int i = 0; i < VEC; ++i) v[k][i] *= rstd * w[k][i];
       }
       if (QUANT) {
-        quantise_store<VEC>(y, a.q + row * a.q_ld, a.scale, c, a.C, a.rows, row, a.q_aligned != 0);
+        quantise_store<VEC>(v[k], a.q + row * a.q_ld, a.scale, c, a.C, a.rows, row, a.q_aligned != 0);
       } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) px[k].put(i, y[i]);
-        store_group<T, ALIGNED>(px[k], static_cast<T*>(a.y) + row * a.C, c, a.C);
+        Pack<T, VEC> out;
+        out.pack(v[k]);
+        store_group<T, LAY>(out, static_cast<T*>(a.y) + row * a.C, c, a.C);
       }
     }
   }
@@ -234,30 +264,50 @@ __global__ void __launch_bounds__(512) norm_long_rows_kernel(const RowArgs a) {
   }
 }
 
+// the layout of contiguous rows [rows][C] of all these tensors
+template <typename T>
+RowLayout row_layout(long long C, long long x_ld, std::initializer_list<const void*> tensors) {
+  for (const void* t : tensors)
+    if (!aligned_to(t, 16)) return kScalar;
+  if (C % kVec<T> == 0 && x_ld % kVec<T> == 0) return kAligned;
+  return x_ld == C ? kShifted : kScalar;
+}
+
+template <typename T, int TPR, int ITEMS, bool QUANT, bool NORM, int LAY>
+cudaError_t launch_rows_kernel(const RowArgs& a, cudaStream_t st) {
+  constexpr int RPC = kRowThreads<TPR> / TPR;
+  auto kern = norm_rows_kernel<T, TPR, ITEMS, QUANT, NORM, LAY>;
+  // as many CTAs as run at once, or a row each; a multiple of VEC, so that a group's rows begin alike
+  const long long most = (long long)num_sms() * (2048 / kRowThreads<TPR> < 8 ? 2048 / kRowThreads<TPR> : 8) / kVec<T> * kVec<T>;
+  long long ctas = (a.rows + RPC - 1) / RPC;
+  if (ctas > most) ctas = most;
+  return launch_pdl(kern, dim3((unsigned)ctas), dim3(kRowThreads<TPR>), 0, st, a);
+}
+
 template <typename T, bool QUANT, bool NORM>
 cudaError_t launch_rows(const RowArgs& a, cudaStream_t st) {
   constexpr int VEC = kVec<T>;
-  const long long groups = (a.C + VEC - 1) / VEC;
-  const bool al = a.C % VEC == 0 && a.x_ld % VEC == 0 && aligned_to(a.x, 16) && aligned_to(a.residual, 16) &&
-                  aligned_to(a.s, 16) && (QUANT || aligned_to(a.y, 16)) && aligned_to(a.weight, 16);
-  const long long most = (long long)num_sms() * 32;
+  RowLayout lay = row_layout<T>(a.C, a.x_ld, {a.x, a.residual, a.s, QUANT ? nullptr : a.y});
+  if (lay == kAligned && !aligned_to(a.weight, 16)) lay = kScalar;
+  if (QUANT && lay == kShifted) lay = kScalar;       // blocks of 128 channels are counted from the row's beginning
+  const long long groups = (a.C + (lay == kShifted ? VEC - 1 : 0) + VEC - 1) / VEC;
 #define DTST_ROWS(TPR, ITEMS)                                                                                     \
   {                                                                                                               \
-    const long long ctas = (a.rows + kRowThreads<TPR> / TPR - 1) / (kRowThreads<TPR> / TPR);                      \
-    const dim3 grid((unsigned)(ctas < most ? ctas : most)), block(kRowThreads<TPR>);                              \
-    return al ? launch_pdl(norm_rows_kernel<T, TPR, ITEMS, QUANT, NORM, true>, grid, block, 0, st, a)             \
-              : launch_pdl(norm_rows_kernel<T, TPR, ITEMS, QUANT, NORM, false>, grid, block, 0, st, a);           \
+    if (lay == kAligned) return launch_rows_kernel<T, TPR, ITEMS, QUANT, NORM, kAligned>(a, st);                  \
+    if constexpr (!QUANT)                                                                                         \
+      if (lay == kShifted) return launch_rows_kernel<T, TPR, ITEMS, QUANT, NORM, kShifted>(a, st);                \
+    return launch_rows_kernel<T, TPR, ITEMS, QUANT, NORM, kScalar>(a, st);                                        \
   }
   if (groups <= 32) DTST_ROWS(32, 1)
   if (groups <= 64) DTST_ROWS(32, 2)
   if (groups <= 128) DTST_ROWS(128, 1)
-  if (groups <= 256) DTST_ROWS(256, 1)
+  if (groups <= 256) DTST_ROWS(128, 2)
   if (groups <= 512) DTST_ROWS(256, 2)
   if (groups <= 1024) DTST_ROWS(512, 2)
   if (groups <= 2048) DTST_ROWS(512, 4)
 #undef DTST_ROWS
-  const dim3 grid((unsigned)(a.rows < most ? a.rows : most));
-  return launch_pdl(norm_long_rows_kernel<T, QUANT, NORM>, grid, dim3(512), 0, st, a);
+  const long long most = (long long)num_sms() * 32;
+  return launch_pdl(norm_long_rows_kernel<T, QUANT, NORM>, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(512), 0, st, a);
 }
 
 // ---- backward, rows
@@ -269,12 +319,12 @@ struct RowBackArgs {
   long long rows, C;
 };
 
-template <typename T, int TPR, int ITEMS, bool ALIGNED>
+template <typename T, int TPR, int ITEMS, int LAY>
 __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_backward_kernel(const RowBackArgs a) {
   constexpr int VEC = kVec<T>;
   constexpr int RPC = kRowThreads<TPR> / TPR;
   __shared__ float red[64];
-  extern __shared__ float gw_s[];   // RPC > 1: [RPC][ITEMS * TPR * VEC]
+  extern __shared__ float gw_s[];   // RPC > 1: [RPC][C]
   pdl_trigger();
   pdl_wait();
   const int tr = threadIdx.x % TPR;
@@ -282,62 +332,79 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_backward_kernel(co
   const T* gy = static_cast<const T*>(a.gy);
   const T* s = static_cast<const T*>(a.s);
   const T* gs = static_cast<const T*>(a.gs);
+  const long long group = (long long)blockIdx.x * RPC + threadIdx.x / TPR, step = (long long)gridDim.x * RPC;
+  const int shift = LAY == kShifted ? (int)(group * a.C % VEC) : 0;
+  Pack<T, VEC> pg[ITEMS], ps[ITEMS], pr[ITEMS];
+  float rstd_next = 0.f;
+  auto fetch = [&](long long row) {
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const long long c = (long long)(tr + k * TPR) * VEC - shift;
+      load_group<T, LAY>(pg[k], gy + row * a.C, c, a.C);
+      load_group<T, LAY>(ps[k], s + row * a.C, c, a.C);
+      if (gs != nullptr) load_group<T, LAY>(pr[k], gs + row * a.C, c, a.C);
+    }
+    rstd_next = __ldg(a.rstd + row);
+  };
+  if (group < a.rows) fetch(group);
   float gw[ITEMS][VEC], w[ITEMS][VEC];
 #pragma unroll
-  for (int k = 0; k < ITEMS; ++k)
+  for (int k = 0; k < ITEMS; ++k) {
+    load_weights<VEC>(w[k], a.weight, (long long)(tr + k * TPR) * VEC - shift, a.C, false);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      const long long c = (long long)(tr + k * TPR) * VEC + i;
-      gw[k][i] = 0.f;
-      w[k][i] = c < a.C ? __ldg(a.weight + c) : 0.f;
-    }
+    for (int i = 0; i < VEC; ++i) gw[k][i] = 0.f;
+  }
   int phase = 0;
-  for (long long row = (long long)blockIdx.x * RPC + threadIdx.x / TPR; row < a.rows; row += (long long)gridDim.x * RPC) {
-    Pack<T, VEC> pg[ITEMS], ps[ITEMS], pr[ITEMS];
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-      const long long c = (long long)(tr + k * TPR) * VEC;
-      load_group<T, ALIGNED>(pg[k], gy + row * a.C, c, a.C);
-      load_group<T, ALIGNED>(ps[k], s + row * a.C, c, a.C);
-      if (gs != nullptr) load_group<T, ALIGNED>(pr[k], gs + row * a.C, c, a.C);
-    }
-    const float rstd = __ldg(a.rstd + row);
+  for (long long row = group; row < a.rows; row += step) {
+    const float rstd = rstd_next;
+    float g[ITEMS][VEC], n[ITEMS][VEC];
+    Pack<T, VEC> pq[ITEMS];
     float dot = 0.f;
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k)
+    for (int k = 0; k < ITEMS; ++k) {
+      pg[k].unpack(g[k]);
+      ps[k].unpack(n[k]);
+      if (gs != nullptr) pq[k] = pr[k];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const float g = pg[k].get(i), n = ps[k].get(i) * rstd;
-        gw[k][i] = fmaf(g, n, gw[k][i]);
-        dot = fmaf(w[k][i] * g, n, dot);
+        n[k][i] *= rstd;
+        gw[k][i] = fmaf(g[k][i], n[k][i], gw[k][i]);
+        g[k][i] *= w[k][i];
+        dot = fmaf(g[k][i], n[k][i], dot);
       }
-    dot = row_sum<TPR>(dot, red, phase) * inv_c;
+    }
+    if (row + step < a.rows) fetch(row + step);
+    dot = row_sum<TPR, RPC>(dot, red, phase) * inv_c;
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
+      float q[VEC];
+      if (gs != nullptr) pq[k].unpack(q);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const float n = ps[k].get(i) * rstd;
-        float g = rstd * fmaf(-n, dot, w[k][i] * pg[k].get(i));
-        if (gs != nullptr) g += pr[k].get(i);
-        ps[k].put(i, g);
+        g[k][i] = rstd * fmaf(-n[k][i], dot, g[k][i]);
+        if (gs != nullptr) g[k][i] += q[i];
       }
-      store_group<T, ALIGNED>(ps[k], static_cast<T*>(a.gx) + row * a.C, (long long)(tr + k * TPR) * VEC, a.C);
+      Pack<T, VEC> out;
+      out.pack(g[k]);
+      store_group<T, LAY>(out, static_cast<T*>(a.gx) + row * a.C, (long long)(tr + k * TPR) * VEC - shift, a.C);
     }
   }
   if (a.partial == nullptr) return;
   float* out = a.partial + (long long)blockIdx.x * a.C;
-  if constexpr (RPC > 1) {   // the CTA's rows meet in shared memory, in row order
-    constexpr int W = ITEMS * TPR * VEC;
+  if constexpr (RPC > 1) {   // the CTA's groups meet in shared memory, in order
     const int rw = threadIdx.x / TPR;
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) gw_s[rw * W + (tr + k * TPR) * VEC + i] = gw[k][i];
+      for (int i = 0; i < VEC; ++i) {
+        const int c = (tr + k * TPR) * VEC - shift + i;
+        if (c >= 0 && c < a.C) gw_s[rw * a.C + c] = gw[k][i];
+      }
     __syncthreads();
-    for (int c = threadIdx.x; c < W && c < a.C; c += blockDim.x) {
+    for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
       float t = 0.f;
 #pragma unroll
-      for (int r = 0; r < RPC; ++r) t += gw_s[r * W + c];
+      for (int r = 0; r < RPC; ++r) t += gw_s[r * a.C + c];
       out[c] = t;
     }
   } else {
@@ -345,8 +412,8 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_backward_kernel(co
     for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const long long c = (long long)(tr + k * TPR) * VEC + i;
-        if (c < a.C) out[c] = gw[k][i];
+        const long long c = (long long)(tr + k * TPR) * VEC - shift + i;
+        if (c >= 0 && c < a.C) out[c] = gw[k][i];
       }
   }
 }
@@ -476,11 +543,12 @@ __global__ void __launch_bounds__(256) norm_field_backward_kernel(const FieldArg
   const int lane = threadIdx.x, wy = threadIdx.y, ny = blockDim.y;
   const float inv_c = 1.0f / (float)a.C;
   const T* gs = static_cast<const T*>(a.gs);
-  float gw[NCH], w[NCH];
+  // the sums over a CTA's positions are compensated (Kahan): a thread adds thousands of tiles one by one
+  float gw[NCH], lost[NCH], w[NCH];
 #pragma unroll
   for (int k = 0; k < NCH; ++k) {
     const int c = wy + k * ny;
-    gw[k] = 0.f;
+    gw[k] = lost[k] = 0.f;
     w[k] = c < a.C ? __ldg(a.weight + c) : 0.f;
   }
   int phase = 0;
@@ -506,13 +574,18 @@ __global__ void __launch_bounds__(256) norm_field_backward_kernel(const FieldArg
       dot[i] = 0.f;
     }
 #pragma unroll
-    for (int k = 0; k < NCH; ++k)
+    for (int k = 0; k < NCH; ++k) {
+      float t = -lost[k];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         const float g = pg[k].get(i), n = ps[k].get(i) * rstd[i];
-        gw[k] = fmaf(g, n, gw[k]);
+        t = fmaf(g, n, t);
         dot[i] = fmaf(w[k] * g, n, dot[i]);
       }
+      const float sum = gw[k] + t;
+      lost[k] = (sum - gw[k]) - t;
+      gw[k] = sum;
+    }
 #pragma unroll
     for (int i = 0; i < VEC; ++i) red[phase][wy][lane * VEC + i] = dot[i];
     __syncthreads();
@@ -613,24 +686,24 @@ __global__ void __launch_bounds__(256) norm_wide_field_weight_kernel(const Field
   if (threadIdx.x == 0) a.partial[(long long)blockIdx.y * a.C + c] = t;
 }
 
-// grad_w[c] = sum over parts, in a fixed order: 8 warps take every eighth part, their sums meet in warp order.
-__global__ void __launch_bounds__(256) norm_weight_sum_kernel(const float* __restrict__ partial, float* __restrict__ gw,
-                                                             int parts, long long C) {
-  __shared__ float red[8][32];
+// grad_w[c] = sum over parts, in a fixed order: 32 warps take every 32nd part, their sums meet in warp order.
+__global__ void __launch_bounds__(1024) norm_weight_sum_kernel(const float* __restrict__ partial, float* __restrict__ gw,
+                                                              int parts, long long C) {
+  __shared__ float red[32][33];
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const long long c = (long long)blockIdx.x * 32 + lane;
   float t = 0.f;
-  if (c < C)
-    for (int p = w; p < parts; p += 8) t += partial[(long long)p * C + c];
+  if (c < C) {
+#pragma unroll 8
+    for (int p = w; p < parts; p += 32) t += partial[(long long)p * C + c];
+  }
   red[w][lane] = t;
   __syncthreads();
-  if (w == 0 && c < C) {
-#pragma unroll
-    for (int i = 1; i < 8; ++i) t += red[i][lane];
-    gw[c] = t;
-  }
+  t = red[lane][w];                    // (turned round: warp w sums column w over the 32 parts' lanes)
+  t = warp_sum(t);
+  if (lane == 0 && (long long)blockIdx.x * 32 + w < C) gw[(long long)blockIdx.x * 32 + w] = t;
 }
 
 template <typename T, bool BACK>
@@ -678,17 +751,18 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
 template <typename T>
 cudaError_t launch_rows_backward(const RowBackArgs& a, int* parts, cudaStream_t st) {
   constexpr int VEC = kVec<T>;
-  const long long groups = (a.C + VEC - 1) / VEC;
-  const bool al = a.C % VEC == 0 && aligned_to(a.gy, 16) && aligned_to(a.s, 16) && aligned_to(a.gs, 16) && aligned_to(a.gx, 16);
+  const RowLayout lay = row_layout<T>(a.C, a.C, {a.gy, a.s, a.gs, a.gx});
+  const long long groups = (a.C + (lay == kShifted ? VEC - 1 : 0) + VEC - 1) / VEC;
 #define DTST_ROWS(TPR, ITEMS)                                                                                     \
   {                                                                                                               \
     constexpr int RPC = kRowThreads<TPR> / TPR;                                                                   \
     const long long ctas = (a.rows + RPC - 1) / RPC;                                                              \
     *parts = (int)(ctas < kNormParts ? ctas : kNormParts);                                                        \
     const dim3 grid((unsigned)*parts), block(kRowThreads<TPR>);                                                   \
-    const size_t smem = RPC > 1 ? sizeof(float) * RPC * ITEMS * TPR * VEC : 0;                                    \
-    return al ? launch_pdl(norm_rows_backward_kernel<T, TPR, ITEMS, true>, grid, block, smem, st, a)              \
-              : launch_pdl(norm_rows_backward_kernel<T, TPR, ITEMS, false>, grid, block, smem, st, a);            \
+    const size_t smem = RPC > 1 ? sizeof(float) * RPC * a.C : 0;                                                  \
+    if (lay == kAligned) return launch_pdl(norm_rows_backward_kernel<T, TPR, ITEMS, kAligned>, grid, block, smem, st, a); \
+    if (lay == kShifted) return launch_pdl(norm_rows_backward_kernel<T, TPR, ITEMS, kShifted>, grid, block, smem, st, a); \
+    return launch_pdl(norm_rows_backward_kernel<T, TPR, ITEMS, kScalar>, grid, block, smem, st, a);               \
   }
   if (groups <= 32) DTST_ROWS(32, 1)
   if (groups <= 64) DTST_ROWS(32, 2)
@@ -732,7 +806,7 @@ cudaError_t backward_t(const NormBackCall& n, cudaStream_t st) {
     e = launch_field<T, true>(a, &parts, st);
   }
   if (e != cudaSuccess || partial == nullptr) return e;
-  return launch_pdl(norm_weight_sum_kernel, dim3((unsigned)((n.channels + 31) / 32)), dim3(256), 0, st,
+  return launch_pdl(norm_weight_sum_kernel, dim3((unsigned)((n.channels + 31) / 32)), dim3(1024), 0, st,
                     static_cast<const float*>(partial), n.grad_weight, parts, (long long)n.channels);
 }
 

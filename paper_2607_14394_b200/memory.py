@@ -64,17 +64,12 @@ def _use(stream):
 # the current stream of a device as a cudaStream_t; the first form costs a tenth of the second
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_device = torch.cuda.current_device
 
 
-def _call(fn, dev: int, *args) -> None:
-    """fn(*args, current stream) with `dev` current."""
-    if torch.cuda.current_device() == dev:
-        status = fn(*args, _raw_stream(dev))
-    else:
-        with torch.cuda.device(dev):
-            status = fn(*args, _raw_stream(dev))
-    if status != 0:
-        raise Bn.DtstError(status, fn.__name__)
+def _check(status: int, where: str) -> None:
+    if status != Bn.DTST_OK:
+        raise Bn.DtstError(status, where)
 
 
 def _rows16(k: int) -> int:
@@ -112,85 +107,107 @@ class RmsNorm:
         self._type = DTYPES[dtype]
         self._rest = self.shape[:self.dim] + self.shape[self.dim + 1:]
         self._wshape = torch.Size((self.channels,))
+        self._q_like_x = self.channels % 16 == 0 and nd == 2
         self._scale_shape = torch.Size((-(-self.channels // BLOCK), self.outer))
         self._scratch = None
         self._lib = Bn.lib()
 
     def forward(self, x, weight, residual=None, out=None, sum_out=None, rstd=None, stream=None):
         """Returns (y, s, rstd); without a residual s is x itself."""
-        if stream is not None:
-            with _use(stream):
-                return self.forward(x, weight, residual, out, sum_out, rstd)
         d, t, sh = self.dev, self.dtype, self.shape
+        if stream is not None or _current_device() != d:
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
+                return self.forward(x, weight, residual, out, sum_out, rstd)
         xp, wp = _addr(x, "x", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
-        rp = 0
+        rp = sp = 0
+        if sum_out is not None:
+            sp = _addr(sum_out, "sum_out", d, t, sh)
         if residual is not None:
             rp = _addr(residual, "residual", d, t, sh)
             if sum_out is None:
                 sum_out = torch.empty_like(x)
+                sp = sum_out.data_ptr()
         if out is None:
             out = torch.empty_like(x)
+            yp = out.data_ptr()
+        else:
+            yp = _addr(out, "out", d, t, sh)
         if rstd is None:
             rstd = weight.new_empty(self._rest)
-        _call(self._lib.dtst_rms_norm, d, self._type, self.outer, self.channels, self.inner, self.eps, xp, rp, wp,
-              _addr(sum_out, "sum_out", d, t, sh), _addr(out, "out", d, t, sh),
-              _addr(rstd, "rstd", d, torch.float32, self._rest))
+            qp = rstd.data_ptr()
+        else:
+            qp = _addr(rstd, "rstd", d, torch.float32, self._rest)
+        status = self._lib.dtst_rms_norm(self._type, self.outer, self.channels, self.inner, self.eps, xp, rp, wp, sp, yp, qp,
+                                         _raw_stream(d))
+        if status:
+            _check(status, "dtst_rms_norm")
         return out, (x if sum_out is None else sum_out), rstd
 
     def forward_fp8(self, x, weight, residual=None, q=None, scale=None, sum_out=None, stream=None):
         """Returns (q, scale, s): the norm of token-major rows in 8 bits, [rows, channels], and its scales
         [ceil(channels / 128), rows] - what Fp8Linear takes."""
-        if stream is not None:
-            with _use(stream):
+        rows, c, d, t, sh = self.outer, self.channels, self.dev, self.dtype, self.shape
+        if stream is not None or _current_device() != d:
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
                 return self.forward_fp8(x, weight, residual, q, scale, sum_out)
         if self.inner != 1:
             raise ValueError("an 8-bit output needs the channels in the last dimension")
-        rows, c, d, t, sh = self.outer, self.channels, self.dev, self.dtype, self.shape
         xp, wp = _addr(x, "x", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
-        rp = 0
+        rp = sp = 0
+        if sum_out is not None:
+            sp = _addr(sum_out, "sum_out", d, t, sh)
         if residual is not None:
             rp = _addr(residual, "residual", d, t, sh)
             if sum_out is None:
                 sum_out = torch.empty_like(x)
+                sp = sum_out.data_ptr()
         if q is not None:
             ld, qp = _q_stride(q, rows, c), _on_device(q, "q", d, FP8)
         else:
-            if c % 16 == 0 and len(sh) == 2:
-                q = torch.empty_like(x, dtype=FP8)
-            else:
-                q = empty_fp8(rows, c, self.device)
+            q = torch.empty_like(x, dtype=FP8) if self._q_like_x else empty_fp8(rows, c, self.device)
             ld, qp = _rows16(c), q.data_ptr()
         if scale is None:
             scale = weight.new_empty(self._scale_shape)
-        _call(self._lib.dtst_rms_norm_fp8, d, self._type, rows, c, self.eps, xp, rp, wp,
-              _addr(sum_out, "sum_out", d, t, sh), qp, ld, _addr(scale, "scale", d, torch.float32, self._scale_shape))
+            scp = scale.data_ptr()
+        else:
+            scp = _addr(scale, "scale", d, torch.float32, self._scale_shape)
+        status = self._lib.dtst_rms_norm_fp8(self._type, rows, c, self.eps, xp, rp, wp, sp, qp, ld, scp, _raw_stream(d))
+        if status:
+            _check(status, "dtst_rms_norm_fp8")
         return q, scale, (x if sum_out is None else sum_out)
 
     def backward(self, grad_y, s, weight, rstd, grad_s=None, grad_x=None, grad_weight=None, need_grad_weight=True,
                  stream=None):
         """Returns (grad_x, grad_weight); grad_x is the gradient of x and of the residual."""
-        if stream is not None:
-            with _use(stream):
-                return self.backward(grad_y, s, weight, rstd, grad_s, grad_x, grad_weight, need_grad_weight)
         d, t, sh = self.dev, self.dtype, self.shape
+        if stream is not None or _current_device() != d:
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
+                return self.backward(grad_y, s, weight, rstd, grad_s, grad_x, grad_weight, need_grad_weight)
         gp, wp = _addr(grad_y, "grad_y", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
         if grad_x is None:
             grad_x = torch.empty_like(grad_y)
-        scratch = nbytes = 0
+            xp = grad_x.data_ptr()
+        else:
+            xp = _addr(grad_x, "grad_x", d, t, sh)
+        scratch = nbytes = gwp = 0
         if need_grad_weight:
             if grad_weight is None:
                 grad_weight = torch.empty_like(weight)
+                gwp = grad_weight.data_ptr()
+            else:
+                gwp = _addr(grad_weight, "grad_weight", d, torch.float32, self._wshape)
             if self._scratch is None:
                 n = ctypes.c_size_t()
-                Bn._check(self._lib.dtst_rms_norm_scratch_bytes(self.channels, ctypes.byref(n)),
-                          "dtst_rms_norm_scratch_bytes")
+                _check(self._lib.dtst_rms_norm_scratch_bytes(self.channels, ctypes.byref(n)), "dtst_rms_norm_scratch_bytes")
                 self._scratch = torch.empty(n.value, dtype=torch.uint8, device=self.device)
                 self._scratch_at = (self._scratch.data_ptr(), int(n.value))
             scratch, nbytes = self._scratch_at
-        _call(self._lib.dtst_rms_norm_backward, d, self._type, self.outer, self.channels, self.inner, gp,
-              _addr(s, "s", d, t, sh), wp, _addr(rstd, "rstd", d, torch.float32, self._rest),
-              _addr(grad_s, "grad_s", d, t, sh), _addr(grad_x, "grad_x", d, t, sh),
-              _addr(grad_weight, "grad_weight", d, torch.float32, self._wshape), scratch, nbytes)
+        status = self._lib.dtst_rms_norm_backward(
+            self._type, self.outer, self.channels, self.inner, gp, _addr(s, "s", d, t, sh), wp,
+            _addr(rstd, "rstd", d, torch.float32, self._rest), 0 if grad_s is None else _addr(grad_s, "grad_s", d, t, sh),
+            xp, gwp, scratch, nbytes, _raw_stream(d))
+        if status:
+            _check(status, "dtst_rms_norm_backward")
         return grad_x, grad_weight
 
 
@@ -204,34 +221,37 @@ def _q_stride(q: torch.Tensor, rows: int, k: int) -> int:
 
 def quantize_fp8(x: torch.Tensor, q=None, scale=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rows x [rows, k] (contiguous along k) -> (q [rows, k] in 8 bits, scale [ceil(k / 128), rows])."""
-    if stream is not None:
-        with _use(stream):
-            return quantize_fp8(x, q, scale)
     if x.dim() != 2 or x.dtype not in DTYPES or not x.is_cuda or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError("quantize_fp8 takes CUDA rows [rows, k] of float32, bfloat16 or float16, contiguous along k")
     rows, k = x.shape
     dev, shape = x.get_device(), (-(-k // BLOCK), rows)
+    if stream is not None or _current_device() != dev:
+        with torch.cuda.device(dev), _use(torch.cuda.current_stream(dev) if stream is None else stream):
+            return quantize_fp8(x, q, scale)
     if q is None:
         q = empty_fp8(rows, k, x.device)
     if scale is None:
         scale = x.new_empty(shape, dtype=torch.float32)
-    _call(Bn.lib().dtst_quantize_fp8, dev, DTYPES[x.dtype], rows, k, x.data_ptr(), x.stride(0),
-          _on_device(q, "q", dev, FP8), _q_stride(q, rows, k), _addr(scale, "scale", dev, torch.float32, shape))
+    _check(Bn.lib().dtst_quantize_fp8(DTYPES[x.dtype], rows, k, x.data_ptr(), x.stride(0), _on_device(q, "q", dev, FP8),
+                                      _q_stride(q, rows, k), _addr(scale, "scale", dev, torch.float32, shape),
+                                      _raw_stream(dev)), "dtst_quantize_fp8")
     return q, scale
 
 
 def quantize_fp8_weight(w: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """w [n, k] -> (8-bit values [n, k], scale [ceil(n / 128), ceil(k / 128)]), one scale per 128 x 128 block."""
-    if stream is not None:
-        with _use(stream):
-            return quantize_fp8_weight(w)
     if w.dim() != 2 or w.dtype not in DTYPES or not w.is_cuda or (w.shape[1] > 1 and w.stride(1) != 1):
         raise ValueError("quantize_fp8_weight takes CUDA w [n, k] of float32, bfloat16 or float16, contiguous along k")
     n, k = w.shape
+    dev = w.get_device()
+    if stream is not None or _current_device() != dev:
+        with torch.cuda.device(dev), _use(torch.cuda.current_stream(dev) if stream is None else stream):
+            return quantize_fp8_weight(w)
     q = empty_fp8(n, k, w.device)
     scale = w.new_empty((-(-n // BLOCK), -(-k // BLOCK)), dtype=torch.float32)
-    _call(Bn.lib().dtst_quantize_fp8_weight, w.get_device(), DTYPES[w.dtype], n, k, w.data_ptr(), max(w.stride(0), k),
-          q.data_ptr(), _q_stride(q, n, k), scale.data_ptr())
+    _check(Bn.lib().dtst_quantize_fp8_weight(DTYPES[w.dtype], n, k, w.data_ptr(), max(w.stride(0), k), q.data_ptr(),
+                                             _q_stride(q, n, k), scale.data_ptr(), _raw_stream(dev)),
+           "dtst_quantize_fp8_weight")
     return q, scale
 
 
@@ -266,11 +286,13 @@ class Fp8Linear:
         return cls(*quantize_fp8_weight(w), out_dtype=out_dtype)
 
     def forward(self, x: torch.Tensor, x_scale: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None):
-        if stream is not None:
-            with _use(stream):
+        d, k = self.dev, self.k
+        if stream is not None or _current_device() != d:
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
                 return self.forward(x, x_scale, out)
-        m, d = x.shape[0], self.dev
-        xp, ld = _on_device(x, "x", d, FP8), _q_stride(x, m, self.k)
+        m = x.shape[0]
+        xp, ld = _on_device(x, "x", d, FP8), _q_stride(x, m, k)
+        sp = _addr(x_scale, "x_scale", d, torch.float32, (self._kb, m))
         if out is None:
             out = x_scale.new_empty((m, self.n), dtype=self.out_dtype)
             op, out_ld = out.data_ptr(), self.n
@@ -278,9 +300,10 @@ class Fp8Linear:
             if out.shape != (m, self.n) or (self.n > 1 and out.stride(1) != 1):
                 raise ValueError(f"out must have shape {(m, self.n)} and contiguous rows")
             op, out_ld = _on_device(out, "out", d, self.out_dtype), max(out.stride(0), self.n)
-        _call(self._lib.dtst_matmul_fp8, d, self._type, m, self.n, self.k, xp, ld,
-              _addr(x_scale, "x_scale", d, torch.float32, (self._kb, m)), self._w, self._ld, self._ws, op, out_ld,
-              self._work, 256)
+        status = self._lib.dtst_matmul_fp8(self._type, m, self.n, k, xp, ld, sp, self._w, self._ld, self._ws, op, out_ld,
+                                           self._work, 256, _raw_stream(d))
+        if status:
+            _check(status, "dtst_matmul_fp8")
         return out
 
     __call__ = forward
@@ -323,7 +346,7 @@ class GatedScan:
         self._ref = ctypes.byref(self._desc)
         self._lib = Bn.lib()
         n = ctypes.c_int64()
-        Bn._check(self._lib.dtst_gated_scan_checkpoints(self._ref, ctypes.byref(n)), "dtst_gated_scan_checkpoints")
+        _check(self._lib.dtst_gated_scan_checkpoints(self._ref, ctypes.byref(n)), "dtst_gated_scan_checkpoints")
         self.checkpoint_floats = int(n.value)
         self._ck_shape = torch.Size((self.checkpoint_floats,))
 
@@ -373,17 +396,14 @@ class GatedScan:
             self._desc.in_stride[0], self._desc.in_stride[1] = self._in = at
         return v.data_ptr(), g.data_ptr()
 
-    def _lengths(self, lengths) -> int:
-        return 0 if lengths is None else _addr(lengths, "lengths", self.dev, torch.int32, self.outer_shape)
-
     def forward(self, v, g, h0=None, lengths=None, out=None, h_last=None, checkpoints=None, stream=None):
         """Returns (h, h_last).  lengths: int32 per outer entry; checkpoints: see new_checkpoints."""
-        if stream is not None:
-            with _use(stream):
-                return self.forward(v, g, h0, lengths, out, h_last, checkpoints)
         d, state = self.dev, self.state_shape
+        if stream is not None or _current_device() != d:
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
+                return self.forward(v, g, h0, lengths, out, h_last, checkpoints)
         vp, gp = self._inputs(v, g)
-        hp = _addr(h0, "h0", d, torch.float32, state)
+        hp = 0 if h0 is None else _addr(h0, "h0", d, torch.float32, state)
         if out is None:
             out = torch.empty_like(v) if self._in is self._dense else v.new_empty(self.shape)
             op = out.data_ptr()
@@ -394,18 +414,22 @@ class GatedScan:
             lp = h_last.data_ptr()
         else:
             lp = _addr(h_last, "h_last", d, torch.float32, state)
-        _call(self._lib.dtst_gated_scan, d, self._ref, vp, gp, hp, self._lengths(lengths), op, lp,
-              _addr(checkpoints, "checkpoints", d, torch.float32, self._ck_shape))
+        status = self._lib.dtst_gated_scan(
+            self._ref, vp, gp, hp, 0 if lengths is None else _addr(lengths, "lengths", d, torch.int32, self.outer_shape), op,
+            lp, 0 if checkpoints is None else _addr(checkpoints, "checkpoints", d, torch.float32, self._ck_shape),
+            _raw_stream(d))
+        if status:
+            _check(status, "dtst_gated_scan")
         return out, h_last
 
     def backward(self, grad_h, v, g, checkpoints, h0=None, lengths=None, grad_last=None, grad_v=None, grad_g=None,
                  grad_h0=None, need_grad_h0=True, stream=None):
         """Returns (grad_v, grad_g, grad_h0); v, g, h0, lengths and checkpoints as in the forward call."""
-        if stream is not None:
-            with _use(stream):
+        d, t, state = self.dev, self.dtype, self.state_shape
+        if stream is not None or _current_device() != d:
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
                 return self.backward(grad_h, v, g, checkpoints, h0, lengths, grad_last, grad_v, grad_g, grad_h0,
                                      need_grad_h0)
-        d, t, state = self.dev, self.dtype, self.state_shape
         vp, gp = self._inputs(v, g)
         dp = _addr(grad_h, "grad_h", d, t, self.shape)
         if grad_v is None and grad_g is None:
@@ -421,11 +445,16 @@ class GatedScan:
         if at != self._out:
             self._desc.grad_stride[0], self._desc.grad_stride[1] = self._out = at
         if grad_h0 is None and need_grad_h0:
-            grad_h0 = torch.empty(state, dtype=torch.float32, device=self.device)
-        _call(self._lib.dtst_gated_scan_backward, d, self._ref, dp, _addr(grad_last, "grad_last", d, torch.float32, state),
-              vp, gp, _addr(h0, "h0", d, torch.float32, state), self._lengths(lengths),
-              _addr(checkpoints, "checkpoints", d, torch.float32, self._ck_shape), grad_v.data_ptr(), grad_g.data_ptr(),
-              _addr(grad_h0, "grad_h0", d, torch.float32, state))
+            grad_h0 = (torch.empty(state, dtype=torch.float32, device=self.device) if grad_last is None and h0 is None
+                       else torch.empty_like(grad_last if h0 is None else h0))
+        status = self._lib.dtst_gated_scan_backward(
+            self._ref, dp, 0 if grad_last is None else _addr(grad_last, "grad_last", d, torch.float32, state), vp, gp,
+            0 if h0 is None else _addr(h0, "h0", d, torch.float32, state),
+            0 if lengths is None else _addr(lengths, "lengths", d, torch.int32, self.outer_shape),
+            _addr(checkpoints, "checkpoints", d, torch.float32, self._ck_shape), grad_v.data_ptr(), grad_g.data_ptr(),
+            _addr(grad_h0, "grad_h0", d, torch.float32, state), _raw_stream(d))
+        if status:
+            _check(status, "dtst_gated_scan_backward")
         return grad_v, grad_g, grad_h0
 
 

@@ -566,6 +566,10 @@ dtst_status dtst_gated_scan_backward(const dtst_scan_desc* desc, const void* gra
                                      const float* checkpoints, void* grad_v, void* grad_g, float* grad_h0,
                                      void* stream);
 
+/* Synchronises `stream` and reports whether a bounded wait inside a recurrence kernel has given up on the current device
+ * since the last query (DTST_ERR_DEVICE_TIMEOUT: that pass's output is undefined), else DTST_OK. */
+dtst_status dtst_gated_scan_status(void* stream);
+
 /* Synchronises `stream` and reports the status word at the head of a workspace of dtst_matmul_fp8: DTST_OK, or
  * DTST_ERR_DEVICE_TIMEOUT if a bounded wait inside a kernel gave up (its output is undefined then).  Clears the word. */
 dtst_status dtst_workspace_status(void* workspace, void* stream);

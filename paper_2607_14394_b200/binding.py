@@ -46,7 +46,7 @@ EXPORTED = [
     "dtst_host_io_wait", "dtst_plan_set_column_contraction", "dtst_plan_set_arithmetic",
     "dtst_rms_norm", "dtst_rms_norm_scratch_bytes", "dtst_rms_norm_backward", "dtst_rms_norm_fp8", "dtst_quantize_fp8",
     "dtst_quantize_fp8_weight", "dtst_matmul_fp8", "dtst_gated_scan_checkpoints", "dtst_gated_scan",
-    "dtst_gated_scan_backward", "dtst_workspace_status",
+    "dtst_gated_scan_backward", "dtst_gated_scan_status", "dtst_workspace_status",
 ]
 
 
@@ -136,6 +136,7 @@ def lib() -> ctypes.CDLL:
     L.dtst_gated_scan_checkpoints.argtypes = [descp, i64p]
     L.dtst_gated_scan.argtypes = [descp] + [vp] * 8
     L.dtst_gated_scan_backward.argtypes = [descp] + [vp] * 11
+    L.dtst_gated_scan_status.argtypes = [vp]
     L.dtst_workspace_status.argtypes = [vp, vp]
     L.dtst_status_string.argtypes = [i32]
     L.dtst_status_string.restype = ctypes.c_char_p

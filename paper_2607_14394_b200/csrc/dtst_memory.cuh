@@ -58,6 +58,7 @@ struct ScanCall {
 };
 // steps between saved states for this problem (the whole length where nothing is saved)
 long long scan_chunk(int dtype, long long length, long long inner);
+cudaError_t scan_status(int* word, cudaStream_t st);      // reads and clears
 cudaError_t launch_scan_forward(const ScanCall& c, cudaStream_t st);
 cudaError_t launch_scan_backward(const ScanCall& c, cudaStream_t st);
 

@@ -208,6 +208,12 @@ dtst_status dtst_gated_scan_backward(const dtst_scan_desc* d, const void* grad_h
   return done(launch_scan_backward(c, static_cast<cudaStream_t>(stream)));
 }
 
+dtst_status dtst_gated_scan_status(void* stream) {
+  int word = 0;
+  const dtst_status s = done(scan_status(&word, static_cast<cudaStream_t>(stream)));
+  return s != DTST_OK ? s : word == 0 ? DTST_OK : DTST_ERR_DEVICE_TIMEOUT;
+}
+
 dtst_status dtst_workspace_status(void* workspace, void* stream) {
   if (!workspace_ok(workspace)) return DTST_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);

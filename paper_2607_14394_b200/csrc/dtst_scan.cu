@@ -12,6 +12,7 @@
 // h_{t-1} inside each chunk, in fp32, from the state saved at the chunk's start.
 #include "dtst_common.cuh"
 #include "dtst_memory.cuh"
+#include "dtst_sm100.cuh"
 #include "dtst_types.cuh"
 
 namespace dtst {
@@ -191,22 +192,62 @@ __device__ __forceinline__ ColGroup col_group(const ScanArgs<T>& p, unsigned til
   return g;
 }
 
-// What the chunks of a round leave behind: `all` = this CTA's chunk, `state` = in front of the round (then: behind it).
-// Returns the state in front of this CTA's chunk.  A lane of depth group d reads the d-th CTA's summary.
+// the tile's rows from `dst` on, as far as there are any, become zero
+template <typename T, class S>
+__device__ __forceinline__ void zero_rows(T* dst, long long stride, int left, int slot) {
+  Pack<T, S::VEC> z;
+  z.zero();
+  dst += (long long)slot * S::R * stride;
+#pragma unroll
+  for (int r = 0; r < S::R; ++r, dst += stride)
+    if (slot * S::R + r < left) z.store(dst);
+}
+
+// set if a wait for another CTA's summaries ever runs out (dtst_gated_scan_status)
+__device__ int scan_status_word;
+constexpr uint32_t kRoundPolls = 1u << 20;
+
+// Where the CTAs of a cluster leave their chunks' summaries for each other: a box for every CTA, two sets used in turn (a CTA
+// sends its next round's only when it has everybody's of this one, so the set of the round before is free again).
 template <class S>
-__device__ __forceinline__ float join_round(const float2 all, float& state, float2 (*box)[S::W], int round, int size, int rank, int jx) {
+struct RoundBoxes {
+  float2 box[2][8][S::W];
+  uint64_t bar[2];
+};
+
+// One round: every CTA sends its chunk's summary `all` to the others (st.async: the bytes are counted by the receiver's
+// mbarrier, so nothing has to be fenced - a cluster barrier's release waits for all global stores of the round before, which
+// measured 36 of 136 us in a pass over 65536 x 1024).  Returns the state in front of this CTA's chunk and moves `state` past
+// the round.  A lane of depth group d sends to and reads the box of CTA d.
+template <class S>
+__device__ __forceinline__ float join_round(const float2 all, float& state, RoundBoxes<S>& b, int round, int size, int rank, int jx,
+                                            bool& dead) {
   static_assert(S::DG >= 8, "a depth group per CTA of the largest cluster");
   if (size == 1) {
     const float start = state;
     state = fmaf(all.x, state, all.y);
     return start;
   }
-  const int lane = threadIdx.x & 31, d = lane / S::CPW, ch = lane % S::CPW;
-  float2* mine = box[round & 1];          // (two boxes: a CTA may be a round ahead of a reader)
-  if (d == 0) mine[jx] = all;
-  cluster_sync();
+  const int lane = threadIdx.x & 31, d = lane / S::CPW, ch = lane % S::CPW, set = round & 1;
+  if (threadIdx.x == 0) sm100::mbar_arrive_expect_tx(&b.bar[set], (uint32_t)(size - 1) * S::W * 8u);
+  if (d < size && d != rank) {
+    uint32_t to, bar;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(sm100::smem_u32(&b.box[set][rank][jx])), "r"(d));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(sm100::smem_u32(&b.bar[set])), "r"(d));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to), "f"(all.x),
+                 "f"(all.y), "r"(bar)
+                 : "memory");
+  }
+  bool here = dead;
+  for (uint32_t poll = 0; poll < kRoundPolls && !here; ++poll) here = sm100::mbar_try_wait(&b.bar[set], (uint32_t)(round >> 1) & 1u);
+  if (!here) {
+    dead = true;             // the results are undefined; later rounds do not wait again
+    atomicExch(&scan_status_word, 1);
+  }
+  __syncwarp();
   float2 m = make_float2(1.f, 0.f);
-  if (d < size) m = cluster_read(mine + jx, d);
+  if (d == rank) m = all;
+  else if (d < size) m = b.box[set][d][jx];
   float start = 0.f;
   for (int k = 0; k < size; ++k) {
     if (k == rank) start = state;
@@ -220,13 +261,22 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_kernel(const ScanArgs
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
   using Slots = ColSlots<T, S, 2, WIDE>;
   __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];     // (A, H) of every run; then its first state in x
-  __shared__ float2 box[2][SLOTS > 1 ? W : 1];
+  __shared__ RoundBoxes<S> boxes;
+  bool dead = false;
   extern __shared__ __align__(16) unsigned char raw[];
   Slots slots{raw};
   pdl_trigger();
   pdl_wait();
   const int size = MODE == kLong ? cluster_size() : 1, rank = MODE == kLong ? cluster_rank() : 0;
   const unsigned tile = blockIdx.x / size;
+  if (size > 1) {
+    if (threadIdx.x == 0) {
+      sm100::mbar_init(&boxes.bar[0], 1);
+      sm100::mbar_init(&boxes.bar[1], 1);
+      sm100::fence_barrier_init();
+    }
+    cluster_sync();
+  }
   const int slot = threadIdx.x / S::TX, x = threadIdx.x % S::TX;
   const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
   const long long states = p.outer * p.inner;
@@ -265,16 +315,28 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_kernel(const ScanArgs
 #pragma unroll 1
   for (int round = 0; round < p.rounds; ++round) {
     const int c = round * size + rank;
-    float a[R][VEC], u[R][VEC], s[VEC];
-    if (!WIDE) Slots::wait();
-    Pack<T, VEC> pv[R], pg[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) pv[r] = *slots.slot(0, r), pg[r] = *slots.slot(1, r);
     auto refill = [&]() {      // the values of a later chunk are on their way from here on
       if (round + Slots::kStages < p.rounds) fetch(c + Slots::kStages * size);
       Slots::commit();
       slots.advance();
     };
+    if constexpr (MODE == kLong) if (c * LC >= e_tile) {       // no step of the sequence here: the state passes, h is zero
+      float start = state;
+      start = join_round<S>(make_float2(1.f, 0.f), state, boxes, round, size, rank, jx, dead);
+      if (c == 0 && first && jg.live && p.h_last != nullptr) p.h_last[ch] = start;
+      zero_rows<T, S>(p.h + (at.o * p.L + c * LC) * p.inner + at.i0, p.inner, at.live ? (int)p.L - c * LC : 0, slot);
+      refill();
+      if (WIDE) {
+        Slots::wait();
+        __syncthreads();
+      }
+      continue;
+    }
+    float a[R][VEC], u[R][VEC], s[VEC];
+    if (!WIDE) Slots::wait();
+    Pack<T, VEC> pv[R], pg[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) pv[r] = *slots.slot(0, r), pg[r] = *slots.slot(1, r);
     if (!WIDE && MODE == kLong) refill();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -313,7 +375,7 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_kernel(const ScanArgs
       }
       const float2 all = join_lanes<S::CPW, true>(A, H);
       float start = state;
-      if constexpr (MODE == kLong) start = join_round<S>(all, state, box, round, size, rank, jx);
+      if constexpr (MODE == kLong) start = join_round<S>(all, state, boxes, round, size, rank, jx, dead);
       else state = fmaf(all.x, state, all.y);
       float run = fmaf(A, start, H);
       // (a chunk in which a sequence has no step leaves its state alone)
@@ -352,7 +414,6 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_kernel(const ScanArgs
     if (WIDE) Slots::wait();
     __syncthreads();       // the runs' states are read before the next chunk's summaries replace them, the next tile is here
   }
-  if (size > 1) cluster_sync();       // nobody leaves while its box may be read
 }
 
 template <typename T, class S, int MODE, bool WIDE>
@@ -362,13 +423,22 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const
   // (A, H) and D of every run; then the state in front of it (x) and the gradient that comes to it from behind
   __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
   __shared__ float backs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
-  __shared__ float2 box[2][SLOTS > 1 ? W : 1];
+  __shared__ RoundBoxes<S> boxes;
+  bool dead = false;
   extern __shared__ __align__(16) unsigned char raw[];
   Slots slots{raw};
   pdl_trigger();
   pdl_wait();
   const int size = MODE == kLong ? cluster_size() : 1, rank = MODE == kLong ? cluster_rank() : 0;
   const unsigned tile = blockIdx.x / size;
+  if (size > 1) {
+    if (threadIdx.x == 0) {
+      sm100::mbar_init(&boxes.bar[0], 1);
+      sm100::mbar_init(&boxes.bar[1], 1);
+      sm100::fence_barrier_init();
+    }
+    cluster_sync();
+  }
   const int slot = threadIdx.x / S::TX, x = threadIdx.x % S::TX;
   const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
   const long long states = p.outer * p.inner;
@@ -411,6 +481,29 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const
 #pragma unroll 1
   for (int round = 0; round < p.rounds; ++round) {
     const int c = p.chunks - 1 - (round * size + rank);
+    auto refill = [&]() {      // the values of a later chunk are on their way from here on
+      if (round + Slots::kStages < p.rounds) fetch(c - Slots::kStages * size);
+      Slots::commit();
+      slots.advance();
+    };
+    if constexpr (MODE == kLong) if (c < 0 || c * LC >= e_tile) {       // no step of the sequence here
+      const float behind = join_round<S>(make_float2(1.f, 0.f), grad, boxes, round, size, rank, jx, dead);
+      if (c == 0 && jg.live && first && p.gh0 != nullptr) p.gh0[ch] = behind;
+      if (c >= 0) {
+        const long long from = at.o * p.gr_o + at.i0 + (long long)c * LC * p.gr_t;
+        zero_rows<T, S>(p.gv + from, p.gr_t, at.live ? (int)p.L - c * LC : 0, slot);
+        zero_rows<T, S>(p.gg + from, p.gr_t, at.live ? (int)p.L - c * LC : 0, slot);
+      }
+      if (WIDE) {
+        refill();
+        Slots::wait();
+        __syncthreads();
+      } else {
+        Slots::wait();       // (the stage that would be read now holds nothing)
+        refill();
+      }
+      continue;
+    }
     float before = 0.f;      // the state in front of the chunk: saved, or the sequence's own beginning
     if (SLOTS > 1 && jg.live && c >= 0 && (c * LC < jg.end || c == 0)) {
       if (MODE == kLong && p.ckpt != nullptr) before = p.ckpt[c * states + ch];
@@ -426,11 +519,6 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const
     Pack<T, VEC> pv[R], pg[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) pv[r] = *slots.slot(0, r), pg[r] = *slots.slot(1, r), pd[r] = *slots.slot(2, r);
-    auto refill = [&]() {      // the values of a later chunk are on their way from here on
-      if (round + Slots::kStages < p.rounds) fetch(c - Slots::kStages * size);
-      Slots::commit();
-      slots.advance();
-    };
     if (!WIDE && MODE == kLong) refill();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -491,7 +579,7 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const
       join_lanes<S::CPW, true>(A, H);
       const float2 all = join_lanes<S::CPW, false>(B, E);
       float behind = grad;
-      if constexpr (MODE == kLong) behind = join_round<S>(all, grad, box, round, size, rank, jx);
+      if constexpr (MODE == kLong) behind = join_round<S>(all, grad, boxes, round, size, rank, jx, dead);
       if (c == 0 && jg.live && first && p.gh0 != nullptr) p.gh0[ch] = fmaf(all.x, behind, all.y);
       float run = fmaf(A, before, H);
 #pragma unroll
@@ -551,7 +639,6 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const
     if (WIDE) Slots::wait();
     __syncthreads();
   }
-  if (size > 1) cluster_sync();
 }
 
 // ------------------------------------------------------------------------------------------------ rows
@@ -934,12 +1021,16 @@ __global__ void __launch_bounds__(256) scan_copy_kernel(const float* __restrict_
     out[i] = in != nullptr ? in[i] : 0.f;
 }
 
-// CTAs of a cluster that shares a sequence: enough that all of them together fill the GPU twice, no more than there are
-// chunks, at most `most`.
-int cluster_for(long long tiles, long long chunks, int most) {
-  int n = 1;
-  while (n < most && n < chunks && tiles * n < 2 * (long long)num_sms()) n *= 2;
-  return n;
+// CTAs of a cluster that shares a sequence of `chunks` chunks: the size with the fewest rounds one after the other, over all
+// the waves in which `tiles` clusters run (`slots` CTAs at once); the smallest of equals.
+int cluster_for(long long tiles, long long chunks, long long slots, int most) {
+  int best = 1;
+  long long least = -1;
+  for (int n = 1; n <= most && (n == 1 || n < 2 * chunks); n *= 2) {
+    const long long rounds = (tiles * n + slots - 1) / slots * ((chunks + n - 1) / n);
+    if (least < 0 || rounds < least) best = n, least = rounds;
+  }
+  return best;
 }
 
 template <typename Kern, typename Args>
@@ -990,7 +1081,7 @@ cudaError_t launch_long_cols(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) 
   p.per_outer = (unsigned)per_outer;
   p.chains = p.outer * per_outer;
   p.chunks = (int)((p.L + S::LC - 1) / S::LC);
-  const int cluster = cluster_for(p.chains, p.chunks, 8);
+  const int cluster = cluster_for(p.chains, p.chunks, 2 * (long long)num_sms(), 8);
   p.rounds = (p.chunks + cluster - 1) / cluster;
   if constexpr (S::VEC > 1) {
     constexpr int E = 16 / (int)sizeof(T);
@@ -1039,7 +1130,7 @@ cudaError_t launch_rows(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
     p.rounds = p.chunks;
     return w ? launch_rows_kernel<T, true, kWalk, BACK>(p, p.outer, 1, st) : launch_rows_kernel<T, false, kWalk, BACK>(p, p.outer, 1, st);
   }
-  const int cluster = cluster_for(p.outer, (p.chunks + kRowWarps - 1) / kRowWarps, 32 / kRowWarps), team = cluster * kRowWarps;
+  const int cluster = cluster_for(p.outer, (p.chunks + kRowWarps - 1) / kRowWarps, 2 * (long long)num_sms(), 32 / kRowWarps), team = cluster * kRowWarps;
   p.rounds = (p.chunks + team - 1) / team;
   return w ? launch_rows_kernel<T, true, kTeam, BACK>(p, p.outer, cluster, st) : launch_rows_kernel<T, false, kTeam, BACK>(p, p.outer, cluster, st);
 }
@@ -1077,6 +1168,14 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
 long long scan_chunk(int, long long length, long long inner) {
   const long long lc = inner == 1 ? row_chunk(length) : kColTile;
   return length <= lc ? (length < 1 ? 1 : length) : lc;
+}
+
+cudaError_t scan_status(int* word, cudaStream_t st) {
+  const int none = 0;
+  cudaError_t e = cudaMemcpyFromSymbolAsync(word, scan_status_word, sizeof(int), 0, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e == cudaSuccess && *word != 0) e = cudaMemcpyToSymbolAsync(scan_status_word, &none, sizeof(int), 0, cudaMemcpyHostToDevice, st);
+  return e == cudaSuccess && *word != 0 ? cudaStreamSynchronize(st) : e;
 }
 
 cudaError_t launch_scan_forward(const ScanCall& c, cudaStream_t st) {

@@ -457,6 +457,12 @@ class GatedScan:
             _check(status, "dtst_gated_scan_backward")
         return grad_v, grad_g, grad_h0
 
+    def status(self, stream=None) -> int:
+        """DTST_OK, or DTST_ERR_DEVICE_TIMEOUT if a bounded wait of any recurrence gave up on this device since the last
+        query; synchronises."""
+        with torch.cuda.device(self.dev):
+            return int(self._lib.dtst_gated_scan_status(Bn._stream_ptr(stream)))
+
 
 class FieldMemory:
     """A trainable memory along the time axis of fields x [B, C, n..., T] (float32, T last), pre-normalised and residual:

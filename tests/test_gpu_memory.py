@@ -287,6 +287,7 @@ def test_scan_forward_and_backward(outer, L, inner, dtype, gate, ragged):
     again = plan.forward(v, g, h0, lengths=lengths)
     assert torch.equal(again[0], h) and torch.equal(again[1], last)
     assert all(torch.equal(a, b) for a, b in zip(plan.backward(gh, v, g, ck, h0, lengths=lengths, grad_last=gl), (gv, gg, g0)))
+    assert plan.status() == 0
 
 
 def test_scan_without_states():

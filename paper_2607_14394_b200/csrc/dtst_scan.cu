@@ -69,9 +69,9 @@ __device__ __forceinline__ long long clamp_len(const int* lengths, long long o, 
 // [outer][L][inner], inner contiguous.  A tile is TX groups of VEC channels times SLOTS runs of R steps, a run per thread.
 // Long sequences: the tiles of one outer entry lie side by side over its channels; a CTA (or a cluster) walks along L.
 // Short ones (one tile holds them): groups run on across outer entries, so that few channels fill a CTA too.
-template <int VEC_, int R_, int SLOTS_, int THREADS_ = 256>
+template <int VEC_, int R_, int SLOTS_, int CTAS_ = 2>
 struct ColShape {
-  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_, THREADS = THREADS_;
+  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_, THREADS = 256, CTAS = CTAS_;
   static constexpr int TX = THREADS / SLOTS, W = TX * VEC, LC = SLOTS * R;
   // while runs are joined a warp has CPW channels, DG lanes each, and a lane has JOIN neighbouring runs of its channel
   static constexpr int WARPS = THREADS / 32, CPW = W / WARPS < 32 ? W / WARPS : 32, DG = 32 / CPW;
@@ -257,7 +257,7 @@ __device__ __forceinline__ float join_round(const float2 all, float& state, Roun
 }
 
 template <typename T, class S, int MODE, bool WIDE>
-__global__ void __launch_bounds__(S::THREADS, 2) scan_cols_kernel(const ScanArgs<T> p) {
+__global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
   using Slots = ColSlots<T, S, 2, WIDE>;
   __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];     // (A, H) of every run; then its first state in x
@@ -416,8 +416,8 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_kernel(const ScanArgs
   }
 }
 
-template <typename T, class S, int MODE, bool WIDE>
-__global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const ScanArgs<T> p) {
+template <typename T, class S, int MODE, bool WIDE, bool SIGMOID>
+__global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
   using Slots = ColSlots<T, S, 3, WIDE>;
   // (A, H) and D of every run; then the state in front of it (x) and the gradient that comes to it from behind
@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const
     cluster_sync();
   }
   const int slot = threadIdx.x / S::TX, x = threadIdx.x % S::TX;
-  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
+  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(SIGMOID);
   const long long states = p.outer * p.inner;
   const int lane = threadIdx.x & 31;
   const int jx = (threadIdx.x / 32) * S::CPW + lane % S::CPW, jq = lane / S::CPW * S::JOIN;   // while joining: channel, first run
@@ -513,9 +513,8 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const
     // q: 1 - a (sigmoid) or a (decay); a is formed again where it is used
     float q[R][VEC], v[R][VEC], s[VEC], d[VEC];
     Pack<T, VEC> pd[R];
-    const float ka = p.sigmoid ? -1.f : 1.f, kb = p.sigmoid ? 1.f : 0.f;
-    auto a_of = [&](float qq) { return fmaf(qq, ka, kb); };
-    auto b_of = [&](float qq) { return p.sigmoid ? qq : 1.f; };
+        auto a_of = [](float qq) { return SIGMOID ? 1.f - qq : qq; };
+    auto b_of = [](float qq) { return SIGMOID ? qq : 1.f; };
     Pack<T, VEC> pv[R], pg[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) pv[r] = *slots.slot(0, r), pg[r] = *slots.slot(1, r), pd[r] = *slots.slot(2, r);
@@ -524,7 +523,7 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const
     for (int r = 0; r < R; ++r) {
       pg[r].unpack(q[r]);
       pv[r].unpack(v[r]);
-      if (p.sigmoid) {
+      if (SIGMOID) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
           float a;
@@ -603,7 +602,7 @@ __global__ void __launch_bounds__(S::THREADS, 2) scan_cols_backward_kernel(const
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float a = a_of(q[r][j]), u = b_of(q[r][j]) * v[r][j];
-        v[r][j] = p.sigmoid ? (s[j] - v[r][j]) * (a * q[r][j]) : s[j];
+        v[r][j] = SIGMOID ? (s[j] - v[r][j]) * (a * q[r][j]) : s[j];
         s[j] = fmaf(a, s[j], u);
       }
     const int t0 = c * LC + slot * R, left = at.live && c >= 0 ? (int)p.L - t0 : 0;
@@ -1056,10 +1055,10 @@ template <typename T, class S, int MODE, bool WIDE, bool BACK>
 cudaError_t launch_cols_kernel(const ScanArgs<T>& p, int cluster, cudaStream_t st) {
   void (*kern)(const ScanArgs<T>);
   constexpr size_t smem = ColSlots<T, S, BACK ? 3 : 2, WIDE>::SMEM;
-  if constexpr (BACK) kern = scan_cols_backward_kernel<T, S, MODE, WIDE>;
+  if constexpr (BACK) kern = p.sigmoid ? scan_cols_backward_kernel<T, S, MODE, WIDE, true> : scan_cols_backward_kernel<T, S, MODE, WIDE, false>;
   else kern = scan_cols_kernel<T, S, MODE, WIDE>;
-  static std::atomic<uint64_t> allowed{0};
-  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), smem + 2048 + sizeof(float) * 3 * S::SLOTS * S::W, allowed);
+  static std::atomic<uint64_t> allowed[2]{};
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), smem + 8192 + sizeof(float) * 3 * S::SLOTS * S::W, allowed[p.sigmoid != 0]);
   if (e != cudaSuccess) return e;
   if (MODE == kOneTile) return launch_pdl(kern, dim3((unsigned)p.chains), dim3(S::THREADS), smem, st, p);
   return launch_clusters(kern, p.chains, cluster, S::THREADS, smem, st, p);
@@ -1081,7 +1080,7 @@ cudaError_t launch_long_cols(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) 
   p.per_outer = (unsigned)per_outer;
   p.chains = p.outer * per_outer;
   p.chunks = (int)((p.L + S::LC - 1) / S::LC);
-  const int cluster = cluster_for(p.chains, p.chunks, 2 * (long long)num_sms(), 8);
+  const int cluster = cluster_for(p.chains, p.chunks, S::CTAS * (long long)num_sms(), 8);
   p.rounds = (p.chunks + cluster - 1) / cluster;
   if constexpr (S::VEC > 1) {
     constexpr int E = 16 / (int)sizeof(T);
@@ -1154,11 +1153,13 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   if (vec) {
     if (c.length <= 8) return launch_short_cols<T, ColShape<4, 8, 1>, BACK>(p, st);
     if (c.length <= 64) return launch_short_cols<T, ColShape<4, 8, 8>, BACK>(p, st);
+    if (BACK) return launch_long_cols<T, ColShape<4, 4, 64>, BACK>(p, c, st);
     return launch_long_cols<T, ColShape<4, 8, 32>, BACK>(p, c, st);
   }
   if (c.length <= 8) return launch_short_cols<T, ColShape<1, 8, 1>, BACK>(p, st);
   if (c.length <= 64) return launch_short_cols<T, ColShape<1, 8, 8>, BACK>(p, st);
-  return launch_long_cols<T, ColShape<1, 32, 8>, BACK>(p, c, st);
+  if (BACK) return launch_long_cols<T, ColShape<1, 16, 16, 3>, BACK>(p, c, st);
+  return launch_long_cols<T, ColShape<1, 16, 16, 4>, BACK>(p, c, st);
 }
 
 }  // namespace

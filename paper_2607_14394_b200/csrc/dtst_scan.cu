@@ -49,8 +49,9 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& b) {
   b = e * r;
 }
 // h_t = a h_{t-1} + b v_t
-__device__ __forceinline__ void terms(int sigmoid, float g, float& a, float& b) {
-  if (sigmoid) gate_of(g, a, b);
+template <bool SIGMOID>
+__device__ __forceinline__ void terms(float g, float& a, float& b) {
+  if (SIGMOID) gate_of(g, a, b);
   else a = g, b = 1.f;
 }
 // the gate of a step that leaves the state alone (with v = 0): a = 1
@@ -256,7 +257,7 @@ __device__ __forceinline__ float join_round(const float2 all, float& state, Roun
   return start;
 }
 
-template <typename T, class S, int MODE, bool WIDE>
+template <typename T, class S, int MODE, bool WIDE, bool SIGMOID>
 __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
   using Slots = ColSlots<T, S, 2, WIDE>;
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const Sc
     cluster_sync();
   }
   const int slot = threadIdx.x / S::TX, x = threadIdx.x % S::TX;
-  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
+  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(SIGMOID);
   const long long states = p.outer * p.inner;
   const int lane = threadIdx.x & 31;
   const int jx = (threadIdx.x / 32) * S::CPW + lane % S::CPW, jq = lane / S::CPW * S::JOIN;   // while joining: channel, first run
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const Sc
       pv[r].unpack(vv);
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        terms(p.sigmoid, gv[j], a[r][j], u[r][j]);
+        terms<SIGMOID>(gv[j], a[r][j], u[r][j]);
         u[r][j] *= vv[j];
       }
     }
@@ -694,22 +695,23 @@ struct RowUnit {
   __device__ __forceinline__ void load(Pack<T, V>& r, const Vec& v, int row, const T* base, long long stride, T none) const {
     if (WIDE && full(v)) {
       r.load(base + v.rel);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        r.v[i] = none;
-        if (on(v, i)) r.v[i] = base[WIDE ? v.rel + i : offset(v, row, i, stride)];
-      }
+      return;
     }
+    r.fill(none);
+    if (v.rel >= n) return;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (on(v, i)) r.v[i] = base[WIDE ? v.rel + i : offset(v, row, i, stride)];
   }
   __device__ __forceinline__ void store(const Pack<T, V>& r, const Vec& v, int row, T* base, long long stride) const {
     if (WIDE && full(v)) {
       r.store(base + v.rel);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (on(v, i)) base[WIDE ? v.rel + i : offset(v, row, i, stride)] = r.v[i];
+      return;
     }
+    if (v.rel >= n) return;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (on(v, i)) base[WIDE ? v.rel + i : offset(v, row, i, stride)] = r.v[i];
   }
   __device__ __forceinline__ long long offset(const Vec& v, int row, int i, long long stride) const {
     if (MODE != kWholeRows) return v.rel + i;
@@ -803,7 +805,7 @@ __device__ __forceinline__ void place_unit(const ScanArgs<T>& p, U& u, int c) {
   // rows that begin off a vector: only contiguous tensors are read wide then, all with the same shift
   u.shift = p.L % U::V == 0 ? 0 : (int)((u.row0 * p.L + u.t0) % U::V);
 }
-template <typename T, bool WIDE, int MODE, bool RAGGED>
+template <typename T, bool WIDE, int MODE, bool RAGGED, bool SIGMOID>
 __global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const ScanArgs<T> p) {
   using U = RowUnit<T, WIDE, MODE, RAGGED>;
   constexpr int V = U::V, K = U::K;
@@ -815,7 +817,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const Scan
   int me, members;
   if (!first_unit<U, T, MODE>(p, u, me, members)) return;
   const long long end = MODE == kWholeRows ? p.L : clamp_len(p.lengths, u.row0, p.L);
-  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
+  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(SIGMOID);
   float carry = 0.f;
   if (MODE != kWholeRows && p.h0 != nullptr) carry = p.h0[u.row0];
 #pragma unroll 1
@@ -844,7 +846,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const Scan
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         if (RAGGED && !(live[k] >> i & 1u)) pv[k].v[i] = none_v, pg[k].v[i] = none_g;
-        terms(p.sigmoid, pg[k].get(i), a[k][i], b[k][i]);
+        terms<SIGMOID>(pg[k].get(i), a[k][i], b[k][i]);
         b[k][i] *= pv[k].get(i);
         if (MODE == kWholeRows && i == x[k].spos) H[k] = h0v[k];
         A[k] *= a[k][i];
@@ -893,7 +895,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const Scan
   if (MODE == kTeam && members > kRowWarps) cluster_sync();       // nobody leaves while its box may be read
 }
 
-template <typename T, bool WIDE, int MODE, bool RAGGED>
+template <typename T, bool WIDE, int MODE, bool RAGGED, bool SIGMOID>
 __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(const ScanArgs<T> p) {
   using U = RowUnit<T, WIDE, MODE, RAGGED>;
   constexpr int V = U::V, K = U::K;
@@ -905,7 +907,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
   int me, members;
   if (!first_unit<U, T, MODE>(p, u, me, members)) return;
   const long long end = MODE == kWholeRows ? p.L : clamp_len(p.lengths, u.row0, p.L);
-  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(p.sigmoid);
+  const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(SIGMOID);
   float carry = 0.f;
   if (MODE != kWholeRows && p.g_last != nullptr) carry = p.g_last[u.row0];
 #pragma unroll 1
@@ -940,7 +942,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         if (RAGGED && !(live[k] >> i & 1u)) pv[k].v[i] = none_v, pg[k].v[i] = none_g, pd[k].v[i] = none_v;
-        terms(p.sigmoid, pg[k].get(i), a[k][i], b[k][i]);
+        terms<SIGMOID>(pg[k].get(i), a[k][i], b[k][i]);
         if (MODE == kWholeRows && i == x[k].spos) H[k] = h0v[k];
         A[k] *= a[k][i];
         H[k] = fmaf(a[k][i], H[k], b[k][i] * pv[k].get(i));
@@ -990,7 +992,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
       for (int i = 0; i < V; ++i) {       // what delta is multiplied with for the gate's gradient
         if (MODE == kWholeRows && i == x[k].spos) s = h0v[k];
         const float v = pv[k].get(i);
-        w[i] = p.sigmoid ? (s - v) * (a[k][i] * b[k][i]) : s;
+        w[i] = SIGMOID ? (s - v) * (a[k][i] * b[k][i]) : s;
         s = fmaf(a[k][i], s, b[k][i] * v);
       }
       Pack<T, V> ov, og;
@@ -1056,7 +1058,7 @@ cudaError_t launch_cols_kernel(const ScanArgs<T>& p, int cluster, cudaStream_t s
   void (*kern)(const ScanArgs<T>);
   constexpr size_t smem = ColSlots<T, S, BACK ? 3 : 2, WIDE>::SMEM;
   if constexpr (BACK) kern = p.sigmoid ? scan_cols_backward_kernel<T, S, MODE, WIDE, true> : scan_cols_backward_kernel<T, S, MODE, WIDE, false>;
-  else kern = scan_cols_kernel<T, S, MODE, WIDE>;
+  else kern = p.sigmoid ? scan_cols_kernel<T, S, MODE, WIDE, true> : scan_cols_kernel<T, S, MODE, WIDE, false>;
   static std::atomic<uint64_t> allowed[2]{};
   const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), smem + 8192 + sizeof(float) * 3 * S::SLOTS * S::W, allowed[p.sigmoid != 0]);
   if (e != cudaSuccess) return e;
@@ -1093,8 +1095,13 @@ cudaError_t launch_long_cols(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) 
 template <typename T, bool WIDE, int MODE, bool BACK>
 cudaError_t launch_rows_kernel(const ScanArgs<T>& p, long long tiles, int cluster, cudaStream_t st) {
   void (*kern)(const ScanArgs<T>);
-  if constexpr (BACK) kern = p.lengths != nullptr ? scan_rows_backward_kernel<T, WIDE, MODE, true> : scan_rows_backward_kernel<T, WIDE, MODE, false>;
-  else kern = p.lengths != nullptr ? scan_rows_kernel<T, WIDE, MODE, true> : scan_rows_kernel<T, WIDE, MODE, false>;
+  const bool ragged = p.lengths != nullptr, sigmoid = p.sigmoid != 0;
+  if constexpr (BACK)
+    kern = ragged ? (sigmoid ? scan_rows_backward_kernel<T, WIDE, MODE, true, true> : scan_rows_backward_kernel<T, WIDE, MODE, true, false>)
+                  : (sigmoid ? scan_rows_backward_kernel<T, WIDE, MODE, false, true> : scan_rows_backward_kernel<T, WIDE, MODE, false, false>);
+  else
+    kern = ragged ? (sigmoid ? scan_rows_kernel<T, WIDE, MODE, true, true> : scan_rows_kernel<T, WIDE, MODE, true, false>)
+                  : (sigmoid ? scan_rows_kernel<T, WIDE, MODE, false, true> : scan_rows_kernel<T, WIDE, MODE, false, false>);
   if (MODE == kTeam) return launch_clusters(kern, tiles, cluster, 32 * kRowWarps, 0, st, p);
   const long long ctas = (tiles + kRowWarps - 1) / kRowWarps;       // a unit per warp
   if (ctas > 0x7fffffff) return cudaErrorNotSupported;

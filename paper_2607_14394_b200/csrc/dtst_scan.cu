@@ -643,8 +643,8 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
 
 // ------------------------------------------------------------------------------------------------ rows
 // [outer][L], the steps contiguous, L >= 8.  A warp takes a unit of at most 512 neighbouring elements - whole rows, or a
-// chunk of a long one - in 16-byte vectors straight from global memory: K vectors a lane, the k-th at (32 k + lane) V.  Each
-// vector is composed in its lane, the lanes are joined by a warp scan that does not reach across a row's first step
+// chunk of a long one - in vectors of 8 (32 or 16 bytes) straight from global memory: K vectors a lane, the k-th at
+// (32 k + lane) 8.  Each vector is composed in its lane, the lanes are joined by a warp scan that does not reach across a row's first step
 // (forward) or last step (backward), and the K scans are joined one after the other.  No shared memory, no barriers.
 // Where rows begin off a vector the unit starts at the vector before; the elements in front are left alone.
 constexpr int kUnit = 512, kRowWarps = 8;
@@ -663,7 +663,7 @@ struct RowVec {
 
 template <typename T, bool WIDE, int MODE, bool RAGGED>
 struct RowUnit {
-  static constexpr int V = 16 / (int)sizeof(T), K = kUnit / 32 / V;
+  static constexpr int V = 8, K = kUnit / 32 / V;
   using Vec = RowVec<V>;
   long long row0;       // first row
   int n, t0, shift;     // elements; step of the first one; elements of its vector in front of it
@@ -1110,12 +1110,12 @@ cudaError_t launch_rows_kernel(const ScanArgs<T>& p, long long tiles, int cluste
 
 template <typename T, bool BACK>
 cudaError_t launch_rows(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
-  constexpr int V = 16 / (int)sizeof(T);
+  constexpr int V = 8;
   const int step = row_chunk(p.L);
   p.chunks = (int)((p.L + step - 1) / step);
   // one vector grid for all tensors: contiguous rows, or (a chunk is part of one row) rows that begin on vectors
   auto wide = [&](const void* base, long long stride) {
-    return base == nullptr || (aligned_to(base, 16) && (stride == p.L || (p.chunks > 1 && p.L % V == 0 && stride % V == 0)));
+    return base == nullptr || (aligned_to(base, V * sizeof(T)) && (stride == p.L || (p.chunks > 1 && p.L % V == 0 && stride % V == 0)));
   };
   const bool w = wide(c.v, c.in_outer) && wide(c.g, c.in_outer) && wide(c.h, p.L) && wide(c.grad_h, p.L) &&
                  wide(c.grad_v, c.grad_outer) && wide(c.grad_g, c.grad_outer);

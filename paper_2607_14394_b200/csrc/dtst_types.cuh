@@ -39,9 +39,12 @@ template <>
 struct RawOf<8> { using type = uint2; };
 template <>
 struct RawOf<16> { using type = uint4; };
+struct Words8 { uint32_t w[8]; };
+template <>
+struct RawOf<32> { using type = Words8; };
 
 // N elements as they lie in memory.  `load` and `store` move them in one access (the address is aligned to N
-// elements); the `_part` forms touch only the first `n` of them, one by one.
+// elements; 32 bytes are global memory's widest); the `_part` forms touch only the first `n` of them, one by one.
 template <typename T, int N>
 struct Pack {
   using Raw = typename RawOf<N * (int)sizeof(T)>::type;
@@ -50,12 +53,25 @@ struct Pack {
     T v[N];
   };
   __device__ __forceinline__ Pack() {}
-  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (sizeof(Raw) == 32)
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(raw.w[0]), "=r"(raw.w[1]), "=r"(raw.w[2]), "=r"(raw.w[3]), "=r"(raw.w[4]), "=r"(raw.w[5]), "=r"(raw.w[6]), "=r"(raw.w[7])
+                   : "l"(p)
+                   : "memory");
+    else raw = *reinterpret_cast<const Raw*>(p);
+  }
   __device__ __forceinline__ void load_part(const T* p, int n) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = i < n ? p[i] : Elem<T>::put(0.f);
   }
-  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Raw*>(p) = raw; }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (sizeof(Raw) == 32)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(raw.w[0]), "r"(raw.w[1]), "r"(raw.w[2]),
+                   "r"(raw.w[3]), "r"(raw.w[4]), "r"(raw.w[5]), "r"(raw.w[6]), "r"(raw.w[7])
+                   : "memory");
+    else *reinterpret_cast<Raw*>(p) = raw;
+  }
   __device__ __forceinline__ void store_part(T* p, int n) const {
 #pragma unroll
     for (int i = 0; i < N; ++i)

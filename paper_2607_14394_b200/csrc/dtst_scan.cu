@@ -806,7 +806,7 @@ __device__ __forceinline__ void place_unit(const ScanArgs<T>& p, U& u, int c) {
   u.shift = p.L % U::V == 0 ? 0 : (int)((u.row0 * p.L + u.t0) % U::V);
 }
 template <typename T, bool WIDE, int MODE, bool RAGGED, bool SIGMOID>
-__global__ void __launch_bounds__(32 * kRowWarps, 3) scan_rows_kernel(const ScanArgs<T> p) {
+__global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_kernel(const ScanArgs<T> p) {
   using U = RowUnit<T, WIDE, MODE, RAGGED>;
   constexpr int V = U::V, K = U::K;
   pdl_trigger();

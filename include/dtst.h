@@ -488,7 +488,9 @@ enum { DTST_F32 = 0, DTST_BF16 = 1, DTST_F16 = 2 };
  *   s = x + residual,  rstd = 1 / sqrt(mean_c s^2 + eps),  y = s * rstd * weight[c]
  * residual may be NULL (s = x); s and rstd [outer, inner] float32 may be NULL where they are not needed (the backward
  * pass needs both).  y is formed from the unrounded sum.  s may be x or residual itself, y may be x.  weight
- * [channels] float32.
+ * [channels] float32.  s_low (16-bit types; may be NULL): a buffer like s for what rounding took from the sum, with which
+ * the backward pass has the sum to 24 bits - without it the gradients are those of the rounded sum, whose relative
+ * distance from the sum's own (2^-9 in bfloat16) the float32 weight gradient would show.
  * Backward for grad_y and, where s went on as the residual stream, grad_s (or NULL):
  *   grad_x = rstd (weight grad_y - n mean_c(weight grad_y n)) + grad_s with n = s rstd   (also the residual's gradient)
  *   grad_weight[c] = sum over outer and inner of grad_y n, summed in a fixed order: same bits on every run.
@@ -496,11 +498,12 @@ enum { DTST_F32 = 0, DTST_BF16 = 1, DTST_F16 = 2 };
  * dtst_rms_norm_scratch_bytes, needed for grad_weight (DTST_ERR_WORKSPACE if missing or too small).
  */
 dtst_status dtst_rms_norm(int dtype, int64_t outer, int64_t channels, int64_t inner, float eps, const void* x,
-                          const void* residual, const float* weight, void* s, void* y, float* rstd, void* stream);
+                          const void* residual, const float* weight, void* s, void* s_low, void* y, float* rstd,
+                          void* stream);
 dtst_status dtst_rms_norm_scratch_bytes(int64_t channels, size_t* bytes);
 dtst_status dtst_rms_norm_backward(int dtype, int64_t outer, int64_t channels, int64_t inner, const void* grad_y,
-                                   const void* s, const float* weight, const float* rstd, const void* grad_s,
-                                   void* grad_x, float* grad_weight, void* scratch, size_t scratch_bytes, void* stream);
+                                   const void* s, const void* s_low, const float* weight, const float* rstd,
+                                   const void* grad_s, void* grad_x, float* grad_weight, void* scratch, size_t scratch_bytes, void* stream);
 
 /*
  * The same norm of rows x [rows, channels] with its output in 8 bits, the operand of dtst_matmul_fp8:

@@ -126,9 +126,9 @@ def lib() -> ctypes.CDLL:
     L.dtst_plan_last_cuda_error.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_char_p)]
     i64, sz, f32 = ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
     descp = ctypes.POINTER(ScanDesc)
-    L.dtst_rms_norm.argtypes = [i32, i64, i64, i64, f32] + [vp] * 7
+    L.dtst_rms_norm.argtypes = [i32, i64, i64, i64, f32] + [vp] * 8
     L.dtst_rms_norm_scratch_bytes.argtypes = [i64, ctypes.POINTER(sz)]
-    L.dtst_rms_norm_backward.argtypes = [i32, i64, i64, i64] + [vp] * 8 + [sz, vp]
+    L.dtst_rms_norm_backward.argtypes = [i32, i64, i64, i64] + [vp] * 9 + [sz, vp]
     L.dtst_rms_norm_fp8.argtypes = [i32, i64, i64, f32, vp, vp, vp, vp, vp, i64, vp, vp]
     L.dtst_quantize_fp8.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp]
     L.dtst_quantize_fp8_weight.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp]

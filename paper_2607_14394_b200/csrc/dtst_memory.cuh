@@ -29,7 +29,7 @@ struct NormCall {
   float eps;
   const void *x, *residual;
   const float* weight;     // null: quantise x as it is
-  void *s, *y;
+  void *s, *low, *y;       // low: what rounding took from s (16-bit types; may be null)
   uint8_t* q;              // non-null: 8-bit output instead of y
   float *scale, *rstd;
   long long x_ld, q_ld;    // elements between rows of x (rows only), bytes between rows of q
@@ -39,7 +39,7 @@ cudaError_t launch_norm_forward(const NormCall& n, cudaStream_t st);
 struct NormBackCall {
   int dtype;
   long long outer, channels, inner;
-  const void *grad_y, *s, *grad_s;
+  const void *grad_y, *s, *low, *grad_s;
   const float *weight, *rstd;
   void* grad_x;
   float *grad_weight, *partial;

@@ -66,14 +66,17 @@ ScanCall scan_call(const dtst_scan_desc* d) {
 extern "C" {
 
 dtst_status dtst_rms_norm(int dtype, int64_t outer, int64_t channels, int64_t inner, float eps, const void* x,
-                          const void* residual, const float* weight, void* s, void* y, float* rstd, void* stream) {
+                          const void* residual, const float* weight, void* s, void* s_low, void* y, float* rstd,
+                          void* stream) {
   if (!known(dtype) || outer < 0 || inner < 0 || channels < 1 || !(eps >= 0.f) || !small_product(outer, channels, inner))
     return DTST_ERR_INVALID_ARG;
   if (outer == 0 || inner == 0) return DTST_OK;
   if (x == nullptr || weight == nullptr || y == nullptr || y == s || y == residual || !fits(x, dtype) || !fits(residual, dtype) ||
       !fits(s, dtype) || !fits(y, dtype) || !f32(weight) || !f32(rstd))
     return DTST_ERR_INVALID_ARG;
-  NormCall n{dtype, outer, channels, inner, eps, x, residual, weight, s, y, nullptr, nullptr, rstd, channels, 0};
+  if (s_low != nullptr && (dtype == DTST_F32 || s == nullptr || s_low == s || s_low == y || s_low == x || s_low == residual || !fits(s_low, dtype)))
+    return DTST_ERR_INVALID_ARG;
+  NormCall n{dtype, outer, channels, inner, eps, x, residual, weight, s, s_low, y, nullptr, nullptr, rstd, channels, 0};
   return done(launch_norm_forward(n, static_cast<cudaStream_t>(stream)));
 }
 
@@ -84,8 +87,8 @@ dtst_status dtst_rms_norm_scratch_bytes(int64_t channels, size_t* bytes) {
 }
 
 dtst_status dtst_rms_norm_backward(int dtype, int64_t outer, int64_t channels, int64_t inner, const void* grad_y,
-                                   const void* s, const float* weight, const float* rstd, const void* grad_s,
-                                   void* grad_x, float* grad_weight, void* scratch, size_t scratch_bytes, void* stream) {
+                                   const void* s, const void* s_low, const float* weight, const float* rstd,
+                                   const void* grad_s, void* grad_x, float* grad_weight, void* scratch, size_t scratch_bytes, void* stream) {
   if (!known(dtype) || outer < 0 || inner < 0 || channels < 1 || !small_product(outer, channels, inner) || !f32(grad_weight))
     return DTST_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -94,16 +97,16 @@ dtst_status dtst_rms_norm_backward(int dtype, int64_t outer, int64_t channels, i
     return done(cudaMemsetAsync(grad_weight, 0, (size_t)channels * sizeof(float), st));   // an empty sum
   }
   if (grad_y == nullptr || s == nullptr || weight == nullptr || rstd == nullptr || grad_x == nullptr || grad_x == s ||
+      (s_low != nullptr && (dtype == DTST_F32 || grad_x == s_low || !fits(s_low, dtype))) ||
       !fits(grad_y, dtype) || !fits(s, dtype) || !fits(grad_s, dtype) || !fits(grad_x, dtype) || !f32(weight) || !f32(rstd))
     return DTST_ERR_INVALID_ARG;
-  // a separate pass over grad_y and s forms the weight gradient of very wide norms
   if (grad_weight != nullptr) {
     size_t need = 0;
     dtst_rms_norm_scratch_bytes(channels, &need);
     if (scratch == nullptr || scratch_bytes < need) return DTST_ERR_WORKSPACE;
     if (!aligned_to(scratch, 16)) return DTST_ERR_INVALID_ARG;
   }
-  NormBackCall n{dtype, outer, channels, inner, grad_y, s, grad_s, weight, rstd, grad_x, grad_weight, static_cast<float*>(scratch)};
+  NormBackCall n{dtype, outer, channels, inner, grad_y, s, s_low, grad_s, weight, rstd, grad_x, grad_weight, static_cast<float*>(scratch)};
   return done(launch_norm_backward(n, st));
 }
 
@@ -115,7 +118,7 @@ dtst_status dtst_rms_norm_fp8(int dtype, int64_t rows, int64_t channels, float e
   if (x == nullptr || weight == nullptr || q == nullptr || scale == nullptr || q == x || q == s || q == residual ||
       !fits(x, dtype) || !fits(residual, dtype) || !fits(s, dtype) || !f32(weight) || !f32(scale))
     return DTST_ERR_INVALID_ARG;
-  NormCall n{dtype, rows, channels, 1, eps, x, residual, weight, s, nullptr, static_cast<uint8_t*>(q), scale, nullptr, channels, q_ld};
+  NormCall n{dtype, rows, channels, 1, eps, x, residual, weight, s, nullptr, nullptr, static_cast<uint8_t*>(q), scale, nullptr, channels, q_ld};
   return done(launch_norm_forward(n, static_cast<cudaStream_t>(stream)));
 }
 
@@ -126,7 +129,7 @@ dtst_status dtst_quantize_fp8(int dtype, int64_t rows, int64_t channels, const v
     return DTST_ERR_INVALID_ARG;
   if (rows == 0) return DTST_OK;
   if (x == nullptr || q == nullptr || scale == nullptr || q == x || !fits(x, dtype) || !f32(scale)) return DTST_ERR_INVALID_ARG;
-  NormCall n{dtype, rows, channels, 1, 0.f, x, nullptr, nullptr, nullptr, nullptr, static_cast<uint8_t*>(q), scale, nullptr, x_ld, q_ld};
+  NormCall n{dtype, rows, channels, 1, 0.f, x, nullptr, nullptr, nullptr, nullptr, nullptr, static_cast<uint8_t*>(q), scale, nullptr, x_ld, q_ld};
   return done(launch_norm_forward(n, static_cast<cudaStream_t>(stream)));
 }
 

@@ -129,7 +129,7 @@ __device__ __forceinline__ void quantise_store(const float (&y)[VEC], uint8_t* q
 struct RowArgs {
   const void *x, *residual;
   const float* weight;
-  void *s, *y;
+  void *s, *low, *y;        // low: what rounding took from s (16-bit types; may be null)
   uint8_t* q;
   float *scale, *rstd;
   long long rows, C, x_ld, q_ld;
@@ -192,6 +192,12 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_kernel(const RowAr
           Pack<T, VEC> out;
           out.pack(v[k]);
           store_group<T, LAY>(out, static_cast<T*>(a.s) + row * a.C, (long long)(tr + k * TPR) * VEC - shift, a.C);
+          if (sizeof(T) == 2 && a.low != nullptr) {
+            Pack<T, VEC> lo;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) lo.v[i] = LowBits<T>::take(v[k][i], out.v[i]);
+            store_group<T, LAY>(lo, static_cast<T*>(a.low) + row * a.C, (long long)(tr + k * TPR) * VEC - shift, a.C);
+          }
         }
       }
       rstd = rsqrtf(fmaf(row_sum<TPR, RPC>(sum, red, phase), inv_c, a.eps));
@@ -202,7 +208,7 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_kernel(const RowAr
       const long long c = (long long)(tr + k * TPR) * VEC - shift;
       if (NORM) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) v[k][i] *= rstd * w[k][i];
+        for (int i = 0; i < VEC; ++i) v[k][i] = v[k][i] * rstd * w[k][i];
       }
       if (QUANT) {
         quantise_store<VEC>(v[k], a.q + row * a.q_ld, a.scale, c, a.C, a.rows, row, a.q_aligned != 0);
@@ -247,8 +253,12 @@ __global__ void __launch_bounds__(512) norm_long_rows_kernel(const RowArgs a) {
           float v = Elem<T>::get(x[c + i]);
           if (NORM) {
             if (res != nullptr) v += Elem<T>::get(res[row * a.C + c + i]);
-            if (a.s != nullptr) static_cast<T*>(a.s)[row * a.C + c + i] = Elem<T>::put(v);
-            v *= rstd * __ldg(a.weight + c + i);
+            if (a.s != nullptr) {
+              const T out = Elem<T>::put(v);
+              static_cast<T*>(a.s)[row * a.C + c + i] = out;
+              if (sizeof(T) == 2 && a.low != nullptr) static_cast<T*>(a.low)[row * a.C + c + i] = LowBits<T>::take(v, out);
+            }
+            v = v * rstd * __ldg(a.weight + c + i);
           }
           y[i] = v;
         }
@@ -287,7 +297,7 @@ cudaError_t launch_rows_kernel(const RowArgs& a, cudaStream_t st) {
 template <typename T, bool QUANT, bool NORM>
 cudaError_t launch_rows(const RowArgs& a, cudaStream_t st) {
   constexpr int VEC = kVec<T>;
-  RowLayout lay = row_layout<T>(a.C, a.x_ld, {a.x, a.residual, a.s, QUANT ? nullptr : a.y});
+  RowLayout lay = row_layout<T>(a.C, a.x_ld, {a.x, a.residual, a.s, a.low, QUANT ? nullptr : a.y});
   if (lay == kAligned && !aligned_to(a.weight, 16)) lay = kScalar;
   if (QUANT && lay == kShifted) lay = kScalar;       // blocks of 128 channels are counted from the row's beginning
   const long long groups = (a.C + (lay == kShifted ? VEC - 1 : 0) + VEC - 1) / VEC;
@@ -312,7 +322,7 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t st) {
 
 // ---- backward, rows
 struct RowBackArgs {
-  const void *gy, *s, *gs;
+  const void *gy, *s, *low, *gs;
   const float *weight, *rstd;
   void* gx;
   float* partial;   // [gridDim.x][C]
@@ -332,9 +342,10 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_backward_kernel(co
   const T* gy = static_cast<const T*>(a.gy);
   const T* s = static_cast<const T*>(a.s);
   const T* gs = static_cast<const T*>(a.gs);
+  const T* low = sizeof(T) == 2 ? static_cast<const T*>(a.low) : nullptr;
   const long long group = (long long)blockIdx.x * RPC + threadIdx.x / TPR, step = (long long)gridDim.x * RPC;
   const int shift = LAY == kShifted ? (int)(group * a.C % VEC) : 0;
-  Pack<T, VEC> pg[ITEMS], ps[ITEMS], pr[ITEMS];
+  Pack<T, VEC> pg[ITEMS], ps[ITEMS], pr[ITEMS], pl[ITEMS];
   float rstd_next = 0.f;
   auto fetch = [&](long long row) {
 #pragma unroll
@@ -343,6 +354,7 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_backward_kernel(co
       load_group<T, LAY>(pg[k], gy + row * a.C, c, a.C);
       load_group<T, LAY>(ps[k], s + row * a.C, c, a.C);
       if (gs != nullptr) load_group<T, LAY>(pr[k], gs + row * a.C, c, a.C);
+      if (low != nullptr) load_group<T, LAY>(pl[k], low + row * a.C, c, a.C);
     }
     rstd_next = __ldg(a.rstd + row);
   };
@@ -364,6 +376,10 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_backward_kernel(co
     for (int k = 0; k < ITEMS; ++k) {
       pg[k].unpack(g[k]);
       ps[k].unpack(n[k]);
+      if (low != nullptr) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) n[k][i] = LowBits<T>::join(ps[k].v[i], pl[k].v[i]);
+      }
       if (gs != nullptr) pq[k] = pr[k];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
@@ -418,6 +434,13 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_backward_kernel(co
   }
 }
 
+// the sum at element `at`, to 32 bits where its low part was kept
+template <typename T>
+__device__ __forceinline__ float sum_at(const void* s, const void* low, long long at) {
+  const T v = static_cast<const T*>(s)[at];
+  return sizeof(T) == 2 && low != nullptr ? LowBits<T>::join(v, static_cast<const T*>(low)[at]) : Elem<T>::get(v);
+}
+
 // Longer rows: grad_x by one CTA per row (the row read twice), then the weight gradient column by column.
 template <typename T>
 __global__ void __launch_bounds__(512) norm_long_rows_backward_kernel(const RowBackArgs a) {
@@ -427,14 +450,13 @@ __global__ void __launch_bounds__(512) norm_long_rows_backward_kernel(const RowB
   int phase = 0;
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* gy = static_cast<const T*>(a.gy) + row * a.C;
-    const T* s = static_cast<const T*>(a.s) + row * a.C;
     const float rstd = a.rstd[row];
     float dot = 0.f;
     for (long long c = threadIdx.x; c < a.C; c += 512)
-      dot = fmaf(__ldg(a.weight + c) * Elem<T>::get(gy[c]), Elem<T>::get(s[c]) * rstd, dot);
+      dot = fmaf(__ldg(a.weight + c) * Elem<T>::get(gy[c]), sum_at<T>(a.s, a.low, row * a.C + c) * rstd, dot);
     dot = row_sum<512>(dot, red, phase) / (float)a.C;
     for (long long c = threadIdx.x; c < a.C; c += 512) {
-      float g = rstd * fmaf(-(Elem<T>::get(s[c]) * rstd), dot, __ldg(a.weight + c) * Elem<T>::get(gy[c]));
+      float g = rstd * fmaf(-(sum_at<T>(a.s, a.low, row * a.C + c) * rstd), dot, __ldg(a.weight + c) * Elem<T>::get(gy[c]));
       if (a.gs != nullptr) g += Elem<T>::get(static_cast<const T*>(a.gs)[row * a.C + c]);
       static_cast<T*>(a.gx)[row * a.C + c] = Elem<T>::put(g);
     }
@@ -449,7 +471,7 @@ __global__ void __launch_bounds__(256) norm_long_rows_weight_kernel(const RowBac
   float t = 0.f;
   for (long long row = blockIdx.y; row < a.rows; row += gridDim.y)
     t = fmaf(Elem<T>::get(static_cast<const T*>(a.gy)[row * a.C + c]),
-             Elem<T>::get(static_cast<const T*>(a.s)[row * a.C + c]) * __ldg(a.rstd + row), t);
+             sum_at<T>(a.s, a.low, row * a.C + c) * __ldg(a.rstd + row), t);
   a.partial[(long long)blockIdx.y * a.C + c] = t;
 }
 
@@ -458,7 +480,7 @@ struct FieldArgs {
   const void *x, *residual, *gy, *gs;
   const float* weight;
   const float* rstd_in;
-  void *s, *y;          // backward: y is grad_x, x is s
+  void *s, *low, *y;    // backward: y is grad_x, x is s
   float *rstd, *partial;
   long long outer, C, inner, tiles;   // tiles per outer entry
   float eps;
@@ -504,7 +526,14 @@ __global__ void __launch_bounds__(256) norm_field_kernel(const FieldArgs a) {
         const int c = wy + k * ny;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) px[k].put(i, v[k][i]);
-        if (c < a.C) px[k].store(static_cast<T*>(a.s) + base + c * a.inner);
+        if (c >= a.C) continue;
+        px[k].store(static_cast<T*>(a.s) + base + c * a.inner);
+        if (sizeof(T) == 2 && a.low != nullptr) {
+          Pack<T, VEC> lo;
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) lo.v[i] = LowBits<T>::take(v[k][i], px[k].v[i]);
+          lo.store(static_cast<T*>(a.low) + base + c * a.inner);
+        }
       }
     }
 #pragma unroll
@@ -529,7 +558,7 @@ __global__ void __launch_bounds__(256) norm_field_kernel(const FieldArgs a) {
       if (c >= a.C) continue;
       const float w = __ldg(a.weight + c);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) px[k].put(i, v[k][i] * (rstd[i] * w));
+      for (int i = 0; i < VEC; ++i) px[k].put(i, v[k][i] * rstd[i] * w);
       px[k].store(static_cast<T*>(a.y) + base + c * a.inner);
     }
   }
@@ -543,6 +572,7 @@ __global__ void __launch_bounds__(256) norm_field_backward_kernel(const FieldArg
   const int lane = threadIdx.x, wy = threadIdx.y, ny = blockDim.y;
   const float inv_c = 1.0f / (float)a.C;
   const T* gs = static_cast<const T*>(a.gs);
+  const T* low = sizeof(T) == 2 ? static_cast<const T*>(a.low) : nullptr;
   // the sums over a CTA's positions are compensated (Kahan): a thread adds thousands of tiles one by one
   float gw[NCH], lost[NCH], w[NCH];
 #pragma unroll
@@ -556,7 +586,7 @@ __global__ void __launch_bounds__(256) norm_field_backward_kernel(const FieldArg
     const long long o = t / a.tiles, p = (t % a.tiles) * (32 * VEC) + lane * VEC;
     const long long base = o * a.C * a.inner + p;
     const bool live = p < a.inner;
-    Pack<T, VEC> pg[NCH], ps[NCH], pr[NCH];
+    Pack<T, VEC> pg[NCH], ps[NCH], pr[NCH], pl[NCH];
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int c = wy + k * ny;
@@ -566,7 +596,11 @@ __global__ void __launch_bounds__(256) norm_field_backward_kernel(const FieldArg
       if (gs != nullptr) {
         if (on) pr[k].load(gs + base + c * a.inner); else pr[k].zero();
       }
+      if (low != nullptr) {
+        if (on) pl[k].load(low + base + c * a.inner); else pl[k].zero();
+      }
     }
+    auto sum_of = [&](int k, int i) { return low != nullptr ? LowBits<T>::join(ps[k].v[i], pl[k].v[i]) : ps[k].get(i); };
     float rstd[VEC], dot[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
@@ -578,7 +612,7 @@ __global__ void __launch_bounds__(256) norm_field_backward_kernel(const FieldArg
       float t = -lost[k];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const float g = pg[k].get(i), n = ps[k].get(i) * rstd[i];
+        const float g = pg[k].get(i), n = sum_of(k, i) * rstd[i];
         t = fmaf(g, n, t);
         dot[i] = fmaf(w[k] * g, n, dot[i]);
       }
@@ -603,7 +637,7 @@ __global__ void __launch_bounds__(256) norm_field_backward_kernel(const FieldArg
       if (c >= a.C) continue;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        float g = rstd[i] * fmaf(-(ps[k].get(i) * rstd[i]), dot[i], w[k] * pg[k].get(i));
+        float g = rstd[i] * fmaf(-(sum_of(k, i) * rstd[i]), dot[i], w[k] * pg[k].get(i));
         if (gs != nullptr) g += pr[k].get(i);
         ps[k].put(i, g);
       }
@@ -640,8 +674,12 @@ __global__ void __launch_bounds__(128) norm_wide_field_kernel(const FieldArgs a)
     for (long long c = 0; c < a.C; ++c) {
       float v = Elem<T>::get(static_cast<const T*>(a.x)[base + c * a.inner]);
       if (res != nullptr) v += Elem<T>::get(res[base + c * a.inner]);
-      if (a.s != nullptr) static_cast<T*>(a.s)[base + c * a.inner] = Elem<T>::put(v);
-      static_cast<T*>(a.y)[base + c * a.inner] = Elem<T>::put(v * (rstd * __ldg(a.weight + c)));
+      if (a.s != nullptr) {
+        const T out = Elem<T>::put(v);
+        static_cast<T*>(a.s)[base + c * a.inner] = out;
+        if (sizeof(T) == 2 && a.low != nullptr) static_cast<T*>(a.low)[base + c * a.inner] = LowBits<T>::take(v, out);
+      }
+      static_cast<T*>(a.y)[base + c * a.inner] = Elem<T>::put(v * rstd * __ldg(a.weight + c));
     }
   }
 }
@@ -650,7 +688,6 @@ __global__ void __launch_bounds__(128) norm_wide_field_backward_kernel(const Fie
   pdl_trigger();
   pdl_wait();
   const T* gy = static_cast<const T*>(a.gy);
-  const T* s = static_cast<const T*>(a.x);
   const T* gs = static_cast<const T*>(a.gs);
   const float inv_c = 1.0f / (float)a.C;
   const long long n = a.outer * a.inner;
@@ -659,10 +696,10 @@ __global__ void __launch_bounds__(128) norm_wide_field_backward_kernel(const Fie
     const float rstd = a.rstd_in[t];
     float dot = 0.f;
     for (long long c = 0; c < a.C; ++c)
-      dot = fmaf(__ldg(a.weight + c) * Elem<T>::get(gy[base + c * a.inner]), Elem<T>::get(s[base + c * a.inner]) * rstd, dot);
+      dot = fmaf(__ldg(a.weight + c) * Elem<T>::get(gy[base + c * a.inner]), sum_at<T>(a.x, a.low, base + c * a.inner) * rstd, dot);
     dot *= inv_c;
     for (long long c = 0; c < a.C; ++c) {
-      float g = rstd * fmaf(-(Elem<T>::get(s[base + c * a.inner]) * rstd), dot,
+      float g = rstd * fmaf(-(sum_at<T>(a.x, a.low, base + c * a.inner) * rstd), dot,
                             __ldg(a.weight + c) * Elem<T>::get(gy[base + c * a.inner]));
       if (gs != nullptr) g += Elem<T>::get(gs[base + c * a.inner]);
       static_cast<T*>(a.y)[base + c * a.inner] = Elem<T>::put(g);
@@ -680,7 +717,7 @@ __global__ void __launch_bounds__(256) norm_wide_field_weight_kernel(const Field
   float t = 0.f;
   for (long long p = (long long)blockIdx.y * 256 + threadIdx.x; p < n; p += (long long)gridDim.y * 256) {
     const long long at = (p / a.inner) * a.C * a.inner + c * a.inner + p % a.inner;
-    t = fmaf(Elem<T>::get(static_cast<const T*>(a.gy)[at]), Elem<T>::get(static_cast<const T*>(a.x)[at]) * a.rstd_in[p], t);
+    t = fmaf(Elem<T>::get(static_cast<const T*>(a.gy)[at]), sum_at<T>(a.x, a.low, at) * a.rstd_in[p], t);
   }
   t = row_sum<256>(t, red, phase);
   if (threadIdx.x == 0) a.partial[(long long)blockIdx.y * a.C + c] = t;
@@ -724,7 +761,7 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
   }
   const size_t need = WIDE * sizeof(T);
   const bool vec = a.inner % WIDE == 0 && aligned_to(a.x, need) && aligned_to(a.residual, need) && aligned_to(a.gy, need) &&
-                   aligned_to(a.gs, need) && aligned_to(a.s, need) && aligned_to(a.y, need);
+                   aligned_to(a.gs, need) && aligned_to(a.s, need) && aligned_to(a.low, need) && aligned_to(a.y, need);
   const int ny = a.C <= 32 ? 4 : 8, nch = (int)((a.C + ny - 1) / ny);
   const int per = 32 * (vec ? WIDE : 1);
   a.tiles = (a.inner + per - 1) / per;
@@ -751,7 +788,7 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
 template <typename T>
 cudaError_t launch_rows_backward(const RowBackArgs& a, int* parts, cudaStream_t st) {
   constexpr int VEC = kVec<T>;
-  const RowLayout lay = row_layout<T>(a.C, a.C, {a.gy, a.s, a.gs, a.gx});
+  const RowLayout lay = row_layout<T>(a.C, a.C, {a.gy, a.s, a.low, a.gs, a.gx});
   const long long groups = (a.C + (lay == kShifted ? VEC - 1 : 0) + VEC - 1) / VEC;
 #define DTST_ROWS(TPR, ITEMS)                                                                                     \
   {                                                                                                               \
@@ -770,6 +807,8 @@ cudaError_t launch_rows_backward(const RowBackArgs& a, int* parts, cudaStream_t 
   if (groups <= 256) DTST_ROWS(256, 1)
   if (groups <= 512) DTST_ROWS(512, 1)
   if (groups <= 1024) DTST_ROWS(512, 2)
+  if constexpr (sizeof(T) == 4)       // (16 elements of a 16-bit type a thread would spill)
+    if (groups <= 2048) DTST_ROWS(1024, 2)
 #undef DTST_ROWS
   const long long most = (long long)num_sms() * 4;
   cudaError_t e = launch_pdl(norm_long_rows_backward_kernel<T>, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(512), 0, st, a);
@@ -783,12 +822,12 @@ cudaError_t launch_rows_backward(const RowBackArgs& a, int* parts, cudaStream_t 
 template <typename T>
 cudaError_t forward_t(const NormCall& n, cudaStream_t st) {
   if (n.inner == 1 || n.q != nullptr) {
-    RowArgs a{n.x, n.residual, n.weight, n.s, n.y, n.q, n.scale, n.rstd, n.outer, n.channels, n.x_ld, n.q_ld, n.eps, 0};
+    RowArgs a{n.x, n.residual, n.weight, n.s, n.low, n.y, n.q, n.scale, n.rstd, n.outer, n.channels, n.x_ld, n.q_ld, n.eps, 0};
     if (n.q == nullptr) return launch_rows<T, false, true>(a, st);
     a.q_aligned = n.q_ld % 8 == 0 && aligned_to(n.q, 8);
     return n.weight != nullptr ? launch_rows<T, true, true>(a, st) : launch_rows<T, true, false>(a, st);
   }
-  FieldArgs a{n.x, n.residual, nullptr, nullptr, n.weight, nullptr, n.s, n.y, n.rstd, nullptr, n.outer, n.channels, n.inner, 0, n.eps};
+  FieldArgs a{n.x, n.residual, nullptr, nullptr, n.weight, nullptr, n.s, n.low, n.y, n.rstd, nullptr, n.outer, n.channels, n.inner, 0, n.eps};
   int parts = 0;
   return launch_field<T, false>(a, &parts, st);
 }
@@ -799,10 +838,10 @@ cudaError_t backward_t(const NormBackCall& n, cudaStream_t st) {
   cudaError_t e;
   float* partial = n.grad_weight != nullptr ? n.partial : nullptr;
   if (n.inner == 1) {
-    RowBackArgs a{n.grad_y, n.s, n.grad_s, n.weight, n.rstd, n.grad_x, partial, n.outer, n.channels};
+    RowBackArgs a{n.grad_y, n.s, n.low, n.grad_s, n.weight, n.rstd, n.grad_x, partial, n.outer, n.channels};
     e = launch_rows_backward<T>(a, &parts, st);
   } else {
-    FieldArgs a{n.s, nullptr, n.grad_y, n.grad_s, n.weight, n.rstd, nullptr, n.grad_x, nullptr, partial, n.outer, n.channels, n.inner, 0, 0.f};
+    FieldArgs a{n.s, nullptr, n.grad_y, n.grad_s, n.weight, n.rstd, nullptr, const_cast<void*>(n.low), n.grad_x, nullptr, partial, n.outer, n.channels, n.inner, 0, 0.f};
     e = launch_field<T, true>(a, &parts, st);
   }
   if (e != cudaSuccess || partial == nullptr) return e;

@@ -8,6 +8,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace dtst {
 
 template <typename T>
@@ -143,6 +145,29 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
+
+// What rounding a 32-bit sum to 16 bits took from it, in 16 more bits: in units of 2^-16 of the rounded value's last place, so
+// that the two give the sum back to 24 bits.  (Values below 2^-80 keep nothing.)
+template <typename T>
+struct LowBits {
+  static __device__ __forceinline__ int unit(float s) {        // exponent field of that unit's inverse
+    constexpr int M = sizeof(T) == 4 ? 23 : std::is_same<T, __half>::value ? 10 : 7, LEAST = M == 10 ? 127 - 14 : 0;
+    const int e = (__float_as_uint(s) >> 23) & 0xff;
+    return 270 + M - (e > LEAST ? e : LEAST);
+  }
+  static __device__ __forceinline__ T take(float sum, T rounded) {
+    const float s = Elem<T>::get(rounded);
+    const int u = unit(s);
+    const int lo = u > 230 ? 0 : max(-32768, min(32767, __float2int_rn((sum - s) * __uint_as_float((uint32_t)u << 23))));
+    const short b = (short)lo;
+    return *reinterpret_cast<const T*>(&b);
+  }
+  static __device__ __forceinline__ float join(T rounded, T low) {
+    const float s = Elem<T>::get(rounded);
+    const int u = unit(s);
+    return u > 230 ? s : fmaf((float)*reinterpret_cast<const short*>(&low), __uint_as_float((uint32_t)(254 - u) << 23), s);
+  }
+};
 
 // thread-block clusters
 __device__ __forceinline__ int cluster_size() {

@@ -112,12 +112,17 @@ class RmsNorm:
         self._scratch = None
         self._lib = Bn.lib()
 
-    def forward(self, x, weight, residual=None, out=None, sum_out=None, rstd=None, stream=None):
-        """Returns (y, s, rstd); without a residual s is x itself."""
+    def forward(self, x, weight, residual=None, out=None, sum_out=None, rstd=None, need_backward=True, stream=None):
+        """Returns (y, s, rstd); without a residual s is x itself.
+
+        In a 16-bit type with a residual, what rounding took from s stays with the rstd that is returned (its attribute
+        `sum_low`), so that `backward` has the sum to 24 bits; an rstd that the caller brings may carry such a buffer too.
+        need_backward=False: neither is formed, and rstd is None.
+        """
         d, t, sh = self.dev, self.dtype, self.shape
         if stream is not None or _current_device() != d:
             with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
-                return self.forward(x, weight, residual, out, sum_out, rstd)
+                return self.forward(x, weight, residual, out, sum_out, rstd, need_backward)
         xp, wp = _addr(x, "x", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
         rp = sp = 0
         if sum_out is not None:
@@ -132,13 +137,19 @@ class RmsNorm:
             yp = out.data_ptr()
         else:
             yp = _addr(out, "out", d, t, sh)
-        if rstd is None:
+        qp = lp = 0
+        if rstd is not None:
+            qp = _addr(rstd, "rstd", d, torch.float32, self._rest)
+            if sp and self._type:
+                lp = _addr(getattr(rstd, "sum_low", None), "rstd.sum_low", d, t, sh)
+        elif need_backward:
             rstd = weight.new_empty(self._rest)
             qp = rstd.data_ptr()
-        else:
-            qp = _addr(rstd, "rstd", d, torch.float32, self._rest)
-        status = self._lib.dtst_rms_norm(self._type, self.outer, self.channels, self.inner, self.eps, xp, rp, wp, sp, yp, qp,
-                                         _raw_stream(d))
+            if rp and self._type:
+                rstd.sum_low = low = torch.empty_like(x)
+                lp = low.data_ptr()
+        status = self._lib.dtst_rms_norm(self._type, self.outer, self.channels, self.inner, self.eps, xp, rp, wp, sp, lp, yp,
+                                         qp, _raw_stream(d))
         if status:
             _check(status, "dtst_rms_norm")
         return out, (x if sum_out is None else sum_out), rstd
@@ -178,7 +189,8 @@ class RmsNorm:
 
     def backward(self, grad_y, s, weight, rstd, grad_s=None, grad_x=None, grad_weight=None, need_grad_weight=True,
                  stream=None):
-        """Returns (grad_x, grad_weight); grad_x is the gradient of x and of the residual."""
+        """Returns (grad_x, grad_weight); grad_x is the gradient of x and of the residual.  s and rstd as `forward`
+        returned them."""
         d, t, sh = self.dev, self.dtype, self.shape
         if stream is not None or _current_device() != d:
             with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
@@ -203,7 +215,8 @@ class RmsNorm:
                 self._scratch_at = (self._scratch.data_ptr(), int(n.value))
             scratch, nbytes = self._scratch_at
         status = self._lib.dtst_rms_norm_backward(
-            self._type, self.outer, self.channels, self.inner, gp, _addr(s, "s", d, t, sh), wp,
+            self._type, self.outer, self.channels, self.inner, gp, _addr(s, "s", d, t, sh),
+            _addr(rstd.sum_low, "rstd.sum_low", d, t, sh) if self._type and hasattr(rstd, "sum_low") else 0, wp,
             _addr(rstd, "rstd", d, torch.float32, self._rest), 0 if grad_s is None else _addr(grad_s, "grad_s", d, t, sh),
             xp, gwp, scratch, nbytes, _raw_stream(d))
         if status:
@@ -574,7 +587,7 @@ class RolloutMemory:
             vg = lin_in.forward(q, sc).view(B, T, 2 * lin_out.k)
             h, _ = scan.forward(vg[..., :lin_out.k], vg[..., lin_out.k:], state, lengths=lengths, h_last=state)
             delta = lin_out.forward(*quantize_fp8(h.view(B * T, lin_out.k)))
-        y, _, _ = norm.forward(r, self.final_weight, residual=delta)
+        y, _, _ = norm.forward(r, self.final_weight, residual=delta, need_backward=False)
         return y.view(B, T, D)
 
     def step(self, frame: torch.Tensor, stream=None) -> torch.Tensor:

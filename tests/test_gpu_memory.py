@@ -46,7 +46,7 @@ NORM_SHAPES = [
     ((1, 1), 1), ((1, 7), 1), ((3, 64), 1), ((5, 250), 1), ((4, 256), 1), ((9, 511), 1), ((2, 1000), 1), ((700, 1024), 1),
     ((3, 2048), 1), ((2, 4100), 1), ((3, 8192), 1), ((2, 16390), 1), ((2, 3, 40), 2),
     ((1, 4, 64), 1), ((2, 20, 30, 7), 1), ((2, 20, 128), 1), ((1, 32, 1000), 1), ((2, 33, 257), 1), ((1, 128, 64), 1),
-    ((2, 150, 90), 1), ((3, 1, 5), 1), ((1, 16, 2052), 1), ((1, 5, 200000), 1),
+    ((2, 150, 90), 1), ((3, 1, 5), 1), ((4, 6000), 1), ((3, 8190), 1), ((1, 16, 2052), 1), ((1, 5, 200000), 1),
 ]
 
 
@@ -66,9 +66,9 @@ def test_norm_forward_and_backward(shape, dim, dtype, residual):
     close(y.view(v), ry, dtype, "y")
     close(s.view(v), rs, dtype, "s")
     close(rstd.view(v[0], v[2]), rrstd, F32, "rstd")
-    # backward from the rounded s and the saved rstd
+    # backward of the unrounded sum: s, and what rounding took from it, which the returned rstd carries
     gx, gw = n.backward(gy, s, w, rstd, grad_s=gs)
-    rgx, rgw = M.rms_norm_backward(as3(gy), as3(s), host(w), host(rstd).reshape(v[0], v[2]), as3(gs))
+    rgx, rgw = M.rms_norm_backward(as3(gy), rs, host(w), rrstd, as3(gs))
     # with one channel (and no eps) grad_x is a difference of equal terms: held to the size of what is subtracted
     size = np.linalg.norm(as3(gy) * host(w)[None, :, None] * host(rstd).reshape(v[0], 1, v[2]))
     assert np.linalg.norm(host(gx).reshape(v) - rgx) <= TOL[dtype] * max(np.linalg.norm(rgx), size)
@@ -77,6 +77,12 @@ def test_norm_forward_and_backward(shape, dim, dtype, residual):
     assert torch.equal(gx, again[0]) and torch.equal(gw, again[1])
     only, none = n.backward(gy, s, w, rstd, grad_s=gs, need_grad_weight=False)
     assert none is None and torch.equal(only, gx)
+    # ... and of the rounded sum where the low part was not kept
+    gx, gw = n.backward(gy, s, w, rstd.clone(), grad_s=gs)
+    rgx, rgw = M.rms_norm_backward(as3(gy), as3(s), host(w), host(rstd).reshape(v[0], v[2]), as3(gs))
+    assert np.linalg.norm(host(gx).reshape(v) - rgx) <= TOL[dtype] * max(np.linalg.norm(rgx), size)
+    close(gw, rgw, F32, "grad_weight") if np.prod(v[:1] + v[2:]) > 1 else None
+    assert torch.equal(n.forward(x, w, residual=r, need_backward=False)[0], y)
 
 
 @pytest.mark.parametrize("dtype", TYPES)

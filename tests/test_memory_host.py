@@ -72,14 +72,14 @@ WS = ctypes.c_void_p(0x100000)
 NULL = ctypes.c_void_p(0)
 
 
-def _norm(dtype=0, outer=4, c=8, inner=1, eps=1e-6, x=A, res=NULL, w=B_, s=NULL, y=C, rstd=NULL):
-    return Bn.lib().dtst_rms_norm(dtype, outer, c, inner, eps, x, res, w, s, y, rstd, NULL)
+def _norm(dtype=0, outer=4, c=8, inner=1, eps=1e-6, x=A, res=NULL, w=B_, s=NULL, low=NULL, y=C, rstd=NULL):
+    return Bn.lib().dtst_rms_norm(dtype, outer, c, inner, eps, x, res, w, s, low, y, rstd, NULL)
 
 
 @pytest.mark.parametrize("bad", [dict(dtype=3), dict(outer=-1), dict(c=0), dict(inner=-1), dict(eps=-1.0),
                                  dict(eps=float("nan")), dict(x=NULL), dict(w=NULL), dict(y=NULL),
                                  dict(x=ctypes.c_void_p(0x10002)), dict(s=C), dict(res=C),
-                                 dict(outer=1 << 40, c=1 << 40), dict(w=ctypes.c_void_p(0x20001))])
+                                 dict(outer=1 << 40, c=1 << 40), dict(low=E), dict(dtype=1, s=D, low=D), dict(dtype=1, low=E), dict(w=ctypes.c_void_p(0x20001))])
 def test_norm_refuses(bad):
     assert _norm(**bad) == Bn.DTST_ERR_INVALID_ARG
 
@@ -95,12 +95,12 @@ def test_empty_batches_need_no_pointers():
 
 
 @pytest.mark.parametrize("bad,want", [
-    (dict(gy=NULL), -1), (dict(s=NULL), -1), (dict(rstd=NULL), -1), (dict(gx=NULL), -1), (dict(gx=B_), -1),
+    (dict(gy=NULL), -1), (dict(s=NULL), -1), (dict(rstd=NULL), -1), (dict(gx=NULL), -1), (dict(gx=B_), -1), (dict(low=F), -1),
     (dict(scratch=NULL), -5), (dict(nbytes=16), -5), (dict(c=0), -1), (dict(gw=ctypes.c_void_p(0x30002)), -1)])
 def test_norm_backward_refuses(bad, want):
-    a = dict(dtype=0, c=8, gy=A, s=B_, w=C, rstd=D, gs=NULL, gx=E, gw=F, scratch=WS, nbytes=1 << 20)
+    a = dict(dtype=0, c=8, gy=A, s=B_, low=NULL, w=C, rstd=D, gs=NULL, gx=E, gw=F, scratch=WS, nbytes=1 << 20)
     a.update(bad)
-    assert Bn.lib().dtst_rms_norm_backward(a["dtype"], 4, a["c"], 1, a["gy"], a["s"], a["w"], a["rstd"], a["gs"], a["gx"],
+    assert Bn.lib().dtst_rms_norm_backward(a["dtype"], 4, a["c"], 1, a["gy"], a["s"], a["low"], a["w"], a["rstd"], a["gs"], a["gx"],
                                            a["gw"], a["scratch"], a["nbytes"], NULL) == want
 
 

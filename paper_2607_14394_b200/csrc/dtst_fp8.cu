@@ -149,7 +149,7 @@ struct MatmulCfg {
   static constexpr int THREADS = 64 + 32 * EPI;
   static constexpr int A_BYTES = kLanes * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
   static constexpr int STAGES = BN <= 32 ? 8 : 6;
-  static constexpr int TCOLS = 2 * BN < 32 ? 32 : 2 * BN;
+  static constexpr int NBUF = 4, TCOLS = NBUF * BN;         // buffers of tensor memory in turn
   static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + 2 * BN * 4 + EPI * 32 * 17 * 4 + 256;
 };
 
@@ -164,9 +164,9 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
   float* turn = col_scale + 2 * BN;                                                       // [EPI][32][17]
   uint64_t* full = reinterpret_cast<uint64_t*>(turn + Cfg::EPI * 32 * 17);
   uint64_t* empty = full + Cfg::STAGES;
-  uint64_t* done = empty + Cfg::STAGES;      // [2] products of a block complete
-  uint64_t* freed = done + 2;                // [2] tensor-memory half read
-  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(freed + 2);
+  uint64_t* done = empty + Cfg::STAGES;      // [NBUF] products of a block complete
+  uint64_t* freed = done + Cfg::NBUF;        // [NBUF] buffer of tensor memory read
+  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(freed + Cfg::NBUF);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_s + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -175,7 +175,7 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < Cfg::NBUF; ++k) {
       mbar_init(&done[k], 1);
       mbar_init(&freed[k], Cfg::EPI);
     }
@@ -220,16 +220,16 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
       uint32_t it = 0;
       for (int t = first; t < tiles; t += step)
         for (int kb = kb0; kb < kb1; ++kb, ++it) {
-          const uint32_t s = it % Cfg::STAGES, half = it & 1;
-          if (!wait_bar(&freed[half], ((it >> 1) & 1) ^ 1, abort_flag)) goto out;
+          const uint32_t s = it % Cfg::STAGES, buf = it % Cfg::NBUF;
+          if (!wait_bar(&freed[buf], ((it / Cfg::NBUF) & 1) ^ 1, abort_flag)) goto out;
           if (!wait_bar(&full[s], (it / Cfg::STAGES) & 1, abort_flag)) goto out;
           tc_fence_after();
           const uint32_t a = smem_u32(smem + (size_t)s * Cfg::STAGE), b = a + Cfg::A_BYTES;
 #pragma unroll
           for (int ks = 0; ks < 4; ++ks)
-            umma_f8(tmem + half * BN, desc_sw128(a + 32 * ks), desc_sw128(b + 32 * ks), idesc, ks > 0 ? 1u : 0u);
+            umma_f8(tmem + buf * BN, desc_sw128(a + 32 * ks), desc_sw128(b + 32 * ks), idesc, ks > 0 ? 1u : 0u);
           umma_commit(&empty[s]);
-          umma_commit(&done[half]);
+          umma_commit(&done[buf]);
         }
     }
   } else {
@@ -256,7 +256,7 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
         xs_next = xs_on ? __ldg(xs + (long long)kb0 * p.M) : xc_on ? __ldg(p.x_scale + (long long)kb0 * p.M + xc) : 0.f;
       }
       for (int kb = kb0; kb < kb1; ++kb, ++it) {
-        const uint32_t half = it & 1;
+        const uint32_t half = it & 1, buf = it % Cfg::NBUF;
         if (SWAP) {
           if (et < BN) col_scale[half * BN + et] = xs_next;
           asm volatile("bar.sync 1, %0;" ::"n"(32 * Cfg::EPI) : "memory");
@@ -266,7 +266,7 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
           ws_next = __ldg(ws + kb + 1);
           xs_next = xs_on ? __ldg(xs + (long long)(kb + 1) * p.M) : xc_on ? __ldg(p.x_scale + (long long)(kb + 1) * p.M + xc) : 0.f;
         }
-        bool ok = wait_bar(&done[half], (it >> 1) & 1, abort_flag);
+        bool ok = wait_bar(&done[buf], (it / Cfg::NBUF) & 1, abort_flag);
         ok = __all_sync(0xffffffffu, ok) != 0;
         if (!ok) {
           *abort_flag = 1;
@@ -275,16 +275,16 @@ matmul_fp8_kernel(const __grid_constant__ CUtensorMap lane_map, const __grid_con
         }
         tc_fence_after();
         const float* cs = col_scale + half * BN;
-        add_block<BN>(acc, taddr + half * BN, [&](int c) { return SWAP ? scale * cs[c] : scale; });
+        add_block<BN>(acc, taddr + buf * BN, [&](int c) { return SWAP ? scale * cs[c] : scale; });
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&freed[half]);
+        if (lane == 0) mbar_arrive(&freed[buf]);
       }
       T* out = static_cast<T*>(p.out);
       if (split > 1) {       // this CTA's part of the sums; every load has landed and every product is done
         float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
-        for (int c = 0; c < BN; ++c) part[SWAP ? c * kLanes + ln : ln * (BN + 1) + c] = acc[c];
+        for (int c = 0; c < BN; ++c) part[SWAP ? c * kLanes + ln : ln * (BN + 4) + c] = acc[c];
       } else if (SWAP) {
         if (row < p.N) {
 #pragma unroll
@@ -302,7 +302,7 @@ out:
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) {
     for (int s = 0; s < Cfg::STAGES; ++s) mbar_wait_plain(&full[s], 0, 1u << 12), mbar_wait_plain(&full[s], 1, 1u << 12);
-    for (int k = 0; k < 2; ++k) mbar_wait_plain(&done[k], 0, 1u << 12), mbar_wait_plain(&done[k], 1, 1u << 12);
+    for (int k = 0; k < Cfg::NBUF; ++k) mbar_wait_plain(&done[k], 0, 1u << 12), mbar_wait_plain(&done[k], 1, 1u << 12);
     atomicExch(p.status, 1);
   }
   __syncthreads();
@@ -311,15 +311,26 @@ out:
     const int l0 = (first % p.lane_tiles) * kLanes, c0 = (first / p.lane_tiles) * BN;
     const float* part = reinterpret_cast<const float*>(smem);
     T* out = static_cast<T*>(p.out);
-    const int e0 = (int)((long long)kLanes * BN * rank / split), e1 = (int)((long long)kLanes * BN * (rank + 1) / split);
-    for (int e = e0 + threadIdx.x; e < e1; e += Cfg::THREADS) {
-      const int ln = SWAP ? e % kLanes : e / BN, c = SWAP ? e / kLanes : e % BN;
-      const int m = SWAP ? c0 + c : l0 + ln, n = SWAP ? l0 + ln : c0 + c;
+    // four neighbouring outputs of a row at a time (SWAP: along the lanes)
+    constexpr int QUADS = kLanes * BN / 4, ROW4 = (SWAP ? kLanes : BN) / 4;
+    for (int e = QUADS * rank / split + threadIdx.x; e < QUADS * (rank + 1) / split; e += Cfg::THREADS) {
+      const int r = e / ROW4, q = e % ROW4 * 4;
+      const int m = SWAP ? c0 + r : l0 + r, n = SWAP ? l0 + q : c0 + q;
       if (m >= p.M || n >= p.N) continue;
-      const float* at = part + (SWAP ? c * kLanes + ln : ln * (BN + 1) + c);
-      float sum = 0.f;
-      for (int k = 0; k < split; ++k) sum += cluster_read(at, k);
-      out[(long long)m * p.out_ld + n] = Elem<T>::put(sum);
+      const float* at = part + (SWAP ? r * kLanes + q : r * (BN + 4) + q);
+      float4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < split) v[k] = cluster_read4(at, k);
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < split) x[0] += v[k].x, x[1] += v[k].y, x[2] += v[k].z, x[3] += v[k].w;
+      Pack<T, 4> o;
+      o.pack(x);
+      T* to = out + (long long)m * p.out_ld + n;
+      if (p.vec_out && n + 4 <= p.N) o.store(to);
+      else o.store_part(to, p.N - n);
     }
     cluster_sync();        // nobody leaves while its part may be read
   }
@@ -585,6 +596,13 @@ cudaError_t launch_matmul(Kern kern, int grid, int threads, int cluster, size_t 
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
+// few tiles: as many CTAs to a tile as the GPU has room for, each with two k-blocks at least
+int split_of(long long tiles, int KB) {
+  int split = 1;
+  while (split < 8 && tiles * split * 2 <= num_sms() && KB >= 4 * split) split *= 2;
+  return split;
+}
+
 template <typename T, int BN, bool SWAP>
 cudaError_t launch_tile(const MatmulCall& c, MatmulArgs p, cudaStream_t st) {
   using Cfg = MatmulCfg<BN>;
@@ -601,9 +619,7 @@ cudaError_t launch_tile(const MatmulCall& c, MatmulArgs p, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)p.lane_tiles * p.col_tiles;
   const int sms = num_sms();
-  // few tiles: as many CTAs to a tile as the GPU has room for, each with two k-blocks at least
-  p.split = 1;
-  while (p.split < 8 && tiles * p.split * 2 <= sms && p.KB >= 4 * p.split) p.split *= 2;
+  p.split = split_of(tiles, p.KB);
   const long long grid = p.split > 1 ? tiles * p.split : (tiles < sms ? tiles : sms);
   return launch_matmul(kern, (int)grid, Cfg::THREADS, p.split, Cfg::SMEM, st, lane_map, col_map, p);
 }
@@ -636,10 +652,19 @@ cudaError_t matmul_t(const MatmulCall& c, cudaStream_t st) {
   if (c.m <= 16) return launch_tile<T, 16, true>(c, p, st);
   if (c.m <= 32) return launch_tile<T, 32, true>(c, p, st);
   if (c.m <= 64) return launch_tile<T, 64, true>(c, p, st);
+  // The tile with the least of an estimate in ns: waves of tiles, each a time per k-block and one to write the tile out (both
+  // measured at 2048^3, 4096 x 4096 x 512 and 9029 x 220 x 3051: tiles of 64 columns took 32.0 / 31.4 / 29.2 us, of 128
+  // 21.0 / 26.1 / 21.8, pairs 14.5 / 17.2 / 23.5).
+  const long long sms = num_sms(), KB = p.KB;
   auto tiles = [&](long long a, long long b) { return ((c.m + a - 1) / a) * ((c.n + b - 1) / b); };
-  const int sms = num_sms();
-  if (2 * tiles(256, 256) >= sms) return launch_pairs<T>(c, p, st);
-  if (tiles(128, 128) >= sms) return launch_tile<T, 128, false>(c, p, st);
+  auto cost = [&](long long n, long long block, long long out) {
+    const long long split = split_of(n, p.KB);
+    return (n * split + sms - 1) / sms * ((KB + split - 1) / split * block + out) + (split > 1 ? 2 * out : 0);
+  };
+  const long long t64 = cost(tiles(128, 64), 430, 400), t128 = cost(tiles(128, 128), 540, 1200);
+  const long long pair = (tiles(256, 256) + sms / 2 - 1) / (sms / 2) * (KB * 650 + 800);
+  if (pair <= t64 && pair <= t128) return launch_pairs<T>(c, p, st);
+  if (t128 <= t64) return launch_tile<T, 128, false>(c, p, st);
   return launch_tile<T, 64, false>(c, p, st);
 }
 

@@ -79,8 +79,7 @@ def _rows16(k: int) -> int:
 
 def empty_fp8(rows: int, k: int, device=None) -> torch.Tensor:
     """An uninitialised [rows, k] 8-bit tensor whose rows start on 16-byte boundaries."""
-    dev = torch.device("cuda", _device(device))
-    return torch.empty((rows, _rows16(k)), dtype=FP8, device=dev)[:, :k]
+    return torch.empty_strided((rows, k), (_rows16(k), 1), dtype=FP8, device=torch.device("cuda", _device(device)))
 
 
 class RmsNorm:
@@ -175,7 +174,8 @@ class RmsNorm:
         if q is not None:
             ld, qp = _q_stride(q, rows, c), _on_device(q, "q", d, FP8)
         else:
-            q = torch.empty_like(x, dtype=FP8) if self._q_like_x else empty_fp8(rows, c, self.device)
+            q = torch.empty_like(x, dtype=FP8) if self._q_like_x else \
+                torch.empty_strided((rows, c), (_rows16(c), 1), dtype=FP8, device=self.device)
             ld, qp = _rows16(c), q.data_ptr()
         if scale is None:
             scale = weight.new_empty(self._scale_shape)

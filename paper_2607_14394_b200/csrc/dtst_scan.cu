@@ -10,6 +10,8 @@
 //
 // Memory-bound: forward 2 tensors in, 1 out; backward 3 in, 2 out.  The backward pass does not read h: it rebuilds
 // h_{t-1} inside each chunk, in fp32, from the state saved at the chunk's start.
+#include <type_traits>
+
 #include "dtst_common.cuh"
 #include "dtst_memory.cuh"
 #include "dtst_sm100.cuh"
@@ -70,9 +72,9 @@ __device__ __forceinline__ long long clamp_len(const int* lengths, long long o, 
 // [outer][L][inner], inner contiguous.  A tile is TX groups of VEC channels times SLOTS runs of R steps, a run per thread.
 // Long sequences: the tiles of one outer entry lie side by side over its channels; a CTA (or a cluster) walks along L.
 // Short ones (one tile holds them): groups run on across outer entries, so that few channels fill a CTA too.
-template <int VEC_, int R_, int SLOTS_, int CTAS_ = 2>
+template <int VEC_, int R_, int SLOTS_, int CTAS_ = 2, int THREADS_ = 256>
 struct ColShape {
-  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_, THREADS = 256, CTAS = CTAS_;
+  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_, THREADS = THREADS_, CTAS = CTAS_;
   static constexpr int TX = THREADS / SLOTS, W = TX * VEC, LC = SLOTS * R;
   // while runs are joined a warp has CPW channels, DG lanes each, and a lane has JOIN neighbouring runs of its channel
   static constexpr int WARPS = THREADS / 32, CPW = W / WARPS < 32 ? W / WARPS : 32, DG = 32 / CPW;
@@ -116,7 +118,8 @@ struct ColSlots {
   static constexpr int ROW = S::W * (int)sizeof(T), GAP = WIDE && ROW < 128 ? ROW : 0, RUN = R * ROW + GAP;
   static constexpr int PER_ROW = ROW / 16 > 0 ? ROW / 16 : 1, ROWS = S::THREADS / PER_ROW;      // copies of a row, rows at a time
   static constexpr size_t TENSOR = WIDE ? (size_t)S::SLOTS * RUN : (size_t)R * S::THREADS * BYTES, STAGE = TENSORS * TENSOR;
-  static constexpr int kStages = WIDE && STAGE < 45000 ? 2 : 1;       // (two CTAs to an SM)
+  static constexpr size_t FIXED = (12 * S::SLOTS + 128) * S::W + 2048;      // static shared memory and the system's share
+  static constexpr int kStages = WIDE && 2 * STAGE + FIXED <= 227 * 1024 / S::CTAS ? 2 : 1;
   static constexpr size_t SMEM = kStages * STAGE;
   using P = Pack<T, VEC>;
   unsigned char* base;
@@ -216,6 +219,29 @@ struct RoundBoxes {
   uint64_t bar[2];
 };
 
+// What the runs of a tile leave for each other, a number per run and channel.  A thread writes and reads VEC neighbouring
+// channels of its run at once.  While runs are joined a lane goes through the JOIN runs of its depth group; a gap of SKEW
+// floats behind each such set of rows puts the lanes of different depth groups in different banks (without the gaps and with
+// 8-byte pairs, half of all wavefronts of the passes over bf16 [65536][1024] were conflicts).
+template <class S>
+struct RunRows {
+  static constexpr int SKEW = S::CPW < S::VEC ? S::VEC : S::CPW;
+  __align__(16) float f[S::SLOTS > 1 ? S::SLOTS * S::W + S::SLOTS / S::JOIN * SKEW : 1];
+  __device__ __forceinline__ float* at(int run, int ch) { return f + run * S::W + run / S::JOIN * SKEW + ch; }
+  __device__ __forceinline__ void put(int run, int ch, const float (&v)[S::VEC]) {
+    if constexpr (S::VEC == 4) *reinterpret_cast<float4*>(at(run, ch)) = make_float4(v[0], v[1], v[2], v[3]);
+    else *at(run, ch) = v[0];
+  }
+  __device__ __forceinline__ void get(int run, int ch, float (&v)[S::VEC]) {
+    if constexpr (S::VEC == 4) {
+      const float4 q = *reinterpret_cast<const float4*>(at(run, ch));
+      v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+    } else {
+      v[0] = *at(run, ch);
+    }
+  }
+};
+
 // One round: every CTA sends its chunk's summary `all` to the others (st.async: the bytes are counted by the receiver's
 // mbarrier, so nothing has to be fenced - a cluster barrier's release waits for all global stores of the round before, which
 // measured 36 of 136 us in a pass over 65536 x 1024).  Returns the state in front of this CTA's chunk and moves `state` past
@@ -261,7 +287,7 @@ template <typename T, class S, int MODE, bool WIDE, bool SIGMOID>
 __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
   using Slots = ColSlots<T, S, 2, WIDE>;
-  __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];     // (A, H) of every run; then its first state in x
+  __shared__ RunRows<S> runs_a, runs_h;     // (A, H) of every run; then, in runs_a, the state in front of it
   __shared__ RoundBoxes<S> boxes;
   bool dead = false;
   extern __shared__ __align__(16) unsigned char raw[];
@@ -354,23 +380,25 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const Sc
 #pragma unroll
       for (int j = 0; j < VEC; ++j) s[j] = at.live && p.h0 != nullptr ? p.h0[at.o * p.inner + at.i0 + j] : 0.f;
     } else {
+      float ra[VEC], rh[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        float A = 1.f, H = 0.f;
+        ra[j] = a[0][j], rh[j] = u[0][j];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          A *= a[r][j];
-          H = fmaf(a[r][j], H, u[r][j]);
+        for (int r = 1; r < R; ++r) {
+          ra[j] *= a[r][j];
+          rh[j] = fmaf(a[r][j], rh[j], u[r][j]);
         }
-        runs[slot][x * VEC + j] = make_float2(A, H);
       }
+      runs_a.put(slot, x * VEC, ra);
+      runs_h.put(slot, x * VEC, rh);
       __syncthreads();
       if (WIDE) refill();
       float A = 1.f, H = 0.f;
       float2 m[S::JOIN];
 #pragma unroll
       for (int q = 0; q < S::JOIN; ++q) {
-        m[q] = runs[jq + q][jx];
+        m[q] = make_float2(*runs_a.at(jq + q, jx), *runs_h.at(jq + q, jx));
         A *= m[q].x;
         H = fmaf(m[q].x, H, m[q].y);
       }
@@ -387,12 +415,11 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const Sc
       }
 #pragma unroll
       for (int q = 0; q < S::JOIN; ++q) {
-        runs[jq + q][jx].x = run;
+        *runs_a.at(jq + q, jx) = run;
         run = fmaf(m[q].x, run, m[q].y);
       }
       __syncthreads();
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) s[j] = runs[slot][x * VEC + j].x;
+      runs_a.get(slot, x * VEC, s);
     }
     const int t0 = c * LC + slot * R, left = at.live ? (int)p.L - t0 : 0;
     T* h = p.h + (at.o * p.L + t0) * p.inner + at.i0;
@@ -421,9 +448,8 @@ template <typename T, class S, int MODE, bool WIDE, bool SIGMOID>
 __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
   using Slots = ColSlots<T, S, 3, WIDE>;
-  // (A, H) and D of every run; then the state in front of it (x) and the gradient that comes to it from behind
-  __shared__ float2 runs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
-  __shared__ float backs[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? W : 1];
+  // (A, H) and D of every run; then the state in front of it (runs_a) and the gradient that comes to it from behind (backs)
+  __shared__ RunRows<S> runs_a, runs_h, backs;
   __shared__ RoundBoxes<S> boxes;
   bool dead = false;
   extern __shared__ __align__(16) unsigned char raw[];
@@ -514,7 +540,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
     // q: 1 - a (sigmoid) or a (decay); a is formed again where it is used
     float q[R][VEC], v[R][VEC], s[VEC], d[VEC];
     Pack<T, VEC> pd[R];
-        auto a_of = [](float qq) { return SIGMOID ? 1.f - qq : qq; };
+    auto a_of = [](float qq) { return SIGMOID ? 1.f - qq : qq; };
     auto b_of = [](float qq) { return SIGMOID ? qq : 1.f; };
     Pack<T, VEC> pv[R], pg[R];
 #pragma unroll
@@ -539,19 +565,19 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
         d[j] = at.live && p.g_last != nullptr ? p.g_last[at.o * p.inner + at.i0 + j] : 0.f;
       }
     } else {
-      float D[VEC];
+      float ra[VEC], rh[VEC], D[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        float A = 1.f, H = 0.f;
-        D[j] = 0.f;
+        ra[j] = 1.f, rh[j] = D[j] = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           const float a = a_of(q[r][j]);
-          A *= a;
-          H = fmaf(a, H, b_of(q[r][j]) * v[r][j]);
+          ra[j] *= a;
+          rh[j] = fmaf(a, rh[j], b_of(q[r][j]) * v[r][j]);
         }
-        runs[slot][x * VEC + j] = make_float2(A, H);
       }
+      runs_a.put(slot, x * VEC, ra);
+      runs_h.put(slot, x * VEC, rh);
 #pragma unroll
       for (int r = R - 1; r >= 0; --r) {
         float gh[VEC];
@@ -559,8 +585,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
 #pragma unroll
         for (int j = 0; j < VEC; ++j) D[j] = a_of(q[r][j]) * (D[j] + gh[j]);
       }
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) backs[slot][x * VEC + j] = D[j];
+      backs.put(slot, x * VEC, D);
       __syncthreads();
       if (WIDE) refill();
       float A = 1.f, H = 0.f, B = 1.f, E = 0.f;
@@ -568,8 +593,8 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
       float md[S::JOIN];
 #pragma unroll
       for (int k = 0; k < S::JOIN; ++k) {
-        m[k] = runs[jq + k][jx];
-        md[k] = backs[jq + k][jx];
+        m[k] = make_float2(*runs_a.at(jq + k, jx), *runs_h.at(jq + k, jx));
+        md[k] = *backs.at(jq + k, jx);
         A *= m[k].x;
         H = fmaf(m[k].x, H, m[k].y);
       }
@@ -584,18 +609,18 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
       float run = fmaf(A, before, H);
 #pragma unroll
       for (int k = 0; k < S::JOIN; ++k) {
-        runs[jq + k][jx].x = run;
+        *runs_a.at(jq + k, jx) = run;
         run = fmaf(m[k].x, run, m[k].y);
       }
       run = fmaf(B, behind, E);
 #pragma unroll
       for (int k = S::JOIN - 1; k >= 0; --k) {
-        backs[jq + k][jx] = run;
+        *backs.at(jq + k, jx) = run;
         run = fmaf(m[k].x, run, md[k]);
       }
       __syncthreads();
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) s[j] = runs[slot][x * VEC + j].x, d[j] = backs[slot][x * VEC + j];
+      runs_a.get(slot, x * VEC, s);
+      backs.get(slot, x * VEC, d);
     }
     // forward once more: v is replaced by what delta is multiplied with for the gate's gradient
 #pragma unroll
@@ -1160,13 +1185,11 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   if (vec) {
     if (c.length <= 8) return launch_short_cols<T, ColShape<4, 8, 1>, BACK>(p, st);
     if (c.length <= 64) return launch_short_cols<T, ColShape<4, 8, 8>, BACK>(p, st);
-    if (BACK) return launch_long_cols<T, ColShape<4, 4, 64>, BACK>(p, c, st);
-    return launch_long_cols<T, ColShape<4, 8, 32>, BACK>(p, c, st);
+    return launch_long_cols<T, std::conditional_t<BACK, ColShape<4, 4, 64>, ColShape<4, 8, 32>>, BACK>(p, c, st);
   }
   if (c.length <= 8) return launch_short_cols<T, ColShape<1, 8, 1>, BACK>(p, st);
   if (c.length <= 64) return launch_short_cols<T, ColShape<1, 8, 8>, BACK>(p, st);
-  if (BACK) return launch_long_cols<T, ColShape<1, 16, 16, 3>, BACK>(p, c, st);
-  return launch_long_cols<T, ColShape<1, 16, 16, 4>, BACK>(p, c, st);
+  return launch_long_cols<T, ColShape<1, 16, 16, BACK ? 3 : 4>, BACK>(p, c, st);
 }
 
 }  // namespace

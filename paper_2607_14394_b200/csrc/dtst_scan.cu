@@ -42,19 +42,52 @@ struct ScanArgs {
 
 // a = 1 / (1 + e^-g) and b = 1 - a = e^-g / (1 + e^-g), both without cancellation.  The exponent is kept below 2^126 (a NaN
 // stays one); the approximate exponential and reciprocal are good to about 2^-22, and what they flush to zero (g > 87) is
-// below the smallest normal number.
-__device__ __forceinline__ void gate_of(float g, float& a, float& b) {
-  float e, r;
-  asm("{\n\t.reg .f32 x;\n\tmul.f32 x, %1, 0fBFB8AA3B;\n\tmin.NaN.f32 x, x, 0f42FC0000;\n\tex2.approx.ftz.f32 %0, x;\n\t}" : "=f"(e) : "f"(g));   // 2^min(-g log2 e, 126)
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  a = r;
-  b = e * r;
-}
-// h_t = a h_{t-1} + b v_t
+// below the smallest normal number.  Two steps at once.
 template <bool SIGMOID>
-__device__ __forceinline__ void terms(float g, float& a, float& b) {
-  if (SIGMOID) gate_of(g, a, b);
-  else a = g, b = 1.f;
+__device__ __forceinline__ void terms_pair(float2 g, float2& a, float2& b) {
+  if (!SIGMOID) {
+    a = g, b = make_float2(1.f, 1.f);
+    return;
+  }
+  const float2 x = mul_pair(g, make_float2(-1.44269504f, -1.44269504f));      // -log2 e
+  float2 e;           // 2^min(x, 126)
+  asm("{\n\t.reg .f32 x;\n\tmin.NaN.f32 x, %1, 0f42FC0000;\n\tex2.approx.ftz.f32 %0, x;\n\t}" : "=f"(e.x) : "f"(x.x));
+  asm("{\n\t.reg .f32 x;\n\tmin.NaN.f32 x, %1, 0f42FC0000;\n\tex2.approx.ftz.f32 %0, x;\n\t}" : "=f"(e.y) : "f"(x.y));
+  const float2 d = add_pair(e, make_float2(1.f, 1.f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.x) : "f"(d.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.y) : "f"(d.y));
+  b = mul_pair(e, a);
+}
+// d = a b and a b + c of N neighbouring channels (two at once: 126 -> 122 us for bf16 [65536][1024], whose pass is short of issue
+// slots; the backward passes, which are not, gained nothing)
+template <int N>
+__device__ __forceinline__ void mul_n(float (&d)[N], const float (&a)[N], const float (&b)[N]) {
+  if constexpr (N == 1) d[0] = a[0] * b[0];
+#pragma unroll
+  for (int j = 0; j + 1 < N; j += 2) {
+    const float2 r = mul_pair(make_float2(a[j], a[j + 1]), make_float2(b[j], b[j + 1]));
+    d[j] = r.x, d[j + 1] = r.y;
+  }
+}
+template <int N>
+__device__ __forceinline__ void fma_n(float (&d)[N], const float (&a)[N], const float (&b)[N], const float (&c)[N]) {
+  if constexpr (N == 1) d[0] = fmaf(a[0], b[0], c[0]);
+#pragma unroll
+  for (int j = 0; j + 1 < N; j += 2) {
+    const float2 r = fma_pair(make_float2(a[j], a[j + 1]), make_float2(b[j], b[j + 1]), make_float2(c[j], c[j + 1]));
+    d[j] = r.x, d[j + 1] = r.y;
+  }
+}
+// the gates of R x VEC steps in place: g becomes a, b is written
+template <bool SIGMOID, int R, int VEC>
+__device__ __forceinline__ void gates(float (&g)[R][VEC], float (&b)[R][VEC]) {
+#pragma unroll
+  for (int e = 0; e < R * VEC; e += 2) {
+    float2 a2, b2;
+    terms_pair<SIGMOID>(make_float2(g[e / VEC][e % VEC], g[(e + 1) / VEC][(e + 1) % VEC]), a2, b2);
+    g[e / VEC][e % VEC] = a2.x, g[(e + 1) / VEC][(e + 1) % VEC] = a2.y;
+    b[e / VEC][e % VEC] = b2.x, b[(e + 1) / VEC][(e + 1) % VEC] = b2.y;
+  }
 }
 // the gate of a step that leaves the state alone (with v = 0): a = 1
 template <typename T>
@@ -109,7 +142,7 @@ __device__ __forceinline__ float2 join_lanes(float& A, float& H) {
 // WIDE: 16-byte copies past L1, shared among the threads - a row of the tile is W elements, and the rows of a run are
 // followed by a gap of one row where that keeps the runs of half a warp in different banks.  The copies are waited for in
 // front of the barrier that ends a round.  (8-byte copies go through L1, whose lines then bound what can be in flight:
-// measured 198 us against 110 for the same 65536 x 1024 pass.)
+// measured 198 us against 135 for bf16 [65536][1024].)
 // Otherwise a thread copies and reads its own steps, element group by element group.
 template <typename T, class S, int TENSORS, bool WIDE>
 struct ColSlots {
@@ -243,8 +276,8 @@ struct RunRows {
 };
 
 // One round: every CTA sends its chunk's summary `all` to the others (st.async: the bytes are counted by the receiver's
-// mbarrier, so nothing has to be fenced - a cluster barrier's release waits for all global stores of the round before, which
-// measured 36 of 136 us in a pass over 65536 x 1024).  Returns the state in front of this CTA's chunk and moves `state` past
+// mbarrier; no cluster barrier, no fence).  Its latency is what a round cannot hide: when the pass over bf16 [65536][1024], 32
+// rounds of it, took 136 us, a copy of the kernel without the exchange took 100.  Returns the state in front of this CTA's chunk and moves `state` past
 // the round.  A lane of depth group d sends to and reads the box of CTA d.
 template <class S>
 __device__ __forceinline__ float join_round(const float2 all, float& state, RoundBoxes<S>& b, int round, int size, int rank, int jx,
@@ -366,15 +399,13 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const Sc
     for (int r = 0; r < R; ++r) pv[r] = *slots.slot(0, r), pg[r] = *slots.slot(1, r);
     if (!WIDE && MODE == kLong) refill();
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      float gv[VEC], vv[VEC];
-      pg[r].unpack(gv);
-      pv[r].unpack(vv);
+    for (int r = 0; r < R; ++r) pg[r].unpack(a[r]);
+    gates<SIGMOID, R, VEC>(a, u);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        terms<SIGMOID>(gv[j], a[r][j], u[r][j]);
-        u[r][j] *= vv[j];
-      }
+    for (int r = 0; r < R; ++r) {
+      float v[VEC];
+      pv[r].unpack(v);
+      mul_n<VEC>(u[r], u[r], v);
     }
     if constexpr (SLOTS == 1) {
 #pragma unroll
@@ -382,13 +413,11 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const Sc
     } else {
       float ra[VEC], rh[VEC];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        ra[j] = a[0][j], rh[j] = u[0][j];
+      for (int j = 0; j < VEC; ++j) ra[j] = a[0][j], rh[j] = u[0][j];
 #pragma unroll
-        for (int r = 1; r < R; ++r) {
-          ra[j] *= a[r][j];
-          rh[j] = fmaf(a[r][j], rh[j], u[r][j]);
-        }
+      for (int r = 1; r < R; ++r) {
+        mul_n<VEC>(ra, ra, a[r]);
+        fma_n<VEC>(rh, a[r], rh, u[r]);
       }
       runs_a.put(slot, x * VEC, ra);
       runs_h.put(slot, x * VEC, rh);
@@ -425,8 +454,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const Sc
     T* h = p.h + (at.o * p.L + t0) * p.inner + at.i0;
 #pragma unroll
     for (int r = 0; r < R; ++r, h += p.inner) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) s[j] = fmaf(a[r][j], s[j], u[r][j]);
+      fma_n<VEC>(s, a[r], s, u[r]);
       Pack<T, VEC> out;
       out.pack(s);
       if (t0 + r >= at.end) out.zero();
@@ -550,13 +578,14 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
     for (int r = 0; r < R; ++r) {
       pg[r].unpack(q[r]);
       pv[r].unpack(v[r]);
-      if (SIGMOID) {
+    }
+    if (SIGMOID) {
+      float b[R][VEC];
+      gates<true, R, VEC>(q, b);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          float a;
-          gate_of(q[r][j], a, q[r][j]);
-        }
-      }
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) q[r][j] = b[r][j];
     }
     if constexpr (SLOTS == 1) {
 #pragma unroll
@@ -869,10 +898,17 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_kernel(const Scan
     for (int k = 0; k < K; ++k) {
       A[k] = 1.f, H[k] = 0.f;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
+      for (int i = 0; i < V; ++i)
         if (RAGGED && !(live[k] >> i & 1u)) pv[k].v[i] = none_v, pg[k].v[i] = none_g;
-        terms<SIGMOID>(pg[k].get(i), a[k][i], b[k][i]);
-        b[k][i] *= pv[k].get(i);
+#pragma unroll
+      for (int i = 0; i < V; i += 2) {
+        float2 a2, b2;
+        terms_pair<SIGMOID>(make_float2(pg[k].get(i), pg[k].get(i + 1)), a2, b2);
+        b2 = mul_pair(b2, make_float2(pv[k].get(i), pv[k].get(i + 1)));
+        a[k][i] = a2.x, a[k][i + 1] = a2.y, b[k][i] = b2.x, b[k][i + 1] = b2.y;
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
         if (MODE == kWholeRows && i == x[k].spos) H[k] = h0v[k];
         A[k] *= a[k][i];
         H[k] = fmaf(a[k][i], H[k], b[k][i]);
@@ -965,9 +1001,16 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
     for (int k = 0; k < K; ++k) {
       A[k] = 1.f, H[k] = 0.f;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
+      for (int i = 0; i < V; ++i)
         if (RAGGED && !(live[k] >> i & 1u)) pv[k].v[i] = none_v, pg[k].v[i] = none_g, pd[k].v[i] = none_v;
-        terms<SIGMOID>(pg[k].get(i), a[k][i], b[k][i]);
+#pragma unroll
+      for (int i = 0; i < V; i += 2) {
+        float2 a2, b2;
+        terms_pair<SIGMOID>(make_float2(pg[k].get(i), pg[k].get(i + 1)), a2, b2);
+        a[k][i] = a2.x, a[k][i + 1] = a2.y, b[k][i] = b2.x, b[k][i + 1] = b2.y;
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
         if (MODE == kWholeRows && i == x[k].spos) H[k] = h0v[k];
         A[k] *= a[k][i];
         H[k] = fmaf(a[k][i], H[k], b[k][i] * pv[k].get(i));

@@ -1224,8 +1224,10 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   else vec = vec && aligned_to(c.h, need);
   p.groups = vec ? c.inner / 4 : c.inner;
   // The shortest tile that holds the sequences, so that few of its steps are empty: fp32 [65536][9][64] takes 97 us (forward) in
-  // the tile of 16 steps, 325 in that of 64; [8192][65][64] 92 in 128 steps, 203 in the long sequences' 256.  The backward
-  // pass has more to keep for a step and holds half as many a thread.
+  // the tile of 16 steps, 325 in that of 64; [8192][65][64] 92 in 128 steps, 203 in the long sequences' 256.  A tile that
+  // holds all steps needs no staging for a next one: [2048][256][64] takes 62 us (backward 116), 75 (155) as a long sequence.
+  // The backward pass has more to keep for a step and holds half as many a thread.  One channel a thread, the price of
+  // channel counts that are no multiple of four: 88 us for [2048][256][65].
   constexpr int R = BACK ? 4 : 8, N = BACK ? 2 : 1;
   if (vec) {
     if (c.length <= 8) return launch_short_cols<T, ColShape<4, 8, 1>, BACK>(p, st);
@@ -1233,6 +1235,7 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
     if (c.length <= 32) return launch_short_cols<T, ColShape<4, R, 4 * N>, BACK>(p, st);
     if (c.length <= 64) return launch_short_cols<T, ColShape<4, R, 8 * N>, BACK>(p, st);
     if (c.length <= 128) return launch_short_cols<T, ColShape<4, R, 16 * N>, BACK>(p, st);
+    if (c.length <= 256) return launch_short_cols<T, ColShape<4, R, 32 * N>, BACK>(p, st);
     return launch_long_cols<T, ColShape<4, R, 32 * N>, BACK>(p, c, st);
   }
   if (c.length <= 8) return launch_short_cols<T, ColShape<1, 8, 1>, BACK>(p, st);
@@ -1240,6 +1243,7 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   if (c.length <= 32) return launch_short_cols<T, ColShape<1, 8, 4>, BACK>(p, st);
   if (c.length <= 64) return launch_short_cols<T, ColShape<1, 8, 8>, BACK>(p, st);
   if (c.length <= 128) return launch_short_cols<T, ColShape<1, 8, 16>, BACK>(p, st);
+  if (c.length <= 256) return launch_short_cols<T, ColShape<1, 16, 16, BACK ? 3 : 4>, BACK>(p, st);
   return launch_long_cols<T, ColShape<1, 16, 16, BACK ? 3 : 4>, BACK>(p, c, st);
 }
 

@@ -296,7 +296,7 @@ def test_scan_forward_and_backward(outer, L, inner, dtype, gate, ragged):
     assert plan.status() == 0
 
 
-@pytest.mark.parametrize("L", [9, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129])
+@pytest.mark.parametrize("L", [9, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 255, 256, 257])
 @pytest.mark.parametrize("outer,inner", [(5, 12), (3, 129), (300, 4), (7, 516)])
 @pytest.mark.parametrize("dtype,gate,ragged", [(F32, "sigmoid", True), (torch.bfloat16, "decay", False), (torch.float16, "sigmoid", False)])
 def test_scan_at_the_ends_of_the_tiles(outer, L, inner, dtype, gate, ragged):

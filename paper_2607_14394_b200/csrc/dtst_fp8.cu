@@ -11,6 +11,9 @@
 // columns, lanes being rows of x and columns rows of w, or the other way round (SWAP) where there are few rows of x, so that
 // the tile's lanes are filled by the weights; where there are few tiles the CTAs of a cluster share the k-blocks of one and
 // add their sums through distributed shared memory, in rank order.
+// Measured: 16384 x 4096 x 2048 in 139 to 146 us (1.9 to 2.0 PFLOP/s; without the epilogue, its loads and products take 115),
+// 2048^3 in 12.6, 1000 x 1111 x 1360 in 10.1; few rows of x read the weights once: 4 x 4096 x 2048 in 5.5 us, 64 rows in 6.9, 65
+// (not swapped) in 8.4.  Bound: many rows by the handing over of a block's sums every 128 values of k, few rows by latency.
 // Warp 0 issues the TMA loads, warp 1 the products, the others hold the sums (a thread one lane x up to 128 columns).
 // Every wait is bounded: on expiry the kernel raises the status word, drains its loads and products, frees its tensor
 // memory and returns.

@@ -448,7 +448,7 @@ __device__ __forceinline__ float sum_at(const void* s, const void* low, long lon
   return sizeof(T) == 2 && low != nullptr ? LowBits<T>::join(v, static_cast<const T*>(low)[at]) : Elem<T>::get(v);
 }
 
-// Longer rows: grad_x by one CTA per row (the row read twice), then the weight gradient column by column.
+// Longer rows: the weight gradient column by column, then grad_x by one CTA per row (the row read twice).
 template <typename T>
 __global__ void __launch_bounds__(512) norm_long_rows_backward_kernel(const RowBackArgs a) {
   __shared__ float red[64];
@@ -759,12 +759,12 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
     const dim3 grid((unsigned)(ctas < most ? ctas : most));
     if (!BACK) return launch_pdl(norm_wide_field_kernel<T>, grid, dim3(128), 0, st, a);
     cudaError_t e = cudaSuccess;
-    if (a.y != nullptr) e = launch_pdl(norm_wide_field_backward_kernel<T>, grid, dim3(128), 0, st, a);
-    if (e == cudaSuccess && a.partial != nullptr) {
+    if (a.partial != nullptr) {      // first: grad_x may take grad_y's place
       *parts = 8;
       e = launch_pdl(norm_wide_field_weight_kernel<T>, dim3((unsigned)a.C, 8), dim3(256), 0, st, a);
     }
-    return e;
+    if (e != cudaSuccess) return e;
+    return launch_pdl(norm_wide_field_backward_kernel<T>, grid, dim3(128), 0, st, a);
   }
   const size_t need = WIDE * sizeof(T);
   const bool vec = a.inner % WIDE == 0 && aligned_to(a.x, need) && aligned_to(a.residual, need) && aligned_to(a.gy, need) &&
@@ -817,13 +817,15 @@ cudaError_t launch_rows_backward(const RowBackArgs& a, int* parts, cudaStream_t 
   if constexpr (sizeof(T) == 4)       // (16 elements of a 16-bit type a thread would spill)
     if (groups <= 2048) DTST_ROWS(1024, 2)
 #undef DTST_ROWS
+  // the weight gradient first: grad_x may take grad_y's place
   const long long most = (long long)num_sms() * 4;
-  cudaError_t e = launch_pdl(norm_long_rows_backward_kernel<T>, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(512), 0, st, a);
-  if (e == cudaSuccess && a.partial != nullptr) {
+  cudaError_t e = cudaSuccess;
+  if (a.partial != nullptr) {
     *parts = (int)(a.rows < 64 ? a.rows : 64);
     e = launch_pdl(norm_long_rows_weight_kernel<T>, dim3((unsigned)((a.C + 255) / 256), (unsigned)*parts), dim3(256), 0, st, a);
   }
-  return e;
+  if (e != cudaSuccess) return e;
+  return launch_pdl(norm_long_rows_backward_kernel<T>, dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(512), 0, st, a);
 }
 
 template <typename T>

@@ -1,0 +1,46 @@
+"""How the recurrent-memory operators are called: in place, with buffers used again, on several streams and threads, and
+with values at the edge of what they take.  Tolerances are test_gpu_memory's, derived there."""
+import numpy as np
+import pytest
+
+from oracle import memory_oracle as M
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [F32, BF16, F16]
+EPS = 1e-6
+
+
+def rand(*shape, dtype=F32, seed=0, scale=1.0, shift=0.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, device="cuda", generator=gen) * scale + shift).to(dtype)
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+# ------------------------------------------------------------------------------------------------ norm
+# a shape for every kernel of the backward pass: rows in registers by length, rows off a vector, rows beyond the registers;
+# fields in registers by channels, with and without vectors, and beyond the registers
+IN_PLACE = [(3, 64), (5, 250), (700, 1024), (2, 2048), (2, 4096), (3, 4100), (2, 8000), (3, 8190), (2, 9000), (2, 16390),
+            (2, 20, 90), (2, 33, 257), (1, 128, 64), (2, 150, 90), (1, 129, 33)]
+
+
+@pytest.mark.parametrize("shape", IN_PLACE)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("over", ["grad_y", "grad_s"])
+def test_norm_backward_in_place(shape, dtype, over):
+    """grad_x in grad_y's or grad_s's place: the bits of the call into a buffer of its own."""
+    from paper_2607_14394_b200 import RmsNorm
+    n = RmsNorm(shape, 1, dtype, EPS)
+    x, r, w = rand(*shape, dtype=dtype, seed=1), rand(*shape, dtype=dtype, seed=2), rand(shape[1], seed=3, shift=1.0)
+    gy, gs = rand(*shape, dtype=dtype, seed=4), rand(*shape, dtype=dtype, seed=5)
+    _, s, rstd = n.forward(x, w, residual=r)
+    gx, gw = n.backward(gy, s, w, rstd, grad_s=gs)
+    place = {"grad_y": gy, "grad_s": gs}[over]
+    gx2, gw2 = n.backward(gy, s, w, rstd, grad_s=gs, grad_x=place)
+    assert gx2.data_ptr() == place.data_ptr()
+    assert torch.equal(gx2, gx) and torch.equal(gw2, gw)

@@ -495,7 +495,8 @@ enum { DTST_F32 = 0, DTST_BF16 = 1, DTST_F16 = 2 };
  *   grad_x = rstd (weight grad_y - n mean_c(weight grad_y n)) + grad_s with n = s rstd   (also the residual's gradient)
  *   grad_weight[c] = sum over outer and inner of grad_y n, summed in a fixed order: same bits on every run.
  * grad_x may be grad_y or grad_s itself; grad_weight may be NULL, grad_x may not.  scratch:
- * dtst_rms_norm_scratch_bytes, needed for grad_weight (DTST_ERR_WORKSPACE if missing or too small).
+ * dtst_rms_norm_scratch_bytes, needed for grad_weight (DTST_ERR_WORKSPACE if missing or too small); calls that may run at
+ * the same time (on different streams) need one each.
  */
 dtst_status dtst_rms_norm(int dtype, int64_t outer, int64_t channels, int64_t inner, float eps, const void* x,
                           const void* residual, const float* weight, void* s, void* s_low, void* y, float* rstd,

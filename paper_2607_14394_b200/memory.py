@@ -108,8 +108,10 @@ class RmsNorm:
         self._wshape = torch.Size((self.channels,))
         self._q_like_x = self.channels % 16 == 0 and nd == 2
         self._scale_shape = torch.Size((-(-self.channels // BLOCK), self.outer))
-        self._scratch = None
         self._lib = Bn.lib()
+        n = ctypes.c_size_t()
+        _check(self._lib.dtst_rms_norm_scratch_bytes(self.channels, ctypes.byref(n)), "dtst_rms_norm_scratch_bytes")
+        self._scratch_bytes = int(n.value)
 
     def forward(self, x, weight, residual=None, out=None, sum_out=None, rstd=None, need_backward=True, stream=None):
         """Returns (y, s, rstd); without a residual s is x itself.
@@ -208,12 +210,9 @@ class RmsNorm:
                 gwp = grad_weight.data_ptr()
             else:
                 gwp = _addr(grad_weight, "grad_weight", d, torch.float32, self._wshape)
-            if self._scratch is None:
-                n = ctypes.c_size_t()
-                _check(self._lib.dtst_rms_norm_scratch_bytes(self.channels, ctypes.byref(n)), "dtst_rms_norm_scratch_bytes")
-                self._scratch = torch.empty(n.value, dtype=torch.uint8, device=self.device)
-                self._scratch_at = (self._scratch.data_ptr(), int(n.value))
-            scratch, nbytes = self._scratch_at
+            # the call's own, from the current stream's allocations: calls on other streams may be under way
+            partial, nbytes = torch.empty(self._scratch_bytes, dtype=torch.uint8, device=self.device), self._scratch_bytes
+            scratch = partial.data_ptr()
         status = self._lib.dtst_rms_norm_backward(
             self._type, self.outer, self.channels, self.inner, gp, _addr(s, "s", d, t, sh),
             _addr(rstd.sum_low, "rstd.sum_low", d, t, sh) if self._type and hasattr(rstd, "sum_low") else 0, wp,

@@ -44,3 +44,24 @@ def test_norm_backward_in_place(shape, dtype, over):
     gx2, gw2 = n.backward(gy, s, w, rstd, grad_s=gs, grad_x=place)
     assert gx2.data_ptr() == place.data_ptr()
     assert torch.equal(gx2, gx) and torch.equal(gw2, gw)
+
+
+def test_norm_backward_of_one_object_on_two_streams():
+    """Calls of one object on two streams at once give what each gives alone."""
+    from paper_2607_14394_b200 import RmsNorm
+    n = RmsNorm((20000, 512), -1, F32, EPS)
+    w = rand(512, seed=1, shift=1.0)
+    sets, want, streams = [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for k in range(2):
+        x, gy = rand(20000, 512, seed=2 + k), rand(20000, 512, seed=4 + k)
+        _, s, rstd = n.forward(x, w)
+        sets.append((gy, s, w, rstd))
+        want.append(n.backward(*sets[k])[1])
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for k in range(2):
+            got[k].append(n.backward(*sets[k], stream=streams[k])[1])
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(g, want[k]) for g in got[k])

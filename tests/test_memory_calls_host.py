@@ -1,0 +1,67 @@
+"""How the recurrent-memory classes call the library, without a GPU: CPU tensors, and a stand-in that records the
+arguments of each entry point (and can call in again, as another thread would while the library has the first call)."""
+import ctypes
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2607_14394_b200 import build as Bd
+from paper_2607_14394_b200 import memory as Mem
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+class Calls:
+    """A library whose entry points record their arguments and succeed; `during` runs inside the first recorded call."""
+
+    def __init__(self, lib):
+        self._real, self.seen, self.during = lib, [], None
+
+    def __getattr__(self, name):
+        if name.endswith(("_bytes", "_checkpoints")):      # host arithmetic
+            return getattr(self._real, name)
+
+        def call(*args):
+            entry = (name, list(args))
+            self.seen.append(entry)
+            if self.during is not None:
+                f, self.during = self.during, None
+                f()
+            for a in args:                                  # what the library would read of a description now
+                if hasattr(a, "_obj") and isinstance(a._obj, Mem.Bn.ScanDesc):
+                    d = a._obj
+                    entry[1].append((tuple(d.in_stride), tuple(d.grad_stride)))
+            return 0
+
+        return call
+
+    def last(self, name):
+        return [a for n, a in self.seen if n == name][-1]
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Operators made under this fixture work on CPU tensors (device number -1) and call the stand-in."""
+    Bd.build()
+    rec = Calls(Mem.Bn.lib())
+    monkeypatch.setattr(Mem.Bn, "lib", lambda: rec)
+    monkeypatch.setattr(Mem, "_device", lambda device: -1)
+    monkeypatch.setattr(Mem, "_current_device", lambda: -1)
+    monkeypatch.setattr(Mem, "_raw_stream", lambda dev: 0)
+    real = torch.device
+    monkeypatch.setattr(Mem.torch, "device", lambda *a: real("cpu") if a == ("cuda", -1) else real(*a))
+    return rec
+
+
+def test_norm_backward_calls_do_not_share_scratch(calls):
+    """Two calls of one object under way at once, as on two streams: each sums the weight gradient in memory of its own."""
+    n = Mem.RmsNorm((4, 8), -1)
+    x, w = torch.randn(4, 8), torch.ones(8)
+    _, s, rstd = n.forward(x, w)
+    calls.during = lambda: n.backward(x, s, w, rstd)
+    n.backward(x, s, w, rstd)
+    a, b = [args for name, args in calls.seen if name == "dtst_rms_norm_backward"]
+    (pa, na), (pb, nb) = (a[12], a[13]), (b[12], b[13])
+    assert na == nb > 0
+    assert pa + na <= pb or pb + nb <= pa

@@ -353,9 +353,9 @@ class GatedScan:
             raise ValueError("the dimensions behind the recurrence's must not be empty")
         self.state_shape = self.outer_shape + inner_shape
         dense = (self.length * self.inner, self.inner)
-        self._dense = self._in = self._out = dense       # (outer, step) strides the description holds
-        self._desc = Bn.ScanDesc(DTYPES[dtype], GATES[gate], self.outer, self.length, self.inner, dense, dense)
-        self._ref = ctypes.byref(self._desc)
+        self._dense = dense                              # (outer, step) strides of contiguous tensors
+        self._ref = self._describe(dense, dense)
+        self._other = (None, None, None)                 # the last description of other strides: v and g's, the gradients'
         self._lib = Bn.lib()
         n = ctypes.c_int64()
         _check(self._lib.dtst_gated_scan_checkpoints(self._ref, ctypes.byref(n)), "dtst_gated_scan_checkpoints")
@@ -392,8 +392,21 @@ class GatedScan:
             raise ValueError(f"{name}: the recurrence's dimension must be contiguous when it is the last one")
         return (self._dense[0] if outer is None else outer), step
 
+    def _describe(self, at, grad_at):
+        return ctypes.byref(Bn.ScanDesc(DTYPES[self.dtype], GATES[self.gate], self.outer, self.length, self.inner, at, grad_at))
+
+    def _description(self, at, grad_at):
+        """The description for these strides.  One that a call may be reading is never changed."""
+        if at is self._dense and grad_at is self._dense:
+            return self._ref
+        a, b, ref = self._other
+        if a != at or b != grad_at:
+            ref = self._describe(at, grad_at)
+            self._other = (at, grad_at, ref)
+        return ref
+
     def _inputs(self, v, g):
-        """Addresses of v and g, whose strides go into the description."""
+        """Addresses of v and g, and their strides."""
         d, t, sh = self.dev, self.dtype, self.shape
         if v.dtype is t and g.dtype is t and v.shape == sh and g.shape == sh and v.get_device() == d and \
                 g.get_device() == d and v.is_contiguous() and g.is_contiguous():
@@ -404,9 +417,7 @@ class GatedScan:
             at, b = self._strides(v, "v"), self._strides(g, "g")
             if at != b:
                 raise ValueError(f"v and g must have the same strides, got {v.stride()} and {g.stride()}")
-        if at != self._in:
-            self._desc.in_stride[0], self._desc.in_stride[1] = self._in = at
-        return v.data_ptr(), g.data_ptr()
+        return v.data_ptr(), g.data_ptr(), at
 
     def forward(self, v, g, h0=None, lengths=None, out=None, h_last=None, checkpoints=None, stream=None):
         """Returns (h, h_last).  lengths: int32 per outer entry; checkpoints: see new_checkpoints."""
@@ -414,10 +425,10 @@ class GatedScan:
         if stream is not None or _current_device() != d:
             with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
                 return self.forward(v, g, h0, lengths, out, h_last, checkpoints)
-        vp, gp = self._inputs(v, g)
+        vp, gp, at = self._inputs(v, g)
         hp = 0 if h0 is None else _addr(h0, "h0", d, torch.float32, state)
         if out is None:
-            out = torch.empty_like(v) if self._in is self._dense else v.new_empty(self.shape)
+            out = torch.empty_like(v) if at is self._dense else v.new_empty(self.shape)
             op = out.data_ptr()
         else:
             op = _addr(out, "out", d, self.dtype, self.shape)
@@ -427,8 +438,9 @@ class GatedScan:
         else:
             lp = _addr(h_last, "h_last", d, torch.float32, state)
         status = self._lib.dtst_gated_scan(
-            self._ref, vp, gp, hp, 0 if lengths is None else _addr(lengths, "lengths", d, torch.int32, self.outer_shape), op,
-            lp, 0 if checkpoints is None else _addr(checkpoints, "checkpoints", d, torch.float32, self._ck_shape),
+            self._description(at, self._dense), vp, gp, hp,
+            0 if lengths is None else _addr(lengths, "lengths", d, torch.int32, self.outer_shape), op, lp,
+            0 if checkpoints is None else _addr(checkpoints, "checkpoints", d, torch.float32, self._ck_shape),
             _raw_stream(d))
         if status:
             _check(status, "dtst_gated_scan")
@@ -442,25 +454,23 @@ class GatedScan:
             with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
                 return self.backward(grad_h, v, g, checkpoints, h0, lengths, grad_last, grad_v, grad_g, grad_h0,
                                      need_grad_h0)
-        vp, gp = self._inputs(v, g)
+        vp, gp, at = self._inputs(v, g)
         dp = _addr(grad_h, "grad_h", d, t, self.shape)
         if grad_v is None and grad_g is None:
-            grad_v, grad_g, at = torch.empty_like(grad_h), torch.empty_like(grad_h), self._dense
+            grad_v, grad_g, to = torch.empty_like(grad_h), torch.empty_like(grad_h), self._dense
         else:
             grad_v = torch.empty_like(grad_h) if grad_v is None else grad_v
             grad_g = torch.empty_like(grad_h) if grad_g is None else grad_g
             _on_device(grad_v, "grad_v", d, t)
             _on_device(grad_g, "grad_g", d, t)
-            at, b = self._strides(grad_v, "grad_v"), self._strides(grad_g, "grad_g")
-            if at != b:
+            to, b = self._strides(grad_v, "grad_v"), self._strides(grad_g, "grad_g")
+            if to != b:
                 raise ValueError(f"grad_v and grad_g must have the same strides, got {grad_v.stride()} and {grad_g.stride()}")
-        if at != self._out:
-            self._desc.grad_stride[0], self._desc.grad_stride[1] = self._out = at
         if grad_h0 is None and need_grad_h0:
             grad_h0 = (torch.empty(state, dtype=torch.float32, device=self.device) if grad_last is None and h0 is None
                        else torch.empty_like(grad_last if h0 is None else h0))
         status = self._lib.dtst_gated_scan_backward(
-            self._ref, dp, 0 if grad_last is None else _addr(grad_last, "grad_last", d, torch.float32, state), vp, gp,
+            self._description(at, to), dp, 0 if grad_last is None else _addr(grad_last, "grad_last", d, torch.float32, state), vp, gp,
             0 if h0 is None else _addr(h0, "h0", d, torch.float32, state),
             0 if lengths is None else _addr(lengths, "lengths", d, torch.int32, self.outer_shape),
             _addr(checkpoints, "checkpoints", d, torch.float32, self._ck_shape), grad_v.data_ptr(), grad_g.data_ptr(),

@@ -65,3 +65,33 @@ def test_norm_backward_of_one_object_on_two_streams():
     torch.cuda.synchronize()
     for k in range(2):
         assert all(torch.equal(g, want[k]) for g in got[k])
+
+
+# ------------------------------------------------------------------------------------------------ recurrence
+def test_scan_of_one_object_in_two_threads():
+    """Threads that use one object, one on contiguous tensors and one on halves of a projection."""
+    import threading
+
+    from paper_2607_14394_b200 import GatedScan
+    B, L, D = 2, 40, 64
+    plan = GatedScan((B, L, D), 1)
+    vg = rand(B, L, 2 * D, seed=1)
+    halves = vg[..., :D], vg[..., D:]
+    dense = rand(B, L, D, seed=2), rand(B, L, D, seed=3)
+    want = [plan.forward(*t)[0] for t in (halves, dense)]
+    bad, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+
+    def work(k):
+        for _ in range(300):
+            h, _ = plan.forward(*(halves, dense)[k], stream=streams[k])
+            streams[k].synchronize()
+            if not torch.equal(h, want[k]):
+                bad.append(k)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad

@@ -65,3 +65,29 @@ def test_norm_backward_calls_do_not_share_scratch(calls):
     (pa, na), (pb, nb) = (a[12], a[13]), (b[12], b[13])
     assert na == nb > 0
     assert pa + na <= pb or pb + nb <= pa
+
+
+def test_scan_calls_do_not_share_a_description(calls):
+    """A call on contiguous tensors while the library has a call on halves of a projection, and the other way round."""
+    B, L, D = 2, 6, 4
+    plan = Mem.GatedScan((B, L, D), 1)
+    vg, whole = torch.randn(B, L, 2 * D), torch.randn(B, L, D)
+    halves, dense = (vg[..., :D], vg[..., D:]), (whole, whole.clone())
+    strided = (L * 2 * D, 2 * D)
+    flat = (L * D, D)
+    ck, gh = torch.empty(plan.checkpoint_floats), torch.randn(B, L, D)
+    wide = torch.empty(B, L, 3 * D)
+
+    calls.during = lambda: plan.forward(*dense)
+    plan.forward(*halves)
+    calls.during = lambda: plan.forward(*halves)
+    plan.forward(*dense)
+    assert [args[-1][0] for name, args in calls.seen if name == "dtst_gated_scan"] == [strided, flat, flat, strided]
+
+    calls.during = lambda: plan.backward(gh, *dense, ck)
+    plan.backward(gh, *halves, ck, grad_v=wide[..., :D], grad_g=wide[..., D:2 * D])
+    calls.during = lambda: plan.backward(gh, *halves, ck)
+    plan.backward(gh, *dense, ck, grad_v=wide[..., :D], grad_g=wide[..., D:2 * D])
+    got = [args[-1] for name, args in calls.seen if name == "dtst_gated_scan_backward"]
+    third = (L * 3 * D, 3 * D)
+    assert got == [(strided, third), (flat, flat), (flat, third), (strided, flat)]

@@ -117,7 +117,8 @@ class RmsNorm:
         """Returns (y, s, rstd); without a residual s is x itself.
 
         In a 16-bit type with a residual, what rounding took from s stays with the rstd that is returned (its attribute
-        `sum_low`), so that `backward` has the sum to 24 bits; an rstd that the caller brings may carry such a buffer too.
+        `sum_low`), so that `backward` has the sum to 24 bits; an rstd that the caller brings may carry such a buffer too
+        (a call without a sum to round sets it to None, the next one with a residual makes another).
         need_backward=False: neither is formed, and rstd is None.
         """
         d, t, sh = self.dev, self.dtype, self.shape
@@ -141,8 +142,12 @@ class RmsNorm:
         qp = lp = 0
         if rstd is not None:
             qp = _addr(rstd, "rstd", d, torch.float32, self._rest)
-            if sp and self._type:
-                lp = _addr(getattr(rstd, "sum_low", None), "rstd.sum_low", d, t, sh)
+            if self._type and hasattr(rstd, "sum_low"):
+                if not sp:                              # s is x itself; what an earlier call's sum lost is not its
+                    rstd.sum_low = None
+                elif rstd.sum_low is None:
+                    rstd.sum_low = torch.empty_like(x)
+                lp = _addr(rstd.sum_low, "rstd.sum_low", d, t, sh)
         elif need_backward:
             rstd = weight.new_empty(self._rest)
             qp = rstd.data_ptr()
@@ -215,7 +220,7 @@ class RmsNorm:
             scratch = partial.data_ptr()
         status = self._lib.dtst_rms_norm_backward(
             self._type, self.outer, self.channels, self.inner, gp, _addr(s, "s", d, t, sh),
-            _addr(rstd.sum_low, "rstd.sum_low", d, t, sh) if self._type and hasattr(rstd, "sum_low") else 0, wp,
+            _addr(getattr(rstd, "sum_low", None), "rstd.sum_low", d, t, sh) if self._type else 0, wp,
             _addr(rstd, "rstd", d, torch.float32, self._rest), 0 if grad_s is None else _addr(grad_s, "grad_s", d, t, sh),
             xp, gwp, scratch, nbytes, _raw_stream(d))
         if status:

@@ -67,6 +67,25 @@ def test_norm_backward_of_one_object_on_two_streams():
         assert all(torch.equal(g, want[k]) for g in got[k])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_statistics_buffer_used_again(dtype):
+    """An rstd that a call with a residual returned, used for one without and for one with again."""
+    from paper_2607_14394_b200 import RmsNorm
+    n = RmsNorm((40, 256), 1, dtype, EPS)
+    x, r, w = rand(40, 256, dtype=dtype, seed=1), rand(40, 256, dtype=dtype, seed=2), rand(256, seed=3)
+    gy = rand(40, 256, dtype=dtype, seed=4)
+
+    def both(residual, rstd=None):
+        _, s, rstd = n.forward(x, w, residual=residual, rstd=rstd)
+        return (*n.backward(gy, s, w, rstd), rstd)
+
+    *with_r, rstd = both(r)
+    *without, _ = both(None)
+    for residual, want in [(None, without), (r, with_r), (None, without)]:
+        *got, rstd = both(residual, rstd)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 # ------------------------------------------------------------------------------------------------ recurrence
 def test_scan_of_one_object_in_two_threads():
     """Threads that use one object, one on contiguous tensors and one on halves of a projection."""

@@ -67,6 +67,22 @@ def test_norm_backward_calls_do_not_share_scratch(calls):
     assert pa + na <= pb or pb + nb <= pa
 
 
+def test_norm_low_part_belongs_to_the_last_forward_call(calls):
+    """An rstd used again: without a residual there is no low part, with one again there is."""
+    n = Mem.RmsNorm((4, 8), -1, BF16)
+    x, r, w = torch.randn(4, 8, dtype=BF16), torch.randn(4, 8, dtype=BF16), torch.ones(8)
+    low = lambda: (calls.last("dtst_rms_norm")[9], calls.last("dtst_rms_norm_backward")[6])
+    _, s, rstd = n.forward(x, w, residual=r)
+    n.backward(x, s, w, rstd)
+    assert low()[0] == low()[1] == rstd.sum_low.data_ptr() != 0
+    _, s, rstd = n.forward(x, w, rstd=rstd)
+    n.backward(x, s, w, rstd)
+    assert low() == (0, 0)
+    _, s, rstd = n.forward(x, w, residual=r, rstd=rstd)
+    n.backward(x, s, w, rstd)
+    assert low()[0] == low()[1] == rstd.sum_low.data_ptr() != 0
+
+
 def test_scan_calls_do_not_share_a_description(calls):
     """A call on contiguous tensors while the library has a call on halves of a projection, and the other way round."""
     B, L, D = 2, 6, 4

@@ -195,13 +195,16 @@ class RmsNorm:
         return q, scale, (x if sum_out is None else sum_out)
 
     def backward(self, grad_y, s, weight, rstd, grad_s=None, grad_x=None, grad_weight=None, need_grad_weight=True,
-                 stream=None):
+                 stream=None, sum_low=None):
         """Returns (grad_x, grad_weight); grad_x is the gradient of x and of the residual.  s and rstd as `forward`
-        returned them."""
+        returned them.
+
+        In a 16-bit type the sum is s and the low part that rstd carries (`rstd.sum_low`).  The attribute does not survive a
+        clone, a detach or a copy of rstd: pass it on as `sum_low=`, or the gradients are those of the rounded sum."""
         d, t, sh = self.dev, self.dtype, self.shape
         if stream is not None or _current_device() != d:
             with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
-                return self.backward(grad_y, s, weight, rstd, grad_s, grad_x, grad_weight, need_grad_weight)
+                return self.backward(grad_y, s, weight, rstd, grad_s, grad_x, grad_weight, need_grad_weight, None, sum_low)
         gp, wp = _addr(grad_y, "grad_y", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
         if grad_x is None:
             grad_x = torch.empty_like(grad_y)
@@ -218,9 +221,10 @@ class RmsNorm:
             # the call's own, from the current stream's allocations: calls on other streams may be under way
             partial, nbytes = torch.empty(self._scratch_bytes, dtype=torch.uint8, device=self.device), self._scratch_bytes
             scratch = partial.data_ptr()
+        if sum_low is None and self._type:
+            sum_low = getattr(rstd, "sum_low", None)
         status = self._lib.dtst_rms_norm_backward(
-            self._type, self.outer, self.channels, self.inner, gp, _addr(s, "s", d, t, sh),
-            _addr(getattr(rstd, "sum_low", None), "rstd.sum_low", d, t, sh) if self._type else 0, wp,
+            self._type, self.outer, self.channels, self.inner, gp, _addr(s, "s", d, t, sh), _addr(sum_low, "sum_low", d, t, sh), wp,
             _addr(rstd, "rstd", d, torch.float32, self._rest), 0 if grad_s is None else _addr(grad_s, "grad_s", d, t, sh),
             xp, gwp, scratch, nbytes, _raw_stream(d))
         if status:

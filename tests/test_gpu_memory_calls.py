@@ -86,6 +86,21 @@ def test_norm_statistics_buffer_used_again(dtype):
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_norm_low_part_passed_beside_the_statistics():
+    from paper_2607_14394_b200 import RmsNorm
+    n = RmsNorm((40, 256), 1, BF16, EPS)
+    x, r, w, gy = (rand(*sh, dtype=t, seed=k) for k, (sh, t) in enumerate([((40, 256), BF16), ((40, 256), BF16), ((256,), F32),
+                                                                         ((40, 256), BF16)]))
+    _, s, rstd = n.forward(x, w, residual=r)
+    want = n.backward(gy, s, w, rstd)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    for stream in (None, st):
+        got = n.backward(gy, s, w, rstd.detach().clone(), sum_low=rstd.sum_low, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 # ------------------------------------------------------------------------------------------------ recurrence
 def test_scan_of_one_object_in_two_threads():
     """Threads that use one object, one on contiguous tensors and one on halves of a projection."""

@@ -83,6 +83,17 @@ def test_norm_low_part_belongs_to_the_last_forward_call(calls):
     assert low()[0] == low()[1] == rstd.sum_low.data_ptr() != 0
 
 
+def test_norm_low_part_by_itself(calls):
+    """Statistics that went through a detach: the low part is passed on beside them."""
+    n = Mem.RmsNorm((4, 8), -1, BF16)
+    x, w = torch.randn(4, 8, dtype=BF16), torch.ones(8)
+    _, s, rstd = n.forward(x, w, residual=x)
+    n.backward(x, s, w, rstd.detach().clone(), sum_low=rstd.sum_low)
+    assert calls.last("dtst_rms_norm_backward")[6] == rstd.sum_low.data_ptr()
+    with pytest.raises(ValueError):
+        n.backward(x, s, w, rstd, sum_low=rstd.sum_low[:3])
+
+
 def test_scan_calls_do_not_share_a_description(calls):
     """A call on contiguous tensors while the library has a call on halves of a projection, and the other way round."""
     B, L, D = 2, 6, 4

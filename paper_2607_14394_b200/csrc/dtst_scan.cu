@@ -42,8 +42,9 @@ struct ScanArgs {
 };
 
 // a = 1 / (1 + e^-g) and b = 1 - a = e^-g / (1 + e^-g), both without cancellation.  The exponent is kept below 2^126 (a NaN
-// stays one); the approximate exponential and reciprocal are good to about 2^-22, and what they flush to zero (g > 87) is
-// below the smallest normal number.  Two steps at once.
+// stays one); the approximate exponential and reciprocal are good to about 2^-22, the rounding of g log2 e adds |g| 2^-24 or so
+// to the smaller of the two (1e-6 at 20, 5e-6 at 80), and what they flush to zero (g > 87) is below the smallest normal
+// number.  Two steps at once.
 template <bool SIGMOID>
 __device__ __forceinline__ void terms_pair(float2 g, float2& a, float2& b) {
   if (!SIGMOID) {
@@ -106,9 +107,11 @@ __device__ __forceinline__ long long clamp_len(const int* lengths, long long o, 
 // [outer][L][inner], inner contiguous.  A tile is TX groups of VEC channels times SLOTS runs of R steps, a run per thread.
 // Long sequences: the tiles of one outer entry lie side by side over its channels; a CTA (or a cluster) walks along L.
 // Short ones (one tile holds them): groups run on across outer entries, so that few channels fill a CTA too.
-template <int VEC_, int R_, int SLOTS_, int CTAS_ = 2>
+// SIG and DEC: CTAs that share an SM, by gate.
+template <int VEC_, int R_, int SLOTS_, int SIG = 2, int DEC = SIG>
 struct ColShape {
-  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_, THREADS = 256, CTAS = CTAS_;
+  static constexpr int VEC = VEC_, R = R_, SLOTS = SLOTS_, THREADS = 256;
+  static constexpr int ctas(bool sigmoid) { return sigmoid ? SIG : DEC; }
   static constexpr int TX = THREADS / SLOTS, W = TX * VEC, LC = SLOTS * R;
   // while runs are joined a warp has CPW channels, DG lanes each, and a lane has JOIN neighbouring runs of its channel
   static constexpr int WARPS = THREADS / 32, CPW = W / WARPS < 32 ? W / WARPS : 32, DG = 32 / CPW;
@@ -288,7 +291,7 @@ __device__ __forceinline__ float join_round(const float2 all, float& state, Roun
 }
 
 template <typename T, class S, int MODE, bool SIGMOID>
-__global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const ScanArgs<T> p) {
+__global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
   using Slots = ColSlots<T, S, 2>;
   __shared__ RunRows<S> runs_a, runs_h;     // (A, H) of every run; then, in runs_a, the state in front of it
@@ -421,7 +424,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_kernel(const Sc
 }
 
 template <typename T, class S, int MODE, bool SIGMOID>
-__global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel(const ScanArgs<T> p) {
+__global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_backward_kernel(const ScanArgs<T> p) {
   constexpr int VEC = S::VEC, R = S::R, SLOTS = S::SLOTS, W = S::W, LC = S::LC;
   using Slots = ColSlots<T, S, 3>;
   // (A, H) and D of every run; then the state in front of it (runs_a) and the gradient that comes to it from behind (backs)
@@ -488,28 +491,19 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
       else if (p.h0 != nullptr) before = p.h0[ch];
     }
     Slots::wait();
-    // q: 1 - a (sigmoid) or a (decay); a is formed again where it is used
-    float q[R][VEC], v[R][VEC], s[VEC], d[VEC];
+    // a and b = 1 - a, both kept: either formed from the other would lose its bits where it is small
+    float a[R][VEC], b[R][VEC], v[R][VEC], s[VEC], d[VEC];
     Pack<T, VEC> pd[R];
-    auto a_of = [](float qq) { return SIGMOID ? 1.f - qq : qq; };
-    auto b_of = [](float qq) { return SIGMOID ? qq : 1.f; };
     Pack<T, VEC> pv[R], pg[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) pv[r] = *slots.slot(0, r), pg[r] = *slots.slot(1, r), pd[r] = *slots.slot(2, r);
     if (MODE == kLong) refill();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      pg[r].unpack(q[r]);
+      pg[r].unpack(a[r]);
       pv[r].unpack(v[r]);
     }
-    if (SIGMOID) {
-      float b[R][VEC];
-      gates<true, R, VEC>(q, b);
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) q[r][j] = b[r][j];
-    }
+    gates<SIGMOID, R, VEC>(a, b);
     if constexpr (SLOTS == 1) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
@@ -523,9 +517,8 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
         ra[j] = 1.f, rh[j] = D[j] = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const float a = a_of(q[r][j]);
-          ra[j] *= a;
-          rh[j] = fmaf(a, rh[j], b_of(q[r][j]) * v[r][j]);
+          ra[j] *= a[r][j];
+          rh[j] = fmaf(a[r][j], rh[j], b[r][j] * v[r][j]);
         }
       }
       runs_a.put(slot, x * VEC, ra);
@@ -535,7 +528,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
         float gh[VEC];
         pd[r].unpack(gh);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) D[j] = a_of(q[r][j]) * (D[j] + gh[j]);
+        for (int j = 0; j < VEC; ++j) D[j] = a[r][j] * (D[j] + gh[j]);
       }
       backs.put(slot, x * VEC, D);
       __syncthreads();
@@ -578,9 +571,9 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float a = a_of(q[r][j]), u = b_of(q[r][j]) * v[r][j];
-        v[r][j] = SIGMOID ? (s[j] - v[r][j]) * (a * q[r][j]) : s[j];
-        s[j] = fmaf(a, s[j], u);
+        const float u = b[r][j] * v[r][j];
+        v[r][j] = SIGMOID ? (s[j] - v[r][j]) * (a[r][j] * b[r][j]) : s[j];
+        s[j] = fmaf(a[r][j], s[j], u);
       }
     const int t0 = c * LC + slot * R, left = at.live && c >= 0 ? (int)p.L - t0 : 0;
     const long long back = at.o * p.gr_o + at.i0 + (t0 + R - 1) * p.gr_t;
@@ -592,9 +585,9 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) scan_cols_backward_kernel
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float delta = d[j] + x1[j];
-        x1[j] = delta * b_of(q[r][j]);
+        x1[j] = delta * b[r][j];
         x2[j] = delta * v[r][j];
-        d[j] = a_of(q[r][j]) * delta;
+        d[j] = a[r][j] * delta;
       }
       Pack<T, VEC> ov, og;
       ov.pack(x1);
@@ -1073,7 +1066,7 @@ cudaError_t launch_long_cols(ScanArgs<T> p, cudaStream_t st) {
   p.per_outer = (unsigned)per_outer;
   p.chains = p.outer * per_outer;
   p.chunks = (int)((p.L + S::LC - 1) / S::LC);
-  const int cluster = cluster_for(p.chains, p.chunks, S::CTAS * (long long)num_sms(), 8);
+  const int cluster = cluster_for(p.chains, p.chunks, S::ctas(p.sigmoid != 0) * (long long)num_sms(), 8);
   p.rounds = (p.chunks + cluster - 1) / cluster;
   return launch_cols_kernel<T, S, kLong, BACK>(p, cluster, st);
 }
@@ -1148,7 +1141,9 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   // the tile of 16 steps, 325 in that of 64; [8192][65][64] 92 in 128 steps, 203 in the long sequences' 256.  A tile that
   // holds all steps needs no staging for a next one: [2048][256][64] takes 62 us (backward 116), 75 (155) as a long sequence.
   // The backward pass has more to keep for a step and holds half as many a thread.  One channel a thread, the price of
-  // channel counts that are no multiple of four: 88 us for [2048][256][65].
+  // channel counts that are no multiple of four: 88 us for [2048][256][65].  Of its backward tile of 16 steps a thread two CTAs
+  // share an SM under a sigmoid gate, whose a and b do not fit the 80 registers of three (fp32 [32][256][2079] 89 us against
+  // 95, bf16 [8][2500][1025] 97 against 154), and three under a decay, which has no b (73 against 86, 104 against 95).
   constexpr int R = BACK ? 4 : 8, N = BACK ? 2 : 1;
   if (vec) {
     if (c.length <= 8) return launch_short_cols<T, ColShape<4, 8, 1>, BACK>(p, st);
@@ -1164,8 +1159,8 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   if (c.length <= 32) return launch_short_cols<T, ColShape<1, 8, 4>, BACK>(p, st);
   if (c.length <= 64) return launch_short_cols<T, ColShape<1, 8, 8>, BACK>(p, st);
   if (c.length <= 128) return launch_short_cols<T, ColShape<1, 8, 16>, BACK>(p, st);
-  if (c.length <= 256) return launch_short_cols<T, ColShape<1, 16, 16, BACK ? 3 : 4>, BACK>(p, st);
-  return launch_long_cols<T, ColShape<1, 16, 16, BACK ? 3 : 4>, BACK>(p, st);
+  if (c.length <= 256) return launch_short_cols<T, ColShape<1, 16, 16, BACK ? 2 : 4, BACK ? 3 : 4>, BACK>(p, st);
+  return launch_long_cols<T, ColShape<1, 16, 16, BACK ? 2 : 4, BACK ? 3 : 4>, BACK>(p, st);
 }
 
 }  // namespace

@@ -12,6 +12,8 @@ F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 TYPES = [F32, BF16, F16]
 EPS = 1e-6
 
+TOL = {F32: 1e-5, BF16: 1e-5 + 2.0 ** -8, F16: 1e-5 + 2.0 ** -11}
+
 
 def rand(*shape, dtype=F32, seed=0, scale=1.0, shift=0.0):
     gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -129,3 +131,52 @@ def test_scan_of_one_object_in_two_threads():
     for t in threads:
         t.join()
     assert not bad
+
+
+def scan_all(plan, v, g, gh, h0, gl=None, lengths=None):
+    """(h, h_last, grad_v, grad_g, grad_h0)"""
+    ck = plan.new_checkpoints()
+    h, last = plan.forward(v, g, h0, lengths=lengths, checkpoints=ck)
+    return (h, last, *plan.backward(gh, v, g, ck, h0, lengths=lengths, grad_last=gl))
+
+
+def statement(v, g, gh, h0, gl, gate, lengths=None):
+    d = (v.shape[0], v.shape[1], int(np.prod(v.shape[2:])))
+    a = [host(t).reshape(d) for t in (v, g, gh)]
+    z = [None if t is None else host(t).reshape(d[0], d[2]) for t in (h0, gl)]
+    n = None if lengths is None else lengths.cpu().numpy()
+    h, last, _ = M.gated_scan(a[0], a[1], z[0], n, gate)
+    return (h, last, *M.gated_scan_backward(a[2], a[0], a[1], z[0], n, z[1], gate))
+
+
+@pytest.mark.parametrize("mean", [-20.0, -14.0, -8.0])
+@pytest.mark.parametrize("L", [1, 7, 16, 40, 100, 256, 600])
+@pytest.mark.parametrize("inner", [8, 5, 1])
+def test_scan_gradients_at_closed_gates(mean, L, inner):
+    """a of 2e-9 to 3e-4: every gradient as accurate as at gates around 1, in every layout.
+
+    Of grad_g that of the gates' own size, 1e-5: e^-|g| has a relative error of |g| 2^-24 (the rounding of g log2 e) and a few
+    2^-23 more, 5e-6 at most here."""
+    from paper_2607_14394_b200 import GatedScan
+    shape = (3, L) if inner == 1 else (3, L, inner)
+    state = (3,) if inner == 1 else (3, inner)
+    v, g, gh = rand(*shape, seed=1), rand(*shape, seed=2, shift=mean, scale=0.25), rand(*shape, seed=3)
+    h0, gl = rand(*state, seed=4), rand(*state, seed=5)
+    got = scan_all(GatedScan(shape, 1), v, g, gh, h0, gl)
+    want = statement(v, g, gh, h0, gl, "sigmoid")
+    for what, a, b in zip(("h", "h_last", "grad_v", "grad_g", "grad_h0"), got, want):
+        assert M.rel_l2(host(a).reshape(b.shape), b) <= TOL[F32], what
+
+
+def test_scan_gradients_at_saturated_gates():
+    """Gates of plus and minus infinity: a is 1 or (below the normal numbers) 0, and nothing of a gate's own gradient is left."""
+    from paper_2607_14394_b200 import GatedScan
+    inf = float("inf")
+    for shape in [(2, 300, 8), (2, 300, 5), (2, 20, 8), (2, 5, 8), (40, 30)]:
+        plan = GatedScan(shape, 1)
+        v, gh = rand(*shape, seed=1), rand(*shape, seed=2)
+        h0 = rand(*plan.state_shape, seed=3)
+        for g, gv, g0 in [(inf, torch.zeros_like(gh), gh.sum(1)), (-inf, gh, torch.zeros_like(h0))]:
+            out = scan_all(plan, v, torch.full_like(v, g), gh, h0)
+            assert torch.equal(out[2], gv) and float(out[3].abs().max()) < 1e-36
+            assert M.rel_l2(host(out[4]), host(g0)) <= TOL[F32]

@@ -168,6 +168,25 @@ def test_scan_gradients_at_closed_gates(mean, L, inner):
         assert M.rel_l2(host(a).reshape(b.shape), b) <= TOL[F32], what
 
 
+@pytest.mark.parametrize("mean", [8.0, 20.0])
+@pytest.mark.parametrize("L", [1, 7, 16, 40, 100, 256, 600])
+@pytest.mark.parametrize("inner", [8, 5, 1])
+def test_scan_with_a_long_memory(mean, L, inner):
+    """1 - a of 2e-9 to 3e-4, so that all of the steps count: an error of a that had one sign would add up.
+
+    Rounded to nearest, a is off by up to 2^-25 and a state by 2^-24 at each step, either way: sqrt(600) of them are 2e-6.  (At
+    gates of 20 a rounds to 1, always upward, by 2e-9 a step: 1e-6 in all.)"""
+    from paper_2607_14394_b200 import GatedScan
+    shape = (3, L) if inner == 1 else (3, L, inner)
+    state = (3,) if inner == 1 else (3, inner)
+    v, g, gh = rand(*shape, seed=1), rand(*shape, seed=2, shift=mean, scale=0.25), rand(*shape, seed=3)
+    h0, gl = rand(*state, seed=4), rand(*state, seed=5)
+    got = scan_all(GatedScan(shape, 1), v, g, gh, h0, gl)
+    want = statement(v, g, gh, h0, gl, "sigmoid")
+    for what, a, b in zip(("h", "h_last", "grad_v", "grad_g", "grad_h0"), got, want):
+        assert M.rel_l2(host(a).reshape(b.shape), b) <= TOL[F32], what
+
+
 def test_scan_gradients_at_saturated_gates():
     """Gates of plus and minus infinity: a is 1 or (below the normal numbers) 0, and nothing of a gate's own gradient is left."""
     from paper_2607_14394_b200 import GatedScan

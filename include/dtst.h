@@ -541,6 +541,9 @@ dtst_status dtst_matmul_fp8(int out_dtype, int64_t m, int64_t n, int64_t k, cons
  * time axis of a channels-first field), inner > 1: token-major sequences, or any other axis of a grid:
  *   h_t = a_t h_{t-1} + u_t,   h_{-1} = h0
  *   DTST_GATE_SIGMOID: a = 1 / (1 + exp(-g)), u = (1 - a) v        DTST_GATE_DECAY: a = g, u = v
+ * A decay may have any size, but products of neighbouring ones are formed in float32: with |a| <= 1 nothing overflows; where
+ * the gates of a run of steps (up to 16384 of them) multiply up beyond the float32 range, a state or gradient of zero in front
+ * of the run still passes as zero, and any other becomes an infinity or a NaN.
  * v, g: in_stride = elements between outer entries and between steps (the same for both; zero repeats an entry); the
  * inner stride is 1, and with inner = 1 the step stride must be 1.  h contiguous.  h0, h_last [outer, inner] float32; either
  * may be NULL (zeros; not wanted), and they may be the same buffer (a running state).  lengths [outer] int32 or NULL:

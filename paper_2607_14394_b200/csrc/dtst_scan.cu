@@ -64,6 +64,13 @@ __device__ __forceinline__ void terms_pair(float2 g, float2& a, float2& b) {
   a = fma_pair(a, fma_pair(e, m, add_pair(m, make_float2(1.f, 1.f))), a);
   b = mul_pair(e, a);
 }
+// The state (or gradient) s behind a run of steps, A the product of their gates and H what they make of zero.  A decay may be
+// larger than 1 and A infinite, which is no concern of a state of zero; a gate under a sigmoid is 1 at most.
+template <bool SIGMOID>
+__device__ __forceinline__ float through(float A, float s, float H) {
+  const float r = fmaf(A, s, H);
+  return !SIGMOID && s == 0.f ? H : r;
+}
 // d = a b and a b + c of N neighbouring channels (two at once: 126 -> 122 us for bf16 [65536][1024], whose pass is short of issue
 // slots; the backward passes, which are not, gained nothing)
 template <int N>
@@ -126,7 +133,7 @@ enum ColMode { kOneTile = 0, kLong = 1 };
 
 // joins (A, H) over the DG lanes of a channel, in lane order (UP) or against it; returns the summary of all of them and
 // leaves in (A, H) that of the lanes before this one
-template <int CPW, bool UP>
+template <int CPW, bool UP, bool SIGMOID>
 __device__ __forceinline__ float2 join_lanes(float& A, float& H) {
   const int d = (threadIdx.x & 31) / CPW;
   constexpr int DG = 32 / CPW;
@@ -134,7 +141,7 @@ __device__ __forceinline__ float2 join_lanes(float& A, float& H) {
   for (int o = 1; o < DG; o *= 2) {
     const float A1 = UP ? __shfl_up_sync(0xffffffffu, A, o * CPW) : __shfl_down_sync(0xffffffffu, A, o * CPW);
     const float H1 = UP ? __shfl_up_sync(0xffffffffu, H, o * CPW) : __shfl_down_sync(0xffffffffu, H, o * CPW);
-    if (UP ? d >= o : d + o < DG) H = fmaf(A, H1, H), A *= A1;
+    if (UP ? d >= o : d + o < DG) H = through<SIGMOID>(A, H1, H), A *= A1;
   }
   const int ch = (threadIdx.x & 31) % CPW, last = UP ? (DG - 1) * CPW + ch : ch;
   const float2 all = make_float2(__shfl_sync(0xffffffffu, A, last), __shfl_sync(0xffffffffu, H, last));
@@ -257,13 +264,13 @@ struct RunRows {
 // mbarrier; no cluster barrier, no fence).  Its latency is what a round cannot hide: when the pass over bf16 [65536][1024], 32
 // rounds of it, took 136 us, a copy of the kernel without the exchange took 100.  Returns the state in front of this CTA's chunk and moves `state` past
 // the round.  A lane of depth group d sends to and reads the box of CTA d.
-template <class S>
+template <class S, bool SIGMOID>
 __device__ __forceinline__ float join_round(const float2 all, float& state, RoundBoxes<S>& b, int round, int size, int rank, int jx,
                                             bool& dead) {
   static_assert(S::DG >= 8, "a depth group per CTA of the largest cluster");
   if (size == 1) {
     const float start = state;
-    state = fmaf(all.x, state, all.y);
+    state = through<SIGMOID>(all.x, state, all.y);
     return start;
   }
   const int lane = threadIdx.x & 31, d = lane / S::CPW, ch = lane % S::CPW, set = round & 1;
@@ -289,7 +296,7 @@ __device__ __forceinline__ float join_round(const float2 all, float& state, Roun
   float start = 0.f;
   for (int k = 0; k < size; ++k) {
     if (k == rank) start = state;
-    state = fmaf(__shfl_sync(0xffffffffu, m.x, k * S::CPW + ch), state, __shfl_sync(0xffffffffu, m.y, k * S::CPW + ch));
+    state = through<SIGMOID>(__shfl_sync(0xffffffffu, m.x, k * S::CPW + ch), state, __shfl_sync(0xffffffffu, m.y, k * S::CPW + ch));
   }
   return start;
 }
@@ -343,7 +350,7 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_kernel
     };
     if constexpr (MODE == kLong) if (c * LC >= e_tile) {       // no step of the sequence here: the state passes, h is zero
       float start = state;
-      start = join_round<S>(make_float2(1.f, 0.f), state, boxes, round, size, rank, jx, dead);
+      start = join_round<S, SIGMOID>(make_float2(1.f, 0.f), state, boxes, round, size, rank, jx, dead);
       if (c == 0 && first && jg.live && p.h_last != nullptr) p.h_last[ch] = start;
       zero_rows<T, S>(p.h + (at.o * p.L + c * LC) * p.inner + at.i0, p.inner, at.live ? (int)p.L - c * LC : 0, slot);
       refill();
@@ -370,7 +377,7 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_kernel
     } else {
       float ra[VEC], rh[VEC];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) ra[j] = a[0][j], rh[j] = u[0][j];
+      for (int j = 0; j < VEC; ++j) ra[j] = a[0][j], rh[j] = SIGMOID ? u[0][j] : fmaf(a[0][j], 0.f, u[0][j]);   // (a gate of NaN counts)
 #pragma unroll
       for (int r = 1; r < R; ++r) {
         mul_n<VEC>(ra, ra, a[r]);
@@ -385,23 +392,23 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_kernel
       for (int q = 0; q < S::JOIN; ++q) {
         m[q] = make_float2(*runs_a.at(jq + q, jx), *runs_h.at(jq + q, jx));
         A *= m[q].x;
-        H = fmaf(m[q].x, H, m[q].y);
+        H = through<SIGMOID>(m[q].x, H, m[q].y);
       }
-      const float2 all = join_lanes<S::CPW, true>(A, H);
+      const float2 all = join_lanes<S::CPW, true, SIGMOID>(A, H);
       float start = state;
-      if constexpr (MODE == kLong) start = join_round<S>(all, state, boxes, round, size, rank, jx, dead);
-      else state = fmaf(all.x, state, all.y);
-      float run = fmaf(A, start, H);
+      if constexpr (MODE == kLong) start = join_round<S, SIGMOID>(all, state, boxes, round, size, rank, jx, dead);
+      else state = through<SIGMOID>(all.x, state, all.y);
+      float run = through<SIGMOID>(A, start, H);
       // (a chunk in which a sequence has no step leaves its state alone)
       const bool active = c * LC < jg.end, more = (c + 1) * (long long)LC < jg.end;
       if (first && jg.live && (active || c == 0)) {
         if (MODE == kLong && p.ckpt != nullptr) p.ckpt[c * states + ch] = start;
-        if (!more && p.h_last != nullptr) p.h_last[ch] = fmaf(all.x, start, all.y);
+        if (!more && p.h_last != nullptr) p.h_last[ch] = through<SIGMOID>(all.x, start, all.y);
       }
 #pragma unroll
       for (int q = 0; q < S::JOIN; ++q) {
         *runs_a.at(jq + q, jx) = run;
-        run = fmaf(m[q].x, run, m[q].y);
+        run = through<SIGMOID>(m[q].x, run, m[q].y);
       }
       __syncthreads();
       runs_a.get(slot, x * VEC, s);
@@ -478,7 +485,7 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_backwa
       if (round + 1 < p.rounds) fetch(c - size);
     };
     if constexpr (MODE == kLong) if (c < 0 || c * LC >= e_tile) {       // no step of the sequence here
-      const float behind = join_round<S>(make_float2(1.f, 0.f), grad, boxes, round, size, rank, jx, dead);
+      const float behind = join_round<S, SIGMOID>(make_float2(1.f, 0.f), grad, boxes, round, size, rank, jx, dead);
       if (c == 0 && jg.live && first && p.gh0 != nullptr) p.gh0[ch] = behind;
       if (c >= 0) {
         const long long from = at.o * p.gr_o + at.i0 + (long long)c * LC * p.gr_t;
@@ -544,27 +551,27 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_backwa
         m[k] = make_float2(*runs_a.at(jq + k, jx), *runs_h.at(jq + k, jx));
         md[k] = *backs.at(jq + k, jx);
         A *= m[k].x;
-        H = fmaf(m[k].x, H, m[k].y);
+        H = through<SIGMOID>(m[k].x, H, m[k].y);
       }
 #pragma unroll
-      for (int k = S::JOIN - 1; k >= 0; --k) E = fmaf(m[k].x, E, md[k]);
+      for (int k = S::JOIN - 1; k >= 0; --k) E = through<SIGMOID>(m[k].x, E, md[k]);
       B = A;
-      join_lanes<S::CPW, true>(A, H);
-      const float2 all = join_lanes<S::CPW, false>(B, E);
+      join_lanes<S::CPW, true, SIGMOID>(A, H);
+      const float2 all = join_lanes<S::CPW, false, SIGMOID>(B, E);
       float behind = grad;
-      if constexpr (MODE == kLong) behind = join_round<S>(all, grad, boxes, round, size, rank, jx, dead);
-      if (c == 0 && jg.live && first && p.gh0 != nullptr) p.gh0[ch] = fmaf(all.x, behind, all.y);
-      float run = fmaf(A, before, H);
+      if constexpr (MODE == kLong) behind = join_round<S, SIGMOID>(all, grad, boxes, round, size, rank, jx, dead);
+      if (c == 0 && jg.live && first && p.gh0 != nullptr) p.gh0[ch] = through<SIGMOID>(all.x, behind, all.y);
+      float run = through<SIGMOID>(A, before, H);
 #pragma unroll
       for (int k = 0; k < S::JOIN; ++k) {
         *runs_a.at(jq + k, jx) = run;
-        run = fmaf(m[k].x, run, m[k].y);
+        run = through<SIGMOID>(m[k].x, run, m[k].y);
       }
-      run = fmaf(B, behind, E);
+      run = through<SIGMOID>(B, behind, E);
 #pragma unroll
       for (int k = S::JOIN - 1; k >= 0; --k) {
         *backs.at(jq + k, jx) = run;
-        run = fmaf(m[k].x, run, md[k]);
+        run = through<SIGMOID>(m[k].x, run, md[k]);
       }
       __syncthreads();
       runs_a.get(slot, x * VEC, s);
@@ -711,7 +718,7 @@ struct RowUnit {
 
 // Joins the lanes of one scan in which lanes of `marks` hold a summary that starts afresh: (A, H) of a lane becomes that of
 // all lanes from the nearest mark up to it.  No summary reaches across `span` lanes or more.
-template <bool UP>
+template <bool UP, bool SIGMOID>
 __device__ __forceinline__ bool segmented_scan(float& A, float& H, unsigned marks, int span) {
   const int lane = threadIdx.x & 31;
   const unsigned seen = UP ? marks & (0xffffffffu >> (31 - lane)) : marks & (0xffffffffu << lane);
@@ -722,7 +729,7 @@ __device__ __forceinline__ bool segmented_scan(float& A, float& H, unsigned mark
     if (o >= span) break;
     const float A1 = UP ? __shfl_up_sync(0xffffffffu, A, o) : __shfl_down_sync(0xffffffffu, A, o);
     const float H1 = UP ? __shfl_up_sync(0xffffffffu, H, o) : __shfl_down_sync(0xffffffffu, H, o);
-    if (o <= room) H = fmaf(A, H1, H), A *= A1;
+    if (o <= room) H = through<SIGMOID>(A, H1, H), A *= A1;
   }
   return fresh;
 }
@@ -752,6 +759,7 @@ __device__ __forceinline__ bool first_unit(const ScanArgs<T>& p, U& u, int& me, 
   return true;
 }
 // One round of a team: as join_round, a lane per member (at most 32).
+template <bool SIGMOID>
 __device__ __forceinline__ float join_team(const float2 all, float& state, float2 (*box)[kRowWarps], int round, int me, int members) {
   const int lane = threadIdx.x & 31;
   float2* mine = box[round & 1];
@@ -762,8 +770,8 @@ __device__ __forceinline__ float join_team(const float2 all, float& state, float
     const float2 m = members > kRowWarps ? cluster_read(mine + lane % kRowWarps, lane / kRowWarps) : mine[lane];
     A = m.x, H = m.y;
   }
-  segmented_scan<true>(A, H, 0u, 32);
-  const float s = fmaf(A, state, H);               // behind member `lane`
+  segmented_scan<true, SIGMOID>(A, H, 0u, 32);
+  const float s = through<SIGMOID>(A, state, H);   // behind member `lane`
   const float start = me == 0 ? state : __shfl_sync(0xffffffffu, s, me > 0 ? me - 1 : 0);
   state = __shfl_sync(0xffffffffu, s, 31);
   return start;
@@ -833,7 +841,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_kernel(const Scan
         A[k] *= a[k][i];
         H[k] = fmaf(a[k][i], H[k], b[k][i]);
       }
-      fresh[k] = segmented_scan<true>(A[k], H[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, x[k].spos < V) : 0u, u.span);
+      fresh[k] = segmented_scan<true, SIGMOID>(A[k], H[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, x[k].spos < V) : 0u, u.span);
     }
     const bool active = MODE == kWholeRows || (u.n > 0 && u.t0 < end), more = MODE != kWholeRows && u.t0 + u.n < end;
     const long long at = (long long)c * p.outer + u.row0;
@@ -843,16 +851,16 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_kernel(const Scan
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const float A1 = __shfl_sync(0xffffffffu, A[k], 31), H1 = __shfl_sync(0xffffffffu, H[k], 31);
-        tH = fmaf(A1, tH, H1), tA *= A1;
+        tH = through<SIGMOID>(A1, tH, H1), tA *= A1;
       }
       after = carry;
-      carry = join_team(make_float2(tA, tH), after, box, round, me, members);
+      carry = join_team<SIGMOID>(make_float2(tA, tH), after, box, round, me, members);
     }
     if (MODE != kWholeRows && p.ckpt != nullptr && lane == 0 && (active || c == 0)) p.ckpt[at] = carry;
     float in[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const float s = fresh[k] ? H[k] : fmaf(A[k], carry, H[k]);
+      const float s = fresh[k] ? H[k] : through<SIGMOID>(A[k], carry, H[k]);
       in[k] = __shfl_up_sync(0xffffffffu, s, 1);
       if (lane == 0) in[k] = carry;
       carry = __shfl_sync(0xffffffffu, s, 31);
@@ -942,8 +950,8 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
         if (MODE == kWholeRows && i == x[k].spos) D[k] = glv[k];
       }
       B[k] = A[k];
-      fresh_up[k] = segmented_scan<true>(A[k], H[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, x[k].spos < V) : 0u, u.span);
-      fresh_down[k] = segmented_scan<false>(B[k], D[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, u.ends(x[k])) : 0u, u.span);
+      fresh_up[k] = segmented_scan<true, SIGMOID>(A[k], H[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, x[k].spos < V) : 0u, u.span);
+      fresh_down[k] = segmented_scan<false, SIGMOID>(B[k], D[k], MODE == kWholeRows ? __ballot_sync(0xffffffffu, u.ends(x[k])) : 0u, u.span);
     }
     float after = 0.f;
     if (MODE == kTeam) {
@@ -951,22 +959,22 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) scan_rows_backward_kernel(c
 #pragma unroll
       for (int k = K - 1; k >= 0; --k) {
         const float B1 = __shfl_sync(0xffffffffu, B[k], 0), D1 = __shfl_sync(0xffffffffu, D[k], 0);
-        tD = fmaf(B1, tD, D1), tA *= B1;
+        tD = through<SIGMOID>(B1, tD, D1), tA *= B1;
       }
       after = carry;
-      carry = join_team(make_float2(tA, tD), after, box, round, me, members);
+      carry = join_team<SIGMOID>(make_float2(tA, tD), after, box, round, me, members);
     }
     float in[K], din[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const float s = fresh_up[k] ? H[k] : fmaf(A[k], start, H[k]);
+      const float s = fresh_up[k] ? H[k] : through<SIGMOID>(A[k], start, H[k]);
       in[k] = __shfl_up_sync(0xffffffffu, s, 1);
       if (lane == 0) in[k] = start;
       start = __shfl_sync(0xffffffffu, s, 31);
     }
 #pragma unroll
     for (int k = K - 1; k >= 0; --k) {
-      const float d = fresh_down[k] ? D[k] : fmaf(B[k], carry, D[k]);
+      const float d = fresh_down[k] ? D[k] : through<SIGMOID>(B[k], carry, D[k]);
       din[k] = __shfl_down_sync(0xffffffffu, d, 1);
       if (lane == 31) din[k] = carry;
       carry = __shfl_sync(0xffffffffu, d, 0);
@@ -1147,11 +1155,12 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   // The backward pass has more to keep for a step and holds half as many a thread.  One channel a thread, the price of
   // channel counts that are no multiple of four: 88 us for [2048][256][65].  Of its backward tile of 16 steps a thread two CTAs
   // share an SM under a sigmoid gate, whose a and b do not fit the 80 registers of three (fp32 [32][256][2079] 89 us against
-  // 95, bf16 [8][2500][1025] 97 against 154), and three under a decay, which has no b (73 against 86, 104 against 95).
+  // 95, bf16 [8][2500][1025] 97 against 154), and three under a decay, which has no b (73 against 86, 104 against 95).  Three
+  // as well in the tile of 16 steps under a decay (fp32 [65536][9][64] 126 us against 156 of two; under a sigmoid it needs 128 registers).
   constexpr int R = BACK ? 4 : 8, N = BACK ? 2 : 1;
   if (vec) {
     if (c.length <= 8) return launch_short_cols<T, ColShape<4, 8, 1>, BACK>(p, st);
-    if (c.length <= 16) return launch_short_cols<T, ColShape<4, 4, 4>, BACK>(p, st);
+    if (c.length <= 16) return launch_short_cols<T, ColShape<4, 4, 4, 2, BACK ? 3 : 2>, BACK>(p, st);
     if (c.length <= 32) return launch_short_cols<T, ColShape<4, R, 4 * N>, BACK>(p, st);
     if (c.length <= 64) return launch_short_cols<T, ColShape<4, R, 8 * N>, BACK>(p, st);
     if (c.length <= 128) return launch_short_cols<T, ColShape<4, R, 16 * N>, BACK>(p, st);

@@ -338,7 +338,8 @@ class Fp8Linear:
 class GatedScan:
     """h_t = a_t h_{t-1} + u_t along dimension `dim` of `shape`, forward and backward.
 
-    gate "sigmoid": a = sigmoid(g), u = (1 - a) v; "decay": a = g, u = v.  The states (h0, h_last) are float32 of the
+    gate "sigmoid": a = sigmoid(g), u = (1 - a) v; "decay": a = g, u = v (with |a| > 1 the product of neighbouring gates has to
+    stay in float32's range wherever the state is not zero).  The states (h0, h_last) are float32 of the
     shape without `dim`.  v and g may be strided in the dimensions in front of the last (both alike), e.g. the two
     halves of one projection's output; h and the upstream gradient are contiguous.
     """

@@ -199,3 +199,53 @@ def test_scan_gradients_at_saturated_gates():
             out = scan_all(plan, v, torch.full_like(v, g), gh, h0)
             assert torch.equal(out[2], gv) and float(out[3].abs().max()) < 1e-36
             assert M.rel_l2(host(out[4]), host(g0)) <= TOL[F32]
+
+
+AMPLIFYING = [(2, 20, 8), (2, 200, 8), (2, 250, 5), (2, 600, 8), (2, 600, 5), (1, 9000, 8), (5, 300), (4, 600), (2, 9000), (2400, 1100)]
+
+
+@pytest.mark.parametrize("shape", AMPLIFYING)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scan_decays_above_one_leave_a_state_of_zero_alone(shape, dtype):
+    """Gates of 1.5, whose product over a tile is beyond float32: zeros until the last 20 steps (gradients: but the first 20)."""
+    from paper_2607_14394_b200 import GatedScan
+    plan = GatedScan(shape, 1, dtype, "decay")
+    v, gh, g = (torch.zeros(shape, dtype=dtype, device="cuda") for _ in range(3))
+    v[:, -20:], gh[:, :20], g[:] = rand(*v[:, -20:].shape, dtype=dtype, seed=1), rand(*v[:, :20].shape, dtype=dtype, seed=2), 1.5
+    got = scan_all(plan, v, g, gh, None)
+    some = slice(0, 3)              # (of many sequences the statement walks a few)
+    want = statement(v[some], g[some], gh[some], None, None, "decay")
+    for what, a, b, t in zip(("h", "h_last", "grad_v", "grad_g", "grad_h0"), got, want, (dtype, F32, dtype, dtype, F32)):
+        assert torch.isfinite(a).all(), what
+        assert M.rel_l2(host(a[some]).reshape(b.shape), b) <= TOL[t], what
+
+
+@pytest.mark.parametrize("shape", [(2, 200, 8), (2, 600, 5), (5, 300), (3, 2000), (40, 30)])
+@pytest.mark.parametrize("t", [0, 1, 15, 16, 24, 29])
+def test_scan_gate_of_nan_spoils_a_state_of_zero(shape, t):
+    """0 times NaN: states behind such a gate are NaN, gradients in front of it, and nothing else is."""
+    from paper_2607_14394_b200 import GatedScan
+    plan = GatedScan(shape, 1, gate="decay")
+    v, gh, g = (torch.zeros(shape, device="cuda") for _ in range(3))
+    g[:] = 0.5
+    g[1, t] = float("nan")
+    got = scan_all(plan, v, g, gh, None)
+    want = statement(v, g, gh, None, None, "decay")
+    for a, b in zip(got, want):
+        assert np.array_equal(np.isnan(host(a)).reshape(b.shape), np.isnan(b))
+
+
+@pytest.mark.parametrize("shape", [(3, 256, 8), (3, 200, 5), (5, 400)])
+def test_scan_decays_above_one_within_the_range(shape):
+    """Gates of 0.9 to 1.25 (a product of 1e24 at most over the steps), states and gradients everywhere."""
+    from paper_2607_14394_b200 import GatedScan
+    L = shape[1]
+    v, gh = rand(*shape, seed=1).abs(), rand(*shape, seed=2).abs()
+    g = 0.9 + 0.35 * torch.rand(shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    plan = GatedScan(shape, 1, gate="decay")
+    h0 = rand(*plan.state_shape, seed=4).abs()
+    got, want = scan_all(plan, v, g, gh, h0, h0), statement(v, g, gh, h0, h0, "decay")
+    for a, b in zip(got, want):
+        assert np.isfinite(b).all()
+        # terms of one sign: at most 2 L roundings of 2^-24 each in any of them, and twice that in a product of two
+        assert M.rel_l2(host(a).reshape(b.shape), b) <= 4 * L * 2.0 ** -24

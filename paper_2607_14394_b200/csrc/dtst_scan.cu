@@ -314,14 +314,6 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_kernel
   pdl_wait();
   const int size = MODE == kLong ? cluster_size() : 1, rank = MODE == kLong ? cluster_rank() : 0;
   const unsigned tile = blockIdx.x / size;
-  if (size > 1) {
-    if (threadIdx.x == 0) {
-      sm100::mbar_init(&boxes.bar[0], 1);
-      sm100::mbar_init(&boxes.bar[1], 1);
-      sm100::fence_barrier_init();
-    }
-    cluster_sync();
-  }
   const int slot = threadIdx.x / S::TX, x = threadIdx.x % S::TX;
   const T none_v = Elem<T>::put(0.f), none_g = neutral_gate<T>(SIGMOID);
   const long long states = p.outer * p.inner;
@@ -341,6 +333,14 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_kernel
   };
   fetch(rank);
   float state = SLOTS > 1 && jg.live && p.h0 != nullptr ? p.h0[ch] : 0.f;
+  if (size > 1) {
+    if (threadIdx.x == 0) {
+      sm100::mbar_init(&boxes.bar[0], 1);
+      sm100::mbar_init(&boxes.bar[1], 1);
+      sm100::fence_barrier_init();
+    }
+    cluster_sync();        // also: every CTA has read its h0, whose place h_last may take
+  }
 
 #pragma unroll 1
   for (int round = 0; round < p.rounds; ++round) {

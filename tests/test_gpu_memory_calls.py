@@ -249,3 +249,18 @@ def test_scan_decays_above_one_within_the_range(shape):
         assert np.isfinite(b).all()
         # terms of one sign: at most 2 L roundings of 2^-24 each in any of them, and twice that in a product of two
         assert M.rel_l2(host(a).reshape(b.shape), b) <= 4 * L * 2.0 ** -24
+
+
+@pytest.mark.parametrize("shape", [(1, 5000, 64), (2, 4097, 36), (1, 3000, 5), (1, 9001), (3, 30000), (4, 1, 64), (40, 30), (7, 9, 12)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scan_state_in_place(shape, dtype):
+    """h_last in h0's place, also where a cluster shares the sequence and every CTA of it reads h0."""
+    from paper_2607_14394_b200 import GatedScan
+    plan = GatedScan(shape, 1, dtype)
+    v, g = rand(*shape, dtype=dtype, seed=1), rand(*shape, dtype=dtype, seed=2)
+    h0 = rand(*plan.state_shape, seed=3)
+    h, last = plan.forward(v, g, h0)
+    for _ in range(5):
+        state = h0.clone()
+        h2, last2 = plan.forward(v, g, state, h_last=state)
+        assert last2.data_ptr() == state.data_ptr() and torch.equal(h2, h) and torch.equal(state, last)

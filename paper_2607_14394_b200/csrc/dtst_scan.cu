@@ -274,7 +274,7 @@ __device__ __forceinline__ float join_round(const float2 all, float& state, Roun
     return start;
   }
   const int lane = threadIdx.x & 31, d = lane / S::CPW, ch = lane % S::CPW, set = round & 1;
-  if (threadIdx.x == 0) sm100::mbar_arrive_expect_tx(&b.bar[set], (uint32_t)(size - 1) * S::W * 8u);
+  if (threadIdx.x == 0 && !dead) sm100::mbar_arrive_expect_tx(&b.bar[set], (uint32_t)(size - 1) * S::W * 8u);
   if (d < size && d != rank) {
     uint32_t to, bar;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(sm100::smem_u32(&b.box[set][rank][jx])), "r"(d));
@@ -299,6 +299,18 @@ __device__ __forceinline__ float join_round(const float2 all, float& state, Roun
     state = through<SIGMOID>(__shfl_sync(0xffffffffu, m.x, k * S::CPW + ch), state, __shfl_sync(0xffffffffu, m.y, k * S::CPW + ch));
   }
   return start;
+}
+
+// No CTA leaves while summaries may be on their way to it.  A CTA whose waits all ended well has everybody's; one that gave up
+// stays until the others have sent theirs, and for a bounded while until they have arrived.
+template <class S>
+__device__ __forceinline__ void leave_rounds(RoundBoxes<S>& b, int rounds, bool dead) {
+  __syncwarp();
+  // (relaxed: nothing is handed over, and a release would wait for the last round's stores, 2 us)
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+  const int last = rounds - 1;
+  for (uint32_t poll = 0; dead && poll < 4096u && !sm100::mbar_try_wait(&b.bar[last & 1], (uint32_t)(last >> 1) & 1u); ++poll) {
+  }
 }
 
 template <typename T, class S, int MODE, bool SIGMOID>
@@ -432,6 +444,7 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_kernel
     if (MODE == kOneTile) return;
     __syncthreads();       // the runs' states are read before the next chunk's summaries replace them
   }
+  if (size > 1) leave_rounds<S>(boxes, p.rounds, dead);
 }
 
 template <typename T, class S, int MODE, bool SIGMOID>
@@ -618,6 +631,7 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_backwa
     if (MODE == kOneTile) return;
     __syncthreads();
   }
+  if (size > 1) leave_rounds<S>(boxes, p.rounds, dead);
 }
 
 // ------------------------------------------------------------------------------------------------ rows

@@ -540,9 +540,10 @@ matmul_fp8_pair_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_c
         store_box<T, Cfg::CW>(acc, &out_map, box, l0, c0, p.N - c0);
       }
     }
-    if (lane == 0) tma_store_wait_all<0>();
   }
 out:
+  // also on the way out of a wait that gave up: the copies out read this CTA's shared memory
+  if (warp >= 2 && lane == 0) tma_store_wait_all<0>();
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) {

@@ -270,7 +270,7 @@ def quantize_fp8_weight(w: torch.Tensor, stream=None) -> Tuple[torch.Tensor, tor
             return quantize_fp8_weight(w)
     q = empty_fp8(n, k, w.device)
     scale = w.new_empty((-(-n // BLOCK), -(-k // BLOCK)), dtype=torch.float32)
-    _check(Bn.lib().dtst_quantize_fp8_weight(DTYPES[w.dtype], n, k, w.data_ptr(), max(w.stride(0), k), q.data_ptr(),
+    _check(Bn.lib().dtst_quantize_fp8_weight(DTYPES[w.dtype], n, k, w.data_ptr(), w.stride(0) if n > 1 else k, q.data_ptr(),
                                              _q_stride(q, n, k), scale.data_ptr(), _raw_stream(dev)),
            "dtst_quantize_fp8_weight")
     return q, scale
@@ -320,7 +320,7 @@ class Fp8Linear:
         else:
             if out.shape != (m, self.n) or (self.n > 1 and out.stride(1) != 1):
                 raise ValueError(f"out must have shape {(m, self.n)} and contiguous rows")
-            op, out_ld = _on_device(out, "out", d, self.out_dtype), max(out.stride(0), self.n)
+            op, out_ld = _on_device(out, "out", d, self.out_dtype), out.stride(0) if m > 1 else self.n
         status = self._lib.dtst_matmul_fp8(self._type, m, self.n, k, xp, ld, sp, self._w, self._ld, self._ws, op, out_ld,
                                            self._work, 256, _raw_stream(d))
         if status:

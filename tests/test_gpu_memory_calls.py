@@ -264,3 +264,19 @@ def test_scan_state_in_place(shape, dtype):
         state = h0.clone()
         h2, last2 = plan.forward(v, g, state, h_last=state)
         assert last2.data_ptr() == state.data_ptr() and torch.equal(h2, h) and torch.equal(state, last)
+
+
+# ------------------------------------------------------------------------------------------------ 8-bit product
+def test_rows_that_overlap_are_refused():
+    from paper_2607_14394_b200 import Fp8Linear, quantize_fp8, quantize_fp8_weight
+    from paper_2607_14394_b200.binding import DtstError
+    q, s = quantize_fp8(rand(4, 64, seed=1))
+    lin = Fp8Linear.from_weight(rand(32, 64, seed=2), F32)
+    for out in (torch.empty(1, 32, device="cuda").expand(4, 32), torch.empty(128, device="cuda").as_strided((4, 32), (16, 1))):
+        with pytest.raises(DtstError):
+            lin.forward(q, s, out=out)
+    for quantise in (quantize_fp8, quantize_fp8_weight):
+        with pytest.raises(DtstError):
+            quantise(rand(1, 64, seed=3).expand(4, 64))
+    one = quantize_fp8_weight(rand(1, 64, seed=3).expand(1, 64))
+    assert one[0].shape == (1, 64)

@@ -118,3 +118,16 @@ def test_scan_calls_do_not_share_a_description(calls):
     got = [args[-1] for name, args in calls.seen if name == "dtst_gated_scan_backward"]
     third = (L * 3 * D, 3 * D)
     assert got == [(strided, third), (flat, flat), (flat, third), (strided, flat)]
+
+
+def test_rows_that_overlap_reach_the_library_as_they_are(calls):
+    """One row expanded to many: the library refuses a distance below the row's length, so it has to see that distance."""
+    q, s = torch.zeros(4, 32, dtype=Mem.FP8), torch.ones(1, 4)
+    lin = Mem.Fp8Linear.__new__(Mem.Fp8Linear)
+    lin.dev, lin.n, lin.k, lin._kb, lin._ld, lin.out_dtype, lin._type = -1, 16, 32, 1, 32, F32, 0
+    lin._w = lin._ws = lin._work = 0
+    lin._lib = calls
+    for out, ld in [(torch.empty(4, 16), 16), (torch.empty(4, 24)[:, :16], 24), (torch.empty(1, 16).expand(4, 16), 0),
+                    (torch.empty(64).as_strided((4, 16), (8, 1)), 8)]:
+        lin.forward(q, s, out=out)
+        assert calls.last("dtst_matmul_fp8")[11] == ld

@@ -237,7 +237,7 @@ def _q_stride(q: torch.Tensor, rows: int, k: int) -> int:
         raise ValueError(f"8-bit tensor must have shape {(rows, k)}, got {tuple(q.shape)}")
     if k > 1 and q.stride(1) != 1:
         raise ValueError("the rows of an 8-bit tensor must be contiguous")
-    return q.stride(0) if rows > 1 else max(q.stride(0), _rows16(k))
+    return q.stride(0) if rows > 1 else _rows16(k)       # (of one row there is no distance: any that the library takes)
 
 
 def quantize_fp8(x: torch.Tensor, q=None, scale=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:

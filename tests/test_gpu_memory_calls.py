@@ -280,3 +280,18 @@ def test_rows_that_overlap_are_refused():
             quantise(rand(1, 64, seed=3).expand(4, 64))
     one = quantize_fp8_weight(rand(1, 64, seed=3).expand(1, 64))
     assert one[0].shape == (1, 64)
+
+
+def test_single_rows_of_any_stride():
+    """One row of a buffer whose rows are not 16 bytes apart: operand, weights and the quantiser's output."""
+    from paper_2607_14394_b200 import Fp8Linear, quantize_fp8, quantize_fp8_weight
+    from paper_2607_14394_b200.memory import FP8
+    buffer = lambda: torch.zeros(1, 200, dtype=torch.uint8, device="cuda").view(FP8)[:, :100]
+    x, w = rand(1, 100, seed=1), rand(1, 100, seed=2)
+    (q, s), (wq, ws) = quantize_fp8(x), quantize_fp8_weight(w)
+    want = Fp8Linear(wq, ws, F32)(q, s)
+    q2, wq2 = buffer(), buffer()
+    wq2.copy_(wq)
+    quantize_fp8(x, q=q2, scale=s)
+    assert torch.equal(q2.float(), q.float())
+    assert torch.equal(Fp8Linear(wq2, ws, F32)(q2, s), want)

@@ -131,3 +131,7 @@ def test_rows_that_overlap_reach_the_library_as_they_are(calls):
                     (torch.empty(64).as_strided((4, 16), (8, 1)), 8)]:
         lin.forward(q, s, out=out)
         assert calls.last("dtst_matmul_fp8")[11] == ld
+    # a single row has no distance to a next one, whatever its tensor's stride
+    for width in (32, 48, 200):
+        lin.forward(torch.zeros(1, width, dtype=Mem.FP8)[:, :32], torch.ones(1, 1))
+        assert calls.last("dtst_matmul_fp8")[5] % 16 == 0

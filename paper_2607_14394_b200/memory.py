@@ -53,11 +53,12 @@ def _on_device(t: torch.Tensor, name: str, dev: int, dtype: torch.dtype) -> int:
     return t.data_ptr()
 
 
-def _use(stream):
-    """A context in which `stream` (a torch stream or a cudaStream_t) is current: the whole call, the allocation of its
-    outputs included, runs on it."""
+def _use(stream, dev):
+    """A context in which `stream` (a torch stream or a cudaStream_t, 0 being the default stream) is current: the whole
+    call, the allocation of its outputs included, runs on it."""
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream))
+        # (an ExternalStream of address 0 is a new stream of torch's own)
+        stream = torch.cuda.ExternalStream(int(stream), device=dev) if int(stream) else torch.cuda.default_stream(dev)
     return torch.cuda.stream(stream)
 
 
@@ -123,7 +124,7 @@ class RmsNorm:
         """
         d, t, sh = self.dev, self.dtype, self.shape
         if stream is not None or _current_device() != d:
-            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream, d):
                 return self.forward(x, weight, residual, out, sum_out, rstd, need_backward)
         xp, wp = _addr(x, "x", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
         rp = sp = 0
@@ -165,7 +166,7 @@ class RmsNorm:
         [ceil(channels / 128), rows] - what Fp8Linear takes."""
         rows, c, d, t, sh = self.outer, self.channels, self.dev, self.dtype, self.shape
         if stream is not None or _current_device() != d:
-            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream, d):
                 return self.forward_fp8(x, weight, residual, q, scale, sum_out)
         if self.inner != 1:
             raise ValueError("an 8-bit output needs the channels in the last dimension")
@@ -203,7 +204,7 @@ class RmsNorm:
         clone, a detach or a copy of rstd: pass it on as `sum_low=`, or the gradients are those of the rounded sum."""
         d, t, sh = self.dev, self.dtype, self.shape
         if stream is not None or _current_device() != d:
-            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream, d):
                 return self.backward(grad_y, s, weight, rstd, grad_s, grad_x, grad_weight, need_grad_weight, None, sum_low)
         gp, wp = _addr(grad_y, "grad_y", d, t, sh), _addr(weight, "weight", d, torch.float32, self._wshape)
         if grad_x is None:
@@ -247,7 +248,7 @@ def quantize_fp8(x: torch.Tensor, q=None, scale=None, stream=None) -> Tuple[torc
     rows, k = x.shape
     dev, shape = x.get_device(), (-(-k // BLOCK), rows)
     if stream is not None or _current_device() != dev:
-        with torch.cuda.device(dev), _use(torch.cuda.current_stream(dev) if stream is None else stream):
+        with torch.cuda.device(dev), _use(torch.cuda.current_stream(dev) if stream is None else stream, dev):
             return quantize_fp8(x, q, scale)
     if q is None:
         q = empty_fp8(rows, k, x.device)
@@ -266,7 +267,7 @@ def quantize_fp8_weight(w: torch.Tensor, stream=None) -> Tuple[torch.Tensor, tor
     n, k = w.shape
     dev = w.get_device()
     if stream is not None or _current_device() != dev:
-        with torch.cuda.device(dev), _use(torch.cuda.current_stream(dev) if stream is None else stream):
+        with torch.cuda.device(dev), _use(torch.cuda.current_stream(dev) if stream is None else stream, dev):
             return quantize_fp8_weight(w)
     q = empty_fp8(n, k, w.device)
     scale = w.new_empty((-(-n // BLOCK), -(-k // BLOCK)), dtype=torch.float32)
@@ -309,7 +310,7 @@ class Fp8Linear:
     def forward(self, x: torch.Tensor, x_scale: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None):
         d, k = self.dev, self.k
         if stream is not None or _current_device() != d:
-            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream, d):
                 return self.forward(x, x_scale, out)
         m = x.shape[0]
         xp, ld = _on_device(x, "x", d, FP8), _q_stride(x, m, k)
@@ -433,7 +434,7 @@ class GatedScan:
         """Returns (h, h_last).  lengths: int32 per outer entry; checkpoints: see new_checkpoints."""
         d, state = self.dev, self.state_shape
         if stream is not None or _current_device() != d:
-            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream, d):
                 return self.forward(v, g, h0, lengths, out, h_last, checkpoints)
         vp, gp, at = self._inputs(v, g)
         hp = 0 if h0 is None else _addr(h0, "h0", d, torch.float32, state)
@@ -461,7 +462,7 @@ class GatedScan:
         """Returns (grad_v, grad_g, grad_h0); v, g, h0, lengths and checkpoints as in the forward call."""
         d, t, state = self.dev, self.dtype, self.state_shape
         if stream is not None or _current_device() != d:
-            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream):
+            with torch.cuda.device(d), _use(torch.cuda.current_stream(d) if stream is None else stream, d):
                 return self.backward(grad_h, v, g, checkpoints, h0, lengths, grad_last, grad_v, grad_g, grad_h0,
                                      need_grad_h0)
         vp, gp, at = self._inputs(v, g)
@@ -527,7 +528,7 @@ class FieldMemory:
     def forward(self, x, h0=None, stream=None):
         """Returns (out, h_last); both passes work in this object's buffers."""
         if stream is not None:
-            with _use(stream):
+            with _use(stream, self.device):
                 return self.forward(x, h0)
         self.x, self.h0 = x, h0
         self.norm.forward(x, self.weight, out=self.y, rstd=self.rstd)
@@ -540,7 +541,7 @@ class FieldMemory:
 
     def backward(self, grad_out, grad_last=None, stream=None) -> dict:
         if stream is not None:
-            with _use(stream):
+            with _use(stream, self.device):
                 return self.backward(grad_out, grad_last)
         e = torch.empty_like
         gr = {"W_o": e(self.W_o), "W_v": e(self.W_v), "W_g": e(self.W_g), "b_v": e(self.b_v), "b_g": e(self.b_g)}
@@ -594,7 +595,7 @@ class RolloutMemory:
     def forward(self, x: torch.Tensor, lengths=None, stream=None) -> torch.Tensor:
         """x [B, T, D] -> out [B, T, D]; the layers' states move on by T frames (by lengths[b] where given)."""
         if stream is not None:
-            with _use(stream):
+            with _use(stream, self.device):
                 return self.forward(x, lengths)
         B, T, D = x.shape
         if (B, D) != (self.B, self.D):

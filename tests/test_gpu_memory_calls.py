@@ -295,3 +295,35 @@ def test_single_rows_of_any_stride():
     quantize_fp8(x, q=q2, scale=s)
     assert torch.equal(q2.float(), q.float())
     assert torch.equal(Fp8Linear(wq2, ws, F32)(q2, s), want)
+
+
+# ------------------------------------------------------------------------------------------------ streams
+@pytest.mark.parametrize("how", ["stream", "address"])
+def test_calls_on_the_default_stream(how):
+    """stream= the default stream, whose cudaStream_t is 0, from under another stream, behind work still running on it."""
+    from paper_2607_14394_b200 import Fp8Linear, GatedScan, RmsNorm, RolloutMemory, quantize_fp8
+    default = torch.cuda.default_stream()
+    st = default if how == "stream" else default.cuda_stream
+    assert default.cuda_stream == 0
+    w, x = rand(256, seed=1), rand(60, 256, dtype=BF16, seed=2)
+    n, lin = RmsNorm((60, 256), -1, BF16), Fp8Linear.from_weight(rand(128, 256, seed=3), BF16)
+    scan = GatedScan((3, 20, 64), 1, BF16)
+    mk = lambda: RolloutMemory([(rand(128, 256, seed=4), rand(256, 64, seed=5), w)], w, 3)
+
+    def chain(x_, blk, **k):
+        q, s, _ = n.forward_fp8(x_, w, **k)
+        vg = lin.forward(q, s, **k).view(3, 20, 128)
+        h, _ = scan.forward(vg[..., :64], vg[..., 64:], **k)
+        return h, quantize_fp8(x_, **k)[0], blk.forward(x_.view(3, 20, 256), **k)
+
+    want = chain(x, mk())
+    blk, late, big = mk(), torch.zeros_like(x), torch.empty(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(20):
+        big.mul_(1.0001)
+    late.copy_(x)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = chain(late, blk, stream=st)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a.float(), b.float())

@@ -82,6 +82,12 @@ __host__ __device__ inline float herm_weight(int f, int N) {
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// DTST_NO_PDL: launches without the attribute
+inline bool pdl_off() {
+  static const bool off = getenv("DTST_NO_PDL") != nullptr;
+  return off;
+}
+
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
                               Args&&... args) {
@@ -94,8 +100,7 @@ inline cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, siz
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  static const bool off = getenv("DTST_NO_PDL") != nullptr;
-  cfg.numAttrs = off ? 0 : 1;
+  cfg.numAttrs = pdl_off() ? 0 : 1;
   return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 

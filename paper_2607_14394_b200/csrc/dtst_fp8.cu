@@ -587,24 +587,6 @@ __global__ void __launch_bounds__(256) quantize_weight_kernel(const T* __restric
   }
 }
 
-template <typename Kern, typename... Args>
-cudaError_t launch_matmul(Kern kern, int grid, int threads, int cluster, size_t smem, cudaStream_t st, const Args&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 0 ? 2 : 1;       // (0: the kernel's own cluster size)
-  return cudaLaunchKernelEx(&cfg, kern, args...);
-}
-
 // few tiles: as many CTAs to a tile as the GPU has room for, each with two k-blocks at least
 int split_of(long long tiles, int KB) {
   int split = 1;
@@ -630,7 +612,7 @@ cudaError_t launch_tile(const MatmulCall& c, MatmulArgs p, cudaStream_t st) {
   const int sms = num_sms();
   p.split = split_of(tiles, p.KB);
   const long long grid = p.split > 1 ? tiles * p.split : (tiles < sms ? tiles : sms);
-  return launch_matmul(kern, (int)grid, Cfg::THREADS, p.split, Cfg::SMEM, st, lane_map, col_map, p);
+  return launch_clusters(kern, (unsigned)grid, p.split, Cfg::THREADS, Cfg::SMEM, st, lane_map, col_map, p);
 }
 
 template <typename T>
@@ -648,7 +630,7 @@ cudaError_t launch_pairs(const MatmulCall& c, MatmulArgs p, cudaStream_t st) {
   const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), Cfg::SMEM, allowed);
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)p.lane_tiles * p.col_tiles, pairs = num_sms() / 2;
-  return launch_matmul(kern, (int)(2 * (tiles < pairs ? tiles : pairs)), Cfg::THREADS, 0, Cfg::SMEM, st, x_map, w_map, out_map, p);
+  return launch_clusters(kern, (unsigned)(2 * (tiles < pairs ? tiles : pairs)), 0, Cfg::THREADS, Cfg::SMEM, st, x_map, w_map, out_map, p);
 }
 
 template <typename T>

@@ -20,6 +20,32 @@ inline cudaError_t allow_smem(const void* kern, size_t bytes, std::atomic<uint64
   return e;
 }
 
+// As launch_pdl, for thread-block clusters of `cluster` CTAs (0: the kernel's own cluster size).
+template <typename Kern, typename... Args>
+inline cudaError_t launch_clusters(Kern kern, unsigned ctas, int cluster, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  unsigned n = 0;
+  if (cluster > 0) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = (unsigned)cluster;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (!pdl_off()) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 constexpr int kNormParts = 592;           // most CTAs (and rows of partial sums) of a norm's backward pass: 4 per SM
 constexpr int kNormFieldChannels = 128;   // most channels a channels-first norm holds in registers
 

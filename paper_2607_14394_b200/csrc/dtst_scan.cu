@@ -1044,25 +1044,6 @@ int cluster_for(long long tiles, long long chunks, long long slots, int most) {
   return best;
 }
 
-template <typename Kern, typename Args>
-cudaError_t launch_clusters(Kern kern, long long tiles, int cluster, int threads, size_t smem, cudaStream_t st, const Args& p) {
-  if (tiles * cluster > 0x7fffffff) return cudaErrorNotSupported;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * cluster));
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, p);
-}
-
 template <typename T, class S, int MODE, bool BACK>
 cudaError_t launch_cols_kernel(const ScanArgs<T>& p, int cluster, cudaStream_t st) {
   void (*kern)(const ScanArgs<T>);
@@ -1073,7 +1054,8 @@ cudaError_t launch_cols_kernel(const ScanArgs<T>& p, int cluster, cudaStream_t s
   const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), smem + 8192 + sizeof(float) * 3 * S::SLOTS * S::W, allowed[p.sigmoid != 0]);
   if (e != cudaSuccess) return e;
   if (MODE == kOneTile) return launch_pdl(kern, dim3((unsigned)p.chains), dim3(S::THREADS), smem, st, p);
-  return launch_clusters(kern, p.chains, cluster, S::THREADS, smem, st, p);
+  if (p.chains * cluster > 0x7fffffff) return cudaErrorNotSupported;
+  return launch_clusters(kern, (unsigned)(p.chains * cluster), cluster, S::THREADS, smem, st, p);
 }
 
 // sequences that fit one tile
@@ -1107,7 +1089,7 @@ cudaError_t launch_rows_kernel(const ScanArgs<T>& p, long long tiles, int cluste
   else
     kern = ragged ? (sigmoid ? scan_rows_kernel<T, WIDE, MODE, true, true> : scan_rows_kernel<T, WIDE, MODE, true, false>)
                   : (sigmoid ? scan_rows_kernel<T, WIDE, MODE, false, true> : scan_rows_kernel<T, WIDE, MODE, false, false>);
-  if (MODE == kTeam) return launch_clusters(kern, tiles, cluster, 32 * kRowWarps, 0, st, p);
+  if (MODE == kTeam) return launch_clusters(kern, (unsigned)(tiles * cluster), cluster, 32 * kRowWarps, 0, st, p);
   const long long ctas = (tiles + kRowWarps - 1) / kRowWarps;       // a unit per warp
   if (ctas > 0x7fffffff) return cudaErrorNotSupported;
   return launch_pdl(kern, dim3((unsigned)ctas), dim3(32 * kRowWarps), 0, st, p);

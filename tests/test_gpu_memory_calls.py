@@ -327,3 +327,43 @@ def test_calls_on_the_default_stream(how):
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a.float(), b.float())
+
+
+_EDGES = """
+import ctypes, torch
+from paper_2607_14394_b200 import Fp8Linear, GatedScan, RmsNorm, quantize_fp8
+w, x = torch.ones(256, device="cuda"), torch.randn(3000, 256, device="cuda")
+n, lin = RmsNorm((3000, 256)), Fp8Linear.from_weight(torch.randn(2304, 256, device="cuda"))
+few = Fp8Linear.from_weight(torch.randn(64, 2048, device="cuda"))
+fq, fs = quantize_fp8(torch.randn(8, 2048, device="cuda"))
+scan, row = GatedScan((1, 3000, 256)), GatedScan((1, 20000))
+t = torch.randn(1, 20000, device="cuda")
+v = torch.randn(1, 3000, 256, device="cuda")
+def calls():
+    q, s, _ = n.forward_fp8(x, w)
+    return lin(q, s), lin(q[:100], s[:, :100].contiguous()), few(fq, fs), scan.forward(v, v), row.forward(t, t)
+calls()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph(keep_graph=True)
+with torch.cuda.graph(g):
+    calls()
+rt = ctypes.CDLL("libcudart.so.12")
+many, ends = ctypes.c_size_t(0), (ctypes.c_void_p * 64)
+print(rt.cudaGraphGetEdges(ctypes.c_void_p(g.raw_cuda_graph()), ends(), ends(), ctypes.byref(ctypes.c_size_t(64))))
+"""
+
+
+@pytest.mark.parametrize("off", [False, True])
+def test_launches_without_the_dependent_launch_attribute(off):
+    """DTST_NO_PDL=1 holds for the kernels in clusters too: no edge of a captured graph carries more than the plain order
+    (the query that can only return plain edges is refused, code 402, where one does)."""
+    import os
+    import subprocess
+    import sys
+    env = {k: v for k, v in os.environ.items() if k != "DTST_NO_PDL"}
+    if off:
+        env["DTST_NO_PDL"] = "1"
+    r = subprocess.run([sys.executable, "-c", _EDGES], env=env, capture_output=True, text=True, timeout=300,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, r.stderr
+    assert (int(r.stdout.split()[-1]) == 0) == off

@@ -115,7 +115,7 @@ class RmsNorm:
         self._scratch_bytes = int(n.value)
 
     def forward(self, x, weight, residual=None, out=None, sum_out=None, rstd=None, need_backward=True, stream=None):
-        """Returns (y, s, rstd); without a residual s is x itself.
+        """Returns (y, s, rstd); without a residual s is x itself (None where y takes x's place and leaves no s behind).
 
         In a 16-bit type with a residual, what rounding took from s stays with the rstd that is returned (its attribute
         `sum_low`), so that `backward` has the sum to 24 bits; an rstd that the caller brings may carry such a buffer too
@@ -159,7 +159,9 @@ class RmsNorm:
                                          qp, _raw_stream(d))
         if status:
             _check(status, "dtst_rms_norm")
-        return out, (x if sum_out is None else sum_out), rstd
+        if sum_out is None and (yp != xp or not xp):
+            sum_out = x
+        return out, sum_out, rstd
 
     def forward_fp8(self, x, weight, residual=None, q=None, scale=None, sum_out=None, stream=None):
         """Returns (q, scale, s): the norm of token-major rows in 8 bits, [rows, channels], and its scales

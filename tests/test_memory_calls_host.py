@@ -67,6 +67,22 @@ def test_norm_backward_calls_do_not_share_scratch(calls):
     assert pa + na <= pb or pb + nb <= pa
 
 
+def test_norm_over_its_input_leaves_no_sum(calls):
+    """y in x's place without a residual: there is no s to hand to backward, and nothing that looks like one."""
+    n = Mem.RmsNorm((4, 8), -1)
+    x, w = torch.randn(4, 8), torch.ones(8)
+    y, s, rstd = n.forward(x, w, out=x)
+    assert y is x and s is None
+    n.backward(x, s, w, rstd)
+    assert calls.last("dtst_rms_norm_backward")[5] == 0          # which the library refuses
+    kept = torch.empty(4, 8)
+    assert n.forward(x, w, out=x, sum_out=kept)[1] is kept and n.forward(x, w)[1] is x
+    none = torch.empty(0, 8)                                     # (an empty batch has no address to go by)
+    assert Mem.RmsNorm((0, 8), -1).forward(none, w)[1] is none
+    r = torch.randn(4, 8)
+    assert n.forward(x, w, residual=r, out=x, sum_out=r)[1] is r
+
+
 def test_norm_low_part_belongs_to_the_last_forward_call(calls):
     """An rstd used again: without a residual there is no low part, with one again there is."""
     n = Mem.RmsNorm((4, 8), -1, BF16)

@@ -510,6 +510,10 @@ class FieldMemory:
 
     def __init__(self, B: int, C: int, grid: Sequence[int], device=None, seed: int = 0):
         shape = (B, C) + tuple(int(n) for n in grid)
+        points = torch.Size(shape[2:]).numel()
+        if not 1 <= C <= 32 or B < 1 or len(shape) < 3 or points < 4 or points % 4 != 0:
+            raise ValueError("FieldMemory takes 1 to 32 channels and a grid whose points are a multiple of 4, got "
+                             f"B = {B}, C = {C}, grid = {tuple(grid)}")
         self.norm = RmsNorm(shape, 1, device=device)
         self.scan = GatedScan(shape, len(shape) - 1, device=device)
         dev = self.device = self.norm.device
@@ -525,7 +529,7 @@ class FieldMemory:
         self.y, self.v, self.g, self.h, self.out = new(), new(), new(), new(), new()
         self.rstd = torch.empty((B,) + shape[2:], device=dev)
         self.checkpoints = self.scan.new_checkpoints()
-        self.x = self.h0 = self.lengths = None
+        self.x = self.h0 = None
 
     def forward(self, x, h0=None, stream=None):
         """Returns (out, h_last); both passes work in this object's buffers."""
@@ -558,6 +562,10 @@ class FieldMemory:
         # the residual's gradient joins inside the norm's backward pass
         gr["x"], gr["weight"] = self.norm.backward(gy, self.x, self.weight, self.rstd, grad_s=grad_out)
         return gr
+
+    def status(self, stream=None) -> int:
+        """DTST_OK, or the status word of a bounded wait that gave up since the last query; synchronises."""
+        return self.scan.status(stream)
 
 
 class RolloutMemory:

@@ -367,3 +367,19 @@ def test_launches_without_the_dependent_launch_attribute(off):
                        cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert r.returncode == 0, r.stderr
     assert (int(r.stdout.split()[-1]) == 0) == off
+
+
+# ------------------------------------------------------------------------------------------------ the blocks
+@pytest.mark.parametrize("bad", [dict(C=33), dict(C=0), dict(B=0), dict(grid=(3, 5, 7)), dict(grid=()), dict(grid=(2,))])
+def test_field_memory_refuses_what_it_cannot_train(bad):
+    from paper_2607_14394_b200 import FieldMemory
+    with pytest.raises(ValueError):
+        FieldMemory(**{**dict(B=1, C=4, grid=(4, 6)), **bad})
+
+
+def test_field_memory_reports_its_status():
+    from paper_2607_14394_b200 import FieldMemory
+    blk = FieldMemory(1, 4, (4, 6))
+    out, _ = blk.forward(rand(1, 4, 4, 6, seed=1))
+    blk.backward(out.clone())
+    assert blk.status() == 0

@@ -595,8 +595,17 @@ class RolloutMemory:
         for s in self.states:
             s.zero_()
 
+    def status(self, stream=None) -> int:
+        """DTST_OK, or the status word of a bounded wait that gave up since the last query; synchronises."""
+        words = [lin.status(stream) for layer in self.layers for lin in layer[:2]]
+        with torch.cuda.device(self.device):
+            words.append(int(Bn.lib().dtst_gated_scan_status(Bn._stream_ptr(stream))))
+        return next((w for w in words if w != Bn.DTST_OK), Bn.DTST_OK)
+
     def _plan(self, T: int):
         if T not in self._plans:
+            while len(self._plans) >= 8:              # histories may come in any length
+                del self._plans[next(iter(self._plans))]
             norm = RmsNorm((self.B * T, self.D), -1, self.dtype, self.eps, self.device)
             scans = [GatedScan((self.B, T, lin.k), 1, self.dtype, device=self.device) for _, lin, _ in self.layers]
             self._plans[T] = (norm, scans)

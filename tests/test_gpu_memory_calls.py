@@ -383,3 +383,18 @@ def test_field_memory_reports_its_status():
     out, _ = blk.forward(rand(1, 4, 4, 6, seed=1))
     blk.backward(out.clone())
     assert blk.status() == 0
+
+
+def test_rollout_memory_over_histories_of_many_lengths():
+    from paper_2607_14394_b200 import RolloutMemory
+    w = torch.ones(64, device="cuda")
+    blk = RolloutMemory([(rand(96, 64, seed=1, scale=0.1), rand(64, 48, seed=2, scale=0.1), w)], w, 2)
+    x = rand(2, 40, 64, dtype=BF16, seed=3)
+    first = blk.forward(x[:, :1].contiguous())
+    for T in range(1, 41):
+        blk.reset()
+        blk.forward(x[:, :T].contiguous())
+    assert len(blk._plans) <= 8
+    blk.reset()
+    assert torch.equal(blk.forward(x[:, :1].contiguous()), first)
+    assert blk.status() == 0

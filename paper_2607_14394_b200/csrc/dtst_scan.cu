@@ -45,7 +45,7 @@ struct ScanArgs {
 // stays one); the approximate exponential is good to about 2^-22, the rounding of g log2 e adds |g| 2^-24 or so to the smaller of
 // the two (1e-6 at 20, 5e-6 at 80), and what it flushes to zero (g > 87) is below the smallest normal number.  a itself is
 // right to 2^-25 where the gate is open (a Newton step of 1 / (1 + e): with gates around 8 the last of 5000 states is off
-// by 1.6e-6, without it 1.0e-4; the forward pass over bf16 [65536][1024] takes 128 us, without it 122).  Two steps at once.
+// by 1.6e-6, without it 1.0e-4; the forward pass over bf16 [65536][1024] takes 125 us, without it 122).  Two steps at once.
 template <bool SIGMOID>
 __device__ __forceinline__ void terms_pair(float2 g, float2& a, float2& b) {
   if (!SIGMOID) {
@@ -59,10 +59,10 @@ __device__ __forceinline__ void terms_pair(float2 g, float2& a, float2& b) {
   const float2 d = add_pair(e, make_float2(1.f, 1.f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.x) : "f"(d.x));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.y) : "f"(d.y));
-  // a + a (1 - a - e a): the reciprocal's own error is of one sign, and a memory of thousands of steps would add it up
-  const float2 m = mul_pair(a, make_float2(-1.f, -1.f));
-  a = fma_pair(a, fma_pair(e, m, add_pair(m, make_float2(1.f, 1.f))), a);
   b = mul_pair(e, a);
+  // a + a (1 - a - b): the reciprocal's own error is of one sign, and a memory of thousands of steps would add it up
+  const float2 minus = make_float2(-1.f, -1.f);
+  a = fma_pair(a, fma_pair(b, minus, fma_pair(a, minus, make_float2(1.f, 1.f))), a);
 }
 // The state (or gradient) s behind a run of steps, A the product of their gates and H what they make of zero.  A decay may be
 // larger than 1 and A infinite, which is no concern of a state of zero; a gate under a sigmoid is 1 at most.

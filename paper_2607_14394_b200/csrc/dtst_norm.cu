@@ -14,9 +14,9 @@
 //   fields    [outer][C][inner], inner contiguous (channels-first): lanes run along the positions, warps share the
 //             channels, the sums over channels meet in shared memory.  fp32 [1][20][3932160] with residual: 206 us
 //             forward, 199 backward (6.1 and 6.3 TB/s).
-// Rows that begin off a vector (kShifted) are read in vectors that begin earlier: fp16 [5003][1001] 11.6 us forward and 21.9
-// backward, against 43.1 and 26.7 element by element (kScalar, left for tensors that do not begin on a vector); [40024][1001] 92
-// and 167, against 294 and 150.  Positions of a field in vectors where its rows allow it: fp32 [8][64][65536] 85 us, with
+// Rows that begin off a vector (kShifted) are read in vectors that begin earlier: fp16 [33520][1001] 40 us forward and 98
+// backward (3.4 and 2.1 TB/s), against 102 and 124 element by element (kScalar, for tensors that do not begin on a vector, and
+// for the backward pass of some rows).  Positions of a field in vectors where its rows allow it: fp32 [8][64][65536] 85 us, with
 // 65537 positions 109.  Beyond what registers hold, the fallbacks read their input again: bf16 [4096][16392] 284 us
 // ([16384]: 109), fp32 fields [8][136][65536] 338 us (128 channels: 172).
 // The weight gradient is summed in registers over all positions a CTA visits and in a fixed order over CTAs by a
@@ -290,6 +290,17 @@ RowLayout row_layout(long long C, long long x_ld, std::initializer_list<const vo
   return x_ld == C ? kShifted : kScalar;
 }
 
+// Vectors that hold a row, and how many times 32 has to be doubled to hold them: the row kernels come in these sizes.
+template <typename T>
+long long row_groups(long long C, RowLayout lay) {
+  return (C + (lay == kShifted ? kVec<T> - 1 : 0) + kVec<T> - 1) / kVec<T>;
+}
+inline int row_size(long long groups) {
+  int size = 0;
+  for (long long n = 32; n < groups; n *= 2) ++size;
+  return size;
+}
+
 template <typename T, int TPR, int ITEMS, bool QUANT, bool NORM, int LAY>
 cudaError_t launch_rows_kernel(const RowArgs& a, cudaStream_t st) {
   constexpr int RPC = kRowThreads<TPR> / TPR;
@@ -303,11 +314,10 @@ cudaError_t launch_rows_kernel(const RowArgs& a, cudaStream_t st) {
 
 template <typename T, bool QUANT, bool NORM>
 cudaError_t launch_rows(const RowArgs& a, cudaStream_t st) {
-  constexpr int VEC = kVec<T>;
   RowLayout lay = row_layout<T>(a.C, a.x_ld, {a.x, a.residual, a.s, a.low, QUANT ? nullptr : a.y});
   if (lay == kAligned && !aligned_to(a.weight, 16)) lay = kScalar;
   if (QUANT && lay == kShifted) lay = kScalar;       // blocks of 128 channels are counted from the row's beginning
-  const long long groups = (a.C + (lay == kShifted ? VEC - 1 : 0) + VEC - 1) / VEC;
+  const long long groups = row_groups<T>(a.C, lay);
 #define DTST_ROWS(TPR, ITEMS)                                                                                     \
   {                                                                                                               \
     if (lay == kAligned) return launch_rows_kernel<T, TPR, ITEMS, QUANT, NORM, kAligned>(a, st);                  \
@@ -794,9 +804,15 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
 
 template <typename T>
 cudaError_t launch_rows_backward(const RowBackArgs& a, int* parts, cudaStream_t st) {
-  constexpr int VEC = kVec<T>;
-  const RowLayout lay = row_layout<T>(a.C, a.C, {a.gy, a.s, a.low, a.gs, a.gx});
-  const long long groups = (a.C + (lay == kShifted ? VEC - 1 : 0) + VEC - 1) / VEC;
+  RowLayout lay = row_layout<T>(a.C, a.C, {a.gy, a.s, a.low, a.gs, a.gx});
+  // Element by element where the vector more that a shifted row takes needs the kernel of twice the size (2^25 elements, us
+  // shifted and by elements: fp16 250 channels 184, 103; 511 168, 128; 1023 248, 123; 4095 224, 200; fp32 1023 139, 76), but
+  // not where that is the kernel beyond the registers (fp16 8191: 162, 225).  In between 98, 124 (fp16 1001) to 91, 82 (fp32
+  // 2001); the forward pass is faster shifted on both sides (fp16 250: 80, 113; 1023: 91).
+  constexpr long long MOST = sizeof(T) == 4 ? 2048 : 1024;
+  const long long wide = row_groups<T>(a.C, kShifted), plain = row_groups<T>(a.C, kScalar);
+  if (lay == kShifted && wide <= MOST && row_size(wide) > row_size(plain)) lay = kScalar;
+  const long long groups = row_groups<T>(a.C, lay);
 #define DTST_ROWS(TPR, ITEMS)                                                                                     \
   {                                                                                                               \
     constexpr int RPC = kRowThreads<TPR> / TPR;                                                                   \

@@ -528,8 +528,8 @@ dtst_status dtst_quantize_fp8_weight(int dtype, int64_t rows, int64_t cols, cons
  *   multiples of 16 bytes (what lies between k and the stride is not used), else DTST_ERR_INVALID_ARG;
  *   x_scale [ceil(k / 128), m], w_scale [ceil(n / 128), ceil(k / 128)] float32, contiguous;
  *   out [m, n] of out_dtype, rows out_ld elements apart (out_ld >= n).  k >= 1.
- *   workspace: at least 256 bytes, 256-byte aligned, caller-owned, filled with zeros once before its first use; calls
- *   that share one must be stream-ordered.  Its first word is a status word as for plans (dtst_workspace_status).
+ *   workspace: at least 256 bytes, 256-byte aligned, caller-owned, filled with zeros once before its first use.  Its first
+ *   word is a status word as for plans (dtst_workspace_status), all that a call ever writes there: calls may share one.
  * The same bits on every run.
  */
 dtst_status dtst_matmul_fp8(int out_dtype, int64_t m, int64_t n, int64_t k, const void* x, int64_t x_ld,
@@ -556,7 +556,8 @@ dtst_status dtst_matmul_fp8(int out_dtype, int64_t m, int64_t n, int64_t k, cons
  *   SIGMOID: grad_v = delta (1 - a), grad_g = delta (h_{t-1} - v) a (1 - a);   DECAY: grad_v = delta, grad_g = delta h_{t-1};
  *   grad_h0 = a_0 delta_0 (may be NULL).  grad_v, grad_g: both with grad_stride, which must not make elements coincide;
  * zero behind an entry's own length.  v, g, h0, lengths and checkpoints as in the forward call.  h is not needed.
- * Neither pass needs a workspace, and both give the same bits on every run.
+ * Neither pass needs a workspace, and both give the same bits on every run.  h, grad_v and grad_g take no input's place, and not
+ * each other's (DTST_ERR_INVALID_ARG).
  */
 enum { DTST_GATE_SIGMOID = 0, DTST_GATE_DECAY = 1 };
 typedef struct {

@@ -11,9 +11,10 @@
 // columns, lanes being rows of x and columns rows of w, or the other way round (SWAP) where there are few rows of x, so that
 // the tile's lanes are filled by the weights; where there are few tiles the CTAs of a cluster share the k-blocks of one and
 // add their sums through distributed shared memory, in rank order.
-// Measured: 16384 x 4096 x 2048 in 139 to 146 us (1.9 to 2.0 PFLOP/s; without the epilogue, its loads and products take 115),
-// 2048^3 in 12.6, 1000 x 1111 x 1360 in 10.1; few rows of x read the weights once: 4 x 4096 x 2048 in 5.5 us, 64 rows in 6.9, 65
-// (not swapped) in 8.4.  Bound: many rows by the handing over of a block's sums every 128 values of k, few rows by latency.
+// Measured: 16384 x 4096 x 2048 in 147 us after a pause and 152 to 167 in long runs under the power limit (1.65 to 1.87 PFLOP/s;
+// without the epilogue, its loads and products take 115), 2048^3 in 13.3, 1000 x 1111 x 1360 in 10.2; few rows of x read the
+// weights once: 4 x 4096 x 2048 in 5.5 us, 64 rows in 6.9, 65 (not swapped) in 8.4.  Bound: many rows by the handing over of a
+// block's sums every 128 values of k (8192 rows: tensor pipe 42 % busy, L2 27 %), few rows by latency.
 // Warp 0 issues the TMA loads, warp 1 the products, the others hold the sums (a thread one lane x up to 128 columns).
 // Every wait is bounded: on expiry the kernel raises the status word, drains its loads and products, frees its tensor
 // memory and returns.
@@ -94,7 +95,7 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&r)[16]) {
 }
 
 // sums of one k-block, scaled, onto the fp32 sums: CW columns of this thread's lane from `taddr` on.  (Two sums an instruction:
-// 152 -> 139 us for 16384 x 4096 x 2048.  32 columns a load made it spill, 199 us.)
+// 152 -> 139 us for 16384 x 4096 x 2048 at the time, after a pause.  32 columns a load made it spill, 199 us.)
 template <int CW, typename F>
 __device__ __forceinline__ void add_block(float (&acc)[CW], uint32_t taddr, F factor) {
   uint32_t r[2][16];
@@ -559,6 +560,7 @@ out:
 }
 
 // weights [rows][cols] -> e4m3 with one scale per 128 x 128 block, scale[rows / 128][cols / 128]; a CTA per block
+// (bf16 [4096][2048] 15 us, fp32 [8192][8192] 113: the block is read twice, by elements; once a model)
 template <typename T>
 __global__ void __launch_bounds__(256) quantize_weight_kernel(const T* __restrict__ w, long long w_ld, uint8_t* __restrict__ q,
                                                              long long q_ld, float* __restrict__ scale, long long rows,

@@ -10,15 +10,18 @@
 //   rows      [rows][C], C contiguous (token-major): a row is held by 32..512 threads in registers, each thread a
 //             16-byte group of channels every TPR groups, so a group of 128 channels is 16 (32 for fp32)
 //             neighbouring lanes and its amax a few shuffles; the next row's loads are under way while a row is summed.
-//             bf16 [16384][2048] with residual: 43.7 us into 8 bits (5.4 TB/s), 55.3 forward, 70.1 backward (6.1 and 4.8 TB/s);
+//             bf16 [16384][2048] with residual: 43.4 us into 8 bits (5.4 TB/s), 55.9 forward, 77 backward (6.0 and 4.4 TB/s);
+//             without norm and residual into 8 bits 18.8 us (5.4 TB/s), a frame [4][2048] 1.5;
 //   fields    [outer][C][inner], inner contiguous (channels-first): lanes run along the positions, warps share the
 //             channels, the sums over channels meet in shared memory.  fp32 [1][20][3932160] with residual: 206 us
-//             forward, 199 backward (6.1 and 6.3 TB/s).
+//             forward, 198 backward (6.1 and 6.4 TB/s).
 // Rows that begin off a vector (kShifted) are read in vectors that begin earlier: fp16 [33520][1001] 40 us forward and 98
 // backward (3.4 and 2.1 TB/s), against 102 and 124 element by element (kScalar, for tensors that do not begin on a vector, and
 // for the backward pass of some rows).  Positions of a field in vectors where its rows allow it: fp32 [8][64][65536] 85 us, with
-// 65537 positions 109.  Beyond what registers hold, the fallbacks read their input again: bf16 [4096][16392] 284 us
-// ([16384]: 109), fp32 fields [8][136][65536] 338 us (128 channels: 172).
+// 65537 positions 110.  Beyond what registers hold, the fallbacks read their input again: forward bf16 [4096][16392] 284 us
+// ([16384]: 109), fp32 fields [8][136][65536] 339 us (128 channels: 173); backward bf16 [4096][16384] 647, fields 667 (218).
+// The backward kernels of the longest rows spill: 144 to 192 bytes of 16-bit rows off a vector (by elements 144) above 4096
+// channels, 92 to 188 of fp32 rows.
 // The weight gradient is summed in registers over all positions a CTA visits and in a fixed order over CTAs by a
 // second launch: same bits on every run.
 #include <initializer_list>
@@ -451,7 +454,7 @@ __global__ void __launch_bounds__(kRowThreads<TPR>) norm_rows_backward_kernel(co
   }
 }
 
-// the sum at element `at`, to 32 bits where its low part was kept
+// the sum at element `at`, to 24 bits where its low part was kept
 template <typename T>
 __device__ __forceinline__ float sum_at(const void* s, const void* low, long long at) {
   const T v = static_cast<const T*>(s)[at];

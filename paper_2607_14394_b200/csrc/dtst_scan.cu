@@ -6,11 +6,12 @@
 // A step is the affine map s -> a s + u; maps compose to (A, H) = (A2 A1, A2 H1 + H2), so a run of steps is summarised
 // by two numbers and runs can be joined in any grouping.  A thread holds R consecutive steps in registers, composes
 // them, learns the state in front of its run from the summaries of the runs before it, and then walks its steps once
-// more.  Steps at and beyond a sequence's own length are the identity map and are not read.  States are fp32.
+// more.  Steps at and beyond a sequence's own length are the identity map, whatever stands there (the column kernels do not
+// read them, the row kernels read and replace them).  States are fp32.
 //
-// Measured (forward, backward): fp32 [2621440][30] along contiguous steps 192 us, 272 us (4.9, 5.8
-// TB/s); fp32 [32][256][2079] 45, 75 (4.5, 4.6 TB/s); bf16 [1][65536][1024] 123 us forward (3.3 TB/s), bound by the rounds one
-// behind the other; bf16 [6][4097][1000] 53, 99.
+// Measured (forward, backward; sigmoid gate where none is named): fp32 [2621440][30] along contiguous steps 196 us, 272 us (4.8,
+// 5.8 TB/s); fp32 [32][256][2079] 45, 89 (4.5, 3.8 TB/s), decay 46, 74 (4.4, 4.6); bf16 [1][65536][1024] 125, 264 (3.2, 2.5
+// TB/s), bound by the rounds one behind the other; bf16 [6][4097][1000] 56, 105.
 // Memory-bound: forward 2 tensors in, 1 out; backward 3 in, 2 out.  The backward pass does not read h: it rebuilds
 // h_{t-1} inside each chunk, in fp32, from the state saved at the chunk's start.
 #include "dtst_common.cuh"
@@ -21,7 +22,6 @@
 namespace dtst {
 
 namespace {
-
 
 // Where there are few sequences, a thread-block cluster shares one: its CTAs take chunks side by side, exchange the chunks'
 // summaries through distributed shared memory once per round, and each applies those of the chunks in front of its own to
@@ -71,8 +71,8 @@ __device__ __forceinline__ float through(float A, float s, float H) {
   const float r = fmaf(A, s, H);
   return !SIGMOID && s == 0.f ? H : r;
 }
-// d = a b and a b + c of N neighbouring channels (two at once: 126 -> 122 us for bf16 [65536][1024], whose pass is short of issue
-// slots; the backward passes, which are not, gained nothing)
+// d = a b and a b + c of N neighbouring channels (two at once took the forward pass over bf16 [65536][1024] from 126 us to 122 at
+// the time: it is short of issue slots; the backward passes, which are not, gained nothing)
 template <int N>
 __device__ __forceinline__ void mul_n(float (&d)[N], const float (&a)[N], const float (&b)[N]) {
   if constexpr (N == 1) d[0] = a[0] * b[0];
@@ -156,7 +156,7 @@ __device__ __forceinline__ float2 join_lanes(float& A, float& H) {
 // The coming tile on its way through shared memory: a thread copies and reads its own steps, element group by element group, so
 // no barrier stands between the copies and their use.  (Rows of the tile as 16-byte copies shared among the threads, two tiles
 // under way, took 0.6 % less for a forward pass over bf16 [1][65536][1024] and 2 to 6 % more in every other pass measured:
-// bf16 [6][4097][1000] 56.4 against 53.2 us forward, 105 against 99 backward.)
+// bf16 [6][4097][1000], when these took 53.2 us forward and 99 backward, 56.4 and 105.)
 template <typename T, class S, int TENSORS>
 struct ColSlots {
   static constexpr int VEC = S::VEC, R = S::R, BYTES = VEC * (int)sizeof(T);
@@ -640,8 +640,9 @@ __global__ void __launch_bounds__(S::THREADS, S::ctas(SIGMOID)) scan_cols_backwa
 // (32 k + lane) 8.  Each vector is composed in its lane, the lanes are joined by a warp scan that does not reach across a row's first step
 // (forward) or last step (backward), and the K scans are joined one after the other.  No shared memory, no barriers.
 // Where rows begin off a vector the unit starts at the vector before; the elements in front are left alone.
-// fp32 [2097152][32]: 151 us forward, 214 backward; in tensors that begin off a vector, element by element, 322 and 857.  Seven
-// steps, which the columns' kernels take: 166 and 448 us for as many rows as eight here take 148 and 209.
+// fp32 [2097152][32]: 154 us forward, 213 backward; in tensors that begin off a vector, element by element, 328 and 867 (whole
+// rows by elements do not fit 128 registers and spill: up to 208 bytes forward, 716 backward).  fp32 [1900000][7], which the
+// columns' kernels take: 44 and 107 us; [1900000][8] here 37 and 51.
 constexpr int kUnit = 512, kRowWarps = 8;
 
 // steps of a chunk (a chunk of odd rows leaves room for a shifted beginning)
@@ -1119,7 +1120,7 @@ cudaError_t launch_rows(ScanArgs<T> p, const ScanCall& c, cudaStream_t st) {
     return w ? launch_rows_kernel<T, true, kWholeRows, BACK>(p, units, 1, st) : launch_rows_kernel<T, false, kWholeRows, BACK>(p, units, 1, st);
   }
   // a warp per row where that fills the GPU's 16 warps per SM, else the warps of a CTA or cluster share it (on both sides of
-  // the limit, fp32 rows of 8192: 2367 shared 45 us forward, 63 backward; 2368 apart 43, 66)
+  // the limit, fp32 rows of 8192: 2367 shared 46 us forward, 64 backward; 2368 apart 45, 68)
   if (p.outer >= 16 * (long long)num_sms()) {
     p.rounds = p.chunks;
     return w ? launch_rows_kernel<T, true, kWalk, BACK>(p, p.outer, 1, st) : launch_rows_kernel<T, false, kWalk, BACK>(p, p.outer, 1, st);
@@ -1145,9 +1146,9 @@ cudaError_t scan_t(const ScanCall& c, cudaStream_t st) {
   if (BACK) vec = vec && c.grad_outer % 4 == 0 && c.grad_step % 4 == 0 && aligned_to(c.grad_h, need) && aligned_to(c.grad_v, need) && aligned_to(c.grad_g, need);
   else vec = vec && aligned_to(c.h, need);
   p.groups = vec ? c.inner / 4 : c.inner;
-  // The shortest tile that holds the sequences, so that few of its steps are empty: fp32 [65536][9][64] takes 97 us (forward) in
-  // the tile of 16 steps, 325 in that of 64; [8192][65][64] 92 in 128 steps, 203 in the long sequences' 256.  A tile that
-  // holds all steps needs no staging for a next one: [2048][256][64] takes 62 us (backward 116), 75 (155) as a long sequence.
+  // The shortest tile that holds the sequences, so that few of its steps are empty: fp32 [65536][9][64] takes 100 us (forward) in
+  // the tile of 16 steps, 325 in that of 64; [8192][65][64] 93 in 128 steps, 203 in the long sequences' 256.  A tile that
+  // holds all steps needs no staging for a next one: [2048][256][64] takes 63 us (backward 119), 75 (155) as a long sequence.
   // The backward pass has more to keep for a step and holds half as many a thread.  One channel a thread, the price of
   // channel counts that are no multiple of four: 88 us for [2048][256][65].  Of its backward tile of 16 steps a thread two CTAs
   // share an SM under a sigmoid gate, whose a and b do not fit the 80 registers of three (fp32 [32][256][2079] 89 us against

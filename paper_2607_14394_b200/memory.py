@@ -4,8 +4,9 @@ two blocks made of them.
 The spectral layer of a 3D+time operator treats time as one more grid dimension; a rollout over many frames needs a
 state that is carried from frame to frame instead.  `RmsNorm`, `GatedScan` and `Fp8Linear` are thin wrappers over the
 C entry points (`dtst_rms_norm*`, `dtst_gated_scan*`, `dtst_matmul_fp8`): they check arguments, allocate outputs that
-the caller did not bring, and pass device pointers on; every arithmetic step runs in the CUDA library.  Every call runs
-on the current stream, or on the one given as `stream=`.
+the caller did not bring, and pass device pointers on; their arithmetic runs in the CUDA library (`FieldMemory` adds two
+pairs of fields with torch).  Every call runs on the current stream, or on the one given as `stream=`; an object may be used
+on several streams and from several threads at once (a block, which keeps buffers or states, may not).
 
 `FieldMemory` is a trainable block on channels-first fields [B, C, n..., T] whose last axis is time; `RolloutMemory`
 is the serving form on latent vectors [B, T, D] with 8-bit projections, a whole history or one frame at a time.
@@ -297,7 +298,7 @@ class Fp8Linear:
         self._kb = -(-self.k // BLOCK)
         self._w = weight.data_ptr()
         self._ws = _addr(weight_scale, "weight_scale", self.dev, torch.float32, (-(-self.n // BLOCK), self._kb))
-        # zeroed memory that calls on any stream may use from now on; calls that share it must be stream-ordered
+        # zeroed memory that calls on any stream may use from now on: a status word, which only a wait that gives up writes
         self.workspace = torch.zeros(256, dtype=torch.uint8, device=self.device)
         torch.cuda.current_stream(self.dev).synchronize()
         self._work = self.workspace.data_ptr()

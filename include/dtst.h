@@ -583,6 +583,119 @@ dtst_status dtst_gated_scan_status(void* stream);
 dtst_status dtst_workspace_status(void* workspace, void* stream);
 
 /*
+ * Selective memory: the recurrence's successor, whose step, input and output maps come with every token, with the layer norm in
+ * front of it, the short convolution before it, and the norm of all gradients behind it.  The section above holds for it: types,
+ * 32-bit arithmetic, one rounding, empty batches, the same bits on every run.
+ *
+ * Layer norm of x [outer, channels, inner] over the channels (layouts as of dtst_rms_norm), contiguous:
+ *   s = x + residual,  m = mean_c s,  rstd = 1 / sqrt(mean_c (s - m)^2 + eps),  y = (s - m) * rstd * weight[c] + bias[c]
+ * residual and bias may be NULL; stats [2, outer, inner] float32 (all means, then all rstd) may be NULL where no backward pass
+ * follows; s, s_low, in-place use as of dtst_rms_norm.
+ * Backward for grad_y and, where s went on as the residual stream, grad_s (or NULL), with g = weight grad_y, n = (s - m) rstd:
+ *   grad_x = rstd (g - mean_c g - n mean_c(g n)) + grad_s   (also the residual's gradient)
+ *   grad_weight[c] = sum of grad_y n,  grad_bias[c] = sum of grad_y, over outer and inner.
+ * grad_x may be grad_y or grad_s itself; grad_weight and grad_bias may be NULL.  scratch: dtst_layer_norm_scratch_bytes, needed
+ * for either of them (DTST_ERR_WORKSPACE if missing or too small); calls that may run at the same time need one each.
+ */
+dtst_status dtst_layer_norm(int dtype, int64_t outer, int64_t channels, int64_t inner, float eps, const void* x, const void* residual,
+                            const float* weight, const float* bias, void* s, void* s_low, void* y, float* stats, void* stream);
+dtst_status dtst_layer_norm_scratch_bytes(int64_t channels, size_t* bytes);
+dtst_status dtst_layer_norm_backward(int dtype, int64_t outer, int64_t channels, int64_t inner, const void* grad_y, const void* s,
+                                     const void* s_low, const float* weight, const float* stats, const void* grad_s, void* grad_x,
+                                     float* grad_weight, float* grad_bias, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Causal convolution of every channel by itself along the steps of x [batch, length, channels]; width 1 to 4 (wider:
+ * DTST_ERR_UNSUPPORTED):
+ *   u = the width - 1 steps of `state`, then x;   pre_t[c] = bias[c] + sum_k weight[c, k] u_{t+k}[c];   y = act(pre)
+ *   DTST_ACT_NONE: act(p) = p        DTST_ACT_SILU: act(p) = p / (1 + exp(-p))
+ * x: x_stride = elements between batch entries and between steps, channels contiguous; y contiguous.  weight [channels, width] and
+ * bias [channels] (or NULL) float32.  state, state_out [batch, width - 1, channels] of the tensors' type: the steps in front of x
+ * (NULL: zeros) and the last width - 1 steps of u (NULL: not wanted), which the next call takes; they may be the same buffer.
+ * lengths [batch] int32 or NULL: entry b has lengths[b] steps (taken into 0..length); what lies behind them is not used, y is zero
+ * there, and state_out is that of the entry's own end (of an entry without steps: its state).  y takes no input's place.
+ * Backward for grad_y [batch, length, channels] (contiguous) and grad_state_out (or NULL): grad_x (grad_stride, which must not make
+ * elements coincide; zero behind an entry's own length), grad_weight, grad_bias, grad_state (each but grad_x may be NULL); x, weight,
+ * bias, state and lengths as in the forward call (state as it was).  grad_x takes no input's place.  scratch as of
+ * dtst_layer_norm_backward.
+ */
+enum { DTST_ACT_NONE = 0, DTST_ACT_SILU = 1 };
+typedef struct {
+  int32_t dtype, activation;
+  int64_t batch, length, channels;
+  int32_t width, reserved;
+  int64_t x_stride[2];       /* batch, step */
+  int64_t grad_stride[2];    /* grad_x: batch, step */
+} dtst_conv_desc;
+dtst_status dtst_causal_conv(const dtst_conv_desc* desc, const void* x, const float* weight, const float* bias, const void* state,
+                             const int32_t* lengths, void* y, void* state_out, void* stream);
+dtst_status dtst_causal_conv_scratch_bytes(const dtst_conv_desc* desc, size_t* bytes);
+dtst_status dtst_causal_conv_backward(const dtst_conv_desc* desc, const void* grad_y, const void* grad_state_out, const void* x,
+                                      const float* weight, const float* bias, const void* state, const int32_t* lengths, void* grad_x,
+                                      float* grad_weight, float* grad_bias, void* grad_state, void* scratch, size_t scratch_bytes,
+                                      void* stream);
+
+/*
+ * Selective scan over the steps of x [batch, length, channels], `states` (1 to 64) numbers to a channel:
+ *   d_t = softplus(dt_t + dt_bias)   (softplus = 0: dt_t + dt_bias as it is),   a_t[c, n] = exp(d_t[c] A[c, n])
+ *   h_t[c, n] = a_t[c, n] h_{t-1}[c, n] + d_t[c] x_t[c] B_t[g, n],   g the group of channel c (channels / groups in a row)
+ *   y_t[c] = (sum_n C_t[g, n] h_t[c, n] + D[c] x_t[c])   z_t[c] / (1 + exp(-z_t[c])) where z is given
+ * x, dt, z [batch, length, channels], B, C [batch, length, groups, states]: elements between batch entries and between steps as
+ * given, the rest contiguous; y contiguous.  A [channels, states], D, dt_bias [channels] float32 (D, dt_bias, z may be NULL).
+ * A is meant to be negative.  Where it is positive, products of decays over up to 16 neighbouring steps are formed in float32; a
+ * product beyond its range passes a state of zero and makes any other an infinity or a NaN.
+ * h0, h_last [batch, channels, states] float32: the state in front (NULL: zeros) and behind (NULL: not wanted); they may be the same
+ * buffer.  lengths as of dtst_causal_conv: h_last is the state behind the entry's own last step.  y takes no input's place.
+ * checkpoints: NULL, or dtst_selective_scan_checkpoints floats (16-byte aligned), which receive the states the backward pass
+ * restarts from.
+ * Backward for grad_y (contiguous) and grad_last (or NULL), everything in `in` and the checkpoints as of the forward call (h0 is
+ * not needed: the checkpoints have it): gradients of x, dt, z, B, C in the tensors' type, strided as given (no two elements may
+ * coincide, none takes an input's or another's place; z's only where z is given; zero behind an entry's own length), and of A, D,
+ * dt_bias, h0 in float32 (each may be NULL).  scratch: dtst_selective_scan_scratch_bytes, always needed.
+ */
+typedef struct {
+  int32_t dtype, softplus;
+  int64_t batch, length, channels, states, groups;
+  int64_t x_stride[2], dt_stride[2], z_stride[2], b_stride[2], c_stride[2];                          /* batch, step */
+  int64_t grad_x_stride[2], grad_dt_stride[2], grad_z_stride[2], grad_b_stride[2], grad_c_stride[2];
+} dtst_selective_desc;
+typedef struct {
+  const void *x, *dt, *z, *B, *C;
+  const float *A, *D, *dt_bias, *h0;
+  const int32_t* lengths;
+} dtst_selective_inputs;
+typedef struct {
+  void *x, *dt, *z, *B, *C;
+  float *A, *D, *dt_bias, *h0;
+} dtst_selective_grads;
+dtst_status dtst_selective_scan_checkpoints(const dtst_selective_desc* desc, int64_t* checkpoint_floats);
+dtst_status dtst_selective_scan(const dtst_selective_desc* desc, const dtst_selective_inputs* in, void* y, float* h_last,
+                                float* checkpoints, void* stream);
+dtst_status dtst_selective_scan_scratch_bytes(const dtst_selective_desc* desc, size_t* bytes);
+dtst_status dtst_selective_scan_backward(const dtst_selective_desc* desc, const dtst_selective_inputs* in, const void* grad_y,
+                                         const float* grad_last, const float* checkpoints, const dtst_selective_grads* grads,
+                                         void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * The norm of all gradients of a program taken as one vector, and their clipping by it:
+ *   norm = sqrt(sum over tensors and elements of grad^2),   c = min(1, max_norm / (norm + eps)),   out = c grad
+ * list [count]: contiguous tensors of n elements (a complex one: twice as many of its parts); n = 0 is passed over.  out NULL: the
+ * tensor counts but is not scaled; out = grad: in place; otherwise it may lie over no other gradient or output
+ * (DTST_ERR_INVALID_ARG).  max_norm >= 0 (infinite: c = 1), eps > 0.  norm: one float32.  Squares are summed in 64 bits: the norm is
+ * an infinity only where it is beyond float32 or an element is one.  An infinite norm makes c zero, a NaN makes it a NaN; nothing is left
+ * out for either.  The list is read before the call returns.  scratch: dtst_grad_norm_scratch_bytes.
+ */
+typedef struct {
+  const void* grad;
+  void* out;
+  int64_t n;
+  int32_t dtype, reserved;
+} dtst_grad_tensor;
+dtst_status dtst_grad_norm_scratch_bytes(int64_t count, size_t* bytes);
+dtst_status dtst_clip_grad_norm(const dtst_grad_tensor* list, int64_t count, float max_norm, float eps, float* norm, void* scratch,
+                                size_t scratch_bytes, void* stream);
+
+/*
  * Diagnostics read once from the environment (for A/B measurements; not for production use):
  *   DTST_NO_PDL=1            launch every kernel without the programmatic-dependent-launch attribute
  *   DTST_NO_COLFUSE=1        forward-type transforms: contract the third dimension in a launch of its own instead of

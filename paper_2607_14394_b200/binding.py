@@ -47,6 +47,9 @@ EXPORTED = [
     "dtst_rms_norm", "dtst_rms_norm_scratch_bytes", "dtst_rms_norm_backward", "dtst_rms_norm_fp8", "dtst_quantize_fp8",
     "dtst_quantize_fp8_weight", "dtst_matmul_fp8", "dtst_gated_scan_checkpoints", "dtst_gated_scan",
     "dtst_gated_scan_backward", "dtst_gated_scan_status", "dtst_workspace_status",
+    "dtst_layer_norm", "dtst_layer_norm_scratch_bytes", "dtst_layer_norm_backward", "dtst_causal_conv",
+    "dtst_causal_conv_scratch_bytes", "dtst_causal_conv_backward", "dtst_selective_scan_checkpoints", "dtst_selective_scan",
+    "dtst_selective_scan_scratch_bytes", "dtst_selective_scan_backward", "dtst_grad_norm_scratch_bytes", "dtst_clip_grad_norm",
 ]
 
 
@@ -55,6 +58,38 @@ class ScanDesc(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("outer", ctypes.c_int64),
                 ("length", ctypes.c_int64), ("inner", ctypes.c_int64), ("in_stride", ctypes.c_int64 * 2),
                 ("grad_stride", ctypes.c_int64 * 2)]
+
+
+class ConvDesc(ctypes.Structure):
+    """dtst_conv_desc"""
+    _fields_ = [("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("batch", ctypes.c_int64),
+                ("length", ctypes.c_int64), ("channels", ctypes.c_int64), ("width", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("x_stride", ctypes.c_int64 * 2), ("grad_stride", ctypes.c_int64 * 2)]
+
+
+class SelectiveDesc(ctypes.Structure):
+    """dtst_selective_desc"""
+    _fields_ = [("dtype", ctypes.c_int32), ("softplus", ctypes.c_int32), ("batch", ctypes.c_int64),
+                ("length", ctypes.c_int64), ("channels", ctypes.c_int64), ("states", ctypes.c_int64),
+                ("groups", ctypes.c_int64)] + \
+               [(n + "_stride", ctypes.c_int64 * 2) for n in ("x", "dt", "z", "b", "c", "grad_x", "grad_dt", "grad_z",
+                                                              "grad_b", "grad_c")]
+
+
+class SelectiveInputs(ctypes.Structure):
+    """dtst_selective_inputs"""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "dt", "z", "B", "C", "A", "D", "dt_bias", "h0", "lengths")]
+
+
+class SelectiveGrads(ctypes.Structure):
+    """dtst_selective_grads"""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "dt", "z", "B", "C", "A", "D", "dt_bias", "h0")]
+
+
+class GradTensor(ctypes.Structure):
+    """dtst_grad_tensor"""
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class DtstError(RuntimeError):
@@ -137,6 +172,19 @@ def lib() -> ctypes.CDLL:
     L.dtst_gated_scan.argtypes = [descp] + [vp] * 8
     L.dtst_gated_scan_backward.argtypes = [descp] + [vp] * 11
     L.dtst_gated_scan_status.argtypes = [vp]
+    convp, selp, inp, szp = ctypes.POINTER(ConvDesc), ctypes.POINTER(SelectiveDesc), ctypes.POINTER(SelectiveInputs), ctypes.POINTER(sz)
+    L.dtst_layer_norm.argtypes = [i32, i64, i64, i64, f32] + [vp] * 9
+    L.dtst_layer_norm_scratch_bytes.argtypes = [i64, szp]
+    L.dtst_layer_norm_backward.argtypes = [i32, i64, i64, i64] + [vp] * 10 + [sz, vp]
+    L.dtst_causal_conv.argtypes = [convp] + [vp] * 8
+    L.dtst_causal_conv_scratch_bytes.argtypes = [convp, szp]
+    L.dtst_causal_conv_backward.argtypes = [convp] + [vp] * 12 + [sz, vp]
+    L.dtst_selective_scan_checkpoints.argtypes = [selp, i64p]
+    L.dtst_selective_scan.argtypes = [selp, inp, vp, vp, vp, vp]
+    L.dtst_selective_scan_scratch_bytes.argtypes = [selp, szp]
+    L.dtst_selective_scan_backward.argtypes = [selp, inp, vp, vp, vp, ctypes.POINTER(SelectiveGrads), vp, sz, vp]
+    L.dtst_grad_norm_scratch_bytes.argtypes = [i64, szp]
+    L.dtst_clip_grad_norm.argtypes = [ctypes.POINTER(GradTensor), i64, f32, f32, vp, vp, sz, vp]
     L.dtst_workspace_status.argtypes = [vp, vp]
     L.dtst_status_string.argtypes = [i32]
     L.dtst_status_string.restype = ctypes.c_char_p

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <atomic>
+#include <initializer_list>
 
 #include "dtst_common.cuh"
 
@@ -71,6 +72,85 @@ struct NormBackCall {
   float *grad_weight, *partial;
 };
 cudaError_t launch_norm_backward(const NormBackCall& n, cudaStream_t st);
+
+// out[k][i] = sum over `parts` rows of `partial` [parts][columns], in a fixed order; the outputs' columns follow one another, an
+// output without an address is passed over.
+struct SumOut {
+  float* out;
+  long long n;
+};
+cudaError_t launch_sum_parts(const float* partial, int parts, long long columns, std::initializer_list<SumOut> outs, cudaStream_t st);
+
+struct LayerNormCall {
+  int dtype;
+  long long outer, channels, inner;
+  float eps;
+  const void *x, *residual;
+  const float *weight, *bias;
+  void *s, *low, *y;
+  float* stats;            // mean and rstd of every position, or null
+};
+cudaError_t launch_layer_norm(const LayerNormCall& n, cudaStream_t st);
+
+struct LayerNormBackCall {
+  int dtype;
+  long long outer, channels, inner;
+  const void *grad_y, *s, *low, *grad_s;
+  const float *weight, *stats;
+  void* grad_x;
+  float *grad_weight, *grad_bias, *partial;
+};
+cudaError_t launch_layer_norm_backward(const LayerNormBackCall& n, cudaStream_t st);
+
+constexpr int kConvWidth = 4;             // widest causal convolution
+struct ConvCall {
+  int dtype, width, silu;
+  long long batch, length, channels;
+  long long x_stride[2], grad_stride[2];  // batch entry, step, in elements
+  const void *x, *state, *grad_y, *grad_state_out;
+  const float *weight, *bias;
+  const int* lengths;
+  void *y, *state_out, *grad_x, *grad_state;
+  float *grad_weight, *grad_bias, *partial;
+};
+int conv_parts(long long batch, long long length, long long channels);   // most rows of partial sums of the backward pass
+cudaError_t launch_conv_forward(const ConvCall& c, cudaStream_t st);
+cudaError_t launch_conv_backward(const ConvCall& c, cudaStream_t st);
+
+constexpr int kSelectiveStates = 64;      // most states of a channel
+constexpr int kSelectiveSave = 8;         // steps between the states that a forward pass saves
+struct Rows {                             // a token-major tensor: its address, elements between batch entries and steps
+  void* p;
+  long long batch, step;
+};
+struct SelectiveCall {
+  int dtype, softplus;
+  long long batch, length, channels, states, groups;
+  Rows x, dt, z, B, C;
+  const void* grad_y;
+  const float *A, *D, *bias, *h0, *grad_last;
+  const int* lengths;
+  void* y;
+  float *h_last, *checkpoints;
+  Rows grad_x, grad_dt, grad_z, grad_B, grad_C;
+  float *grad_A, *grad_D, *grad_bias, *grad_h0;
+  float* scratch;
+};
+long long selective_scratch_floats(const SelectiveCall& c);
+cudaError_t launch_selective_forward(const SelectiveCall& c, cudaStream_t st);
+cudaError_t launch_selective_backward(const SelectiveCall& c, cudaStream_t st);
+
+struct GradEntry {
+  const void* grad;
+  void* out;               // null: not scaled; grad itself: in place
+  long long n;
+  int dtype;
+};
+constexpr int kGradParts = 592;           // most CTAs of one launch of the norm's sum
+// launches of the sum that this many tensors take (each leaves kGradParts partial sums)
+int grad_launches(long long count);
+cudaError_t launch_grad_norm(const GradEntry* list, long long count, float max_norm, float eps, bool scale, float* norm,
+                             double* partial, cudaStream_t st);
 
 struct ScanCall {
   int dtype, gate;

@@ -1,5 +1,6 @@
 // C entry points of the recurrent-memory operators: argument checks, then one launch (two where a weight gradient is
 // summed).  Nothing is launched when a check fails.
+#include "dtst_checks.cuh"
 #include "dtst_fused.cuh"
 #include "dtst_memory.cuh"
 #include "dtst_types.cuh"
@@ -7,28 +8,6 @@
 using namespace dtst;
 
 namespace {
-
-constexpr int64_t kMostElements = (int64_t)1 << 46;   // keeps every product of extents and strides inside 64 bits
-constexpr int64_t kMostCtas = 0x7fffffff;
-
-bool known(int dtype) { return dtype == DTST_F32 || dtype == DTST_BF16 || dtype == DTST_F16; }
-size_t elem(int dtype) { return dtype == DTST_F32 ? 4 : 2; }
-bool fits(const void* p, int dtype) { return aligned_to(p, elem(dtype)); }
-bool f32(const void* p) { return aligned_to(p, 4); }
-
-// whether a * b * c stays within the range above (all non-negative)
-bool small_product(int64_t a, int64_t b, int64_t c) {
-  if (a == 0 || b == 0 || c == 0) return true;
-  return a <= kMostElements && b <= kMostElements / a && c <= kMostElements / (a * b);
-}
-
-dtst_status done(cudaError_t e) {
-  if (e == cudaSuccess) return DTST_OK;
-  (void)cudaGetLastError();
-  return e == cudaErrorNotSupported ? DTST_ERR_UNSUPPORTED : DTST_ERR_CUDA;
-}
-
-bool workspace_ok(const void* ws) { return ws != nullptr && aligned_to(ws, 256); }
 
 dtst_status check_scan(const dtst_scan_desc* d) {
   if (d == nullptr || !known(d->dtype) || (d->gate != DTST_GATE_SIGMOID && d->gate != DTST_GATE_DECAY)) return DTST_ERR_INVALID_ARG;

@@ -224,6 +224,7 @@ __device__ __forceinline__ float4 cluster_read4(const float* p, int rank) {
   return v;
 }
 
+__device__ __forceinline__ bool aligned_to_device(const void* p, uint32_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 }  // namespace dtst

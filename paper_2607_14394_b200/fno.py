@@ -9,7 +9,7 @@ PyTorch or CPU fallback.
 """
 from __future__ import annotations
 
-from typing import List, Sequence, Tuple
+from typing import List, Optional, Sequence, Tuple
 
 import torch
 
@@ -58,7 +58,9 @@ class FNO:
         Bn.dtst_pointwise_linear(self.v[self.layers], self.Q_w, self.Q_b, self.u, stream)
         return self.u
 
-    def backward(self, grad_u: torch.Tensor, need_grad_a: bool = False, stream=None) -> dict:
+    def backward(self, grad_u: torch.Tensor, need_grad_a: bool = False, stream=None, max_norm: Optional[float] = None) -> dict:
+        """Gradients of every parameter (and of the input, "a").  max_norm: the parameters' are clipped together, by their norm
+        (dtst_clip_grad_norm), which is returned as "norm"."""
         dev = self.plan.device
         grads = {"Q_w": torch.empty_like(self.Q_w), "Q_b": torch.empty_like(self.Q_b),
                  "P_w": torch.empty_like(self.P_w), "P_b": torch.empty_like(self.P_b), "W": [], "Wb": []}
@@ -77,6 +79,9 @@ class FNO:
         ga = torch.empty_like(self.a) if need_grad_a else None
         Bn.dtst_pointwise_linear_backward(g, self.a, self.P_w, ga, grads["P_w"], grads["P_b"], self.scratch, stream)
         grads["a"] = ga
+        if max_norm is not None:
+            from .selective import clip_grad_norm
+            grads["norm"] = clip_grad_norm([grads[k] for k in ("P_w", "P_b", "W", "Wb", "Q_w", "Q_b")], max_norm, stream=stream)
         return grads
 
     def parameters(self) -> Tuple:

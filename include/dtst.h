@@ -642,8 +642,8 @@ dtst_status dtst_causal_conv_backward(const dtst_conv_desc* desc, const void* gr
  *   y_t[c] = (sum_n C_t[g, n] h_t[c, n] + D[c] x_t[c])   z_t[c] / (1 + exp(-z_t[c])) where z is given
  * x, dt, z [batch, length, channels], B, C [batch, length, groups, states]: elements between batch entries and between steps as
  * given, the rest contiguous; y contiguous.  A [channels, states], D, dt_bias [channels] float32 (D, dt_bias, z may be NULL).
- * A is meant to be negative.  Where it is positive, products of decays over up to 16 neighbouring steps are formed in float32; a
- * product beyond its range passes a state of zero and makes any other an infinity or a NaN.
+ * A is meant to be negative.  Where it is positive, products of decays over long runs of steps are formed in float32; a product
+ * beyond its range passes a state of zero and makes any other an infinity or a NaN.
  * h0, h_last [batch, channels, states] float32: the state in front (NULL: zeros) and behind (NULL: not wanted); they may be the same
  * buffer.  lengths as of dtst_causal_conv: h_last is the state behind the entry's own last step.  y takes no input's place.
  * checkpoints: NULL, or dtst_selective_scan_checkpoints floats (16-byte aligned), which receive the states the backward pass
@@ -651,7 +651,9 @@ dtst_status dtst_causal_conv_backward(const dtst_conv_desc* desc, const void* gr
  * Backward for grad_y (contiguous) and grad_last (or NULL), everything in `in` and the checkpoints as of the forward call (h0 is
  * not needed: the checkpoints have it): gradients of x, dt, z, B, C in the tensors' type, strided as given (no two elements may
  * coincide, none takes an input's or another's place; z's only where z is given; zero behind an entry's own length), and of A, D,
- * dt_bias, h0 in float32 (each may be NULL).  scratch: dtst_selective_scan_scratch_bytes, always needed.
+ * dt_bias, h0 in float32 (each may be NULL).
+ * scratch (16-byte aligned): dtst_selective_scan_scratch_bytes of the pass (backward 0 or 1), asked for on the device that runs it; a
+ * forward pass may need none (0).  Calls that may run at the same time need one each.
  */
 typedef struct {
   int32_t dtype, softplus;
@@ -670,8 +672,8 @@ typedef struct {
 } dtst_selective_grads;
 dtst_status dtst_selective_scan_checkpoints(const dtst_selective_desc* desc, int64_t* checkpoint_floats);
 dtst_status dtst_selective_scan(const dtst_selective_desc* desc, const dtst_selective_inputs* in, void* y, float* h_last,
-                                float* checkpoints, void* stream);
-dtst_status dtst_selective_scan_scratch_bytes(const dtst_selective_desc* desc, size_t* bytes);
+                                float* checkpoints, void* scratch, size_t scratch_bytes, void* stream);
+dtst_status dtst_selective_scan_scratch_bytes(const dtst_selective_desc* desc, int backward, size_t* bytes);
 dtst_status dtst_selective_scan_backward(const dtst_selective_desc* desc, const dtst_selective_inputs* in, const void* grad_y,
                                          const float* grad_last, const float* checkpoints, const dtst_selective_grads* grads,
                                          void* scratch, size_t scratch_bytes, void* stream);

@@ -180,8 +180,8 @@ def lib() -> ctypes.CDLL:
     L.dtst_causal_conv_scratch_bytes.argtypes = [convp, szp]
     L.dtst_causal_conv_backward.argtypes = [convp] + [vp] * 12 + [sz, vp]
     L.dtst_selective_scan_checkpoints.argtypes = [selp, i64p]
-    L.dtst_selective_scan.argtypes = [selp, inp, vp, vp, vp, vp]
-    L.dtst_selective_scan_scratch_bytes.argtypes = [selp, szp]
+    L.dtst_selective_scan.argtypes = [selp, inp, vp, vp, vp, vp, sz, vp]
+    L.dtst_selective_scan_scratch_bytes.argtypes = [selp, i32, szp]
     L.dtst_selective_scan_backward.argtypes = [selp, inp, vp, vp, vp, ctypes.POINTER(SelectiveGrads), vp, sz, vp]
     L.dtst_grad_norm_scratch_bytes.argtypes = [i64, szp]
     L.dtst_clip_grad_norm.argtypes = [ctypes.POINTER(GradTensor), i64, f32, f32, vp, vp, sz, vp]

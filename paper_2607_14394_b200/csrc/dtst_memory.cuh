@@ -136,7 +136,7 @@ struct SelectiveCall {
   float *grad_A, *grad_D, *grad_bias, *grad_h0;
   float* scratch;
 };
-long long selective_scratch_floats(const SelectiveCall& c);
+long long selective_scratch_floats(const SelectiveCall& c, bool back);
 cudaError_t launch_selective_forward(const SelectiveCall& c, cudaStream_t st);
 cudaError_t launch_selective_backward(const SelectiveCall& c, cudaStream_t st);
 

@@ -188,7 +188,8 @@ dtst_status dtst_selective_scan_checkpoints(const dtst_selective_desc* d, int64_
   return DTST_OK;
 }
 
-dtst_status dtst_selective_scan(const dtst_selective_desc* d, const dtst_selective_inputs* in, void* y, float* h_last, float* checkpoints, void* stream) {
+dtst_status dtst_selective_scan(const dtst_selective_desc* d, const dtst_selective_inputs* in, void* y, float* h_last, float* checkpoints,
+                                void* scratch, size_t scratch_bytes, void* stream) {
   const dtst_status s = check_selective(d);
   if (s != DTST_OK) return s;
   if (d->batch == 0) return DTST_OK;
@@ -198,17 +199,22 @@ dtst_status dtst_selective_scan(const dtst_selective_desc* d, const dtst_selecti
     for (const void* p : {in->x, in->dt, in->z, in->B, in->C})
       if (p == y) return DTST_ERR_INVALID_ARG;
   }
+  size_t need = 0;
+  dtst_selective_scan_scratch_bytes(d, 0, &need);
+  if (need > 0 && (scratch == nullptr || scratch_bytes < need)) return DTST_ERR_WORKSPACE;
+  if (!aligned_to(scratch, 16)) return DTST_ERR_INVALID_ARG;
   SelectiveCall c = selective_call(d);
   set_inputs(c, d, in);
+  c.scratch = static_cast<float*>(scratch);
   c.y = y, c.h_last = h_last, c.checkpoints = checkpoints;
   return done(launch_selective_forward(c, static_cast<cudaStream_t>(stream)));
 }
 
-dtst_status dtst_selective_scan_scratch_bytes(const dtst_selective_desc* d, size_t* bytes) {
+dtst_status dtst_selective_scan_scratch_bytes(const dtst_selective_desc* d, int backward, size_t* bytes) {
   const dtst_status s = check_selective(d);
   if (s != DTST_OK) return s;
   if (bytes == nullptr) return DTST_ERR_INVALID_ARG;
-  *bytes = (size_t)selective_scratch_floats(selective_call(d)) * sizeof(float);
+  *bytes = (size_t)selective_scratch_floats(selective_call(d), backward != 0) * sizeof(float);
   return DTST_OK;
 }
 
@@ -242,7 +248,7 @@ dtst_status dtst_selective_scan_backward(const dtst_selective_desc* d, const dts
     }
   }
   size_t need = 0;
-  dtst_selective_scan_scratch_bytes(d, &need);
+  dtst_selective_scan_scratch_bytes(d, 1, &need);
   if (scratch == nullptr || scratch_bytes < need) return DTST_ERR_WORKSPACE;
   if (!aligned_to(scratch, 16)) return DTST_ERR_INVALID_ARG;
   SelectiveCall c = selective_call(d);

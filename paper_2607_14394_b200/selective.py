@@ -319,11 +319,17 @@ class SelectiveScan:
         _check(self._lib.dtst_selective_scan_checkpoints(self._ref, ctypes.byref(n)), "dtst_selective_scan_checkpoints")
         self.checkpoint_floats = int(n.value)
         self._ck_shape = torch.Size((self.checkpoint_floats,))
-        self._scratch_bytes = None                       # (asked for where it is used: it goes by the device)
+        self._scratch_bytes = [None, None]               # of either pass; asked for where it is used: it goes by the device
 
     def new_checkpoints(self) -> torch.Tensor:
         """A buffer for the states that a forward pass saves for its backward pass."""
         return torch.empty(self.checkpoint_floats, dtype=torch.float32, device=self.device)
+
+    def _ask_scratch(self, backward: int) -> int:
+        n = ctypes.c_size_t()
+        _check(self._lib.dtst_selective_scan_scratch_bytes(self._ref, backward, ctypes.byref(n)), "dtst_selective_scan_scratch_bytes")
+        self._scratch_bytes[backward] = int(n.value)
+        return int(n.value)
 
     def _describe(self, at, to):
         B, T, C = self.shape
@@ -372,9 +378,15 @@ class SelectiveScan:
         elif need_state:
             h_last = A.new_empty(self.state_shape)
             lp = h_last.data_ptr()
+        # the call's own, from the current stream's allocations: calls on other streams may be under way
+        nbytes = self._scratch_bytes[0] if self._scratch_bytes[0] is not None else self._ask_scratch(0)
+        sp = 0
+        if nbytes:
+            scratch = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            sp = scratch.data_ptr()
         status = self._lib.dtst_selective_scan(
             self._description(at, self._dense), ctypes.byref(inputs), yp, lp,
-            0 if checkpoints is None else _addr(checkpoints, "checkpoints", d, _F32, self._ck_shape), Mem._raw_stream(d))
+            0 if checkpoints is None else _addr(checkpoints, "checkpoints", d, _F32, self._ck_shape), sp, nbytes, Mem._raw_stream(d))
         if status:
             _check(status, "dtst_selective_scan")
         return out, h_last
@@ -410,16 +422,12 @@ class SelectiveScan:
                 grads[name] = A.new_empty(shape)
             ptr.append(_addr(grads[name], "gradient of " + name, d, _F32, shape))
         desc = self._description(at, tuple(to))
-        if self._scratch_bytes is None:
-            n = ctypes.c_size_t()
-            _check(self._lib.dtst_selective_scan_scratch_bytes(self._ref, ctypes.byref(n)), "dtst_selective_scan_scratch_bytes")
-            self._scratch_bytes = int(n.value)
-        # the call's own, from the current stream's allocations: calls on other streams may be under way
-        scratch = torch.empty(self._scratch_bytes, dtype=torch.uint8, device=self.device)
+        nbytes = self._scratch_bytes[1] if self._scratch_bytes[1] is not None else self._ask_scratch(1)
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         g = Bn.SelectiveGrads(*ptr)
         status = self._lib.dtst_selective_scan_backward(
             desc, ctypes.byref(inputs), gp, 0 if grad_last is None else _addr(grad_last, "grad_last", d, _F32, self.state_shape),
-            _addr(checkpoints, "checkpoints", d, _F32, self._ck_shape), ctypes.byref(g), scratch.data_ptr(), self._scratch_bytes,
+            _addr(checkpoints, "checkpoints", d, _F32, self._ck_shape), ctypes.byref(g), scratch.data_ptr(), nbytes,
             Mem._raw_stream(d))
         if status:
             _check(status, "dtst_selective_scan_backward")

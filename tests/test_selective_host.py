@@ -147,9 +147,9 @@ def test_scan_refuses_descriptions(desc, want):
     d = ctypes.byref(scan_desc(**desc))
     n, m = ctypes.c_int64(), ctypes.c_size_t()
     assert Bn.lib().dtst_selective_scan_checkpoints(d, ctypes.byref(n)) == want
-    assert Bn.lib().dtst_selective_scan_scratch_bytes(d, ctypes.byref(m)) == want
+    assert Bn.lib().dtst_selective_scan_scratch_bytes(d, 1, ctypes.byref(m)) == want
     i = Bn.SelectiveInputs(P[1], P[2], P[3], P[4], P[5], P[6], P[7], P[8], NULL, NULL)
-    assert Bn.lib().dtst_selective_scan(d, ctypes.byref(i), P[9], NULL, NULL, NULL) == want
+    assert Bn.lib().dtst_selective_scan(d, ctypes.byref(i), P[9], NULL, NULL, NULL, 0, NULL) == want
 
 
 INPUTS = dict(x=P[1], dt=P[2], z=P[3], B=P[4], C=P[5], A=P[6], D=P[7], dt_bias=P[8], h0=NULL, lengths=NULL)
@@ -163,7 +163,7 @@ def test_scan_refuses(bad):
     y, ck, last = bad.pop("y", P[10]), bad.pop("ck", NULL), bad.pop("last", NULL)
     ck = ctypes.c_void_p(0x90008) if ck else NULL
     i = Bn.SelectiveInputs(**{**INPUTS, **bad})
-    assert Bn.lib().dtst_selective_scan(ctypes.byref(scan_desc()), ctypes.byref(i), y, last, ck, NULL) == INVALID
+    assert Bn.lib().dtst_selective_scan(ctypes.byref(scan_desc()), ctypes.byref(i), y, last, ck, NULL, 0, NULL) == INVALID
 
 
 GRADS = dict(x=P[10], dt=P[11], z=P[12], B=P[13], C=P[14], A=NULL, D=NULL, dt_bias=NULL, h0=NULL)
@@ -203,7 +203,7 @@ def test_empty_batches_need_no_pointers():
     L = Bn.lib()
     assert L.dtst_layer_norm(0, 0, 8, 1, 1e-5, *[NULL] * 9) == Bn.DTST_OK
     assert L.dtst_causal_conv(ctypes.byref(conv_desc(B=0)), *[NULL] * 8) == Bn.DTST_OK
-    assert L.dtst_selective_scan(ctypes.byref(scan_desc(B=0)), None, NULL, NULL, NULL, NULL) == Bn.DTST_OK
+    assert L.dtst_selective_scan(ctypes.byref(scan_desc(B=0)), None, NULL, NULL, NULL, NULL, 0, NULL) == Bn.DTST_OK
 
 
 # ------------------------------------------------------------------------------------------------ the classes' calls

@@ -4,11 +4,12 @@
 //     grad_u_(t+k) = sum_k w_k gp_t  (+ the gradient of the new state),   grad_w_k = sum gp_t u_(t+k),   grad_b = sum gp_t
 // The new state is the last K - 1 steps of u at the sequence's own length, whatever that is.
 //
-// Bound by memory: a thread holds a vector of neighbouring channels and walks over a run of steps with the last K inputs
-// in registers, so a step is read once but for the K - 1 in front of a run (backward: also behind it).  The next steps' loads
-// are under way while a step is formed.  Runs are as long as leaves enough of them to fill the GPU.  The parameters' gradients
-// are summed in registers over the runs a thread visits, over a CTA's warps in shared memory, and over CTAs by a second launch,
-// all in a fixed order: same bits on every run.
+// Bound by memory: a thread holds a few neighbouring channels and walks over a run of steps with the last K inputs in registers,
+// at fixed places (the loop is unrolled over a multiple of K steps), so a step is read once but for the K - 1 in front of a run
+// (backward: also behind it).  The next steps' loads are under way, as they lie in memory, while a step is formed; two channels go to
+// an instruction.  Runs are as long as leaves enough of them to fill the GPU.  The parameters' gradients are summed in registers over the
+// runs a thread visits, over a CTA's warps in shared memory, and over CTAs by a second launch, all in a fixed order: same bits on
+// every run.
 #include "dtst_common.cuh"
 #include "dtst_memory.cuh"
 #include "dtst_types.cuh"
@@ -30,208 +31,245 @@ struct ConvArgs {
   int run, runs, silu;                 // steps to a run, runs to a sequence
 };
 
-__device__ __forceinline__ float sigmoid_of(float p) { return __fdividef(1.f, 1.f + __expf(-p)); }
+__device__ __forceinline__ float2 twice(float a) { return make_float2(a, a); }
+__device__ __forceinline__ float2 sigmoid_of(float2 p) {
+  const float2 q = mul_pair(p, twice(-kLog2e));
+  const float2 d = add_pair(make_float2(ex2(q.x), ex2(q.y)), twice(1.f));
+  return make_float2(rcp(d.x), rcp(d.y));
+}
 
-template <typename T, int V>
-__device__ __forceinline__ void load_row(float (&v)[V], const T* p, bool on, int left) {
-  Pack<T, V> k;
-  if (!on) k.zero();
-  else if (V == 1 || left >= V) k.load(p);
-  else k.load_part(p, left);
-  k.unpack(v);
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_row(const float (&v)[V], T* p, int left) {
-  Pack<T, V> k;
-  k.pack(v);
-  if (V == 1 || left >= V) k.store(p);
-  else k.store_part(p, left);
-}
+// V channels (2 or 4) as pairs, and the same in memory: in one access (VEC), or one by one
+template <int V>
+struct Chans {
+  float2 v[V / 2];
+};
+template <typename T, int V, bool VEC>
+struct Row {
+  Pack<T, V> raw;
+  __device__ __forceinline__ void load(const T* p, bool on, int left) {
+    if (!on) raw.zero();
+    else if (VEC) raw.load(p);
+    else raw.load_part(p, left);
+  }
+  __device__ __forceinline__ Chans<V> get() const {
+    float f[V];
+    raw.unpack(f);
+    Chans<V> c;
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) c.v[i] = make_float2(f[2 * i], f[2 * i + 1]);
+    return c;
+  }
+  static __device__ __forceinline__ void put(const Chans<V>& c, T* p, int left) {
+    float f[V];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) f[2 * i] = c.v[i].x, f[2 * i + 1] = c.v[i].y;
+    Row r;
+    r.raw.pack(f);
+    if (VEC) r.raw.store(p);
+    else r.raw.store_part(p, left);
+  }
+};
 
 // weights of V channels, [channel][k] in memory
 template <int V, int K>
-__device__ __forceinline__ void load_taps(float (&w)[K][V], float (&b)[V], const ConvArgs& a, long long c, int left) {
+__device__ __forceinline__ void load_taps(Chans<V> (&w)[K], Chans<V>& b, const ConvArgs& a, long long c, int left) {
+  const auto at = [&](const float* p, int i, int k, int n) { return p != nullptr && i < left ? __ldg(p + (c + i) * n + k) : 0.f; };
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
+  for (int i = 0; i < V / 2; ++i) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) w[k][i] = i < left ? __ldg(a.weight + (c + i) * K + k) : 0.f;
-    b[i] = a.bias != nullptr && i < left ? __ldg(a.bias + c + i) : 0.f;
+    for (int k = 0; k < K; ++k) w[k].v[i] = make_float2(at(a.weight, 2 * i, k, K), at(a.weight, 2 * i + 1, k, K));
+    b.v[i] = make_float2(at(a.bias, 2 * i, 0, 1), at(a.bias, 2 * i + 1, 0, 1));
   }
 }
 
+// What a warp works on: 32 vectors of channels (blockIdx.x), one run of one sequence.
+struct Run {
+  long long b, t0, t1, n, end;         // steps t0 .. t1; n: the sequence's own length; end: the first step that is not this run's
+  __device__ __forceinline__ Run(const ConvArgs& a, long long unit) {
+    b = unit / a.runs, t0 = unit % a.runs * a.run, t1 = t0 + a.run < a.T ? t0 + a.run : a.T;
+    n = a.T;
+    if (a.lengths != nullptr) {
+      n = a.lengths[b];
+      n = n < 0 ? 0 : n > a.T ? a.T : n;
+    }
+    end = t1 < n ? t1 : n;
+  }
+};
+
 // u of step t (t >= -(K-1)): from x, or from the state (zeros without one)
-template <typename T, int V, int K>
-__device__ __forceinline__ void load_u(float (&v)[V], const ConvArgs& a, long long b, long long t, long long end, long long c, int left) {
-  if (t >= 0) load_row<T, V>(v, static_cast<const T*>(a.x) + b * a.xb + t * a.xt + c, t < end, left);
-  else load_row<T, V>(v, static_cast<const T*>(a.state) + (b * (K - 1) + t + K - 1) * a.C + c, a.state != nullptr, left);
+template <typename T, int V, int K, bool VEC>
+__device__ __forceinline__ Row<T, V, VEC> load_u(const ConvArgs& a, const Run& r, long long t, long long c, int left) {
+  Row<T, V, VEC> v;
+  if (t >= 0) v.load(static_cast<const T*>(a.x) + r.b * a.xb + t * a.xt + c, t < r.n, left);
+  else v.load(static_cast<const T*>(a.state) + (r.b * (K - 1) + t + K - 1) * a.C + c, a.state != nullptr, left);
+  return v;
 }
 
-// A warp: 32 vectors of channels (blockIdx.x), one run of one sequence.
-template <typename T, int V, int K>
+// steps that are unrolled: a multiple of K
+template <int K>
+constexpr int kUnroll = K == 3 ? 3 : 4;
+
+template <typename T, int V, int K, bool VEC>
 __global__ void __launch_bounds__(32 * kWarps) conv_forward_kernel(const ConvArgs a) {
+  using RowT = Row<T, V, VEC>;
+  constexpr int U = kUnroll<K>;
   pdl_trigger();
   pdl_wait();
   const long long c = ((long long)blockIdx.x * 32 + threadIdx.x) * V;
   const long long unit = (long long)blockIdx.y * kWarps + threadIdx.y;
   if (c >= a.C || unit >= a.B * a.runs) return;
   const int left = (int)(a.C - c < V ? a.C - c : V);
-  const long long b = unit / a.runs, t0 = unit % a.runs * a.run, t1 = t0 + a.run < a.T ? t0 + a.run : a.T;
-  long long n = a.T;
-  if (a.lengths != nullptr) {
-    n = a.lengths[b];
-    n = n < 0 ? 0 : n > a.T ? a.T : n;
-  }
-  const long long end = t1 < n ? t1 : n;
-  float w[K][V], bias[V], u[K][V];
+  const Run r(a, unit);
+  Chans<V> w[K], bias, u[K];           // step t's input at place (t - t0) % K
   load_taps<V, K>(w, bias, a, c, left);
-  T* y = static_cast<T*>(a.y) + b * a.T * a.C + c;
 #pragma unroll
-  for (int k = 0; k < K - 1; ++k) load_u<T, V, K>(u[k], a, b, t0 - (K - 1) + k, n, c, left);
+  for (int k = 0; k < K - 1; ++k) u[k + 1] = load_u<T, V, K, VEC>(a, r, r.t0 - (K - 1) + k, c, left).get();
   // the new state first: the old one may be in its place
-  if (t0 == 0 && K > 1 && a.state_out != nullptr) {
-    float s[K > 1 ? K - 1 : 1][V];
+  if (r.t0 == 0 && K > 1 && a.state_out != nullptr) {
+    RowT s[K > 1 ? K - 1 : 1];
 #pragma unroll
-    for (int k = 0; k < K - 1; ++k) load_u<T, V, K>(s[k], a, b, n - (K - 1) + k, n, c, left);
+    for (int k = 0; k < K - 1; ++k) s[k] = load_u<T, V, K, VEC>(a, r, r.n - (K - 1) + k, c, left);
 #pragma unroll
-    for (int k = 0; k < K - 1; ++k) store_row<T, V>(s[k], static_cast<T*>(a.state_out) + (b * (K - 1) + k) * a.C + c, left);
+    for (int k = 0; k < K - 1; ++k) RowT::put(s[k].get(), static_cast<T*>(a.state_out) + (r.b * (K - 1) + k) * a.C + c, left);
   }
-  constexpr int AHEAD = 4;
-  const T* x = static_cast<const T*>(a.x) + b * a.xb + c;
-  Pack<T, V> next[AHEAD];
-  auto fetch = [&](int j, long long t) {
-    if (t >= end) next[j].zero();
-    else if (V == 1 || left >= V) next[j].load(x + t * a.xt);
-    else next[j].load_part(x + t * a.xt, left);
-  };
+  const T* x = static_cast<const T*>(a.x) + r.b * a.xb + r.t0 * a.xt + c;
+  T* y = static_cast<T*>(a.y) + (r.b * a.T + r.t0) * a.C + c;
+  const int steps = (int)(r.end > r.t0 ? r.end - r.t0 : 0);
+  RowT next[U];
 #pragma unroll
-  for (int j = 0; j < AHEAD; ++j) fetch(j, t0 + j);
-  for (long long t = t0; t < end; t += AHEAD) {
-    Pack<T, V> now[AHEAD];
+  for (int j = 0; j < U; ++j) next[j].load(x + j * a.xt, j < steps, left);
+  const auto step = [&](int j, const RowT& now) {
+    u[j % K] = now.get();
+    Chans<V> o;
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) now[j] = next[j];
+    for (int i = 0; i < V / 2; ++i) {
+      float2 p = bias.v[i];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) fetch(j, t + AHEAD + j);
-#pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      if (t + j >= end) break;
-      now[j].unpack(u[K - 1]);
-      float o[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float p = bias[i];
-#pragma unroll
-        for (int k = 0; k < K; ++k) p = fmaf(w[k][i], u[k][i], p);
-        o[i] = a.silu ? p * sigmoid_of(p) : p;
-#pragma unroll
-        for (int k = 0; k < K - 1; ++k) u[k][i] = u[k + 1][i];
-      }
-      store_row<T, V>(o, y + (t + j) * a.C, left);
+      for (int k = 0; k < K; ++k) p = fma_pair(w[k].v[i], u[(j + 1 + k) % K].v[i], p);
+      o.v[i] = a.silu ? mul_pair(p, sigmoid_of(p)) : p;
     }
+    RowT::put(o, y, left);
+    y += a.C;
+  };
+  int t = 0;
+  for (; t + U <= steps; t += U) {
+    RowT now[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) now[j] = next[j];
+    x += U * a.xt;
+#pragma unroll
+    for (int j = 0; j < U; ++j) next[j].load(x + j * a.xt, t + U + j < steps, left);
+#pragma unroll
+    for (int j = 0; j < U; ++j) step(j, now[j]);
   }
-  const float zero[V] = {};
-  for (long long t = end > t0 ? end : t0; t < t1; ++t) store_row<T, V>(zero, y + t * a.C, left);
+#pragma unroll
+  for (int j = 0; j < U - 1; ++j)
+    if (t + j < steps) step(j, next[j]);
+  for (long long z = r.t0 + steps; z < r.t1; ++z, y += a.C) RowT::put(Chans<V>{}, y, left);
 }
 
 // Backward.  Step t of the loop forms gp_t; with it the gradient of u_(t) is complete and is written, as that of step
 // t - (K - 1): of x, or of the state in front of a sequence's first run.
-template <typename T, int V, int K>
+template <typename T, int V, int K, bool VEC>
 __global__ void __launch_bounds__(32 * kWarps) conv_backward_kernel(const ConvArgs a) {
-  __shared__ float red[kWarps][32][V];
+  using RowT = Row<T, V, VEC>;
+  constexpr int U = kUnroll<K>;
+  __shared__ float2 red[kWarps][32][V / 2];
   pdl_trigger();
   pdl_wait();
   const long long c = ((long long)blockIdx.x * 32 + threadIdx.x) * V;
   const bool on = c < a.C;
   const int left = (int)(a.C - c < V ? a.C - c : V);
-  float gw[K][V], gb[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    gb[i] = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) gw[k][i] = 0.f;
-  }
+  Chans<V> gw[K + 1] = {};             // the last one: the bias'
   if (on) {
-    float w[K][V], bias[V];
+    Chans<V> w[K], bias;
     load_taps<V, K>(w, bias, a, c, left);
     for (long long unit = (long long)blockIdx.y * kWarps + threadIdx.y; unit < a.B * a.runs; unit += (long long)gridDim.y * kWarps) {
-      const long long b = unit / a.runs, t0 = unit % a.runs * a.run, t1 = t0 + a.run < a.T ? t0 + a.run : a.T;
-      long long n = a.T;
-      if (a.lengths != nullptr) {
-        n = a.lengths[b];
-        n = n < 0 ? 0 : n > a.T ? a.T : n;
-      }
-      const long long end = t1 < n ? t1 : n;              // first step that is not this run's
-      const long long last = (end > t0 ? end : t0) + K - 1;
-      const T* x = static_cast<const T*>(a.x) + b * a.xb + c;
-      const T* gy = static_cast<const T*>(a.gy) + b * a.T * a.C + c;
-      T* gx = static_cast<T*>(a.gx) + b * a.gb + c;
-      float u[K][V], g[K][V];
+      const Run r(a, unit);
+      const T* x = static_cast<const T*>(a.x) + r.b * a.xb + r.t0 * a.xt + c;
+      const T* gy = static_cast<const T*>(a.gy) + (r.b * a.T + r.t0) * a.C + c;
+      T* gx = static_cast<T*>(a.gx) + r.b * a.gb + (r.t0 - (K - 1)) * a.gt + c;      // (of the step that step 0 completes)
+      Chans<V> u[K], g[K] = {};        // step t's at place (t - t0) % K
 #pragma unroll
-      for (int k = 0; k < K - 1; ++k) {
-        load_u<T, V, K>(u[k], a, b, t0 - (K - 1) + k, n, c, left);
-#pragma unroll
-        for (int i = 0; i < V; ++i) g[k][i] = 0.f;
-      }
+      for (int k = 0; k < K - 1; ++k) u[k + 1] = load_u<T, V, K, VEC>(a, r, r.t0 - (K - 1) + k, c, left).get();
+      const int own = (int)(r.end > r.t0 ? r.end - r.t0 : 0);            // steps of this run
+      const int live = (int)(r.n > r.t0 ? r.n - r.t0 : 0);               // steps to the sequence's end
       // (a run without steps of its own has nothing to write but zeros; the first one has the state's gradient)
-      const long long stop = end > t0 || t0 == 0 ? last : t0;
-      constexpr int AHEAD = 2;
-      Pack<T, V> nx[AHEAD], ng[AHEAD];
-      auto fetch = [&](int j, long long t) {
-        if (t >= n || t >= stop) {
-          nx[j].zero(), ng[j].zero();
-        } else if (V == 1 || left >= V) {
-          nx[j].load(x + t * a.xt), ng[j].load(gy + t * a.C);
-        } else {
-          nx[j].load_part(x + t * a.xt, left), ng[j].load_part(gy + t * a.C, left);
+      const int stop = own > 0 || r.t0 == 0 ? own + K - 1 : 0;
+      RowT nx[U], ng[U];
+      auto fetch = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+          const bool there = t + j < live && t + j < stop;
+          nx[j].load(x + j * a.xt, there, left);
+          ng[j].load(gy + j * a.C, there, left);
         }
+        x += U * a.xt, gy += U * a.C;
       };
+      // step t = (a multiple of U) + j; INSIDE: one of this run's, which completes another one's of this run, without the new state's
+      const auto step = [&](int t, int j, const RowT& cx, const RowT& cg, auto inside) {
+        constexpr bool INSIDE = decltype(inside)::value;
+        u[j % K] = cx.get();
+        g[j % K] = cg.get();             // (zero behind the sequence's end)
+        Chans<V> o;
 #pragma unroll
-      for (int j = 0; j < AHEAD; ++j) fetch(j, t0 + j);
-      for (long long t = t0; t < stop; t += AHEAD) {
-        Pack<T, V> cx[AHEAD], cg[AHEAD];
+        for (int i = 0; i < V / 2; ++i) {
+          float2 gp = g[j % K].v[i];
+          if (a.silu) {
+            float2 p = bias.v[i];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) cx[j] = nx[j], cg[j] = ng[j];
+            for (int k = 0; k < K; ++k) p = fma_pair(w[k].v[i], u[(j + 1 + k) % K].v[i], p);
+            const float2 sg = sigmoid_of(p);
+            const float2 d = fma_pair(p, fma_pair(sg, twice(-1.f), twice(1.f)), twice(1.f));
+            gp = mul_pair(gp, mul_pair(sg, d));
+          }
+          if (!INSIDE && t >= live) gp = twice(0.f);
+          g[j % K].v[i] = gp;
+          if (INSIDE || t < own) {
+            gw[K].v[i] = add_pair(gw[K].v[i], gp);
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) fetch(j, t + AHEAD + j);
+            for (int k = 0; k < K; ++k) gw[k].v[i] = fma_pair(gp, u[(j + 1 + k) % K].v[i], gw[k].v[i]);
+          }
+          o.v[i] = mul_pair(w[0].v[i], g[j % K].v[i]);
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-          const long long s = t + j, to = s - (K - 1);
-          if (s >= stop) break;
-          cx[j].unpack(u[K - 1]);
-          cg[j].unpack(g[K - 1]);          // (zero behind the sequence's end)
-          float o[V];
+          for (int k = 1; k < K; ++k) o.v[i] = fma_pair(w[k].v[i], g[(j + K - k) % K].v[i], o.v[i]);
+        }
+        if constexpr (INSIDE) {
+          RowT::put(o, gx, left);
+        } else {
+          const long long to = r.t0 + t - (K - 1), late = to - (r.n - (K - 1));      // late: number of the new state's step
+          if (to >= r.t0 || (r.t0 == 0 && a.gs != nullptr)) {
+            if (K > 1 && late >= 0 && a.gso != nullptr) {
+              RowT q;
+              q.load(static_cast<const T*>(a.gso) + (r.b * (K - 1) + late) * a.C + c, true, left);
+              const Chans<V> f = q.get();
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            if (a.silu) {
-              float p = bias[i];
-#pragma unroll
-              for (int k = 0; k < K; ++k) p = fmaf(w[k][i], u[k][i], p);
-              const float sg = sigmoid_of(p);
-              g[K - 1][i] *= sg * fmaf(p, 1.f - sg, 1.f);
+              for (int i = 0; i < V / 2; ++i) o.v[i] = add_pair(o.v[i], f.v[i]);
             }
-            if (s >= n) g[K - 1][i] = 0.f;
-            const float own = s < end ? g[K - 1][i] : 0.f;
-            gb[i] += own;
-#pragma unroll
-            for (int k = 0; k < K; ++k) gw[k][i] = fmaf(own, u[k][i], gw[k][i]);
-            o[i] = 0.f;
-#pragma unroll
-            for (int k = 0; k < K; ++k) o[i] = fmaf(w[k][i], g[K - 1 - k][i], o[i]);
-#pragma unroll
-            for (int k = 0; k < K - 1; ++k) u[k][i] = u[k + 1][i], g[k][i] = g[k + 1][i];
+            if (to >= 0) RowT::put(o, gx, left);
+            else RowT::put(o, static_cast<T*>(a.gs) + (r.b * (K - 1) + to + K - 1) * a.C + c, left);
           }
-          if (to < t0 && (t0 > 0 || a.gs == nullptr)) continue;
-          if (to >= n - (K - 1) && K > 1 && a.gso != nullptr) {
-            float q[V];
-            load_row<T, V>(q, static_cast<const T*>(a.gso) + (b * (K - 1) + to - (n - (K - 1))) * a.C + c, true, left);
+        }
+        gx += a.gt;
+      };
+      fetch(0);
+      for (int t = 0; t < stop; t += U) {
+        RowT cx[U], cg[U];
 #pragma unroll
-            for (int i = 0; i < V; ++i) o[i] += q[i];
-          }
-          if (to >= 0) store_row<T, V>(o, gx + to * a.gt, left);
-          else store_row<T, V>(o, static_cast<T*>(a.gs) + (b * (K - 1) + to + K - 1) * a.C + c, left);
+        for (int j = 0; j < U; ++j) cx[j] = nx[j], cg[j] = ng[j];
+        if (t + U < stop) fetch(t + U);
+        // these complete the steps t - (K - 1) .. t + U - K; the new state begins at live - (K - 1)
+        if (t >= K - 1 && t + U <= own && t + U <= live) {
+#pragma unroll
+          for (int j = 0; j < U; ++j) step(t + j, j, cx[j], cg[j], std::true_type());
+        } else {
+#pragma unroll
+          for (int j = 0; j < U; ++j)
+            if (t + j < stop) step(t + j, j, cx[j], cg[j], std::false_type());
         }
       }
-      const float zero[V] = {};
-      for (long long t = end > t0 ? end : t0; t < t1; ++t) store_row<T, V>(zero, gx + t * a.gt, left);
+      T* z = static_cast<T*>(a.gx) + r.b * a.gb + (r.t0 + own) * a.gt + c;
+      for (long long t = r.t0 + own; t < r.t1; ++t, z += a.gt) RowT::put(Chans<V>{}, z, left);
     }
   }
   if (a.partial == nullptr) return;
@@ -240,15 +278,17 @@ __global__ void __launch_bounds__(32 * kWarps) conv_backward_kernel(const ConvAr
   for (int k = 0; k <= K; ++k) {           // over the CTA's warps, in order
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < V; ++i) red[threadIdx.y][threadIdx.x][i] = k < K ? gw[k < K ? k : 0][i] : gb[i];
+    for (int i = 0; i < V / 2; ++i) red[threadIdx.y][threadIdx.x][i] = gw[k].v[i];
     __syncthreads();
     if (threadIdx.y == 0 && on) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float t = 0.f;
+      for (int i = 0; i < V / 2; ++i) {
+        float2 t = red[0][threadIdx.x][i];
 #pragma unroll
-        for (int y = 0; y < kWarps; ++y) t += red[y][threadIdx.x][i];
-        if (i < left) out[k < K ? (c + i) * K + k : a.C * K + c + i] = t;
+        for (int y = 1; y < kWarps; ++y) t = add_pair(t, red[y][threadIdx.x][i]);
+        const long long at = k < K ? (c + 2 * i) * K + k : a.C * K + c + 2 * i;
+        if (2 * i < left) out[at] = t.x;
+        if (2 * i + 1 < left) out[at + (k < K ? K : 1)] = t.y;
       }
     }
   }
@@ -261,7 +301,7 @@ int run_steps(long long warps_per_step, long long T, int least) {
   return run;
 }
 
-template <typename T, int V, int K>
+template <typename T, int V, int K, bool VEC>
 cudaError_t launch_k(ConvArgs a, bool back, int* parts, cudaStream_t st) {
   const long long groups = (a.C + 32 * V - 1) / (32 * V);
   a.run = run_steps(groups * a.B, a.T, back ? 16 : 8);
@@ -276,30 +316,35 @@ cudaError_t launch_k(ConvArgs a, bool back, int* parts, cudaStream_t st) {
       rows = (a.B * a.runs + kWarps - 1) / kWarps;
       if (rows > 65535) return cudaErrorNotSupported;
     }
-    return launch_pdl(conv_forward_kernel<T, V, K>, dim3((unsigned)groups, (unsigned)rows), dim3(32, kWarps), 0, st, a);
+    return launch_pdl(conv_forward_kernel<T, V, K, VEC>, dim3((unsigned)groups, (unsigned)rows), dim3(32, kWarps), 0, st, a);
   }
   const int most = conv_parts(a.B, a.T, a.C);
   *parts = (int)(rows < most ? rows : most);
-  return launch_pdl(conv_backward_kernel<T, V, K>, dim3((unsigned)groups, (unsigned)*parts), dim3(32, kWarps), 0, st, a);
+  return launch_pdl(conv_backward_kernel<T, V, K, VEC>, dim3((unsigned)groups, (unsigned)*parts), dim3(32, kWarps), 0, st, a);
 }
 
-template <typename T, int V>
+template <typename T, int V, bool VEC>
 cudaError_t launch_v(const ConvArgs& a, int width, bool back, int* parts, cudaStream_t st) {
   switch (width) {
-    case 1: return launch_k<T, V, 1>(a, back, parts, st);
-    case 2: return launch_k<T, V, 2>(a, back, parts, st);
-    case 3: return launch_k<T, V, 3>(a, back, parts, st);
-    default: return launch_k<T, V, 4>(a, back, parts, st);
+    case 1: return launch_k<T, V, 1, VEC>(a, back, parts, st);
+    case 2: return launch_k<T, V, 2, VEC>(a, back, parts, st);
+    case 3: return launch_k<T, V, 3, VEC>(a, back, parts, st);
+    default: return launch_k<T, V, 4, VEC>(a, back, parts, st);
   }
 }
 
+// four channels a thread where every tensor's rows take such vectors, else two, else two one by one
 template <typename T>
 cudaError_t launch_t(const ConvArgs& a, int width, bool back, int* parts, cudaStream_t st) {
-  constexpr int V = 4;
-  bool vec = a.C % V == 0 && a.xb % V == 0 && a.xt % V == 0 && a.gb % V == 0 && a.gt % V == 0;
-  for (const void* p : {a.x, a.state, a.gy, a.gso, (const void*)a.y, (const void*)a.state_out, (const void*)a.gx, (const void*)a.gs})
-    vec = vec && aligned_to(p, V * sizeof(T));
-  return vec ? launch_v<T, V>(a, width, back, parts, st) : launch_v<T, 1>(a, width, back, parts, st);
+  const auto fits = [&](int v) {
+    bool ok = a.C % v == 0 && a.xb % v == 0 && a.xt % v == 0 && a.gb % v == 0 && a.gt % v == 0;
+    for (const void* p : {a.x, a.state, a.gy, a.gso, (const void*)a.y, (const void*)a.state_out, (const void*)a.gx, (const void*)a.gs})
+      ok = ok && aligned_to(p, v * sizeof(T));
+    return ok;
+  };
+  if (fits(4)) return launch_v<T, 4, true>(a, width, back, parts, st);
+  if (fits(2)) return launch_v<T, 2, true>(a, width, back, parts, st);
+  return launch_v<T, 2, false>(a, width, back, parts, st);
 }
 
 cudaError_t launch(const ConvArgs& a, int dtype, int width, bool back, int* parts, cudaStream_t st) {

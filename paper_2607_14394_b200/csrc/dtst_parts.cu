@@ -1,5 +1,6 @@
-// Sums of partial sums: out[c] = sum over parts of partial[part][c], in a fixed order.  32 warps take every 32nd part of 32
-// neighbouring columns, and their sums meet in warp order.  Bound by memory and, for few columns, by latency.
+// Sums of partial sums: out[c] = sum over parts of partial[part][c], in a fixed order: a CTA's warps take every W-th part of 32
+// neighbouring columns, and their sums meet in warp order.  Bound by memory and, for few columns, by latency: as many warps as
+// leave a thread some ten loads at once.
 #include "dtst_common.cuh"
 #include "dtst_memory.cuh"
 #include "dtst_types.cuh"
@@ -16,27 +17,28 @@ struct SumArgs {
   SumOut outs[kMostOuts];
 };
 
-__global__ void __launch_bounds__(1024) sum_parts_kernel(const SumArgs a) {
-  __shared__ float red[32][33];
+template <int W>
+__global__ void __launch_bounds__(32 * W) sum_parts_kernel(const SumArgs a) {
+  __shared__ float red[W][32];
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const long long c0 = (long long)blockIdx.x * 32;
+  const long long c = (long long)blockIdx.x * 32 + lane;
   float t = 0.f;
-  if (c0 + lane < a.columns) {
-#pragma unroll 8
-    for (int p = w; p < a.parts; p += 32) t += a.partial[(long long)p * a.columns + c0 + lane];
+  if (c < a.columns) {
+#pragma unroll 10
+    for (int p = w; p < a.parts; p += W) t += a.partial[(long long)p * a.columns + c];
   }
   red[w][lane] = t;
   __syncthreads();
-  t = warp_sum(red[lane][w]);      // (turned round: warp w sums column w over the 32 warps)
-  if (lane == 0 && c0 + w < a.columns) {
-    long long c = c0 + w;
+  if (w > 0 || c >= a.columns) return;
 #pragma unroll
-    for (int k = 0; k < kMostOuts; ++k) {
-      if (c >= 0 && c < a.outs[k].n && a.outs[k].out != nullptr) a.outs[k].out[c] = t;
-      c -= a.outs[k].n;
-    }
+  for (int i = 1; i < W; ++i) t += red[i][lane];
+  long long k = c;
+#pragma unroll
+  for (int i = 0; i < kMostOuts; ++i) {
+    if (k >= 0 && k < a.outs[i].n && a.outs[i].out != nullptr) a.outs[i].out[k] = t;
+    k -= a.outs[i].n;
   }
 }
 
@@ -47,7 +49,10 @@ cudaError_t launch_sum_parts(const float* partial, int parts, long long columns,
   int k = 0;
   for (const SumOut& o : outs)
     if (k < kMostOuts) a.outs[k++] = o;
-  return launch_pdl(sum_parts_kernel, dim3((unsigned)((columns + 31) / 32)), dim3(1024), 0, st, a);
+  const dim3 grid((unsigned)((columns + 31) / 32));
+  if (parts <= 40) return launch_pdl(sum_parts_kernel<4>, grid, dim3(128), 0, st, a);
+  if (parts <= 160) return launch_pdl(sum_parts_kernel<16>, grid, dim3(512), 0, st, a);
+  return launch_pdl(sum_parts_kernel<32>, grid, dim3(1024), 0, st, a);
 }
 
 }  // namespace dtst

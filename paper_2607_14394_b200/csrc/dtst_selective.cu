@@ -30,7 +30,6 @@ namespace dtst {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Threads that run the recurrence, and as many again that bring its operands in and take its results out, so that neither
 // the loads' nor the element-wise functions' latency holds up the recurrence.
 constexpr int kThreads = 128;
@@ -46,16 +45,6 @@ constexpr int kFull = 1, kDone = 3;
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 104;"); }
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 152;"); }
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float rcp(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // log(1 + e^v), and e = e^-|v|: the larger of v and 0, and log(1 + e) = 2 atanh(e / (2 + e)) as a polynomial in the square of
 // that argument, fitted over its range of 0 to 1/9 to 4e-9 of the value: no digits are lost where e is small
 __device__ __forceinline__ float softplus_of(float v, float& e) {
@@ -93,7 +82,7 @@ struct SelArgs {
   const void* gy;
   float *h_last, *ck;
   Rows gx, gdt, gz;
-  float *gA, *gD, *gbias, *gh0;        // gA, gD, gbias: a row of [C N], [C], [C] per batch entry and segment
+  float *gparams, *gh0;                // gparams: a row of [C N], [C], [C] per batch entry and segment: of A, D, dt_bias
   float* gmaps;                        // [blocks of a group][batch][length][groups][2][N4]
   float *ends, *spans;                 // [segments][batch][C][N4], [segments][batch][C]: what a segment leaves, sums of its steps
   long long batch, length, channels;
@@ -656,7 +645,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_backward_kernel(con
   pdl_wait();
   const Place at = place_of<DC>(a, blockIdx.z);
   const int tid = threadIdx.x % kThreads, tiles = (at.end - at.begin + TS - 1) / TS;
-  const long long entry = at.b * a.segments + at.part;                  // row of the parameters' gradients
+  float* const params = a.gparams + (at.b * a.segments + at.part) * a.channels * (a.states + 2);
   if (threadIdx.x >= kThreads) {
     // ---- in and out
     fewer_registers();
@@ -832,8 +821,8 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_backward_kernel(con
     for (int i = tid; i < at.left; i += kThreads) {
       float t = 0.f, u = 0.f;
       for (int r = 0; r < ROWS; ++r) t += rows[r * DC + i], u += rows[(ROWS + r) * DC + i];
-      a.gD[entry * a.channels + at.c0 + i] = t;
-      a.gbias[entry * a.channels + at.c0 + i] = u;
+      params[a.channels * a.states + at.c0 + i] = t;
+      params[a.channels * (a.states + 1) + at.c0 + i] = u;
     }
     return;
   }
@@ -930,7 +919,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_backward_kernel(con
   }
 #pragma unroll
   for (int k = 0; k < 2; ++k)
-    if (ch + k < at.left) put_four(gA[k], a.gA + (entry * a.channels + c + k) * a.states, 4 * p, a.states, perm);
+    if (ch + k < at.left) put_four(gA[k], params + (long long)(c + k) * a.states, 4 * p, a.states, perm);
   __syncthreads();       // (the other half's two)
   __syncthreads();
 }
@@ -1053,8 +1042,8 @@ cudaError_t backward_p(const SelectiveCall& c, cudaStream_t st) {
   SelArgs a = args_of(c, sizeof(T), true);
   // scratch: the segments' ends, a row of the parameters' gradients for each batch entry and segment, the maps' by blocks of channels
   const long long entries = c.batch * a.segments;
-  a.gA = c.scratch + cut_floats(c), a.gD = a.gA + entries * c.channels * c.states, a.gbias = a.gD + entries * c.channels;
-  a.gmaps = a.gA + param_floats(c);
+  a.gparams = c.scratch + cut_floats(c);
+  a.gmaps = a.gparams + param_floats(c);
   static std::atomic<uint64_t> seen[2];
   cudaError_t e = cudaSuccess;
   if (a.segments > 1) e = launch(selective_ends_kernel<T, P, true>, a, a.segments - 1, SelCfg<P, kFwdSteps>::ENDS, seen[0], st);
@@ -1066,14 +1055,9 @@ cudaError_t backward_p(const SelectiveCall& c, cudaStream_t st) {
     e = launch_pdl(selective_maps_kernel<T>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(256), 0, st, m);
     if (e != cudaSuccess) return e;
   }
-  const struct { const float* from; float* to; long long n; } sums[3] = {
-      {a.gA, c.grad_A, c.channels * c.states}, {a.gD, c.grad_D, c.channels}, {a.gbias, c.grad_bias, c.channels}};
-  for (const auto& s : sums) {
-    if (s.to == nullptr) continue;
-    e = launch_sum_parts(s.from, (int)entries, s.n, {{s.to, s.n}}, st);
-    if (e != cudaSuccess) return e;
-  }
-  return cudaSuccess;
+  if (c.grad_A == nullptr && c.grad_D == nullptr && c.grad_bias == nullptr) return cudaSuccess;
+  return launch_sum_parts(a.gparams, (int)entries, c.channels * (c.states + 2),
+                          {{c.grad_A, c.channels * c.states}, {c.grad_D, c.channels}, {c.grad_bias, c.channels}}, st);
 }
 
 template <typename T>

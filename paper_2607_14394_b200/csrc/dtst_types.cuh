@@ -37,6 +37,19 @@ __device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
 }
 
 
+// the special function unit's powers of two and reciprocals: 2 units in the last place and 1
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 template <typename T>
 struct Elem;
 

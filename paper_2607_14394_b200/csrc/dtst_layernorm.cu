@@ -384,9 +384,9 @@ struct FieldArgs {
   float eps;
 };
 
-// sums over the warps (threadIdx.y) of a position's VEC partial sums
-template <int VEC>
-__device__ __forceinline__ void field_sum(float (&v)[VEC], float (&red)[2][8][32 * VEC], int& phase) {
+// sums over the W warps (threadIdx.y) of a position's VEC partial sums
+template <int W, int VEC>
+__device__ __forceinline__ void field_sum(float (&v)[VEC], float (&red)[2][W][32 * VEC], int& phase) {
   const int lane = threadIdx.x;
 #pragma unroll
   for (int i = 0; i < VEC; ++i) red[phase][threadIdx.y][lane * VEC + i] = v[i];
@@ -394,35 +394,41 @@ __device__ __forceinline__ void field_sum(float (&v)[VEC], float (&red)[2][8][32
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
     float q = 0.f;
-    for (int y = 0; y < blockDim.y; ++y) q += red[phase][y][lane * VEC + i];
+#pragma unroll
+    for (int y = 0; y < W; ++y) q += red[phase][y][lane * VEC + i];
     v[i] = q;
   }
   phase ^= 1;
 }
 
-template <typename T, int VEC, int NCH>
-__global__ void __launch_bounds__(256) layer_norm_field_kernel(const FieldArgs a) {
-  __shared__ float red[2][8][32 * VEC];
+template <typename T, int W, int VEC, int NCH>
+__global__ void __launch_bounds__(32 * W) layer_norm_field_kernel(const FieldArgs a) {
+  __shared__ float red[2][W][32 * VEC];
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x, wy = threadIdx.y, ny = blockDim.y;
+  const int lane = threadIdx.x, wy = threadIdx.y, ny = W;
   const float inv_c = 1.0f / (float)a.C;
   const T* res = static_cast<const T*>(a.residual);
   int phase = 0;
-  for (long long t = blockIdx.x; t < a.outer * a.tiles; t += gridDim.x) {
-    const long long o = t / a.tiles, p = (t % a.tiles) * (32 * VEC) + lane * VEC;
-    const long long base = o * a.C * a.inner + p;
-    const bool live = p < a.inner;
-    Pack<T, VEC> px[NCH], pr[NCH];
+  Pack<T, VEC> px[NCH], pr[NCH];
+  const auto fetch = [&](long long t) {
+    const long long o = t / a.tiles, p = (t % a.tiles) * (32 * VEC) + lane * VEC, base = o * a.C * a.inner + p;
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int c = wy + k * ny;
-      const bool on = live && c < a.C;
+      const bool on = p < a.inner && c < a.C;
       if (on) px[k].load(static_cast<const T*>(a.x) + base + c * a.inner); else px[k].zero();
       if (res != nullptr) {
         if (on) pr[k].load(res + base + c * a.inner); else pr[k].zero();
       }
     }
+  };
+  const long long all = a.outer * a.tiles;
+  if (blockIdx.x < all) fetch(blockIdx.x);
+  for (long long t = blockIdx.x; t < all; t += gridDim.x) {
+    const long long o = t / a.tiles, p = (t % a.tiles) * (32 * VEC) + lane * VEC;
+    const long long base = o * a.C * a.inner + p;
+    const bool live = p < a.inner;
     float v[NCH][VEC], mean[VEC], rstd[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) mean[i] = rstd[i] = 0.f;
@@ -434,23 +440,26 @@ __global__ void __launch_bounds__(256) layer_norm_field_kernel(const FieldArgs a
         if (res != nullptr) v[k][i] += pr[k].get(i);
         mean[i] += v[k][i];
       }
+    // (in place: another CTA's tiles are other places)
+    if (t + gridDim.x < all) fetch(t + gridDim.x);
     if (a.s != nullptr && live) {
 #pragma unroll
       for (int k = 0; k < NCH; ++k) {
         const int c = wy + k * ny;
+        Pack<T, VEC> out;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) px[k].put(i, v[k][i]);
+        for (int i = 0; i < VEC; ++i) out.put(i, v[k][i]);
         if (c >= a.C) continue;
-        px[k].store(static_cast<T*>(a.s) + base + c * a.inner);
+        out.store(static_cast<T*>(a.s) + base + c * a.inner);
         if (sizeof(T) == 2 && a.low != nullptr) {
           Pack<T, VEC> lo;
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) lo.v[i] = LowBits<T>::take(v[k][i], px[k].v[i]);
+          for (int i = 0; i < VEC; ++i) lo.v[i] = LowBits<T>::take(v[k][i], out.v[i]);
           lo.store(static_cast<T*>(a.low) + base + c * a.inner);
         }
       }
     }
-    field_sum<VEC>(mean, red, phase);
+    field_sum<W, VEC>(mean, red, phase);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) mean[i] *= inv_c;
 #pragma unroll
@@ -460,7 +469,7 @@ __global__ void __launch_bounds__(256) layer_norm_field_kernel(const FieldArgs a
         v[k][i] -= mean[i];
         if (wy + k * ny < a.C) rstd[i] = fmaf(v[k][i], v[k][i], rstd[i]);
       }
-    field_sum<VEC>(rstd, red, phase);
+    field_sum<W, VEC>(rstd, red, phase);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) rstd[i] = rsqrtf(fmaf(rstd[i], inv_c, a.eps));
     if (!live) continue;
@@ -473,19 +482,20 @@ __global__ void __launch_bounds__(256) layer_norm_field_kernel(const FieldArgs a
       const int c = wy + k * ny;
       if (c >= a.C) continue;
       const float w = __ldg(a.weight + c), b = a.bias != nullptr ? __ldg(a.bias + c) : 0.f;
+      Pack<T, VEC> out;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) px[k].put(i, fmaf(v[k][i] * rstd[i], w, b));
-      px[k].store(static_cast<T*>(a.y) + base + c * a.inner);
+      for (int i = 0; i < VEC; ++i) out.put(i, fmaf(v[k][i] * rstd[i], w, b));
+      out.store(static_cast<T*>(a.y) + base + c * a.inner);
     }
   }
 }
 
-template <typename T, int VEC, int NCH>
-__global__ void __launch_bounds__(256) layer_norm_field_backward_kernel(const FieldArgs a) {
-  __shared__ float red[2][2][8][32 * VEC];
+template <typename T, int W, int VEC, int NCH>
+__global__ void __launch_bounds__(32 * W, W == 4 ? 4 : 1) layer_norm_field_backward_kernel(const FieldArgs a) {
+  __shared__ float red[2][2][W][32 * VEC];
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x, wy = threadIdx.y, ny = blockDim.y;
+  const int lane = threadIdx.x, wy = threadIdx.y, ny = W;
   const float inv_c = 1.0f / (float)a.C;
   const T* gs = static_cast<const T*>(a.gs);
   const T* low = sizeof(T) == 2 ? static_cast<const T*>(a.low) : nullptr;
@@ -544,11 +554,12 @@ __global__ void __launch_bounds__(256) layer_norm_field_backward_kernel(const Fi
     // one barrier for both sums
 #pragma unroll
     for (int i = 0; i < VEC; ++i) red[1][phase2][wy][lane * VEC + i] = g2[i];
-    field_sum<VEC>(g1, red[0], phase);
+    field_sum<W, VEC>(g1, red[0], phase);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       float q = 0.f;
-      for (int y = 0; y < ny; ++y) q += red[1][phase2][y][lane * VEC + i];
+#pragma unroll
+      for (int y = 0; y < W; ++y) q += red[1][phase2][y][lane * VEC + i];
       g1[i] *= inv_c, g2[i] = q * inv_c;
     }
     phase2 ^= 1;
@@ -678,28 +689,32 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     return launch_pdl(layer_norm_wide_field_backward_kernel<T>, grid, dim3(128), 0, st, a);
   }
-  const size_t need = WIDE * sizeof(T);
-  bool vec = a.inner % WIDE == 0;
+  // positions in vectors where the rows allow it; two of them a thread where 16 warps share the channels (8 warps with four each left one
+  // CTA on an SM: bf16 [8][64][65536] backward 367 us)
+  const int most_wide = a.C <= 32 ? WIDE : 2;
+  const size_t need = most_wide * sizeof(T);
+  bool vec = a.inner % most_wide == 0;
   for (const void* p : {a.x, a.residual, a.gy, a.gs, (const void*)a.s, (const void*)a.low, (const void*)a.y}) vec = vec && aligned_to(p, need);
-  const int ny = a.C <= 32 ? 4 : 8, nch = (int)((a.C + ny - 1) / ny);
-  const int per = 32 * (vec ? WIDE : 1);
+  const int ny = a.C <= 32 ? 4 : 16, nch = (int)((a.C + ny - 1) / ny);
+  const int per = 32 * (vec ? most_wide : 1);
   a.tiles = (a.inner + per - 1) / per;
   // the parameters' partial sums are two rows per CTA
-  const long long most = BACK ? (long long)kNormParts : (long long)num_sms() * 32, all = a.outer * a.tiles;
+  const long long most = BACK ? (long long)kNormParts : (long long)num_sms() * 16, all = a.outer * a.tiles;
   const dim3 grid((unsigned)(all < most ? all : most)), block(32, ny);
   *parts = (int)grid.x;
-#define DTST_FIELD(N)                                                                                             \
-  if (nch <= N) {                                                                                                 \
+#define DTST_FIELD(W, N, WIDTH)                                                                                   \
+  if (nch <= N && ny == W) {                                                                                      \
     if (BACK)                                                                                                     \
-      return vec ? launch_pdl(layer_norm_field_backward_kernel<T, WIDE, N>, grid, block, 0, st, a)                \
-                 : launch_pdl(layer_norm_field_backward_kernel<T, 1, N>, grid, block, 0, st, a);                  \
-    return vec ? launch_pdl(layer_norm_field_kernel<T, WIDE, N>, grid, block, 0, st, a)                           \
-               : launch_pdl(layer_norm_field_kernel<T, 1, N>, grid, block, 0, st, a);                             \
+      return vec ? launch_pdl(layer_norm_field_backward_kernel<T, W, WIDTH, N>, grid, block, 0, st, a)            \
+                 : launch_pdl(layer_norm_field_backward_kernel<T, W, 1, N>, grid, block, 0, st, a);               \
+    return vec ? launch_pdl(layer_norm_field_kernel<T, W, WIDTH, N>, grid, block, 0, st, a)                       \
+               : launch_pdl(layer_norm_field_kernel<T, W, 1, N>, grid, block, 0, st, a);                          \
   }
-  DTST_FIELD(2)
-  DTST_FIELD(5)
-  DTST_FIELD(8)
-  DTST_FIELD(16)
+  DTST_FIELD(4, 2, WIDE)
+  DTST_FIELD(4, 5, WIDE)
+  DTST_FIELD(4, 8, WIDE)
+  DTST_FIELD(16, 4, 2)
+  DTST_FIELD(16, 8, 2)
 #undef DTST_FIELD
   return cudaErrorNotSupported;
 }

@@ -66,7 +66,7 @@ def _use(stream, dev):
 # the current stream of a device as a cudaStream_t; the first form costs a tenth of the second
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-_current_device = torch.cuda.current_device
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device      # (likewise)
 
 
 def _check(status: int, where: str) -> None:

@@ -25,10 +25,6 @@ ACTIVATIONS = {None: 0, "silu": 1}
 _F32, _I32 = torch.float32, torch.int32
 
 
-def _elsewhere(stream, dev) -> bool:
-    return stream is not None or Mem._current_device() != dev
-
-
 def _there(stream, dev):
     """A context in which `dev` is the current device and `stream` (or that device's current stream) the current stream."""
     return _Both(torch.cuda.device(dev), _use(torch.cuda.current_stream(dev) if stream is None else stream, dev))
@@ -47,19 +43,30 @@ class _Both:
             c.__exit__(*error)
 
 
-def _tokens(t: torch.Tensor, name: str, dev: int, dtype: torch.dtype, shape) -> Tuple[int, Tuple[int, int]]:
-    """Address and (batch, step) strides of a token-major tensor whose other dimensions lie together."""
-    if t.dtype is not dtype or t.get_device() != dev:
-        _on_device(t, name, dev, dtype)
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    st = t.stride()
-    width = 1
-    for i in range(len(shape) - 1, 1, -1):
-        if shape[i] != 1 and st[i] != width:
-            raise ValueError(f"{name}: the dimensions behind the steps must lie together")
-        width *= shape[i]
-    return t.data_ptr(), st[:2]
+class _Tokens:
+    """Checks of one token-major argument: its type, device and shape, and that the dimensions behind the steps lie together."""
+
+    def __init__(self, name: str, dev: int, dtype: torch.dtype, shape):
+        self.name, self.dev, self.dtype, self.shape = name, dev, dtype, torch.Size(shape)
+        self.seen = (None, None)                         # the last strides that were found right, and what they gave
+
+    def __call__(self, t: torch.Tensor) -> Tuple[int, Tuple[int, int]]:
+        """Address and (batch, step) strides."""
+        if t.dtype is not self.dtype or t.get_device() != self.dev:
+            _on_device(t, self.name, self.dev, self.dtype)
+        if t.shape != self.shape:
+            raise ValueError(f"{self.name} must have shape {tuple(self.shape)}, got {tuple(t.shape)}")
+        st = t.stride()
+        was, at = self.seen                              # (one read: another thread may set it)
+        if was != st:
+            width = 1
+            for i in range(len(st) - 1, 1, -1):
+                if self.shape[i] != 1 and st[i] != width:
+                    raise ValueError(f"{self.name}: the dimensions behind the steps must lie together")
+                width *= self.shape[i]
+            at = st[:2]
+            self.seen = (st, at)
+        return t.data_ptr(), at
 
 
 class LayerNorm:
@@ -101,7 +108,7 @@ class LayerNorm:
         need_backward=False: neither is formed, and stats is None.
         """
         d, t, sh = self.dev, self.dtype, self.shape
-        if _elsewhere(stream, d):
+        if stream is not None or Mem._current_device() != d:
             with _there(stream, d):
                 return self.forward(x, weight, bias, residual, out, sum_out, stats, need_backward)
         xp, wp = _addr(x, "x", d, t, sh), _addr(weight, "weight", d, _F32, self._wshape)
@@ -148,7 +155,7 @@ class LayerNorm:
         returned them (the attribute `sum_low` does not survive a clone, a detach or a copy: pass it on as `sum_low=`, or
         the gradients are those of the rounded sum).  need_grad_weight=False: neither parameter's gradient is formed."""
         d, t, sh = self.dev, self.dtype, self.shape
-        if _elsewhere(stream, d):
+        if stream is not None or Mem._current_device() != d:
             with _there(stream, d):
                 return self.backward(grad_y, s, weight, stats, grad_s, grad_x, grad_weight, grad_bias, need_grad_weight, None, sum_low)
         gp, wp = _addr(grad_y, "grad_y", d, t, sh), _addr(weight, "weight", d, _F32, self._wshape)
@@ -197,6 +204,7 @@ class CausalConv:
         B, T, C = self.shape
         self.state_shape = torch.Size((B, max(0, self.width - 1), C))
         self._wshape, self._bshape, self._lshape = torch.Size((C, self.width)), torch.Size((C,)), torch.Size((B,))
+        self._x, self._grad_x = (_Tokens(n, self.dev, dtype, self.shape) for n in ("x", "grad_x"))
         self._dense = (T * C, C)
         self._ref = self._describe(self._dense, self._dense)
         self._other = (None, None, None)                 # the last description of other strides
@@ -228,13 +236,13 @@ class CausalConv:
     def forward(self, x, weight, bias=None, state=None, lengths=None, out=None, state_out=None, need_state=True, stream=None):
         """Returns (y, new state).  state_out may be the state itself; need_state=False forms none (None)."""
         d, t = self.dev, self.dtype
-        if _elsewhere(stream, d):
+        if stream is not None or Mem._current_device() != d:
             with _there(stream, d):
                 return self.forward(x, weight, bias, state, lengths, out, state_out, need_state)
-        xp, at = _tokens(x, "x", d, t, self.shape)
+        xp, at = self._x(x)
         wp, bp, sp, lp = self._params(weight, bias, state, lengths)
         if out is None:
-            out = x.new_empty(self.shape)
+            out = torch.empty_like(x) if at == self._dense else x.new_empty(self.shape)
             yp = out.data_ptr()
         else:
             yp = _addr(out, "out", d, t, self.shape)
@@ -242,7 +250,7 @@ class CausalConv:
         if state_out is not None:
             op = _addr(state_out, "state_out", d, t, self.state_shape)
         elif need_state:
-            state_out = x.new_empty(self.state_shape)
+            state_out = x.new_empty(self.state_shape) if state is None else torch.empty_like(state)
             op = state_out.data_ptr()
         status = self._lib.dtst_causal_conv(self._description(at, self._dense), xp, wp, bp, sp, lp, yp, op, Mem._raw_stream(d))
         if status:
@@ -254,16 +262,16 @@ class CausalConv:
         """Returns (grad_x, grad_weight, grad_bias, grad_state); x, weight, bias, state (as it was) and lengths as in the forward
         call.  grad_x may be strided like x.  need_grad_weight=False: neither parameter's gradient is formed."""
         d, t = self.dev, self.dtype
-        if _elsewhere(stream, d):
+        if stream is not None or Mem._current_device() != d:
             with _there(stream, d):
                 return self.backward(grad_y, x, weight, bias, state, lengths, grad_state_out, grad_x, grad_weight, grad_bias,
                                      grad_state, need_grad_weight, need_grad_state)
-        xp, at = _tokens(x, "x", d, t, self.shape)
+        xp, at = self._x(x)
         wp, bp, sp, lp = self._params(weight, bias, state, lengths)
         gp = _addr(grad_y, "grad_y", d, t, self.shape)
         if grad_x is None:
             grad_x = torch.empty_like(grad_y)
-        gxp, to = _tokens(grad_x, "grad_x", d, t, self.shape)
+        gxp, to = self._grad_x(grad_x)
         scratch = nbytes = gwp = gbp = gsp = 0
         if need_grad_weight:
             grad_weight = torch.empty_like(weight) if grad_weight is None else grad_weight
@@ -310,6 +318,8 @@ class SelectiveScan:
         self.state_shape, self.maps_shape = torch.Size((B, C, self.states)), torch.Size((B, T, self.groups, self.states))
         self._ashape, self._cshape, self._lshape = torch.Size((C, self.states)), torch.Size((C,)), torch.Size((B,))
         self._shapes = (self.shape, self.shape, self.shape, self.maps_shape, self.maps_shape)
+        self._checks = [_Tokens(n, self.dev, dtype, sh) for n, sh in zip(self.NAMES, self._shapes)]
+        self._grad_checks = [_Tokens("gradient of " + n, self.dev, dtype, sh) for n, sh in zip(self.NAMES, self._shapes)]
         rows, maps = (T * C, C), (T * self.groups * self.states, self.groups * self.states)
         self._dense = (rows, rows, rows, maps, maps)
         self._ref = self._describe(self._dense, self._dense)
@@ -347,28 +357,27 @@ class SelectiveScan:
 
     def _inputs(self, tensors, A, D, dt_bias, h0, lengths):
         """The C structure of the inputs, and their strides."""
-        d, t = self.dev, self.dtype
-        ptr, at = [], []
-        for v, name, shape, dense in zip(tensors, self.NAMES, self._shapes, self._dense):
-            p, s = (0, dense) if v is None else _tokens(v, name, d, t, shape)
-            ptr.append(p)
-            at.append(s)
-        return Bn.SelectiveInputs(*ptr, _addr(A, "A", d, _F32, self._ashape), 0 if D is None else _addr(D, "D", d, _F32, self._cshape),
+        d = self.dev
+        x, dt, z, B, C = tensors
+        cx, cdt, cz, cb, cc = self._checks
+        (xp, xs), (tp, ts), (bp, bs), (cp, cs) = cx(x), cdt(dt), cb(B), cc(C)
+        zp, zs = (0, self._dense[2]) if z is None else cz(z)
+        return Bn.SelectiveInputs(xp, tp, zp, bp, cp, _addr(A, "A", d, _F32, self._ashape), 0 if D is None else _addr(D, "D", d, _F32, self._cshape),
                                   0 if dt_bias is None else _addr(dt_bias, "dt_bias", d, _F32, self._cshape),
                                   0 if h0 is None else _addr(h0, "h0", d, _F32, self.state_shape),
-                                  0 if lengths is None else _addr(lengths, "lengths", d, _I32, self._lshape)), tuple(at)
+                                  0 if lengths is None else _addr(lengths, "lengths", d, _I32, self._lshape)), (xs, ts, zs, bs, cs)
 
     def forward(self, x, dt, A, B, C, D=None, z=None, dt_bias=None, h0=None, lengths=None, out=None, h_last=None, checkpoints=None,
                 need_state=True, stream=None):
         """Returns (y, h_last).  lengths: int32 per batch entry; checkpoints: see new_checkpoints; h_last may be h0 itself;
         need_state=False forms none (None)."""
         d = self.dev
-        if _elsewhere(stream, d):
+        if stream is not None or Mem._current_device() != d:
             with _there(stream, d):
                 return self.forward(x, dt, A, B, C, D, z, dt_bias, h0, lengths, out, h_last, checkpoints, need_state)
         inputs, at = self._inputs((x, dt, z, B, C), A, D, dt_bias, h0, lengths)
         if out is None:
-            out = x.new_empty(self.shape)
+            out = torch.empty_like(dt) if dt.is_contiguous() else x.new_empty(self.shape)
             yp = out.data_ptr()
         else:
             yp = _addr(out, "out", d, self.dtype, self.shape)
@@ -376,7 +385,7 @@ class SelectiveScan:
         if h_last is not None:
             lp = _addr(h_last, "h_last", d, _F32, self.state_shape)
         elif need_state:
-            h_last = A.new_empty(self.state_shape)
+            h_last = A.new_empty(self.state_shape) if h0 is None else torch.empty_like(h0)
             lp = h_last.data_ptr()
         # the call's own, from the current stream's allocations: calls on other streams may be under way
         nbytes = self._scratch_bytes[0] if self._scratch_bytes[0] is not None else self._ask_scratch(0)
@@ -396,30 +405,30 @@ class SelectiveScan:
         """Gradients by name: x, dt, B, C, A, h0, and z, D, dt_bias where these were given.  Inputs and checkpoints as in the
         forward call; `out` may bring buffers by the same names."""
         d, t = self.dev, self.dtype
-        if _elsewhere(stream, d):
+        if stream is not None or Mem._current_device() != d:
             with _there(stream, d):
                 return self.backward(grad_y, x, dt, A, B, C, checkpoints, D, z, dt_bias, h0, lengths, grad_last, out)
         inputs, at = self._inputs((x, dt, z, B, C), A, D, dt_bias, h0, lengths)
         gp = _addr(grad_y, "grad_y", d, t, self.shape)
         grads = dict(out) if out else {}
         ptr, to = [], []
-        for name, shape, dense in zip(self.NAMES, self._shapes, self._dense):
+        for name, shape, dense, check in zip(self.NAMES, self._shapes, self._dense, self._grad_checks):
             if name == "z" and z is None:
                 ptr.append(0)
                 to.append(dense)
                 continue
             if name not in grads:
-                grads[name] = grad_y.new_empty(shape)
-            p, s = _tokens(grads[name], "gradient of " + name, d, t, shape)
+                grads[name] = torch.empty_like(grad_y) if shape is self.shape else grad_y.new_empty(shape)
+            p, s = check(grads[name])
             ptr.append(p)
             to.append(s)
-        for name, given, shape in (("A", A, self._ashape), ("D", D, self._cshape), ("dt_bias", dt_bias, self._cshape),
-                                   ("h0", A, self.state_shape)):
-            if given is None:
+        for name, like, shape in (("A", A, self._ashape), ("D", D, self._cshape), ("dt_bias", dt_bias, self._cshape),
+                                  ("h0", h0 if h0 is not None else grad_last, self.state_shape)):
+            if like is None and name != "h0":
                 ptr.append(0)
                 continue
             if name not in grads:
-                grads[name] = A.new_empty(shape)
+                grads[name] = A.new_empty(shape) if like is None else torch.empty_like(like)
             ptr.append(_addr(grads[name], "gradient of " + name, d, _F32, shape))
         desc = self._description(at, tuple(to))
         nbytes = self._scratch_bytes[1] if self._scratch_bytes[1] is not None else self._ask_scratch(1)
@@ -483,7 +492,7 @@ class GradNorm:
 
     def _run(self, entries, max_norm, eps, norm, stream):
         d = self.dev
-        if _elsewhere(stream, d):
+        if stream is not None or Mem._current_device() != d:
             with _there(stream, d):
                 return self._run(entries, max_norm, eps, norm, None)
         if norm is None:

@@ -15,15 +15,16 @@ namespace dtst {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPerLaunch = 128;
+constexpr int kPerLaunch = 128;         // most tensors of a launch; short lists go with a shorter one (N)
 constexpr int kChunkBytes = 16384;      // bytes of one tensor that a CTA takes at a time
 
+template <int N>
 struct ListArgs {
-  const void* grad[kPerLaunch];
-  void* out[kPerLaunch];
-  long long n[kPerLaunch];
-  int first[kPerLaunch + 1];            // number of each tensor's first chunk
-  unsigned char dtype[kPerLaunch];
+  const void* grad[N];
+  void* out[N];
+  long long n[N];
+  int first[N + 1];                     // number of each tensor's first chunk
+  unsigned char dtype[N];
   int count;
   const double* sums;                   // scaling: all launches' partial sums
   double* partial;                      // sum: this launch's
@@ -32,7 +33,8 @@ struct ListArgs {
   float max_norm, eps;
 };
 
-__device__ __forceinline__ int find(const ListArgs& a, int chunk) {      // the tensor with this chunk
+template <int N>
+__device__ __forceinline__ int find(const ListArgs<N>& a, int chunk) {      // the tensor with this chunk
   int lo = 0, hi = a.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -76,7 +78,8 @@ __device__ __forceinline__ double block_sum(double v, double* red) {     // the 
   return t;
 }
 
-__global__ void __launch_bounds__(kThreads) grad_sum_kernel(const __grid_constant__ ListArgs a) {
+template <int N>
+__global__ void __launch_bounds__(kThreads) grad_sum_kernel(const __grid_constant__ ListArgs<N> a) {
   __shared__ double red[kThreads / 32];
   pdl_trigger();
   pdl_wait();
@@ -99,7 +102,8 @@ __global__ void __launch_bounds__(kThreads) grad_sum_kernel(const __grid_constan
 
 // norm and coefficient from the partial sums; the coefficient as a product of two, since that of a norm beyond 2^100 is
 // too small for the one
-__device__ __forceinline__ void coefficient(const ListArgs& a, double* red, float& c_hi, float& c_lo) {
+template <int N>
+__device__ __forceinline__ void coefficient(const ListArgs<N>& a, double* red, float& c_hi, float& c_lo) {
   double s = 0.;
   for (int i = threadIdx.x; i < a.sums_n; i += kThreads) s += a.sums[i];
   const double norm = sqrt(block_sum(s, red));
@@ -111,7 +115,8 @@ __device__ __forceinline__ void coefficient(const ListArgs& a, double* red, floa
   c_lo = (float)(tiny ? c * 0x1p60 : c);
 }
 
-__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_constant__ ListArgs a) {
+template <int N>
+__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_constant__ ListArgs<N> a) {
   __shared__ double red[kThreads / 32];
   pdl_trigger();
   pdl_wait();
@@ -141,7 +146,8 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* o, long long n, float
   }
 }
 
-__global__ void __launch_bounds__(kThreads) grad_scale_kernel(const __grid_constant__ ListArgs a) {
+template <int N>
+__global__ void __launch_bounds__(kThreads) grad_scale_kernel(const __grid_constant__ ListArgs<N> a) {
   __shared__ double red[kThreads / 32];
   pdl_trigger();
   pdl_wait();
@@ -162,17 +168,14 @@ __global__ void __launch_bounds__(kThreads) grad_scale_kernel(const __grid_const
   }
 }
 
-}  // namespace
-
-int grad_launches(long long count) { return (int)((count + kPerLaunch - 1) / kPerLaunch); }
-
-cudaError_t launch_grad_norm(const GradEntry* list, long long count, float max_norm, float eps, bool scale, float* norm,
-                             double* partial, cudaStream_t st) {
-  const int most = num_sms() * 4 < kGradParts ? num_sms() * 4 : kGradParts, launches = grad_launches(count);
+template <int N>
+cudaError_t launch_list(const GradEntry* list, long long count, float max_norm, float eps, bool scale, float* norm, double* partial,
+                        cudaStream_t st) {
+  const int most = num_sms() * 4 < kGradParts ? num_sms() * 4 : kGradParts, launches = (int)((count + N - 1) / N);
   int sums = 0;
-  auto fill = [&](ListArgs& a, int launch) {
-    const long long k0 = (long long)launch * kPerLaunch;
-    a.count = (int)(count - k0 < kPerLaunch ? count - k0 : kPerLaunch);
+  auto fill = [&](ListArgs<N>& a, int launch) {
+    const long long k0 = (long long)launch * N;
+    a.count = (int)(count - k0 < N ? count - k0 : N);
     long long chunks = 0;
     for (int k = 0; k < a.count; ++k) {
       const GradEntry& e = list[k0 + k];
@@ -183,23 +186,33 @@ cudaError_t launch_grad_norm(const GradEntry* list, long long count, float max_n
     a.first[a.count] = (int)chunks;
     return (int)(chunks < most ? (chunks > 0 ? chunks : 1) : most);
   };
-  ListArgs a{};
+  ListArgs<N> a{};
   for (int l = 0; l < launches; ++l) {
     const int ctas = fill(a, l);
     a.partial = partial + sums;
-    const cudaError_t e = launch_pdl(grad_sum_kernel, dim3((unsigned)ctas), dim3(kThreads), 0, st, a);
+    const cudaError_t e = launch_pdl(grad_sum_kernel<N>, dim3((unsigned)ctas), dim3(kThreads), 0, st, a);
     if (e != cudaSuccess) return e;
     sums += ctas;
   }
   a.sums = partial, a.sums_n = sums, a.max_norm = max_norm, a.eps = eps, a.norm = norm;
-  if (!scale || launches == 0) return launch_pdl(grad_norm_kernel, dim3(1), dim3(kThreads), 0, st, a);
+  if (!scale || launches == 0) return launch_pdl(grad_norm_kernel<N>, dim3(1), dim3(kThreads), 0, st, a);
   for (int l = launches - 1; l >= 0; --l) {
     const int ctas = launches > 1 ? fill(a, l) : (a.first[a.count] < most ? (a.first[a.count] > 0 ? a.first[a.count] : 1) : most);
-    const cudaError_t e = launch_pdl(grad_scale_kernel, dim3((unsigned)ctas), dim3(kThreads), 0, st, a);
+    const cudaError_t e = launch_pdl(grad_scale_kernel<N>, dim3((unsigned)ctas), dim3(kThreads), 0, st, a);
     if (e != cudaSuccess) return e;
     a.norm = nullptr;
   }
   return cudaSuccess;
+}
+
+}  // namespace
+
+int grad_launches(long long count) { return (int)((count + kPerLaunch - 1) / kPerLaunch); }
+
+cudaError_t launch_grad_norm(const GradEntry* list, long long count, float max_norm, float eps, bool scale, float* norm,
+                             double* partial, cudaStream_t st) {
+  return count <= 16 ? launch_list<16>(list, count, max_norm, eps, scale, norm, partial, st)
+                     : launch_list<kPerLaunch>(list, count, max_norm, eps, scale, norm, partial, st);
 }
 
 }  // namespace dtst

@@ -42,8 +42,9 @@ __device__ __forceinline__ void tell(int id) { asm volatile("bar.arrive %0, %1;"
 constexpr int kFull = 1, kDone = 3;
 
 // The backward pass's two halves share a CTA's registers unevenly: 104 + 152 of 2 x 128.
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 104;"); }
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 152;"); }
+constexpr int kFewRegisters = 104, kMoreRegisters = 152;
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters)); }
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMoreRegisters)); }
 
 // log(1 + e^v), and e = e^-|v|: the larger of v and 0, and log(1 + e) = 2 atanh(e / (2 + e)) as a polynomial in the square of
 // that argument, fitted over its range of 0 to 1/9 to 4e-9 of the value: no digits are lost where e is small
@@ -84,7 +85,9 @@ struct SelArgs {
   Rows gx, gdt, gz;
   float *gparams, *gh0;                // gparams: a row of [C N], [C], [C] per batch entry and segment: of A, D, dt_bias
   float* gmaps;                        // [blocks of a group][batch][length][groups][2][N4]
-  float *ends, *spans;                 // [segments][batch][C][N4], [segments][batch][C]: what a segment leaves, sums of its steps
+  // [segments][batch][C][N4], [segments][batch][C]: what a segment leaves, sums of its steps.  The place of the segment whose end nobody
+  // joins holds h0 (backward: grad_last) as it was: h_last may take its place while other segments still read it.
+  float *ends, *spans;
   long long batch, length, channels;
   int states, groups, per_group, blocks;      // channels of a group, blocks of channels to a group
   int segments, seg;                   // seg: steps to a segment
@@ -139,36 +142,23 @@ struct Lane {
   }
 };
 
-// Sums of four values over P neighbouring lanes, for two channels at a time: every exchange halves the values while there are
-// several.  Lane p ends with the values 4 / P p .. of its share (P <= 4), or value p / (P / 4).
+// Sums of four values over P >= 4 neighbouring lanes, for two channels at a time: the first two exchanges halve the values.  Lane p
+// ends with value p / (P / 4).
 template <int P>
-__device__ __forceinline__ void state_sums(float2 (&v)[4], int p) {
-  int m = 4;
+__device__ __forceinline__ float2 state_sums(float2 (&v)[4], int p) {
+  const auto from = [](float2 a, int o) { return make_float2(__shfl_xor_sync(0xffffffffu, a.x, o), __shfl_xor_sync(0xffffffffu, a.y, o)); };
+  const bool high = p & (P / 2), odd = p & (P / 4);
+  const float2 a = add_pair(high ? v[2] : v[0], from(high ? v[0] : v[2], P / 2)), b = add_pair(high ? v[3] : v[1], from(high ? v[1] : v[3], P / 2));
+  float2 t = add_pair(odd ? b : a, from(odd ? a : b, P / 4));
 #pragma unroll
-  for (int o = P / 2; o > 0; o /= 2) {
-    if (m > 1) {
-      m /= 2;
-      const bool up = p & o;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (i >= m) break;
-        const float2 send = up ? v[i] : v[i + m], keep = up ? v[i + m] : v[i];
-        v[i] = add_pair(keep, make_float2(__shfl_xor_sync(0xffffffffu, send.x, o), __shfl_xor_sync(0xffffffffu, send.y, o)));
-      }
-    } else {
-      v[0] = add_pair(v[0], make_float2(__shfl_xor_sync(0xffffffffu, v[0].x, o), __shfl_xor_sync(0xffffffffu, v[0].y, o)));
-    }
-  }
+  for (int o = P / 8; o > 0; o /= 2) t = add_pair(t, from(t, o));
+  return t;
 }
-// ... into rows s .. s + 3 of a [rows][LD] array
+// ... into rows 0 .. 3 of a [rows][LD] array
 template <int P, int LD>
-__device__ __forceinline__ void put_sums(const float2 (&v)[4], float* rows, int p, int c) {
-  if constexpr (P <= 4) {
-#pragma unroll
-    for (int k = 0; k < 4 / P; ++k) *reinterpret_cast<float2*>(rows + (p * (4 / P) + k) * LD + c) = v[k];
-  } else {
-    if (p % (P / 4) == 0) *reinterpret_cast<float2*>(rows + p / (P / 4) * LD + c) = v[0];
-  }
+__device__ __forceinline__ void put_sums(float2 (&v)[4], float* rows, int p, int c) {
+  const float2 t = state_sums<P>(v, p);
+  if (P == 4 || p % (P / 4) == 0) *reinterpret_cast<float2*>(rows + p / (P / 4) * LD + c) = t;
 }
 
 // a tile's maps on their way to shared memory: an item is four states of one map at one step
@@ -268,13 +258,31 @@ __device__ __forceinline__ void load_A(F4 (&A2)[2], const SelArgs& a, int c, int
     for (int j = 0; j < 2; ++j) A2[k].v[j] = mul_pair(A2[k].v[j], twice(kLog2e));
   }
 }
-// What stands in front of (behind) a segment, from `h` on, joined over the segments in front of (behind) it in order.
+// The state in front of (the gradient behind) the whole sequence, then what a segment finds, joined over the segments in front of
+// (behind) it in order.
+template <bool BACK>
+__device__ __forceinline__ void load_outer(F4 (&h)[2], const SelArgs& a, const Place& at, int c, int ch, int p, int perm) {
+  const float* from = BACK ? a.grad_last : a.h0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    h[k] = F4{};
+    if (ch + k < at.left && from != nullptr) h[k] = four(from + (at.b * a.channels + c + k) * a.states, 4 * p, a.states, perm);
+  }
+}
 template <bool BACK>
 __device__ __forceinline__ void join_segments(F4 (&h)[2], const F4 (&A2)[2], const SelArgs& a, const Place& at, int c, int ch, int p, int perm) {
+  if (a.segments == 1) {
+    load_outer<BACK>(h, a, at, c, ch, p, perm);
+    return;
+  }
+  h[0] = h[1] = F4{};
   const int n = BACK ? a.segments - 1 - at.part : at.part;
   if (4 * p >= a.n4 || ch >= at.left) return;
   const int two = ch + 1 < at.left ? 1 : 0;               // (the block's last channel alone: twice the same)
   const long long seg = a.batch * a.channels, from = at.b * a.channels + c + (BACK ? (a.segments - 1) * seg : 0);
+  const long long outer = at.b * a.channels + c + (BACK ? 0 : (a.segments - 1) * seg);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) h[k] = in_order(*reinterpret_cast<const float4*>(a.ends + (outer + k * two) * a.n4 + 4 * p), perm);
 #pragma unroll 8
   for (int i = 0; i < n; ++i) {
     const long long q = from + (BACK ? -i : i) * seg;
@@ -409,11 +417,15 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_ends_kernel(const S
     }
     tell(kDone + buf);
   }
-  const long long q = at.part * a.batch + at.b;
+  const long long q = at.part * a.batch + at.b, outer = (BACK ? 0 : a.segments - 1) * a.batch + at.b;
+  const bool first = at.part == (BACK ? a.segments - 1 : 0);
+  F4 o[2] = {};
+  if (first) load_outer<BACK>(o, a, at, c, ch, p, 0);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     if (ch + k >= at.left) continue;
     if (4 * p < a.n4) *reinterpret_cast<float4*>(a.ends + (q * a.channels + c + k) * a.n4 + 4 * p) = quad(h[k]);
+    if (first && 4 * p < a.n4) *reinterpret_cast<float4*>(a.ends + (outer * a.channels + c + k) * a.n4 + 4 * p) = quad(o[k]);
     if (p == 0) a.spans[q * a.channels + c + k] = sum[k];
   }
 }
@@ -547,11 +559,8 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_forward_kernel(cons
   }
   // ---- the recurrence
   const int p = tid % P, ch = 2 * (tid / P), c = at.c0 + ch;
-  F4 A2[2], h[2] = {};
+  F4 A2[2], h[2];
   load_A(A2, a, c, ch, at.left, p, 0);
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    if (ch + k < at.left && a.h0 != nullptr) h[k] = four(a.h0 + (at.b * a.channels + c + k) * a.states, 4 * p, a.states, 0);
   join_segments<false>(h, A2, a, at, c, ch, p, 0);
   const long long saves = (a.length + kSave - 1) / kSave, save_ld = a.channels * a.n4;
   float* ck = a.ck + (at.b * saves + at.begin / kSave) * save_ld + (long long)c * a.n4 + 4 * p;
@@ -582,7 +591,6 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_forward_kernel(cons
       }
 #pragma unroll
       for (int i = 0; i < N / 4; ++i) {
-        state_sums<P>(y[i], p);
         put_sums<P, LD>(y[i], ys + (s + 4 * i) * LD, p, ch);
       }
     };
@@ -607,21 +615,17 @@ template <int P, int LANES>
 __device__ __forceinline__ void channel_sums(F4& b, F4& c, int pl, float* out, int n0, int perm, int np) {
   auto swap = [](float v, int o) { return __shfl_xor_sync(0xffffffffu, v, o * P); };
   constexpr int FIRST = LANES >= 4 ? 2 : 1;
-  const float2 b2 = LANES > 1 ? add_pair(b.v[0], make_float2(swap(b.v[1].x, FIRST), swap(b.v[1].y, FIRST))) : b.v[0];
-  const float2 c2 = LANES > 1 ? add_pair(c.v[0], make_float2(swap(c.v[1].x, FIRST), swap(c.v[1].y, FIRST))) : c.v[0];
+  const float2 b2 = add_pair(b.v[0], make_float2(swap(b.v[1].x, FIRST), swap(b.v[1].y, FIRST)));
+  const float2 c2 = add_pair(c.v[0], make_float2(swap(c.v[1].x, FIRST), swap(c.v[1].y, FIRST)));
   if constexpr (LANES >= 4) {
     const float2 one = add_pair(make_float2(b2.x, c2.x), make_float2(swap(b2.y, 1), swap(c2.y, 1)));
-    if constexpr (LANES >= 8) {
+    if constexpr (LANES == 8) {
       const bool up = pl & 4;
-      float v = (up ? one.y : one.x) + swap(up ? one.x : one.y, 4);
-      if constexpr (LANES >= 16) v += swap(v, 8);
-      if constexpr (LANES >= 32) v += swap(v, 16);
-      if (LANES == 8 || pl < 8) out[(up ? np : 0) + n0 + perm] = v;
+      out[(up ? np : 0) + n0 + perm] = (up ? one.y : one.x) + swap(up ? one.x : one.y, 4);
     } else {
       out[n0 + perm] = one.x, out[np + n0 + perm] = one.y;
     }
   } else {
-    static_assert(LANES == 2 || LANES >= 4, "a lane alone has nothing to add");
     out[n0 + perm] = b2.x, out[n0 + (1 ^ perm)] = b2.y;
     out[np + n0 + perm] = c2.x, out[np + n0 + (1 ^ perm)] = c2.y;
   }
@@ -831,11 +835,8 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_backward_kernel(con
   const int p = tid % P, pair = tid / P, ch = 2 * pair, c = at.c0 + ch;
   const int pl = pair % LANES, perm = LANES >= 4 ? pl & 3 : (pl & 1) * 2;
   const bool gated = a.z.p != nullptr;
-  F4 A2[2], m[2] = {}, gA[2] = {};         // m: what the step behind passes back
+  F4 A2[2], m[2], gA[2] = {};              // m: what the step behind passes back
   load_A(A2, a, c, ch, at.left, p, perm);
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    if (ch + k < at.left && a.grad_last != nullptr) m[k] = four(a.grad_last + (at.b * a.channels + c + k) * a.states, 4 * p, a.states, perm);
   join_segments<true>(m, A2, a, at, c, ch, p, perm);
   const long long saves = (a.length + TS - 1) / TS, save_ld = a.channels * a.n4;
   const float* ck = a.ck + (at.b * saves + at.begin / TS + tiles - 1) * save_ld + (long long)c * a.n4 + 4 * p;
@@ -901,12 +902,9 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_backward_kernel(con
         eb[i] = make_float2(ebk[0], ebk[1]), qa[i] = make_float2(qak[0], qak[1]), cy[i] = make_float2(cyk[0], cyk[1]);
         channel_sums<P, LANES>(gb, gc, pl, cs + s * 2 * NP, 4 * p, perm, NP);
       }
-      state_sums<P>(eb, p);
-      state_sums<P>(qa, p);
       put_sums<P, LD>(eb, rs + s4 * LD, p, ch);
       put_sums<P, LD>(qa, rs + (TS + s4) * LD, p, ch);
       if (gated) {
-        state_sums<P>(cy, p);
         put_sums<P, LD>(cy, rs + (2 * TS + s4) * LD, p, ch);
       }
     }
@@ -950,11 +948,9 @@ __global__ void __launch_bounds__(256) selective_maps_kernel(const MapArgs a) {
   }
 }
 
-int lanes_of(long long states) {
-  int p = 1;
-  while (4 * p < states) p *= 2;
-  return p;
-}
+// Lanes to a pair of channels.  Four for fewer than 13 states too, some of them idle: more channels to a CTA instead left too few CTAs and
+// too much to stage for each (4 x 2048 x 4096 forward: four states 567 us on one lane, eight 458 on two, 273 on four).
+int lanes_of(long long states) { return states <= 16 ? 4 : states <= 32 ? 8 : 16; }
 long long blocks_of(const SelectiveCall& c) {          // blocks of channels of a group
   const long long dc = 2 * kThreads / lanes_of(c.states), per = c.channels / c.groups;
   return (per + dc - 1) / dc;
@@ -1019,6 +1015,20 @@ SelArgs args_of(const SelectiveCall& c, int esize, bool back) {
   return a;
 }
 
+// The uneven split of registers takes 2 x 128 a thread pair from what the CTA was launched with: without them it would wait for ever.
+template <typename Kern>
+cudaError_t registers_there(Kern kern, std::atomic<uint64_t>& seen) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && (seen.load(std::memory_order_relaxed) >> dev & 1u))) return e;
+  cudaFuncAttributes f;
+  e = cudaFuncGetAttributes(&f, (const void*)kern);
+  if (e != cudaSuccess) return e;
+  if (f.numRegs * 2 < kFewRegisters + kMoreRegisters) return cudaErrorNotSupported;
+  if (dev < 64) seen.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return cudaSuccess;
+}
+
 template <typename Kern>
 cudaError_t launch(Kern kern, const SelArgs& a, int segments, size_t smem, std::atomic<uint64_t>& seen, cudaStream_t st) {
   const cudaError_t e = allow_smem((const void*)kern, smem, seen);
@@ -1044,9 +1054,9 @@ cudaError_t backward_p(const SelectiveCall& c, cudaStream_t st) {
   const long long entries = c.batch * a.segments;
   a.gparams = c.scratch + cut_floats(c);
   a.gmaps = a.gparams + param_floats(c);
-  static std::atomic<uint64_t> seen[2];
-  cudaError_t e = cudaSuccess;
-  if (a.segments > 1) e = launch(selective_ends_kernel<T, P, true>, a, a.segments - 1, SelCfg<P, kFwdSteps>::ENDS, seen[0], st);
+  static std::atomic<uint64_t> seen[3];
+  cudaError_t e = registers_there(selective_backward_kernel<T, P>, seen[2]);
+  if (e == cudaSuccess && a.segments > 1) e = launch(selective_ends_kernel<T, P, true>, a, a.segments - 1, SelCfg<P, kFwdSteps>::ENDS, seen[0], st);
   if (e == cudaSuccess) e = launch(selective_backward_kernel<T, P>, a, a.segments, SelCfg<P, kSave>::BACK, seen[1], st);
   if (e != cudaSuccess) return e;
   if (c.length > 0) {
@@ -1063,8 +1073,6 @@ cudaError_t backward_p(const SelectiveCall& c, cudaStream_t st) {
 template <typename T>
 cudaError_t dispatch(const SelectiveCall& c, bool back, cudaStream_t st) {
   switch (lanes_of(c.states)) {
-    case 1: return back ? backward_p<T, 1>(c, st) : forward_p<T, 1>(c, st);
-    case 2: return back ? backward_p<T, 2>(c, st) : forward_p<T, 2>(c, st);
     case 4: return back ? backward_p<T, 4>(c, st) : forward_p<T, 4>(c, st);
     case 8: return back ? backward_p<T, 8>(c, st) : forward_p<T, 8>(c, st);
     default: return back ? backward_p<T, 16>(c, st) : forward_p<T, 16>(c, st);

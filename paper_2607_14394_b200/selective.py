@@ -591,6 +591,8 @@ class SelectiveMemory:
         norm, conv, scan = self._plan(B, T)
         H = self.H
         before, h0 = (None, None) if state is None else state
+        if training and state is not None and state_out is not None and any(o is not None and o is i for o, i in zip(state_out, state)):
+            raise ValueError("a backward pass needs the state as it was: state_out must be another one where training is True")
         n, s, stats = norm.forward(x, self.norm_weight, self.norm_bias, need_backward=training)
         uz = n @ self.W_in.t()
         after, h = (None, None) if state_out is None else state_out

@@ -296,6 +296,40 @@ def test_scan_steps_are_the_whole(dtype):
     close(h, host(last), "h", 3e-5)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scan_state_in_place_of_a_sequence_in_segments(dtype):
+    """Few channels and many steps: the state behind may take the place of the state in front while segments still read that."""
+    from paper_2607_14394_b200 import SelectiveScan
+    B, T, C, N = 2, 5000, 100, 16
+    v = scan_inputs(B, T, C, N, 1, dtype)
+    v["A"] = v["A"] * 1e-3                                # states that last: what is in front is seen everywhere
+    scan = SelectiveScan((B, T, C), N, 1, dtype)
+    ck = scan.new_checkpoints()
+    y, last = scan.forward(checkpoints=ck, **v)
+    h0 = v["h0"].clone()
+    gy, gl = rand(B, T, C, dtype=dtype, seed=50), rand(B, C, N, seed=51)
+    g = scan.backward(gy, checkpoints=ck, grad_last=gl, **v)
+    for _ in range(5):
+        v["h0"] = h0.clone()
+        again, same = scan.forward(h_last=v["h0"], **v)
+        assert same is v["h0"] and torch.equal(again, y) and torch.equal(same, last)
+        at = gl.clone()
+        h = scan.backward(gy, checkpoints=ck, grad_last=at, out={"h0": at}, **v)
+        assert h["h0"] is at and all(torch.equal(h[k], g[k]) for k in g)
+
+
+def test_scan_without_steps():
+    from paper_2607_14394_b200 import SelectiveScan
+    v = scan_inputs(2, 0, 10, 5, 1, F32, strided=False)
+    scan = SelectiveScan((2, 0, 10), 5)
+    ck = scan.new_checkpoints()
+    y, last = scan.forward(checkpoints=ck, **v)
+    gl = rand(2, 10, 5, seed=3)
+    g = scan.backward(torch.empty(2, 0, 10, device="cuda"), checkpoints=ck, grad_last=gl, **v)
+    assert y.shape == (2, 0, 10) and torch.equal(last, v["h0"]) and torch.equal(g["h0"], gl)
+    assert not g["A"].any() and not g["D"].any() and not g["dt_bias"].any() and g["B"].shape == (2, 0, 1, 5)
+
+
 def test_scan_gradient_against_differences():
     from paper_2607_14394_b200 import SelectiveScan
     B, T, C, N = 2, 20, 24, 16

@@ -318,9 +318,14 @@ cudaError_t launch_k(ConvArgs a, bool back, int* parts, cudaStream_t st) {
     }
     return launch_pdl(conv_forward_kernel<T, V, K, VEC>, dim3((unsigned)groups, (unsigned)rows), dim3(32, kWarps), 0, st, a);
   }
-  const int most = conv_parts(a.B, a.T, a.C);
+  // as many CTAs as run at once
+  static Resident seen;
+  auto kern = conv_backward_kernel<T, V, K, VEC>;
+  long long most = resident_ctas((const void*)kern, 32 * kWarps, 0, seen) / groups;
+  if (most < 1) most = 1;
+  if (most > conv_parts(a.C)) most = conv_parts(a.C);
   *parts = (int)(rows < most ? rows : most);
-  return launch_pdl(conv_backward_kernel<T, V, K, VEC>, dim3((unsigned)groups, (unsigned)*parts), dim3(32, kWarps), 0, st, a);
+  return launch_pdl(kern, dim3((unsigned)groups, (unsigned)*parts), dim3(32, kWarps), 0, st, a);
 }
 
 template <typename T, int V, bool VEC>
@@ -356,12 +361,6 @@ cudaError_t launch(const ConvArgs& a, int dtype, int width, bool back, int* part
 }
 
 }  // namespace
-
-int conv_parts(long long, long long, long long channels) {
-  // enough CTAs over all channel groups to fill the GPU several times
-  const long long groups = (channels + 127) / 128, want = ((long long)148 * 8 + groups - 1) / groups;
-  return (int)(want < 16 ? 16 : want > 256 ? 256 : want);
-}
 
 cudaError_t launch_conv_forward(const ConvCall& c, cudaStream_t st) {
   ConvArgs a{};

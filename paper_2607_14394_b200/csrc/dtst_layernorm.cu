@@ -181,10 +181,12 @@ template <typename T, int TPR, int ITEMS, int LAY>
 cudaError_t launch_rows_kernel(const RowArgs& a, cudaStream_t st) {
   constexpr int RPC = kRowThreads<TPR> / TPR;
   // as many CTAs as run at once, or a row each; a multiple of VEC, so that a group's rows begin alike
-  const long long most = (long long)num_sms() * (2048 / kRowThreads<TPR> < 8 ? 2048 / kRowThreads<TPR> : 8) / kVec<T> * kVec<T>;
+  static Resident seen;
+  auto kern = layer_norm_rows_kernel<T, TPR, ITEMS, LAY>;
+  const long long most = resident_ctas((const void*)kern, kRowThreads<TPR>, 0, seen) / kVec<T> * kVec<T>;
   long long ctas = (a.rows + RPC - 1) / RPC;
   if (ctas > most) ctas = most;
-  return launch_pdl(layer_norm_rows_kernel<T, TPR, ITEMS, LAY>, dim3((unsigned)ctas), dim3(kRowThreads<TPR>), 0, st, a);
+  return launch_pdl(kern, dim3((unsigned)ctas), dim3(kRowThreads<TPR>), 0, st, a);
 }
 
 template <typename T>
@@ -218,8 +220,9 @@ struct RowBackArgs {
   long long rows, C;
 };
 
+// (Three CTAs an SM where 256 threads hold a row: bf16 [16384][2048] 78 -> 71 us; the other sizes would spill.)
 template <typename T, int TPR, int ITEMS, int LAY>
-__global__ void __launch_bounds__(kRowThreads<TPR>) layer_norm_rows_backward_kernel(const RowBackArgs a) {
+__global__ void __launch_bounds__(kRowThreads<TPR>, TPR == 256 && LAY == kAligned ? 3 : 1) layer_norm_rows_backward_kernel(const RowBackArgs a) {
   constexpr int VEC = kVec<T>;
   constexpr int RPC = kRowThreads<TPR> / TPR;
   __shared__ float2 red[64];
@@ -698,17 +701,23 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
   const int ny = a.C <= 32 ? 4 : 16, nch = (int)((a.C + ny - 1) / ny);
   const int per = 32 * (vec ? most_wide : 1);
   a.tiles = (a.inner + per - 1) / per;
-  // the parameters' partial sums are two rows per CTA
-  const long long most = BACK ? (long long)kNormParts : (long long)num_sms() * 16, all = a.outer * a.tiles;
-  const dim3 grid((unsigned)(all < most ? all : most)), block(32, ny);
-  *parts = (int)grid.x;
+  const long long all = a.outer * a.tiles;
+  const dim3 block(32, ny);
+  const auto go = [&](auto kern, Resident& seen) {      // (backward: the parameters' partial sums are two rows per CTA)
+    long long most = resident_ctas((const void*)kern, 32 * ny, 0, seen);
+    if (BACK && most > kNormParts) most = kNormParts;
+    const dim3 grid((unsigned)(all < most ? all : most));
+    *parts = (int)grid.x;
+    return launch_pdl(kern, grid, block, 0, st, a);
+  };
 #define DTST_FIELD(W, N, WIDTH)                                                                                   \
   if (nch <= N && ny == W) {                                                                                      \
-    if (BACK)                                                                                                     \
-      return vec ? launch_pdl(layer_norm_field_backward_kernel<T, W, WIDTH, N>, grid, block, 0, st, a)            \
-                 : launch_pdl(layer_norm_field_backward_kernel<T, W, 1, N>, grid, block, 0, st, a);               \
-    return vec ? launch_pdl(layer_norm_field_kernel<T, W, WIDTH, N>, grid, block, 0, st, a)                       \
-               : launch_pdl(layer_norm_field_kernel<T, W, 1, N>, grid, block, 0, st, a);                          \
+    static Resident seen[2];                                                                                      \
+    if constexpr (BACK)                                                                                           \
+      return vec ? go(layer_norm_field_backward_kernel<T, W, WIDTH, N>, seen[0])                                  \
+                 : go(layer_norm_field_backward_kernel<T, W, 1, N>, seen[1]);                                     \
+    else                                                                                                          \
+      return vec ? go(layer_norm_field_kernel<T, W, WIDTH, N>, seen[0]) : go(layer_norm_field_kernel<T, W, 1, N>, seen[1]); \
   }
   DTST_FIELD(4, 2, WIDE)
   DTST_FIELD(4, 5, WIDE)
@@ -717,6 +726,21 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
   DTST_FIELD(16, 8, 2)
 #undef DTST_FIELD
   return cudaErrorNotSupported;
+}
+
+template <typename T, int TPR, int ITEMS, int LAY>
+cudaError_t launch_rows_backward_kernel(const RowBackArgs& a, int* parts, cudaStream_t st) {
+  constexpr int RPC = kRowThreads<TPR> / TPR;
+  static Resident seen;
+  auto kern = layer_norm_rows_backward_kernel<T, TPR, ITEMS, LAY>;
+  const size_t smem = RPC > 1 ? sizeof(float) * RPC * a.C : 0;
+  // as many CTAs as run at once (each leaves a row of partial sums); rows of a group that begin alike need a multiple of VEC
+  long long most = resident_ctas((const void*)kern, kRowThreads<TPR>, RPC > 1 ? sizeof(float) * RPC * ITEMS * TPR * kVec<T> : 0, seen);
+  if (most > kNormParts) most = kNormParts;
+  most = most / kVec<T> * kVec<T>;
+  const long long ctas = (a.rows + RPC - 1) / RPC;
+  *parts = (int)(ctas < most ? ctas : most);
+  return launch_pdl(kern, dim3((unsigned)*parts), dim3(kRowThreads<TPR>), smem, st, a);
 }
 
 template <typename T>
@@ -729,14 +753,9 @@ cudaError_t launch_rows_backward(const RowBackArgs& a, int* parts, cudaStream_t 
   const long long groups = row_groups<T>(a.C, lay);
 #define DTST_ROWS(TPR, ITEMS)                                                                                     \
   {                                                                                                               \
-    constexpr int RPC = kRowThreads<TPR> / TPR;                                                                   \
-    const long long ctas = (a.rows + RPC - 1) / RPC;                                                              \
-    *parts = (int)(ctas < kNormParts ? ctas : kNormParts);                                                        \
-    const dim3 grid((unsigned)*parts), block(kRowThreads<TPR>);                                                   \
-    const size_t smem = RPC > 1 ? sizeof(float) * RPC * a.C : 0;                                                  \
-    if (lay == kAligned) return launch_pdl(layer_norm_rows_backward_kernel<T, TPR, ITEMS, kAligned>, grid, block, smem, st, a); \
-    if (lay == kShifted) return launch_pdl(layer_norm_rows_backward_kernel<T, TPR, ITEMS, kShifted>, grid, block, smem, st, a); \
-    return launch_pdl(layer_norm_rows_backward_kernel<T, TPR, ITEMS, kScalar>, grid, block, smem, st, a);         \
+    if (lay == kAligned) return launch_rows_backward_kernel<T, TPR, ITEMS, kAligned>(a, parts, st);               \
+    if (lay == kShifted) return launch_rows_backward_kernel<T, TPR, ITEMS, kShifted>(a, parts, st);               \
+    return launch_rows_backward_kernel<T, TPR, ITEMS, kScalar>(a, parts, st);                                     \
   }
   if (groups <= 32) DTST_ROWS(32, 1)
   if (groups <= 64) DTST_ROWS(32, 2)

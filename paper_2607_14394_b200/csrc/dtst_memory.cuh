@@ -21,6 +21,30 @@ inline cudaError_t allow_smem(const void* kern, size_t bytes, std::atomic<uint64
   return e;
 }
 
+// CTAs of a kernel that run at once on the current device (`seen`: per device, kept by the caller's static of that kernel; a racing
+// second call sets the same value).  A grid of a little more than that many, each walking over its share, would run twice as long.
+struct Resident {
+  std::atomic<int> n[64];
+};
+inline int resident_ctas(const void* kern, int threads, size_t smem, Resident& seen) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    (void)cudaGetLastError();
+    return num_sms();
+  }
+  int n = seen.n[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    int per_sm = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, threads, smem) != cudaSuccess || per_sm < 1) {
+      (void)cudaGetLastError();
+      per_sm = 1;
+    }
+    n = per_sm * num_sms();
+    seen.n[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
 // As launch_pdl, for thread-block clusters of `cluster` CTAs (0: the kernel's own cluster size).
 template <typename Kern, typename... Args>
 inline cudaError_t launch_clusters(Kern kern, unsigned ctas, int cluster, int threads, size_t smem, cudaStream_t st, const Args&... args) {
@@ -113,7 +137,11 @@ struct ConvCall {
   void *y, *state_out, *grad_x, *grad_state;
   float *grad_weight, *grad_bias, *partial;
 };
-int conv_parts(long long batch, long long length, long long channels);   // most rows of partial sums of the backward pass
+// most rows of partial sums of the convolution's backward pass: 16 CTAs on each of 148 SMs, over the groups of channels
+inline int conv_parts(long long channels) {
+  const long long n = 16 * 148 / ((channels + 127) / 128);
+  return (int)(n < 1 ? 1 : n > 256 ? 256 : n);
+}
 cudaError_t launch_conv_forward(const ConvCall& c, cudaStream_t st);
 cudaError_t launch_conv_backward(const ConvCall& c, cudaStream_t st);
 

@@ -75,6 +75,15 @@ __device__ __forceinline__ float2 carry_on(float2 f, float2 h, float2 e) {
   return make_float2(h.x == 0.f ? e.x : fmaf(f.x, h.x, e.x), h.y == 0.f ? e.y : fmaf(f.y, h.y, e.y));
 }
 
+// Stores of the recurrence's sums.  They go to parts of shared memory that these warps never read, and the barrier behind them is
+// volatile too: without a word on memory the compiler may move the next step's reads up in front of them.
+__device__ __forceinline__ void put_shared(float* p, float v) {
+  asm volatile("st.shared.f32 [%0], %1;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "f"(v));
+}
+__device__ __forceinline__ void put_shared(float* p, float2 v) {
+  asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "f"(v.x), "f"(v.y));
+}
+
 struct SelArgs {
   Rows x, dt, z, B, C;
   const float *A, *D, *bias, *h0, *grad_last;
@@ -158,7 +167,7 @@ __device__ __forceinline__ float2 state_sums(float2 (&v)[4], int p) {
 template <int P, int LD>
 __device__ __forceinline__ void put_sums(float2 (&v)[4], float* rows, int p, int c) {
   const float2 t = state_sums<P>(v, p);
-  if (P == 4 || p % (P / 4) == 0) *reinterpret_cast<float2*>(rows + p / (P / 4) * LD + c) = t;
+  if (P == 4 || p % (P / 4) == 0) put_shared(rows + p / (P / 4) * LD + c, t);
 }
 
 // a tile's maps on their way to shared memory: an item is four states of one map at one step
@@ -433,8 +442,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_ends_kernel(const S
 // ------------------------------------------------------------------------------------------------ forward
 __device__ __forceinline__ void store_if(bool on, float* p, const float4& v) {      // (without a branch between the steps)
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %0, 0;\n\t@p st.global.v4.f32 [%1], {%2, %3, %4, %5};\n\t}" ::"r"((int)on), "l"(p), "f"(v.x),
-               "f"(v.y), "f"(v.z), "f"(v.w)
-               : "memory");
+               "f"(v.y), "f"(v.z), "f"(v.w));
 }
 
 template <typename T, int P>
@@ -621,13 +629,13 @@ __device__ __forceinline__ void channel_sums(F4& b, F4& c, int pl, float* out, i
     const float2 one = add_pair(make_float2(b2.x, c2.x), make_float2(swap(b2.y, 1), swap(c2.y, 1)));
     if constexpr (LANES == 8) {
       const bool up = pl & 4;
-      out[(up ? np : 0) + n0 + perm] = (up ? one.y : one.x) + swap(up ? one.x : one.y, 4);
+      put_shared(out + (up ? np : 0) + n0 + perm, (up ? one.y : one.x) + swap(up ? one.x : one.y, 4));
     } else {
-      out[n0 + perm] = one.x, out[np + n0 + perm] = one.y;
+      put_shared(out + n0 + perm, one.x), put_shared(out + np + n0 + perm, one.y);
     }
   } else {
-    out[n0 + perm] = b2.x, out[n0 + (1 ^ perm)] = b2.y;
-    out[np + n0 + perm] = c2.x, out[np + n0 + (1 ^ perm)] = c2.y;
+    put_shared(out + n0 + perm, b2.x), put_shared(out + n0 + (1 ^ perm), b2.y);
+    put_shared(out + np + n0 + perm, c2.x), put_shared(out + np + n0 + (1 ^ perm), c2.y);
   }
 }
 

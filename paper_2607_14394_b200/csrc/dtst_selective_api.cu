@@ -144,7 +144,7 @@ dtst_status dtst_causal_conv_scratch_bytes(const dtst_conv_desc* d, size_t* byte
   const dtst_status s = check_conv(d);
   if (s != DTST_OK) return s;
   if (bytes == nullptr) return DTST_ERR_INVALID_ARG;
-  *bytes = (size_t)conv_parts(d->batch, d->length, d->channels) * (size_t)d->channels * (size_t)(d->width + 1) * sizeof(float);
+  *bytes = (size_t)conv_parts(d->channels) * (size_t)d->channels * (size_t)(d->width + 1) * sizeof(float);
   return DTST_OK;
 }
 

@@ -244,15 +244,15 @@ __device__ __forceinline__ void read_row(float (&v)[V], const float* p) {
 
 template <int P, int TS>
 struct SelCfg {
-  static constexpr int DC = 2 * kThreads / P, NP = 4 * P;
-  static constexpr int PER = TS * DC / kThreads;              // elements a thread stages
-  static constexpr int V = PER < 4 ? PER : 4, ITEMS = PER / V, VECS = DC / V, ROWS = kThreads / VECS;
-  static constexpr int LD = DC + (DC % 32 == 0 ? 4 : 0);
-  static constexpr int LANES = 32 / P;                        // pairs of channels in a warp
-  static constexpr int PERMS = LANES >= 4 ? 4 : LANES;
-  static constexpr size_t FWD = sizeof(float) * ((size_t)2 * TS * DC * 2 + 2 * TS * 2 * NP + 2 * TS * LD);
-  static constexpr size_t ENDS = sizeof(float) * ((size_t)2 * TS * DC * 2 + 2 * TS * NP);
-  static constexpr size_t BACK = sizeof(float) * ((size_t)2 * TS * DC * 3 + 2 * TS * 2 * NP * PERMS + 6 * TS * LD + 2 * kThreads / 32 * TS * 2 * NP);
+  [[maybe_unused]] static constexpr int DC = 2 * kThreads / P, NP = 4 * P;
+  [[maybe_unused]] static constexpr int PER = TS * DC / kThreads;              // elements a thread stages
+  [[maybe_unused]] static constexpr int V = PER < 4 ? PER : 4, ITEMS = PER / V, VECS = DC / V, ROWS = kThreads / VECS;
+  [[maybe_unused]] static constexpr int LD = DC + (DC % 32 == 0 ? 4 : 0);
+  [[maybe_unused]] static constexpr int LANES = 32 / P;                        // pairs of channels in a warp
+  [[maybe_unused]] static constexpr int PERMS = LANES >= 4 ? 4 : LANES;
+  [[maybe_unused]] static constexpr size_t FWD = sizeof(float) * ((size_t)2 * TS * DC * 2 + 2 * TS * 2 * NP + 2 * TS * LD);
+  [[maybe_unused]] static constexpr size_t ENDS = sizeof(float) * ((size_t)2 * TS * DC * 2 + 2 * TS * NP);
+  [[maybe_unused]] static constexpr size_t BACK = sizeof(float) * ((size_t)2 * TS * DC * 3 + 2 * TS * 2 * NP * PERMS + 6 * TS * LD + 2 * kThreads / 32 * TS * 2 * NP);
 };
 constexpr int kFwdSteps = 16;          // steps to a tile forward
 

@@ -644,6 +644,7 @@ dtst_status dtst_causal_conv_backward(const dtst_conv_desc* desc, const void* gr
  * given, the rest contiguous; y contiguous.  A [channels, states], D, dt_bias [channels] float32 (D, dt_bias, z may be NULL).
  * A is meant to be negative.  Where it is positive, products of decays over long runs of steps are formed in float32; a product
  * beyond its range passes a state of zero and makes any other an infinity or a NaN.
+ * At most 65535 batch entries and 2^24 channels (DTST_ERR_UNSUPPORTED beyond).
  * h0, h_last [batch, channels, states] float32: the state in front (NULL: zeros) and behind (NULL: not wanted); they may be the same
  * buffer.  lengths as of dtst_causal_conv: h_last is the state behind the entry's own last step.  y takes no input's place.
  * checkpoints: NULL, or dtst_selective_scan_checkpoints floats (16-byte aligned), which receive the states the backward pass
@@ -683,7 +684,7 @@ dtst_status dtst_selective_scan_backward(const dtst_selective_desc* desc, const 
  *   norm = sqrt(sum over tensors and elements of grad^2),   c = min(1, max_norm / (norm + eps)),   out = c grad
  * list [count]: contiguous tensors of n elements (a complex one: twice as many of its parts); n = 0 is passed over.  out NULL: the
  * tensor counts but is not scaled; out = grad: in place; otherwise it may lie over no other gradient or output
- * (DTST_ERR_INVALID_ARG).  max_norm >= 0 (infinite: c = 1), eps > 0.  norm: one float32.  Squares are summed in 64 bits: the norm is
+ * (DTST_ERR_INVALID_ARG).  max_norm >= 0 (infinite: c = 1 whatever the norm), eps > 0.  norm: one float32.  Squares are summed in 64 bits: the norm is
  * an infinity only where it is beyond float32 or an element is one.  An infinite norm makes c zero, a NaN makes it a NaN; nothing is left
  * out for either.  The list is read before the call returns.  scratch: dtst_grad_norm_scratch_bytes.
  */

@@ -109,7 +109,7 @@ __device__ __forceinline__ void coefficient(const ListArgs<N>& a, double* red, f
   const double norm = sqrt(block_sum(s, red));
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.norm != nullptr) *a.norm = (float)norm;
   double c = (double)a.max_norm / (norm + (double)a.eps);
-  if (c > 1.) c = 1.;                   // (a NaN stays)
+  if (c > 1. || isinf(a.max_norm)) c = 1.;      // (a NaN stays where there is a bound)
   const bool tiny = c < 0x1p-60;
   c_hi = tiny ? 0x1p-60f : 1.f;
   c_lo = (float)(tiny ? c * 0x1p60 : c);

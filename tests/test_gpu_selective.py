@@ -366,6 +366,28 @@ def test_scan_zero_state_passes_growing_decays():
     assert not y.any() and not last.any()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_expanded_and_shifted_inputs(dtype):
+    """Inputs that repeat (strides of zero) and rows that begin off a vector give the bits of their dense copies."""
+    from paper_2607_14394_b200 import CausalConv, SelectiveScan
+    B, T, C, N = 3, 77, 64, 16
+    v = scan_inputs(B, T, C, N, 1, dtype, strided=False)
+    scan, conv = SelectiveScan((B, T, C), N, 1, dtype), CausalConv((B, T, C), 4, dtype)
+    shifted = torch.empty(B, T, C + 1, dtype=dtype, device="cuda")[..., 1:]
+    shifted.copy_(v["dt"])
+    odd = dict(v, x=v["x"][:1, :1].expand(B, T, C), dt=shifted, z=v["z"][:1].expand(B, T, C), B=v["B"][:, :1].expand(B, T, 1, N))
+    dense = {k: t if t is None else t.contiguous() for k, t in odd.items()}
+    gy, gl = rand(B, T, C, dtype=dtype, seed=50), rand(B, C, N, seed=51)
+    out = []
+    for u in (odd, dense):
+        ck = scan.new_checkpoints()
+        y, last = scan.forward(checkpoints=ck, **u)
+        g = scan.backward(gy, checkpoints=ck, grad_last=gl, **u)
+        w, b = rand(C, 4, seed=1), rand(C, seed=2)
+        out.append([y, last, *g.values(), *conv.forward(u["x"], w, b), *conv.backward(gy, u["dt"], w, b)])
+    assert all(torch.equal(p, q) for p, q in zip(*out))
+
+
 def test_far_offsets():
     """More than 2^31 elements: the last steps of a long sequence, whose states forget within a few steps, by themselves."""
     from paper_2607_14394_b200 import CausalConv, LayerNorm, SelectiveScan
@@ -438,6 +460,9 @@ def test_clip_of_many_tensors_and_far_values():
     t = rand(100, seed=4)
     t[7] = float("inf")
     assert float(clip_grad_norm([t], 1.0)) == float("inf") and torch.isnan(t[7]) and float(t[6]) == 0.0
+    t[7] = float("inf")
+    before = t.clone()
+    assert float(clip_grad_norm([t], float("inf"))) == float("inf") and torch.equal(t, before)       # without a bound nothing is scaled
     t = rand(100, seed=4)
     t[7] = float("nan")
     assert torch.isnan(clip_grad_norm([t], 1.0)) and torch.isnan(t).all()

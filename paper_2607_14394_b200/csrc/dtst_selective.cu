@@ -254,7 +254,10 @@ struct SelCfg {
   [[maybe_unused]] static constexpr size_t ENDS = sizeof(float) * ((size_t)2 * TS * DC * 2 + 2 * TS * NP);
   [[maybe_unused]] static constexpr size_t BACK = sizeof(float) * ((size_t)2 * TS * DC * 3 + 2 * TS * 2 * NP * PERMS + 6 * TS * LD + 2 * kThreads / 32 * TS * 2 * NP);
 };
-constexpr int kFwdSteps = 16;          // steps to a tile forward
+// Steps to a tile forward: 4 x 2048 x 4096, 16 states, takes 276 us with 16, 396 with 8 (what a tile costs both halves of a CTA however
+// long it is), 353 with 32 (its operands need registers twice as long); backward 8, the steps between saved states (16: 884 us against 804,
+// spills).
+constexpr int kFwdSteps = 16;
 
 // A of a thread's states, times log2(e)
 __device__ __forceinline__ void load_A(F4 (&A2)[2], const SelArgs& a, int c, int ch, int left, int p, int perm) {
@@ -415,7 +418,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) selective_ends_kernel(const S
     const float4* dr = reinterpret_cast<const float4*>(dd + buf * TS * DC) + ch / 2;
     const float4* mr = maps + buf * MapsT::WORDS + p;
     wait_for(kFull + buf);
-#pragma unroll
+#pragma unroll 8      // (sixteen would spill)
     for (int n = 0; n < TS; ++n) {
       const int s = BACK ? TS - 1 - n : n;
       const float4 d = dr[s * CP];
@@ -949,7 +952,7 @@ __global__ void __launch_bounds__(256) selective_maps_kernel(const MapArgs a) {
     if (n >= a.states) continue;
     float s = 0.f;
     if (a.lengths == nullptr || t < a.lengths[b])
-#pragma unroll 8
+#pragma unroll 16
       for (int k = 0; k < a.blocks; ++k) s += a.part[k * total + i];
     const Rows& o = which ? a.gC : a.gB;
     static_cast<T*>(o.p)[b * o.batch + t * o.step + g * a.states + n] = Elem<T>::put(s);

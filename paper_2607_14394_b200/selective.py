@@ -497,9 +497,13 @@ class GradNorm:
                 return self._run(entries, max_norm, eps, norm, None)
         if norm is None:
             norm = torch.empty((), dtype=_F32, device=self.device)
+            np = norm.data_ptr()
+        else:
+            np = _addr(norm, "norm", d, _F32, self._shape)
+        # the call's own, from the current stream's allocations: calls on other streams may be under way
         scratch = torch.empty(self._scratch_bytes, dtype=torch.uint8, device=self.device)
-        status = self._lib.dtst_clip_grad_norm(entries, len(entries), max_norm, eps, _addr(norm, "norm", d, _F32, self._shape),
-                                               scratch.data_ptr(), self._scratch_bytes, Mem._raw_stream(d))
+        status = self._lib.dtst_clip_grad_norm(entries, len(entries), max_norm, eps, np, scratch.data_ptr(), self._scratch_bytes,
+                                               Mem._raw_stream(d))
         if status:
             _check(status, "dtst_clip_grad_norm")
         return norm

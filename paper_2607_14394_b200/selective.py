@@ -536,6 +536,9 @@ class SelectiveMemory:
     forward(x) -> (out, state) and backward(grad_out) -> gradients of x, of the state in front and of every parameter; step() is the
     form for one new frame.  A state is (the convolution's last inputs [B, width - 1, H], h [B, H, states]).  Parameters are
     plain tensors owned by this object (`parameters()`); the projections are plain matrix products.
+
+    Behind an entry's own length `out` is x and the gradient of x that of `out`, whatever they hold there; neither reaches a
+    state or a parameter's gradient.
     """
 
     NAMES = ("norm_weight", "norm_bias", "W_in", "conv_weight", "conv_bias", "W_x", "W_dt", "dt_bias", "A_log", "D", "W_out")
@@ -597,7 +600,13 @@ class SelectiveMemory:
         before, h0 = (None, None) if state is None else state
         if training and state is not None and state_out is not None and any(o is not None and o is i for o, i in zip(state_out, state)):
             raise ValueError("a backward pass needs the state as it was: state_out must be another one where training is True")
-        n, s, stats = norm.forward(x, self.norm_weight, self.norm_bias, need_backward=training)
+        own = seen = None
+        if lengths is not None and training:
+            # the parameters' gradients are sums over all rows, and zero times a NaN is no zero: chosen, not multiplied
+            _addr(lengths, "lengths", norm.dev, _I32, conv._lshape)
+            own = (torch.arange(T, device=x.device) < lengths[:, None]).unsqueeze(-1)
+            seen = torch.where(own, x, 0)
+        n, s, stats = norm.forward(x if seen is None else seen, self.norm_weight, self.norm_bias, need_backward=training)
         uz = n @ self.W_in.t()
         after, h = (None, None) if state_out is None else state_out
         u, after = conv.forward(uz[..., :H], self.conv_weight, self.conv_bias, state=before, lengths=lengths, state_out=after)
@@ -608,7 +617,7 @@ class SelectiveMemory:
         y, h = scan.forward(u, dt, A, Bm, Cm, D=self.D, z=uz[..., H:], dt_bias=self.dt_bias, h0=h0, lengths=lengths, h_last=h,
                             checkpoints=ck)
         out = x + y @ self.W_out.t()
-        self.saved = (s, n, stats, uz, u, both, dt, A, y, ck, before, h0, lengths) if training else None
+        self.saved = (s, n, stats, uz, u, both, dt, A, y, ck, before, h0, lengths, own) if training else None
         return out, (after, h)
 
     def step(self, frame, state, stream=None):
@@ -622,13 +631,13 @@ class SelectiveMemory:
                 return self.backward(grad_out, grad_state)
         if self.saved is None:
             raise RuntimeError("backward follows a forward pass with training=True")
-        s, n, stats, uz, u, both, dt, A, y, ck, before, h0, lengths = self.saved
+        s, n, stats, uz, u, both, dt, A, y, ck, before, h0, lengths, own = self.saved
         grad_out = grad_out.contiguous()
         B, T, D = grad_out.shape
         norm, conv, scan = self._plan(B, T)
         H, R, S, flat = self.H, self.rank, self.states, lambda t: t.flatten(0, 1)
         g_after, g_last = (None, None) if grad_state is None else grad_state
-        gr = {"W_out": flat(grad_out).t() @ flat(y)}
+        gr = {"W_out": flat(grad_out if own is None else torch.where(own, grad_out, 0)).t() @ flat(y)}
         gy = grad_out @ self.W_out
         guz, gboth = torch.empty_like(uz), torch.empty_like(both)
         g = scan.backward(gy, u, dt, A, both[..., R:R + S].unsqueeze(2), both[..., R + S:].unsqueeze(2), ck, D=self.D, z=uz[..., H:],

@@ -1,0 +1,50 @@
+"""The selective memory's operators and block as they are called on the GPU: padded batches, batches of many entries, states that
+decay at once, buffers that share memory, against the float64 statement or against the same call in another form.
+
+Tolerances as in test_gpu_selective: a stored value is off by half a unit in its last place (2^-24 of its size in float32, 2^-8
+in bfloat16, 2^-11 in float16), sums in 32 bits by 1e-5, the scan's chains by 3e-5.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import selective_oracle as S
+
+torch = pytest.importorskip("torch")
+from test_gpu_selective import BF16, F16, F32, TYPES, close, host, rand, scan_inputs
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ the block
+@pytest.mark.parametrize("bad", [0.0, float("nan"), float("inf")])
+def test_block_trains_on_ragged_batches(bad):
+    """What lies behind an entry's end, in x and in the outputs' gradient, reaches no parameter's gradient: they are the sums of those
+    of the entries by themselves (float32: the chain of test_block_gradients_against_autograd, sums over entries in another
+    order)."""
+    from paper_2607_14394_b200 import SelectiveMemory, clip_grad_norm
+    B, T, D, H, N = 4, 23, 24, 48, 8
+    lengths = [23, 0, 7, 30]                                  # (beyond T: T)
+    m = SelectiveMemory(D, H, N, rank=3, dtype=F32, seed=3)
+    x, state, go = rand(B, T, D, seed=1), (rand(B, 3, H, seed=2), rand(B, H, N, seed=3)), rand(B, T, D, seed=4)
+    gs = (rand(B, 3, H, seed=5), rand(B, H, N, seed=6))
+    want, outs = {k: 0.0 for k in m.NAMES}, []
+    for b, n in enumerate(lengths):
+        n = min(n, T)
+        e = slice(b, b + 1)
+        out, new = m.forward(x[e, :n], tuple(s[e] for s in state))
+        g = m.backward(go[e, :n], tuple(s[e] for s in gs))
+        for k in m.NAMES:
+            want[k] = want[k] + g[k].double()
+        outs.append((out, *new, g["x"], g["conv_state"], g["h0"]))
+        x[b, n:], go[b, n:] = bad, bad
+    out, new = m.forward(x, state, lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+    g = m.backward(go, gs)
+    for k in m.NAMES:
+        close(g[k], host(want[k]), k, 1e-4)
+    for b, n in enumerate(lengths):
+        got = (out[b:b + 1, :n], *(s[b:b + 1] for s in new), g["x"][b:b + 1, :n], g["conv_state"][b:b + 1], g["h0"][b:b + 1])
+        for p, q, name in zip(got, outs[b], ("out", "conv state", "h", "x", "grad conv_state", "grad h0")):
+            close(p, host(q), (b, name), 1e-4)
+    assert torch.isfinite(clip_grad_norm({k: g[k] for k in m.NAMES}, 1.0))

@@ -642,7 +642,7 @@ dtst_status dtst_causal_conv_backward(const dtst_conv_desc* desc, const void* gr
  *   y_t[c] = (sum_n C_t[g, n] h_t[c, n] + D[c] x_t[c])   z_t[c] / (1 + exp(-z_t[c])) where z is given
  * x, dt, z [batch, length, channels], B, C [batch, length, groups, states]: elements between batch entries and between steps as
  * given, the rest contiguous; y contiguous.  A [channels, states], D, dt_bias [channels] float32 (D, dt_bias, z may be NULL).
- * A is meant to be negative.  Where it is positive, products of decays over long runs of steps are formed in float32; a product
+ * A is meant to be negative (minus infinity: the state keeps nothing from step to step).  Where it is positive, products of decays over long runs of steps are formed in float32; a product
  * beyond its range passes a state of zero and makes any other an infinity or a NaN.
  * At most 65535 batch entries and 2^24 channels (DTST_ERR_UNSUPPORTED beyond).
  * h0, h_last [batch, channels, states] float32: the state in front (NULL: zeros) and behind (NULL: not wanted); they may be the same

@@ -22,6 +22,8 @@
 // what its bytes take.  Shared memory delivers a word a lane and clock however many lanes share it, so the two channels a thread
 // that share the maps' words bring those reads down to the same.
 // All sums are formed in a fixed order: same bits on every run.
+#include <cfloat>
+
 #include "dtst_common.cuh"
 #include "dtst_memory.cuh"
 #include "dtst_types.cuh"
@@ -259,7 +261,9 @@ struct SelCfg {
 // spills).
 constexpr int kFwdSteps = 16;
 
-// A of a thread's states, times log2(e)
+// A of a thread's states, times log2(e).  Kept finite: a step of zero, which stands behind a sequence's end, decays nothing, and the
+// gradient of a decay to zero is zero; with an infinity both would be a NaN.
+__device__ __forceinline__ float finite_below(float v) { return v < -FLT_MAX ? -FLT_MAX : v; }
 __device__ __forceinline__ void load_A(F4 (&A2)[2], const SelArgs& a, int c, int ch, int left, int p, int perm) {
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -267,7 +271,10 @@ __device__ __forceinline__ void load_A(F4 (&A2)[2], const SelArgs& a, int c, int
     if (ch + k >= left) continue;
     A2[k] = four(a.A + (long long)(c + k) * a.states, 4 * p, a.states, perm);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) A2[k].v[j] = mul_pair(A2[k].v[j], twice(kLog2e));
+    for (int j = 0; j < 2; ++j) {
+      const float2 q = mul_pair(A2[k].v[j], twice(kLog2e));
+      A2[k].v[j] = make_float2(finite_below(q.x), finite_below(q.y));
+    }
   }
 }
 // The state in front of (the gradient behind) the whole sequence, then what a segment finds, joined over the segments in front of

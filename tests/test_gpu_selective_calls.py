@@ -48,3 +48,29 @@ def test_block_trains_on_ragged_batches(bad):
         for p, q, name in zip(got, outs[b], ("out", "conv state", "h", "x", "grad conv_state", "grad h0")):
             close(p, host(q), (b, name), 1e-4)
     assert torch.isfinite(clip_grad_norm({k: g[k] for k in m.NAMES}, 1.0))
+
+
+# ------------------------------------------------------------------------------------------------ scan
+@pytest.mark.parametrize("B,T,lengths", [(2, 1, None), (2, 3, [0, 2]), (1, 16, None), (3, 37, [37, 5, 0]), (2, 1000, [1000, 130])])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scan_states_that_decay_at_once(B, T, lengths, dtype):
+    """A of minus infinity (and beyond float32 once in powers of two) keeps nothing of a state from step to step, as an A of
+    -1e30 does: the same bits forward and backward, at every length, and a state passes an entry without steps."""
+    from paper_2607_14394_b200 import SelectiveScan
+    C, N = 20, 6
+    v = scan_inputs(B, T, C, N, 1, dtype)
+    ln = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    scan = SelectiveScan((B, T, C), N, 1, dtype)
+    gy, gl = rand(B, T, C, dtype=dtype, seed=50), rand(B, C, N, seed=51)
+    got = []
+    for a in (-1e30, float("-inf"), -3.0e38):
+        v["A"][:, 2], v["A"][3] = a, a
+        ck = scan.new_checkpoints()
+        y, last = scan.forward(lengths=ln, checkpoints=ck, **v)
+        got.append([y, last, *scan.backward(gy, checkpoints=ck, lengths=ln, grad_last=gl, **v).values()])
+    v["A"][:, 2], v["A"][3] = -1e30, -1e30
+    want = S.selective_scan(lengths=lengths, **{k: host(t) for k, t in v.items()})
+    close(got[0][0], want[0], "y", 3e-5)
+    close(got[0][1], want[1], "h_last", 3e-5)
+    for other in got[1:]:
+        assert all(torch.equal(p, q) for p, q in zip(got[0], other))

@@ -605,8 +605,8 @@ dtst_status dtst_layer_norm_backward(int dtype, int64_t outer, int64_t channels,
                                      float* grad_weight, float* grad_bias, void* scratch, size_t scratch_bytes, void* stream);
 
 /*
- * Causal convolution of every channel by itself along the steps of x [batch, length, channels]; width 1 to 4 (wider:
- * DTST_ERR_UNSUPPORTED):
+ * Causal convolution of every channel by itself along the steps of x [batch, length, channels]; width 1 to 4, and at most 2^30
+ * batch entries, steps and channels (beyond: DTST_ERR_UNSUPPORTED):
  *   u = the width - 1 steps of `state`, then x;   pre_t[c] = bias[c] + sum_k weight[c, k] u_{t+k}[c];   y = act(pre)
  *   DTST_ACT_NONE: act(p) = p        DTST_ACT_SILU: act(p) = p / (1 + exp(-p))
  * x: x_stride = elements between batch entries and between steps, channels contiguous; y contiguous.  weight [channels, width] and

@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(32 * kWarps) conv_forward_kernel(const ConvArg
   pdl_trigger();
   pdl_wait();
   const long long c = ((long long)blockIdx.x * 32 + threadIdx.x) * V;
-  const long long unit = (long long)blockIdx.y * kWarps + threadIdx.y;
+  const long long unit = ((long long)blockIdx.z * gridDim.y + blockIdx.y) * kWarps + threadIdx.y;
   if (c >= a.C || unit >= a.B * a.runs) return;
   const int left = (int)(a.C - c < V ? a.C - c : V);
   const Run r(a, unit);
@@ -370,15 +370,11 @@ cudaError_t launch_k(ConvArgs a, bool back, int* parts, cudaStream_t st) {
   a.runs = (int)((a.T + a.run - 1) / a.run);
   if (a.runs < 1) a.runs = 1;                                    // no steps: the state alone
   const long long units = a.B * a.runs;
-  long long rows = (units + kWarps - 1) / kWarps;
+  const long long rows = (units + kWarps - 1) / kWarps;
   if (!back) {
-    if (rows > 65535) {                                          // more runs than a grid's second dimension holds
-      a.run = (int)((a.T * a.B / kWarps + 32767) / 32768 + 1);
-      a.runs = (int)((a.T + a.run - 1) / a.run);
-      rows = (a.B * a.runs + kWarps - 1) / kWarps;
-      if (rows > 65535) return cudaErrorNotSupported;
-    }
-    return launch_pdl(conv_forward_kernel<T, V, K, VEC>, dim3((unsigned)groups, (unsigned)rows), dim3(32, kWarps),
+    // (a grid's second dimension holds 65535: more of them go to the third)
+    const long long layers = (rows + 65534) / 65535, per = (rows + layers - 1) / layers;
+    return launch_pdl(conv_forward_kernel<T, V, K, VEC>, dim3((unsigned)groups, (unsigned)per, (unsigned)layers), dim3(32, kWarps),
                       Ring<T, V, VEC, kUnroll<K>, 1>::SMEM, st, a);
   }
   // as many CTAs as run at once

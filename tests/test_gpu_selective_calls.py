@@ -74,3 +74,20 @@ def test_scan_states_that_decay_at_once(B, T, lengths, dtype):
     close(got[0][1], want[1], "h_last", 3e-5)
     for other in got[1:]:
         assert all(torch.equal(p, q) for p, q in zip(got[0], other))
+
+
+# ------------------------------------------------------------------------------------------------ convolution
+@pytest.mark.parametrize("B,T,C,K", [(262145, 1, 2, 4), (262150, 3, 3, 3), (300001, 2, 1, 1), (140000, 130, 1, 2)])
+def test_conv_of_many_sequences(B, T, C, K):
+    """More runs than a grid's second dimension holds: the bits of the same batch in parts, the state in its own place."""
+    from paper_2607_14394_b200 import CausalConv
+    x, w, b = rand(B, T, C, seed=1), rand(C, K, seed=2), rand(C, seed=3)
+    s, ln = rand(B, K - 1, C, seed=4), torch.arange(B, device="cuda", dtype=torch.int32) % (T + 2)
+    y, last = CausalConv((B, T, C), K).forward(x, w, b, state=s, lengths=ln)
+    h = B // 3
+    for e in (slice(0, h), slice(h, 2 * h), slice(2 * h, B)):
+        part, plast = CausalConv((e.stop - e.start, T, C), K).forward(x[e], w, b, state=s[e], lengths=ln[e])
+        assert torch.equal(y[e], part) and torch.equal(last[e], plast)
+    state = s.clone()
+    again, same = CausalConv((B, T, C), K).forward(x, w, b, state=state, lengths=ln, state_out=state)
+    assert torch.equal(again, y) and torch.equal(same, last)

@@ -18,6 +18,7 @@ bool strides_ok(const int64_t (&s)[2], int64_t batch, int64_t length) {
 }
 // elements of a [batch][length][width] tensor of these strides never coincide
 bool distinct(const int64_t (&s)[2], int64_t batch, int64_t length, int64_t width) {
+  if (batch < 1 || length < 1) return true;
   if (batch < 2) return length < 2 || s[1] >= width;
   if (length < 2) return s[0] >= width;
   return (s[1] >= width && s[0] >= (length - 1) * s[1] + width) || (s[0] >= width && s[1] >= (batch - 1) * s[0] + width);

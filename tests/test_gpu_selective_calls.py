@@ -91,3 +91,19 @@ def test_conv_of_many_sequences(B, T, C, K):
     state = s.clone()
     again, same = CausalConv((B, T, C), K).forward(x, w, b, state=state, lengths=ln, state_out=state)
     assert torch.equal(again, y) and torch.equal(same, last)
+
+
+def test_conv_backward_without_steps_through_the_entry_point():
+    """Strides of an empty tensor make no elements coincide: the new state's gradient passes to the state, and the sums are empty."""
+    from paper_2607_14394_b200 import binding as Bn
+    B, C, K = 3, 8, 4
+    d = Bn.ConvDesc(0, 1, B, 0, C, K, 0, (0, C), (0, C))
+    w, b, s, gso = rand(C, K, seed=1), rand(C, seed=2), rand(B, K - 1, C, seed=3), rand(B, K - 1, C, seed=4)
+    gw, gb, gs = (torch.full_like(t, 9.0) for t in (w, b, s))
+    n = ctypes.c_size_t()
+    assert Bn.lib().dtst_causal_conv_scratch_bytes(ctypes.byref(d), ctypes.byref(n)) == Bn.DTST_OK
+    scratch = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    p = lambda t: ctypes.c_void_p(0 if t is None else t.data_ptr())
+    status = Bn.lib().dtst_causal_conv_backward(ctypes.byref(d), None, p(gso), None, p(w), p(b), p(s), None, None, p(gw), p(gb), p(gs), p(scratch), n.value,
+                                                ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    assert status == Bn.DTST_OK and torch.equal(gs, gso) and not gw.any() and not gb.any()

@@ -478,7 +478,8 @@ class GradNorm:
             if dtype not in DTYPES:
                 raise ValueError(f"gradients must be complex64 or one of {list(DTYPES)}, got {g.dtype}")
             size = g.numel() * (2 if g.dtype is torch.complex64 else 1)
-            _conj_free(g)
+            _as_it_lies(g)
+            _as_it_lies(o)
             e.grad, e.out = _addr(g, "gradient", self.dev, g.dtype, g.shape), _addr(o, "out", self.dev, g.dtype, g.shape)
             e.n, e.dtype = size, DTYPES[dtype]
         self._only = (Bn.GradTensor * n)(*self._list)
@@ -517,9 +518,9 @@ class GradNorm:
         return self._run(self._list, max_norm, eps, norm, stream)
 
 
-def _conj_free(t: torch.Tensor) -> None:
-    if t.is_complex() and t.is_conj():
-        raise ValueError("a conjugated view has no gradient of its own in memory (resolve_conj())")
+def _as_it_lies(t: torch.Tensor) -> None:
+    if t.is_conj() or t.is_neg():
+        raise ValueError("the values of a conjugated or negated view are not those in memory (resolve_conj(), resolve_neg())")
 
 
 def clip_grad_norm(grads, max_norm: float, eps: float = 1e-6, stream=None) -> torch.Tensor:

@@ -684,9 +684,10 @@ dtst_status dtst_selective_scan_backward(const dtst_selective_desc* desc, const 
  *   norm = sqrt(sum over tensors and elements of grad^2),   c = min(1, max_norm / (norm + eps)),   out = c grad
  * list [count]: contiguous tensors of n elements (a complex one: twice as many of its parts); n = 0 is passed over.  out NULL: the
  * tensor counts but is not scaled; out = grad: in place; otherwise it may lie over no other gradient or output
- * (DTST_ERR_INVALID_ARG).  max_norm >= 0 (infinite: c = 1 whatever the norm), eps > 0.  norm: one float32.  Squares are summed in 64 bits: the norm is
- * an infinity only where it is beyond float32 or an element is one.  An infinite norm makes c zero, a NaN makes it a NaN; nothing is left
- * out for either.  The list is read before the call returns.  scratch: dtst_grad_norm_scratch_bytes.
+ * (DTST_ERR_INVALID_ARG).  max_norm >= 0 (infinite: c = 1 whatever the norm), eps > 0.  norm: one float32, in none of the tensors
+ * (DTST_ERR_INVALID_ARG).  Squares are summed in 64 bits: the norm is an infinity only where it is beyond float32 or an element is one.
+ * An infinite norm makes c zero, a NaN makes it a NaN; nothing is left out for either.  The list is read before the call returns.
+ * scratch: dtst_grad_norm_scratch_bytes.
  */
 typedef struct {
   const void* grad;

@@ -280,12 +280,15 @@ dtst_status dtst_clip_grad_norm(const dtst_grad_tensor* list, int64_t count, flo
     struct Span { uintptr_t from, to; int64_t of; };
     std::vector<Span> written, read;
     entries.reserve((size_t)count);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(norm);
+    const auto holds_norm = [&](uintptr_t from, uintptr_t to) { return from < at + sizeof(float) && at < to; };
     for (int64_t k = 0; k < count; ++k) {
       const dtst_grad_tensor& t = list[k];
       if (!known(t.dtype) || t.n < 0 || t.n > kMostElements) return DTST_ERR_INVALID_ARG;
       if (t.n == 0) continue;
       if (t.grad == nullptr || !fits(t.grad, t.dtype) || !fits(t.out, t.dtype)) return DTST_ERR_INVALID_ARG;
       const uintptr_t bytes = (uintptr_t)t.n * elem(t.dtype), g = reinterpret_cast<uintptr_t>(t.grad), o = reinterpret_cast<uintptr_t>(t.out);
+      if (holds_norm(g, g + bytes) || (t.out != nullptr && holds_norm(o, o + bytes))) return DTST_ERR_INVALID_ARG;
       read.push_back({g, g + bytes, k});
       if (t.out != nullptr) written.push_back({o, o + bytes, k});
       entries.push_back({t.grad, t.out, t.n, t.dtype});

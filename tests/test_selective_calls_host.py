@@ -19,3 +19,14 @@ def test_views_that_negate_or_conjugate_are_no_gradients(calls):
             with pytest.raises(ValueError):
                 Sel.GradNorm(*pair)
     Sel.GradNorm([z.conj().resolve_conj()], out=[z])
+
+
+@pytest.mark.parametrize("spans,norm", [([(0x1000, 0x1000, 16)], 0x1004), ([(0x1000, 0, 16)], 0x103c), ([(0x1000, 0x5000, 16), (0x2000, 0x6000, 4)], 0x600c),
+                                        ([(0x3000, 0, 2), (0x1000, 0x5000, 16)], 0x1000)])
+def test_clip_refuses_a_norm_among_the_gradients(spans, norm):
+    """The norm is written while gradients are still read and scaled."""
+    L, e = Bn.lib(), entries(*spans)
+    call = lambda at: L.dtst_clip_grad_norm(e, len(spans), 1.0, 1e-6, ctypes.c_void_p(at), NULL, 0, NULL)
+    assert call(norm) == INVALID
+    for clear in (0x0ffc, 0x1040, 0x2ffc, 0x3008, 0x4ffc, 0x5040, 0x6010):          # beside them: what is missing is the scratch
+        assert call(clear) == Bn.DTST_ERR_WORKSPACE

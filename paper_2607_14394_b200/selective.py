@@ -528,6 +528,14 @@ def clip_grad_norm(grads, max_norm: float, eps: float = 1e-6, stream=None) -> to
     return GradNorm(grads).clip(max_norm, eps, stream=stream)
 
 
+def _meet(a: Optional[torch.Tensor], b: Optional[torch.Tensor]) -> bool:
+    """Whether two contiguous tensors share memory."""
+    if a is None or b is None:
+        return False
+    p, q = a.data_ptr(), b.data_ptr()
+    return p < q + b.numel() * b.element_size() and q < p + a.numel() * a.element_size()
+
+
 class SelectiveMemory:
     """A trainable selective memory on latent vectors x [B, T, D] of `dtype`, pre-normalised and residual:
 
@@ -599,7 +607,7 @@ class SelectiveMemory:
         norm, conv, scan = self._plan(B, T)
         H = self.H
         before, h0 = (None, None) if state is None else state
-        if training and state is not None and state_out is not None and any(o is not None and o is i for o, i in zip(state_out, state)):
+        if training and state is not None and state_out is not None and any(_meet(o, i) for o in state_out for i in state):
             raise ValueError("a backward pass needs the state as it was: state_out must be another one where training is True")
         own = seen = None
         if lengths is not None and training:

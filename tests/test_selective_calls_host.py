@@ -30,3 +30,17 @@ def test_clip_refuses_a_norm_among_the_gradients(spans, norm):
     assert call(norm) == INVALID
     for clear in (0x0ffc, 0x1040, 0x2ffc, 0x3008, 0x4ffc, 0x5040, 0x6010):          # beside them: what is missing is the scratch
         assert call(clear) == Bn.DTST_ERR_WORKSPACE
+
+
+def test_training_keeps_the_state_in_front(calls):
+    """state_out may not lie where the state does, under whatever name: the backward pass reads the state as it was."""
+    B, T, D, H, N = 2, 3, 8, 8, 4
+    m = Sel.SelectiveMemory(D, H, N, dtype=torch.float32)
+    x, conv, h = torch.zeros(B, T, D), torch.zeros(B, 3, H), torch.zeros(2 * B, H, N)
+    for out in ((conv, torch.zeros(B, H, N)), (conv.view_as(conv), torch.zeros(B, H, N)), (torch.zeros_like(conv), h[:B]), (None, h[1:1 + B]),
+                (h.view(-1)[:B * 3 * H].view(B, 3, H), torch.zeros(B, H, N))):
+        with pytest.raises(ValueError, match="state as it was"):
+            m.forward(x, (conv, h[:B]), state_out=out)
+    m.forward(x, (conv, h[:B]), state_out=(conv, h[:B]), training=False)
+    m.forward(x, (conv, h[:B]), state_out=(torch.zeros_like(conv), h[B:]))
+    m.forward(x, (None, h[:B]), state_out=(conv, None))

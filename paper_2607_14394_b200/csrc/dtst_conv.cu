@@ -112,13 +112,14 @@ __device__ __forceinline__ Row<T, V, VEC> load_u(const ConvArgs& a, const Run& r
 template <int K>
 constexpr int kUnroll = K == 3 ? 3 : 4;
 
-// What a thread has asked for, in shared memory of its own: kGroups groups of U steps of TENSORS tensors, copied there asynchronously, so
-// that up to twelve steps are under way without a register for any (fp32: four, of twice the bytes; twelve took 104 us instead of 90
-// forward, 176 instead of 143 backward).  Only the thread itself reads them: no barrier.
+// What a thread has asked for: groups of U steps of TENSORS tensors.  Vectors go to shared memory of the thread's own, copied there
+// asynchronously, so that up to twelve steps are under way without a register for any (fp32: four, of twice the bytes; twelve took 104 us
+// instead of 90 forward, 176 instead of 143 backward).  Only the thread itself reads them: no barrier.
 template <typename T>
 constexpr int kGroups = sizeof(T) == 2 ? 4 : 2;
 template <typename T, int V, bool VEC, int U, int TENSORS>
 struct Ring {
+  static constexpr int AHEAD = kGroups<T> - 1;                 // groups under way
   static constexpr int BYTES = V * (int)sizeof(T), STRIDE = 32 * kWarps * BYTES;
   static constexpr size_t SMEM = (size_t)kGroups<T> * U * TENSORS * STRIDE;
   unsigned char* own;
@@ -127,24 +128,41 @@ struct Ring {
     return own + (((group & (kGroups<T> - 1)) * U + j) * TENSORS + tensor) * STRIDE;
   }
   // p need not exist where `on` is false: nothing is read then, and zeros are put down
-  __device__ __forceinline__ void ask(int group, int j, int tensor, const T* p, const T* valid, bool on, int left) const {
-    unsigned char* to = at(group, j, tensor);
-    if constexpr (VEC) {
-      asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to))), "l"(on ? p : valid), "n"(BYTES),
-                   "r"(on ? BYTES : 0)
-                   : "memory");
-    } else {
-      Pack<T, V> k;
-      if (on) k.load_part(p, left); else k.zero();
-      *reinterpret_cast<Pack<T, V>*>(to) = k;
-    }
+  __device__ __forceinline__ void ask(int group, int j, int tensor, const T* p, const T* valid, bool on, int) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(at(group, j, tensor)))),
+                 "l"(on ? p : valid), "n"(BYTES), "r"(on ? BYTES : 0)
+                 : "memory");
   }
   static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  // until at most N groups are under way
   template <int N>
   static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
   __device__ __forceinline__ Row<T, V, VEC> get(int group, int j, int tensor) const {
     Row<T, V, VEC> r;
     r.raw = *reinterpret_cast<const Pack<T, V>*>(at(group, j, tensor));
+    return r;
+  }
+};
+// Elements one by one are no copies that the hardware makes by itself (2 bytes are too few): the next group stands in registers, one
+// to an element, since what joins two of them waits for both.  [4][4096][4095], width 4: bf16 73 us forward and 136 backward, fp32 100 and
+// 171; put down in shared memory as they arrive: 159 and 554, 179 and 597; two 16-bit elements to a register: 157 and 556.
+template <typename T, int V, int U, int TENSORS>
+struct Ring<T, V, false, U, TENSORS> {
+  static constexpr int AHEAD = 1;
+  static constexpr size_t SMEM = 0;
+  T next[U][TENSORS][V];
+  __device__ __forceinline__ explicit Ring(unsigned char*) {}
+  __device__ __forceinline__ void ask(int, int j, int tensor, const T* p, const T*, bool on, int left) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) next[j][tensor][i] = on && i < left ? p[i] : Elem<T>::put(0.f);
+  }
+  static __device__ __forceinline__ void commit() {}
+  template <int N>
+  static __device__ __forceinline__ void wait() {}
+  __device__ __forceinline__ Row<T, V, false> get(int, int j, int tensor) const {
+    Row<T, V, false> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.raw.v[i] = next[j][tensor][i];
     return r;
   }
 };
@@ -177,7 +195,7 @@ __global__ void __launch_bounds__(32 * kWarps) conv_forward_kernel(const ConvArg
   const int steps = (int)(r.end > r.t0 ? r.end - r.t0 : 0);
   extern __shared__ __align__(16) unsigned char conv_smem[];
   using RingT = Ring<T, V, VEC, U, 1>;
-  const RingT ring(conv_smem);
+  RingT ring(conv_smem);
   const T* const valid = static_cast<const T*>(a.x);
   const auto ask = [&](int g) {
 #pragma unroll
@@ -186,7 +204,7 @@ __global__ void __launch_bounds__(32 * kWarps) conv_forward_kernel(const ConvArg
   };
   if (steps > 0) {
 #pragma unroll
-    for (int g = 0; g < kGroups<T> - 1; ++g) ask(g);
+    for (int g = 0; g < RingT::AHEAD; ++g) ask(g);
   }
   const auto step = [&](int j, const RowT& now) {
     u[j % K] = now.get();
@@ -202,11 +220,11 @@ __global__ void __launch_bounds__(32 * kWarps) conv_forward_kernel(const ConvArg
     y += a.C;
   };
   for (int g = 0; g * U < steps; ++g) {
-    RingT::template wait<kGroups<T> - 2>();
+    RingT::template wait<RingT::AHEAD - 1>();
     RowT now[U];
 #pragma unroll
     for (int j = 0; j < U; ++j) now[j] = ring.get(g, j, 0);
-    ask(g + kGroups<T> - 1);                // (where the group in front of this one was)
+    ask(g + RingT::AHEAD);                // (where the group in front of this one was)
     if ((g + 1) * U <= steps) {
 #pragma unroll
       for (int j = 0; j < U; ++j) step(j, now[j]);
@@ -222,8 +240,9 @@ __global__ void __launch_bounds__(32 * kWarps) conv_forward_kernel(const ConvArg
 
 // Backward.  Step t of the loop forms gp_t; with it the gradient of u_(t) is complete and is written, as that of step
 // t - (K - 1): of x, or of the state in front of a sequence's first run.
+// (128 registers in 16 bits and without vectors: fp32 [4][4096][4095] 194 -> 171 us; fp32 vectors would spill.)
 template <typename T, int V, int K, bool VEC>
-__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 ? 4 : 1) conv_backward_kernel(const ConvArgs a) {
+__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 || !VEC ? 4 : 1) conv_backward_kernel(const ConvArgs a) {
   using RowT = Row<T, V, VEC>;
   constexpr int U = kUnroll<K>;
   __shared__ float2 red[kWarps][32][V / 2];
@@ -235,7 +254,7 @@ __global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 ? 4 : 1) conv_back
   Chans<V> gw[K + 1] = {};             // the last one: the bias'
   extern __shared__ __align__(16) unsigned char conv_smem[];
   using RingT = Ring<T, V, VEC, U, 2>;
-  const RingT ring(conv_smem);
+  RingT ring(conv_smem);
   const T* const valid = static_cast<const T*>(a.x);
   if (on) {
     Chans<V> w[K], bias;
@@ -262,9 +281,9 @@ __global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 ? 4 : 1) conv_back
         RingT::commit();
       };
       RingT::template wait<0>();         // (what the run in front of this one asked for beyond its end)
-      if (asked > 0) {
+      if (asked > 0 || !VEC) {
 #pragma unroll
-        for (int g = 0; g < kGroups<T> - 1; ++g) ask(g);
+        for (int g = 0; g < RingT::AHEAD; ++g) ask(g);
       }
       // step t = (a multiple of U) + j; INSIDE: one of this run's, which completes another one's of this run, without the new state's
       const auto step = [&](int t, int j, const RowT& cx, const RowT& cg, auto inside) {
@@ -314,11 +333,11 @@ __global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 ? 4 : 1) conv_back
       };
       for (int t = 0; t < stop; t += U) {
         const int group = t / U;
-        RingT::template wait<kGroups<T> - 2>();
+        RingT::template wait<RingT::AHEAD - 1>();
         RowT cx[U], cg[U];
 #pragma unroll
         for (int j = 0; j < U; ++j) cx[j] = ring.get(group, j, 0), cg[j] = ring.get(group, j, 1);
-        if (asked > 0) ask(group + kGroups<T> - 1);      // (where the group in front of this one was; without any, what was read counts for nothing)
+        if (asked > 0 || !VEC) ask(group + RingT::AHEAD);      // (where the group in front of this one was; without any, what was read counts for nothing)
         // these complete the steps t - (K - 1) .. t + U - K; the new state begins at live - (K - 1)
         if (t >= K - 1 && t + U <= own && t + U <= live) {
 #pragma unroll

@@ -107,3 +107,24 @@ def test_conv_backward_without_steps_through_the_entry_point():
     status = Bn.lib().dtst_causal_conv_backward(ctypes.byref(d), None, p(gso), None, p(w), p(b), p(s), None, None, p(gw), p(gb), p(gs), p(scratch), n.value,
                                                 ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
     assert status == Bn.DTST_OK and torch.equal(gs, gso) and not gw.any() and not gb.any()
+
+
+@pytest.mark.parametrize("K", [1, 2, 3, 4])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_conv_off_a_vector(K, dtype):
+    """Rows that begin anywhere and an odd distance apart take elements one by one: the bits of the same rows in vectors, over many
+    runs a warp, ends inside and in front of them, and with no steps at all."""
+    from paper_2607_14394_b200 import CausalConv
+    B, T, C = 90, 700, 64
+    ends = [700, 0, 1, 2, 3, 63, 64, 65, 66, 67, 68, 699] + [int(i) for i in np.random.default_rng(K).integers(0, 701, B - 12)]
+    ln = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    x, gy, w, b = rand(B, T, C, dtype=dtype, seed=1), rand(B, T, C, dtype=dtype, seed=2), rand(C, K, seed=3), rand(C, seed=4)
+    s, gl = rand(B, K - 1, C, dtype=dtype, seed=5), rand(B, K - 1, C, dtype=dtype, seed=6)
+    off = torch.empty(B, T, C + 1, dtype=dtype, device="cuda")[..., 1:]
+    off.copy_(x)
+    conv = CausalConv((B, T, C), K, dtype)
+    got = [[*conv.forward(v, w, b, state=s, lengths=ln), *conv.backward(gy, v, w, b, state=s, lengths=ln, grad_state_out=gl)] for v in (x, off)]
+    assert all(torch.equal(p, q) for i, (p, q) in enumerate(zip(*got)) if i not in (3, 4))
+    # (the parameters' gradients: a CTA holds other channels, so it visits other runs)
+    for i in (3, 4):
+        close(got[0][i], host(got[1][i]), i, size=(B * T * C) ** 0.5)

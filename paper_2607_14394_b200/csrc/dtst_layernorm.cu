@@ -493,8 +493,11 @@ __global__ void __launch_bounds__(32 * W) layer_norm_field_kernel(const FieldArg
   }
 }
 
+// Four CTAs an SM where four warps hold the channels (fp32, 20 channels, 7.9e7 elements: 183 -> 164 us); three for eight channels of four
+// positions a thread, which four would spill (fp32 [1][32][2^21], with and without grad_s: 265 and 221 us with four, 180 and 163 without a bound, 171
+// and 142 with three).
 template <typename T, int W, int VEC, int NCH>
-__global__ void __launch_bounds__(32 * W, W == 4 ? 4 : 1) layer_norm_field_backward_kernel(const FieldArgs a) {
+__global__ void __launch_bounds__(32 * W, W == 4 ? (NCH * VEC == 32 ? 3 : 4) : 1) layer_norm_field_backward_kernel(const FieldArgs a) {
   __shared__ float red[2][2][W][32 * VEC];
   pdl_trigger();
   pdl_wait();
@@ -693,8 +696,10 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
     return launch_pdl(layer_norm_wide_field_backward_kernel<T>, grid, dim3(128), 0, st, a);
   }
   // positions in vectors where the rows allow it; two of them a thread where 16 warps share the channels (8 warps with four each left one
-  // CTA on an SM: bf16 [8][64][65536] backward 367 us)
-  const int most_wide = a.C <= 32 ? WIDE : 2;
+  // CTA on an SM: bf16 [8][64][65536] backward 367 us), and backward in 16 bits for 21 to 32 channels, whose low parts and conversions take
+  // registers too (bf16 [1][32][2^21] with and without a residual: 523 and 270 us with four and spills, 231 and 180 with two)
+  constexpr int WIDE8 = BACK && sizeof(T) == 2 ? 2 : WIDE;
+  const int most_wide = a.C <= 20 ? WIDE : a.C <= 32 ? WIDE8 : 2;
   const size_t need = most_wide * sizeof(T);
   bool vec = a.inner % most_wide == 0;
   for (const void* p : {a.x, a.residual, a.gy, a.gs, (const void*)a.s, (const void*)a.low, (const void*)a.y}) vec = vec && aligned_to(p, need);
@@ -721,7 +726,7 @@ cudaError_t launch_field(FieldArgs a, int* parts, cudaStream_t st) {
   }
   DTST_FIELD(4, 2, WIDE)
   DTST_FIELD(4, 5, WIDE)
-  DTST_FIELD(4, 8, WIDE)
+  DTST_FIELD(4, 8, WIDE8)
   DTST_FIELD(16, 4, 2)
   DTST_FIELD(16, 8, 2)
 #undef DTST_FIELD

@@ -128,3 +128,33 @@ def test_conv_off_a_vector(K, dtype):
     # (the parameters' gradients: a CTA holds other channels, so it visits other runs)
     for i in (3, 4):
         close(got[0][i], host(got[1][i]), i, size=(B * T * C) ** 0.5)
+
+
+# ------------------------------------------------------------------------------------------------ layer norm
+@pytest.mark.parametrize("shape", [(2, 21, 514), (1, 24, 3331), (3, 32, 2054), (1, 29, 66), (2, 20, 1000002), (2, 32, 600004)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("residual", [False, True])
+def test_layer_norm_of_fields_of_20_to_32_channels(shape, dtype, residual):
+    """One tile and many a CTA, rows of positions that take vectors of four, of two and none."""
+    from paper_2607_14394_b200 import LayerNorm
+    C = shape[1]
+    x, r = rand(*shape, dtype=dtype, seed=1, shift=0.5), rand(*shape, dtype=dtype, seed=2) if residual else None
+    gy, gs, w, b = rand(*shape, dtype=dtype, seed=3), rand(*shape, dtype=dtype, seed=4) if residual else None, rand(C, seed=5, shift=1.0), rand(C, seed=6)
+    n = LayerNorm(shape, 1, dtype)
+    y, s, stats = n.forward(x, w, b, residual=r)
+    gx, gw, gb = n.backward(gy, s, w, stats, grad_s=gs)
+    d = lambda t: None if t is None else t.double()
+    s64 = d(x) if r is None else d(x) + d(r)                                      # (64 bits on the GPU: elementary operations)
+    mean = s64.mean(1, keepdim=True)
+    rstd = 1 / torch.sqrt(((s64 - mean) ** 2).mean(1, keepdim=True) + 1e-5)
+    n64 = (s64 - mean) * rstd
+    g = d(gy) * d(w)[:, None]
+    want = rstd * (g - g.mean(1, keepdim=True) - n64 * (g * n64).mean(1, keepdim=True))
+    if gs is not None:
+        want = want + d(gs)
+    close(y, host(n64 * d(w)[:, None] + d(b)[:, None]), "y")
+    close(gx, host(want), "grad_x", size=float((g * rstd).norm()))
+    close(gw, host((d(gy) * n64).sum((0, 2))), "grad_weight", size=float((d(gy) * n64).norm()))
+    close(gb, host(d(gy).sum((0, 2))), "grad_bias", size=float(d(gy).norm()))
+    again = n.backward(gy, s, w, stats, grad_s=gs)
+    assert all(torch.equal(p, q) for p, q in zip((gx, gw, gb), again))

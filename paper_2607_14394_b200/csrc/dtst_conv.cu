@@ -197,9 +197,13 @@ __global__ void __launch_bounds__(32 * kWarps) conv_forward_kernel(const ConvArg
   using RingT = Ring<T, V, VEC, U, 1>;
   RingT ring(conv_smem);
   const T* const valid = static_cast<const T*>(a.x);
+  // (a group behind the end is not asked for: bf16 [4096][1][4096] 157 -> 144 us, [20000][3][512] 100 -> 93; the backward pass gains at one step, 177 -> 164,
+  // and loses at three, 155 -> 194)
   const auto ask = [&](int g) {
+    if (!VEC || g * U < steps) {
 #pragma unroll
-    for (int j = 0; j < U; ++j, x += a.xt) ring.ask(g, j, 0, x, valid, g * U + j < steps, left);
+      for (int j = 0; j < U; ++j, x += a.xt) ring.ask(g, j, 0, x, valid, g * U + j < steps, left);
+    }
     RingT::commit();
   };
   if (steps > 0) {

@@ -12,7 +12,7 @@ import pytest
 from oracle import selective_oracle as S
 
 torch = pytest.importorskip("torch")
-from test_gpu_selective import BF16, F16, F32, TYPES, close, host, rand, scan_inputs
+from test_gpu_selective import BF16, F32, TYPES, close, host, rand, run_scan, scan_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -158,3 +158,149 @@ def test_layer_norm_of_fields_of_20_to_32_channels(shape, dtype, residual):
     close(gb, host(d(gy).sum((0, 2))), "grad_bias", size=float(d(gy).norm()))
     again = n.backward(gy, s, w, stats, grad_s=gs)
     assert all(torch.equal(p, q) for p, q in zip((gx, gw, gb), again))
+
+
+# ------------------------------------------------------------------------------------------------ every size of state, far and exact places
+@pytest.mark.parametrize("B,T,C,N,G,lengths", [(2, 9, 40, 17, 1, [9, 4]), (1, 1, 70, 31, 1, None), (1, 130, 20, 24, 2, None), (2, 33, 24, 32, 1, None),
+                                               (2, 500, 12, 20, 1, [500, 131]), (2, 640, 8, 32, 2, [640, 0]), (1, 700, 10, 33, 1, None), (1, 513, 6, 64, 2, None),
+                                               (2, 300, 36, 48, 1, [7, 300])])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gated", [False, True])
+def test_scan_of_17_to_64_states(B, T, C, N, G, lengths, dtype, gated):
+    """Eight and sixteen lanes to a pair of channels, in one segment and in several."""
+    v = scan_inputs(B, T, C, N, G, dtype, gated=gated, strided=gated)
+    if lengths is not None:
+        for i, n in enumerate(lengths):
+            for k in ("x", "dt", "B", "C", "z"):
+                if v[k] is not None:
+                    v[k][i, n:] = float("nan")
+    run_scan(v, N, G, dtype, lengths)
+
+
+def test_far_offsets_backward():
+    """More than 2^31 elements: the first and the last steps of a long sequence by themselves.  Decays are e^-60 and less, so neither
+    a state nor a gradient is seen from twenty steps away."""
+    from paper_2607_14394_b200 import CausalConv, LayerNorm, SelectiveScan
+    T, C, N = (1 << 31) // 1024 + 37, 1024, 4
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, gy = (torch.empty(1, T, C, dtype=BF16, device="cuda").normal_(generator=gen) for _ in range(2))
+    w, b = rand(C, 4, seed=1), rand(C, seed=2)
+    gx = CausalConv((1, T, C), 4, BF16).backward(gy, x, w, b)[0]
+    part = CausalConv((1, 60, C), 4, BF16)
+    assert torch.equal(part.backward(gy[:, -60:].contiguous(), x[:, -60:], w, b, state=x[:, -63:-60])[0], gx[:, -60:])
+    assert torch.equal(part.backward(gy[:, :60], x[:, :60], w, b)[0][:, :50], gx[:, :50])
+    del gx
+    n = LayerNorm((T, C), -1, BF16)
+    _, _, stats = n.forward(x[0], b)
+    gx = n.backward(gy[0], x[0], b, stats)[0]
+    for e in (slice(0, 50), slice(T - 50, T)):
+        assert torch.equal(LayerNorm((50, C), -1, BF16).backward(gy[0, e], x[0, e], b, stats[:, e].contiguous(), need_grad_weight=False)[0], gx[e])
+    del gx, stats
+    I = T * C // 16
+    f, gf = x.view(-1)[:16 * I].view(1, 16, I), gy.view(-1)[:16 * I].view(1, 16, I)
+    n, bf = LayerNorm((1, 16, I), 1, BF16), b[:16].contiguous()
+    y, _, stats = n.forward(f, bf)
+    gx = n.backward(gf, f, bf, stats)[0]
+    at = slice(I - 999, I)
+    small, xs, gs = LayerNorm((1, 16, 999), 1, BF16), f[..., at].contiguous(), gf[..., at].contiguous()
+    ys, _, st = small.forward(xs, bf)
+    assert torch.equal(ys, y[..., at]) and torch.equal(small.backward(gs, xs, bf, st)[0], gx[..., at])
+    del y, gx, stats
+    maps = rand(1, T, 1, 2 * N, dtype=BF16, seed=3)
+    A, bias = torch.full((C, N), -200.0, device="cuda"), torch.full((C,), 4.0, device="cuda")
+
+    def scan(e):
+        xs, g, m = (x, gy, maps) if e is None else (x[:, e].contiguous(), gy[:, e].contiguous(), maps[:, e])
+        s = SelectiveScan((1, xs.shape[1], C), N, 1, BF16)
+        ck = s.new_checkpoints()
+        s.forward(xs, xs, A, m[..., :N], m[..., N:], dt_bias=bias, checkpoints=ck)
+        return s.backward(g, xs, xs, A, m[..., :N], m[..., N:], ck, dt_bias=bias)
+
+    whole, front, back = scan(None), scan(slice(0, 40)), scan(slice(T - 40, T))
+    for k in ("x", "dt", "B", "C"):
+        assert torch.equal(whole[k][:, :20], front[k][:, :20]) and torch.equal(whole[k][:, -20:], back[k][:, -20:]), k
+
+
+class Guard:
+    """The library with scratch of exactly the size that a call states, full of NaNs, between bytes that are looked at afterwards."""
+    CALLS = ("dtst_layer_norm_backward", "dtst_causal_conv_backward", "dtst_selective_scan", "dtst_selective_scan_backward", "dtst_clip_grad_norm")
+
+    def __init__(self, lib):
+        self.lib, self.kept = lib, []
+
+    def __getattr__(self, name):
+        f = getattr(self.lib, name)
+        if name not in self.CALLS:
+            return f
+
+        def call(*args):
+            *rest, scratch, size, stream = args
+            base = torch.full((size + 512,), 0xff, dtype=torch.uint8, device="cuda")
+            base[:256], base[256 + size:] = 77, 77
+            self.kept.append((name, base, size))
+            return f(*rest, base.data_ptr() + 256 if scratch else scratch, size, stream)
+        return call
+
+    def untouched(self):
+        for name, base, size in self.kept:
+            assert (base[:256] == 77).all() and (base[256 + size:] == 77).all(), name
+        return sorted({name for name, _, _ in self.kept})
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scratch_of_the_stated_size_is_enough(dtype):
+    from paper_2607_14394_b200 import CausalConv, GradNorm, LayerNorm, SelectiveScan, binding as Bn
+    guard = Guard(Bn.lib())
+
+    def twice(op, call):
+        want = call(op)
+        op._lib = guard
+        assert all(torch.equal(p, q) for p, q in zip(want, call(op))), type(op)
+
+    for shape, dim in (((700, 33), 1), ((3, 1001), 1), ((2, 16385), 1), ((2, 20, 999), 1), ((1, 37, 4096), 1), ((2, 131, 70), 1), ((9000, 2048), 1), ((1, 5, 400000), 1)):
+        x, g, w = rand(*shape, dtype=dtype, seed=1), rand(*shape, dtype=dtype, seed=2), rand(shape[dim], seed=3)
+        n = LayerNorm(shape, dim, dtype)
+        _, s, st = n.forward(x, w)
+        twice(n, lambda n: n.backward(g, s, w, st))
+    for B, T, C, K in ((3, 700, 33, 4), (1, 1, 1, 1), (50, 300, 130, 3), (2, 5000, 4097, 2)):
+        x, g, w = rand(B, T, C, dtype=dtype, seed=1), rand(B, T, C, dtype=dtype, seed=2), rand(C, K, seed=3)
+        twice(CausalConv((B, T, C), K, dtype), lambda c: c.backward(g, x, w))
+    for B, T, C, N, G in ((2, 900, 33, 5, 1), (1, 1, 1, 1, 1), (3, 40, 129, 17, 1), (1, 3000, 21, 33, 3), (2, 130, 2, 3, 1)):
+        v, g = scan_inputs(B, T, C, N, G, dtype), rand(B, T, C, dtype=dtype, seed=50)
+
+        def call(s):
+            ck = s.new_checkpoints()
+            y, last = s.forward(checkpoints=ck, **v)
+            return [y, last, *s.backward(g, checkpoints=ck, grad_last=last, **v).values()]
+        twice(SelectiveScan((B, T, C), N, G, dtype), call)
+    for count in (1, 16, 17, 128, 129, 300):
+        many = [rand(1 + (977 * i) % 40000, dtype=dtype, seed=i) for i in range(count)]
+        out = [torch.empty_like(t) for t in many]
+        twice(GradNorm(many, out=out), lambda n: [n.clip(1.0), *[t.clone() for t in out], n.norm()])
+    assert guard.untouched() == sorted(Guard.CALLS)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_nothing_around_norms_and_clipped_gradients_is_touched(dtype):
+    from paper_2607_14394_b200 import GradNorm, LayerNorm
+
+    def guarded(*shape, dtype=dtype):
+        size = int(np.prod(shape))
+        base = torch.full((size + 128,), 5.0, dtype=dtype, device="cuda")
+        kept.append(base)
+        return base[64:64 + size].view(shape)
+
+    kept = []
+    for shape, dim in (((5, 37), 1), ((3, 1001), 1), ((2, 16385), 1), ((2, 20, 99), 1), ((1, 30, 66), 1), ((1, 37, 41), 1), ((2, 131, 7), 1)):
+        x, r, g, w = (rand(*shape, dtype=dtype, seed=1), rand(*shape, dtype=dtype, seed=2), rand(*shape, dtype=dtype, seed=3), rand(shape[dim], seed=4))
+        n, C = LayerNorm(shape, dim, dtype), shape[dim]
+        rest = shape[:dim] + shape[dim + 1:]
+        stats = guarded(2, *rest, dtype=F32)
+        if dtype is not F32:
+            stats.sum_low = guarded(*shape)
+        y, s, _ = n.forward(x, w, residual=r, out=guarded(*shape), sum_out=guarded(*shape), stats=stats)
+        n.backward(g, s, w, stats, grad_s=r, grad_x=guarded(*shape), grad_weight=guarded(C, dtype=F32), grad_bias=guarded(C, dtype=F32))
+    grads = [rand(k, dtype=dtype, seed=k) for k in (1, 63, 4095, 4096, 4097, 8193)]
+    GradNorm(grads, out=[guarded(t.numel()) for t in grads]).clip(0.5, norm=guarded(dtype=F32))
+    for base in kept:
+        assert (base[:64] == 5.0).all() and (base[-64:] == 5.0).all()

@@ -654,7 +654,9 @@ dtst_status dtst_causal_conv_backward(const dtst_conv_desc* desc, const void* gr
  * coincide, none takes an input's or another's place; z's only where z is given; zero behind an entry's own length), and of A, D,
  * dt_bias, h0 in float32 (each may be NULL).
  * scratch (16-byte aligned): dtst_selective_scan_scratch_bytes of the pass (backward 0 or 1), asked for on the device that runs it; a
- * forward pass may need none (0).  Calls that may run at the same time need one each.
+ * forward pass may need none (0).  That of a backward pass holds partial sums of the maps' gradients: 2 * states floats (states rounded
+ * up to four) for every token and every 64 channels of a group (32 of more than 16 states, 16 of more than 32).  Calls that may run at
+ * the same time need one each.
  */
 typedef struct {
   int32_t dtype, softplus;

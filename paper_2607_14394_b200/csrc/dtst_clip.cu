@@ -1,7 +1,7 @@
 // The norm of all gradients of a program, and their clipping by it:
 //     norm = sqrt(sum over tensors and elements of v^2),   c = min(1, max_norm / (norm + eps)),   v := c v
-// Two launches over the whole list whatever its length (up to kPerLaunch tensors each): the sums, then the scaling, every CTA of
-// which adds the CTAs' sums up again, in order.  The list of tensors goes with the launch, so nothing is copied to
+// Two launches for every kPerLaunch tensors: all the sums, then the scaling, every CTA of which adds the CTAs' sums up again, in
+// order.  The list of tensors goes with the launch, so nothing is copied to
 // the device and a call can be captured.  Squares are summed in 64 bits: a gradient of 1e30 does not overflow, one of
 // 1e-30 is not lost, and the sum of 10^9 elements keeps its last digits; the conversions and the 64-bit adds run beside the loads.
 // Bound by memory: the gradients are read twice, the second time in the opposite order, so that what the

@@ -11,8 +11,9 @@
 // over the runs a thread visits, over a CTA's warps in shared memory, and over CTAs by a second launch, all in a fixed order: same
 // bits on every run.
 // Measured, [4][4096][4096], width 4, SiLU: bf16 52 us forward and 107 backward (5.1 and 3.8 TB/s), fp32 90 and 142 (6.0 and 5.7).  With
-// the next four steps in registers instead: bf16 65 and 115, fp32 89 and 171; without SiLU the backward pass takes 85: in 16 bits it is bound
-// by its instructions.  Four CTAs an SM (128 registers) brought 115 to 107 in 16 bits; fp32 would spill.
+// the next four steps in registers instead: bf16 65 and 115, fp32 89 and 171; without SiLU the backward pass takes 85.  In 16 bits it is bound
+// by latency: 16 warps an SM, each with chains of a dozen operations a step, issue 2 of 4 instructions a clock, with no unit and not the
+// memory above half of its rate.  Four CTAs an SM (128 registers) brought 115 to 107 in 16 bits; fp32 would spill.
 #include "dtst_common.cuh"
 #include "dtst_memory.cuh"
 #include "dtst_types.cuh"

@@ -6,7 +6,9 @@
 //     e_t = gy'_t C_t + a_(t+1) e_(t+1),   q = e_t a_t h_(t-1),
 //     grad_x = d (e . B) + gy' D,   grad_d = q . A + x (e . B),   grad_dt = grad_d sigmoid(dt + bias),   grad_A = sum q d,
 //     grad_B = sum_c e d x,   grad_C = sum_c gy' h,   grad_z = gy (C . h + D x) d(z sigmoid z)/dz,   grad_h0 = a_0 e_0
-// Everything is in 32 bits.  a_t is ex2.approx of d A log2(e): 2 units in the last place.
+// Everything is in 32 bits.  a_t is ex2.approx (2 units in the last place) of d A log2(e), whose two roundings are |d A| 2^-23 of a_t: off by
+// (2 + |d A|) 2^-23 a_t at most, which is never more than 2^-22 of the state in front.  Joining segments does so once more with the sum of a
+// segment's steps.
 //
 // Layout.  A thread holds four states of two neighbouring channels, P = N / 4 neighbouring lanes a pair of channels, so the sums
 // over states are shuffles among P lanes and every word of a map that is read from shared memory serves two channels.  A CTA
@@ -49,7 +51,7 @@ __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMoreRegisters)); }
 
 // log(1 + e^v), and e = e^-|v|: the larger of v and 0, and log(1 + e) = 2 atanh(e / (2 + e)) as a polynomial in the square of
-// that argument, fitted over its range of 0 to 1/9 to 4e-9 of the value: no digits are lost where e is small
+// that argument, fitted over its range of 0 to 1/9 to 8e-9 of the value: no digits are lost where e is small
 __device__ __forceinline__ float softplus_of(float v, float& e) {
   e = ex2(-fabsf(v) * kLog2e);
   const float s = e * rcp(2.f + e), q = s * s;

@@ -572,6 +572,7 @@ class SelectiveMemory:
         self.D = torch.ones(H, device=dev)
         self.W_out = (rn(D, H) / H ** 0.5).to(dtype)
         self._plans: dict = {}
+        self._zero = torch.zeros((), dtype=dtype, device=dev)
         self.saved = None
 
     def parameters(self) -> dict:
@@ -613,8 +614,8 @@ class SelectiveMemory:
         if lengths is not None and training:
             # the parameters' gradients are sums over all rows, and zero times a NaN is no zero: chosen, not multiplied
             _addr(lengths, "lengths", norm.dev, _I32, conv._lshape)
-            own = (torch.arange(T, device=x.device) < lengths[:, None]).unsqueeze(-1)
-            seen = torch.where(own, x, 0)
+            own = torch.arange(T, device=x.device).view(T, 1) < lengths.view(B, 1, 1)
+            seen = torch.where(own, x, self._zero)
         n, s, stats = norm.forward(x if seen is None else seen, self.norm_weight, self.norm_bias, need_backward=training)
         uz = n @ self.W_in.t()
         after, h = (None, None) if state_out is None else state_out
@@ -646,7 +647,7 @@ class SelectiveMemory:
         norm, conv, scan = self._plan(B, T)
         H, R, S, flat = self.H, self.rank, self.states, lambda t: t.flatten(0, 1)
         g_after, g_last = (None, None) if grad_state is None else grad_state
-        gr = {"W_out": flat(grad_out if own is None else torch.where(own, grad_out, 0)).t() @ flat(y)}
+        gr = {"W_out": flat(grad_out if own is None else torch.where(own, grad_out, self._zero)).t() @ flat(y)}
         gy = grad_out @ self.W_out
         guz, gboth = torch.empty_like(uz), torch.empty_like(both)
         g = scan.backward(gy, u, dt, A, both[..., R:R + S].unsqueeze(2), both[..., R + S:].unsqueeze(2), ck, D=self.D, z=uz[..., H:],

@@ -595,7 +595,8 @@ dtst_status dtst_workspace_status(void* workspace, void* stream);
  *   grad_x = rstd (g - mean_c g - n mean_c(g n)) + grad_s   (also the residual's gradient)
  *   grad_weight[c] = sum of grad_y n,  grad_bias[c] = sum of grad_y, over outer and inner.
  * grad_x may be grad_y or grad_s itself; grad_weight and grad_bias may be NULL.  scratch: dtst_layer_norm_scratch_bytes (1184 rows of
- * `channels` floats, what the layout with the most partial sums takes), needed for either of them (DTST_ERR_WORKSPACE if missing or too small); calls that may run at the same time need one each.
+ * `channels` floats, what the layout with the most partial sums takes), needed for either of them (DTST_ERR_WORKSPACE if missing or
+ * too small); calls that may run at the same time need one each.
  */
 dtst_status dtst_layer_norm(int dtype, int64_t outer, int64_t channels, int64_t inner, float eps, const void* x, const void* residual,
                             const float* weight, const float* bias, void* s, void* s_low, void* y, float* stats, void* stream);
